@@ -397,6 +397,102 @@ GNN_API int gnn_sage_layer_bwd(const void *indptr_t, const int32_t *indices_t, c
 GNN_API int64_t gnn_sage_layer_saved_elems(int64_t N, int64_t F_in, int64_t F_out, int order);
 GNN_API int64_t gnn_sage_layer_workspace_bytes(int64_t N, int64_t F_in, int64_t F_out, int relu, int order);
 
+/* ------------------------------------- between and behind the layers of a training step */
+
+/* Group norm with an activation over vertex features (rows = vertices, channels last).
+ * Samples: sample_ptr [B+1] (int32 or int64, device; sample_ptr[0] = 0, non-decreasing, sample_ptr[B] = N) cuts the rows into B
+ * samples, the graphs of a batch, each normalised by itself; a sample may be empty.  NULL: B samples of N / B rows (N must be
+ * a multiple of B): B = 1 normalises over the whole graph, B = N every vertex by itself.  G groups of K = C / G neighbouring
+ * channels (C must be a multiple of G).  Per sample and group, over the K channels of all its rows:
+ *     mean, var = their mean and (biased) variance,  rstd = 1 / sqrt(var + eps),
+ *     Y[v, c] = act( (X[v, c] - mean) rstd gamma[c] + beta[c] )
+ * X, Y [N, C] fp32 or bf16, not overlapping; gamma, beta [C] fp32 or NULL (1 and 0); mean, rstd [B, G] fp32, written (an empty sample
+ * has mean 0 and rstd 1 / sqrt(eps)).  All sums are fp32 or wider, of distances from a value near the mean. */
+typedef enum gnn_act { GNN_ACT_NONE = 0, GNN_ACT_RELU = 1, GNN_ACT_SILU = 2 /* z / (1 + exp(-z)) */ } gnn_act;
+typedef struct gnn_norm_opts {
+    int32_t dtype;        /* gnn_dtype of X, Y, dY and dX */
+    int32_t act;          /* gnn_act */
+    int32_t ptr_is_64;    /* 0: sample_ptr is int32_t[B+1];  1: int64_t[B+1] */
+    float eps;            /* >= 0; the forward call's only */
+    int64_t ldx, ldy, lddx; /* row strides in elements of X, of Y or dY, and of dX; 0 = C */
+    int64_t max_sample_rows; /* with sample_ptr: no sample has more rows than this; 0 = not known.  A wrong one costs time only */
+    void *stream;
+    void *workspace;      /* device scratch of gnn_group_norm_workspace_bytes(), 16-byte aligned; nothing is kept in it */
+    int64_t workspace_bytes;
+} gnn_norm_opts;
+/* Asynchronous on opts->stream; allocates nothing.  N == 0 or C == 0 is GNN_OK and does nothing.  At most 2^31 - 1 rows and samples and
+ * 2^24 channels. */
+GNN_API int gnn_group_norm_fwd(const void *X, const float *gamma, const float *beta, const void *sample_ptr, void *Y, float *mean,
+                               float *rstd, int64_t N, int64_t C, int64_t G, int64_t B, const gnn_norm_opts *opts);
+/* Gradients of sum dY Y: dX [N, C] (type of X; does not overlap X or dY), dgamma, dbeta [C] fp32; each may be NULL.  X, gamma, beta
+ * and act as in the forward call, mean and rstd as it wrote them; the activation's derivative is taken where it is formed again from them (a
+ * rectifier passes gradient where its argument is > 0).  Sums over vertices are formed in a fixed order: results are
+ * reproducible run to run.  N == 0 sets dgamma and dbeta to 0. */
+GNN_API int gnn_group_norm_bwd(const void *X, const float *gamma, const float *beta, const float *mean, const float *rstd,
+                               const void *dY, const void *sample_ptr, void *dX, float *dgamma, float *dbeta, int64_t N, int64_t C,
+                               int64_t G, int64_t B, const gnn_norm_opts *opts);
+GNN_API int64_t gnn_group_norm_workspace_bytes(int64_t N, int64_t C, int64_t G, int64_t B, int backward);
+
+/* Softmax cross-entropy of the labelled vertices, with the gradient of the class scores X [N, C] (fp32 or bf16) in the same pass.
+ * labels [N] int32 or int64: a label outside 0 .. C-1 (usually -1) means none, whatever the row of X holds: it is not read.
+ *     loss_v = log(sum_j exp X[v, j]) - X[v, labels[v]],   dX[v, j] = w (exp X[v, j] / sum_i exp X[v, i] - [j = labels[v]])
+ *     loss = w * sum of loss_v over the labelled v;   w = scale (SUM) or scale / number of labelled rows (MEAN)
+ * dX [N, C] of X's type, does not overlap X, rows without a label are 0; NULL: the loss only.  loss [1] fp32; loss_rows [N] fp32 (loss_v,
+ * 0 without a label; not weighted) or NULL.  Without labelled rows loss is 0.  A score of -infinity has probability 0; NaN, +infinity
+ * or nothing but -infinity in a labelled row make its results NaN.  Sums are fp32, in a fixed order. */
+typedef enum gnn_loss_reduction { GNN_LOSS_SUM = 0, GNN_LOSS_MEAN = 1 } gnn_loss_reduction;
+typedef struct gnn_loss_opts {
+    int32_t dtype;         /* gnn_dtype of X and dX */
+    int32_t labels_is_64;  /* 0: labels are int32_t;  1: int64_t */
+    int32_t reduction;     /* gnn_loss_reduction */
+    float scale;           /* set it: 1 for the plain loss */
+    int64_t ldx, ldg;      /* row strides in elements of X and dX; 0 = C */
+    void *stream;
+    void *workspace;       /* device scratch of gnn_softmax_xent_workspace_bytes(), 16-byte aligned; nothing is kept in it */
+    int64_t workspace_bytes;
+} gnn_loss_opts;
+/* Asynchronous on opts->stream; allocates nothing.  N == 0 or C == 0 writes loss = 0. */
+GNN_API int gnn_softmax_xent(const void *X, const void *labels, float *loss, void *dX, float *loss_rows, int64_t N, int64_t C,
+                             const gnn_loss_opts *opts);
+GNN_API int64_t gnn_softmax_xent_workspace_bytes(int64_t N, int64_t C);
+
+/* One AdamW step over many tensors at once, in place:
+ *     g = grad * grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *     p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * States (m = exp_avg, v = exp_avg_sq) are fp32, or 8 bits: OCP e4m3 numbers times an fp32 scale for every GNN_ADAMW_BLOCK neighbouring
+ * elements (the last ones may be fewer).  scale = largest finite magnitude of the block / 448; a block below 2^-118 is held as zeros.
+ * All zero is a new state.  m is rounded to the nearest number; v up or down at random such that its mean stays, since with beta2 near 1 a
+ * step is less than half a step of the code, and never from above 0 to 0; both after they have been used.  Of element i of tensor k the 20
+ * random bits are the upper ones of h, all mod 2^32:
+ *     h = (i mod 2^32) 0x9E3779B9 + (i div 2^32) 0x6A09E667 + seed + step 0x3C6EF373 + k 0xBB67AE85;
+ *     h = (h xor h >> 16) 0x6A09E667;  h = (h xor h >> 15) 0xBB67AE85
+ * Gradients that are not finite make their own element's parameter and states NaN (or fp32 what the formulas give), no other's. */
+#define GNN_ADAMW_BLOCK 256
+typedef struct gnn_adamw_tensor {
+    void *param;           /* [n] of dtype, updated */
+    const void *grad;      /* [n] of dtype; NULL: the tensor is left alone, decay included */
+    void *exp_avg;         /* [n] fp32, or e4m3 bytes; updated */
+    void *exp_avg_sq;      /* the same */
+    float *scale;          /* [ceil(n / GNN_ADAMW_BLOCK)] of exp_avg in 8 bits, updated; else not read */
+    float *scale_sq;       /* of exp_avg_sq */
+    float *master;         /* bf16 parameters: [n] fp32, the parameters themselves, of which param becomes the rounded copy; or NULL */
+    int64_t n;
+    int32_t dtype;         /* gnn_dtype of param and grad; a bf16 parameter is rounded to nearest-even once */
+    int32_t state_bits;    /* 8 or 32 */
+    float weight_decay;    /* >= 0 */
+    int32_t reserved;      /* 0 */
+} gnn_adamw_tensor;
+typedef struct gnn_adamw_opts {
+    double lr, beta1, beta2, eps;  /* lr, eps >= 0; betas in [0, 1) */
+    int64_t step;                  /* 1 in the first step; a captured graph repeats the step it was captured with */
+    int64_t seed;                  /* of the random bits (its lower 32 bits) */
+    const float *grad_scale;       /* device: one factor for all gradients (clipping, loss scaling); NULL = 1 */
+    void *stream;
+} gnn_adamw_opts;
+/* `tensors` is a HOST array, read before the call returns.  No buffer may appear twice or overlap another.  Asynchronous on opts->stream;
+ * allocates nothing; one launch for up to 40 tensors. */
+GNN_API int gnn_adamw_step(const gnn_adamw_tensor *tensors /* host */, int64_t n_tensors, const gnn_adamw_opts *opts);
+
 /* ------------------------------------------------------- once-per-graph setup */
 
 /* Row pointers of the destination-indexed CSR (Section 4.1 requires the graph

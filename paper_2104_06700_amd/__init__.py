@@ -17,6 +17,9 @@ from .binding import (  # noqa: F401
     gnn_graph_build, gnn_release_cached_memory,
     gnn_plan_default_params, gnn_plan_create, gnn_calib_copy, gnn_calib_gather,
     gnn_ap_fwd, gnn_ap_bwd_vertex, gnn_ap_bwd_vertex_arg, gnn_ap_bwd_edge, gnn_matmul, gnn_matmul_workspace_bytes,
+    GNN_ACT_NONE, GNN_ACT_RELU, GNN_ACT_SILU, GNN_LOSS_SUM, GNN_LOSS_MEAN, GNN_ADAMW_BLOCK,
+    GnnNormOpts, GnnLossOpts, GnnAdamWTensor, GnnAdamWOpts, AdamWTensors, gnn_group_norm_fwd, gnn_group_norm_bwd, gnn_group_norm_workspace_bytes,
+    gnn_softmax_xent, gnn_softmax_xent_workspace_bytes, gnn_adamw_step,
     gnn_sage_layer_fwd, gnn_sage_layer_bwd, gnn_sage_layer_saved_elems, gnn_sage_layer_workspace_bytes,
 )
 from .graph import DeviceGraph, build_device_graph  # noqa: F401

@@ -35,6 +35,9 @@ GNN_FLAG_NO_SHORT_ROW_OVERLAP = 512
 GNN_FLAG_NO_DENSE_TAIL = 1024
 GNN_BIN_ADD, GNN_BIN_SUB, GNN_BIN_MUL, GNN_BIN_DIV, GNN_BIN_COPY_LHS, GNN_BIN_COPY_RHS = range(6)
 GNN_RED_SUM, GNN_RED_MAX, GNN_RED_MIN = range(3)
+GNN_ACT_NONE, GNN_ACT_RELU, GNN_ACT_SILU = range(3)
+GNN_LOSS_SUM, GNN_LOSS_MEAN = range(2)
+GNN_ADAMW_BLOCK = 256
 
 EXPORTED_SYMBOLS = (
     "gnn_aggregate_fwd", "gnn_aggregate_bwd", "gnn_aggregate_fwd_noalloc", "gnn_packed_bytes", "gnn_pack_rows",
@@ -47,6 +50,8 @@ EXPORTED_SYMBOLS = (
     "gnn_ap_fwd", "gnn_ap_bwd_vertex", "gnn_ap_bwd_vertex_arg", "gnn_ap_bwd_vertex_arg_edges", "gnn_ap_bwd_edge",
     "gnn_matmul", "gnn_matmul_workspace_bytes",
     "gnn_sage_layer_fwd", "gnn_sage_layer_bwd", "gnn_sage_layer_saved_elems", "gnn_sage_layer_workspace_bytes",
+    "gnn_group_norm_fwd", "gnn_group_norm_bwd", "gnn_group_norm_workspace_bytes", "gnn_softmax_xent", "gnn_softmax_xent_workspace_bytes",
+    "gnn_adamw_step",
     "gnn_status_string", "gnn_calib_copy", "gnn_calib_gather",
 )
 
@@ -75,6 +80,37 @@ class GnnLayerOpts(ctypes.Structure):
         ("indptr_is_64", ctypes.c_int32), ("relu", ctypes.c_int32), ("order", ctypes.c_int32), ("flags", ctypes.c_int32),
         ("stream", ctypes.c_void_p), ("plan", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
         ("workspace_bytes", ctypes.c_int64),
+    ]
+
+
+class GnnNormOpts(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("ptr_is_64", ctypes.c_int32), ("eps", ctypes.c_float),
+        ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64), ("lddx", ctypes.c_int64), ("max_sample_rows", ctypes.c_int64),
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64),
+    ]
+
+
+class GnnLossOpts(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("labels_is_64", ctypes.c_int32), ("reduction", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("ldx", ctypes.c_int64), ("ldg", ctypes.c_int64),
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64),
+    ]
+
+
+class GnnAdamWTensor(ctypes.Structure):
+    _fields_ = [
+        ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p),
+        ("scale", ctypes.c_void_p), ("scale_sq", ctypes.c_void_p), ("master", ctypes.c_void_p), ("n", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("weight_decay", ctypes.c_float), ("reserved", ctypes.c_int32),
+    ]
+
+
+class GnnAdamWOpts(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+        ("step", ctypes.c_int64), ("seed", ctypes.c_int64), ("grad_scale", ctypes.c_void_p), ("stream", ctypes.c_void_p),
     ]
 
 
@@ -161,6 +197,14 @@ def load_library() -> ctypes.CDLL:
         lib.gnn_sage_layer_saved_elems.restype = i64
         lib.gnn_sage_layer_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
         lib.gnn_sage_layer_workspace_bytes.restype = i64
+        lib.gnn_group_norm_fwd.argtypes = [vp] * 7 + [i64] * 4 + [ctypes.POINTER(GnnNormOpts)]
+        lib.gnn_group_norm_bwd.argtypes = [vp] * 10 + [i64] * 4 + [ctypes.POINTER(GnnNormOpts)]
+        lib.gnn_group_norm_workspace_bytes.argtypes = [i64, i64, i64, i64, i32]
+        lib.gnn_group_norm_workspace_bytes.restype = i64
+        lib.gnn_softmax_xent.argtypes = [vp] * 5 + [i64] * 2 + [ctypes.POINTER(GnnLossOpts)]
+        lib.gnn_softmax_xent_workspace_bytes.argtypes = [i64, i64]
+        lib.gnn_softmax_xent_workspace_bytes.restype = i64
+        lib.gnn_adamw_step.argtypes = [vp, i64, ctypes.POINTER(GnnAdamWOpts)]
         lib.gnn_status_string.argtypes = [i32]
         lib.gnn_status_string.restype = ctypes.c_char_p
         lib.gnn_calib_copy.argtypes = [vp, vp, i64, vp]
@@ -177,7 +221,8 @@ def _connect_calls():
     except ImportError as err:
         raise ImportError("the extension module _pycall is missing: run `python -c 'import __graft_entry__ as g; g.build()'`") from err
     names = ("gnn_aggregate_fwd", "gnn_aggregate_bwd", "gnn_ap_fwd", "gnn_ap_bwd_vertex", "gnn_ap_bwd_vertex_arg_edges",
-             "gnn_ap_bwd_edge", "gnn_sage_layer_fwd", "gnn_sage_layer_bwd")
+             "gnn_ap_bwd_edge", "gnn_sage_layer_fwd", "gnn_sage_layer_bwd", "gnn_group_norm_fwd", "gnn_group_norm_bwd",
+             "gnn_softmax_xent", "gnn_adamw_step")
     _pycall.connect({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names}, torch)
     _calls = _pycall
     return _pycall
@@ -512,6 +557,88 @@ def gnn_sage_layer_bwd(indptr_t, indices_t, X, W, saved, H, dH, dX, dW, db, plan
                        stream=None, flags=0) -> None:
     """Gradients of one layer over the transposed graph (see include/gnnagg.h)."""
     _hot("gnn_sage_layer_bwd", "sage_layer_bwd", indptr_t, indices_t, X, W, saved, H, dH, dX, dW, db, plan, workspace, relu, order, stream, flags)
+
+
+def gnn_group_norm_workspace_bytes(N, C, groups, n_samples=1, backward=False) -> int:
+    return int(load_library().gnn_group_norm_workspace_bytes(int(N), int(C), int(groups), int(n_samples), 1 if backward else 0))
+
+
+def gnn_group_norm_fwd(X, gamma, beta, Y, mean, rstd, groups, sample_ptr=None, n_samples=1, act=GNN_ACT_NONE, eps=1e-5, workspace=None,
+                       max_sample_rows=0, stream=None) -> None:
+    """Y = act(group norm of X), channels last, with mean and rstd [samples, groups] (see include/gnnagg.h).  sample_ptr
+    [samples + 1] cuts the rows into samples of any size; without it there are n_samples of equal size."""
+    _hot("gnn_group_norm_fwd", "group_norm_fwd", X, gamma, beta, Y, mean, rstd, groups, eps, sample_ptr, n_samples, max_sample_rows, act, workspace,
+         stream)
+
+
+def gnn_group_norm_bwd(X, gamma, beta, mean, rstd, dY, dX, dgamma, dbeta, groups, sample_ptr=None, n_samples=1, act=GNN_ACT_NONE, workspace=None,
+                       max_sample_rows=0, stream=None) -> None:
+    """Gradients of gnn_group_norm_fwd; dX, dgamma and dbeta may be None (see include/gnnagg.h)."""
+    _hot("gnn_group_norm_bwd", "group_norm_bwd", X, gamma, beta, mean, rstd, dY, dX, dgamma, dbeta, groups, sample_ptr, n_samples, max_sample_rows,
+         act, workspace, stream)
+
+
+def gnn_softmax_xent_workspace_bytes(N, C) -> int:
+    return int(load_library().gnn_softmax_xent_workspace_bytes(int(N), int(C)))
+
+
+def gnn_softmax_xent(X, labels, loss, dX=None, loss_rows=None, reduction=GNN_LOSS_MEAN, scale=1.0, workspace=None, stream=None) -> None:
+    """Softmax cross-entropy of the labelled rows of X [N, C] into loss [1], and its gradient dX (see include/gnnagg.h).
+    A label outside 0 .. C-1 means none."""
+    _hot("gnn_softmax_xent", "softmax_xent", X, labels, loss, dX, loss_rows, reduction, scale, workspace, stream)
+
+
+class AdamWTensors:
+    """The tensors of a model as gnn_adamw_step takes them: the descriptors, made once, and the tensors that they point to.
+
+    params, grads, exp_avg, exp_avg_sq: lists of contiguous device tensors of the same sizes; a gradient may be None (the
+    tensor is left alone).  Parameters and gradients are float32 or bfloat16.  The states are float32, or 8 bits (torch.float8_e4m3fn or uint8) with
+    float32 scales [ceil(n / GNN_ADAMW_BLOCK)] in `scale` and `scale_sq` (None for float32 states).  master: float32 copies of
+    bfloat16 parameters, or None.  weight_decay: one number, or one for each tensor."""
+
+    def __init__(self, params, grads, exp_avg, exp_avg_sq, scale=None, scale_sq=None, master=None, weight_decay=0.0):
+        count = len(params)
+        lists = [list(t) if t is not None else [None] * count for t in (params, grads, exp_avg, exp_avg_sq, scale, scale_sq, master)]
+        decay = [float(weight_decay)] * count if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        if any(len(t) != count for t in lists) or len(decay) != count:
+            raise ValueError("one entry a tensor expected in every list")
+        self._tensors = lists  # what the descriptors point to stays alive
+        self.count = count
+        self._array = (GnnAdamWTensor * max(count, 1))()
+        eight = (torch.float8_e4m3fn, torch.uint8)
+        for d, w, (p, g, m, v, ms, vs, master_p) in zip(self._array, decay, zip(*lists)):
+            for t in (p, g, m, v, ms, vs, master_p):
+                if t is not None and not (t.is_contiguous() and t.is_cuda):
+                    raise ValueError("contiguous device tensors expected")
+            n = p.numel()
+            if m.dtype != v.dtype or m.dtype not in (torch.float32,) + eight:
+                raise TypeError("states must both be float32, or both float8_e4m3fn or uint8")
+            bits = 32 if m.dtype == torch.float32 else 8
+            blocks = -(-n // GNN_ADAMW_BLOCK)
+            if g is not None and g.dtype != p.dtype:
+                raise TypeError("a gradient must have its parameter's dtype")
+            if bits == 8 and (ms is None or vs is None):
+                raise ValueError("8-bit states need their scales")
+            for t, want, dtype in ((g, n, None), (m, n, None), (v, n, None), (ms, blocks, torch.float32), (vs, blocks, torch.float32),
+                                   (master_p, n, torch.float32)):
+                if t is not None and t.numel() != want:
+                    raise ValueError(f"{want} values expected, {t.numel()} given")
+                if t is not None and dtype is not None and t.dtype != dtype:
+                    raise TypeError("scales and master copies are float32")
+            if master_p is not None and p.dtype != torch.bfloat16:
+                raise TypeError("a master copy belongs to bfloat16 parameters")
+            d.param, d.exp_avg, d.exp_avg_sq = p.data_ptr(), m.data_ptr(), v.data_ptr()
+            d.grad = g.data_ptr() if g is not None else None
+            d.scale, d.scale_sq = (ms.data_ptr(), vs.data_ptr()) if bits == 8 else (None, None)
+            d.master = master_p.data_ptr() if master_p is not None else None
+            d.n, d.dtype, d.state_bits, d.weight_decay = n, _dtype_code(p), bits, w
+        self.address = ctypes.addressof(self._array)
+
+
+def gnn_adamw_step(tensors: AdamWTensors, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, seed=0, stream=None) -> None:
+    """One AdamW step over all tensors, in place; `step` is 1 in the first one (see include/gnnagg.h).  grad_scale: a float32
+    device tensor of one value that multiplies every gradient."""
+    _hot("gnn_adamw_step", "adamw_step", tensors.address, tensors.count, step, lr, beta1, beta2, eps, grad_scale, seed, stream)
 
 
 def gnn_csr_from_sorted_coo(dst_sorted: torch.Tensor, N: int, indptr_out: torch.Tensor, stream=None) -> None:

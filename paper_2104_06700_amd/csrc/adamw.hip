@@ -1,0 +1,256 @@
+// One AdamW step over many tensors.
+//
+// Per element, with gradient g (times *grad_scale), step number t, decoupled weight decay wd:
+//     m = b1 m + (1 - b1) g,   v = b2 v + (1 - b2) g^2,
+//     p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps).
+//
+// States are fp32, or 8 bits: e4m3 numbers (4 exponent bits, 3 mantissa bits, largest number 448) times an fp32 scale for every
+// 256 neighbouring elements, scale = largest finite magnitude of the 256 / 448.  The step computes with the fp32 values of m and v; rounding
+// to 8 bits is what the next step reads.  m is rounded to the nearest number (half a step is at most 1/16 of the value, less than a step of
+// b1 = 0.9 takes off).  v is rounded up or down at random, with the probability that keeps its mean: with b2 = 0.999 one step moves
+// v by far less than half a step of the code, so that to the nearest it would stand still beside the largest of its 256 (3000 steps over
+// values of a wide spread with rare large gradients: sqrt(v) off by 0.39 rms and 17 % on average to the nearest, by 0.11 and 1 % at
+// random).  The random bits are a hash of seed, step, tensor and element.  v > 0 is never held as 0, which would divide m by eps.
+//
+// The tensors' descriptors are kernel arguments: no copy of them, no allocation, at most kTensors per launch.  A workgroup has
+// kChunk neighbouring elements of one tensor, a wavefront 256 at a time, the elements of a scale.
+#include "common.h"
+#include "rows.h"
+
+#include <math.h>
+
+#pragma clang fp contract(off)  // the states' rounding to 8 bits is defined on products and sums that are rounded one by one
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBlock = 256;      // elements of a scale: four a lane
+constexpr int kChunk = 4096;     // elements of a workgroup
+constexpr int kTensors = 40;     // of a launch; 4 KB of arguments at most
+constexpr float kTop = 448.0f;
+constexpr float kTiny = 0x1p-118f;  // below it 448 / x would overflow: such a block is held as zeros
+
+struct Tensor {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale, *master;
+    int64_t n;
+    uint32_t salt;    // of the random bits
+    float decay;      // 1 - lr wd
+    int32_t first;    // workgroup that begins it
+    int32_t flags;    // 1: bf16, 2: 8-bit states
+};
+struct Step {
+    Tensor t[kTensors];
+    int32_t count;
+    float b1, c1, b2, c2, rate, root, eps;  // c = 1 - b, rate = lr / (1 - b1^t), root = 1 / sqrt(1 - b2^t)
+    const float *grad_scale;
+};
+static_assert(sizeof(Step) <= 4096, "kernel arguments");
+
+__device__ __forceinline__ uint32_t random_bits(uint64_t element, uint32_t salt) {  // 20 of them
+    uint32_t h = uint32_t(element) * 0x9E3779B9u + uint32_t(element >> 32) * 0x6A09E667u + salt;
+    h = (h ^ (h >> 16)) * 0x6A09E667u;
+    h = (h ^ (h >> 15)) * 0xBB67AE85u;
+    return h >> 12;
+}
+
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
+
+// four numbers to the nearest; not finite ones become NaN
+__device__ __forceinline__ uint32_t code_nearest(const float (&x)[4], float factor) {
+    int w = 0;
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * factor, x[1] * factor, w, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * factor, x[3] * factor, w, true);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (!finite(x[j])) w |= 0x7F << (8 * j);
+    return uint32_t(w);
+}
+
+// four numbers x >= 0, up or down by their random bits.  From 2^-6 on, the 20 bits are added to the 20 of the mantissa that go;
+// below, numbers are multiples of 2^-9.
+__device__ __forceinline__ uint32_t code_random(const float (&v)[4], float factor, uint64_t element, uint32_t salt) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float x = v[j] * factor;
+        x = x < kTop ? x : kTop;
+        const uint32_t bits = random_bits(element + j, salt);
+        uint32_t c = x >= 0x1p-6f ? ((__float_as_uint(x) + bits) >> 20) - (120u << 3) : uint32_t(x * 512.0f + float(bits) * 0x1p-20f);
+        if (v[j] > 0.0f && factor > 0.0f && c == 0) c = 1;
+        if (!finite(v[j])) c = 0x7F;
+        w |= c << (8 * j);
+    }
+    return w;
+}
+
+template <typename T, bool EIGHT, bool WHOLE>
+__device__ __forceinline__ void update(const Step &s, const Tensor &t, int64_t i, float gs) {
+    // elements i .. i + 3 of the tensor, or as many of them as there are
+    const int64_t left = t.n - i;
+    const int have = WHOLE ? 4 : left < 0 ? 0 : left < 4 ? int(left) : 4;
+    const T *param = static_cast<const T *>(t.param);
+    const T *grad = static_cast<const T *>(t.grad);
+    float p[4], g[4], m[4], v[4];
+    uint32_t mc = 0, vc = 0;
+    const uint8_t *m8 = static_cast<const uint8_t *>(t.m), *v8 = static_cast<const uint8_t *>(t.v);
+    const float *m32 = static_cast<const float *>(t.m), *v32 = static_cast<const float *>(t.v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        p[j] = g[j] = m[j] = v[j] = 0.0f;
+        if (j >= have) continue;
+        p[j] = t.master ? t.master[i + j] : gnn_rows<T>::get(param + i + j);
+        g[j] = gnn_rows<T>::get(grad + i + j);
+        if constexpr (EIGHT) {
+            mc |= uint32_t(m8[i + j]) << (8 * j);
+            vc |= uint32_t(v8[i + j]) << (8 * j);
+        } else {
+            m[j] = m32[i + j];
+            v[j] = v32[i + j];
+        }
+    }
+    if constexpr (EIGHT) {
+        const int64_t block = i / kBlock;
+        const float ms = have ? t.m_scale[block] : 0.0f, vs = have ? t.v_scale[block] : 0.0f;
+        m[0] = __builtin_amdgcn_cvt_f32_fp8(int(mc), 0) * ms;
+        m[1] = __builtin_amdgcn_cvt_f32_fp8(int(mc), 1) * ms;
+        m[2] = __builtin_amdgcn_cvt_f32_fp8(int(mc), 2) * ms;
+        m[3] = __builtin_amdgcn_cvt_f32_fp8(int(mc), 3) * ms;
+        v[0] = __builtin_amdgcn_cvt_f32_fp8(int(vc), 0) * vs;
+        v[1] = __builtin_amdgcn_cvt_f32_fp8(int(vc), 1) * vs;
+        v[2] = __builtin_amdgcn_cvt_f32_fp8(int(vc), 2) * vs;
+        v[3] = __builtin_amdgcn_cvt_f32_fp8(int(vc), 3) * vs;
+    }
+    float m_top = 0.0f, v_top = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float gj = g[j] * gs;
+        m[j] = m[j] * s.b1 + gj * s.c1;
+        v[j] = v[j] * s.b2 + (gj * gj) * s.c2;
+        p[j] = p[j] * t.decay - s.rate * (m[j] / (sqrtf(v[j]) * s.root + s.eps));
+        if (finite(m[j])) m_top = fmaxf(m_top, fabsf(m[j]));
+        if (finite(v[j])) v_top = fmaxf(v_top, v[j]);
+    }
+    if constexpr (EIGHT) {
+        m_top = wave_max(m_top);
+        v_top = wave_max(v_top);
+        const float mf = m_top >= kTiny ? kTop / m_top : 0.0f, vf = v_top >= kTiny ? kTop / v_top : 0.0f;
+        mc = code_nearest(m, mf);
+        vc = code_random(v, vf, uint64_t(i), t.salt);
+        if ((threadIdx.x & 63) == 0 && have) {
+            t.m_scale[i / kBlock] = m_top >= kTiny ? m_top / kTop : 0.0f;
+            t.v_scale[i / kBlock] = v_top >= kTiny ? v_top / kTop : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (j >= have) continue;
+        gnn_rows<T>::set(static_cast<T *>(t.param) + i + j, p[j]);
+        if (t.master) t.master[i + j] = p[j];
+        if constexpr (EIGHT) {
+            static_cast<uint8_t *>(t.m)[i + j] = uint8_t(mc >> (8 * j));
+            static_cast<uint8_t *>(t.v)[i + j] = uint8_t(vc >> (8 * j));
+        } else {
+            static_cast<float *>(t.m)[i + j] = m[j];
+            static_cast<float *>(t.v)[i + j] = v[j];
+        }
+    }
+}
+
+template <typename T, bool EIGHT> __device__ __forceinline__ void update_chunk(const Step &s, const Tensor &t, int64_t begin, float gs) {
+    for (int k = 0; k < kChunk; k += kThreads * 4) {
+        const int64_t i = begin + k + int64_t(threadIdx.x) * 4;
+        update<T, EIGHT, false>(s, t, i, gs);
+    }
+}
+
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const Step s) {
+    int k = 0;
+    while (k + 1 < s.count && int(blockIdx.x) >= s.t[k + 1].first) ++k;
+    const Tensor &t = s.t[k];
+    const int64_t begin = int64_t(int(blockIdx.x) - t.first) * kChunk;
+    const float gs = s.grad_scale ? *s.grad_scale : 1.0f;
+    if (t.flags == 0) update_chunk<float, false>(s, t, begin, gs);
+    else if (t.flags == 1) update_chunk<gnn_bf16, false>(s, t, begin, gs);
+    else if (t.flags == 2) update_chunk<float, true>(s, t, begin, gs);
+    else update_chunk<gnn_bf16, true>(s, t, begin, gs);
+}
+
+bool misaligned(const void *p, int64_t to) { return reinterpret_cast<uintptr_t>(p) % uintptr_t(to) != 0; }
+
+int check_tensor(const gnn_adamw_tensor &t) {
+    if (t.n < 0 || (t.dtype != GNN_F32 && t.dtype != GNN_BF16) || (t.state_bits != 8 && t.state_bits != 32)) return GNN_ERR_INVALID_ARG;
+    if (!(t.weight_decay >= 0.0f)) return GNN_ERR_INVALID_ARG;
+    if (t.n == 0 || !t.grad) return GNN_OK;
+    if (!t.param || !t.exp_avg || !t.exp_avg_sq) return GNN_ERR_INVALID_ARG;
+    if (t.state_bits == 8 && (!t.scale || !t.scale_sq)) return GNN_ERR_INVALID_ARG;
+    if (t.master && t.dtype == GNN_F32) return GNN_ERR_INVALID_ARG;
+    const int size = t.dtype == GNN_F32 ? 4 : 2, state = t.state_bits == 8 ? 1 : 4;
+    if (misaligned(t.param, size) || misaligned(t.grad, size) || misaligned(t.exp_avg, state) || misaligned(t.exp_avg_sq, state) ||
+        misaligned(t.scale, 4) || misaligned(t.scale_sq, 4) || misaligned(t.master, 4))
+        return GNN_ERR_INVALID_ARG;
+    return GNN_OK;
+}
+
+}  // namespace
+
+extern "C" GNN_API int gnn_adamw_step(const gnn_adamw_tensor *tensors, int64_t n_tensors, const gnn_adamw_opts *opts) {
+    if (!opts || n_tensors < 0 || (n_tensors > 0 && !tensors)) return GNN_ERR_INVALID_ARG;
+    const gnn_adamw_opts &o = *opts;
+    if (o.step < 1 || !(o.lr >= 0.0) || !(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0) || !(o.eps >= 0.0)) return GNN_ERR_INVALID_ARG;
+    int64_t blocks = 0;
+    for (int64_t k = 0; k < n_tensors; ++k) {
+        const int rc = check_tensor(tensors[k]);
+        if (rc != GNN_OK) return rc;
+        if (tensors[k].grad && (tensors[k].n + kChunk - 1) / kChunk > INT32_MAX / 2) return GNN_ERR_INVALID_ARG;
+    }
+    (void)hipGetLastError();
+    Step s{};
+    s.b1 = float(o.beta1);
+    s.c1 = float(1.0 - o.beta1);
+    s.b2 = float(o.beta2);
+    s.c2 = float(1.0 - o.beta2);
+    s.rate = float(o.lr / (1.0 - pow(o.beta1, double(o.step))));
+    s.root = float(1.0 / sqrt(1.0 - pow(o.beta2, double(o.step))));
+    s.eps = float(o.eps);
+    s.grad_scale = o.grad_scale;
+    auto flush = [&]() -> int {
+        if (s.count == 0) return GNN_OK;
+        adamw_kernel<<<unsigned(blocks), kThreads, 0, static_cast<hipStream_t>(o.stream)>>>(s);
+        s.count = 0;
+        blocks = 0;
+        GNN_HIP_TRY(hipGetLastError());
+        return GNN_OK;
+    };
+    for (int64_t k = 0; k < n_tensors; ++k) {
+        const gnn_adamw_tensor &d = tensors[k];
+        if (d.n == 0 || !d.grad) continue;
+        const int64_t more = (d.n + kChunk - 1) / kChunk;
+        if (s.count == kTensors || blocks + more > INT32_MAX / 2) {
+            const int rc = flush();
+            if (rc != GNN_OK) return rc;
+        }
+        Tensor &t = s.t[s.count++];
+        t.param = d.param;
+        t.grad = d.grad;
+        t.m = d.exp_avg;
+        t.v = d.exp_avg_sq;
+        t.m_scale = d.scale;
+        t.v_scale = d.scale_sq;
+        t.master = d.master;
+        t.n = d.n;
+        t.salt = uint32_t(o.seed) + uint32_t(o.step) * 0x3C6EF373u + uint32_t(k) * 0xBB67AE85u;
+        t.decay = float(1.0 - o.lr * double(d.weight_decay));
+        t.first = int32_t(blocks);
+        t.flags = (d.dtype == GNN_BF16 ? 1 : 0) | (d.state_bits == 8 ? 2 : 0);
+        blocks += more;
+    }
+    return flush();
+}

@@ -13,7 +13,7 @@
 #include "gnnagg.h"
 
 static PyObject *dtype_f32, *dtype_bf16, *dtype_i32, *dtype_i64, *get_device, *get_raw_stream, *stream_type;
-static PyObject *s_data_ptr, *s_stride, *s_dtype, *s_handle, *s_cuda_stream, *s_is_contiguous, *s_nbytes, *s_shape;
+static PyObject *s_data_ptr, *s_stride, *s_dtype, *s_handle, *s_cuda_stream, *s_is_contiguous, *s_nbytes, *s_shape, *s_is_cuda;
 
 static __typeof__(&gnn_aggregate_fwd) fn_aggregate_fwd;
 static __typeof__(&gnn_aggregate_bwd) fn_aggregate_bwd;
@@ -23,6 +23,10 @@ static __typeof__(&gnn_ap_bwd_vertex_arg_edges) fn_ap_bwd_vertex_arg;
 static __typeof__(&gnn_ap_bwd_edge) fn_ap_bwd_edge;
 static __typeof__(&gnn_sage_layer_fwd) fn_sage_layer_fwd;
 static __typeof__(&gnn_sage_layer_bwd) fn_sage_layer_bwd;
+static __typeof__(&gnn_group_norm_fwd) fn_group_norm_fwd;
+static __typeof__(&gnn_group_norm_bwd) fn_group_norm_bwd;
+static __typeof__(&gnn_softmax_xent) fn_softmax_xent;
+static __typeof__(&gnn_adamw_step) fn_adamw_step;
 
 /* ---- scalars: 0 on success, -1 with an exception set */
 
@@ -413,6 +417,202 @@ static PyObject *sage_layer_bwd(PyObject *self, PyObject *const *a, Py_ssize_t n
     return PyLong_FromLong(status);
 }
 
+/* ---- norm, loss and optimizer: shapes are checked, since the kernels take them from the first argument */
+
+static int on_device(PyObject *t) {
+    PyObject *d = PyObject_GetAttr(t, s_is_cuda);
+    if (!d) return -1;
+    const int yes = d == Py_True;
+    Py_DECREF(d);
+    if (!yes) PyErr_SetString(PyExc_ValueError, "device tensors expected");
+    return yes ? 0 : -1;
+}
+
+/* A matrix [N, C] of features, fp32 or bf16, with unit column stride.  shape[0] < 0: takes N, C and the type from it, else they have
+ * to be those.  None only where `optional`: a null pointer. */
+static int feature_matrix(PyObject *t, int optional, int64_t shape[2], int32_t *dtype, void **out, int64_t *ld) {
+    *out = NULL;
+    *ld = 0;
+    if (t == Py_None && optional) return 0;
+    PyObject *d = dtype_of(t);
+    if (!d) return -1;
+    const int code = d == dtype_f32 ? GNN_F32 : d == dtype_bf16 ? GNN_BF16 : -1;
+    Py_DECREF(d);
+    if (code < 0) { PyErr_SetString(PyExc_TypeError, "features must be float32 or bfloat16"); return -1; }
+    int dims;
+    int64_t stride[2], size[2];
+    if (on_device(t) || strides_of(t, &dims, stride) || size_of(t, size)) return -1;
+    if (dims != 2) { PyErr_SetString(PyExc_ValueError, "features are two-dimensional"); return -1; }
+    if (shape[0] < 0) {
+        shape[0] = size[0];
+        shape[1] = size[1];
+        *dtype = code;
+    } else if (size[0] != shape[0] || size[1] != shape[1]) {
+        PyErr_SetString(PyExc_ValueError, "feature matrices must have the same shape");
+        return -1;
+    } else if (code != *dtype) {
+        PyErr_SetString(PyExc_TypeError, "feature matrices must have the same dtype");
+        return -1;
+    }
+    if (size[1] > 1 && size[0] > 0 && stride[1] != 1) {
+        PyErr_SetString(PyExc_ValueError, "feature matrices must have unit column stride");
+        return -1;
+    }
+    if (size[0] > 1) {
+        if (stride[0] < size[1]) { PyErr_SetString(PyExc_ValueError, "rows of a feature matrix must not overlap"); return -1; }
+        *ld = stride[0];
+    }
+    return data_ptr(t, out);
+}
+
+/* n values of four bytes each, dense and fp32, or None where `optional` */
+static int floats(PyObject *t, int optional, int64_t n, void **out) {
+    *out = NULL;
+    if (t == Py_None && optional) return 0;
+    if (is_f32(t, "parameters, statistics and losses are float32")) return -1;
+    const int dense = is_contiguous(t);
+    if (dense < 0) return -1;
+    if (!dense) { PyErr_SetString(PyExc_ValueError, "contiguous tensor expected"); return -1; }
+    void *p;
+    int64_t bytes;
+    if (on_device(t) || workspace_of(t, &p, &bytes)) return -1;
+    if (bytes != 4 * n) { PyErr_Format(PyExc_ValueError, "%lld values expected, %lld given", (long long)n, (long long)(bytes / 4)); return -1; }
+    *out = p;
+    return 0;
+}
+
+/* A dense vector of int32 or int64; its length into *n */
+static int integers(PyObject *t, void **out, int32_t *is_64, int64_t *n) {
+    PyObject *d = dtype_of(t);
+    if (!d) return -1;
+    const int ok = d == dtype_i64 || d == dtype_i32;
+    *is_64 = d == dtype_i64;
+    Py_DECREF(d);
+    if (!ok) { PyErr_SetString(PyExc_TypeError, "int32 or int64 expected"); return -1; }
+    const int dense = is_contiguous(t);
+    if (dense < 0) return -1;
+    int dims;
+    int64_t stride[2], size[2];
+    if (strides_of(t, &dims, stride) || size_of(t, size)) return -1;
+    if (!dense || dims != 1) { PyErr_SetString(PyExc_ValueError, "contiguous vector expected"); return -1; }
+    *n = size[0];
+    return on_device(t) || data_ptr(t, out) ? -1 : 0;
+}
+
+static int to_double(PyObject *o, double *out) {
+    *out = PyFloat_AsDouble(o);
+    return *out == -1.0 && PyErr_Occurred() ? -1 : 0;
+}
+
+static int scratch_of(PyObject *t, void **out, int64_t *bytes) {
+    *out = NULL;
+    *bytes = 0;
+    return t == Py_None ? 0 : on_device(t) || workspace_of(t, out, bytes) ? -1 : 0;
+}
+
+/* samples of a norm: sample_ptr or their number, the hint on their size; then act, workspace and stream */
+static int norm_options(PyObject *const *a, gnn_norm_opts *o, void **ptr, int64_t *samples) {
+    *ptr = NULL;
+    if (to_i64(a[1], samples)) return -1;
+    if (a[0] != Py_None) {
+        if (integers(a[0], ptr, &o->ptr_is_64, samples)) return -1;
+        if (*samples < 1) { PyErr_SetString(PyExc_ValueError, "sample_ptr has one entry more than there are samples"); return -1; }
+        --*samples;
+    }
+    return to_i64(a[2], &o->max_sample_rows) || to_int(a[3], &o->act) || scratch_of(a[4], &o->workspace, &o->workspace_bytes) ||
+           stream_ptr(a[5], &o->stream) ? -1 : 0;
+}
+
+/* number of statistics, or -1 with an exception set */
+static int64_t pairs_of(int64_t samples, int64_t groups) {
+    if (samples >= 0 && samples <= INT32_MAX && groups >= 0 && groups <= INT32_MAX) return samples * groups;
+    PyErr_SetString(PyExc_ValueError, "number of samples or groups out of range");
+    return -1;
+}
+
+/* X, gamma, beta, Y, mean, rstd, groups, eps, sample_ptr, n_samples, max_sample_rows, act, workspace, stream */
+static PyObject *group_norm_fwd(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    if (expect(n, 14)) return NULL;
+    if (!fn_group_norm_fwd) { PyErr_SetString(PyExc_RuntimeError, "connect() first"); return NULL; }
+    gnn_norm_opts o = {0};
+    void *X, *Y, *gamma, *beta, *mean, *rstd, *ptr;
+    int64_t shape[2] = {-1, -1}, G, B, pairs;
+    double eps;
+    if (feature_matrix(a[0], 0, shape, &o.dtype, &X, &o.ldx) || feature_matrix(a[3], 0, shape, &o.dtype, &Y, &o.ldy) || to_i64(a[6], &G) ||
+        to_double(a[7], &eps) || norm_options(a + 8, &o, &ptr, &B) || (pairs = pairs_of(B, G)) < 0 || floats(a[1], 1, shape[1], &gamma) ||
+        floats(a[2], 1, shape[1], &beta) || floats(a[4], 0, pairs, &mean) || floats(a[5], 0, pairs, &rstd))
+        return NULL;
+    o.eps = (float)eps;
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn_group_norm_fwd(X, gamma, beta, ptr, Y, mean, rstd, shape[0], shape[1], G, B, &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* X, gamma, beta, mean, rstd, dY, dX, dgamma, dbeta, groups, sample_ptr, n_samples, max_sample_rows, act, workspace, stream */
+static PyObject *group_norm_bwd(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    if (expect(n, 16)) return NULL;
+    if (!fn_group_norm_bwd) { PyErr_SetString(PyExc_RuntimeError, "connect() first"); return NULL; }
+    gnn_norm_opts o = {0};
+    void *X, *dY, *dX, *gamma, *beta, *mean, *rstd, *dgamma, *dbeta, *ptr;
+    int64_t shape[2] = {-1, -1}, G, B, pairs;
+    if (feature_matrix(a[0], 0, shape, &o.dtype, &X, &o.ldx) || feature_matrix(a[5], 0, shape, &o.dtype, &dY, &o.ldy) ||
+        feature_matrix(a[6], 1, shape, &o.dtype, &dX, &o.lddx) || to_i64(a[9], &G) || norm_options(a + 10, &o, &ptr, &B) ||
+        (pairs = pairs_of(B, G)) < 0 || floats(a[1], 1, shape[1], &gamma) || floats(a[2], 1, shape[1], &beta) || floats(a[3], 0, pairs, &mean) ||
+        floats(a[4], 0, pairs, &rstd) ||
+        floats(a[7], 1, shape[1], &dgamma) || floats(a[8], 1, shape[1], &dbeta))
+        return NULL;
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn_group_norm_bwd(X, gamma, beta, mean, rstd, dY, ptr, dX, dgamma, dbeta, shape[0], shape[1], G, B, &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* X, labels, loss, dX, loss_rows, reduction, scale, workspace, stream */
+static PyObject *softmax_xent(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    if (expect(n, 9)) return NULL;
+    if (!fn_softmax_xent) { PyErr_SetString(PyExc_RuntimeError, "connect() first"); return NULL; }
+    gnn_loss_opts o = {0};
+    void *X, *labels, *loss, *dX, *rows;
+    int64_t shape[2] = {-1, -1}, n_labels;
+    double scale;
+    if (feature_matrix(a[0], 0, shape, &o.dtype, &X, &o.ldx) || integers(a[1], &labels, &o.labels_is_64, &n_labels) || floats(a[2], 0, 1, &loss) ||
+        feature_matrix(a[3], 1, shape, &o.dtype, &dX, &o.ldg) || floats(a[4], 1, shape[0], &rows) || to_int(a[5], &o.reduction) ||
+        to_double(a[6], &scale) || scratch_of(a[7], &o.workspace, &o.workspace_bytes) || stream_ptr(a[8], &o.stream))
+        return NULL;
+    if (n_labels != shape[0]) { PyErr_SetString(PyExc_ValueError, "one label a row expected"); return NULL; }
+    o.scale = (float)scale;
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn_softmax_xent(X, labels, loss, dX, rows, shape[0], shape[1], &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* address of the descriptors, their number, step, lr, beta1, beta2, eps, grad_scale, seed, stream */
+static PyObject *adamw_step(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    if (expect(n, 10)) return NULL;
+    if (!fn_adamw_step) { PyErr_SetString(PyExc_RuntimeError, "connect() first"); return NULL; }
+    gnn_adamw_opts o = {0};
+    int64_t address, count;
+    void *scale;
+    if (to_i64(a[0], &address) || to_i64(a[1], &count) || to_i64(a[2], &o.step) || to_double(a[3], &o.lr) || to_double(a[4], &o.beta1) ||
+        to_double(a[5], &o.beta2) || to_double(a[6], &o.eps) || floats(a[7], 1, 1, &scale) || to_i64(a[8], &o.seed) || stream_ptr(a[9], &o.stream))
+        return NULL;
+    o.grad_scale = scale;
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn_adamw_step((const gnn_adamw_tensor *)(intptr_t)address, count, &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
 /* connect({name: address}, torch): the library's entry points and torch's types */
 static PyObject *connect(PyObject *self, PyObject *args) {
     (void)self;
@@ -422,7 +622,9 @@ static PyObject *connect(PyObject *self, PyObject *args) {
         {"gnn_aggregate_fwd", (void **)&fn_aggregate_fwd}, {"gnn_aggregate_bwd", (void **)&fn_aggregate_bwd},
         {"gnn_ap_fwd", (void **)&fn_ap_fwd}, {"gnn_ap_bwd_vertex", (void **)&fn_ap_bwd_vertex},
         {"gnn_ap_bwd_vertex_arg_edges", (void **)&fn_ap_bwd_vertex_arg}, {"gnn_ap_bwd_edge", (void **)&fn_ap_bwd_edge},
-        {"gnn_sage_layer_fwd", (void **)&fn_sage_layer_fwd}, {"gnn_sage_layer_bwd", (void **)&fn_sage_layer_bwd}};
+        {"gnn_sage_layer_fwd", (void **)&fn_sage_layer_fwd}, {"gnn_sage_layer_bwd", (void **)&fn_sage_layer_bwd},
+        {"gnn_group_norm_fwd", (void **)&fn_group_norm_fwd}, {"gnn_group_norm_bwd", (void **)&fn_group_norm_bwd},
+        {"gnn_softmax_xent", (void **)&fn_softmax_xent}, {"gnn_adamw_step", (void **)&fn_adamw_step}};
     const struct { const char *name; PyObject **slot; } attrs[] = {
         {"float32", &dtype_f32}, {"bfloat16", &dtype_bf16}, {"int32", &dtype_i32}, {"int64", &dtype_i64}};
     for (size_t i = 0; i < sizeof(attrs) / sizeof(attrs[0]); ++i)
@@ -451,7 +653,8 @@ static PyObject *connect(PyObject *self, PyObject *args) {
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {FAST(aggregate), FAST(ap_fwd), FAST(ap_bwd_vertex), FAST(ap_bwd_vertex_arg), FAST(ap_bwd_edge),
-                                FAST(sage_layer_fwd), FAST(sage_layer_bwd), {"connect", connect, METH_VARARGS, NULL},
+                                FAST(sage_layer_fwd), FAST(sage_layer_bwd), FAST(group_norm_fwd), FAST(group_norm_bwd),
+                                FAST(softmax_xent), FAST(adamw_step), {"connect", connect, METH_VARARGS, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", "Argument marshalling of the hot entry points.", -1, methods,
                                     NULL, NULL, NULL, NULL};
@@ -459,7 +662,8 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", "Argument 
 PyMODINIT_FUNC PyInit__pycall(void) {
     const struct { const char *text; PyObject **slot; } names[] = {
         {"data_ptr", &s_data_ptr}, {"stride", &s_stride}, {"dtype", &s_dtype}, {"handle", &s_handle},
-        {"cuda_stream", &s_cuda_stream}, {"is_contiguous", &s_is_contiguous}, {"nbytes", &s_nbytes}, {"shape", &s_shape}};
+        {"cuda_stream", &s_cuda_stream}, {"is_contiguous", &s_is_contiguous}, {"nbytes", &s_nbytes}, {"shape", &s_shape},
+        {"is_cuda", &s_is_cuda}};
     for (size_t i = 0; i < sizeof(names) / sizeof(names[0]); ++i)
         if (!(*names[i].slot = PyUnicode_InternFromString(names[i].text))) return NULL;
     return PyModule_Create(&module);

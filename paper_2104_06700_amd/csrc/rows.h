@@ -1,0 +1,60 @@
+// Rows of vertex matrices in fp32 and bf16 for the kernels of norm.hip, loss.hip and adamw.hip: VEC elements at a time, in fp32
+// registers, at the alignment of one element (global loads and stores of 16 bytes need no more).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+struct gnn_bf16 { uint16_t bits; };
+
+typedef float gnn_f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t gnn_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+typedef float gnn_f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 gnn_bf16x2 __attribute__((ext_vector_type(2)));
+
+template <typename T> struct gnn_rows;
+
+template <> struct gnn_rows<float> {
+    static constexpr int VEC = 4;
+    typedef gnn_f32x4 raw;
+    static __device__ __forceinline__ raw fetch(const float *p) { return *reinterpret_cast<const gnn_f32x4 *>(p); }
+    static __device__ __forceinline__ void put(float *p, raw t) { *reinterpret_cast<gnn_f32x4 *>(p) = t; }
+    static __device__ __forceinline__ void unpack(raw t, float (&v)[4]) { v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w; }
+    static __device__ __forceinline__ raw pack(const float (&v)[4]) { return raw{v[0], v[1], v[2], v[3]}; }
+    static __device__ __forceinline__ float get(const float *p) { return *p; }
+    static __device__ __forceinline__ void set(float *p, float v) { *p = v; }
+};
+
+template <> struct gnn_rows<gnn_bf16> {
+    static constexpr int VEC = 8;
+    typedef gnn_u32x4 raw;
+    static __device__ __forceinline__ raw fetch(const gnn_bf16 *p) { return *reinterpret_cast<const gnn_u32x4 *>(p); }
+    static __device__ __forceinline__ void put(gnn_bf16 *p, raw t) { *reinterpret_cast<gnn_u32x4 *>(p) = t; }
+    static __device__ __forceinline__ void unpack(raw t, float (&v)[8]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(t[i] << 16);
+            v[2 * i + 1] = __uint_as_float(t[i] & 0xFFFF0000u);
+        }
+    }
+    // to the nearest, ties to even: one instruction for two elements
+    static __device__ __forceinline__ raw pack(const float (&v)[8]) {
+        raw t;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            t[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(gnn_f32x2{v[2 * i], v[2 * i + 1]}, gnn_bf16x2));
+        return t;
+    }
+    static __device__ __forceinline__ float get(const gnn_bf16 *p) { return __uint_as_float(uint32_t(p->bits) << 16); }
+    static __device__ __forceinline__ void set(gnn_bf16 *p, float v) { p->bits = __builtin_bit_cast(uint16_t, __bf16(v)); }
+};
+
+// VEC == 1: rows narrower than a vector
+template <typename T, int VEC> __device__ __forceinline__ void gnn_load_row(const T *p, float (&v)[VEC]) {
+    if constexpr (VEC == 1) v[0] = gnn_rows<T>::get(p);
+    else gnn_rows<T>::unpack(gnn_rows<T>::fetch(p), v);
+}
+template <typename T, int VEC> __device__ __forceinline__ void gnn_store_row(T *p, const float (&v)[VEC]) {
+    if constexpr (VEC == 1) gnn_rows<T>::set(p, v[0]);
+    else gnn_rows<T>::put(p, gnn_rows<T>::pack(v));
+}
