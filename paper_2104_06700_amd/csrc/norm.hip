@@ -8,7 +8,8 @@
 //     dbeta[c] = sum dz,  dgamma[c] = sum dz xh  (over all rows),
 //     s1 = sum dz gamma / n,  s2 = sum dz gamma xh / n  (over the sample and group),  dX = rstd (dz gamma - s1 - xh s2).
 //
-// Rows are cut into tiles of equal size whatever the samples' sizes are, one workgroup each.  A tile adds up each sample's part of
+// Two ways.  Samples that fit a workgroup's registers (small_kernel, small_bwd_kernel) are read once and done in one launch.  All others: the
+// rows are cut into tiles of equal size whatever the samples' sizes are, one workgroup each, which adds up each sample's part of
 // it per column; the partial sums of tile t and sample b lie in slot t + b (from one pair to the next at least one of the two
 // grows, so no two share a slot).  A second kernel merges the slots of every sample, in their order: results do not depend on
 // timing.  A third reads the rows again and writes the result.
@@ -17,8 +18,9 @@
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kJoinedThreads = 512;
 constexpr int64_t kMaxTiles = 2048;  // as many workgroups as are resident at once
+constexpr int kJoined = 8192;        // partial sums that the writing kernel joins by itself
 
 // Rows of every sample: from `ptr` (ragged), or `rows` of them each.  What ptr holds is kept inside the matrix.
 struct Samples {
@@ -32,7 +34,7 @@ struct Samples {
     }
     // the first sample that ends behind `row`
     __device__ __forceinline__ int64_t of(int64_t row) const {
-        if (!ptr) return row / rows;
+        if (!ptr) return count == 1 ? 0 : int64_t(uint32_t(row) / uint32_t(rows));
         int64_t lo = 0, hi = count;
         while (lo < hi) {
             const int64_t mid = (lo + hi) >> 1;
@@ -43,17 +45,20 @@ struct Samples {
     }
 };
 
+constexpr float kLog2e = 1.44269504088896340736f;
+// 1 / (1 + exp(-z)): exp2 of a product, sum, reciprocal
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * z)); }
 template <int ACT> __device__ __forceinline__ float activate(float z) {
     if constexpr (ACT == GNN_ACT_RELU) return z > 0.0f ? z : z == z ? 0.0f : z;  // NaN stays
-    else if constexpr (ACT == GNN_ACT_SILU) return z / (1.0f + __expf(-z));
+    else if constexpr (ACT == GNN_ACT_SILU) return z * sigmoid(z);
     else return z;
 }
 // the activation's derivative
 template <int ACT> __device__ __forceinline__ float slope(float z) {
     if constexpr (ACT == GNN_ACT_RELU) return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
     else if constexpr (ACT == GNN_ACT_SILU) {
-        const float s = 1.0f / (1.0f + __expf(-z));
-        return s * (1.0f + z * (1.0f - s));
+        const float s = sigmoid(z);
+        return s + s * (z - z * s);
     } else return 1.0f;
 }
 
@@ -63,6 +68,7 @@ struct Shape {
     int C, group_width, G;
     int cols;       // vectors of columns of a workgroup; threads: cols x row_lanes
     int row_lanes;
+    int32_t *sample_of;  // [N] ragged samples: the sample of every row, for the kernels that write results
 };
 
 // What a thread of a tile works on: VEC neighbouring columns from `col`, every row_lanes-th row.  The last vector of a row starts
@@ -88,127 +94,209 @@ template <typename F> __device__ __forceinline__ void for_parts(const Shape &s, 
         const int64_t end = s.samples.begin(b + 1);
         const int64_t stop = end < r1 ? end : r1;
         if (stop <= row) continue;
+        if (s.sample_of && blockIdx.y == 0)
+            for (int64_t r = row + threadIdx.x; r < stop; r += blockDim.x) s.sample_of[r] = int32_t(b);
         f(b, row, stop);
         row = stop;
     }
 }
 
-// Per part and column: the mean and the sum of squared distances from it.  Sums are taken of the distances from the thread's first
-// row, which is of the values' own size, so that a mean far from zero costs no bits.
-template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads) norm_part_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, float2 *__restrict__ part) {
-    __shared__ float red_mean[kThreads * VEC], red_m2[kThreads * VEC];
+// sums over the row lanes of a tile: red [row_lanes][cols * VEC]; the sum of lane 0's columns is left in lane 0's places
+template <int VEC> __device__ __forceinline__ void add_row_lanes(float *a, float *b, const Shape &s, const Place<VEC> &at, int lanes) {
+    const int width = s.cols * VEC;
+    while (lanes > 1) {
+        const int half = (lanes + 1) >> 1;
+        __syncthreads();
+        if (at.row_lane + half < lanes) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const int i = at.row_lane * width + at.lane * VEC + j;
+                a[i] += a[i + half * width];
+                b[i] += b[i + half * width];
+            }
+        }
+        lanes = half;
+    }
+    __syncthreads();
+}
+
+// Per part and column: the mean and the sum of squared distances from it.  Sums are taken of the distances from the part's first
+// row, which is of the values' own size, so that a mean far from zero costs no bits; four rows and then
+// eight times four are added up by themselves, so that long sums do not lose them.
+template <typename T, int VEC, bool NT, int THREADS>
+__global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, float2 *__restrict__ part) {
+    extern __shared__ float tile_lds[];
+    float *const red_1 = tile_lds, *const red_2 = tile_lds + blockDim.x * VEC;
     const Place<VEC> at(s);
     for_parts(s, [&](int64_t b, int64_t row, int64_t stop) {
-        float mean[VEC], m2[VEC];
-        const int64_t first = row + at.row_lane;
-        if (at.active && first < stop) {
-            float pivot[VEC], s1[VEC], s2[VEC];
-            gnn_load_row<T, VEC>(X + first * ldx + at.col, pivot);
+        constexpr int U = 4;
+        float pivot[VEC], s1[VEC], s2[VEC];
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) s1[j] = s2[j] = 0.0f;
-            int n = 1;
-            for (int64_t r = first + s.row_lanes; r < stop; r += s.row_lanes, ++n) {
-                float x[VEC];
-                gnn_load_row<T, VEC>(X + r * ldx + at.col, x);
+        for (int j = 0; j < VEC; ++j) pivot[j] = s1[j] = s2[j] = 0.0f;
+        if (at.active) {
+            gnn_load_row<T, VEC>(X + row * ldx + at.col, pivot);
+            int64_t r = row + at.row_lane;
+            const T *x = X + r * ldx + at.col;
+            const int64_t step = s.row_lanes * ldx;
+            while (r < stop) {
+                float t1[VEC], t2[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) t1[j] = t2[j] = 0.0f;
+                for (int k = 0; k < 8 && r < stop; ++k, r += U * s.row_lanes, x += U * step) {
+                    float v[U][VEC];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        if (r + u * s.row_lanes < stop) gnn_load_row<T, VEC, NT>(x + u * step, v[u]);
+                        else
+#pragma unroll
+                            for (int j = 0; j < VEC; ++j) v[u][j] = pivot[j];
+                    }
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) v[u][j] -= pivot[j];
+                        t1[j] += (v[0][j] + v[1][j]) + (v[2][j] + v[3][j]);
+                        t2[j] += (v[0][j] * v[0][j] + v[1][j] * v[1][j]) + (v[2][j] * v[2][j] + v[3][j] * v[3][j]);
+                    }
+                }
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    const float d = x[j] - pivot[j];
-                    s1[j] += d;
-                    s2[j] += d * d;
+                    s1[j] += t1[j];
+                    s2[j] += t2[j];
                 }
             }
-            const float inv = 1.0f / float(n);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                mean[j] = pivot[j] + s1[j] * inv;
-                m2[j] = s2[j] - s1[j] * s1[j] * inv;
-                m2[j] = m2[j] < 0.0f ? 0.0f : m2[j];
-            }
         }
+        // the distances of all row lanes are from one row, so their sums are added as they are
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            red_mean[threadIdx.x * VEC + j] = mean[j];
-            red_m2[threadIdx.x * VEC + j] = m2[j];
+            red_1[threadIdx.x * VEC + j] = s1[j];
+            red_2[threadIdx.x * VEC + j] = s2[j];
         }
-        __syncthreads();
+        add_row_lanes<VEC>(red_1, red_2, s, at, s.row_lanes);
         if (at.active && at.row_lane == 0) {
-            const int64_t rows = stop - row;
-            const int lanes = rows < s.row_lanes ? int(rows) : s.row_lanes;
-            const int64_t full = rows / s.row_lanes, rest = rows % s.row_lanes;
-            float2 out[VEC];
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                float sum = 0.0f;
-                const float base = red_mean[at.lane * VEC + j];
-                for (int l = 0; l < lanes; ++l) sum += float(full + (l < rest)) * (red_mean[(l * s.cols + at.lane) * VEC + j] - base);
-                const float m = base + sum / float(rows);
-                float q = 0.0f;
-                for (int l = 0; l < lanes; ++l) {
-                    const int i = (l * s.cols + at.lane) * VEC + j;
-                    const float d = red_mean[i] - m;
-                    q += red_m2[i] + float(full + (l < rest)) * d * d;
-                }
-                out[j] = make_float2(m, q);
-            }
+            const float inv = 1.0f / float(stop - row);
             float2 *o = part + (int64_t(blockIdx.x) + b) * s.C + at.col;
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) o[j] = out[j];
+            for (int j = 0; j < VEC; ++j) {
+                const float a = red_1[at.lane * VEC + j], q = red_2[at.lane * VEC + j] - a * a * inv;
+                o[j] = make_float2(pivot[j] + a * inv, q < 0.0f ? 0.0f : q);
+            }
         }
         __syncthreads();
     });
 }
 
-template <int THREADS> __device__ __forceinline__ double team_sum(double v, double *red) {
+template <int THREADS> __device__ __forceinline__ double2 team_sum(double2 v, double2 *red) {
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    for (int d = 32; d > 0; d >>= 1) {
+        v.x += __shfl_xor(v.x, d);
+        v.y += __shfl_xor(v.y, d);
+    }
     if constexpr (THREADS > 64) {
         __syncthreads();
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = 0.0;
-        for (int i = 0; i < THREADS / 64; ++i) v += red[i];
+        v = red[0];
+#pragma unroll
+        for (int i = 1; i < THREADS / 64; ++i) {
+            v.x += red[i].x;
+            v.y += red[i].y;
+        }
     }
     return v;
 }
+
+// A sample's tiles, and THREADS threads on them: `wide` neighbouring columns of a group side by side, every `deep`-th tile.
+template <int THREADS> struct Merge {
+    int64_t lo, hi, t0, t1;
+    int wide, deep, k, d;
+    __device__ __forceinline__ Merge(const Shape &s, int64_t b) {
+        lo = s.samples.begin(b);
+        hi = s.samples.begin(b + 1);
+        t0 = lo / s.tile_rows;
+        t1 = hi > lo ? (hi - 1) / s.tile_rows : t0 - 1;
+        wide = s.group_width < THREADS ? s.group_width : THREADS;
+        deep = THREADS / wide;
+        k = int(threadIdx.x) % wide;
+        d = int(threadIdx.x) / wide;
+    }
+    // f(rows of the sample in tile t, partial sums of column c there), four loads in flight
+    template <typename F> __device__ __forceinline__ void tiles(const Shape &s, const float2 *part, int64_t b, int c, F f) const {
+        constexpr int U = 4;
+        if (d >= deep) return;
+        for (int64_t t = t0 + d; t <= t1; t += U * deep) {
+            float2 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (t + u * deep <= t1) v[u] = part[(t + u * deep + b) * s.C + c];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t w = t + u * deep;
+                if (w > t1) continue;
+                const int64_t r0 = w * s.tile_rows > lo ? w * s.tile_rows : lo, r1 = (w + 1) * s.tile_rows < hi ? (w + 1) * s.tile_rows : hi;
+                f(double(r1 - r0), v[u]);
+            }
+        }
+    }
+};
 
 // Mean and reciprocal deviation of a sample and group from its parts: THREADS threads for a pair.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const float2 *__restrict__ part, const Shape s, float eps, float *__restrict__ mean,
                                                              float *__restrict__ rstd) {
-    __shared__ double red[THREADS / 64];
+    __shared__ double2 red[THREADS / 64];
     const int64_t pairs = s.samples.count * s.G;
     for (int64_t p = blockIdx.x; p < pairs; p += gridDim.x) {
         const int64_t b = p / s.G;
-        const int g = int(p % s.G);
-        const int64_t lo = s.samples.begin(b), hi = s.samples.begin(b + 1);
-        double m = 0.0, q = 0.0;
-        const double n = double(hi > lo ? hi - lo : 0) * s.group_width;
-        if (hi > lo) {
-            const int64_t t0 = lo / s.tile_rows, t1 = (hi - 1) / s.tile_rows;
-            const int64_t items = (t1 - t0 + 1) * s.group_width;
-            for (int64_t i = threadIdx.x; i < items; i += THREADS) {
-                const int64_t t = t0 + i / s.group_width;
-                const int64_t r0 = t * s.tile_rows > lo ? t * s.tile_rows : lo;
-                const int64_t r1 = (t + 1) * s.tile_rows < hi ? (t + 1) * s.tile_rows : hi;
-                m += double(r1 - r0) * part[(t + b) * s.C + g * s.group_width + i % s.group_width].x;
-            }
-            m = team_sum<THREADS>(m, red) / n;
-            for (int64_t i = threadIdx.x; i < items; i += THREADS) {
-                const int64_t t = t0 + i / s.group_width;
-                const int64_t r0 = t * s.tile_rows > lo ? t * s.tile_rows : lo;
-                const int64_t r1 = (t + 1) * s.tile_rows < hi ? (t + 1) * s.tile_rows : hi;
-                const float2 v = part[(t + b) * s.C + g * s.group_width + i % s.group_width];
-                const double d = v.x - m;
-                q += double(v.y) + double(r1 - r0) * d * d;
-            }
-            q = team_sum<THREADS>(q, red) / n;
+        const int c0 = int(p % s.G) * s.group_width;
+        const Merge<THREADS> m(s, b);
+        double mid = 0.0, var = 0.0;
+        if (m.hi > m.lo) {
+            const double pivot = part[(m.t0 + b) * s.C + c0].x;
+            double2 u = {0.0, 0.0};
+            for (int k = m.k; k < s.group_width; k += m.wide)
+                m.tiles(s, part, b, c0 + k, [&](double rows, float2 v) {
+                    const double d = double(v.x) - pivot;
+                    u.x += rows * d;
+                    u.y += double(v.y) + rows * d * d;
+                });
+            u = team_sum<THREADS>(u, red);
+            const double n = double(m.hi - m.lo) * s.group_width, off = u.x / n;
+            mid = pivot + off;
+            var = u.y / n - off * off;
+            var = var < 0.0 ? 0.0 : var;  // (NaN stays)
         }
         if (threadIdx.x == 0) {
-            mean[p] = float(m);
-            rstd[p] = float(1.0 / sqrt(q + double(eps)));
+            mean[p] = float(mid);
+            rstd[p] = float(1.0 / sqrt(var + double(eps)));
         }
     }
+}
+
+// Sums of `groups` runs of n values each, sixteen to one at a time, between two areas of LDS; returns where they are.  All threads of the
+// workgroup call it together, `threads` of them with their number i (others with i >= threads).
+template <typename V> __device__ __forceinline__ void add_to(V &a, const V &b) {
+    if constexpr (sizeof(V) == 8) { a.x += b.x; a.y += b.y; }
+    else a += b;
+}
+template <typename V> __device__ __forceinline__ const V *group_sums(V *from, V *to, int groups, int n, int i, int threads) {
+    while (n > 1) {
+        const int out = (n + 15) >> 4;
+        __syncthreads();
+        if (i < threads)
+            for (int k = i; k < groups * out; k += threads) {
+                const int g = out == 1 ? k : int(unsigned(k) / unsigned(out)), o = k - g * out;
+                V t = from[g * n + o];
+                for (int e = o + out; e < n; e += out) add_to(t, from[g * n + e]);
+                to[k] = t;
+            }
+        n = out;
+        V *const swap = from;
+        from = to;
+        to = swap;
+    }
+    __syncthreads();
+    return from;
 }
 
 // gamma and beta of a thread's columns, and their groups
@@ -218,70 +306,222 @@ template <int VEC> struct Affine {
     __device__ __forceinline__ Affine(const Shape &s, int col, const float *g, const float *b) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            gamma[j] = g ? g[col + j] : 1.0f;
-            beta[j] = b ? b[col + j] : 0.0f;
-            group[j] = (col + j) / s.group_width;
+            gamma[j] = 1.0f;
+            beta[j] = 0.0f;
+        }
+        if (g) columns(g + col, gamma);
+        if (b) columns(b + col, beta);
+        const int first = col / s.group_width;
+        int g0 = first, left = (first + 1) * s.group_width - col;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            if (left == 0) { ++g0; left = s.group_width; }
+            group[j] = g0;
+            --left;
+        }
+    }
+    static __device__ __forceinline__ void columns(const float *p, float (&out)[VEC]) {
+        if constexpr (VEC == 1) out[0] = *p;
+        else
+#pragma unroll
+            for (int j = 0; j < VEC; j += 4) {
+                const gnn_f32x4 v = *reinterpret_cast<const gnn_f32x4 *>(p + j);
+                out[j] = v.x; out[j + 1] = v.y; out[j + 2] = v.z; out[j + 3] = v.w;
+            }
+    }
+    template <typename V> __device__ __forceinline__ void gather(const Shape &s, const V *stat, int64_t b, V (&out)[VEC]) const {
+        const V *p = stat + b * s.G;
+        if (group[0] == group[VEC - 1]) {  // one load where a vector has one group
+            const V v = p[group[0]];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) out[j] = v;
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) out[j] = p[group[j]];
         }
     }
 };
 
-template <typename T, int VEC, int ACT>
-__global__ void __launch_bounds__(kThreads) norm_apply_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, const float *__restrict__ gamma,
-                                                              const float *__restrict__ beta, const float *__restrict__ mean,
-                                                              const float *__restrict__ rstd, T *__restrict__ Y, int64_t ldy) {
-    const Place<VEC> at(s);
-    if (!at.active) return;
-    const Affine<VEC> aff(s, at.col, gamma, beta);
-    for_parts(s, [&](int64_t b, int64_t row, int64_t stop) {
-        float m[VEC], a[VEC];
+// The kernels that write results: a workgroup of cols x row_lanes threads has kRows * row_lanes neighbouring rows and ends with them, a thread
+// kRows vectors of one column.  Small workgroups that end are faster here than ones that stay and walk: the writes
+// and reads of all of them move through the matrix as one front (2.5 GB copied by one-vector threads 6.5 TB/s, four vectors 6.1, resident
+// workgroups 5.0; norm of 2.4 M x 256 fp32 in workgroups of 128 threads with 1, 2, 4, 8 rows each 1268, 1159, 1205, 1224 us, of 256 threads with 2, 4, 8 1202,
+// 1237, 1248).
+constexpr int kRows = 2, kBlockMost = 128;
+template <int VEC> __device__ __forceinline__ int column_of_block(const Shape &s) {
+    const int vec = int(blockIdx.y) * s.cols + int(threadIdx.x);
+    return vec * VEC >= s.C ? -1 : vec * VEC < s.C - VEC ? vec * VEC : s.C - VEC;
+}
+// One sample of few tiles: the writing kernel joins their partial sums by itself, every workgroup for all columns, which costs less than a
+// launch.  f(partial, rows, column) -> what a column's tiles add up; g(group, sum over its columns) -> what the group keeps.
+// The threads are (vector of columns, row lane) of all columns.  Returns the groups' results in LDS.
+template <int VEC, typename F, typename G> __device__ __forceinline__ const float2 *join_tiles(const Shape &s, const float2 *part, int64_t tiles, int col, F f, G g) {
+    extern __shared__ float2 join_lds[];
+    float2 *const sums = join_lds, *const next = join_lds + s.row_lanes * s.C;
+    float2 u[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) u[j] = make_float2(0.0f, 0.0f);
+    constexpr int U = 4;
+    for (int64_t t = threadIdx.y; t < tiles; t += U * s.row_lanes) {
+        float2 v[U][VEC];
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (t + k * s.row_lanes < tiles)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) v[k][j] = part[(t + k * s.row_lanes) * s.C + col + j];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t w = t + k * s.row_lanes;
+            if (w >= tiles) break;
+            const float rows = float(w + 1 < tiles ? s.tile_rows : s.N - w * s.tile_rows);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) add_to(u[j], f(v[k][j], rows, col + j));
+        }
+    }
+    // [group][row lane][column of it]; columns that two vectors share are written twice, alike
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        const int group = int(unsigned(col + j) / unsigned(s.group_width));
+        sums[(group * s.row_lanes + threadIdx.y) * s.group_width + col + j - group * s.group_width] = u[j];
+    }
+    const int i = int(threadIdx.y) * s.cols + int(threadIdx.x), threads = s.cols * s.row_lanes;
+    const float2 *all = group_sums(sums, next, s.G, s.row_lanes * s.group_width, i, threads);
+    float2 *const out = all == sums ? next : sums;
+    __syncthreads();
+    for (int k = i; k < s.G; k += threads) out[k] = g(k, all[k]);
+    __syncthreads();
+    return out;
+}
+__device__ __forceinline__ int64_t sample_of_row(const Shape &s, int64_t r) {
+    return s.sample_of ? int64_t(s.sample_of[r]) : s.samples.of(r);
+}
+
+enum Stats { kMany, kOne, kJoin };  // statistics of many samples, of one, of one that has to be joined from tiles first
+
+template <typename T, int VEC, int ACT, bool NT, Stats STATS>
+__global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, const float *__restrict__ gamma,
+                                                         const float *__restrict__ beta, float *__restrict__ mean, float *__restrict__ rstd,
+                                                         T *__restrict__ Y, int64_t ldy, const float2 *__restrict__ part, float eps) {
+    const int col = column_of_block<VEC>(s);
+    const int64_t r0 = int64_t(blockIdx.x) * (kRows * s.row_lanes) + threadIdx.y;
+    if (STATS != kJoin && (col < 0 || r0 >= s.N)) return;
+    gnn_strip<T, VEC, NT> strip[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u)
+        if (r0 + u * s.row_lanes < s.N) strip[u].load(X + (r0 + u * s.row_lanes) * ldx + col);
+    const Affine<VEC> aff(s, col, gamma, beta);
+    float w[VEC], o[VEC];  // z = x w + o
+    auto fold = [&]() {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            m[j] = mean[b * s.G + aff.group[j]];
-            a[j] = rstd[b * s.G + aff.group[j]] * aff.gamma[j];
+            w[j] *= aff.gamma[j];
+            o[j] = aff.beta[j] - o[j] * w[j];
         }
-        for (int64_t r = row + at.row_lane; r < stop; r += s.row_lanes) {
-            float x[VEC];
-            gnn_load_row<T, VEC>(X + r * ldx + at.col, x);
+    };
+    if constexpr (STATS == kOne) {
+        aff.gather(s, mean, 0, o);
+        aff.gather(s, rstd, 0, w);
+        fold();
+    } else if constexpr (STATS == kJoin) {
+        // distances from the first tile's mean of the group's first column
+        const float n = float(s.N) * float(s.group_width);
+        const float2 *stat = join_tiles<VEC>(s, part, (s.N + s.tile_rows - 1) / s.tile_rows, col,
+            [&](float2 v, float rows, int c) {
+                const float d = v.x - part[c - c % s.group_width].x;
+                return make_float2(rows * d, v.y + rows * d * d);
+            },
+            [&](int g, float2 u) {
+                const float off = u.x / n, var = u.y / n - off * off;
+                const float2 r = make_float2(part[g * s.group_width].x + off, 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps));
+                if (blockIdx.x == 0) {
+                    mean[g] = r.x;
+                    rstd[g] = r.y;
+                }
+                return r;
+            });
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) x[j] = activate<ACT>((x[j] - m[j]) * a[j] + aff.beta[j]);
-            gnn_store_row<T, VEC>(Y + r * ldy + at.col, x);
+        for (int j = 0; j < VEC; ++j) {
+            o[j] = stat[aff.group[j]].x;
+            w[j] = stat[aff.group[j]].y;
         }
-    });
+        fold();
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+        const int64_t r = r0 + u * s.row_lanes;
+        if (r >= s.N) break;
+        if constexpr (STATS == kMany) {
+            const int64_t b = sample_of_row(s, r);
+            aff.gather(s, mean, b, o);
+            aff.gather(s, rstd, b, w);
+            fold();
+        }
+        float x[VEC];
+        strip[u].get(x);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[j] = activate<ACT>(x[j] * w[j] + o[j]);
+        gnn_store_row<T, VEC, NT>(Y + r * ldy + col, x);
+    }
 }
 
 // Per part and column: sum dz and sum dz xh; per tile and column their sums over its parts (total; NULL where there is one sample).
-template <typename T, int VEC, int ACT>
-__global__ void __launch_bounds__(kThreads) norm_bwd_part_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const Shape s,
+template <typename T, int VEC, int ACT, bool NT, int THREADS>
+__global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const Shape s,
                                                                  const float *__restrict__ gamma, const float *__restrict__ beta,
                                                                  const float *__restrict__ mean, const float *__restrict__ rstd,
                                                                  float2 *__restrict__ part, float2 *__restrict__ total) {
-    __shared__ float red_1[kThreads * VEC], red_x[kThreads * VEC];
+    extern __shared__ float tile_lds[];
+    float *const red_1 = tile_lds, *const red_x = tile_lds + blockDim.x * VEC;
     const Place<VEC> at(s);
     const Affine<VEC> aff(s, at.col, gamma, beta);
     float t1[VEC], tx[VEC];
 #pragma unroll
     for (int j = 0; j < VEC; ++j) t1[j] = tx[j] = 0.0f;
     for_parts(s, [&](int64_t b, int64_t row, int64_t stop) {
+        constexpr int U = VEC == 8 && THREADS > kThreads ? 2 : 4;
         float a1[VEC], ax[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) a1[j] = ax[j] = 0.0f;
         if (at.active) {
-            float m[VEC], r[VEC];
+            float o[VEC], rs[VEC];  // xh = x rs + o
+            aff.gather(s, mean, b, o);
+            aff.gather(s, rstd, b, rs);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                m[j] = mean[b * s.G + aff.group[j]];
-                r[j] = rstd[b * s.G + aff.group[j]];
-            }
-            for (int64_t i = row + at.row_lane; i < stop; i += s.row_lanes) {
-                float x[VEC], d[VEC];
-                gnn_load_row<T, VEC>(X + i * ldx + at.col, x);
-                gnn_load_row<T, VEC>(dY + i * ldy + at.col, d);
+            for (int j = 0; j < VEC; ++j) o[j] = -o[j] * rs[j];
+            int64_t r = row + at.row_lane;
+            while (r < stop) {
+                float c1[VEC], cx[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) c1[j] = cx[j] = 0.0f;
+                for (int k = 0; k < 32 / U && r < stop; ++k, r += U * s.row_lanes) {
+                    gnn_strip<T, VEC, NT> sx[U], sd[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int64_t i = r + u * s.row_lanes;
+                        if (i < stop) {
+                            sx[u].load(X + i * ldx + at.col);
+                            sd[u].load(dY + i * ldy + at.col);
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        if (r + u * s.row_lanes >= stop) break;
+                        float x[VEC], d[VEC];
+                        sx[u].get(x);
+                        sd[u].get(d);
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) {
+                            const float xh = x[j] * rs[j] + o[j];
+                            const float dz = d[j] * slope<ACT>(xh * aff.gamma[j] + aff.beta[j]);
+                            c1[j] += dz;
+                            cx[j] += dz * xh;
+                        }
+                    }
+                }
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    const float xh = (x[j] - m[j]) * r[j];
-                    const float dz = d[j] * slope<ACT>(xh * aff.gamma[j] + aff.beta[j]);
-                    a1[j] += dz;
-                    ax[j] += dz * xh;
+                    a1[j] += c1[j];
+                    ax[j] += cx[j];
                 }
             }
         }
@@ -290,16 +530,12 @@ __global__ void __launch_bounds__(kThreads) norm_bwd_part_kernel(const T *__rest
             red_1[threadIdx.x * VEC + j] = a1[j];
             red_x[threadIdx.x * VEC + j] = ax[j];
         }
-        __syncthreads();
+        add_row_lanes<VEC>(red_1, red_x, s, at, s.row_lanes);
         if (at.active && at.row_lane == 0) {
             float2 *o = part + (int64_t(blockIdx.x) + b) * s.C + at.col;
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                float u1 = 0.0f, ux = 0.0f;
-                for (int l = 0; l < s.row_lanes; ++l) {
-                    u1 += red_1[(l * s.cols + at.lane) * VEC + j];
-                    ux += red_x[(l * s.cols + at.lane) * VEC + j];
-                }
+                const float u1 = red_1[at.lane * VEC + j], ux = red_x[at.lane * VEC + j];
                 o[j] = make_float2(u1, ux);
                 t1[j] += u1;
                 tx[j] += ux;
@@ -313,111 +549,527 @@ __global__ void __launch_bounds__(kThreads) norm_bwd_part_kernel(const T *__rest
     }
 }
 
-// s1 and s2 of a sample and group from its parts.
+// sums over the `deep` rows of THREADS / wide threads each, left in the first row; wide * deep <= THREADS
+template <int THREADS> __device__ __forceinline__ double2 add_deep(double2 v, double2 *red, int wide, int deep) {
+    __syncthreads();
+    red[threadIdx.x] = v;
+    const int d = int(threadIdx.x) / wide;
+    while (deep > 1) {
+        const int half = (deep + 1) >> 1;
+        __syncthreads();
+        if (d + half < deep) {
+            red[threadIdx.x].x += red[threadIdx.x + half * wide].x;
+            red[threadIdx.x].y += red[threadIdx.x + half * wide].y;
+        }
+        deep = half;
+    }
+    __syncthreads();
+    return red[threadIdx.x];
+}
+
+// s1 and s2 of a sample and group from its parts.  With one sample its columns' sums are dbeta and dgamma too.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_bwd_stats_kernel(const float2 *__restrict__ part, const Shape s, const float *__restrict__ gamma,
-                                                                 float2 *__restrict__ sums) {
-    __shared__ double red[THREADS / 64];
+                                                                 float2 *__restrict__ sums, float *__restrict__ dgamma, float *__restrict__ dbeta) {
+    __shared__ double2 red[THREADS];
     const int64_t pairs = s.samples.count * s.G;
     for (int64_t p = blockIdx.x; p < pairs; p += gridDim.x) {
         const int64_t b = p / s.G;
-        const int g = int(p % s.G);
-        const int64_t lo = s.samples.begin(b), hi = s.samples.begin(b + 1);
-        if (hi <= lo) continue;
-        const int64_t t0 = lo / s.tile_rows, t1 = (hi - 1) / s.tile_rows;
-        const int64_t items = (t1 - t0 + 1) * s.group_width;
-        double u1 = 0.0, ux = 0.0;
-        for (int64_t i = threadIdx.x; i < items; i += THREADS) {
-            const int c = g * s.group_width + int(i % s.group_width);
-            const float2 v = part[(t0 + i / s.group_width + b) * s.C + c];
-            const double w = gamma ? gamma[c] : 1.0f;
-            u1 += w * v.x;
-            ux += w * v.y;
+        const int c0 = int(p % s.G) * s.group_width;
+        const Merge<THREADS> m(s, b);
+        if (m.hi <= m.lo) continue;
+        double2 all = {0.0, 0.0};
+        for (int k0 = 0; k0 < s.group_width; k0 += m.wide) {
+            const int c = c0 + k0 + m.k;
+            const bool there = k0 + m.k < s.group_width;
+            double2 u = {0.0, 0.0};
+            if (there) m.tiles(s, part, b, c, [&](double, float2 v) { u.x += v.x; u.y += v.y; });
+            if (dgamma || dbeta) {
+                u = add_deep<THREADS>(u, red, m.wide, m.deep);
+                if (there && m.d == 0) {
+                    if (dbeta) dbeta[c] = float(u.x);
+                    if (dgamma) dgamma[c] = float(u.y);
+                } else u = {0.0, 0.0};
+            }
+            const double w = there ? gamma ? gamma[c] : 1.0f : 0.0;
+            if (there) { all.x += w * u.x; all.y += w * u.y; }
         }
-        u1 = team_sum<THREADS>(u1, red);
-        ux = team_sum<THREADS>(ux, red);
-        const double n = double(hi - lo) * s.group_width;
-        if (threadIdx.x == 0) sums[p] = make_float2(float(u1 / n), float(ux / n));
+        all = team_sum<THREADS>(all, red);
+        const double n = double(m.hi - m.lo) * s.group_width;
+        if (threadIdx.x == 0 && sums) sums[p] = make_float2(float(all.x / n), float(all.y / n));
+        __syncthreads();
     }
 }
 
-// dbeta and dgamma: the sums of all tiles' totals, 16 columns and 16 row lanes a workgroup.
-__global__ void __launch_bounds__(256) norm_bwd_columns_kernel(const float2 *__restrict__ total, int64_t tiles, int C, float *__restrict__ dgamma,
-                                                               float *__restrict__ dbeta) {
-    __shared__ double red_1[256], red_x[256];
+// dbeta and dgamma: the sums of n rows of partial sums, 16 columns and 64 row lanes a workgroup.
+__global__ void __launch_bounds__(1024) norm_bwd_columns_kernel(const float2 *__restrict__ total, int64_t n, int C, float *__restrict__ dgamma,
+                                                                float *__restrict__ dbeta) {
+    __shared__ double2 red[1024];
+    constexpr int U = 4;
     const int c = int(blockIdx.x) * 16 + int(threadIdx.x & 15);
-    double u1 = 0.0, ux = 0.0;
+    double2 u = {0.0, 0.0};
     if (c < C)
-        for (int64_t t = threadIdx.x >> 4; t < tiles; t += 16) {
-            const float2 v = total[t * C + c];
-            u1 += v.x;
-            ux += v.y;
+        for (int64_t t = threadIdx.x >> 4; t < n; t += 64 * U) {
+            float2 v[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) v[k] = t + 64 * k < n ? total[(t + 64 * k) * C + c] : make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int k = 0; k < U; ++k) { u.x += v[k].x; u.y += v[k].y; }
         }
-    red_1[threadIdx.x] = u1;
-    red_x[threadIdx.x] = ux;
-    __syncthreads();
+    u = add_deep<1024>(u, red, 16, 64);
     if (threadIdx.x < 16 && c < C) {
-        for (int l = 1; l < 16; ++l) {
-            u1 += red_1[l * 16 + threadIdx.x];
-            ux += red_x[l * 16 + threadIdx.x];
-        }
-        if (dbeta) dbeta[c] = float(u1);
-        if (dgamma) dgamma[c] = float(ux);
+        if (dbeta) dbeta[c] = float(u.x);
+        if (dgamma) dgamma[c] = float(u.y);
     }
 }
 
-template <typename T, int VEC, int ACT>
-__global__ void __launch_bounds__(kThreads) norm_bwd_apply_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const Shape s,
-                                                                  const float *__restrict__ gamma, const float *__restrict__ beta,
-                                                                  const float *__restrict__ mean, const float *__restrict__ rstd,
-                                                                  const float2 *__restrict__ sums, T *__restrict__ dX, int64_t lddx) {
-    const Place<VEC> at(s);
-    if (!at.active) return;
-    const Affine<VEC> aff(s, at.col, gamma, beta);
-    for_parts(s, [&](int64_t b, int64_t row, int64_t stop) {
-        float m[VEC], r[VEC];
-        float2 u[VEC];
+template <typename T, int VEC, int ACT, bool NT, Stats STATS>
+__global__ void __launch_bounds__(512) norm_bwd_apply_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const Shape s,
+                                                             const float *__restrict__ gamma, const float *__restrict__ beta,
+                                                             const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                             const float2 *__restrict__ sums, T *__restrict__ dX, int64_t lddx, const float2 *__restrict__ part) {
+    const int col = column_of_block<VEC>(s);
+    const int64_t r0 = int64_t(blockIdx.x) * (kRows * s.row_lanes) + threadIdx.y;
+    if (STATS != kJoin && (col < 0 || r0 >= s.N)) return;
+    gnn_strip<T, VEC, NT> sx[kRows], sd[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u)
+        if (r0 + u * s.row_lanes < s.N) {
+            sx[u].load(X + (r0 + u * s.row_lanes) * ldx + col);
+            sd[u].load(dY + (r0 + u * s.row_lanes) * ldy + col);
+        }
+    const Affine<VEC> aff(s, col, gamma, beta);
+    float r[VEC], o[VEC], g[VEC], p[VEC], q[VEC];  // xh = x r + o, dX = dz g - p - xh q
+    auto fold = [&](int64_t b, const float2 (&w)[VEC]) {
+        aff.gather(s, mean, b, o);
+        aff.gather(s, rstd, b, r);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            m[j] = mean[b * s.G + aff.group[j]];
-            r[j] = rstd[b * s.G + aff.group[j]];
-            u[j] = sums[b * s.G + aff.group[j]];
+            o[j] = -o[j] * r[j];
+            g[j] = r[j] * aff.gamma[j];
+            p[j] = r[j] * w[j].x;
+            q[j] = r[j] * w[j].y;
         }
-        for (int64_t i = row + at.row_lane; i < stop; i += s.row_lanes) {
-            float x[VEC], d[VEC];
-            gnn_load_row<T, VEC>(X + i * ldx + at.col, x);
-            gnn_load_row<T, VEC>(dY + i * ldy + at.col, d);
+    };
+    float2 w[VEC];
+    if constexpr (STATS == kOne) {
+        aff.gather(s, sums, 0, w);
+        fold(0, w);
+    } else if constexpr (STATS == kJoin) {
+        const float n = float(s.N) * float(s.group_width);
+        const float2 *stat = join_tiles<VEC>(s, part, (s.N + s.tile_rows - 1) / s.tile_rows, col,
+            [&](float2 v, float, int c) {
+                const float k = gamma ? gamma[c] : 1.0f;
+                return make_float2(v.x * k, v.y * k);
+            },
+            [&](int, float2 u) { return make_float2(u.x / n, u.y / n); });
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) w[j] = stat[aff.group[j]];
+        fold(0, w);
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+        const int64_t i = r0 + u * s.row_lanes;
+        if (i >= s.N) break;
+        if constexpr (STATS == kMany) {
+            const int64_t b = sample_of_row(s, i);
+            aff.gather(s, sums, b, w);
+            fold(b, w);
+        }
+        float x[VEC], d[VEC];
+        sx[u].get(x);
+        sd[u].get(d);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float xh = x[j] * r[j] + o[j];
+            const float dz = d[j] * slope<ACT>(xh * aff.gamma[j] + aff.beta[j]);
+            x[j] = dz * g[j] - p[j] - xh * q[j];
+        }
+        gnn_store_row<T, VEC, NT>(dX + i * lddx + col, x);
+    }
+}
+
+// ---------------------------------------------------------------- samples that fit a workgroup
+
+// Vectors of a thread: 16 values, in backward of each of the two matrices
+template <typename T> __host__ __device__ constexpr int held() { return 16 / gnn_rows<T>::VEC; }
+
+// A team of threads has a sample's rows of `groups` neighbouring groups in registers: cols x lanes threads, thread (lane, row
+// lane) the vector `lane` of every lanes-th row.  The last vector of the columns may be short.
+struct Small {
+    Samples samples;
+    int C, G, K;
+    int groups;        // of a team (blockIdx.y: which); the last one may have fewer
+    int cols, lanes, team, teams;
+    int len;           // partial sums of a group: lanes x K, or x K / VEC where vectors lie inside groups
+    int team_sums;     // of a team in LDS
+};
+
+template <int VEC, bool INSIDE, typename V> struct Team {
+    int team, i, lane, row_lane, col, have, c0, groups;
+    bool active;
+    V *sums;
+    int g0, k0;  // group of the first column, and its place there
+    __device__ __forceinline__ Team(const Small &s, V *lds) {
+        team = int(threadIdx.x / unsigned(s.team));
+        i = int(threadIdx.x) - team * s.team;
+        row_lane = int(unsigned(i) / unsigned(s.cols));
+        lane = i - row_lane * s.cols;
+        c0 = int(blockIdx.y) * s.groups * s.K;
+        const int left = (s.C - c0) / s.K;
+        groups = left < s.groups ? left : s.groups;
+        col = lane * VEC;
+        have = groups * s.K - col;
+        have = have < 0 ? 0 : have < VEC ? have : VEC;
+        active = team < s.teams && row_lane < s.lanes && have > 0;
+        sums = lds + (team < s.teams ? team : 0) * s.team_sums;
+        g0 = int(unsigned(col) / unsigned(s.K));
+        k0 = col - g0 * s.K;
+    }
+    // f(j, group of column j, place of its sum)
+    template <typename F> __device__ __forceinline__ void columns(const Small &s, F f) const {
+        int g = g0, k = k0, at = g0 * s.len + row_lane * s.K + k0;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            if (j < have) f(j, g, at);
+            if constexpr (!INSIDE) {
+                ++at;
+                if (++k == s.K) {
+                    k = 0;
+                    ++g;
+                    at += s.len - s.K;
+                }
+            }
+        }
+    }
+    // the sums of every group over the team's threads' v; the places that are returned hold them until the next call.  Sixteen to one at a
+    // time; all threads of the workgroup call it together.
+    __device__ __forceinline__ const V *reduce(const Small &s, const V (&v)[VEC]) const {
+        __syncthreads();
+        if (active) {
+            if constexpr (INSIDE) {
+                V t = v[0];
+#pragma unroll
+                for (int j = 1; j < VEC; ++j) add_to(t, v[j]);
+                sums[g0 * s.len + row_lane * (s.K / VEC) + k0 / VEC] = t;
+            } else {
+                columns(s, [&](int j, int, int at) { sums[at] = v[j]; });
+            }
+        }
+        return group_sums(sums, sums + s.groups * s.len, groups, s.len, team < s.teams ? i : s.team, s.team);
+    }
+};
+
+// A thread's vectors of a sample: `mine` of them, `step` elements apart from `p` on.  The first held() are in registers; a sample of more
+// rows than the caller said is fetched again by every pass.
+template <typename T, typename P> struct Held {
+    static constexpr int VEC = gnn_rows<T>::VEC;
+    typename gnn_rows<T>::raw v[held<T>()];
+    __device__ __forceinline__ static typename gnn_rows<T>::raw one(const P &t, const T *p) {
+        if (t.have == VEC) return gnn_rows<T>::fetch(p);
+        float f[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) f[j] = j < t.have ? gnn_rows<T>::get(p + j) : 0.0f;
+        return gnn_rows<T>::pack(f);
+    }
+    __device__ __forceinline__ void fetch(const P &t, const T *p, int64_t step, int mine) {
+#pragma unroll
+        for (int k = 0; k < held<T>(); ++k)
+            if (k < mine) v[k] = one(t, p + k * step);
+    }
+    // the vector of row k, from the registers where k is a constant
+    __device__ __forceinline__ void get(int k, float (&f)[VEC]) const {
+        typename gnn_rows<T>::raw t = v[k];
+        if constexpr (VEC == 8) asm volatile("" : "+v"(t));  // unpacked again by every pass: kept unpacked it takes twice the registers
+        gnn_rows<T>::unpack(t, f);
+    }
+    __device__ __forceinline__ static void get_far(const P &t, const T *p, int64_t step, int k, float (&f)[VEC]) { gnn_rows<T>::unpack(one(t, p + k * step), f); }
+};
+template <typename T, typename P> __device__ __forceinline__ void put_row(const P &t, T *q, const float (&f)[gnn_rows<T>::VEC]) {
+    constexpr int VEC = gnn_rows<T>::VEC;
+    if (t.have == VEC) gnn_store_row<T, VEC>(q, f);
+    else
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+            if (j < t.have) gnn_rows<T>::set(q + j, f[j]);
+}
+// the sample of a team: its first row, rows, and how many of them a thread has
+struct Span {
+    int64_t lo;
+    int rows, mine;
+    bool there;
+    template <typename P> __device__ __forceinline__ Span(const Small &s, const P &t, int64_t b) {
+        there = t.team < s.teams && b < s.samples.count;
+        lo = there ? s.samples.begin(b) : 0;
+        const int64_t hi = there ? s.samples.begin(b + 1) : 0;
+        rows = hi > lo ? int(hi - lo) : 0;
+        mine = t.active && rows > t.row_lane ? (rows - t.row_lane + s.lanes - 1) / s.lanes : 0;
+    }
+};
+
+// Forward.  Mean first, then the squared distances from it, both from the registers.
+template <typename T, int ACT, bool INSIDE>
+__global__ void __launch_bounds__(1024) small_kernel(const T *X, int64_t ldx, const Small s, const float *__restrict__ gamma,
+                                                     const float *__restrict__ beta, float eps, float *__restrict__ mean, float *__restrict__ rstd,
+                                                     T *Y, int64_t ldy) {
+    extern __shared__ float small_lds[];
+    constexpr int VEC = gnn_rows<T>::VEC;
+    typedef Team<VEC, INSIDE, float> P;
+    const P t(s, small_lds);
+    float gm[VEC], bt[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        const int c = t.c0 + t.col + j;
+        gm[j] = gamma && j < t.have ? gamma[c] : 1.0f;
+        bt[j] = beta && j < t.have ? beta[c] : 0.0f;
+    }
+    const int64_t xstep = s.lanes * ldx, ystep = s.lanes * ldy;
+    for (int64_t b0 = int64_t(blockIdx.x) * s.teams; b0 < s.samples.count; b0 += int64_t(gridDim.x) * s.teams) {
+        const int64_t b = b0 + t.team;
+        const Span n(s, t, b);
+        const T *x = X + (n.lo + t.row_lane) * ldx + t.c0 + t.col;
+        Held<T, P> h;
+        h.fetch(t, x, xstep, n.mine);
+        const float inv = 1.0f / (float(n.rows > 0 ? n.rows : 1) * float(s.K));
+        // sums over the thread's rows; beyond the registers by thirty-two at a time, so that long sums do not lose bits
+        auto sum_rows = [&](float (&a)[VEC], auto term) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) a[j] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < held<T>(); ++k)
+                if (k < n.mine) {
+                    float f[VEC];
+                    h.get(k, f);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) a[j] += term(f[j], j);
+                }
+#pragma clang loop unroll(disable)
+            for (int k0 = held<T>(); k0 < n.mine; k0 += 32) {
+                float part[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) part[j] = 0.0f;
+#pragma clang loop unroll(disable)
+                for (int k = k0; k < k0 + 32 && k < n.mine; ++k) {
+                    float f[VEC];
+                    h.get_far(t, x, xstep, k, f);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) part[j] += term(f[j], j);
+                }
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) a[j] += part[j];
+            }
+        };
+        float a[VEC], m[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) m[j] = 0.0f;
+        sum_rows(a, [](float f, int) { return f; });
+        const float *sum = t.reduce(s, a);
+        t.columns(s, [&](int j, int g, int) { m[j] = sum[g] * inv; });
+        if (n.there)
+            for (int g = t.i; g < t.groups; g += s.team) mean[b * s.G + int(blockIdx.y) * s.groups + g] = sum[g] * inv;
+        sum_rows(a, [&](float f, int j) { return (f - m[j]) * (f - m[j]); });
+        sum = t.reduce(s, a);
+        t.columns(s, [&](int j, int g, int) { a[j] = (1.0f / sqrtf(sum[g] * inv + eps)) * gm[j]; });
+        if (n.there)
+            for (int g = t.i; g < t.groups; g += s.team) rstd[b * s.G + int(blockIdx.y) * s.groups + g] = 1.0f / sqrtf(sum[g] * inv + eps);
+        T *y = Y + (n.lo + t.row_lane) * ldy + t.c0 + t.col;
+        auto write = [&](int k, float (&f)[VEC]) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) f[j] = activate<ACT>((f[j] - m[j]) * a[j] + bt[j]);
+            put_row<T>(t, y + k * ystep, f);
+        };
+#pragma unroll
+        for (int k = 0; k < held<T>(); ++k)
+            if (k < n.mine) {
+                float f[VEC];
+                h.get(k, f);
+                write(k, f);
+            }
+#pragma clang loop unroll(disable)
+        for (int k = held<T>(); k < n.mine; ++k) {
+            float f[VEC];
+            h.get_far(t, x, xstep, k, f);
+            write(k, f);
+        }
+    }
+}
+
+// Backward.  A workgroup adds up its samples' column sums for dbeta and dgamma and leaves them in its row of `part`.  In fp32 the registers
+// of X and dY take xh and dz, so that the activation's derivative is formed once; bf16 pairs are unpacked twice.
+template <typename T, int ACT, bool INSIDE>
+__global__ void __launch_bounds__(512) small_bwd_kernel(const T *X, int64_t ldx, const T *dY, int64_t ldy, const Small s,
+                                                        const float *__restrict__ gamma, const float *__restrict__ beta, const float *__restrict__ mean,
+                                                        const float *__restrict__ rstd, T *dX, int64_t lddx, float2 *__restrict__ part) {
+    extern __shared__ float2 small_lds2[];
+    constexpr int VEC = gnn_rows<T>::VEC;
+    constexpr bool KEEP = VEC == 4;
+    typedef Team<VEC, INSIDE, float2> P;
+    const P t(s, small_lds2);
+    float gm[VEC], bt[VEC];
+    float2 total[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        const int c = t.c0 + t.col + j;
+        gm[j] = gamma && j < t.have ? gamma[c] : 1.0f;
+        bt[j] = beta && j < t.have ? beta[c] : 0.0f;
+        total[j] = make_float2(0.0f, 0.0f);
+    }
+    const int64_t xstep = s.lanes * ldx, ystep = s.lanes * ldy, ostep = s.lanes * lddx;
+    for (int64_t b0 = int64_t(blockIdx.x) * s.teams; b0 < s.samples.count; b0 += int64_t(gridDim.x) * s.teams) {
+        const int64_t b = b0 + t.team;
+        const Span n(s, t, b);
+        const T *xp = X + (n.lo + t.row_lane) * ldx + t.c0 + t.col, *dp = dY + (n.lo + t.row_lane) * ldy + t.c0 + t.col;
+        Held<T, P> x, d;
+        x.fetch(t, xp, xstep, n.mine);
+        d.fetch(t, dp, ystep, n.mine);
+        float m[VEC], r[VEC];
+        float2 a[VEC];
+        const int64_t first = b * s.G + int64_t(blockIdx.y) * s.groups;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            m[j] = r[j] = 0.0f;
+            a[j] = make_float2(0.0f, 0.0f);
+        }
+        if (n.mine)
+            t.columns(s, [&](int j, int g, int) {
+                m[j] = mean[first + g];
+                r[j] = rstd[first + g];
+            });
+        // x, dY -> xh, dz
+        auto turn = [&](float (&f)[VEC], float (&g)[VEC]) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const float xh = (x[j] - m[j]) * r[j];
-                const float dz = d[j] * slope<ACT>(xh * aff.gamma[j] + aff.beta[j]);
-                x[j] = r[j] * (dz * aff.gamma[j] - u[j].x - xh * u[j].y);
+                f[j] = (f[j] - m[j]) * r[j];
+                g[j] *= slope<ACT>(f[j] * gm[j] + bt[j]);
             }
-            gnn_store_row<T, VEC>(dX + i * lddx + at.col, x);
+        };
+        auto add = [&](float2 (&to)[VEC], const float (&f)[VEC], const float (&g)[VEC]) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                to[j].x += g[j];
+                to[j].y += g[j] * f[j];
+            }
+        };
+#pragma unroll
+        for (int k = 0; k < held<T>(); ++k)
+            if (k < n.mine) {
+                float f[VEC], g[VEC];
+                x.get(k, f);
+                d.get(k, g);
+                turn(f, g);
+                add(a, f, g);
+                if constexpr (KEEP) {
+                    x.v[k] = gnn_rows<T>::pack(f);
+                    d.v[k] = gnn_rows<T>::pack(g);
+                }
+            }
+#pragma clang loop unroll(disable)
+        for (int k0 = held<T>(); k0 < n.mine; k0 += 32) {
+            float2 some[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) some[j] = make_float2(0.0f, 0.0f);
+#pragma clang loop unroll(disable)
+            for (int k = k0; k < k0 + 32 && k < n.mine; ++k) {
+                float f[VEC], g[VEC];
+                x.get_far(t, xp, xstep, k, f);
+                d.get_far(t, dp, ystep, k, g);
+                turn(f, g);
+                add(some, f, g);
+            }
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) { a[j].x += some[j].x; a[j].y += some[j].y; }
         }
-    });
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            total[j].x += a[j].x;
+            total[j].y += a[j].y;
+            a[j].x *= gm[j];
+            a[j].y *= gm[j];
+        }
+        if (!dX) continue;  // the same for the whole launch
+        const float2 *sum = t.reduce(s, a);
+        const float inv = 1.0f / (float(n.rows > 0 ? n.rows : 1) * float(s.K));
+        t.columns(s, [&](int j, int g, int) { a[j] = make_float2(sum[g].x * inv, sum[g].y * inv); });
+        T *o = dX + (n.lo + t.row_lane) * lddx + t.c0 + t.col;
+        auto write = [&](int k, float (&f)[VEC], const float (&g)[VEC]) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) f[j] = r[j] * (g[j] * gm[j] - a[j].x - f[j] * a[j].y);
+            put_row<T>(t, o + k * ostep, f);
+        };
+#pragma unroll
+        for (int k = 0; k < held<T>(); ++k)
+            if (k < n.mine) {
+                float f[VEC], g[VEC];
+                x.get(k, f);
+                d.get(k, g);
+                if constexpr (!KEEP) turn(f, g);
+                write(k, f, g);
+            }
+#pragma clang loop unroll(disable)
+        for (int k = held<T>(); k < n.mine; ++k) {
+            float f[VEC], g[VEC];
+            x.get_far(t, xp, xstep, k, f);
+            d.get_far(t, dp, ystep, k, g);
+            turn(f, g);
+            write(k, f, g);
+        }
+    }
+    if (!part) return;  // the same for the whole launch
+    // the column sums of all teams and row lanes: units of cols * VEC places
+    const int width = s.cols * VEC;
+    int units = s.teams * s.lanes;
+    const int unit = t.team * s.lanes + t.row_lane;
+    const bool in = t.team < s.teams && t.row_lane < s.lanes;
+    __syncthreads();
+    if (in)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) small_lds2[unit * width + t.lane * VEC + j] = total[j];
+    while (units > 1) {
+        const int half = (units + 1) >> 1;
+        __syncthreads();
+        if (in && unit + half < units)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                float2 &w = small_lds2[unit * width + t.lane * VEC + j];
+                const float2 u = small_lds2[(unit + half) * width + t.lane * VEC + j];
+                w.x += u.x;
+                w.y += u.y;
+            }
+        units = half;
+    }
+    if (in && unit == 0)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+            if (j < t.have) part[int64_t(blockIdx.x) * s.C + t.c0 + t.col + j] = small_lds2[t.lane * VEC + j];
 }
 
 // ---------------------------------------------------------------- host
 
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-// A tile has at least about 4096 values, and there are at most kMaxTiles of them.
-int64_t tile_rows_of(int64_t N, int64_t C) {
-    const int64_t least = C < 1024 ? 4096 / C : 4;
-    const int64_t even = (N + kMaxTiles - 1) / kMaxTiles;
-    return even > least ? even : least;
-}
-
 struct Layout {
-    int64_t tile_rows, tiles, part_off, total_off, sums_off, bytes;
+    int64_t tile_rows, tiles, map_off, total_off, sums_off, bytes;
+    bool joined;  // one sample, few tiles: two launches
 };
 
+// One sample of up to 64 K values for each of the 64 (wide rows: fewer) tiles whose partial sums every writing workgroup can join: tiles of at
+// least 16 K values.  Else tiles of at least 4 K values, at most kMaxTiles of them.
 Layout layout_of(int64_t N, int64_t C, int64_t G, int64_t B, bool backward) {
     Layout L{};
-    L.tile_rows = tile_rows_of(N, C);
+    const int64_t most = kJoined / C < 64 ? kJoined / C : 64;
+    L.joined = B == 1 && C <= 1024 && N * C <= most * 65536;
+    if (L.joined) {
+        int64_t tiles = (N * C + 16383) / 16384;
+        tiles = tiles < most ? tiles : most;
+        L.tile_rows = (N + tiles - 1) / tiles;
+    } else {
+        const int64_t least = C < 1024 ? 4096 / C : 4, even = (N + kMaxTiles - 1) / kMaxTiles;
+        L.tile_rows = even > least ? even : least;
+    }
     L.tiles = (N + L.tile_rows - 1) / L.tile_rows;
     int64_t off = round_up((L.tiles + B) * C * int64_t(sizeof(float2)), 256);
+    L.map_off = off;
+    if (B > 1) off += round_up(N * 4, 256);
     if (backward) {
         L.total_off = off;
         if (B > 1) off += round_up(L.tiles * C * int64_t(sizeof(float2)), 256);
@@ -433,7 +1085,7 @@ int check_norm(int64_t N, int64_t C, int64_t G, int64_t B, const void *sample_pt
     o = *opts;
     if (o.dtype != GNN_F32 && o.dtype != GNN_BF16) return GNN_ERR_INVALID_ARG;
     if (o.act < GNN_ACT_NONE || o.act > GNN_ACT_SILU) return GNN_ERR_INVALID_ARG;
-    if (N < 0 || C < 0 || B < 0 || G <= 0 || N > INT64_MAX / 2 || C > (1 << 24) || B > INT32_MAX || N > INT32_MAX) return GNN_ERR_INVALID_ARG;
+    if (N < 0 || C < 0 || B < 0 || G <= 0 || C > (1 << 24) || B > INT32_MAX || N > INT32_MAX) return GNN_ERR_INVALID_ARG;
     if (C % G) return GNN_ERR_INVALID_ARG;
     if (!(o.eps >= 0.0f)) return GNN_ERR_INVALID_ARG;
     if (N > 0 && (B == 0 || (!sample_ptr && N % B))) return GNN_ERR_INVALID_ARG;
@@ -444,64 +1096,206 @@ int check_norm(int64_t N, int64_t C, int64_t G, int64_t B, const void *sample_pt
     return GNN_OK;
 }
 
-Shape shape_of(int64_t N, int64_t C, int64_t G, int64_t B, const void *sample_ptr, const gnn_norm_opts &o, const Layout &L, int vec, dim3 *grid) {
+struct Call {
+    const void *X, *dY, *sample_ptr;
+    const float *gamma, *beta;
+    float *mean, *rstd;
+    void *out;  // Y or dX
+    float *dgamma, *dbeta;
+    int64_t N, C, G, B;
+    gnn_norm_opts o;
+    Layout L;
+    bool backward;
+    bool past_caches;  // more data than the last-level cache keeps until it is read again
+    Samples samples() const { return Samples{sample_ptr, o.ptr_is_64, sample_ptr ? 0 : N / B, B, N}; }
+    hipStream_t stream() const { return static_cast<hipStream_t>(o.stream); }
+    char *scratch(int64_t off) const { return static_cast<char *>(o.workspace) + off; }
+};
+
+// Rows of `cols` vectors that fill whole wavefronts best, in workgroups of about 256 threads.
+int row_lanes_of(int cols) {
+    int best = 1;
+    double share = 0.0;
+    for (int r = 1; r * cols <= kBlockMost || r == 1; ++r) {
+        const double full = double(r * cols) / double(round_up(r * cols, 64));
+        if (full >= share - 0.02) {
+            best = r;
+            if (full > share) share = full;
+        }
+    }
+    return best;
+}
+
+Shape shape_of(const Call &c, int vec, bool writes, dim3 *grid, dim3 *block) {
     Shape s{};
-    s.samples.ptr = sample_ptr;
-    s.samples.is_64 = o.ptr_is_64;
-    s.samples.count = B;
-    s.samples.rows = sample_ptr ? 0 : N / B;
-    s.samples.N = N;
-    s.N = N;
-    s.C = int(C);
-    s.G = int(G);
-    s.group_width = int(C / G);
-    s.tile_rows = L.tile_rows;
-    const int64_t vecs = (C + vec - 1) / vec, chunks = (vecs + kThreads - 1) / kThreads;
+    s.samples = c.samples();
+    s.N = c.N;
+    s.C = int(c.C);
+    s.G = int(c.G);
+    s.group_width = int(c.C / c.G);
+    s.tile_rows = c.L.tile_rows;
+    s.sample_of = c.sample_ptr && c.B > 1 ? reinterpret_cast<int32_t *>(c.scratch(c.L.map_off)) : nullptr;
+    const int64_t vecs = (c.C + vec - 1) / vec, chunks = (vecs + kThreads - 1) / kThreads;
     s.cols = int((vecs + chunks - 1) / chunks);
-    s.row_lanes = kThreads / s.cols;
-    *grid = dim3(unsigned(L.tiles), unsigned(chunks));
+    if (writes) {
+        s.row_lanes = row_lanes_of(s.cols);
+        *block = dim3(unsigned(s.cols), unsigned(s.row_lanes));
+        *grid = dim3(unsigned((c.N + kRows * s.row_lanes - 1) / (kRows * s.row_lanes)), unsigned(chunks));
+    } else {
+        const int threads = c.L.joined ? kJoinedThreads : kThreads;
+        s.row_lanes = threads / s.cols;
+        *block = dim3(unsigned(threads));
+        *grid = dim3(unsigned(c.L.tiles), unsigned(chunks));
+    }
     return s;
 }
 
-template <typename T, int VEC>
-int norm_fwd(const T *X, const float *gamma, const float *beta, T *Y, float *mean, float *rstd, Shape s, dim3 grid, const gnn_norm_opts &o, const Layout &L) {
-    hipStream_t stream = static_cast<hipStream_t>(o.stream);
-    float2 *part = static_cast<float2 *>(o.workspace);
-    norm_part_kernel<T, VEC><<<grid, kThreads, 0, stream>>>(X, o.ldx, s, part);
-    const int64_t pairs = s.samples.count * s.G;
-    if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(part, s, o.eps, mean, rstd);
-    else norm_stats_kernel<64><<<unsigned(pairs < 65536 ? pairs : 65536), 64, 0, stream>>>(part, s, o.eps, mean, rstd);
-    if (o.act == GNN_ACT_RELU) norm_apply_kernel<T, VEC, GNN_ACT_RELU><<<grid, kThreads, 0, stream>>>(X, o.ldx, s, gamma, beta, mean, rstd, Y, o.ldy);
-    else if (o.act == GNN_ACT_SILU) norm_apply_kernel<T, VEC, GNN_ACT_SILU><<<grid, kThreads, 0, stream>>>(X, o.ldx, s, gamma, beta, mean, rstd, Y, o.ldy);
-    else norm_apply_kernel<T, VEC, GNN_ACT_NONE><<<grid, kThreads, 0, stream>>>(X, o.ldx, s, gamma, beta, mean, rstd, Y, o.ldy);
-    GNN_HIP_TRY(hipGetLastError());
-    return GNN_OK;
-}
-
-template <typename T, int VEC, int ACT>
-int norm_bwd(const T *X, const float *gamma, const float *beta, const float *mean, const float *rstd, const T *dY, T *dX, float *dgamma, float *dbeta,
-             Shape s, dim3 grid, const gnn_norm_opts &o, const Layout &L) {
-    hipStream_t stream = static_cast<hipStream_t>(o.stream);
-    char *ws = static_cast<char *>(o.workspace);
-    float2 *part = reinterpret_cast<float2 *>(ws), *sums = reinterpret_cast<float2 *>(ws + L.sums_off);
-    float2 *total = s.samples.count > 1 ? reinterpret_cast<float2 *>(ws + L.total_off) : nullptr;
-    norm_bwd_part_kernel<T, VEC, ACT><<<grid, kThreads, 0, stream>>>(X, o.ldx, dY, o.ldy, s, gamma, beta, mean, rstd, part, total);
-    if (dgamma || dbeta)
-        norm_bwd_columns_kernel<<<unsigned((s.C + 15) / 16), 256, 0, stream>>>(total ? total : part, L.tiles, s.C, dgamma, dbeta);
-    if (dX) {
-        const int64_t pairs = s.samples.count * s.G;
-        if (pairs < 4096) norm_bwd_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(part, s, gamma, sums);
-        else norm_bwd_stats_kernel<64><<<unsigned(pairs < 65536 ? pairs : 65536), 64, 0, stream>>>(part, s, gamma, sums);
-        norm_bwd_apply_kernel<T, VEC, ACT><<<grid, kThreads, 0, stream>>>(X, o.ldx, dY, o.ldy, s, gamma, beta, mean, rstd, sums, dX, o.lddx);
+template <typename T, int VEC, int ACT, bool NT> int run_tiles(const Call &c) {
+    dim3 grid, threads, out_grid, out_threads;
+    const Shape s = shape_of(c, VEC, false, &grid, &threads), w = shape_of(c, VEC, true, &out_grid, &out_threads);
+    const T *X = static_cast<const T *>(c.X), *dY = static_cast<const T *>(c.dY);
+    T *out = static_cast<T *>(c.out);
+    hipStream_t stream = c.stream();
+    float2 *part = reinterpret_cast<float2 *>(c.scratch(0));
+    const int64_t pairs = c.B * c.G;
+    const unsigned many = unsigned(pairs < 65536 ? pairs : 65536);
+    const size_t lds = size_t(threads.x) * VEC * 2 * sizeof(float);
+    // what join_tiles keeps: the sums of every row lane, and a sixteenth
+    const size_t values = size_t(w.row_lanes) * size_t(c.C), join = (values + c.G * ((values / c.G + 15) / 16)) * sizeof(float2);
+    if (!c.backward) {
+        if (c.L.joined) {
+            norm_part_kernel<T, VEC, false, kJoinedThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part);
+            norm_apply_kernel<T, VEC, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, part, c.o.eps);
+        } else {
+            norm_part_kernel<T, VEC, NT, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part);
+            if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd);
+            else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd);
+            else norm_stats_kernel<64><<<many, 64, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd);
+            auto *apply = c.B == 1 ? norm_apply_kernel<T, VEC, ACT, NT, kOne> : norm_apply_kernel<T, VEC, ACT, NT, kMany>;
+            apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, nullptr, 0.0f);
+        }
+    } else {
+        float2 *sums = c.out ? reinterpret_cast<float2 *>(c.scratch(c.L.sums_off)) : nullptr;
+        float2 *total = c.B > 1 && (c.dgamma || c.dbeta) ? reinterpret_cast<float2 *>(c.scratch(c.L.total_off)) : nullptr;
+        if (c.L.joined) {
+            norm_bwd_part_kernel<T, VEC, ACT, false, kJoinedThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, nullptr);
+            if (c.dgamma || c.dbeta) norm_bwd_columns_kernel<<<unsigned((c.C + 15) / 16), 1024, 0, stream>>>(part, c.L.tiles, int(c.C), c.dgamma, c.dbeta);
+            if (c.out)
+                norm_bwd_apply_kernel<T, VEC, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, dY, c.o.ldy, w, c.gamma, c.beta, c.mean, c.rstd,
+                                                                                                     nullptr, out, c.o.lddx, part);
+        } else {
+            norm_bwd_part_kernel<T, VEC, ACT, NT, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, total);
+            float *dgamma = c.B == 1 ? c.dgamma : nullptr, *dbeta = c.B == 1 ? c.dbeta : nullptr;
+            if (sums || dgamma || dbeta) {
+                if (pairs <= 512) norm_bwd_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(part, s, c.gamma, sums, dgamma, dbeta);
+                else if (pairs < 4096) norm_bwd_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(part, s, c.gamma, sums, dgamma, dbeta);
+                else norm_bwd_stats_kernel<64><<<many, 64, 0, stream>>>(part, s, c.gamma, sums, dgamma, dbeta);
+            }
+            if (total) norm_bwd_columns_kernel<<<unsigned((c.C + 15) / 16), 1024, 0, stream>>>(total, c.L.tiles, int(c.C), c.dgamma, c.dbeta);
+            if (c.out) {
+                auto *apply = c.B == 1 ? norm_bwd_apply_kernel<T, VEC, ACT, NT, kOne> : norm_bwd_apply_kernel<T, VEC, ACT, NT, kMany>;
+                apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, dY, c.o.ldy, w, c.gamma, c.beta, c.mean, c.rstd, sums, out, c.o.lddx, nullptr);
+            }
+        }
     }
     GNN_HIP_TRY(hipGetLastError());
     return GNN_OK;
 }
 
-template <typename T, int VEC, typename... A> int norm_bwd_act(const gnn_norm_opts &o, A... a) {
-    if (o.act == GNN_ACT_RELU) return norm_bwd<T, VEC, GNN_ACT_RELU>(a...);
-    if (o.act == GNN_ACT_SILU) return norm_bwd<T, VEC, GNN_ACT_SILU>(a...);
-    return norm_bwd<T, VEC, GNN_ACT_NONE>(a...);
+// Whether samples of up to `rows` rows fit a workgroup, and how.  With few samples a team has one group, or as many as make 16
+// columns (64 bytes of a row), so that there are more workgroups; with many all groups that fit.
+struct SmallPlan {
+    Small s;
+    dim3 grid;
+    int threads;
+    size_t lds;
+    bool inside;
+};
+bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
+    const int64_t rows = c.sample_ptr ? c.o.max_sample_rows : c.N / c.B;
+    if (rows <= 0) return false;
+    const int64_t K = c.C / c.G;
+    auto fits = [&](int64_t groups) {
+        const int64_t cols = (groups * K + vec - 1) / vec;
+        return cols <= most && rows <= held * (most / cols);
+    };
+    int64_t groups = c.G;
+    if (c.B < 256) {
+        const int64_t least = (16 + K - 1) / K, even = (c.G * c.B + 255) / 256;  // 256 teams
+        groups = least > even ? least : even;
+        groups = groups < c.G ? groups : c.G;
+    }
+    while (groups > 1 && !fits(groups)) groups = (groups + 1) / 2;
+    if (!fits(groups)) return false;
+    const int64_t cols = (groups * K + vec - 1) / vec;
+    int64_t lanes = (rows + held - 1) / held;
+    // Ragged samples: the registers have room for one and a half times the mean, if that takes less than the longest; the few rows
+    // beyond are fetched again.  Four wavefronts then, one on every SIMD: workgroups of six leave half of the places free.
+    const int64_t mean = (c.N + c.B - 1) / c.B;
+    if (c.sample_ptr && cols * lanes > kThreads && held * (kThreads / cols) * 2 >= 3 * mean) lanes = kThreads / cols;
+    Small &s = p.s;
+    s = Small{};
+    s.samples = c.samples();
+    s.C = int(c.C);
+    s.G = int(c.G);
+    s.K = int(K);
+    s.groups = int(groups);
+    s.cols = int(cols);
+    s.lanes = int(lanes);
+    s.team = int(round_up(cols * lanes, 16) < most ? round_up(cols * lanes, 16) : cols * lanes);
+    s.teams = s.team < kThreads ? kThreads / s.team : 1;
+    p.inside = K % vec == 0;
+    s.len = int(lanes * (p.inside ? K / vec : K));
+    s.team_sums = int(groups) * (s.len + (s.len + 15) / 16);
+    p.threads = int(round_up(s.team * s.teams, 64));
+    const int64_t blocks = (c.B + s.teams - 1) / s.teams;
+    p.grid = dim3(unsigned(c.backward && blocks > 1024 ? 1024 : blocks), unsigned((c.G + groups - 1) / groups));
+    size_t values = size_t(s.teams) * s.team_sums;
+    if (c.backward) {
+        const size_t columns = size_t(s.teams) * s.lanes * s.cols * vec;
+        values = 2 * (values > columns ? values : columns);
+    }
+    p.lds = values * sizeof(float);
+    return p.grid.y <= 65535 && p.lds <= 65536;
+}
+
+template <typename T, int ACT, bool INSIDE> int run_small(const Call &c, const SmallPlan &p) {
+    const T *X = static_cast<const T *>(c.X);
+    hipStream_t stream = c.stream();
+    if (!c.backward) {
+        small_kernel<T, ACT, INSIDE><<<p.grid, p.threads, p.lds, stream>>>(X, c.o.ldx, p.s, c.gamma, c.beta, c.o.eps, c.mean, c.rstd, static_cast<T *>(c.out),
+                                                                           c.o.ldy);
+    } else {
+        float2 *part = c.dgamma || c.dbeta ? reinterpret_cast<float2 *>(c.scratch(0)) : nullptr;
+        small_bwd_kernel<T, ACT, INSIDE><<<p.grid, p.threads, p.lds, stream>>>(X, c.o.ldx, static_cast<const T *>(c.dY), c.o.ldy, p.s, c.gamma, c.beta, c.mean,
+                                                                               c.rstd, static_cast<T *>(c.out), c.o.lddx, part);
+        if (part) norm_bwd_columns_kernel<<<unsigned((c.C + 15) / 16), 1024, 0, stream>>>(part, p.grid.x, int(c.C), c.dgamma, c.dbeta);
+    }
+    GNN_HIP_TRY(hipGetLastError());
+    return GNN_OK;
+}
+
+template <typename T, int ACT> int run_act(const Call &c) {
+    constexpr int V = gnn_rows<T>::VEC;
+    SmallPlan p;
+    if (small_plan(c, V, held<T>(), c.backward ? 512 : 1024, p)) return p.inside ? run_small<T, ACT, true>(c, p) : run_small<T, ACT, false>(c, p);
+    if (c.C < V) return run_tiles<T, 1, ACT, false>(c);
+    return c.past_caches ? run_tiles<T, V, ACT, true>(c) : run_tiles<T, V, ACT, false>(c);
+}
+
+template <typename T> int run(const Call &c) {
+    (void)hipGetLastError();
+    if (c.o.act == GNN_ACT_RELU) return run_act<T, GNN_ACT_RELU>(c);
+    if (c.o.act == GNN_ACT_SILU) return run_act<T, GNN_ACT_SILU>(c);
+    return run_act<T, GNN_ACT_NONE>(c);
+}
+
+int run(Call &c) {
+    c.L = layout_of(c.N, c.C, c.G, c.B, c.backward);
+    if (!c.o.workspace || c.o.workspace_bytes < c.L.bytes || reinterpret_cast<uintptr_t>(c.o.workspace) % 16) return GNN_ERR_INVALID_ARG;
+    const int64_t size = c.o.dtype == GNN_F32 ? 4 : 2;
+    c.past_caches = c.N * c.C * size > (int64_t(256) << 20);
+    return c.o.dtype == GNN_F32 ? run<float>(c) : run<gnn_bf16>(c);
 }
 
 __global__ void __launch_bounds__(256) norm_zero_kernel(float *__restrict__ a, float *__restrict__ b, int64_t n) {
@@ -520,63 +1314,53 @@ extern "C" GNN_API int64_t gnn_group_norm_workspace_bytes(int64_t N, int64_t C, 
 
 extern "C" GNN_API int gnn_group_norm_fwd(const void *X, const float *gamma, const float *beta, const void *sample_ptr, void *Y, float *mean, float *rstd,
                                           int64_t N, int64_t C, int64_t G, int64_t B, const gnn_norm_opts *opts) {
-    gnn_norm_opts o;
-    const int rc = check_norm(N, C, G, B, sample_ptr, opts, o);
+    Call c{};
+    const int rc = check_norm(N, C, G, B, sample_ptr, opts, c.o);
     if (rc != GNN_OK) return rc;
     if (N == 0 || C == 0) return GNN_OK;
     if (!X || !Y || !mean || !rstd || X == Y) return GNN_ERR_INVALID_ARG;
-    const Layout L = layout_of(N, C, G, B, false);
-    if (!o.workspace || o.workspace_bytes < L.bytes || reinterpret_cast<uintptr_t>(o.workspace) % 16) return GNN_ERR_INVALID_ARG;
-    (void)hipGetLastError();
-    dim3 grid;
-    if (o.dtype == GNN_F32) {
-        const float *x = static_cast<const float *>(X);
-        float *y = static_cast<float *>(Y);
-        if (C >= 4) { const Shape s = shape_of(N, C, G, B, sample_ptr, o, L, 4, &grid); return norm_fwd<float, 4>(x, gamma, beta, y, mean, rstd, s, grid, o, L); }
-        const Shape s = shape_of(N, C, G, B, sample_ptr, o, L, 1, &grid);
-        return norm_fwd<float, 1>(x, gamma, beta, y, mean, rstd, s, grid, o, L);
-    }
-    const gnn_bf16 *x = static_cast<const gnn_bf16 *>(X);
-    gnn_bf16 *y = static_cast<gnn_bf16 *>(Y);
-    if (C >= 8) { const Shape s = shape_of(N, C, G, B, sample_ptr, o, L, 8, &grid); return norm_fwd<gnn_bf16, 8>(x, gamma, beta, y, mean, rstd, s, grid, o, L); }
-    const Shape s = shape_of(N, C, G, B, sample_ptr, o, L, 1, &grid);
-    return norm_fwd<gnn_bf16, 1>(x, gamma, beta, y, mean, rstd, s, grid, o, L);
+    c.X = X;
+    c.sample_ptr = sample_ptr;
+    c.gamma = gamma;
+    c.beta = beta;
+    c.mean = mean;
+    c.rstd = rstd;
+    c.out = Y;
+    c.N = N;
+    c.C = C;
+    c.G = G;
+    c.B = B;
+    return run(c);
 }
 
 extern "C" GNN_API int gnn_group_norm_bwd(const void *X, const float *gamma, const float *beta, const float *mean, const float *rstd, const void *dY,
                                           const void *sample_ptr, void *dX, float *dgamma, float *dbeta, int64_t N, int64_t C, int64_t G, int64_t B,
                                           const gnn_norm_opts *opts) {
-    gnn_norm_opts o;
-    const int rc = check_norm(N, C, G, B, sample_ptr, opts, o);
+    Call c{};
+    const int rc = check_norm(N, C, G, B, sample_ptr, opts, c.o);
     if (rc != GNN_OK) return rc;
     if (C == 0 || (!dX && !dgamma && !dbeta)) return GNN_OK;
-    hipStream_t stream = static_cast<hipStream_t>(o.stream);
-    (void)hipGetLastError();
     if (N == 0) {
-        if (dgamma || dbeta) norm_zero_kernel<<<64, 256, 0, stream>>>(dgamma, dbeta, C);
+        (void)hipGetLastError();
+        if (dgamma || dbeta) norm_zero_kernel<<<64, 256, 0, static_cast<hipStream_t>(opts->stream)>>>(dgamma, dbeta, C);
         GNN_HIP_TRY(hipGetLastError());
         return GNN_OK;
     }
     if (!X || !dY || !mean || !rstd || dX == X || dX == dY) return GNN_ERR_INVALID_ARG;
-    const Layout L = layout_of(N, C, G, B, true);
-    if (!o.workspace || o.workspace_bytes < L.bytes || reinterpret_cast<uintptr_t>(o.workspace) % 16) return GNN_ERR_INVALID_ARG;
-    dim3 grid;
-    if (o.dtype == GNN_F32) {
-        const float *x = static_cast<const float *>(X), *dy = static_cast<const float *>(dY);
-        float *dx = static_cast<float *>(dX);
-        if (C >= 4) {
-            const Shape s = shape_of(N, C, G, B, sample_ptr, o, L, 4, &grid);
-            return norm_bwd_act<float, 4>(o, x, gamma, beta, mean, rstd, dy, dx, dgamma, dbeta, s, grid, o, L);
-        }
-        const Shape s = shape_of(N, C, G, B, sample_ptr, o, L, 1, &grid);
-        return norm_bwd_act<float, 1>(o, x, gamma, beta, mean, rstd, dy, dx, dgamma, dbeta, s, grid, o, L);
-    }
-    const gnn_bf16 *x = static_cast<const gnn_bf16 *>(X), *dy = static_cast<const gnn_bf16 *>(dY);
-    gnn_bf16 *dx = static_cast<gnn_bf16 *>(dX);
-    if (C >= 8) {
-        const Shape s = shape_of(N, C, G, B, sample_ptr, o, L, 8, &grid);
-        return norm_bwd_act<gnn_bf16, 8>(o, x, gamma, beta, mean, rstd, dy, dx, dgamma, dbeta, s, grid, o, L);
-    }
-    const Shape s = shape_of(N, C, G, B, sample_ptr, o, L, 1, &grid);
-    return norm_bwd_act<gnn_bf16, 1>(o, x, gamma, beta, mean, rstd, dy, dx, dgamma, dbeta, s, grid, o, L);
+    c.X = X;
+    c.dY = dY;
+    c.sample_ptr = sample_ptr;
+    c.gamma = gamma;
+    c.beta = beta;
+    c.mean = const_cast<float *>(mean);
+    c.rstd = const_cast<float *>(rstd);
+    c.out = dX;
+    c.dgamma = dgamma;
+    c.dbeta = dbeta;
+    c.N = N;
+    c.C = C;
+    c.G = G;
+    c.B = B;
+    c.backward = true;
+    return run(c);
 }
