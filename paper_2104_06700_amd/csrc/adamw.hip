@@ -13,7 +13,8 @@
 // random).  The random bits are a hash of seed, step, tensor and element.  v > 0 is never held as 0, which would divide m by eps.
 //
 // The tensors' descriptors are kernel arguments: no copy of them, no allocation, at most kTensors per launch.  A workgroup has
-// kChunk neighbouring elements of one tensor, a wavefront 256 at a time, the elements of a scale.
+// kChunk neighbouring elements of one tensor and ends with them; its loads are all issued before the first is waited for.  A
+// scale's 256 elements are 64 lanes of four (fp32) or 32 of eight (bf16), whose maximum is formed by lane permutations.
 #include "common.h"
 #include "rows.h"
 
@@ -39,10 +40,11 @@ struct Tensor {
     uint32_t salt;    // of the random bits
     float decay;      // 1 - lr wd
     int32_t first;    // workgroup that begins it
-    int32_t flags;    // 1: bf16, 2: 8-bit states
+    int32_t flags;    // 1: bf16, 2: 8-bit states, 4: a master copy
 };
 struct Step {
     Tensor t[kTensors];
+    int32_t first[kTensors];  // t[].first side by side
     int32_t count;
     float b1, c1, b2, c2, rate, root, eps;  // c = 1 - b, rate = lr / (1 - b1^t), root = 1 / sqrt(1 - b2^t)
     const float *grad_scale;
@@ -63,39 +65,45 @@ __device__ __forceinline__ float wave_max(float v) {
     return v;
 }
 
-// four numbers to the nearest; not finite ones become NaN
-__device__ __forceinline__ uint32_t code_nearest(const float (&x)[4], float factor) {
+// four numbers to the nearest; not finite ones become NaN (odd: there may be some)
+__device__ __forceinline__ uint32_t code_nearest(const float (&x)[4], float factor, bool odd) {
     int w = 0;
     w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * factor, x[1] * factor, w, false);
     w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * factor, x[3] * factor, w, true);
+    if (odd)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (!finite(x[j])) w |= 0x7F << (8 * j);
+        for (int j = 0; j < 4; ++j)
+            if (!finite(x[j])) w |= 0x7F << (8 * j);
     return uint32_t(w);
 }
 
 // four numbers x >= 0, up or down by their random bits.  From 2^-6 on, the 20 bits are added to the 20 of the mantissa that go;
 // below, numbers are multiples of 2^-9.
-__device__ __forceinline__ uint32_t code_random(const float (&v)[4], float factor, uint64_t element, uint32_t salt) {
+__device__ __forceinline__ uint32_t code_random(const float (&v)[4], float factor, uint64_t element, uint32_t salt, bool odd) {
     uint32_t w = 0;
+    const uint32_t least = factor > 0.0f ? 1 : 0;  // for what is above 0
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        float x = v[j] * factor;
-        x = x < kTop ? x : kTop;
+        const float x = fminf(v[j] * factor, kTop);
         const uint32_t bits = random_bits(element + j, salt);
         uint32_t c = x >= 0x1p-6f ? ((__float_as_uint(x) + bits) >> 20) - (120u << 3) : uint32_t(x * 512.0f + float(bits) * 0x1p-20f);
-        if (v[j] > 0.0f && factor > 0.0f && c == 0) c = 1;
-        if (!finite(v[j])) c = 0x7F;
+        const uint32_t low = v[j] > 0.0f ? least : 0;
+        c = c > low ? c : low;
         w |= c << (8 * j);
     }
+    if (odd)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (!finite(v[j])) w = (w & ~(0xFFu << (8 * j))) | (0x7Fu << (8 * j));
     return w;
 }
 
-template <typename T, bool EIGHT, bool WHOLE>
+// Any four elements, one by one.
+template <typename T, bool EIGHT>
 __device__ __forceinline__ void update(const Step &s, const Tensor &t, int64_t i, float gs) {
     // elements i .. i + 3 of the tensor, or as many of them as there are
     const int64_t left = t.n - i;
-    const int have = WHOLE ? 4 : left < 0 ? 0 : left < 4 ? int(left) : 4;
+    const int have = left < 0 ? 0 : left < 4 ? int(left) : 4;
     const T *param = static_cast<const T *>(t.param);
     const T *grad = static_cast<const T *>(t.grad);
     float p[4], g[4], m[4], v[4];
@@ -142,8 +150,8 @@ __device__ __forceinline__ void update(const Step &s, const Tensor &t, int64_t i
         m_top = wave_max(m_top);
         v_top = wave_max(v_top);
         const float mf = m_top >= kTiny ? kTop / m_top : 0.0f, vf = v_top >= kTiny ? kTop / v_top : 0.0f;
-        mc = code_nearest(m, mf);
-        vc = code_random(v, vf, uint64_t(i), t.salt);
+        mc = code_nearest(m, mf, true);
+        vc = code_random(v, vf, uint64_t(i), t.salt, true);
         if ((threadIdx.x & 63) == 0 && have) {
             t.m_scale[i / kBlock] = m_top >= kTiny ? m_top / kTop : 0.0f;
             t.v_scale[i / kBlock] = v_top >= kTiny ? v_top / kTop : 0.0f;
@@ -164,23 +172,209 @@ __device__ __forceinline__ void update(const Step &s, const Tensor &t, int64_t i
     }
 }
 
-template <typename T, bool EIGHT> __device__ __forceinline__ void update_chunk(const Step &s, const Tensor &t, int64_t begin, float gs) {
-    for (int k = 0; k < kChunk; k += kThreads * 4) {
-        const int64_t i = begin + k + int64_t(threadIdx.x) * 4;
-        update<T, EIGHT, false>(s, t, i, gs);
+// ---- whole chunks
+
+typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+
+// the largest of 64 lanes' values (0 is the least); with HALF of lanes 0 - 31 and of 32 - 63
+template <bool HALF> __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+#define GNN_DPP_MAX(ctrl, rows)                                                                                    \
+    {                                                                                                             \
+        const uint32_t o = uint32_t(__builtin_amdgcn_update_dpp(0, int(v), ctrl, rows, 0xf, false));               \
+        v = o > v ? o : v;                                                                                        \
+    }
+    GNN_DPP_MAX(0x111, 0xf)  // row_shr:1, 2, 4, 8: the last of 16 lanes has their largest
+    GNN_DPP_MAX(0x112, 0xf)
+    GNN_DPP_MAX(0x114, 0xf)
+    GNN_DPP_MAX(0x118, 0xf)
+    GNN_DPP_MAX(0x142, 0xa)  // row_bcast:15 into rows 1 and 3
+    if constexpr (HALF) {
+        const uint32_t lo = uint32_t(__builtin_amdgcn_readlane(int(v), 31)), hi = uint32_t(__builtin_amdgcn_readlane(int(v), 63));
+        return (threadIdx.x & 32) ? hi : lo;
+    } else {
+        GNN_DPP_MAX(0x143, 0xc)  // row_bcast:31 into rows 2 and 3
+        return uint32_t(__builtin_amdgcn_readlane(int(v), 63));
+    }
+#undef GNN_DPP_MAX
+}
+
+// E neighbouring fp32 values
+template <int E> struct Floats {
+    gnn_f32x4 v[E / 4];
+    __device__ __forceinline__ void load(const float *p) {
+#pragma unroll
+        for (int k = 0; k < E / 4; ++k) v[k] = __builtin_nontemporal_load(reinterpret_cast<const gnn_f32x4 *>(p) + k);
+    }
+    __device__ __forceinline__ float get(int j) const { return v[j / 4][j % 4]; }
+    __device__ __forceinline__ void set(int j, float x) { v[j / 4][j % 4] = x; }
+    __device__ __forceinline__ void store(float *p) const {
+#pragma unroll
+        for (int k = 0; k < E / 4; ++k) __builtin_nontemporal_store(v[k], reinterpret_cast<gnn_f32x4 *>(p) + k);
+    }
+};
+// E neighbouring bytes
+template <int E> struct Codes {
+    uint32_t w[E / 4];
+    __device__ __forceinline__ void load(const void *at) {
+        const uint8_t *p = static_cast<const uint8_t *>(at);
+        if constexpr (E == 4) w[0] = __builtin_nontemporal_load(reinterpret_cast<const u32_any *>(p));
+        else {
+            const u32x2_any t = __builtin_nontemporal_load(reinterpret_cast<const u32x2_any *>(p));
+            w[0] = t.x;
+            w[1] = t.y;
+        }
+    }
+    __device__ __forceinline__ void store(void *at) const {
+        uint8_t *p = static_cast<uint8_t *>(at);
+        if constexpr (E == 4) __builtin_nontemporal_store(w[0], reinterpret_cast<u32_any *>(p));
+        else __builtin_nontemporal_store(u32x2_any{w[0], w[1]}, reinterpret_cast<u32x2_any *>(p));
+    }
+};
+__device__ __forceinline__ void decode(uint32_t w, float scale, float (&x)[4]) {
+    x[0] = __builtin_amdgcn_cvt_f32_fp8(int(w), 0) * scale;
+    x[1] = __builtin_amdgcn_cvt_f32_fp8(int(w), 1) * scale;
+    x[2] = __builtin_amdgcn_cvt_f32_fp8(int(w), 2) * scale;
+    x[3] = __builtin_amdgcn_cvt_f32_fp8(int(w), 3) * scale;
+}
+
+// kChunk elements from `begin` on, all inside the tensor.
+template <typename T, bool EIGHT, bool MASTER> __device__ __forceinline__ void update_chunk(const Step &s, const Tensor &t, int64_t begin, float gs) {
+    constexpr int E = gnn_rows<T>::VEC, U = kChunk / (kThreads * E);
+    typedef typename gnn_rows<T>::raw raw;
+    raw p[MASTER ? 1 : U], g[U];
+    Floats<E> master[MASTER ? U : 1], m32[EIGHT ? 1 : U], v32[EIGHT ? 1 : U];
+    Codes<E> m8[EIGHT ? U : 1], v8[EIGHT ? U : 1];
+    float ms[U], vs[U];
+    const int64_t i0 = begin + int64_t(threadIdx.x) * E;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = i0 + u * (kThreads * E);
+        g[u] = __builtin_nontemporal_load(reinterpret_cast<const raw *>(static_cast<const T *>(t.grad) + i));
+        if constexpr (MASTER) master[u].load(t.master + i);
+        else p[u] = __builtin_nontemporal_load(reinterpret_cast<const raw *>(static_cast<const T *>(t.param) + i));
+        if constexpr (EIGHT) {
+            m8[u].load(static_cast<const uint8_t *>(t.m) + i);
+            v8[u].load(static_cast<const uint8_t *>(t.v) + i);
+            ms[u] = t.m_scale[i / kBlock];
+            vs[u] = t.v_scale[i / kBlock];
+        } else {
+            m32[u].load(static_cast<const float *>(t.m) + i);
+            v32[u].load(static_cast<const float *>(t.v) + i);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = i0 + u * (kThreads * E);
+        float gf[E], pf[E], m[E], v[E];
+        gnn_rows<T>::unpack(g[u], gf);
+        if constexpr (!MASTER) gnn_rows<T>::unpack(p[u], pf);
+        uint32_t m_top = 0, v_top = 0;
+#pragma unroll
+        for (int q = 0; q < E / 4; ++q) {
+            float mo[4], vo[4];
+            if constexpr (EIGHT) {
+                decode(m8[u].w[q], ms[u], mo);
+                decode(v8[u].w[q], vs[u], vo);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int j = 4 * q + r;
+                if constexpr (!EIGHT) {
+                    mo[r] = m32[u].get(j);
+                    vo[r] = v32[u].get(j);
+                }
+                const float po = MASTER ? master[u].get(j) : pf[j];
+                const float x = gf[j] * gs;
+                m[j] = mo[r] * s.b1 + x * s.c1;
+                v[j] = vo[r] * s.b2 + (x * x) * s.c2;
+                // (both instructions are good to a unit in the last place, but for roots below 2^-63, which eps covers)
+                pf[j] = po * t.decay - s.rate * (m[j] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[j]) * s.root + s.eps));
+                if constexpr (EIGHT) {
+                    const uint32_t mb = __float_as_uint(m[j]) & 0x7FFFFFFFu, vb = __float_as_uint(v[j]) & 0x7FFFFFFFu;
+                    m_top = mb > m_top ? mb : m_top;
+                    v_top = vb > v_top ? vb : v_top;
+                }
+            }
+        }
+        if constexpr (MASTER) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) master[u].set(j, pf[j]);
+            master[u].store(t.master + i);
+        }
+        __builtin_nontemporal_store(gnn_rows<T>::pack(pf), reinterpret_cast<raw *>(static_cast<T *>(t.param) + i));
+        if constexpr (EIGHT) {
+            m_top = lanes_max<E == 8>(m_top);
+            v_top = lanes_max<E == 8>(v_top);
+            const bool odd = m_top >= 0x7F800000u || v_top >= 0x7F800000u;  // something is not finite: the largest of the others counts
+            if (odd) {
+                m_top = v_top = 0;
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    const uint32_t mb = __float_as_uint(m[j]) & 0x7FFFFFFFu, vb = __float_as_uint(v[j]) & 0x7FFFFFFFu;
+                    if (mb < 0x7F800000u && mb > m_top) m_top = mb;
+                    if (vb < 0x7F800000u && vb > v_top) v_top = vb;
+                }
+            }
+            if (__ballot(odd)) {  // (all lanes take part in the permutations; the others' values are what they have)
+                const uint32_t mt = lanes_max<E == 8>(m_top), vt = lanes_max<E == 8>(v_top);
+                m_top = mt;
+                v_top = vt;
+            }
+            const float mt = __uint_as_float(m_top), vt = __uint_as_float(v_top);
+            const float mf = mt >= kTiny ? kTop / mt : 0.0f, vf = vt >= kTiny ? kTop / vt : 0.0f;
+#pragma unroll
+            for (int q = 0; q < E / 4; ++q) {
+                const float mq[4] = {m[4 * q], m[4 * q + 1], m[4 * q + 2], m[4 * q + 3]}, vq[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                m8[u].w[q] = code_nearest(mq, mf, odd);
+                v8[u].w[q] = code_random(vq, vf, uint64_t(i + 4 * q), t.salt, odd);
+            }
+            m8[u].store(static_cast<uint8_t *>(t.m) + i);
+            v8[u].store(static_cast<uint8_t *>(t.v) + i);
+            if ((threadIdx.x & (kBlock / E - 1)) == 0) {
+                t.m_scale[i / kBlock] = mt >= kTiny ? mt / kTop : 0.0f;
+                t.v_scale[i / kBlock] = vt >= kTiny ? vt / kTop : 0.0f;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                m32[u].set(j, m[j]);
+                v32[u].set(j, v[j]);
+            }
+            m32[u].store(static_cast<float *>(t.m) + i);
+            v32[u].store(static_cast<float *>(t.v) + i);
+        }
     }
 }
 
+template <typename T, bool EIGHT> __device__ __forceinline__ void update_rest(const Step &s, const Tensor &t, int64_t begin, float gs) {
+    for (int k = 0; k < kChunk && begin + k < t.n; k += kThreads * 4) update<T, EIGHT>(s, t, begin + k + int64_t(threadIdx.x) * 4, gs);
+}
+
 __global__ void __launch_bounds__(kThreads) adamw_kernel(const Step s) {
-    int k = 0;
-    while (k + 1 < s.count && int(blockIdx.x) >= s.t[k + 1].first) ++k;
+    // the last tensor that begins at this workgroup or before
+    const int lane = int(threadIdx.x & 63);
+    const bool before = lane < s.count && s.first[lane < kTensors ? lane : 0] <= int(blockIdx.x);
+    const int k = __popcll(__ballot(before)) - 1;
     const Tensor &t = s.t[k];
     const int64_t begin = int64_t(int(blockIdx.x) - t.first) * kChunk;
     const float gs = s.grad_scale ? *s.grad_scale : 1.0f;
-    if (t.flags == 0) update_chunk<float, false>(s, t, begin, gs);
-    else if (t.flags == 1) update_chunk<gnn_bf16, false>(s, t, begin, gs);
-    else if (t.flags == 2) update_chunk<float, true>(s, t, begin, gs);
-    else update_chunk<gnn_bf16, true>(s, t, begin, gs);
+    // the last elements, and an eps so small that quotients near the ends of the range matter: one by one
+    if (begin + kChunk > t.n || s.eps < 0x1p-40f) {
+        if ((t.flags & 3) == 0) update_rest<float, false>(s, t, begin, gs);
+        else if ((t.flags & 3) == 1) update_rest<gnn_bf16, false>(s, t, begin, gs);
+        else if ((t.flags & 3) == 2) update_rest<float, true>(s, t, begin, gs);
+        else update_rest<gnn_bf16, true>(s, t, begin, gs);
+        return;
+    }
+    switch (t.flags) {
+        case 0: update_chunk<float, false, false>(s, t, begin, gs); break;
+        case 1: update_chunk<gnn_bf16, false, false>(s, t, begin, gs); break;
+        case 2: update_chunk<float, true, false>(s, t, begin, gs); break;
+        case 3: update_chunk<gnn_bf16, true, false>(s, t, begin, gs); break;
+        case 5: update_chunk<gnn_bf16, false, true>(s, t, begin, gs); break;
+        default: update_chunk<gnn_bf16, true, true>(s, t, begin, gs); break;
+    }
 }
 
 bool misaligned(const void *p, int64_t to) { return reinterpret_cast<uintptr_t>(p) % uintptr_t(to) != 0; }
@@ -248,8 +442,8 @@ extern "C" GNN_API int gnn_adamw_step(const gnn_adamw_tensor *tensors, int64_t n
         t.n = d.n;
         t.salt = uint32_t(o.seed) + uint32_t(o.step) * 0x3C6EF373u + uint32_t(k) * 0xBB67AE85u;
         t.decay = float(1.0 - o.lr * double(d.weight_decay));
-        t.first = int32_t(blocks);
-        t.flags = (d.dtype == GNN_BF16 ? 1 : 0) | (d.state_bits == 8 ? 2 : 0);
+        t.first = s.first[s.count - 1] = int32_t(blocks);
+        t.flags = (d.dtype == GNN_BF16 ? 1 : 0) | (d.state_bits == 8 ? 2 : 0) | (d.master ? 4 : 0);
         blocks += more;
     }
     return flush();
