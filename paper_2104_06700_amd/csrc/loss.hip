@@ -3,33 +3,53 @@
 // For a row x of C scores with label t:   m = max_j x_j,  s = sum_j exp(x_j - m),  loss = log s + m - x_t,
 //     dx_j = w (exp(x_j - m) / s - [j = t]),   w = scale, or scale / number of labelled rows.
 // A row without a label is not read; its gradient is 0.  Every row is read once and stays in registers, 16 bytes a lane: LANES lanes
-// of a wavefront (or a whole workgroup) have a row.  Rows wider than that are read twice.
+// of a wavefront (or a whole workgroup) have a row, and a workgroup ends with its rows.  Rows wider than that are read twice.
 //
 // Three launches: the labelled rows of every piece of the label array are counted, the rows are done with the sum of these
-// counts, and the workgroups' sums of row losses are added in their order; results do not depend on timing.
+// counts, and the workgroups' sums of row losses are added in their order; results do not depend on timing.  Up to kCountHere rows
+// every workgroup counts by itself, which is one launch less.
 #include "common.h"
 #include "rows.h"
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kCountBlocks = 256;   // partial counts
-constexpr int kLossBlocks = 4096;   // partial losses at most
+constexpr int kCountBlocks = 256;       // partial counts
+constexpr int64_t kCountHere = 16384;
+constexpr int kLossBlocks = 65536;      // partial losses at most
 
 struct Labels {
     const void *p;
     int is_64;
     int64_t C;
     // the label of a row, -1 where it has none
-    __device__ __forceinline__ int64_t at(int64_t r) const {
-        const int64_t t = is_64 ? static_cast<const int64_t *>(p)[r] : int64_t(static_cast<const int32_t *>(p)[r]);
+    __device__ __forceinline__ int at(int64_t r) const {
+        if (is_64) {
+            const int64_t t = static_cast<const int64_t *>(p)[r];
+            return t >= 0 && t < C ? int(t) : -1;
+        }
+        const int t = static_cast<const int32_t *>(p)[r];
         return t >= 0 && t < C ? t : -1;
     }
 };
 
-template <int THREADS, typename V, typename F> __device__ __forceinline__ V group_reduce(V v, V *red, F f) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = f(v, __shfl_xor(v, d));
+// ctrl: a permutation of the 16 lanes of a row
+template <int CTRL> __device__ __forceinline__ float from_lane(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// f over LANES neighbouring lanes, in all of them
+template <int LANES, typename F> __device__ __forceinline__ float lanes_reduce(float v, F f) {
+    if constexpr (LANES >= 2) v = f(v, from_lane<0xB1>(v));    // the other of a pair
+    if constexpr (LANES >= 4) v = f(v, from_lane<0x4E>(v));    // the other pair of four
+    if constexpr (LANES >= 8) v = f(v, from_lane<0x141>(v));   // mirrored in eight: the other four
+    if constexpr (LANES >= 16) v = f(v, from_lane<0x140>(v));  // mirrored in sixteen: the other eight
+    if constexpr (LANES >= 32) v = f(v, __shfl_xor(v, 16));
+    if constexpr (LANES >= 64) v = f(v, __shfl_xor(v, 32));
+    return v;
+}
+// f over a workgroup, in all of its threads; red: a value for every wavefront
+template <int THREADS, typename F> __device__ __forceinline__ float group_reduce(float v, float *red, F f) {
+    v = lanes_reduce<64>(v, f);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -38,144 +58,181 @@ template <int THREADS, typename V, typename F> __device__ __forceinline__ V grou
     for (int i = 1; i < THREADS / 64; ++i) v = f(v, red[i]);
     return v;
 }
+struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };  // (a NaN is met by the sum)
+
+template <int THREADS> __device__ __forceinline__ int group_count(int n, int *red) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
+    __syncthreads();
+    n = red[0];
+#pragma unroll
+    for (int i = 1; i < THREADS / 64; ++i) n += red[i];
+    return n;
+}
 
 __global__ void __launch_bounds__(kThreads) count_labels_kernel(const Labels labels, int64_t N, int32_t *__restrict__ counts) {
     __shared__ int red[kThreads / 64];
     const int64_t each = (N + gridDim.x - 1) / gridDim.x, r0 = each * blockIdx.x, r1 = r0 + each < N ? r0 + each : N;
     int n = 0;
     for (int64_t r = r0 + threadIdx.x; r < r1; r += kThreads) n += labels.at(r) >= 0;
-    n = group_reduce<kThreads>(n, red, [](int a, int b) { return a + b; });
+    n = group_count<kThreads>(n, red);
     if (threadIdx.x == 0) counts[blockIdx.x] = n;
 }
 
+enum Weight { kSum, kMeanCounted, kMeanHere };
 // scale, or scale / number of labelled rows; the same in every thread of a workgroup
-__device__ __forceinline__ float row_weight(const int32_t *counts, float scale) {
-    if (!counts) return scale;
-    __shared__ int red[kThreads / 64];
-    static_assert(kCountBlocks == kThreads, "one count a thread");
-    const int n = group_reduce<kThreads>(counts[threadIdx.x], red, [](int a, int b) { return a + b; });
+template <int WEIGHT, int THREADS> __device__ __forceinline__ float row_weight(const Labels &labels, int64_t N, const int32_t *counts, float scale, int *red) {
+    if constexpr (WEIGHT == kSum) return scale;
+    int n = 0;
+    if constexpr (WEIGHT == kMeanCounted) {
+        static_assert(kCountBlocks <= THREADS, "one count a thread");
+        if (threadIdx.x < kCountBlocks) n = counts[threadIdx.x];
+    } else {
+        for (int64_t r = threadIdx.x; r < N; r += THREADS) n += labels.at(r) >= 0;
+    }
+    n = group_count<THREADS>(n, red);
     return scale / float(n > 1 ? n : 1);
 }
 
-// max that keeps NaN
-__device__ __forceinline__ float max_nan(float a, float b) { return a != a ? a : b != b ? b : a > b ? a : b; }
-
 // Rows in registers: LANES lanes with NV vectors of VEC elements each.  The last vector of a row ends with the row; elements that
-// it shares with the one before (or, of a lane without a vector, all) are left out of the sums.
-template <typename T, int VEC, int LANES, int NV>
-__global__ void __launch_bounds__(kThreads) xent_kernel(const T *__restrict__ X, int64_t ldx, const Labels labels, T *__restrict__ dX, int64_t ldg,
+// it shares with the one before are left out of the sum and written twice, alike.  PASSES rows a team, all fetched first.
+template <typename T, int VEC, int LANES, int NV, int PASSES, int WEIGHT, int THREADS = (LANES > kThreads ? LANES : kThreads)>
+__global__ void __launch_bounds__(THREADS) xent_kernel(const T *__restrict__ X, int64_t ldx, const Labels labels, T *__restrict__ dX, int64_t ldg,
                                                         float *__restrict__ loss_rows, const int32_t *__restrict__ counts, float scale,
                                                         float *__restrict__ loss_part, int64_t N, int C) {
-    __shared__ float red[kThreads / 64];
-    const float w = row_weight(counts, scale);
-    constexpr int ROWS = kThreads / LANES;
+    __shared__ float red[THREADS / 64];
+    __shared__ int red_n[THREADS / 64];
+    constexpr int ROWS = THREADS / LANES;
     const int lane = int(threadIdx.x) % LANES, team = int(threadIdx.x) / LANES;
-    int col[NV], skip[NV];
+    const int vecs = (C + VEC - 1) / VEC;
+    float sum = 0.0f, w = 0.0f;
+    bool weighed = false;
+    for (int64_t r0 = int64_t(blockIdx.x) * (ROWS * PASSES) + team; r0 - team < N; r0 += int64_t(gridDim.x) * (ROWS * PASSES)) {
+        int t[PASSES];
+        float xt[PASSES];
+        gnn_strip<T, VEC, false> strip[PASSES][NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int c = (lane + k * LANES) * VEC;
-        col[k] = c < C - VEC ? c : C - VEC;
-        skip[k] = c < C ? c - col[k] : VEC;
-    }
-    float sum = 0.0f;
-    for (int64_t r = int64_t(blockIdx.x) * ROWS + team; r < N; r += int64_t(gridDim.x) * ROWS) {
-        const int64_t t = labels.at(r);
-        float v[NV][VEC];
-        float loss = 0.0f;
-        if (t >= 0) {
-            float m = -__builtin_inff();
+        for (int q = 0; q < PASSES; ++q) t[q] = r0 + q * ROWS < N ? labels.at(r0 + q * ROWS) : -1;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                if (skip[k] < VEC) gnn_load_row<T, VEC>(X + r * ldx + col[k], v[k]);
+        for (int q = 0; q < PASSES; ++q)
+            if (t[q] >= 0) {
+                const T *x = X + (r0 + q * ROWS) * ldx;
 #pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    if (j >= skip[k]) m = max_nan(m, v[k][j]);
-            }
-            auto larger = [](float a, float b) { return max_nan(a, b); };
-            auto add = [](float a, float b) { return a + b; };
-            if constexpr (LANES <= 64) {
-#pragma unroll
-                for (int d = LANES / 2; d > 0; d >>= 1) m = larger(m, __shfl_xor(m, d));
-            } else m = group_reduce<kThreads>(m, red, larger);
-            float s = 0.0f, xt = 0.0f;
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    if (j < skip[k]) continue;
-                    if (col[k] + j == t) xt = v[k][j];
-                    v[k][j] = __expf(v[k][j] - m);
-                    s += v[k][j];
+                for (int k = 0; k < NV; ++k) {
+                    const int v = lane + k * LANES;
+                    if (v < vecs) strip[q][k].load(x + (v * VEC < C - VEC ? v * VEC : C - VEC));
                 }
-            if constexpr (LANES <= 64) {
-#pragma unroll
-                for (int d = LANES / 2; d > 0; d >>= 1) { s = add(s, __shfl_xor(s, d)); xt = add(xt, __shfl_xor(xt, d)); }
-            } else { s = group_reduce<kThreads>(s, red, add); xt = group_reduce<kThreads>(xt, red, add); }
-            loss = logf(s) + (m - xt);
-            const float inv = w / s;
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) v[k][j] = v[k][j] * inv - (col[k] + j == t ? w : 0.0f);
-        } else {
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) v[k][j] = 0.0f;
+                xt[q] = gnn_rows<T>::get(x + t[q]);
+            }
+        if (!weighed) {  // while the rows are under way
+            w = row_weight<WEIGHT, THREADS>(labels, N, counts, scale, red_n);
+            weighed = true;
         }
-        if (dX) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                if (skip[k] == 0) gnn_store_row<T, VEC>(dX + r * ldg + col[k], v[k]);
-                else
+        for (int q = 0; q < PASSES; ++q) {
+            const int64_t r = r0 + q * ROWS;
+            if (LANES <= 64 && r >= N) break;
+            float v[NV][VEC];
+            float loss = 0.0f;
+            if (t[q] >= 0) {
+                float m = -__builtin_inff();
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j)
-                        if (j >= skip[k]) gnn_rows<T>::set(dX + r * ldg + col[k] + j, v[k][j]);
+                for (int k = 0; k < NV; ++k)
+                    if (lane + k * LANES < vecs) {
+                        strip[q][k].get(v[k]);
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) m = fmaxf(m, v[k][j]);
+                    }
+                if constexpr (LANES <= 64) m = lanes_reduce<LANES>(m, Max());
+                else m = group_reduce<THREADS>(m, red, Max());
+                float s = 0.0f;
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if (lane + k * LANES < vecs) {
+                        const int first = (lane + k * LANES) * VEC, shared = first - (first < C - VEC ? first : C - VEC);
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) {
+                            v[k][j] = __expf(v[k][j] - m);
+                            s += j >= shared ? v[k][j] : 0.0f;
+                        }
+                    }
+                if constexpr (LANES <= 64) s = lanes_reduce<LANES>(s, Add());
+                else s = group_reduce<THREADS>(s, red, Add());
+                loss = __logf(s) + (m - xt[q]);
+                const float inv = w / s;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    const int first = (lane + k * LANES) * VEC, col = first < C - VEC ? first : C - VEC;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) v[k][j] = v[k][j] * inv - (col + j == t[q] ? w : 0.0f);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) v[k][j] = 0.0f;
+            }
+            if (dX) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    const int first = (lane + k * LANES) * VEC;
+                    if (lane + k * LANES < vecs) gnn_store_row<T, VEC, true>(dX + r * ldg + (first < C - VEC ? first : C - VEC), v[k]);
+                }
+            }
+            if (lane == 0) {
+                if (loss_rows) loss_rows[r] = loss;
+                sum += loss;
             }
         }
-        if (lane == 0) {
-            if (loss_rows) loss_rows[r] = loss;
-            sum += loss;
-        }
     }
-    sum = group_reduce<kThreads>(sum, red, [](float a, float b) { return a + b; });
+    sum = group_reduce<THREADS>(sum, red, Add());
     if (threadIdx.x == 0) loss_part[blockIdx.x] = sum * w;
 }
 
 // Rows beyond the registers: a workgroup reads its row twice, first for the running maximum and the sum of the exponentials.
-template <typename T, int VEC>
+template <typename T, int VEC, int WEIGHT>
 __global__ void __launch_bounds__(kThreads) xent_wide_kernel(const T *__restrict__ X, int64_t ldx, const Labels labels, T *__restrict__ dX, int64_t ldg,
                                                              float *__restrict__ loss_rows, const int32_t *__restrict__ counts, float scale,
                                                              float *__restrict__ loss_part, int64_t N, int64_t C) {
     __shared__ float red[kThreads / 64];
-    const float w = row_weight(counts, scale);
+    __shared__ int red_n[kThreads / 64];
+    const float w = row_weight<WEIGHT, kThreads>(labels, N, counts, scale, red_n);
     const int64_t whole = C / VEC * VEC;
     float sum = 0.0f;
     for (int64_t r = blockIdx.x; r < N; r += gridDim.x) {
-        const int64_t t = labels.at(r);
+        const int t = labels.at(r);
         const T *x = X + r * ldx;
         T *g = dX ? dX + r * ldg : nullptr;
         float loss = 0.0f, top = 0.0f, inv = 0.0f;
         if (t >= 0) {
             float m = -__builtin_inff(), s = 0.0f;
-            auto take = [&](float v) {
-                const float up = max_nan(m, v);
-                if (up != m) {  // also NaN
-                    s = m == -__builtin_inff() ? 0.0f : s * __expf(m - up);
-                    m = up;
+            // the maximum of so many, then their exponentials; before the first finite score there is nothing to scale
+            auto take = [&](const float *v, int n) {
+                float up = m;
+                for (int j = 0; j < n; ++j) up = fmaxf(up, v[j]);
+                if (up == -__builtin_inff()) {
+                    for (int j = 0; j < n; ++j) s += v[j] != v[j] ? v[j] : 0.0f;
+                    return;
                 }
-                if (m != -__builtin_inff()) s += __expf(v - m);
+                s *= m == up ? 1.0f : __expf(m - up);
+                m = up;
+                for (int j = 0; j < n; ++j) s += __expf(v[j] - m);
             };
             for (int64_t c = int64_t(threadIdx.x) * VEC; c < whole; c += int64_t(kThreads) * VEC) {
                 float v[VEC];
                 gnn_load_row<T, VEC>(x + c, v);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) take(v[j]);
+                take(v, VEC);
             }
-            if (whole + threadIdx.x < C) take(gnn_rows<T>::get(x + whole + threadIdx.x));
-            top = group_reduce<kThreads>(m, red, [](float a, float b) { return max_nan(a, b); });
-            s = group_reduce<kThreads>(m == -__builtin_inff() ? 0.0f : s * __expf(m - top), red, [](float a, float b) { return a + b; });
-            loss = logf(s) + (top - gnn_rows<T>::get(x + t));
+            if (whole + threadIdx.x < C) {
+                const float v = gnn_rows<T>::get(x + whole + threadIdx.x);
+                take(&v, 1);
+            }
+            top = group_reduce<kThreads>(m, red, Max());
+            s = group_reduce<kThreads>(m == -__builtin_inff() ? s : s * __expf(m - top), red, Add());
+            loss = __logf(s) + (top - gnn_rows<T>::get(x + t));
             inv = w / s;
         }
         if (g) {
@@ -188,7 +245,7 @@ __global__ void __launch_bounds__(kThreads) xent_wide_kernel(const T *__restrict
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) v[j] = __expf(v[j] - top) * inv - (c + j == t ? w : 0.0f);
                 }
-                gnn_store_row<T, VEC>(g + c, v);
+                gnn_store_row<T, VEC, true>(g + c, v);
             }
             if (whole + threadIdx.x < C) {
                 const int64_t c = whole + threadIdx.x;
@@ -203,18 +260,32 @@ __global__ void __launch_bounds__(kThreads) xent_wide_kernel(const T *__restrict
     if (threadIdx.x == 0) loss_part[blockIdx.x] = sum * w;
 }
 
-__global__ void __launch_bounds__(kThreads) add_losses_kernel(const float *__restrict__ part, int n, float *__restrict__ loss) {
-    __shared__ double red[kThreads / 64];
+template <int THREADS> __global__ void __launch_bounds__(THREADS) add_losses_kernel(const float *__restrict__ part, int n, float *__restrict__ loss) {
+    __shared__ double red[THREADS / 64];
     double s = 0.0;
-    for (int i = threadIdx.x; i < n; i += kThreads) s += part[i];
-    s = group_reduce<kThreads>(s, red, [](double a, double b) { return a + b; });
-    if (threadIdx.x == 0) *loss = float(s);
+    constexpr int U = 4;
+    for (int i = threadIdx.x; i < n; i += THREADS * U) {
+        float v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = i + u * THREADS < n ? part[i + u * THREADS] : 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) s += v[u];
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < THREADS / 64; ++i) s += red[i];
+        *loss = float(s);
+    }
 }
 
 struct Call {
     Labels labels;
     float *loss_rows, *loss, *part;
     int32_t *counts;
+    bool mean;
     float scale;
     int64_t N, C, ldx, ldg;
     hipStream_t stream;
@@ -225,31 +296,40 @@ int blocks_of(int64_t N, int rows) {
     return int(b < kLossBlocks ? b : kLossBlocks);
 }
 
-template <typename T, int VEC, int LANES, int NV> int launch(const T *X, T *dX, const Call &c) {
-    const int blocks = blocks_of(c.N, kThreads / LANES);
-    xent_kernel<T, VEC, LANES, NV><<<blocks, kThreads, 0, c.stream>>>(X, c.ldx, c.labels, dX, c.ldg, c.loss_rows, c.counts, c.scale, c.part, c.N, int(c.C));
+template <typename T, int VEC, int LANES, int NV, int PASSES, int WEIGHT> int launch(const T *X, T *dX, const Call &c) {
+    constexpr int threads = LANES > kThreads ? LANES : kThreads;
+    const int blocks = blocks_of(c.N, threads / LANES * PASSES);
+    xent_kernel<T, VEC, LANES, NV, PASSES, WEIGHT><<<blocks, threads, 0, c.stream>>>(X, c.ldx, c.labels, dX, c.ldg, c.loss_rows, c.counts, c.scale, c.part, c.N,
+                                                                                  int(c.C));
+    return blocks;
+}
+
+template <typename T, int WEIGHT> int rows(const T *X, T *dX, const Call &c) {
+    constexpr int V = gnn_rows<T>::VEC;
+    if (c.C < V) return launch<T, 1, 8, 1, 2, WEIGHT>(X, dX, c);
+    if (c.C <= 4 * V) return launch<T, V, 4, 1, 2, WEIGHT>(X, dX, c);
+    if (c.C <= 8 * V) return launch<T, V, 8, 1, 2, WEIGHT>(X, dX, c);
+    if (c.C <= 16 * V) return launch<T, V, 16, 1, 2, WEIGHT>(X, dX, c);
+    if (c.C <= 32 * V) return launch<T, V, 32, 1, 2, WEIGHT>(X, dX, c);
+    if (c.C <= 64 * V) return launch<T, V, 64, 1, 2, WEIGHT>(X, dX, c);
+    if (c.C <= 128 * V) return launch<T, V, 64, 2, 1, WEIGHT>(X, dX, c);
+    if (c.C <= 512 * V) return launch<T, V, 256, 2, 1, WEIGHT>(X, dX, c);
+    if (c.C <= 2048 * V) return launch<T, V, 1024, 2, 1, WEIGHT>(X, dX, c);
+    const int blocks = blocks_of(c.N, 1);
+    xent_wide_kernel<T, V, WEIGHT><<<blocks, kThreads, 0, c.stream>>>(X, c.ldx, c.labels, dX, c.ldg, c.loss_rows, c.counts, c.scale, c.part, c.N, c.C);
     return blocks;
 }
 
 template <typename T> int xent(const T *X, T *dX, const Call &c) {
-    constexpr int V = gnn_rows<T>::VEC;
-    if (c.counts) count_labels_kernel<<<kCountBlocks, kThreads, 0, c.stream>>>(c.labels, c.N, c.counts);
     int blocks;
-    if (c.C < V) blocks = launch<T, 1, 8, 1>(X, dX, c);
-    else if (c.C <= 4 * V) blocks = launch<T, V, 4, 1>(X, dX, c);
-    else if (c.C <= 8 * V) blocks = launch<T, V, 8, 1>(X, dX, c);
-    else if (c.C <= 16 * V) blocks = launch<T, V, 16, 1>(X, dX, c);
-    else if (c.C <= 32 * V) blocks = launch<T, V, 32, 1>(X, dX, c);
-    else if (c.C <= 64 * V) blocks = launch<T, V, 64, 1>(X, dX, c);
-    else if (c.C <= 128 * V) blocks = launch<T, V, 64, 2>(X, dX, c);
-    else if (c.C <= 256 * V) blocks = launch<T, V, 256, 1>(X, dX, c);
-    else if (c.C <= 512 * V) blocks = launch<T, V, 256, 2>(X, dX, c);
-    else if (c.C <= 1024 * V) blocks = launch<T, V, 256, 4>(X, dX, c);
+    if (!c.mean) blocks = rows<T, kSum>(X, dX, c);
+    else if (c.N <= kCountHere) blocks = rows<T, kMeanHere>(X, dX, c);
     else {
-        blocks = blocks_of(c.N, 1);
-        xent_wide_kernel<T, V><<<blocks, kThreads, 0, c.stream>>>(X, c.ldx, c.labels, dX, c.ldg, c.loss_rows, c.counts, c.scale, c.part, c.N, c.C);
+        count_labels_kernel<<<kCountBlocks, kThreads, 0, c.stream>>>(c.labels, c.N, c.counts);
+        blocks = rows<T, kMeanCounted>(X, dX, c);
     }
-    add_losses_kernel<<<1, kThreads, 0, c.stream>>>(c.part, blocks, c.loss);
+    if (blocks <= 1024) add_losses_kernel<256><<<1, 256, 0, c.stream>>>(c.part, blocks, c.loss);
+    else add_losses_kernel<1024><<<1, 1024, 0, c.stream>>>(c.part, blocks, c.loss);
     GNN_HIP_TRY(hipGetLastError());
     return GNN_OK;
 }
@@ -260,7 +340,7 @@ __global__ void zero_loss_kernel(float *loss) { *loss = 0.0f; }
 
 extern "C" GNN_API int64_t gnn_softmax_xent_workspace_bytes(int64_t N, int64_t C) {
     if (N <= 0 || C <= 0) return 0;
-    return kCountBlocks * 4 + kLossBlocks * 4;
+    return kCountBlocks * 4 + (N < kLossBlocks ? N : kLossBlocks) * 4;
 }
 
 extern "C" GNN_API int gnn_softmax_xent(const void *X, const void *labels, float *loss, void *dX, float *loss_rows, int64_t N, int64_t C,
@@ -285,7 +365,8 @@ extern "C" GNN_API int gnn_softmax_xent(const void *X, const void *labels, float
         return GNN_ERR_INVALID_ARG;
     Call c{};
     c.labels = Labels{labels, o.labels_is_64, C};
-    c.counts = o.reduction == GNN_LOSS_MEAN ? static_cast<int32_t *>(o.workspace) : nullptr;
+    c.mean = o.reduction == GNN_LOSS_MEAN;
+    c.counts = static_cast<int32_t *>(o.workspace);
     c.part = reinterpret_cast<float *>(static_cast<char *>(o.workspace) + kCountBlocks * 4);
     c.loss = loss;
     c.loss_rows = loss_rows;
