@@ -26,8 +26,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBlock = 256;      // elements of a scale: four a lane
-constexpr int kChunk = 4096;     // elements of a workgroup
+constexpr int kChunk = 4096, kShortChunk = 2048;  // elements of a workgroup
 constexpr int kTensors = 40;     // of a launch; 4 KB of arguments at most
+constexpr int64_t kShort = 4 << 20;  // elements below which chunks are short
 constexpr float kTop = 448.0f;
 constexpr float kTiny = 0x1p-118f;  // below it 448 / x would overflow: such a block is held as zeros
 
@@ -45,7 +46,7 @@ struct Tensor {
 struct Step {
     Tensor t[kTensors];
     int32_t first[kTensors];  // t[].first side by side
-    int32_t count;
+    int32_t count, chunk;
     float b1, c1, b2, c2, rate, root, eps;  // c = 1 - b, rate = lr / (1 - b1^t), root = 1 / sqrt(1 - b2^t)
     const float *grad_scale;
 };
@@ -98,7 +99,29 @@ __device__ __forceinline__ uint32_t code_random(const float (&v)[4], float facto
     return w;
 }
 
-// Any four elements, one by one.
+typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t u32x2_half __attribute__((ext_vector_type(2), aligned(2)));
+
+// four neighbouring elements
+__device__ __forceinline__ void load4(const float *p, float (&v)[4]) { gnn_rows<float>::unpack(gnn_rows<float>::fetch(p), v); }
+__device__ __forceinline__ void load4(const gnn_bf16 *p, float (&v)[4]) {
+    const u32x2_half t = *reinterpret_cast<const u32x2_half *>(p);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        v[2 * i] = __uint_as_float(t[i] << 16);
+        v[2 * i + 1] = __uint_as_float(t[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void store4(float *p, const float (&v)[4]) { gnn_rows<float>::put(p, gnn_rows<float>::pack(v)); }
+__device__ __forceinline__ void store4(gnn_bf16 *p, const float (&v)[4]) {
+    u32x2_half t;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) t[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(gnn_f32x2{v[2 * i], v[2 * i + 1]}, gnn_bf16x2));
+    *reinterpret_cast<u32x2_half *>(p) = t;
+}
+
+// Any four elements, or as many as the tensor has left.
 template <typename T, bool EIGHT>
 __device__ __forceinline__ void update(const Step &s, const Tensor &t, int64_t i, float gs) {
     // elements i .. i + 3 of the tensor, or as many of them as there are
@@ -110,18 +133,31 @@ __device__ __forceinline__ void update(const Step &s, const Tensor &t, int64_t i
     uint32_t mc = 0, vc = 0;
     const uint8_t *m8 = static_cast<const uint8_t *>(t.m), *v8 = static_cast<const uint8_t *>(t.v);
     const float *m32 = static_cast<const float *>(t.m), *v32 = static_cast<const float *>(t.v);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        p[j] = g[j] = m[j] = v[j] = 0.0f;
-        if (j >= have) continue;
-        p[j] = t.master ? t.master[i + j] : gnn_rows<T>::get(param + i + j);
-        g[j] = gnn_rows<T>::get(grad + i + j);
+    if (have == 4) {
+        load4(grad + i, g);
+        if (t.master) load4(t.master + i, p);
+        else load4(param + i, p);
         if constexpr (EIGHT) {
-            mc |= uint32_t(m8[i + j]) << (8 * j);
-            vc |= uint32_t(v8[i + j]) << (8 * j);
+            mc = *reinterpret_cast<const u32_any *>(m8 + i);
+            vc = *reinterpret_cast<const u32_any *>(v8 + i);
         } else {
-            m[j] = m32[i + j];
-            v[j] = v32[i + j];
+            load4(m32 + i, m);
+            load4(v32 + i, v);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            p[j] = g[j] = m[j] = v[j] = 0.0f;
+            if (j >= have) continue;
+            p[j] = t.master ? t.master[i + j] : gnn_rows<T>::get(param + i + j);
+            g[j] = gnn_rows<T>::get(grad + i + j);
+            if constexpr (EIGHT) {
+                mc |= uint32_t(m8[i + j]) << (8 * j);
+                vc |= uint32_t(v8[i + j]) << (8 * j);
+            } else {
+                m[j] = m32[i + j];
+                v[j] = v32[i + j];
+            }
         }
     }
     if constexpr (EIGHT) {
@@ -157,6 +193,18 @@ __device__ __forceinline__ void update(const Step &s, const Tensor &t, int64_t i
             t.v_scale[i / kBlock] = v_top >= kTiny ? v_top / kTop : 0.0f;
         }
     }
+    if (have == 4) {
+        store4(static_cast<T *>(t.param) + i, p);
+        if (t.master) store4(t.master + i, p);
+        if constexpr (EIGHT) {
+            *reinterpret_cast<u32_any *>(static_cast<uint8_t *>(t.m) + i) = mc;
+            *reinterpret_cast<u32_any *>(static_cast<uint8_t *>(t.v) + i) = vc;
+        } else {
+            store4(static_cast<float *>(t.m) + i, m);
+            store4(static_cast<float *>(t.v) + i, v);
+        }
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         if (j >= have) continue;
@@ -173,9 +221,6 @@ __device__ __forceinline__ void update(const Step &s, const Tensor &t, int64_t i
 }
 
 // ---- whole chunks
-
-typedef uint32_t u32_any __attribute__((aligned(1)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 
 // the largest of 64 lanes' values (0 is the least); with HALF of lanes 0 - 31 and of 32 - 63
 template <bool HALF> __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
@@ -238,9 +283,9 @@ __device__ __forceinline__ void decode(uint32_t w, float scale, float (&x)[4]) {
     x[3] = __builtin_amdgcn_cvt_f32_fp8(int(w), 3) * scale;
 }
 
-// kChunk elements from `begin` on, all inside the tensor.
-template <typename T, bool EIGHT, bool MASTER> __device__ __forceinline__ void update_chunk(const Step &s, const Tensor &t, int64_t begin, float gs) {
-    constexpr int E = gnn_rows<T>::VEC, U = kChunk / (kThreads * E);
+// CHUNK elements from `begin` on, all inside the tensor.
+template <int CHUNK, typename T, bool EIGHT, bool MASTER> __device__ __forceinline__ void update_chunk(const Step &s, const Tensor &t, int64_t begin, float gs) {
+    constexpr int E = gnn_rows<T>::VEC, U = CHUNK / (kThreads * E);
     typedef typename gnn_rows<T>::raw raw;
     raw p[MASTER ? 1 : U], g[U];
     Floats<E> master[MASTER ? U : 1], m32[EIGHT ? 1 : U], v32[EIGHT ? 1 : U];
@@ -348,19 +393,19 @@ template <typename T, bool EIGHT, bool MASTER> __device__ __forceinline__ void u
 }
 
 template <typename T, bool EIGHT> __device__ __forceinline__ void update_rest(const Step &s, const Tensor &t, int64_t begin, float gs) {
-    for (int k = 0; k < kChunk && begin + k < t.n; k += kThreads * 4) update<T, EIGHT>(s, t, begin + k + int64_t(threadIdx.x) * 4, gs);
+    for (int k = 0; k < s.chunk && begin + k < t.n; k += kThreads * 4) update<T, EIGHT>(s, t, begin + k + int64_t(threadIdx.x) * 4, gs);
 }
 
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const Step s) {
+template <int CHUNK> __global__ void __launch_bounds__(kThreads) adamw_kernel(const Step s) {
     // the last tensor that begins at this workgroup or before
     const int lane = int(threadIdx.x & 63);
     const bool before = lane < s.count && s.first[lane < kTensors ? lane : 0] <= int(blockIdx.x);
     const int k = __popcll(__ballot(before)) - 1;
     const Tensor &t = s.t[k];
-    const int64_t begin = int64_t(int(blockIdx.x) - t.first) * kChunk;
+    const int64_t begin = int64_t(int(blockIdx.x) - t.first) * CHUNK;
     const float gs = s.grad_scale ? *s.grad_scale : 1.0f;
     // the last elements, and an eps so small that quotients near the ends of the range matter: one by one
-    if (begin + kChunk > t.n || s.eps < 0x1p-40f) {
+    if (begin + CHUNK > t.n || s.eps < 0x1p-40f) {
         if ((t.flags & 3) == 0) update_rest<float, false>(s, t, begin, gs);
         else if ((t.flags & 3) == 1) update_rest<gnn_bf16, false>(s, t, begin, gs);
         else if ((t.flags & 3) == 2) update_rest<float, true>(s, t, begin, gs);
@@ -368,12 +413,12 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const Step s) {
         return;
     }
     switch (t.flags) {
-        case 0: update_chunk<float, false, false>(s, t, begin, gs); break;
-        case 1: update_chunk<gnn_bf16, false, false>(s, t, begin, gs); break;
-        case 2: update_chunk<float, true, false>(s, t, begin, gs); break;
-        case 3: update_chunk<gnn_bf16, true, false>(s, t, begin, gs); break;
-        case 5: update_chunk<gnn_bf16, false, true>(s, t, begin, gs); break;
-        default: update_chunk<gnn_bf16, true, true>(s, t, begin, gs); break;
+        case 0: update_chunk<CHUNK, float, false, false>(s, t, begin, gs); break;
+        case 1: update_chunk<CHUNK, gnn_bf16, false, false>(s, t, begin, gs); break;
+        case 2: update_chunk<CHUNK, float, true, false>(s, t, begin, gs); break;
+        case 3: update_chunk<CHUNK, gnn_bf16, true, false>(s, t, begin, gs); break;
+        case 5: update_chunk<CHUNK, gnn_bf16, false, true>(s, t, begin, gs); break;
+        default: update_chunk<CHUNK, gnn_bf16, true, true>(s, t, begin, gs); break;
     }
 }
 
@@ -399,11 +444,12 @@ extern "C" GNN_API int gnn_adamw_step(const gnn_adamw_tensor *tensors, int64_t n
     if (!opts || n_tensors < 0 || (n_tensors > 0 && !tensors)) return GNN_ERR_INVALID_ARG;
     const gnn_adamw_opts &o = *opts;
     if (o.step < 1 || !(o.lr >= 0.0) || !(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0) || !(o.eps >= 0.0)) return GNN_ERR_INVALID_ARG;
-    int64_t blocks = 0;
+    int64_t blocks = 0, elements = 0;
     for (int64_t k = 0; k < n_tensors; ++k) {
         const int rc = check_tensor(tensors[k]);
         if (rc != GNN_OK) return rc;
-        if (tensors[k].grad && (tensors[k].n + kChunk - 1) / kChunk > INT32_MAX / 2) return GNN_ERR_INVALID_ARG;
+        if (tensors[k].grad && tensors[k].n / kChunk > INT32_MAX / 4) return GNN_ERR_INVALID_ARG;
+        if (tensors[k].grad) elements += tensors[k].n < (int64_t(1) << 40) ? tensors[k].n : 0;
     }
     (void)hipGetLastError();
     Step s{};
@@ -415,9 +461,12 @@ extern "C" GNN_API int gnn_adamw_step(const gnn_adamw_tensor *tensors, int64_t n
     s.root = float(1.0 / sqrt(1.0 - pow(o.beta2, double(o.step))));
     s.eps = float(o.eps);
     s.grad_scale = o.grad_scale;
+    // few elements: shorter chunks, so that more workgroups share them
+    s.chunk = elements < kShort ? kShortChunk : kChunk;
     auto flush = [&]() -> int {
         if (s.count == 0) return GNN_OK;
-        adamw_kernel<<<unsigned(blocks), kThreads, 0, static_cast<hipStream_t>(o.stream)>>>(s);
+        auto *kernel = s.chunk == kChunk ? adamw_kernel<kChunk> : adamw_kernel<kShortChunk>;
+        kernel<<<unsigned(blocks), kThreads, 0, static_cast<hipStream_t>(o.stream)>>>(s);
         s.count = 0;
         blocks = 0;
         GNN_HIP_TRY(hipGetLastError());
@@ -426,7 +475,7 @@ extern "C" GNN_API int gnn_adamw_step(const gnn_adamw_tensor *tensors, int64_t n
     for (int64_t k = 0; k < n_tensors; ++k) {
         const gnn_adamw_tensor &d = tensors[k];
         if (d.n == 0 || !d.grad) continue;
-        const int64_t more = (d.n + kChunk - 1) / kChunk;
+        const int64_t more = (d.n + s.chunk - 1) / s.chunk;
         if (s.count == kTensors || blocks + more > INT32_MAX / 2) {
             const int rc = flush();
             if (rc != GNN_OK) return rc;

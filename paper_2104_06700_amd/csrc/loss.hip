@@ -17,19 +17,26 @@ constexpr int kThreads = 256;
 constexpr int kCountBlocks = 256;       // partial counts
 constexpr int64_t kCountHere = 16384;
 constexpr int kLossBlocks = 65536;      // partial losses at most
+constexpr int64_t kMostStride = 1 << 22;  // 128 rows of it are offsets of 32 bits
 
 struct Labels {
     const void *p;
     int is_64;
-    int64_t C;
+    unsigned classes;
     // the label of a row, -1 where it has none
     __device__ __forceinline__ int at(int64_t r) const {
         if (is_64) {
             const int64_t t = static_cast<const int64_t *>(p)[r];
-            return t >= 0 && t < C ? int(t) : -1;
+            return uint64_t(t) < classes ? int(t) : -1;
         }
         const int t = static_cast<const int32_t *>(p)[r];
-        return t >= 0 && t < C ? t : -1;
+        return unsigned(t) < classes ? t : -1;
+    }
+    // of row first + r, with a 32-bit offset
+    template <typename I> __device__ __forceinline__ int at(int64_t first, I r) const {
+        if (is_64) return at(first + int64_t(r));
+        const int t = (static_cast<const int32_t *>(p) + first)[r];
+        return unsigned(t) < classes ? t : -1;
     }
 };
 
@@ -61,10 +68,27 @@ template <int THREADS, typename F> __device__ __forceinline__ float group_reduce
 struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
 struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };  // (a NaN is met by the sum)
 
-template <int THREADS> __device__ __forceinline__ int group_count(int n, int *red) {
+__device__ __forceinline__ int wave_add(int n) {
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
-    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(n);
+}
+
+// labelled rows among r0 + threadIdx.x, every THREADS-th of them up to r1; eight loads in flight
+template <int THREADS> __device__ __forceinline__ int count_rows(const Labels &labels, int64_t r0, int64_t r1) {
+    constexpr int U = 8;
+    int n = 0;
+    for (int64_t r = r0 + threadIdx.x; r < r1; r += THREADS * U) {
+        int t[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) t[u] = r + u * THREADS < r1 ? labels.at(r + u * THREADS) : -1;
+#pragma unroll
+        for (int u = 0; u < U; ++u) n += t[u] >= 0;
+    }
+    return n;
+}
+template <int THREADS> __device__ __forceinline__ int group_count(int n, int *red) {
+    n = wave_add(n);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
     __syncthreads();
     n = red[0];
@@ -73,68 +97,72 @@ template <int THREADS> __device__ __forceinline__ int group_count(int n, int *re
     return n;
 }
 
-__global__ void __launch_bounds__(kThreads) count_labels_kernel(const Labels labels, int64_t N, int32_t *__restrict__ counts) {
-    __shared__ int red[kThreads / 64];
+__global__ void __launch_bounds__(1024) count_labels_kernel(const Labels labels, int64_t N, int32_t *__restrict__ counts) {
+    __shared__ int red[1024 / 64];
     const int64_t each = (N + gridDim.x - 1) / gridDim.x, r0 = each * blockIdx.x, r1 = r0 + each < N ? r0 + each : N;
-    int n = 0;
-    for (int64_t r = r0 + threadIdx.x; r < r1; r += kThreads) n += labels.at(r) >= 0;
-    n = group_count<kThreads>(n, red);
+    const int n = group_count<1024>(count_rows<1024>(labels, r0, r1), red);
     if (threadIdx.x == 0) counts[blockIdx.x] = n;
 }
 
 enum Weight { kSum, kMeanCounted, kMeanHere };
-// scale, or scale / number of labelled rows; the same in every thread of a workgroup
+// scale, or scale / number of labelled rows; the same in every thread of a workgroup.  Every wavefront adds up the counts: no barrier.
 template <int WEIGHT, int THREADS> __device__ __forceinline__ float row_weight(const Labels &labels, int64_t N, const int32_t *counts, float scale, int *red) {
     if constexpr (WEIGHT == kSum) return scale;
     int n = 0;
     if constexpr (WEIGHT == kMeanCounted) {
-        static_assert(kCountBlocks <= THREADS, "one count a thread");
-        if (threadIdx.x < kCountBlocks) n = counts[threadIdx.x];
-    } else {
-        for (int64_t r = threadIdx.x; r < N; r += THREADS) n += labels.at(r) >= 0;
-    }
-    n = group_count<THREADS>(n, red);
+        static_assert(kCountBlocks == 4 * 64, "four counts a lane");
+        const int4 c = reinterpret_cast<const int4 *>(counts)[threadIdx.x & 63];
+        n = wave_add((c.x + c.y) + (c.z + c.w));
+    } else n = group_count<THREADS>(count_rows<THREADS>(labels, 0, N), red);
     return scale / float(n > 1 ? n : 1);
 }
 
 // Rows in registers: LANES lanes with NV vectors of VEC elements each.  The last vector of a row ends with the row; elements that
 // it shares with the one before are left out of the sum and written twice, alike.  PASSES rows a team, all fetched first.
-template <typename T, int VEC, int LANES, int NV, int PASSES, int WEIGHT, int THREADS = (LANES > kThreads ? LANES : kThreads)>
-__global__ void __launch_bounds__(THREADS) xent_kernel(const T *__restrict__ X, int64_t ldx, const Labels labels, T *__restrict__ dX, int64_t ldg,
+// Addresses are 32-bit offsets from the workgroup's first row (wide strides go the other way): 64-bit products for every row are
+// a good part of a row's vector instructions (2.4 M rows of 47 scores, 8 % labelled: 107 -> 98 us).  Listing the labelled rows first and sharing them
+// among the teams saves instructions where labels are few and no time: 98 us, and a row per workgroup pays for its barriers (177 -> 194).
+template <typename T, int VEC, int LANES, int NV, int PASSES, int WEIGHT>
+__global__ void __launch_bounds__(kThreads) xent_kernel(const T *__restrict__ X, int64_t ldx, const Labels labels, T *__restrict__ dX, int64_t ldg,
                                                         float *__restrict__ loss_rows, const int32_t *__restrict__ counts, float scale,
                                                         float *__restrict__ loss_part, int64_t N, int C) {
-    __shared__ float red[THREADS / 64];
-    __shared__ int red_n[THREADS / 64];
-    constexpr int ROWS = THREADS / LANES;
-    const int lane = int(threadIdx.x) % LANES, team = int(threadIdx.x) / LANES;
+    __shared__ float red[kThreads / 64];
+    __shared__ int red_n[kThreads / 64];
+    constexpr int ROWS = kThreads / LANES;
+    const int lane = int(threadIdx.x) % LANES, team = LANES == kThreads ? 0 : int(threadIdx.x) / LANES;
+    const unsigned sx = unsigned(ldx), sg = unsigned(ldg);
     const int vecs = (C + VEC - 1) / VEC;
+    unsigned col[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) col[k] = unsigned((lane + k * LANES) * VEC < C - VEC ? (lane + k * LANES) * VEC : C - VEC);
     float sum = 0.0f, w = 0.0f;
     bool weighed = false;
-    for (int64_t r0 = int64_t(blockIdx.x) * (ROWS * PASSES) + team; r0 - team < N; r0 += int64_t(gridDim.x) * (ROWS * PASSES)) {
+    for (int64_t b0 = int64_t(blockIdx.x) * (ROWS * PASSES); b0 < N; b0 += int64_t(gridDim.x) * (ROWS * PASSES)) {
+        const int left = N - b0 < ROWS * PASSES ? int(N - b0) : ROWS * PASSES;
+        const T *const x0 = X + b0 * ldx;
+        T *const g0 = dX ? dX + b0 * ldg : nullptr;
         int t[PASSES];
         float xt[PASSES];
         gnn_strip<T, VEC, false> strip[PASSES][NV];
 #pragma unroll
-        for (int q = 0; q < PASSES; ++q) t[q] = r0 + q * ROWS < N ? labels.at(r0 + q * ROWS) : -1;
+        for (int q = 0; q < PASSES; ++q) t[q] = team + q * ROWS < left ? labels.at(b0, unsigned(team + q * ROWS)) : -1;
 #pragma unroll
         for (int q = 0; q < PASSES; ++q)
             if (t[q] >= 0) {
-                const T *x = X + (r0 + q * ROWS) * ldx;
+                const unsigned row = unsigned(team + q * ROWS) * sx;
 #pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    const int v = lane + k * LANES;
-                    if (v < vecs) strip[q][k].load(x + (v * VEC < C - VEC ? v * VEC : C - VEC));
-                }
-                xt[q] = gnn_rows<T>::get(x + t[q]);
+                for (int k = 0; k < NV; ++k)
+                    if (lane + k * LANES < vecs) strip[q][k].load(x0 + (row + col[k]));
+                xt[q] = gnn_rows<T>::get(x0 + (row + unsigned(t[q])));
             }
         if (!weighed) {  // while the rows are under way
-            w = row_weight<WEIGHT, THREADS>(labels, N, counts, scale, red_n);
+            w = row_weight<WEIGHT, kThreads>(labels, N, counts, scale, red_n);
             weighed = true;
         }
 #pragma unroll
         for (int q = 0; q < PASSES; ++q) {
-            const int64_t r = r0 + q * ROWS;
-            if (LANES <= 64 && r >= N) break;
+            const int r = team + q * ROWS;
+            if (r >= left) break;
             float v[NV][VEC];
             float loss = 0.0f;
             if (t[q] >= 0) {
@@ -147,27 +175,42 @@ __global__ void __launch_bounds__(THREADS) xent_kernel(const T *__restrict__ X, 
                         for (int j = 0; j < VEC; ++j) m = fmaxf(m, v[k][j]);
                     }
                 if constexpr (LANES <= 64) m = lanes_reduce<LANES>(m, Max());
-                else m = group_reduce<THREADS>(m, red, Max());
+                else m = group_reduce<kThreads>(m, red, Max());
                 float s = 0.0f;
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
                     if (lane + k * LANES < vecs) {
-                        const int first = (lane + k * LANES) * VEC, shared = first - (first < C - VEC ? first : C - VEC);
+                        if constexpr (VEC == 8 && NV > 1) {
+                            strip[q][k].forget();
+                            strip[q][k].get(v[k]);
+                        }
+                        float part = 0.0f;
 #pragma unroll
                         for (int j = 0; j < VEC; ++j) {
                             v[k][j] = __expf(v[k][j] - m);
-                            s += j >= shared ? v[k][j] : 0.0f;
+                            part += v[k][j];
                         }
+                        const int over = (lane + k * LANES) * VEC - (C - VEC);  // > 0: so many elements are the vector's before, too
+                        if (over > 0) {
+                            part = 0.0f;
+#pragma unroll
+                            for (int j = 0; j < VEC; ++j) part += j >= over ? v[k][j] : 0.0f;
+                        }
+                        s += part;
                     }
                 if constexpr (LANES <= 64) s = lanes_reduce<LANES>(s, Add());
-                else s = group_reduce<THREADS>(s, red, Add());
+                else s = group_reduce<kThreads>(s, red, Add());
                 loss = __logf(s) + (m - xt[q]);
                 const float inv = w / s;
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
-                    const int first = (lane + k * LANES) * VEC, col = first < C - VEC ? first : C - VEC;
+                    const unsigned at = unsigned(t[q]) - col[k];
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) v[k][j] = v[k][j] * inv - (col + j == t[q] ? w : 0.0f);
+                    for (int j = 0; j < VEC; ++j) v[k][j] *= inv;
+                    if (at < unsigned(VEC)) {  // one vector of the row, or two that share the element
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) v[k][j] -= j == int(at) ? w : 0.0f;
+                    }
                 }
             } else {
 #pragma unroll
@@ -175,20 +218,17 @@ __global__ void __launch_bounds__(THREADS) xent_kernel(const T *__restrict__ X, 
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) v[k][j] = 0.0f;
             }
-            if (dX) {
+            if (g0) {
+                const unsigned row = unsigned(r) * sg;
 #pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    const int first = (lane + k * LANES) * VEC;
-                    if (lane + k * LANES < vecs) gnn_store_row<T, VEC, true>(dX + r * ldg + (first < C - VEC ? first : C - VEC), v[k]);
-                }
+                for (int k = 0; k < NV; ++k)
+                    if (lane + k * LANES < vecs) gnn_store_row<T, VEC, true>(g0 + (row + col[k]), v[k]);
             }
-            if (lane == 0) {
-                if (loss_rows) loss_rows[r] = loss;
-                sum += loss;
-            }
+            if (loss_rows && lane == 0) loss_rows[b0 + r] = loss;
+            sum += loss;
         }
     }
-    sum = group_reduce<THREADS>(sum, red, Add());
+    sum = group_reduce<kThreads>(lane == 0 ? sum : 0.0f, red, Add());
     if (threadIdx.x == 0) loss_part[blockIdx.x] = sum * w;
 }
 
@@ -260,17 +300,20 @@ __global__ void __launch_bounds__(kThreads) xent_wide_kernel(const T *__restrict
     if (threadIdx.x == 0) loss_part[blockIdx.x] = sum * w;
 }
 
-template <int THREADS> __global__ void __launch_bounds__(THREADS) add_losses_kernel(const float *__restrict__ part, int n, float *__restrict__ loss) {
+// All loads of the up to kLossBlocks values are in flight together.
+template <int THREADS, int U> __global__ void __launch_bounds__(THREADS) add_losses_kernel(const float *__restrict__ part, int n, float *__restrict__ loss) {
     __shared__ double red[THREADS / 64];
-    double s = 0.0;
-    constexpr int U = 4;
-    for (int i = threadIdx.x; i < n; i += THREADS * U) {
-        float v[U];
+    static_assert(THREADS * U * 4 <= kLossBlocks, "one round");
+    float4 v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = i + u * THREADS < n ? part[i + u * THREADS] : 0.0f;
-#pragma unroll
-        for (int u = 0; u < U; ++u) s += v[u];
+    for (int u = 0; u < U; ++u) {
+        const int i = (u * THREADS + int(threadIdx.x)) * 4;
+        if (i + 3 < n) v[u] = *reinterpret_cast<const float4 *>(part + i);
+        else v[u] = make_float4(i < n ? part[i] : 0.0f, i + 1 < n ? part[i + 1] : 0.0f, i + 2 < n ? part[i + 2] : 0.0f, 0.0f);
     }
+    double s = 0.0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) s += (double(v[u].x) + double(v[u].y)) + (double(v[u].z) + double(v[u].w));
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
@@ -297,24 +340,27 @@ int blocks_of(int64_t N, int rows) {
 }
 
 template <typename T, int VEC, int LANES, int NV, int PASSES, int WEIGHT> int launch(const T *X, T *dX, const Call &c) {
-    constexpr int threads = LANES > kThreads ? LANES : kThreads;
-    const int blocks = blocks_of(c.N, threads / LANES * PASSES);
-    xent_kernel<T, VEC, LANES, NV, PASSES, WEIGHT><<<blocks, threads, 0, c.stream>>>(X, c.ldx, c.labels, dX, c.ldg, c.loss_rows, c.counts, c.scale, c.part, c.N,
+    const int blocks = blocks_of(c.N, kThreads / LANES * PASSES);
+    xent_kernel<T, VEC, LANES, NV, PASSES, WEIGHT><<<blocks, kThreads, 0, c.stream>>>(X, c.ldx, c.labels, dX, c.ldg, c.loss_rows, c.counts, c.scale, c.part, c.N,
                                                                                   int(c.C));
     return blocks;
 }
 
 template <typename T, int WEIGHT> int rows(const T *X, T *dX, const Call &c) {
     constexpr int V = gnn_rows<T>::VEC;
-    if (c.C < V) return launch<T, 1, 8, 1, 2, WEIGHT>(X, dX, c);
-    if (c.C <= 4 * V) return launch<T, V, 4, 1, 2, WEIGHT>(X, dX, c);
-    if (c.C <= 8 * V) return launch<T, V, 8, 1, 2, WEIGHT>(X, dX, c);
-    if (c.C <= 16 * V) return launch<T, V, 16, 1, 2, WEIGHT>(X, dX, c);
-    if (c.C <= 32 * V) return launch<T, V, 32, 1, 2, WEIGHT>(X, dX, c);
-    if (c.C <= 64 * V) return launch<T, V, 64, 1, 2, WEIGHT>(X, dX, c);
-    if (c.C <= 128 * V) return launch<T, V, 64, 2, 1, WEIGHT>(X, dX, c);
-    if (c.C <= 512 * V) return launch<T, V, 256, 2, 1, WEIGHT>(X, dX, c);
-    if (c.C <= 2048 * V) return launch<T, V, 1024, 2, 1, WEIGHT>(X, dX, c);
+    if (c.ldx < kMostStride && c.ldg < kMostStride) {
+        if (c.C < V) return launch<T, 1, 8, 1, 4, WEIGHT>(X, dX, c);
+        if (c.C <= 4 * V) return launch<T, V, 4, 1, 2, WEIGHT>(X, dX, c);
+        if (c.C <= 8 * V) return launch<T, V, 8, 1, 4, WEIGHT>(X, dX, c);
+        if (c.C <= 16 * V) return launch<T, V, 16, 1, 4, WEIGHT>(X, dX, c);
+        if (c.C <= 32 * V) return launch<T, V, 32, 1, 4, WEIGHT>(X, dX, c);
+        if (c.C <= 64 * V) return launch<T, V, 64, 1, 4, WEIGHT>(X, dX, c);
+        if (c.C <= 128 * V) return launch<T, V, 64, 2, 2, WEIGHT>(X, dX, c);
+        if (c.C <= 512 * V) return launch<T, V, 256, 2, 1, WEIGHT>(X, dX, c);
+        if (c.C <= 1024 * V) return launch<T, V, 256, 4, 1, WEIGHT>(X, dX, c);
+        if (c.C <= 1536 * V) return launch<T, V, 256, 6, 1, WEIGHT>(X, dX, c);
+        if (c.C <= 2048 * V) return launch<T, V, 256, 8, 1, WEIGHT>(X, dX, c);
+    }
     const int blocks = blocks_of(c.N, 1);
     xent_wide_kernel<T, V, WEIGHT><<<blocks, kThreads, 0, c.stream>>>(X, c.ldx, c.labels, dX, c.ldg, c.loss_rows, c.counts, c.scale, c.part, c.N, c.C);
     return blocks;
@@ -325,11 +371,12 @@ template <typename T> int xent(const T *X, T *dX, const Call &c) {
     if (!c.mean) blocks = rows<T, kSum>(X, dX, c);
     else if (c.N <= kCountHere) blocks = rows<T, kMeanHere>(X, dX, c);
     else {
-        count_labels_kernel<<<kCountBlocks, kThreads, 0, c.stream>>>(c.labels, c.N, c.counts);
+        count_labels_kernel<<<kCountBlocks, 1024, 0, c.stream>>>(c.labels, c.N, c.counts);
         blocks = rows<T, kMeanCounted>(X, dX, c);
     }
-    if (blocks <= 1024) add_losses_kernel<256><<<1, 256, 0, c.stream>>>(c.part, blocks, c.loss);
-    else add_losses_kernel<1024><<<1, 1024, 0, c.stream>>>(c.part, blocks, c.loss);
+    if (blocks <= 1024) add_losses_kernel<256, 1><<<1, 256, 0, c.stream>>>(c.part, blocks, c.loss);
+    else if (blocks <= 16384) add_losses_kernel<1024, 4><<<1, 1024, 0, c.stream>>>(c.part, blocks, c.loss);
+    else add_losses_kernel<1024, 16><<<1, 1024, 0, c.stream>>>(c.part, blocks, c.loss);
     GNN_HIP_TRY(hipGetLastError());
     return GNN_OK;
 }
@@ -364,7 +411,7 @@ extern "C" GNN_API int gnn_softmax_xent(const void *X, const void *labels, float
     if (!o.workspace || o.workspace_bytes < gnn_softmax_xent_workspace_bytes(N, C) || reinterpret_cast<uintptr_t>(o.workspace) % 16)
         return GNN_ERR_INVALID_ARG;
     Call c{};
-    c.labels = Labels{labels, o.labels_is_64, C};
+    c.labels = Labels{labels, o.labels_is_64, unsigned(C)};
     c.mean = o.reduction == GNN_LOSS_MEAN;
     c.counts = static_cast<int32_t *>(o.workspace);
     c.part = reinterpret_cast<float *>(static_cast<char *>(o.workspace) + kCountBlocks * 4);

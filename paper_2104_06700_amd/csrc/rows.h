@@ -77,9 +77,13 @@ template <typename T, int VEC, bool NT> struct gnn_strip {
         else v = gnn_rows<T>::fetch(p);
     }
     __device__ __forceinline__ void get(float (&f)[VEC]) const { gnn_rows<T>::unpack(v, f); }
+    __device__ __forceinline__ void set(const float (&f)[VEC]) { v = gnn_rows<T>::pack(f); }
+    // unpacked again from here on: elements that stay unpacked take twice the registers
+    __device__ __forceinline__ void forget() { asm volatile("" : "+v"(v)); }
 };
 template <typename T, bool NT> struct gnn_strip<T, 1, NT> {
     float v;
     __device__ __forceinline__ void load(const T *p) { v = gnn_rows<T>::get(p); }
     __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = v; }
+    __device__ __forceinline__ void set(const float (&f)[1]) { v = f[0]; }
 };

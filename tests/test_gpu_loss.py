@@ -107,6 +107,15 @@ def test_strides_and_alignment(ld, front, dtype):
 
 
 @pytest.mark.gpu
+def test_rows_far_apart():
+    """Row offsets beyond 32 bits, by many rows and by wide strides."""
+    for ld, n in ((1 << 22, 70), ((1 << 22) - 8, 130), (33_000_001, 40)):
+        check(n, 47, ld=ld)
+        check(n, 3, torch.bfloat16, ld=ld)
+        check(n, 700, torch.bfloat16, ld=ld)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("c", [5, 47, 600, 5000, 17000])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_masked_classes_and_unlabelled_rows_that_hold_anything(c, dtype):
