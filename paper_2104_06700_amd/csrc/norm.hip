@@ -62,6 +62,15 @@ template <int ACT> __device__ __forceinline__ float slope(float z) {
     } else return 1.0f;
 }
 
+// rstd (dz gamma - s1 - xh s2).  The product is rounded by itself, as in the sum that s1 is: where a group has one value it is s1, and the
+// gradient exactly 0.
+__device__ __forceinline__ float gradient(float dz, float gamma, float xh, float r, float2 s) {
+#pragma clang fp contract(off)
+    const float t = dz * gamma;
+    const float u = t - s.x;
+    return r * __builtin_fmaf(-xh, s.y, u);
+}
+
 struct Shape {
     Samples samples;
     int64_t N, tile_rows;
@@ -410,13 +419,10 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
     for (int u = 0; u < kRows; ++u)
         if (r0 + u * s.row_lanes < s.N) strip[u].load(X + (r0 + u * s.row_lanes) * ldx + col);
     const Affine<VEC> aff(s, col, gamma, beta);
-    float w[VEC], o[VEC];  // z = x w + o
+    float w[VEC], o[VEC];  // z = (x - o) w + beta: a value that is the mean gives beta, whatever rstd is
     auto fold = [&]() {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            w[j] *= aff.gamma[j];
-            o[j] = aff.beta[j] - o[j] * w[j];
-        }
+        for (int j = 0; j < VEC; ++j) w[j] *= aff.gamma[j];
     };
     if constexpr (STATS == kOne) {
         aff.gather(s, mean, 0, o);
@@ -459,7 +465,7 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
         float x[VEC];
         strip[u].get(x);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) x[j] = activate<ACT>(x[j] * w[j] + o[j]);
+        for (int j = 0; j < VEC; ++j) x[j] = activate<ACT>((x[j] - o[j]) * w[j] + aff.beta[j]);
         gnn_store_row<T, VEC, NT>(Y + r * ldy + col, x);
     }
 }
@@ -483,11 +489,9 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restr
 #pragma unroll
         for (int j = 0; j < VEC; ++j) a1[j] = ax[j] = 0.0f;
         if (at.active) {
-            float o[VEC], rs[VEC];  // xh = x rs + o
+            float o[VEC], rs[VEC];
             aff.gather(s, mean, b, o);
             aff.gather(s, rstd, b, rs);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) o[j] = -o[j] * rs[j];
             int64_t r = row + at.row_lane;
             while (r < stop) {
                 float c1[VEC], cx[VEC];
@@ -511,7 +515,7 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restr
                         sd[u].get(d);
 #pragma unroll
                         for (int j = 0; j < VEC; ++j) {
-                            const float xh = x[j] * rs[j] + o[j];
+                            const float xh = (x[j] - o[j]) * rs[j];
                             const float dz = d[j] * slope<ACT>(xh * aff.gamma[j] + aff.beta[j]);
                             c1[j] += dz;
                             cx[j] += dz * xh;
@@ -639,22 +643,15 @@ __global__ void __launch_bounds__(512) norm_bwd_apply_kernel(const T *__restrict
             sd[u].load(dY + (r0 + u * s.row_lanes) * ldy + col);
         }
     const Affine<VEC> aff(s, col, gamma, beta);
-    float r[VEC], o[VEC], g[VEC], p[VEC], q[VEC];  // xh = x r + o, dX = dz g - p - xh q
-    auto fold = [&](int64_t b, const float2 (&w)[VEC]) {
+    float r[VEC], o[VEC];  // xh = (x - o) r
+    auto fold = [&](int64_t b) {
         aff.gather(s, mean, b, o);
         aff.gather(s, rstd, b, r);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            o[j] = -o[j] * r[j];
-            g[j] = r[j] * aff.gamma[j];
-            p[j] = r[j] * w[j].x;
-            q[j] = r[j] * w[j].y;
-        }
     };
     float2 w[VEC];
     if constexpr (STATS == kOne) {
         aff.gather(s, sums, 0, w);
-        fold(0, w);
+        fold(0);
     } else if constexpr (STATS == kJoin) {
         const float n = float(s.N) * float(s.group_width);
         const float2 *stat = join_tiles<VEC>(s, part, (s.N + s.tile_rows - 1) / s.tile_rows, col,
@@ -665,7 +662,7 @@ __global__ void __launch_bounds__(512) norm_bwd_apply_kernel(const T *__restrict
             [&](int, float2 u) { return make_float2(u.x / n, u.y / n); });
 #pragma unroll
         for (int j = 0; j < VEC; ++j) w[j] = stat[aff.group[j]];
-        fold(0, w);
+        fold(0);
     }
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
@@ -674,16 +671,16 @@ __global__ void __launch_bounds__(512) norm_bwd_apply_kernel(const T *__restrict
         if constexpr (STATS == kMany) {
             const int64_t b = sample_of_row(s, i);
             aff.gather(s, sums, b, w);
-            fold(b, w);
+            fold(b);
         }
         float x[VEC], d[VEC];
         sx[u].get(x);
         sd[u].get(d);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            const float xh = x[j] * r[j] + o[j];
+            const float xh = (x[j] - o[j]) * r[j];
             const float dz = d[j] * slope<ACT>(xh * aff.gamma[j] + aff.beta[j]);
-            x[j] = dz * g[j] - p[j] - xh * q[j];
+            x[j] = gradient(dz, aff.gamma[j], xh, r[j], w[j]);
         }
         gnn_store_row<T, VEC, NT>(dX + i * lddx + col, x);
     }
@@ -993,7 +990,7 @@ __global__ void __launch_bounds__(512) small_bwd_kernel(const T *X, int64_t ldx,
         T *o = dX + (n.lo + t.row_lane) * lddx + t.c0 + t.col;
         auto write = [&](int k, float (&f)[VEC], const float (&g)[VEC]) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) f[j] = r[j] * (g[j] * gm[j] - a[j].x - f[j] * a[j].y);
+            for (int j = 0; j < VEC; ++j) f[j] = gradient(g[j], gm[j], f[j], r[j], a[j]);
             put_row<T>(t, o + k * ostep, f);
         };
 #pragma unroll
