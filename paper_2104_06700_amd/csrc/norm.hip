@@ -18,9 +18,12 @@
 
 namespace {
 
-constexpr int kThreads = 256, kJoinedThreads = 512;
-constexpr int64_t kMaxTiles = 2048;  // as many workgroups as are resident at once
-constexpr int kJoined = 8192;        // partial sums that the writing kernel joins by itself
+// Tiles of at least kTileValues values, at most kTiles of them with kThreads threads each; matrices of kLarge values and more in kLargeTiles with
+// kLargeThreads.  Few tiles are few partial sums to merge (103 K x 141 in 3 groups, backward, 512 tiles 41 us, 1024 47, 2048 of half the threads
+// 72), many small workgroups read best (2.4 M x 256 forward, 512 tiles 1186 us, 2048 of half the threads 1163).
+constexpr int kThreads = 512, kLargeThreads = 256;
+constexpr int64_t kTiles = 512, kLargeTiles = 2048, kLarge = int64_t(1) << 28, kTileValues = 16384;
+constexpr int64_t kJoined = 4096;       // partial sums that the writing kernel joins by itself
 
 // Rows of every sample: from `ptr` (ragged), or `rows` of them each.  What ptr holds is kept inside the matrix.
 struct Samples {
@@ -249,10 +252,11 @@ template <int THREADS> struct Merge {
     }
 };
 
-// Mean and reciprocal deviation of a sample and group from its parts: THREADS threads for a pair.
+// Mean and reciprocal deviation of a sample and group from its parts: THREADS threads for a pair.  One sample: also for every column, as
+// the kernel that writes the result reads them.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const float2 *__restrict__ part, const Shape s, float eps, float *__restrict__ mean,
-                                                             float *__restrict__ rstd) {
+                                                             float *__restrict__ rstd, float *__restrict__ table) {
     __shared__ double2 red[THREADS / 64];
     const int64_t pairs = s.samples.count * s.G;
     for (int64_t p = blockIdx.x; p < pairs; p += gridDim.x) {
@@ -275,10 +279,16 @@ __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const float2 *__res
             var = u.y / n - off * off;
             var = var < 0.0 ? 0.0 : var;  // (NaN stays)
         }
+        const float r = float(1.0 / sqrt(var + double(eps)));
         if (threadIdx.x == 0) {
             mean[p] = float(mid);
-            rstd[p] = float(1.0 / sqrt(var + double(eps)));
+            rstd[p] = r;
         }
+        if (table)
+            for (int k = int(threadIdx.x); k < s.group_width; k += THREADS) {
+                table[c0 + k] = float(mid);
+                table[s.C + c0 + k] = r;
+            }
     }
 }
 
@@ -351,12 +361,12 @@ template <int VEC> struct Affine {
     }
 };
 
-// The kernels that write results: a workgroup of cols x row_lanes threads has kRows * row_lanes neighbouring rows and ends with them, a thread
-// kRows vectors of one column.  Small workgroups that end are faster here than ones that stay and walk: the writes
+// The kernels that write results: a workgroup of cols x row_lanes threads has rows_of() * row_lanes neighbouring rows and ends with them, a thread
+// rows_of() vectors of one column.  Small workgroups that end are faster here than ones that stay and walk: the writes
 // and reads of all of them move through the matrix as one front (2.5 GB copied by one-vector threads 6.5 TB/s, four vectors 6.1, resident
 // workgroups 5.0; norm of 2.4 M x 256 fp32 in workgroups of 128 threads with 1, 2, 4, 8 rows each 1268, 1159, 1205, 1224 us, of 256 threads with 2, 4, 8 1202,
 // 1237, 1248).
-constexpr int kRows = 2, kBlockMost = 128;
+constexpr int kBlockMost = 128;
 template <int VEC> __device__ __forceinline__ int column_of_block(const Shape &s) {
     const int vec = int(blockIdx.y) * s.cols + int(threadIdx.x);
     return vec * VEC >= s.C ? -1 : vec * VEC < s.C - VEC ? vec * VEC : s.C - VEC;
@@ -405,12 +415,16 @@ __device__ __forceinline__ int64_t sample_of_row(const Shape &s, int64_t r) {
     return s.sample_of ? int64_t(s.sample_of[r]) : s.samples.of(r);
 }
 
-enum Stats { kMany, kOne, kJoin };  // statistics of many samples, of one, of one that has to be joined from tiles first
+enum Stats { kMany, kOne, kJoin };  // statistics of many samples, of one (a table of columns), of one that has to be joined from tiles first
+
+// rows of a thread: with two the parameters of the gradient of a bf16 vector, six for each of eight columns, are more than its data
+template <typename T> __host__ __device__ constexpr int rows_of(bool backward) { return sizeof(T) == 4 || !backward ? 2 : 4; }
 
 template <typename T, int VEC, int ACT, bool NT, Stats STATS>
 __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, const float *__restrict__ gamma,
                                                          const float *__restrict__ beta, float *__restrict__ mean, float *__restrict__ rstd,
-                                                         T *__restrict__ Y, int64_t ldy, const float2 *__restrict__ part, float eps) {
+                                                         T *__restrict__ Y, int64_t ldy, const float2 *__restrict__ part, float eps, const float *__restrict__ table) {
+    constexpr int kRows = rows_of<T>(false);
     const int col = column_of_block<VEC>(s);
     const int64_t r0 = int64_t(blockIdx.x) * (kRows * s.row_lanes) + threadIdx.y;
     if (STATS != kJoin && (col < 0 || r0 >= s.N)) return;
@@ -425,8 +439,13 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
         for (int j = 0; j < VEC; ++j) w[j] *= aff.gamma[j];
     };
     if constexpr (STATS == kOne) {
-        aff.gather(s, mean, 0, o);
-        aff.gather(s, rstd, 0, w);
+        if (s.group_width % VEC == 0) {  // a vector has one group: its two values instead of two vectors
+            aff.gather(s, mean, 0, o);
+            aff.gather(s, rstd, 0, w);
+        } else {
+            Affine<VEC>::columns(table + col, o);
+            Affine<VEC>::columns(table + s.C + col, w);
+        }
         fold();
     } else if constexpr (STATS == kJoin) {
         // distances from the first tile's mean of the group's first column
@@ -484,7 +503,7 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restr
 #pragma unroll
     for (int j = 0; j < VEC; ++j) t1[j] = tx[j] = 0.0f;
     for_parts(s, [&](int64_t b, int64_t row, int64_t stop) {
-        constexpr int U = VEC == 8 && THREADS > kThreads ? 2 : 4;
+        constexpr int U = 4;
         float a1[VEC], ax[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) a1[j] = ax[j] = 0.0f;
@@ -574,7 +593,8 @@ template <int THREADS> __device__ __forceinline__ double2 add_deep(double2 v, do
 // s1 and s2 of a sample and group from its parts.  With one sample its columns' sums are dbeta and dgamma too.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_bwd_stats_kernel(const float2 *__restrict__ part, const Shape s, const float *__restrict__ gamma,
-                                                                 float2 *__restrict__ sums, float *__restrict__ dgamma, float *__restrict__ dbeta) {
+                                                                 float2 *__restrict__ sums, float *__restrict__ dgamma, float *__restrict__ dbeta,
+                                                                 const float *__restrict__ mean, const float *__restrict__ rstd, float *__restrict__ table) {
     __shared__ double2 red[THREADS];
     const int64_t pairs = s.samples.count * s.G;
     for (int64_t p = blockIdx.x; p < pairs; p += gridDim.x) {
@@ -601,6 +621,12 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_stats_kernel(const float2 *_
         all = team_sum<THREADS>(all, red);
         const double n = double(m.hi - m.lo) * s.group_width;
         if (threadIdx.x == 0 && sums) sums[p] = make_float2(float(all.x / n), float(all.y / n));
+        if (table) {
+            const float v[4] = {mean[p], rstd[p], float(all.x / n), float(all.y / n)};
+            for (int k = int(threadIdx.x); k < s.group_width; k += THREADS)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) table[int64_t(i) * s.C + c0 + k] = v[i];
+        }
         __syncthreads();
     }
 }
@@ -631,7 +657,8 @@ template <typename T, int VEC, int ACT, bool NT, Stats STATS>
 __global__ void __launch_bounds__(512) norm_bwd_apply_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const Shape s,
                                                              const float *__restrict__ gamma, const float *__restrict__ beta,
                                                              const float *__restrict__ mean, const float *__restrict__ rstd,
-                                                             const float2 *__restrict__ sums, T *__restrict__ dX, int64_t lddx, const float2 *__restrict__ part) {
+                                                             const float2 *__restrict__ sums, T *__restrict__ dX, int64_t lddx, const float2 *__restrict__ part, const float *__restrict__ table) {
+    constexpr int kRows = rows_of<T>(true);
     const int col = column_of_block<VEC>(s);
     const int64_t r0 = int64_t(blockIdx.x) * (kRows * s.row_lanes) + threadIdx.y;
     if (STATS != kJoin && (col < 0 || r0 >= s.N)) return;
@@ -650,8 +677,18 @@ __global__ void __launch_bounds__(512) norm_bwd_apply_kernel(const T *__restrict
     };
     float2 w[VEC];
     if constexpr (STATS == kOne) {
-        aff.gather(s, sums, 0, w);
-        fold(0);
+        if (s.group_width % VEC == 0) {
+            aff.gather(s, sums, 0, w);
+            fold(0);
+        } else {
+            Affine<VEC>::columns(table + col, o);
+            Affine<VEC>::columns(table + s.C + col, r);
+            float a[VEC], b[VEC];
+            Affine<VEC>::columns(table + 2 * int64_t(s.C) + col, a);
+            Affine<VEC>::columns(table + 3 * int64_t(s.C) + col, b);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) w[j] = make_float2(a[j], b[j]);
+        }
     } else if constexpr (STATS == kJoin) {
         const float n = float(s.N) * float(s.group_width);
         const float2 *stat = join_tiles<VEC>(s, part, (s.N + s.tile_rows - 1) / s.tile_rows, col,
@@ -1045,28 +1082,28 @@ __global__ void __launch_bounds__(512) small_bwd_kernel(const T *X, int64_t ldx,
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct Layout {
-    int64_t tile_rows, tiles, map_off, total_off, sums_off, bytes;
+    int64_t tile_rows, tiles, map_off, total_off, sums_off, table_off, bytes;
+    int threads;  // of a tile
     bool joined;  // one sample, few tiles: two launches
 };
 
-// One sample of up to 64 K values for each of the 64 (wide rows: fewer) tiles whose partial sums every writing workgroup can join: tiles of at
-// least 16 K values.  Else tiles of at least 4 K values, at most kMaxTiles of them.
+// One sample of up to 32 K values for each of the tiles whose partial
+// sums every writing workgroup can join by itself saves a launch.
 Layout layout_of(int64_t N, int64_t C, int64_t G, int64_t B, bool backward) {
     Layout L{};
-    const int64_t most = kJoined / C < 64 ? kJoined / C : 64;
-    L.joined = B == 1 && C <= 1024 && N * C <= most * 65536;
-    if (L.joined) {
-        int64_t tiles = (N * C + 16383) / 16384;
-        tiles = tiles < most ? tiles : most;
-        L.tile_rows = (N + tiles - 1) / tiles;
-    } else {
-        const int64_t least = C < 1024 ? 4096 / C : 4, even = (N + kMaxTiles - 1) / kMaxTiles;
-        L.tile_rows = even > least ? even : least;
-    }
+    const int64_t few = kJoined / C < 32 ? kJoined / C : 32;
+    L.joined = B == 1 && C <= 1024 && N * C <= few * 32768;
+    L.threads = N * C < kLarge ? kThreads : kLargeThreads;
+    const int64_t most = L.joined ? few : N * C < kLarge ? kTiles : kLargeTiles;
+    int64_t tiles = (N * C + kTileValues - 1) / kTileValues;
+    tiles = tiles < most ? tiles : most;
+    L.tile_rows = (N + tiles - 1) / tiles;
     L.tiles = (N + L.tile_rows - 1) / L.tile_rows;
     int64_t off = round_up((L.tiles + B) * C * int64_t(sizeof(float2)), 256);
     L.map_off = off;
     if (B > 1) off += round_up(N * 4, 256);
+    L.table_off = off;
+    if (B == 1) off += round_up(4 * C * 4, 256);
     if (backward) {
         L.total_off = off;
         if (B > 1) off += round_up(L.tiles * C * int64_t(sizeof(float2)), 256);
@@ -1123,7 +1160,7 @@ int row_lanes_of(int cols) {
     return best;
 }
 
-Shape shape_of(const Call &c, int vec, bool writes, dim3 *grid, dim3 *block) {
+Shape shape_of(const Call &c, int vec, int rows, dim3 *grid, dim3 *block) {  // rows > 0: of a kernel that writes results
     Shape s{};
     s.samples = c.samples();
     s.N = c.N;
@@ -1132,66 +1169,69 @@ Shape shape_of(const Call &c, int vec, bool writes, dim3 *grid, dim3 *block) {
     s.group_width = int(c.C / c.G);
     s.tile_rows = c.L.tile_rows;
     s.sample_of = c.sample_ptr && c.B > 1 ? reinterpret_cast<int32_t *>(c.scratch(c.L.map_off)) : nullptr;
-    const int64_t vecs = (c.C + vec - 1) / vec, chunks = (vecs + kThreads - 1) / kThreads;
+    const int64_t vecs = (c.C + vec - 1) / vec, chunks = (vecs + 255) / 256;
     s.cols = int((vecs + chunks - 1) / chunks);
-    if (writes) {
+    if (rows) {
         s.row_lanes = row_lanes_of(s.cols);
         *block = dim3(unsigned(s.cols), unsigned(s.row_lanes));
-        *grid = dim3(unsigned((c.N + kRows * s.row_lanes - 1) / (kRows * s.row_lanes)), unsigned(chunks));
+        *grid = dim3(unsigned((c.N + rows * s.row_lanes - 1) / (rows * s.row_lanes)), unsigned(chunks));
     } else {
-        const int threads = c.L.joined ? kJoinedThreads : kThreads;
-        s.row_lanes = threads / s.cols;
-        *block = dim3(unsigned(threads));
+        s.row_lanes = c.L.threads / s.cols;
+        *block = dim3(unsigned(c.L.threads));
         *grid = dim3(unsigned(c.L.tiles), unsigned(chunks));
     }
     return s;
 }
 
-template <typename T, int VEC, int ACT, bool NT> int run_tiles(const Call &c) {
+// PART, OUT: elements of a thread's vectors in the kernel that adds up and in the one that writes.
+template <typename T, int PART, int OUT, int ACT, bool NT> int run_tiles(const Call &c) {
     dim3 grid, threads, out_grid, out_threads;
-    const Shape s = shape_of(c, VEC, false, &grid, &threads), w = shape_of(c, VEC, true, &out_grid, &out_threads);
+    const Shape s = shape_of(c, PART, 0, &grid, &threads), w = shape_of(c, OUT, rows_of<T>(c.backward), &out_grid, &out_threads);
     const T *X = static_cast<const T *>(c.X), *dY = static_cast<const T *>(c.dY);
     T *out = static_cast<T *>(c.out);
     hipStream_t stream = c.stream();
     float2 *part = reinterpret_cast<float2 *>(c.scratch(0));
+    float *table = c.B == 1 ? reinterpret_cast<float *>(c.scratch(c.L.table_off)) : nullptr;
     const int64_t pairs = c.B * c.G;
     const unsigned many = unsigned(pairs < 65536 ? pairs : 65536);
-    const size_t lds = size_t(threads.x) * VEC * 2 * sizeof(float);
+    const size_t lds = size_t(threads.x) * PART * 2 * sizeof(float);
     // what join_tiles keeps: the sums of every row lane, and a sixteenth
     const size_t values = size_t(w.row_lanes) * size_t(c.C), join = (values + c.G * ((values / c.G + 15) / 16)) * sizeof(float2);
     if (!c.backward) {
         if (c.L.joined) {
-            norm_part_kernel<T, VEC, false, kJoinedThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part);
-            norm_apply_kernel<T, VEC, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, part, c.o.eps);
+            norm_part_kernel<T, PART, false, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part);
+            norm_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, part, c.o.eps, nullptr);
         } else {
-            norm_part_kernel<T, VEC, NT, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part);
-            if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd);
-            else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd);
-            else norm_stats_kernel<64><<<many, 64, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd);
-            auto *apply = c.B == 1 ? norm_apply_kernel<T, VEC, ACT, NT, kOne> : norm_apply_kernel<T, VEC, ACT, NT, kMany>;
-            apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, nullptr, 0.0f);
+            auto *sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads> : norm_part_kernel<T, PART, NT, kLargeThreads>;
+            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part);
+            if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd, table);
+            else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd, table);
+            else norm_stats_kernel<64><<<many, 64, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd, table);
+            auto *apply = c.B == 1 ? norm_apply_kernel<T, OUT, ACT, NT, kOne> : norm_apply_kernel<T, OUT, ACT, NT, kMany>;
+            apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, nullptr, 0.0f, table);
         }
     } else {
         float2 *sums = c.out ? reinterpret_cast<float2 *>(c.scratch(c.L.sums_off)) : nullptr;
         float2 *total = c.B > 1 && (c.dgamma || c.dbeta) ? reinterpret_cast<float2 *>(c.scratch(c.L.total_off)) : nullptr;
         if (c.L.joined) {
-            norm_bwd_part_kernel<T, VEC, ACT, false, kJoinedThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, nullptr);
+            norm_bwd_part_kernel<T, PART, ACT, false, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, nullptr);
             if (c.dgamma || c.dbeta) norm_bwd_columns_kernel<<<unsigned((c.C + 15) / 16), 1024, 0, stream>>>(part, c.L.tiles, int(c.C), c.dgamma, c.dbeta);
             if (c.out)
-                norm_bwd_apply_kernel<T, VEC, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, dY, c.o.ldy, w, c.gamma, c.beta, c.mean, c.rstd,
-                                                                                                     nullptr, out, c.o.lddx, part);
+                norm_bwd_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, dY, c.o.ldy, w, c.gamma, c.beta, c.mean, c.rstd,
+                                                                                                     nullptr, out, c.o.lddx, part, nullptr);
         } else {
-            norm_bwd_part_kernel<T, VEC, ACT, NT, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, total);
+            auto *sum = c.L.threads == kThreads ? norm_bwd_part_kernel<T, PART, ACT, NT, kThreads> : norm_bwd_part_kernel<T, PART, ACT, NT, kLargeThreads>;
+            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, total);
             float *dgamma = c.B == 1 ? c.dgamma : nullptr, *dbeta = c.B == 1 ? c.dbeta : nullptr;
             if (sums || dgamma || dbeta) {
-                if (pairs <= 512) norm_bwd_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(part, s, c.gamma, sums, dgamma, dbeta);
-                else if (pairs < 4096) norm_bwd_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(part, s, c.gamma, sums, dgamma, dbeta);
-                else norm_bwd_stats_kernel<64><<<many, 64, 0, stream>>>(part, s, c.gamma, sums, dgamma, dbeta);
+                if (pairs <= 512) norm_bwd_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(part, s, c.gamma, sums, dgamma, dbeta, c.mean, c.rstd, c.out ? table : nullptr);
+                else if (pairs < 4096) norm_bwd_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(part, s, c.gamma, sums, dgamma, dbeta, c.mean, c.rstd, c.out ? table : nullptr);
+                else norm_bwd_stats_kernel<64><<<many, 64, 0, stream>>>(part, s, c.gamma, sums, dgamma, dbeta, c.mean, c.rstd, c.out ? table : nullptr);
             }
             if (total) norm_bwd_columns_kernel<<<unsigned((c.C + 15) / 16), 1024, 0, stream>>>(total, c.L.tiles, int(c.C), c.dgamma, c.dbeta);
             if (c.out) {
-                auto *apply = c.B == 1 ? norm_bwd_apply_kernel<T, VEC, ACT, NT, kOne> : norm_bwd_apply_kernel<T, VEC, ACT, NT, kMany>;
-                apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, dY, c.o.ldy, w, c.gamma, c.beta, c.mean, c.rstd, sums, out, c.o.lddx, nullptr);
+                auto *apply = c.B == 1 ? norm_bwd_apply_kernel<T, OUT, ACT, NT, kOne> : norm_bwd_apply_kernel<T, OUT, ACT, NT, kMany>;
+                apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, dY, c.o.ldy, w, c.gamma, c.beta, c.mean, c.rstd, sums, out, c.o.lddx, nullptr, table);
             }
         }
     }
@@ -1201,6 +1241,7 @@ template <typename T, int VEC, int ACT, bool NT> int run_tiles(const Call &c) {
 
 // Whether samples of up to `rows` rows fit a workgroup, and how.  With few samples a team has one group, or as many as make 16
 // columns (64 bytes of a row), so that there are more workgroups; with many all groups that fit.
+constexpr int64_t kTeam = 256;  // threads of a workgroup of small samples, or more where one needs them
 struct SmallPlan {
     Small s;
     dim3 grid;
@@ -1224,12 +1265,15 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     }
     while (groups > 1 && !fits(groups)) groups = (groups + 1) / 2;
     if (!fits(groups)) return false;
+    // Slices of a row narrower than two 128-byte lines fetch lines that others fetch too: 100 samples of 1,000 rows, slices of 10 of 100 columns,
+    // 69 us, in tiles 25.
+    if (groups < c.G && groups * K * (16 / vec) < 256 && c.N * c.C > (64 << 10)) return false;
     const int64_t cols = (groups * K + vec - 1) / vec;
     int64_t lanes = (rows + held - 1) / held;
     // Ragged samples: the registers have room for one and a half times the mean, if that takes less than the longest; the few rows
     // beyond are fetched again.  Four wavefronts then, one on every SIMD: workgroups of six leave half of the places free.
     const int64_t mean = (c.N + c.B - 1) / c.B;
-    if (c.sample_ptr && cols * lanes > kThreads && held * (kThreads / cols) * 2 >= 3 * mean) lanes = kThreads / cols;
+    if (c.sample_ptr && cols * lanes > kTeam && held * (kTeam / cols) * 2 >= 3 * mean) lanes = kTeam / cols;
     Small &s = p.s;
     s = Small{};
     s.samples = c.samples();
@@ -1240,7 +1284,7 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     s.cols = int(cols);
     s.lanes = int(lanes);
     s.team = int(round_up(cols * lanes, 16) < most ? round_up(cols * lanes, 16) : cols * lanes);
-    s.teams = s.team < kThreads ? kThreads / s.team : 1;
+    s.teams = s.team < kTeam ? int(kTeam) / s.team : 1;
     p.inside = K % vec == 0;
     s.len = int(lanes * (p.inside ? K / vec : K));
     s.team_sums = int(groups) * (s.len + (s.len + 15) / 16);
@@ -1276,8 +1320,12 @@ template <typename T, int ACT> int run_act(const Call &c) {
     constexpr int V = gnn_rows<T>::VEC;
     SmallPlan p;
     if (small_plan(c, V, held<T>(), c.backward ? 512 : 1024, p)) return p.inside ? run_small<T, ACT, true>(c, p) : run_small<T, ACT, false>(c, p);
-    if (c.C < V) return run_tiles<T, 1, ACT, false>(c);
-    return c.past_caches ? run_tiles<T, V, ACT, true>(c) : run_tiles<T, V, ACT, false>(c);
+    if (c.C < V) return run_tiles<T, 1, 1, ACT, false>(c);
+    // The backward sums keep eleven values for every column: with eight bf16 columns a thread only two of its wavefronts fit a SIMD, and half vectors are faster
+    // (us, eight -> four; 400 K x 128 silu 128 -> 109, 1 M x 256 446 -> 424, 103 K x 141 69 -> 47, 1.1 M x 351 identity 740 -> 765).  Results are written
+    // as whole vectors (1.1 M x 351 840 -> 765, 3.5 M x 128 749 -> 726).
+    if (c.backward) return c.past_caches ? run_tiles<T, 4, V, ACT, true>(c) : run_tiles<T, 4, V, ACT, false>(c);
+    return c.past_caches ? run_tiles<T, V, V, ACT, true>(c) : run_tiles<T, V, V, ACT, false>(c);
 }
 
 template <typename T> int run(const Call &c) {

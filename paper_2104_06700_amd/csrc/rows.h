@@ -49,41 +49,63 @@ template <> struct gnn_rows<gnn_bf16> {
     static __device__ __forceinline__ void set(gnn_bf16 *p, float v) { p->bits = __builtin_bit_cast(uint16_t, __bf16(v)); }
 };
 
-// VEC == 1: rows narrower than a vector.  NT: data that is not read again soon goes past the caches (reads alone 6.2 -> 7.0 TB/s, copies
-// 6.2 -> 6.5 TB/s at 2.5 GB).
-template <typename T, int VEC, bool NT = false> __device__ __forceinline__ void gnn_load_row(const T *p, float (&v)[VEC]) {
-    if constexpr (VEC == 1) v[0] = gnn_rows<T>::get(p);
-    else {
-        typedef typename gnn_rows<T>::raw raw;
-        if constexpr (NT) gnn_rows<T>::unpack(__builtin_nontemporal_load(reinterpret_cast<const raw *>(p)), v);
-        else gnn_rows<T>::unpack(gnn_rows<T>::fetch(p), v);
-    }
-}
-template <typename T, int VEC, bool NT = false> __device__ __forceinline__ void gnn_store_row(T *p, const float (&v)[VEC]) {
-    if constexpr (VEC == 1) gnn_rows<T>::set(p, v[0]);
-    else {
-        typedef typename gnn_rows<T>::raw raw;
-        if constexpr (NT) __builtin_nontemporal_store(gnn_rows<T>::pack(v), reinterpret_cast<raw *>(p));
-        else gnn_rows<T>::put(p, gnn_rows<T>::pack(v));
-    }
-}
-
-// VEC elements as they lie in memory
+// VEC elements as they lie in memory: a whole vector, half a bf16 vector, or one element of rows narrower than that.  NT: data that is not
+// read again soon goes past the caches (reads alone 6.2 -> 7.0 TB/s, copies 6.2 -> 6.5 TB/s at 2.5 GB).
 template <typename T, int VEC, bool NT> struct gnn_strip {
+    static_assert(VEC == gnn_rows<T>::VEC, "a whole vector");
     typedef typename gnn_rows<T>::raw raw;
     raw v;
     __device__ __forceinline__ void load(const T *p) {
         if constexpr (NT) v = __builtin_nontemporal_load(reinterpret_cast<const raw *>(p));
         else v = gnn_rows<T>::fetch(p);
     }
+    __device__ __forceinline__ void store(T *p) const {
+        if constexpr (NT) __builtin_nontemporal_store(v, reinterpret_cast<raw *>(p));
+        else gnn_rows<T>::put(p, v);
+    }
     __device__ __forceinline__ void get(float (&f)[VEC]) const { gnn_rows<T>::unpack(v, f); }
     __device__ __forceinline__ void set(const float (&f)[VEC]) { v = gnn_rows<T>::pack(f); }
     // unpacked again from here on: elements that stay unpacked take twice the registers
     __device__ __forceinline__ void forget() { asm volatile("" : "+v"(v)); }
 };
+typedef uint32_t gnn_u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+template <bool NT> struct gnn_strip<gnn_bf16, 4, NT> {
+    gnn_u32x2 v;
+    __device__ __forceinline__ void load(const gnn_bf16 *p) {
+        if constexpr (NT) v = __builtin_nontemporal_load(reinterpret_cast<const gnn_u32x2 *>(p));
+        else v = *reinterpret_cast<const gnn_u32x2 *>(p);
+    }
+    __device__ __forceinline__ void store(gnn_bf16 *p) const {
+        if constexpr (NT) __builtin_nontemporal_store(v, reinterpret_cast<gnn_u32x2 *>(p));
+        else *reinterpret_cast<gnn_u32x2 *>(p) = v;
+    }
+    __device__ __forceinline__ void get(float (&f)[4]) const {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            f[2 * i] = __uint_as_float(v[i] << 16);
+            f[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+        }
+    }
+    __device__ __forceinline__ void set(const float (&f)[4]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(gnn_f32x2{f[2 * i], f[2 * i + 1]}, gnn_bf16x2));
+    }
+};
 template <typename T, bool NT> struct gnn_strip<T, 1, NT> {
     float v;
     __device__ __forceinline__ void load(const T *p) { v = gnn_rows<T>::get(p); }
+    __device__ __forceinline__ void store(T *p) const { gnn_rows<T>::set(p, v); }
     __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = v; }
     __device__ __forceinline__ void set(const float (&f)[1]) { v = f[0]; }
 };
+
+template <typename T, int VEC, bool NT = false> __device__ __forceinline__ void gnn_load_row(const T *p, float (&v)[VEC]) {
+    gnn_strip<T, VEC, NT> t;
+    t.load(p);
+    t.get(v);
+}
+template <typename T, int VEC, bool NT = false> __device__ __forceinline__ void gnn_store_row(T *p, const float (&v)[VEC]) {
+    gnn_strip<T, VEC, NT> t;
+    t.set(v);
+    t.store(p);
+}
