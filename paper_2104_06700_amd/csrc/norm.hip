@@ -634,8 +634,8 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_stats_kernel(const float2 *_
 // dbeta and dgamma: the sums of n rows of partial sums, 16 columns and 64 row lanes a workgroup.
 __global__ void __launch_bounds__(1024) norm_bwd_columns_kernel(const float2 *__restrict__ total, int64_t n, int C, float *__restrict__ dgamma,
                                                                 float *__restrict__ dbeta) {
-    __shared__ double2 red[1024];
-    constexpr int U = 4;
+    __shared__ double2 red[16][16];
+    constexpr int U = 16;
     const int c = int(blockIdx.x) * 16 + int(threadIdx.x & 15);
     double2 u = {0.0, 0.0};
     if (c < C)
@@ -646,8 +646,19 @@ __global__ void __launch_bounds__(1024) norm_bwd_columns_kernel(const float2 *__
 #pragma unroll
             for (int k = 0; k < U; ++k) { u.x += v[k].x; u.y += v[k].y; }
         }
-    u = add_deep<1024>(u, red, 16, 64);
+    // the four row lanes of a wavefront, then the sixteen wavefronts
+#pragma unroll
+    for (int d = 16; d <= 32; d <<= 1) {
+        u.x += __shfl_xor(u.x, d);
+        u.y += __shfl_xor(u.y, d);
+    }
+    if ((threadIdx.x & 63) < 16) red[threadIdx.x >> 6][threadIdx.x & 15] = u;
+    __syncthreads();
     if (threadIdx.x < 16 && c < C) {
+        for (int w = 1; w < 16; ++w) {
+            u.x += red[w][threadIdx.x].x;
+            u.y += red[w][threadIdx.x].y;
+        }
         if (dbeta) dbeta[c] = float(u.x);
         if (dgamma) dgamma[c] = float(u.y);
     }
@@ -1290,7 +1301,7 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     s.team_sums = int(groups) * (s.len + (s.len + 15) / 16);
     p.threads = int(round_up(s.team * s.teams, 64));
     const int64_t blocks = (c.B + s.teams - 1) / s.teams;
-    p.grid = dim3(unsigned(c.backward && blocks > 1024 ? 1024 : blocks), unsigned((c.G + groups - 1) / groups));
+    p.grid = dim3(unsigned(blocks), unsigned((c.G + groups - 1) / groups));
     size_t values = size_t(s.teams) * s.team_sums;
     if (c.backward) {
         const size_t columns = size_t(s.teams) * s.lanes * s.cols * vec;
@@ -1300,9 +1311,27 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     return p.grid.y <= 65535 && p.lds <= 65536;
 }
 
-template <typename T, int ACT, bool INSIDE> int run_small(const Call &c, const SmallPlan &p) {
+// Workgroups of small_bwd_kernel that are resident at once: wavefronts of its registers on the 256 CUs, and what fits their LDS.  More would be
+// a second round with few of them (2,449 graphs of 25 vertices x 100, us: 768 workgroups 35, 1024 40, 2048 45, 4096 48).
+template <typename T, int ACT, bool INSIDE> unsigned resident(const SmallPlan &p) {
+    static const int waves = [] {
+        int blocks = 0;
+        const hipError_t err = hipOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, reinterpret_cast<const void *>(small_bwd_kernel<T, ACT, INSIDE>), int(kTeam), 0);
+        if (err != hipSuccess) (void)hipGetLastError();
+        return err == hipSuccess && blocks > 0 ? blocks * int(kTeam / 64) : 8;
+    }();
+    const int by_waves = waves / (p.threads / 64), by_lds = p.lds ? int((160u << 10) / p.lds) : by_waves;
+    const int each = by_waves < by_lds ? by_waves : by_lds;
+    return 256u * unsigned(each > 1 ? each : 1);
+}
+
+template <typename T, int ACT, bool INSIDE> int run_small(const Call &c, SmallPlan &p) {
     const T *X = static_cast<const T *>(c.X);
     hipStream_t stream = c.stream();
+    if (c.backward) {
+        const unsigned most = resident<T, ACT, INSIDE>(p);
+        if (p.grid.x > most) p.grid.x = most;
+    }
     if (!c.backward) {
         small_kernel<T, ACT, INSIDE><<<p.grid, p.threads, p.lds, stream>>>(X, c.o.ldx, p.s, c.gamma, c.beta, c.o.eps, c.mean, c.rstd, static_cast<T *>(c.out),
                                                                            c.o.ldy);
