@@ -10,9 +10,8 @@
 //
 // Two ways.  Samples that fit a workgroup's registers (small_kernel, small_bwd_kernel) are read once and done in one launch.  All others: the
 // rows are cut into tiles of equal size whatever the samples' sizes are, one workgroup each, which adds up each sample's part of
-// it per column; the partial sums of tile t and sample b lie in slot t + b (from one pair to the next at least one of the two
-// grows, so no two share a slot).  A second kernel merges the slots of every sample, in their order: results do not depend on
-// timing.  A third reads the rows again and writes the result.
+// it per column.  A sample inside a tile is finished there; of one that crosses tiles, each leaves its partial sums in a slot of its own, and a second
+// kernel merges them in their order: results do not depend on timing.  A third reads the rows again and writes the result.
 #include "common.h"
 #include "rows.h"
 
@@ -23,6 +22,7 @@ namespace {
 // 72), many small workgroups read best (2.4 M x 256 forward, 512 tiles 1186 us, 2048 of half the threads 1163).
 constexpr int kThreads = 512, kLargeThreads = 256;
 constexpr int64_t kTiles = 512, kLargeTiles = 2048, kLarge = int64_t(1) << 28, kTileValues = 16384;
+constexpr int64_t kSmallParts = 4096;   // at most so many workgroups of samples that fit one leave column sums
 constexpr int64_t kJoined = 4096;       // partial sums that the writing kernel joins by itself
 
 // Rows of every sample: from `ptr` (ragged), or `rows` of them each.  What ptr holds is kept inside the matrix.
@@ -81,7 +81,14 @@ struct Shape {
     int cols;       // vectors of columns of a workgroup; threads: cols x row_lanes
     int row_lanes;
     int32_t *sample_of;  // [N] ragged samples: the sample of every row, for the kernels that write results
+    bool inside;    // samples inside a tile are finished there (more than one sample, rows of one workgroup's width)
 };
+
+// The slot of a sample's part in tile t: at most one sample comes into a tile from the one before (2 t), one goes out of it (2 t + 1).  Without
+// `inside` every part has one, t + b: from one pair to the next at least one of the two grows.
+__device__ __forceinline__ int64_t slot_of(const Shape &s, int64_t t, int64_t b, int64_t begin) {
+    return !s.inside ? t + b : begin > t * s.tile_rows ? 2 * t + 1 : 2 * t;
+}
 
 // What a thread of a tile works on: VEC neighbouring columns from `col`, every row_lanes-th row.  The last vector of a row starts
 // where it ends with the row: columns that it shares with the one before are computed twice, to the same bits.
@@ -132,14 +139,53 @@ template <int VEC> __device__ __forceinline__ void add_row_lanes(float *a, float
     __syncthreads();
 }
 
+// Sums of `groups` runs of n values each, sixteen to one at a time, between two areas of LDS; returns where they are.  All threads of the
+// workgroup call it together, `threads` of them with their number i (others with i >= threads).
+template <typename V> __device__ __forceinline__ void add_to(V &a, const V &b) {
+    if constexpr (sizeof(V) == 8) { a.x += b.x; a.y += b.y; }
+    else a += b;
+}
+template <typename V> __device__ __forceinline__ const V *group_sums(V *from, V *to, int groups, int n, int i, int threads) {
+    while (n > 1) {
+        const int out = (n + 15) >> 4;
+        __syncthreads();
+        if (i < threads)
+            for (int k = i; k < groups * out; k += threads) {
+                const int g = out == 1 ? k : int(unsigned(k) / unsigned(out)), o = k - g * out;
+                V t = from[g * n + o];
+                for (int e = o + out; e < n; e += out) add_to(t, from[g * n + e]);
+                to[k] = t;
+            }
+        n = out;
+        V *const swap = from;
+        from = to;
+        to = swap;
+    }
+    __syncthreads();
+    return from;
+}
+
+// What a tile has in LDS: two sums of every thread's columns; behind them, to finish samples, a value of every column, the columns' contributions by
+// group, and room to add these up.
+__device__ __forceinline__ float *tile_means(const Shape &s, float *lds, int vec) { return lds + 2 * int(blockDim.x) * vec; }
+__device__ __forceinline__ float2 *tile_sums(const Shape &s, float *lds, int vec) { return reinterpret_cast<float2 *>(tile_means(s, lds, vec) + ((s.C + 1) & ~1)); }
+
 // Per part and column: the mean and the sum of squared distances from it.  Sums are taken of the distances from the part's first
 // row, which is of the values' own size, so that a mean far from zero costs no bits; four rows and then
 // eight times four are added up by themselves, so that long sums do not lose them.
 template <typename T, int VEC, bool NT, int THREADS>
-__global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, float2 *__restrict__ part) {
+__global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, float2 *__restrict__ part, float eps,
+                                                             float *__restrict__ mean_out, float *__restrict__ rstd_out) {
     extern __shared__ float tile_lds[];
     float *const red_1 = tile_lds, *const red_2 = tile_lds + blockDim.x * VEC;
     const Place<VEC> at(s);
+    if (s.inside && s.samples.ptr)  // samples without rows are in no tile
+        for (int64_t b = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; b < s.samples.count; b += int64_t(gridDim.x) * blockDim.x)
+            if (s.samples.begin(b + 1) <= s.samples.begin(b))
+                for (int g = 0; g < s.G; ++g) {
+                    mean_out[b * s.G + g] = 0.0f;
+                    rstd_out[b * s.G + g] = 1.0f / sqrtf(eps);
+                }
     for_parts(s, [&](int64_t b, int64_t row, int64_t stop) {
         constexpr int U = 4;
         float pivot[VEC], s1[VEC], s2[VEC];
@@ -185,13 +231,45 @@ __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict_
             red_2[threadIdx.x * VEC + j] = s2[j];
         }
         add_row_lanes<VEC>(red_1, red_2, s, at, s.row_lanes);
-        if (at.active && at.row_lane == 0) {
-            const float inv = 1.0f / float(stop - row);
-            float2 *o = part + (int64_t(blockIdx.x) + b) * s.C + at.col;
+        const float rows = float(stop - row), inv = 1.0f / rows;
+        const int64_t begin = s.inside ? s.samples.begin(b) : 0;
+        const bool whole = s.inside && begin == row && s.samples.begin(b + 1) == stop;  // the same for all threads
+        const bool mine = at.active && at.row_lane == 0;
+        float mean[VEC], m2[VEC];
+        if (mine) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 const float a = red_1[at.lane * VEC + j], q = red_2[at.lane * VEC + j] - a * a * inv;
-                o[j] = make_float2(pivot[j] + a * inv, q < 0.0f ? 0.0f : q);
+                mean[j] = pivot[j] + a * inv;
+                m2[j] = q < 0.0f ? 0.0f : q;
+            }
+        }
+        if (!whole) {
+            if (mine) {
+                float2 *o = part + slot_of(s, blockIdx.x, b, begin) * s.C + at.col;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) o[j] = make_float2(mean[j], m2[j]);
+            }
+        } else {
+            float *const means = tile_means(s, tile_lds, VEC);
+            float2 *const sums = tile_sums(s, tile_lds, VEC);
+            if (mine)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) means[at.col + j] = mean[j];
+            __syncthreads();
+            if (mine) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const int c = at.col + j;
+                    const float d = mean[j] - means[c - c % s.group_width];
+                    sums[c] = make_float2(rows * d, m2[j] + rows * d * d);
+                }
+            }
+            const float2 *all = group_sums(sums, sums + s.C, s.G, s.group_width, int(threadIdx.x), int(blockDim.x));
+            for (int g = int(threadIdx.x); g < s.G; g += int(blockDim.x)) {
+                const float n = rows * float(s.group_width), off = all[g].x / n, var = all[g].y / n - off * off;
+                mean_out[b * s.G + g] = means[g * s.group_width] + off;
+                rstd_out[b * s.G + g] = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);
             }
         }
         __syncthreads();
@@ -222,11 +300,13 @@ template <int THREADS> __device__ __forceinline__ double2 team_sum(double2 v, do
 template <int THREADS> struct Merge {
     int64_t lo, hi, t0, t1;
     int wide, deep, k, d;
+    bool done;  // by the tile that the sample is in
     __device__ __forceinline__ Merge(const Shape &s, int64_t b) {
         lo = s.samples.begin(b);
         hi = s.samples.begin(b + 1);
         t0 = lo / s.tile_rows;
         t1 = hi > lo ? (hi - 1) / s.tile_rows : t0 - 1;
+        done = s.inside && t1 <= t0;
         wide = s.group_width < THREADS ? s.group_width : THREADS;
         deep = THREADS / wide;
         k = int(threadIdx.x) % wide;
@@ -240,7 +320,7 @@ template <int THREADS> struct Merge {
             float2 v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (t + u * deep <= t1) v[u] = part[(t + u * deep + b) * s.C + c];
+                if (t + u * deep <= t1) v[u] = part[slot_of(s, t + u * deep, b, lo) * s.C + c];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int64_t w = t + u * deep;
@@ -252,20 +332,36 @@ template <int THREADS> struct Merge {
     }
 };
 
+// Sample and group of pair p: by sample, or, where there are fewer tiles than samples, the sample that goes out of tile p / G; -1: none does.
+__device__ __forceinline__ int64_t sample_of_pair(const Shape &s, int64_t p, int64_t tiles, int *group) {
+    const int64_t i = p / s.G;
+    *group = int(p - i * s.G);
+    if (!s.inside || s.samples.count <= tiles) return i;
+    const int64_t end = (i + 1) * s.tile_rows;
+    if (end >= s.N) return -1;
+    const int64_t b = s.samples.of(end - 1);
+    return b < s.samples.count && s.samples.begin(b) >= i * s.tile_rows && s.samples.begin(b + 1) > end ? b : -1;
+}
+
 // Mean and reciprocal deviation of a sample and group from its parts: THREADS threads for a pair.  One sample: also for every column, as
 // the kernel that writes the result reads them.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const float2 *__restrict__ part, const Shape s, float eps, float *__restrict__ mean,
                                                              float *__restrict__ rstd, float *__restrict__ table) {
     __shared__ double2 red[THREADS / 64];
-    const int64_t pairs = s.samples.count * s.G;
-    for (int64_t p = blockIdx.x; p < pairs; p += gridDim.x) {
-        const int64_t b = p / s.G;
-        const int c0 = int(p % s.G) * s.group_width;
+    const int64_t tiles = (s.N + s.tile_rows - 1) / s.tile_rows;
+    const int64_t pairs = (s.inside && s.samples.count > tiles ? tiles : s.samples.count) * s.G;
+    for (int64_t i = blockIdx.x; i < pairs; i += gridDim.x) {
+        int group;
+        const int64_t b = sample_of_pair(s, i, tiles, &group);
+        if (b < 0) continue;
+        const int c0 = group * s.group_width;
+        const int64_t p = b * s.G + group;
         const Merge<THREADS> m(s, b);
+        if (m.done) continue;
         double mid = 0.0, var = 0.0;
         if (m.hi > m.lo) {
-            const double pivot = part[(m.t0 + b) * s.C + c0].x;
+            const double pivot = part[slot_of(s, m.t0, b, m.lo) * s.C + c0].x;
             double2 u = {0.0, 0.0};
             for (int k = m.k; k < s.group_width; k += m.wide)
                 m.tiles(s, part, b, c0 + k, [&](double rows, float2 v) {
@@ -290,32 +386,6 @@ __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const float2 *__res
                 table[s.C + c0 + k] = r;
             }
     }
-}
-
-// Sums of `groups` runs of n values each, sixteen to one at a time, between two areas of LDS; returns where they are.  All threads of the
-// workgroup call it together, `threads` of them with their number i (others with i >= threads).
-template <typename V> __device__ __forceinline__ void add_to(V &a, const V &b) {
-    if constexpr (sizeof(V) == 8) { a.x += b.x; a.y += b.y; }
-    else a += b;
-}
-template <typename V> __device__ __forceinline__ const V *group_sums(V *from, V *to, int groups, int n, int i, int threads) {
-    while (n > 1) {
-        const int out = (n + 15) >> 4;
-        __syncthreads();
-        if (i < threads)
-            for (int k = i; k < groups * out; k += threads) {
-                const int g = out == 1 ? k : int(unsigned(k) / unsigned(out)), o = k - g * out;
-                V t = from[g * n + o];
-                for (int e = o + out; e < n; e += out) add_to(t, from[g * n + e]);
-                to[k] = t;
-            }
-        n = out;
-        V *const swap = from;
-        from = to;
-        to = swap;
-    }
-    __syncthreads();
-    return from;
 }
 
 // gamma and beta of a thread's columns, and their groups
@@ -412,7 +482,9 @@ template <int VEC, typename F, typename G> __device__ __forceinline__ const floa
     return out;
 }
 __device__ __forceinline__ int64_t sample_of_row(const Shape &s, int64_t r) {
-    return s.sample_of ? int64_t(s.sample_of[r]) : s.samples.of(r);
+    if (!s.sample_of) return s.samples.of(r);
+    const uint32_t b = uint32_t(s.sample_of[r]), last = uint32_t(s.samples.count - 1);
+    return b < last ? b : last;  // a row that ptr leaves to no sample was given none
 }
 
 enum Stats { kMany, kOne, kJoin };  // statistics of many samples, of one (a table of columns), of one that has to be joined from tiles first
@@ -494,7 +566,7 @@ template <typename T, int VEC, int ACT, bool NT, int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const Shape s,
                                                                  const float *__restrict__ gamma, const float *__restrict__ beta,
                                                                  const float *__restrict__ mean, const float *__restrict__ rstd,
-                                                                 float2 *__restrict__ part, float2 *__restrict__ total) {
+                                                                 float2 *__restrict__ part, float2 *__restrict__ total, float2 *__restrict__ sums_out) {
     extern __shared__ float tile_lds[];
     float *const red_1 = tile_lds, *const red_x = tile_lds + blockDim.x * VEC;
     const Place<VEC> at(s);
@@ -554,15 +626,24 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restr
             red_x[threadIdx.x * VEC + j] = ax[j];
         }
         add_row_lanes<VEC>(red_1, red_x, s, at, s.row_lanes);
+        const int64_t begin = s.inside ? s.samples.begin(b) : 0;
+        const bool whole = s.inside && begin == row && s.samples.begin(b + 1) == stop;  // the same for all threads
+        float2 *const sums = tile_sums(s, tile_lds, VEC);
         if (at.active && at.row_lane == 0) {
-            float2 *o = part + (int64_t(blockIdx.x) + b) * s.C + at.col;
+            float2 *o = part + (whole ? 0 : slot_of(s, blockIdx.x, b, begin)) * s.C + at.col;
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 const float u1 = red_1[at.lane * VEC + j], ux = red_x[at.lane * VEC + j];
-                o[j] = make_float2(u1, ux);
+                if (whole) sums[at.col + j] = make_float2(u1 * aff.gamma[j], ux * aff.gamma[j]);
+                else o[j] = make_float2(u1, ux);
                 t1[j] += u1;
                 tx[j] += ux;
             }
+        }
+        if (whole && sums_out) {
+            const float2 *all = group_sums(sums, sums + s.C, s.G, s.group_width, int(threadIdx.x), int(blockDim.x));
+            const float n = float(stop - row) * float(s.group_width);
+            for (int g = int(threadIdx.x); g < s.G; g += int(blockDim.x)) sums_out[b * s.G + g] = make_float2(all[g].x / n, all[g].y / n);
         }
         __syncthreads();
     });
@@ -596,11 +677,16 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_stats_kernel(const float2 *_
                                                                  float2 *__restrict__ sums, float *__restrict__ dgamma, float *__restrict__ dbeta,
                                                                  const float *__restrict__ mean, const float *__restrict__ rstd, float *__restrict__ table) {
     __shared__ double2 red[THREADS];
-    const int64_t pairs = s.samples.count * s.G;
-    for (int64_t p = blockIdx.x; p < pairs; p += gridDim.x) {
-        const int64_t b = p / s.G;
-        const int c0 = int(p % s.G) * s.group_width;
+    const int64_t tiles = (s.N + s.tile_rows - 1) / s.tile_rows;
+    const int64_t pairs = (s.inside && s.samples.count > tiles ? tiles : s.samples.count) * s.G;
+    for (int64_t i = blockIdx.x; i < pairs; i += gridDim.x) {
+        int group;
+        const int64_t b = sample_of_pair(s, i, tiles, &group);
+        if (b < 0) continue;
+        const int c0 = group * s.group_width;
+        const int64_t p = b * s.G + group;
         const Merge<THREADS> m(s, b);
+        if (m.done) continue;
         if (m.hi <= m.lo) continue;
         double2 all = {0.0, 0.0};
         for (int k0 = 0; k0 < s.group_width; k0 += m.wide) {
@@ -1093,7 +1179,8 @@ __global__ void __launch_bounds__(512) small_bwd_kernel(const T *X, int64_t ldx,
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct Layout {
-    int64_t tile_rows, tiles, map_off, total_off, sums_off, table_off, bytes;
+    int64_t tile_rows, tiles, parts, map_off, total_off, sums_off, table_off, bytes;
+    bool inside;  // samples inside a tile are finished there
     int threads;  // of a tile
     bool joined;  // one sample, few tiles: two launches
 };
@@ -1110,7 +1197,12 @@ Layout layout_of(int64_t N, int64_t C, int64_t G, int64_t B, bool backward) {
     tiles = tiles < most ? tiles : most;
     L.tile_rows = (N + tiles - 1) / tiles;
     L.tiles = (N + L.tile_rows - 1) / L.tile_rows;
-    int64_t off = round_up((L.tiles + B) * C * int64_t(sizeof(float2)), 256);
+    L.inside = B > 1 && C <= 1024;  // rows of at most 256 vectors: one workgroup has whole rows
+    // partial sums: of the tiles, or of the workgroups of small_bwd_kernel
+    L.parts = L.inside ? 2 * L.tiles : L.tiles + B;
+    const int64_t small = B < kSmallParts ? B : kSmallParts;
+    if (backward && L.parts < small) L.parts = small;
+    int64_t off = round_up(L.parts * C * int64_t(sizeof(float2)), 256);
     L.map_off = off;
     if (B > 1) off += round_up(N * 4, 256);
     L.table_off = off;
@@ -1179,6 +1271,7 @@ Shape shape_of(const Call &c, int vec, int rows, dim3 *grid, dim3 *block) {  // 
     s.G = int(c.G);
     s.group_width = int(c.C / c.G);
     s.tile_rows = c.L.tile_rows;
+    s.inside = c.L.inside;
     s.sample_of = c.sample_ptr && c.B > 1 ? reinterpret_cast<int32_t *>(c.scratch(c.L.map_off)) : nullptr;
     const int64_t vecs = (c.C + vec - 1) / vec, chunks = (vecs + 255) / 256;
     s.cols = int((vecs + chunks - 1) / chunks);
@@ -1203,18 +1296,19 @@ template <typename T, int PART, int OUT, int ACT, bool NT> int run_tiles(const C
     hipStream_t stream = c.stream();
     float2 *part = reinterpret_cast<float2 *>(c.scratch(0));
     float *table = c.B == 1 ? reinterpret_cast<float *>(c.scratch(c.L.table_off)) : nullptr;
-    const int64_t pairs = c.B * c.G;
+    const int64_t pairs = (c.L.inside && c.B > c.L.tiles ? c.L.tiles : c.B) * c.G;
     const unsigned many = unsigned(pairs < 65536 ? pairs : 65536);
-    const size_t lds = size_t(threads.x) * PART * 2 * sizeof(float);
+    const int64_t finish = c.L.inside ? (c.C + 1) / 2 * 2 + 2 * (c.C + c.G * ((c.C / c.G + 15) / 16)) : 0;  // floats: tile_means, tile_sums
+    const size_t lds = (size_t(threads.x) * PART * 2 + size_t(finish)) * sizeof(float);
     // what join_tiles keeps: the sums of every row lane, and a sixteenth
     const size_t values = size_t(w.row_lanes) * size_t(c.C), join = (values + c.G * ((values / c.G + 15) / 16)) * sizeof(float2);
     if (!c.backward) {
         if (c.L.joined) {
-            norm_part_kernel<T, PART, false, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part);
+            norm_part_kernel<T, PART, false, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part, c.o.eps, c.mean, c.rstd);
             norm_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, part, c.o.eps, nullptr);
         } else {
             auto *sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads> : norm_part_kernel<T, PART, NT, kLargeThreads>;
-            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part);
+            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part, c.o.eps, c.mean, c.rstd);
             if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd, table);
             else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd, table);
             else norm_stats_kernel<64><<<many, 64, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd, table);
@@ -1225,14 +1319,14 @@ template <typename T, int PART, int OUT, int ACT, bool NT> int run_tiles(const C
         float2 *sums = c.out ? reinterpret_cast<float2 *>(c.scratch(c.L.sums_off)) : nullptr;
         float2 *total = c.B > 1 && (c.dgamma || c.dbeta) ? reinterpret_cast<float2 *>(c.scratch(c.L.total_off)) : nullptr;
         if (c.L.joined) {
-            norm_bwd_part_kernel<T, PART, ACT, false, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, nullptr);
+            norm_bwd_part_kernel<T, PART, ACT, false, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, nullptr, nullptr);
             if (c.dgamma || c.dbeta) norm_bwd_columns_kernel<<<unsigned((c.C + 15) / 16), 1024, 0, stream>>>(part, c.L.tiles, int(c.C), c.dgamma, c.dbeta);
             if (c.out)
                 norm_bwd_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, dY, c.o.ldy, w, c.gamma, c.beta, c.mean, c.rstd,
                                                                                                      nullptr, out, c.o.lddx, part, nullptr);
         } else {
             auto *sum = c.L.threads == kThreads ? norm_bwd_part_kernel<T, PART, ACT, NT, kThreads> : norm_bwd_part_kernel<T, PART, ACT, NT, kLargeThreads>;
-            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, total);
+            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, total, sums);
             float *dgamma = c.B == 1 ? c.dgamma : nullptr, *dbeta = c.B == 1 ? c.dbeta : nullptr;
             if (sums || dgamma || dbeta) {
                 if (pairs <= 512) norm_bwd_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(part, s, c.gamma, sums, dgamma, dbeta, c.mean, c.rstd, c.out ? table : nullptr);
@@ -1329,8 +1423,8 @@ template <typename T, int ACT, bool INSIDE> int run_small(const Call &c, SmallPl
     const T *X = static_cast<const T *>(c.X);
     hipStream_t stream = c.stream();
     if (c.backward) {
-        const unsigned most = resident<T, ACT, INSIDE>(p);
-        if (p.grid.x > most) p.grid.x = most;
+        const int64_t here = resident<T, ACT, INSIDE>(p), most = here < c.L.parts ? here : c.L.parts;
+        if (p.grid.x > most) p.grid.x = unsigned(most);
     }
     if (!c.backward) {
         small_kernel<T, ACT, INSIDE><<<p.grid, p.threads, p.lds, stream>>>(X, c.o.ldx, p.s, c.gamma, c.beta, c.o.eps, c.mean, c.rstd, static_cast<T *>(c.out),

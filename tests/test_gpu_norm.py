@@ -201,6 +201,21 @@ def test_ragged_samples(name, c, groups, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("c,groups,dtype", [(1000, 8, torch.float32), (1024, 1, torch.bfloat16), (1030, 5, torch.float32), (7, 1, torch.bfloat16), (512, 512, torch.float32)])
+def test_samples_inside_and_across_tiles(c, groups, dtype):
+    """Samples that begin and end with a tile, fill it, cross one border or several, and share one, beside samples without rows."""
+    # a tile has 16384 values: 16 or 17 rows of the widest
+    sizes = [16, 1, 15, 17, 16, 0, 3, 0, 13, 40, 8, 0, 0, 2, 1, 1, 33, 16, 100, 5, 0]
+    ptr = [0] + [int(v) for v in np.cumsum(sizes)]
+    for act, ptr_dtype in (("silu", torch.int64), ("relu", torch.int32)):
+        print("tiles", c, groups, dtype, act, flush=True)
+        check(ptr[-1], c, groups, ptr, act, dtype, ptr_dtype=ptr_dtype)
+    # many more samples than tiles
+    ptr = [0] + [int(v) for v in np.cumsum(np.random.default_rng(5).integers(0, 4, 400))]
+    check(ptr[-1], c, groups, ptr, "silu", dtype)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("lds,front", [((100, 104, 128), 0), ((101, 103, 107), 3), ((300, 100, 100), 1)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_strides_and_alignment(lds, front, dtype):
