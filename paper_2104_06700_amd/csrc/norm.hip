@@ -23,6 +23,7 @@ namespace {
 constexpr int kThreads = 512, kLargeThreads = 256;
 constexpr int64_t kTiles = 512, kLargeTiles = 2048, kLarge = int64_t(1) << 28, kTileValues = 16384;
 constexpr int64_t kSmallParts = 4096;   // at most so many workgroups of samples that fit one leave column sums
+constexpr int64_t kRowParts = 2048;     // and of workgroups that have samples of one row
 constexpr int64_t kJoined = 4096;       // partial sums that the writing kernel joins by itself
 
 // Rows of every sample: from `ptr` (ragged), or `rows` of them each.  What ptr holds is kept inside the matrix.
@@ -826,7 +827,8 @@ __global__ void __launch_bounds__(512) norm_bwd_apply_kernel(const T *__restrict
 template <typename T> __host__ __device__ constexpr int held() { return 16 / gnn_rows<T>::VEC; }
 
 // A team of threads has a sample's rows of `groups` neighbouring groups in registers: cols x lanes threads, thread (lane, row
-// lane) the vector `lane` of every lanes-th row.  The last vector of the columns may be short.
+// lane) the vector `lane` of every lanes-th row.  The last vector ends with the columns: those that it shares with the one before it are computed by
+// both to the same bits (2,449 graphs of 25 vertices x 100 bf16, backward, with a short last vector instead 90 us, so 69).  Fewer columns than a vector has are one short vector.
 struct Small {
     Samples samples;
     int C, G, K;
@@ -849,9 +851,9 @@ template <int VEC, bool INSIDE, typename V> struct Team {
         c0 = int(blockIdx.y) * s.groups * s.K;
         const int left = (s.C - c0) / s.K;
         groups = left < s.groups ? left : s.groups;
-        col = lane * VEC;
-        have = groups * s.K - col;
-        have = have < 0 ? 0 : have < VEC ? have : VEC;
+        const int columns = groups * s.K;
+        col = lane * VEC < columns - VEC || columns < VEC ? lane * VEC : columns - VEC;
+        have = lane * VEC >= columns ? 0 : columns < VEC ? columns : VEC;
         active = team < s.teams && row_lane < s.lanes && have > 0;
         sums = lds + (team < s.teams ? team : 0) * s.team_sums;
         g0 = int(unsigned(col) / unsigned(s.K));
@@ -1174,6 +1176,235 @@ __global__ void __launch_bounds__(512) small_bwd_kernel(const T *X, int64_t ldx,
             if (j < t.have) part[int64_t(blockIdx.x) * s.C + t.c0 + t.col + j] = small_lds2[t.lane * VEC + j];
 }
 
+// ---------------------------------------------------------------- samples of one row
+
+// Per vertex: `lanes` lanes of a wavefront, a power of two, have a row in registers, vector i of a lane in columns (i lanes + lane) VEC.  A
+// group is `width` neighbouring lanes, or the row; sums go by lane permutations, without LDS and without waiting for other wavefronts.
+struct PerRow {
+    int64_t N;
+    int C, G, K;
+    int lanes, shift, width;  // lanes = 1 << shift
+};
+constexpr int kRowThreads = 256;
+
+template <int CTRL> __device__ __forceinline__ float from_lane(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// sum over `width` neighbouring lanes, in all of them; all lanes of the wavefront are here
+__device__ __forceinline__ float add_lanes(float v, int width) {
+    if (width >= 2) v += from_lane<0xB1>(v);    // the other of a pair
+    if (width >= 4) v += from_lane<0x4E>(v);    // the other pair of four
+    if (width >= 8) v += from_lane<0x141>(v);   // mirrored in eight: the other four
+    if (width >= 16) v += from_lane<0x140>(v);  // mirrored in sixteen: the other eight
+    if (width >= 32) v += __shfl_xor(v, 16);
+    if (width >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
+
+// The last vector of a row ends with it; its first `skip` columns are the vector's before it, computed by both to the same bits and counted there.
+template <int VEC, int NV> struct RowPlace {
+    int lane, unit, units;
+    int col[NV], skip[NV];
+    bool active[NV];
+    __device__ __forceinline__ explicit RowPlace(const PerRow &s) {
+        lane = int(threadIdx.x) & (s.lanes - 1);
+        unit = int(threadIdx.x) >> s.shift;
+        units = kRowThreads >> s.shift;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * s.lanes + lane) * VEC;
+            active[i] = c < s.C;
+            col[i] = c < s.C - VEC ? c : s.C - VEC;
+            skip[i] = active[i] ? c - col[i] : VEC;
+        }
+    }
+    // a[i]: of vector i; sums of the groups they belong to
+    __device__ __forceinline__ void groups(const PerRow &s, float (&a)[NV]) const {
+        if (s.G == 1) {
+            float t = a[0];
+#pragma unroll
+            for (int i = 1; i < NV; ++i) t += a[i];
+            t = add_lanes(t, s.width);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) a[i] = t;
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) a[i] = add_lanes(a[i], s.width);
+        }
+    }
+    template <typename T, bool NT> __device__ __forceinline__ void load(gnn_strip<T, VEC, NT> (&x)[NV], const T *row, bool there) const {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            x[i].v = {};
+            if (there && active[i]) x[i].load(row + col[i]);
+        }
+    }
+    __device__ __forceinline__ void columns(const float *p, float otherwise, float (&f)[NV][VEC]) const {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) f[i][j] = otherwise;
+            if (p && active[i]) Affine<VEC>::columns(p + col[i], f[i]);
+        }
+    }
+};
+// rows that a thread has vectors of at once
+template <typename T> __host__ __device__ constexpr int rows_held(int nv, bool backward) {
+    const int r = (backward ? 16 / gnn_rows<T>::VEC : 2) / nv;
+    return r > 1 ? r : 1;
+}
+
+template <typename T, int ACT, int NV, bool NT>
+__global__ void __launch_bounds__(kRowThreads) row_kernel(const T *__restrict__ X, int64_t ldx, const PerRow s, const float *__restrict__ gamma,
+                                                          const float *__restrict__ beta, float eps, float *__restrict__ mean, float *__restrict__ rstd,
+                                                          T *__restrict__ Y, int64_t ldy) {
+    constexpr int VEC = gnn_rows<T>::VEC, R = rows_held<T>(NV, false);
+    const RowPlace<VEC, NV> at(s);
+    const int64_t r0 = int64_t(blockIdx.x) * (at.units * R) + at.unit;
+    gnn_strip<T, VEC, NT> x[R][NV];
+#pragma unroll
+    for (int u = 0; u < R; ++u) at.load(x[u], X + (r0 + u * at.units) * ldx, r0 + u * at.units < s.N);
+    float gm[NV][VEC], bt[NV][VEC];
+    at.columns(gamma, 1.0f, gm);
+    at.columns(beta, 0.0f, bt);
+    const float inv = 1.0f / float(s.K);
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+        const int64_t r = r0 + u * at.units;
+        float f[NV][VEC], m[NV], q[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            x[u][i].get(f[i]);
+            m[i] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) m[i] += j >= at.skip[i] ? f[i][j] : 0.0f;
+        }
+        at.groups(s, m);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            m[i] *= inv;
+            q[i] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                f[i][j] -= m[i];
+                q[i] += j >= at.skip[i] ? f[i][j] * f[i][j] : 0.0f;
+            }
+        }
+        at.groups(s, q);
+        if (r >= s.N) continue;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (!at.active[i]) continue;
+            const float k = 1.0f / sqrtf(q[i] * inv + eps);
+            if ((at.lane & (s.width - 1)) == 0 && (i == 0 || s.G > 1)) {
+                const int64_t p = r * s.G + at.col[i] / s.K;
+                mean[p] = m[i];
+                rstd[p] = k;
+            }
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) f[i][j] = activate<ACT>(f[i][j] * (k * gm[i][j]) + bt[i][j]);
+            gnn_store_row<T, VEC, NT>(Y + r * ldy + at.col[i], f[i]);
+        }
+    }
+}
+
+// Workgroups walk over the rows where the parameters' gradients are asked for, with the column sums in registers, and leave them in their row
+// of `part`.
+template <typename T, int ACT, int NV, bool NT>
+__global__ void __launch_bounds__(kRowThreads) row_bwd_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const PerRow s,
+                                                              const float *__restrict__ gamma, const float *__restrict__ beta,
+                                                              const float *__restrict__ mean, const float *__restrict__ rstd, T *__restrict__ dX,
+                                                              int64_t lddx, float2 *__restrict__ part) {
+    extern __shared__ float2 row_lds[];
+    constexpr int VEC = gnn_rows<T>::VEC, R = rows_held<T>(NV, true);
+    const RowPlace<VEC, NV> at(s);
+    float gm[NV][VEC], bt[NV][VEC];
+    at.columns(gamma, 1.0f, gm);
+    at.columns(beta, 0.0f, bt);
+    float2 total[NV][VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) total[i][j] = make_float2(0.0f, 0.0f);
+    const float inv = 1.0f / float(s.K);
+    for (int64_t base = int64_t(blockIdx.x) * (at.units * R); base < s.N; base += int64_t(gridDim.x) * (at.units * R)) {
+        const int64_t r0 = base + at.unit;
+        gnn_strip<T, VEC, NT> x[R][NV], d[R][NV];
+        float m[R][NV], k[R][NV];
+#pragma unroll
+        for (int u = 0; u < R; ++u) {
+            const int64_t r = r0 + u * at.units;
+            at.load(x[u], X + r * ldx, r < s.N);
+            at.load(d[u], dY + r * ldy, r < s.N);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const bool there = r < s.N && at.active[i];
+                const int64_t p = r * s.G + (s.G > 1 ? at.col[i] / s.K : 0);
+                m[u][i] = there ? mean[p] : 0.0f;
+                k[u][i] = there ? rstd[p] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < R; ++u) {
+            const int64_t r = r0 + u * at.units;
+            float f[NV][VEC], g[NV][VEC], s1[NV], s2[NV];
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                x[u][i].get(f[i]);
+                d[u][i].get(g[i]);
+                s1[i] = s2[i] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    f[i][j] = (f[i][j] - m[u][i]) * k[u][i];
+                    g[i][j] *= slope<ACT>(f[i][j] * gm[i][j] + bt[i][j]);
+                    total[i][j].x += g[i][j];
+                    total[i][j].y += g[i][j] * f[i][j];
+                    const float t = j >= at.skip[i] ? g[i][j] * gm[i][j] : 0.0f;
+                    s1[i] += t;
+                    s2[i] += j >= at.skip[i] ? t * f[i][j] : 0.0f;
+                }
+            }
+            if (!dX) continue;  // the same for the whole launch
+            at.groups(s, s1);
+            at.groups(s, s2);
+            if (r >= s.N) continue;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const float2 sum = make_float2(s1[i] * inv, s2[i] * inv);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) f[i][j] = gradient(g[i][j], gm[i][j], f[i][j], k[u][i], sum);
+                if (at.active[i]) gnn_store_row<T, VEC, NT>(dX + r * lddx + at.col[i], f[i]);
+            }
+        }
+    }
+    if (!part) return;  // the same for the whole launch
+    // the rows of a wavefront, then the wavefronts
+    const int width = NV * VEC * s.lanes, wave = int(threadIdx.x) >> 6;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            float2 &t = total[i][j];
+            for (int e = s.lanes; e < 64; e <<= 1) {
+                t.x += __shfl_xor(t.x, e);
+                t.y += __shfl_xor(t.y, e);
+            }
+            if (wave && (threadIdx.x & 63) < unsigned(s.lanes)) row_lds[(wave - 1) * width + (i * s.lanes + at.lane) * VEC + j] = t;
+        }
+    __syncthreads();
+    if (threadIdx.x >= unsigned(s.lanes)) return;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            if (j < at.skip[i]) continue;
+            float2 t = total[i][j];
+#pragma unroll
+            for (int w = 0; w < kRowThreads / 64 - 1; ++w) add_to(t, row_lds[w * width + (i * s.lanes + at.lane) * VEC + j]);
+            part[int64_t(blockIdx.x) * s.C + at.col[i] + j] = t;
+        }
+}
+
 // ---------------------------------------------------------------- host
 
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -1439,8 +1670,55 @@ template <typename T, int ACT, bool INSIDE> int run_small(const Call &c, SmallPl
     return GNN_OK;
 }
 
+// Whether rows are samples whose groups are whole powers of two of lanes, and how: as few places for vectors as will do.
+bool row_plan(const Call &c, int vec, PerRow &s, int &nv) {
+    if (c.sample_ptr || c.N != c.B || c.C < vec) return false;
+    const int64_t K = c.C / c.G, most = 16 / vec;
+    s = PerRow{c.N, int(c.C), int(c.G), int(K), 0, 0, 0};
+    for (int n = 1; n <= most; ++n) {
+        int shift = 0;
+        while (((c.C + vec - 1) / vec + n - 1) / n > int64_t(1) << shift) ++shift;
+        if (shift > 6 || (s.lanes && (n << shift) >= nv * s.lanes)) continue;
+        if (c.G > 1 && (K % vec || (K / vec & (K / vec - 1)) || K / vec > int64_t(1) << shift)) continue;
+        s.lanes = 1 << shift;
+        s.shift = shift;
+        nv = n;
+    }
+    s.width = c.G > 1 ? int(K / vec) : s.lanes;
+    return s.lanes > 0;
+}
+
+template <typename T, int ACT, int NV, bool NT> int run_rows(const Call &c, const PerRow &s) {
+    const T *X = static_cast<const T *>(c.X);
+    hipStream_t stream = c.stream();
+    const int64_t each = (kRowThreads >> s.shift) * rows_held<T>(NV, c.backward), blocks = (c.N + each - 1) / each;
+    if (!c.backward) {
+        row_kernel<T, ACT, NV, NT><<<unsigned(blocks), kRowThreads, 0, stream>>>(X, c.o.ldx, s, c.gamma, c.beta, c.o.eps, c.mean, c.rstd, static_cast<T *>(c.out), c.o.ldy);
+    } else {
+        const bool sums = c.dgamma || c.dbeta;
+        float2 *part = sums ? reinterpret_cast<float2 *>(c.scratch(0)) : nullptr;
+        const int64_t rows = c.N * c.C < kLarge ? kRowParts / 2 : kRowParts, most = rows < c.L.parts ? rows : c.L.parts, grid = sums && blocks > most ? most : blocks;
+        const size_t lds = sums ? size_t(kRowThreads / 64 - 1) * NV * gnn_rows<T>::VEC * s.lanes * sizeof(float2) : 0;
+        row_bwd_kernel<T, ACT, NV, NT><<<unsigned(grid), kRowThreads, lds, stream>>>(X, c.o.ldx, static_cast<const T *>(c.dY), c.o.ldy, s, c.gamma, c.beta, c.mean,
+                                                                                     c.rstd, static_cast<T *>(c.out), c.o.lddx, part);
+        if (part) norm_bwd_columns_kernel<<<unsigned((c.C + 15) / 16), 1024, 0, stream>>>(part, grid, int(c.C), c.dgamma, c.dbeta);
+    }
+    GNN_HIP_TRY(hipGetLastError());
+    return GNN_OK;
+}
+template <typename T, int ACT, int NV> int run_rows(const Call &c, const PerRow &s) {
+    return c.past_caches ? run_rows<T, ACT, NV, true>(c, s) : run_rows<T, ACT, NV, false>(c, s);
+}
+
 template <typename T, int ACT> int run_act(const Call &c) {
     constexpr int V = gnn_rows<T>::VEC;
+    PerRow rows;
+    int nv = 0;
+    if (row_plan(c, V, rows, nv)) {
+        if (nv == 1) return run_rows<T, ACT, 1>(c, rows);
+        if (nv == 2) return run_rows<T, ACT, 2>(c, rows);
+        if constexpr (V == 4) return nv == 3 ? run_rows<T, ACT, 3>(c, rows) : run_rows<T, ACT, 4>(c, rows);
+    }
     SmallPlan p;
     if (small_plan(c, V, held<T>(), c.backward ? 512 : 1024, p)) return p.inside ? run_small<T, ACT, true>(c, p) : run_small<T, ACT, false>(c, p);
     if (c.C < V) return run_tiles<T, 1, 1, ACT, false>(c);
