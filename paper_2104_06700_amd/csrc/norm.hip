@@ -1577,7 +1577,7 @@ template <typename T, int PART, int OUT, int ACT, bool NT> int run_tiles(const C
 
 // Whether samples of up to `rows` rows fit a workgroup, and how.  With few samples a team has one group, or as many as make 16
 // columns (64 bytes of a row), so that there are more workgroups; with many all groups that fit.
-constexpr int64_t kTeam = 256;  // threads of a workgroup of small samples, or more where one needs them
+constexpr int64_t kTeam = 256;  // threads of a workgroup of small samples
 struct SmallPlan {
     Small s;
     dim3 grid;
@@ -1589,9 +1589,11 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     const int64_t rows = c.sample_ptr ? c.o.max_sample_rows : c.N / c.B;
     if (rows <= 0) return false;
     const int64_t K = c.C / c.G;
+    // many samples may have four times the rows that the registers of the largest workgroup hold: 612 graphs of 0 to 200 vertices x 128 bf16, 25 us, in
+    // tiles 78; sixteen times, 1,000 graphs of 0 to 800 x 64 backward, 147, in tiles 136
     auto fits = [&](int64_t groups) {
         const int64_t cols = (groups * K + vec - 1) / vec;
-        return cols <= most && rows <= held * (most / cols);
+        return cols <= most && rows <= (c.B < 256 ? 1 : 4) * held * (most / cols);
     };
     int64_t groups = c.G;
     if (c.B < 256) {
@@ -1606,10 +1608,15 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     if (groups < c.G && groups * K * (16 / vec) < 256 && c.N * c.C > (64 << 10)) return false;
     const int64_t cols = (groups * K + vec - 1) / vec;
     int64_t lanes = (rows + held - 1) / held;
-    // Ragged samples: the registers have room for one and a half times the mean, if that takes less than the longest; the few rows
-    // beyond are fetched again.  Four wavefronts then, one on every SIMD: workgroups of six leave half of the places free.
+    // A workgroup of 64 to 512 threads with about seven vectors each of a mean sample; what does not stay in its registers is fetched again by the
+    // later passes, from the caches.  More threads wait for each other at every sum, fewer have too long a way through their rows (us; 2,449 graphs
+    // of 25 vertices, ragged, forward: 100 bf16 columns 64 threads 24, 128 27, 256 37, 384 that hold the longest 63; 100 fp32 31, 20, 23, 40;
+    // 256 fp32 62, 40, 35, 74.  612 graphs of 100 x 128 fp32 55, 30, 21 and 512 threads 18).  Backward, with its column sums to join, 256 (100 fp32 128
+    // threads 37, 256 33, 384 51).
     const int64_t mean = (c.N + c.B - 1) / c.B;
-    if (c.sample_ptr && cols * lanes > kTeam && held * (kTeam / cols) * 2 >= 3 * mean) lanes = kTeam / cols;
+    int64_t wide = c.backward ? kTeam : 2 * kTeam;
+    while (!c.backward && wide > 64 && cols <= wide / 2 && mean * cols <= wide / 2 * 7) wide /= 2;
+    if (cols * lanes > wide && cols <= wide) lanes = wide / cols;
     Small &s = p.s;
     s = Small{};
     s.samples = c.samples();
@@ -1620,7 +1627,7 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     s.cols = int(cols);
     s.lanes = int(lanes);
     s.team = int(round_up(cols * lanes, 16) < most ? round_up(cols * lanes, 16) : cols * lanes);
-    s.teams = s.team < kTeam ? int(kTeam) / s.team : 1;
+    s.teams = s.team < wide ? int(wide) / s.team : 1;
     p.inside = K % vec == 0;
     s.len = int(lanes * (p.inside ? K / vec : K));
     s.team_sums = int(groups) * (s.len + (s.len + 15) / 16);
