@@ -176,6 +176,29 @@ def test_samples_of_equal_size(samples, rows, c, groups):
         check(samples * rows, c, groups, list(range(0, samples * rows + 1, rows)), act, dtype, uniform=1)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("c,groups", [(3, 1), (4, 1), (8, 1), (9, 1), (64, 16), (129, 1), (192, 3), (256, 2), (256, 64), (300, 1), (512, 16), (602, 1), (770, 1),
+                                      (1023, 1), (1024, 1), (1024, 128), (1025, 1)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_every_vertex_by_itself(c, groups, dtype):
+    for n, act in ((1, "silu"), (5, "none"), (1003, "silu"), (258, "relu")):
+        print("rows", n, c, groups, dtype, act, flush=True)
+        check(n, c, groups, list(range(n + 1)), act, dtype, uniform=1)
+    check(77, c, groups, list(range(78)), "silu", dtype, uniform=1, lds=(c + 3, c + 1, c + 5), front=3, affine=False)
+
+
+@pytest.mark.gpu
+def test_small_samples_longer_than_registers_hold():
+    """Many samples that one workgroup each reads again and again, narrow groups and a last vector that ends with the row among them."""
+    rng = np.random.default_rng(7)
+    for c, groups, most in ((128, 16, 250), (99, 9, 120), (35, 35, 700)):
+        sizes = list(rng.integers(0, most, 260))
+        ptr = [0] + [int(v) for v in np.cumsum(sizes)]
+        for dtype in (torch.float32, torch.bfloat16):
+            print("long", c, groups, most, dtype, flush=True)
+            check(ptr[-1], c, groups, ptr, "silu", dtype, hint=most)
+
+
 def ragged(name, rng):
     if name == "empty ones":
         sizes = [0, 0, 5, 0, 1, 130, 0, 64, 0, 0]
