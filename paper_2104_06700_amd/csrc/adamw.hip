@@ -15,6 +15,10 @@
 // The tensors' descriptors are kernel arguments: no copy of them, no allocation, at most kTensors per launch.  A workgroup has
 // kChunk neighbouring elements of one tensor and ends with them; its loads are all issued before the first is waited for.  A
 // scale's 256 elements are 64 lanes of four (fp32) or 32 of eight (bf16), whose maximum is formed by lane permutations.
+//
+// Bound by the memory: 245 M fp32 elements 1162 us with fp32 states (28 bytes an element, 5.9 TB/s), 677 with 8-bit states (16 bytes, 5.8); 140 M in bf16
+// with a master copy and 8-bit states 431 (16 bytes, 5.2).  Workgroups that stay and walk reach 4.3 to 4.9 TB/s.  The 103 K elements of a model of
+// eight tensors 3.8 us in chunks of 2,048.
 #include "common.h"
 #include "rows.h"
 

@@ -8,6 +8,9 @@
 // Three launches: the labelled rows of every piece of the label array are counted, the rows are done with the sum of these
 // counts, and the workgroups' sums of row losses are added in their order; results do not depend on timing.  Up to kCountHere rows
 // every workgroup counts by itself, which is one launch less.
+//
+// Bound by the memory in wide rows (24,490 x 8,195 bf16, all labelled, 176 us = 4.6 TB/s, a workgroup's row waits twice for all its wavefronts), by
+// instructions in narrow ones (2.4 M x 47 fp32, 8 % labelled, 98 us = 5.2 TB/s).
 #include "common.h"
 #include "rows.h"
 
@@ -40,16 +43,12 @@ struct Labels {
     }
 };
 
-// ctrl: a permutation of the 16 lanes of a row
-template <int CTRL> __device__ __forceinline__ float from_lane(float v) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
-}
 // f over LANES neighbouring lanes, in all of them
 template <int LANES, typename F> __device__ __forceinline__ float lanes_reduce(float v, F f) {
-    if constexpr (LANES >= 2) v = f(v, from_lane<0xB1>(v));    // the other of a pair
-    if constexpr (LANES >= 4) v = f(v, from_lane<0x4E>(v));    // the other pair of four
-    if constexpr (LANES >= 8) v = f(v, from_lane<0x141>(v));   // mirrored in eight: the other four
-    if constexpr (LANES >= 16) v = f(v, from_lane<0x140>(v));  // mirrored in sixteen: the other eight
+    if constexpr (LANES >= 2) v = f(v, gnn_from_lane<0xB1>(v));    // the other of a pair
+    if constexpr (LANES >= 4) v = f(v, gnn_from_lane<0x4E>(v));    // the other pair of four
+    if constexpr (LANES >= 8) v = f(v, gnn_from_lane<0x141>(v));   // mirrored in eight: the other four
+    if constexpr (LANES >= 16) v = f(v, gnn_from_lane<0x140>(v));  // mirrored in sixteen: the other eight
     if constexpr (LANES >= 32) v = f(v, __shfl_xor(v, 16));
     if constexpr (LANES >= 64) v = f(v, __shfl_xor(v, 32));
     return v;

@@ -99,6 +99,11 @@ template <typename T, bool NT> struct gnn_strip<T, 1, NT> {
     __device__ __forceinline__ void set(const float (&f)[1]) { v = f[0]; }
 };
 
+// CTRL: a permutation of the 16 lanes of a row
+template <int CTRL> __device__ __forceinline__ float gnn_from_lane(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
 template <typename T, int VEC, bool NT = false> __device__ __forceinline__ void gnn_load_row(const T *p, float (&v)[VEC]) {
     gnn_strip<T, VEC, NT> t;
     t.load(p);
