@@ -1616,7 +1616,8 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     const int64_t mean = (c.N + c.B - 1) / c.B;
     int64_t wide = c.backward ? kTeam : 2 * kTeam;
     while (!c.backward && wide > 64 && cols <= wide / 2 && mean * cols <= wide / 2 * 7) wide /= 2;
-    if (cols * lanes > wide && cols <= wide) lanes = wide / cols;
+    const int64_t room = cols <= wide ? wide : most;  // threads; wide rows take what a workgroup can have
+    if (cols * lanes > room) lanes = room / cols;
     Small &s = p.s;
     s = Small{};
     s.samples = c.samples();

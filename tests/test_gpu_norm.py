@@ -199,6 +199,15 @@ def test_small_samples_longer_than_registers_hold():
             check(ptr[-1], c, groups, ptr, "silu", dtype, hint=most)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("c,groups", [(1500, 3), (2000, 4), (2600, 2), (4096, 8), (4100, 5)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_wide_rows_in_many_small_samples(c, groups, dtype):
+    for rows in (3, 9, 17):
+        print("wide", rows, c, groups, dtype, flush=True)
+        check(260 * rows, c, groups, list(range(0, 260 * rows + 1, rows)), "silu", dtype, uniform=1)
+
+
 def ragged(name, rng):
     if name == "empty ones":
         sizes = [0, 0, 5, 0, 1, 130, 0, 64, 0, 0]
