@@ -108,10 +108,11 @@ template <int VEC> struct Place {
     }
 };
 
-// Runs f(sample, first row, row behind the last) for the parts of the samples in this workgroup's tile.  The same for all threads.
-template <typename F> __device__ __forceinline__ void for_parts(const Shape &s, F f) {
+// Runs f(sample, first row, row behind the last) for the parts of the samples in this workgroup's tile; ONE: there is one sample.  The same for all threads.
+template <bool ONE, typename F> __device__ __forceinline__ void for_parts(const Shape &s, F f) {
     const int64_t r0 = int64_t(blockIdx.x) * s.tile_rows;
     const int64_t r1 = r0 + s.tile_rows < s.N ? r0 + s.tile_rows : s.N;
+    if constexpr (ONE) return f(int64_t(0), r0, r1);
     int64_t row = r0;
     for (int64_t b = s.samples.of(r0); b < s.samples.count && row < r1; ++b) {
         const int64_t end = s.samples.begin(b + 1);
@@ -145,10 +146,9 @@ template <int VEC> __device__ __forceinline__ void add_row_lanes(float *a, float
 
 // Sums of `groups` runs of n values each, sixteen to one at a time, between two areas of LDS; returns where they are.  All threads of the
 // workgroup call it together, `threads` of them with their number i (others with i >= threads).
-template <typename V> __device__ __forceinline__ void add_to(V &a, const V &b) {
-    if constexpr (sizeof(V) == 8) { a.x += b.x; a.y += b.y; }
-    else a += b;
-}
+__device__ __forceinline__ void add_to(float &a, float b) { a += b; }
+__device__ __forceinline__ void add_to(float2 &a, float2 b) { a.x += b.x; a.y += b.y; }
+__device__ __forceinline__ void add_to(double2 &a, double2 b) { a.x += b.x; a.y += b.y; }
 template <typename V> __device__ __forceinline__ const V *group_sums(V *from, V *to, int groups, int n, int i, int threads) {
     while (n > 1) {
         const int out = (n + 15) >> 4;
@@ -169,111 +169,157 @@ template <typename V> __device__ __forceinline__ const V *group_sums(V *from, V 
     return from;
 }
 
-// What a tile has in LDS: two sums of every thread's columns; behind them, to finish samples, a value of every column, the columns' contributions by
-// group, and room to add these up.
-__device__ __forceinline__ float *tile_means(const Shape &s, float *lds, int vec) { return lds + 2 * int(blockDim.x) * vec; }
-__device__ __forceinline__ float2 *tile_sums(const Shape &s, float *lds, int vec) { return reinterpret_cast<float2 *>(tile_means(s, lds, vec) + ((s.C + 1) & ~1)); }
+// What a tile has in LDS, in floats: `each` for every column of a thread.  Their place is taken by what finishes samples, the columns' contributions (V) by
+// group and the room to add these up, once the threads' values have been added up.
+template <typename V> __host__ __device__ constexpr int64_t tile_values(int64_t threads, int64_t vec, int64_t each, int64_t C, int64_t G, bool inside) {
+    const int64_t own = each * threads * vec, sums = inside ? int64_t(sizeof(V) / 4) * (C + (C > G ? G * ((C / G + 15) / 16) : 0)) : 0;
+    return (own > sums ? own : sums) + 3 & ~int64_t(3);
+}
 
-// Per part and column: the mean and the sum of squared distances from it.  Sums are taken of the distances from the part's first
-// row, which is of the values' own size, so that a mean far from zero costs no bits; four rows and then
-// eight times four are added up by themselves, so that long sums do not lose them.
-template <typename T, int VEC, bool NT, int THREADS>
-__global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, float2 *__restrict__ part, float eps,
+// Joins the moments (mean, sum of squared distances from it) of some values to those of others before: share = their part of all, weight =
+// share * number of values before
+template <typename M> __device__ __forceinline__ void join(M &mean, float &m2, M other, float other_m2, float share, float weight) {
+    const M d = other - mean;
+    mean += d * M(share);
+    m2 += other_m2 + float(d) * float(d) * weight;
+}
+
+// The moments of a tile's row lanes, each of `each` rows and one more in the first `rest` lanes, are joined in LDS: mean and m2
+// [row_lanes][cols * VEC], the result in row lane 0's places.
+template <int VEC> __device__ __forceinline__ void join_row_lanes(double *mean, float *m2, const Shape &s, const Place<VEC> &at, int each, int rest) {
+    const int width = s.cols * VEC;
+    const auto count = [&](int first, int end) { return (end - first) * each + (rest > first ? (rest < end ? rest : end) - first : 0); };
+    for (int step = 1; step < s.row_lanes; step *= 2) {
+        __syncthreads();
+        const int other = at.row_lane + step;
+        if (!at.active || (at.row_lane & (2 * step - 1)) || other >= s.row_lanes) continue;
+        const int n = count(other, other + step < s.row_lanes ? other + step : s.row_lanes);
+        if (n == 0) continue;
+        const float before = float(count(at.row_lane, other)), share = float(n) * __builtin_amdgcn_rcpf(before + float(n));
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const int i = at.row_lane * width + at.lane * VEC + j, o = i + step * width;
+            join(mean[i], m2[i], mean[o], m2[o], share, share * before);
+        }
+    }
+    __syncthreads();
+}
+
+// Per part and column: the mean and the sum of squared distances from it.  A thread takes its rows in runs of up to 32 and sums up their distances from
+// a value that no single row can move far: the mean of the rows before, for the first run that of its first four.  Each run's moments are then
+// joined to those of the rows before (d = difference of the means: m2 = m2 + m2' + d^2 n n' / (n + n'), all terms positive), so that
+// the difference s2 - s1^2 / n takes off at most what the run is worth, whatever row comes first: with all distances taken from a part's first row instead a zero
+// row in front of 16,384 of mean 100 and deviation 1 costs rstd 4e-4.
+template <typename T, int VEC, bool NT, int THREADS, bool ONE>
+__global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, double2 *__restrict__ part, float eps,
                                                              float *__restrict__ mean_out, float *__restrict__ rstd_out) {
-    extern __shared__ float tile_lds[];
-    float *const red_1 = tile_lds, *const red_2 = tile_lds + blockDim.x * VEC;
+    extern __shared__ double tile_lds[];
+    double *const red_1 = tile_lds;
+    float *const red_2 = reinterpret_cast<float *>(tile_lds + blockDim.x * VEC);
+    double2 *const sums = reinterpret_cast<double2 *>(tile_lds);
+    double *const means = tile_lds + tile_values<double2>(blockDim.x, VEC, 3, s.C, s.G, s.inside) / 2;
     const Place<VEC> at(s);
-    if (s.inside && s.samples.ptr)  // samples without rows are in no tile
+    if (!ONE && s.inside && s.samples.ptr)  // samples without rows are in no tile
         for (int64_t b = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; b < s.samples.count; b += int64_t(gridDim.x) * blockDim.x)
             if (s.samples.begin(b + 1) <= s.samples.begin(b))
                 for (int g = 0; g < s.G; ++g) {
                     mean_out[b * s.G + g] = 0.0f;
                     rstd_out[b * s.G + g] = 1.0f / sqrtf(eps);
                 }
-    for_parts(s, [&](int64_t b, int64_t row, int64_t stop) {
-        constexpr int U = 4;
-        float pivot[VEC], s1[VEC], s2[VEC];
+    for_parts<ONE>(s, [&](int64_t b, int64_t row, int64_t stop) {
+        constexpr int U = 4, RUN = 32;
+        const int rows = int(stop - row), each = int(unsigned(rows) / unsigned(s.row_lanes)), rest = rows - each * s.row_lanes;
+        float base[VEC], off[VEC], m2[VEC];  // the mean is base + off
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) pivot[j] = s1[j] = s2[j] = 0.0f;
+        for (int j = 0; j < VEC; ++j) base[j] = off[j] = m2[j] = 0.0f;
         if (at.active) {
-            gnn_load_row<T, VEC>(X + row * ldx + at.col, pivot);
-            int64_t r = row + at.row_lane;
-            const T *x = X + r * ldx + at.col;
+            const T *x = X + (row + at.row_lane) * ldx + at.col;
             const int64_t step = s.row_lanes * ldx;
-            while (r < stop) {
+            int left = each + (at.row_lane < rest);  // rows of this thread
+            float before = 0.0f;
+            if (left > 0) {
+                float v[U][VEC];
+#pragma unroll
+                for (int u = 0; u < U; ++u) gnn_load_row<T, VEC>(x + (u < left ? u : 0) * step, v[u]);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) base[j] = v[0][j] + 0.25f * ((v[1][j] - v[0][j]) + (v[2][j] - v[0][j]) + (v[3][j] - v[0][j]));
+            }
+            while (left > 0) {
+                const int run = left < RUN ? left : RUN;
                 float t1[VEC], t2[VEC];
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) t1[j] = t2[j] = 0.0f;
-                for (int k = 0; k < 8 && r < stop; ++k, r += U * s.row_lanes, x += U * step) {
+                for (int k = 0; k < run; k += U, x += U * step) {
+                    gnn_strip<T, VEC, NT> strip[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) strip[u].load(x + (k + u < run ? u : 0) * step);
                     float v[U][VEC];
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
-                        if (r + u * s.row_lanes < stop) gnn_load_row<T, VEC, NT>(x + u * step, v[u]);
-                        else
+                        strip[u].get(v[u]);
+                        if (u > 0)
 #pragma unroll
-                            for (int j = 0; j < VEC; ++j) v[u][j] = pivot[j];
+                            for (int j = 0; j < VEC; ++j) v[u][j] = k + u < run ? v[u][j] : base[j];
                     }
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
 #pragma unroll
-                        for (int u = 0; u < U; ++u) v[u][j] -= pivot[j];
+                        for (int u = 0; u < U; ++u) v[u][j] -= base[j];
                         t1[j] += (v[0][j] + v[1][j]) + (v[2][j] + v[3][j]);
                         t2[j] += (v[0][j] * v[0][j] + v[1][j] * v[1][j]) + (v[2][j] * v[2][j] + v[3][j] * v[3][j]);
                     }
                 }
+                const float n = float(run), inv = __builtin_amdgcn_rcpf(n), share = n * __builtin_amdgcn_rcpf(before + n), weight = share * before;
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    s1[j] += t1[j];
-                    s2[j] += t2[j];
+                    const float o = t1[j] * inv, q = t2[j] - t1[j] * o;
+                    join(off[j], m2[j], o, q < 0.0f ? 0.0f : q, share, weight);
+                    const float next = base[j] + off[j];  // the next run's distances are from here
+                    off[j] -= next - base[j];
+                    base[j] = next;
                 }
+                before += n;
+                left -= run;
             }
         }
-        // the distances of all row lanes are from one row, so their sums are added as they are
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            red_1[threadIdx.x * VEC + j] = s1[j];
-            red_2[threadIdx.x * VEC + j] = s2[j];
-        }
-        add_row_lanes<VEC>(red_1, red_2, s, at, s.row_lanes);
-        const float rows = float(stop - row), inv = 1.0f / rows;
-        const int64_t begin = s.inside ? s.samples.begin(b) : 0;
-        const bool whole = s.inside && begin == row && s.samples.begin(b + 1) == stop;  // the same for all threads
-        const bool mine = at.active && at.row_lane == 0;
-        float mean[VEC], m2[VEC];
-        if (mine) {
+        if (at.active)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const float a = red_1[at.lane * VEC + j], q = red_2[at.lane * VEC + j] - a * a * inv;
-                mean[j] = pivot[j] + a * inv;
-                m2[j] = q < 0.0f ? 0.0f : q;
+                red_1[threadIdx.x * VEC + j] = double(base[j]) + double(off[j]);
+                red_2[threadIdx.x * VEC + j] = m2[j];
             }
-        }
+        join_row_lanes<VEC>(red_1, red_2, s, at, each, rest);
+        const int64_t begin = !ONE && s.inside ? s.samples.begin(b) : 0;
+        const bool whole = !ONE && s.inside && begin == row && s.samples.begin(b + 1) == stop;  // the same for all threads
+        const bool mine = at.active && at.row_lane == 0;
+        double2 v[VEC];
+        if (mine)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[j] = make_double2(red_1[at.lane * VEC + j], red_2[at.lane * VEC + j]);
         if (!whole) {
             if (mine) {
-                float2 *o = part + slot_of(s, blockIdx.x, b, begin) * s.C + at.col;
+                double2 *o = part + slot_of(s, blockIdx.x, b, begin) * s.C + at.col;
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) o[j] = make_float2(mean[j], m2[j]);
+                for (int j = 0; j < VEC; ++j) o[j] = v[j];
             }
         } else {
-            float *const means = tile_means(s, tile_lds, VEC);
-            float2 *const sums = tile_sums(s, tile_lds, VEC);
             if (mine)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) means[at.col + j] = mean[j];
+                for (int j = 0; j < VEC; ++j) means[at.col + j] = v[j].x;
             __syncthreads();
             if (mine) {
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
                     const int c = at.col + j;
-                    const float d = mean[j] - means[c - c % s.group_width];
-                    sums[c] = make_float2(rows * d, m2[j] + rows * d * d);
+                    const double d = v[j].x - means[c - c % s.group_width];
+                    sums[c] = make_double2(double(rows) * d, v[j].y + double(rows) * d * d);
                 }
             }
-            const float2 *all = group_sums(sums, sums + s.C, s.G, s.group_width, int(threadIdx.x), int(blockDim.x));
+            const double2 *all = group_sums(sums, sums + s.C, s.G, s.group_width, int(threadIdx.x), int(blockDim.x));
             for (int g = int(threadIdx.x); g < s.G; g += int(blockDim.x)) {
-                const float n = rows * float(s.group_width), off = all[g].x / n, var = all[g].y / n - off * off;
-                mean_out[b * s.G + g] = means[g * s.group_width] + off;
-                rstd_out[b * s.G + g] = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);
+                const double n = double(rows) * s.group_width, off = all[g].x / n, var = all[g].y / n - off * off;
+                mean_out[b * s.G + g] = float(means[g * s.group_width] + off);
+                rstd_out[b * s.G + g] = 1.0f / sqrtf(float(var < 0.0 ? 0.0 : var) + eps);
             }
         }
         __syncthreads();
@@ -317,11 +363,11 @@ template <int THREADS> struct Merge {
         d = int(threadIdx.x) / wide;
     }
     // f(rows of the sample in tile t, partial sums of column c there), four loads in flight
-    template <typename F> __device__ __forceinline__ void tiles(const Shape &s, const float2 *part, int64_t b, int c, F f) const {
+    template <typename V, typename F> __device__ __forceinline__ void tiles(const Shape &s, const V *part, int64_t b, int c, F f) const {
         constexpr int U = 4;
         if (d >= deep) return;
         for (int64_t t = t0 + d; t <= t1; t += U * deep) {
-            float2 v[U];
+            V v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (t + u * deep <= t1) v[u] = part[slot_of(s, t + u * deep, b, lo) * s.C + c];
@@ -350,7 +396,7 @@ __device__ __forceinline__ int64_t sample_of_pair(const Shape &s, int64_t p, int
 // Mean and reciprocal deviation of a sample and group from its parts: THREADS threads for a pair.  One sample: also for every column, as
 // the kernel that writes the result reads them.
 template <int THREADS>
-__global__ void __launch_bounds__(THREADS) norm_stats_kernel(const float2 *__restrict__ part, const Shape s, float eps, float *__restrict__ mean,
+__global__ void __launch_bounds__(THREADS) norm_stats_kernel(const double2 *__restrict__ part, const Shape s, float eps, float *__restrict__ mean,
                                                              float *__restrict__ rstd, float *__restrict__ table) {
     __shared__ double2 red[THREADS / 64];
     const int64_t tiles = (s.N + s.tile_rows - 1) / s.tile_rows;
@@ -368,10 +414,10 @@ __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const float2 *__res
             const double pivot = part[slot_of(s, m.t0, b, m.lo) * s.C + c0].x;
             double2 u = {0.0, 0.0};
             for (int k = m.k; k < s.group_width; k += m.wide)
-                m.tiles(s, part, b, c0 + k, [&](double rows, float2 v) {
-                    const double d = double(v.x) - pivot;
+                m.tiles(s, part, b, c0 + k, [&](double rows, double2 v) {
+                    const double d = v.x - pivot;
                     u.x += rows * d;
-                    u.y += double(v.y) + rows * d * d;
+                    u.y += v.y + rows * d * d;
                 });
             u = team_sum<THREADS>(u, red);
             const double n = double(m.hi - m.lo) * s.group_width, off = u.x / n;
@@ -445,18 +491,20 @@ template <int VEC> __device__ __forceinline__ int column_of_block(const Shape &s
     const int vec = int(blockIdx.y) * s.cols + int(threadIdx.x);
     return vec * VEC >= s.C ? -1 : vec * VEC < s.C - VEC ? vec * VEC : s.C - VEC;
 }
-// One sample of few tiles: the writing kernel joins their partial sums by itself, every workgroup for all columns, which costs less than a
-// launch.  f(partial, rows, column) -> what a column's tiles add up; g(group, sum over its columns) -> what the group keeps.
+// One sample of few tiles: the writing kernel joins their partial sums (V) by itself, every workgroup for all columns, which costs less than a
+// launch.  f(partial, rows, column) -> what a column's tiles add up; g(group, sum over its columns) -> what the group keeps, in as many bytes.
 // The threads are (vector of columns, row lane) of all columns.  Returns the groups' results in LDS.
-template <int VEC, typename F, typename G> __device__ __forceinline__ const float2 *join_tiles(const Shape &s, const float2 *part, int64_t tiles, int col, F f, G g) {
-    extern __shared__ float2 join_lds[];
-    float2 *const sums = join_lds, *const next = join_lds + s.row_lanes * s.C;
-    float2 u[VEC];
+template <int VEC, typename R, typename V, typename F, typename G>
+__device__ __forceinline__ const R *join_tiles(const Shape &s, const V *part, int64_t tiles, int col, F f, G g) {
+    static_assert(sizeof(R) == sizeof(V), "the results take the sums' places");
+    extern __shared__ double2 join_lds[];
+    V *const sums = reinterpret_cast<V *>(join_lds), *const next = sums + s.row_lanes * s.C;
+    V u[VEC];
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) u[j] = make_float2(0.0f, 0.0f);
-    constexpr int U = 4;
+    for (int j = 0; j < VEC; ++j) u[j] = V{0, 0};
+    constexpr int U = 64 / (VEC * int(sizeof(V) / 4)) < 4 ? 64 / (VEC * int(sizeof(V) / 4)) : 4;  // in at most 64 registers
     for (int64_t t = threadIdx.y; t < tiles; t += U * s.row_lanes) {
-        float2 v[U][VEC];
+        V v[U][VEC];
 #pragma unroll
         for (int k = 0; k < U; ++k)
             if (t + k * s.row_lanes < tiles)
@@ -478,8 +526,8 @@ template <int VEC, typename F, typename G> __device__ __forceinline__ const floa
         sums[(group * s.row_lanes + threadIdx.y) * s.group_width + col + j - group * s.group_width] = u[j];
     }
     const int i = int(threadIdx.y) * s.cols + int(threadIdx.x), threads = s.cols * s.row_lanes;
-    const float2 *all = group_sums(sums, next, s.G, s.row_lanes * s.group_width, i, threads);
-    float2 *const out = all == sums ? next : sums;
+    const V *all = group_sums(sums, next, s.G, s.row_lanes * s.group_width, i, threads);
+    R *const out = reinterpret_cast<R *>(all == sums ? next : sums);
     __syncthreads();
     for (int k = i; k < s.G; k += threads) out[k] = g(k, all[k]);
     __syncthreads();
@@ -499,7 +547,7 @@ template <typename T> __host__ __device__ constexpr int rows_of(bool backward) {
 template <typename T, int VEC, int ACT, bool NT, Stats STATS>
 __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, const float *__restrict__ gamma,
                                                          const float *__restrict__ beta, float *__restrict__ mean, float *__restrict__ rstd,
-                                                         T *__restrict__ Y, int64_t ldy, const float2 *__restrict__ part, float eps, const float *__restrict__ table) {
+                                                         T *__restrict__ Y, int64_t ldy, const double2 *__restrict__ part, float eps, const float *__restrict__ table) {
     constexpr int kRows = rows_of<T>(false);
     const int col = column_of_block<VEC>(s);
     const int64_t r0 = int64_t(blockIdx.x) * (kRows * s.row_lanes) + threadIdx.y;
@@ -525,15 +573,15 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
         fold();
     } else if constexpr (STATS == kJoin) {
         // distances from the first tile's mean of the group's first column
-        const float n = float(s.N) * float(s.group_width);
-        const float2 *stat = join_tiles<VEC>(s, part, (s.N + s.tile_rows - 1) / s.tile_rows, col,
-            [&](float2 v, float rows, int c) {
-                const float d = v.x - part[c - c % s.group_width].x;
-                return make_float2(rows * d, v.y + rows * d * d);
+        const double inv = 1.0 / (double(s.N) * s.group_width);
+        const float4 *stat = join_tiles<VEC, float4>(s, part, (s.N + s.tile_rows - 1) / s.tile_rows, col,
+            [&](double2 v, float rows, int c) {
+                const double d = v.x - part[c - c % s.group_width].x;
+                return make_double2(double(rows) * d, v.y + double(rows) * d * d);
             },
-            [&](int g, float2 u) {
-                const float off = u.x / n, var = u.y / n - off * off;
-                const float2 r = make_float2(part[g * s.group_width].x + off, 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps));
+            [&](int g, double2 u) {
+                const double off = u.x * inv, var = u.y * inv - off * off;
+                const float4 r = make_float4(float(part[g * s.group_width].x + off), 1.0f / sqrtf(float(var < 0.0 ? 0.0 : var) + eps), 0.0f, 0.0f);
                 if (blockIdx.x == 0) {
                     mean[g] = r.x;
                     rstd[g] = r.y;
@@ -571,14 +619,15 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restr
                                                                  const float *__restrict__ gamma, const float *__restrict__ beta,
                                                                  const float *__restrict__ mean, const float *__restrict__ rstd,
                                                                  float2 *__restrict__ part, float2 *__restrict__ total, float2 *__restrict__ sums_out) {
-    extern __shared__ float tile_lds[];
-    float *const red_1 = tile_lds, *const red_x = tile_lds + blockDim.x * VEC;
+    extern __shared__ double tile_lds[];
+    float *const red_1 = reinterpret_cast<float *>(tile_lds), *const red_x = red_1 + blockDim.x * VEC;
+    float2 *const sums = reinterpret_cast<float2 *>(tile_lds);
     const Place<VEC> at(s);
     const Affine<VEC> aff(s, at.col, gamma, beta);
     float t1[VEC], tx[VEC];
 #pragma unroll
     for (int j = 0; j < VEC; ++j) t1[j] = tx[j] = 0.0f;
-    for_parts(s, [&](int64_t b, int64_t row, int64_t stop) {
+    for_parts<false>(s, [&](int64_t b, int64_t row, int64_t stop) {
         constexpr int U = 4;
         float a1[VEC], ax[VEC];
 #pragma unroll
@@ -632,19 +681,27 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restr
         add_row_lanes<VEC>(red_1, red_x, s, at, s.row_lanes);
         const int64_t begin = s.inside ? s.samples.begin(b) : 0;
         const bool whole = s.inside && begin == row && s.samples.begin(b + 1) == stop;  // the same for all threads
-        float2 *const sums = tile_sums(s, tile_lds, VEC);
-        if (at.active && at.row_lane == 0) {
-            float2 *o = part + (whole ? 0 : slot_of(s, blockIdx.x, b, begin)) * s.C + at.col;
+        const bool mine = at.active && at.row_lane == 0;
+        float u1[VEC], ux[VEC];
+        if (mine) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const float u1 = red_1[at.lane * VEC + j], ux = red_x[at.lane * VEC + j];
-                if (whole) sums[at.col + j] = make_float2(u1 * aff.gamma[j], ux * aff.gamma[j]);
-                else o[j] = make_float2(u1, ux);
-                t1[j] += u1;
-                tx[j] += ux;
+                u1[j] = red_1[at.lane * VEC + j];
+                ux[j] = red_x[at.lane * VEC + j];
+                t1[j] += u1[j];
+                tx[j] += ux[j];
+            }
+            if (!whole) {
+                float2 *o = part + slot_of(s, blockIdx.x, b, begin) * s.C + at.col;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) o[j] = make_float2(u1[j], ux[j]);
             }
         }
         if (whole && sums_out) {
+            __syncthreads();
+            if (mine)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) sums[at.col + j] = make_float2(u1[j] * aff.gamma[j], ux[j] * aff.gamma[j]);
             const float2 *all = group_sums(sums, sums + s.C, s.G, s.group_width, int(threadIdx.x), int(blockDim.x));
             const float n = float(stop - row) * float(s.group_width);
             for (int g = int(threadIdx.x); g < s.G; g += int(blockDim.x)) sums_out[b * s.G + g] = make_float2(all[g].x / n, all[g].y / n);
@@ -792,7 +849,7 @@ __global__ void __launch_bounds__(512) norm_bwd_apply_kernel(const T *__restrict
         }
     } else if constexpr (STATS == kJoin) {
         const float n = float(s.N) * float(s.group_width);
-        const float2 *stat = join_tiles<VEC>(s, part, (s.N + s.tile_rows - 1) / s.tile_rows, col,
+        const float2 *stat = join_tiles<VEC, float2>(s, part, (s.N + s.tile_rows - 1) / s.tile_rows, col,
             [&](float2 v, float, int c) {
                 const float k = gamma ? gamma[c] : 1.0f;
                 return make_float2(v.x * k, v.y * k);
@@ -1433,7 +1490,10 @@ Layout layout_of(int64_t N, int64_t C, int64_t G, int64_t B, bool backward) {
     L.parts = L.inside ? 2 * L.tiles : L.tiles + B;
     const int64_t small = B < kSmallParts ? B : kSmallParts;
     if (backward && L.parts < small) L.parts = small;
-    int64_t off = round_up(L.parts * C * int64_t(sizeof(float2)), 256);
+    // (a backward call's workspace does for the forward call, too)
+    const int64_t moments = L.inside ? 2 * L.tiles : L.tiles + B;
+    int64_t off = round_up(L.parts * C * int64_t(sizeof(float2)) > moments * C * int64_t(sizeof(double2)) ? L.parts * C * int64_t(sizeof(float2))
+                                                                                                          : moments * C * int64_t(sizeof(double2)), 256);
     L.map_off = off;
     if (B > 1) off += round_up(N * 4, 256);
     L.table_off = off;
@@ -1526,23 +1586,26 @@ template <typename T, int PART, int OUT, int ACT, bool NT> int run_tiles(const C
     T *out = static_cast<T *>(c.out);
     hipStream_t stream = c.stream();
     float2 *part = reinterpret_cast<float2 *>(c.scratch(0));
+    double2 *moments = reinterpret_cast<double2 *>(c.scratch(0));
     float *table = c.B == 1 ? reinterpret_cast<float *>(c.scratch(c.L.table_off)) : nullptr;
     const int64_t pairs = (c.L.inside && c.B > c.L.tiles ? c.L.tiles : c.B) * c.G;
     const unsigned many = unsigned(pairs < 65536 ? pairs : 65536);
-    const int64_t finish = c.L.inside ? (c.C + 1) / 2 * 2 + 2 * (c.C + c.G * ((c.C / c.G + 15) / 16)) : 0;  // floats: tile_means, tile_sums
-    const size_t lds = (size_t(threads.x) * PART * 2 + size_t(finish)) * sizeof(float);
+    size_t lds;
+    if (c.backward) lds = size_t(tile_values<float2>(threads.x, PART, 2, c.C, c.G, c.L.inside)) * sizeof(float);
+    else lds = size_t(tile_values<double2>(threads.x, PART, 3, c.C, c.G, c.L.inside) + (c.L.inside ? 2 * c.C : 0)) * sizeof(float);
     // what join_tiles keeps: the sums of every row lane, and a sixteenth
-    const size_t values = size_t(w.row_lanes) * size_t(c.C), join = (values + c.G * ((values / c.G + 15) / 16)) * sizeof(float2);
+    const size_t values = size_t(w.row_lanes) * size_t(c.C), join = (values + c.G * ((values / c.G + 15) / 16)) * (c.backward ? sizeof(float2) : sizeof(double2));
     if (!c.backward) {
         if (c.L.joined) {
-            norm_part_kernel<T, PART, false, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part, c.o.eps, c.mean, c.rstd);
-            norm_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, part, c.o.eps, nullptr);
+            norm_part_kernel<T, PART, false, kThreads, true><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd);
+            norm_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, moments, c.o.eps, nullptr);
         } else {
-            auto *sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads> : norm_part_kernel<T, PART, NT, kLargeThreads>;
-            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, s, part, c.o.eps, c.mean, c.rstd);
-            if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd, table);
-            else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd, table);
-            else norm_stats_kernel<64><<<many, 64, 0, stream>>>(part, s, c.o.eps, c.mean, c.rstd, table);
+            auto *sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, false> : norm_part_kernel<T, PART, NT, kLargeThreads, false>;
+            if (c.B == 1) sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, true> : norm_part_kernel<T, PART, NT, kLargeThreads, true>;
+            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd);
+            if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, table);
+            else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, table);
+            else norm_stats_kernel<64><<<many, 64, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, table);
             auto *apply = c.B == 1 ? norm_apply_kernel<T, OUT, ACT, NT, kOne> : norm_apply_kernel<T, OUT, ACT, NT, kMany>;
             apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, nullptr, 0.0f, table);
         }
