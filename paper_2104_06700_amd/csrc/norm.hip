@@ -18,6 +18,8 @@
 #include "common.h"
 #include "rows.h"
 
+#include <type_traits>
+
 namespace {
 
 // Tiles of at least kTileValues values, at most kTiles of them with kThreads threads each; matrices of kLarge values and more in kLargeTiles with
@@ -76,6 +78,17 @@ __device__ __forceinline__ float gradient(float dz, float gamma, float xh, float
     const float t = dz * gamma;
     const float u = t - s.x;
     return r * __builtin_fmaf(-xh, s.y, u);
+}
+
+// a b, rounded: not part of a fused operation that takes distances from the product as it was before
+__device__ __forceinline__ float product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+// sum / n with inv = 1 / n: what the product with inv is off by is taken back, so that the mean of equal values is that value
+__device__ __forceinline__ float quotient(float sum, float n, float inv) {
+    const float q = sum * inv;
+    return __builtin_fmaf(__builtin_fmaf(-q, n, sum), inv, q);
 }
 
 struct Shape {
@@ -184,6 +197,10 @@ template <typename M> __device__ __forceinline__ void join(M &mean, float &m2, M
     m2 += other_m2 + float(d) * float(d) * weight;
 }
 
+// What a mean loses when it is rounded to fp32.  The results are formed from both: of values whose mean is 10,000 times their deviation a half unit of
+// the mean's last place is 5e-4 of the deviation.
+__device__ __forceinline__ float rounding(double mean) { return float(mean - double(float(mean))); }
+
 // The moments of a tile's row lanes, each of `each` rows and one more in the first `rest` lanes, are joined in LDS: mean and m2
 // [row_lanes][cols * VEC], the result in row lane 0's places.
 template <int VEC> __device__ __forceinline__ void join_row_lanes(double *mean, float *m2, const Shape &s, const Place<VEC> &at, int each, int rest) {
@@ -212,7 +229,7 @@ template <int VEC> __device__ __forceinline__ void join_row_lanes(double *mean, 
 // row in front of 16,384 of mean 100 and deviation 1 costs rstd 4e-4.
 template <typename T, int VEC, bool NT, int THREADS, bool ONE>
 __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, double2 *__restrict__ part, float eps,
-                                                             float *__restrict__ mean_out, float *__restrict__ rstd_out) {
+                                                             float *__restrict__ mean_out, float *__restrict__ rstd_out, float *__restrict__ low) {
     extern __shared__ double tile_lds[];
     double *const red_1 = tile_lds;
     float *const red_2 = reinterpret_cast<float *>(tile_lds + blockDim.x * VEC);
@@ -225,7 +242,7 @@ __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict_
                 for (int g = 0; g < s.G; ++g) {
                     mean_out[b * s.G + g] = 0.0f;
                     rstd_out[b * s.G + g] = 1.0f / sqrtf(eps);
-                }
+                }  // (no row asks for their part of `low`)
     for_parts<ONE>(s, [&](int64_t b, int64_t row, int64_t stop) {
         constexpr int U = 4, RUN = 32;
         const int rows = int(stop - row), each = int(unsigned(rows) / unsigned(s.row_lanes)), rest = rows - each * s.row_lanes;
@@ -303,6 +320,7 @@ __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict_
                 for (int j = 0; j < VEC; ++j) o[j] = v[j];
             }
         } else {
+            const double inv = 1.0 / (double(rows) * s.group_width);
             if (mine)
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) means[at.col + j] = v[j].x;
@@ -317,8 +335,9 @@ __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict_
             }
             const double2 *all = group_sums(sums, sums + s.C, s.G, s.group_width, int(threadIdx.x), int(blockDim.x));
             for (int g = int(threadIdx.x); g < s.G; g += int(blockDim.x)) {
-                const double n = double(rows) * s.group_width, off = all[g].x / n, var = all[g].y / n - off * off;
-                mean_out[b * s.G + g] = float(means[g * s.group_width] + off);
+                const double off = all[g].x * inv, var = all[g].y * inv - off * off, mid = means[g * s.group_width] + off;
+                mean_out[b * s.G + g] = float(mid);
+                low[b * s.G + g] = rounding(mid);
                 rstd_out[b * s.G + g] = 1.0f / sqrtf(float(var < 0.0 ? 0.0 : var) + eps);
             }
         }
@@ -397,7 +416,7 @@ __device__ __forceinline__ int64_t sample_of_pair(const Shape &s, int64_t p, int
 // the kernel that writes the result reads them.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const double2 *__restrict__ part, const Shape s, float eps, float *__restrict__ mean,
-                                                             float *__restrict__ rstd, float *__restrict__ table) {
+                                                             float *__restrict__ rstd, float *__restrict__ low, float *__restrict__ table) {
     __shared__ double2 red[THREADS / 64];
     const int64_t tiles = (s.N + s.tile_rows - 1) / s.tile_rows;
     const int64_t pairs = (s.inside && s.samples.count > tiles ? tiles : s.samples.count) * s.G;
@@ -429,11 +448,13 @@ __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const double2 *__re
         if (threadIdx.x == 0) {
             mean[p] = float(mid);
             rstd[p] = r;
+            low[p] = rounding(mid);
         }
         if (table)
             for (int k = int(threadIdx.x); k < s.group_width; k += THREADS) {
                 table[c0 + k] = float(mid);
                 table[s.C + c0 + k] = r;
+                table[2 * int64_t(s.C) + c0 + k] = rounding(mid);
             }
     }
 }
@@ -547,7 +568,7 @@ template <typename T> __host__ __device__ constexpr int rows_of(bool backward) {
 template <typename T, int VEC, int ACT, bool NT, Stats STATS>
 __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, const float *__restrict__ gamma,
                                                          const float *__restrict__ beta, float *__restrict__ mean, float *__restrict__ rstd,
-                                                         T *__restrict__ Y, int64_t ldy, const double2 *__restrict__ part, float eps, const float *__restrict__ table) {
+                                                         const float *__restrict__ low, T *__restrict__ Y, int64_t ldy, const double2 *__restrict__ part, float eps, const float *__restrict__ table) {
     constexpr int kRows = rows_of<T>(false);
     const int col = column_of_block<VEC>(s);
     const int64_t r0 = int64_t(blockIdx.x) * (kRows * s.row_lanes) + threadIdx.y;
@@ -557,18 +578,23 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
     for (int u = 0; u < kRows; ++u)
         if (r0 + u * s.row_lanes < s.N) strip[u].load(X + (r0 + u * s.row_lanes) * ldx + col);
     const Affine<VEC> aff(s, col, gamma, beta);
-    float w[VEC], o[VEC];  // z = (x - o) w + beta: a value that is the mean gives beta, whatever rstd is
+    float w[VEC], o[VEC], l[VEC], bt[VEC];  // z = (x - o) w + (beta - l w): the mean is o + l.  A value that is the mean gives beta where rstd is finite
     auto fold = [&]() {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) w[j] *= aff.gamma[j];
+        for (int j = 0; j < VEC; ++j) {
+            w[j] *= aff.gamma[j];
+            bt[j] = aff.beta[j] - l[j] * w[j];
+        }
     };
     if constexpr (STATS == kOne) {
-        if (s.group_width % VEC == 0) {  // a vector has one group: its two values instead of two vectors
+        if (s.group_width % VEC == 0) {  // a vector has one group: its three values instead of three vectors
             aff.gather(s, mean, 0, o);
             aff.gather(s, rstd, 0, w);
+            aff.gather(s, low, 0, l);
         } else {
             Affine<VEC>::columns(table + col, o);
             Affine<VEC>::columns(table + s.C + col, w);
+            Affine<VEC>::columns(table + 2 * int64_t(s.C) + col, l);
         }
         fold();
     } else if constexpr (STATS == kJoin) {
@@ -580,8 +606,8 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
                 return make_double2(double(rows) * d, v.y + double(rows) * d * d);
             },
             [&](int g, double2 u) {
-                const double off = u.x * inv, var = u.y * inv - off * off;
-                const float4 r = make_float4(float(part[g * s.group_width].x + off), 1.0f / sqrtf(float(var < 0.0 ? 0.0 : var) + eps), 0.0f, 0.0f);
+                const double off = u.x * inv, var = u.y * inv - off * off, mid = part[g * s.group_width].x + off;
+                const float4 r = make_float4(float(mid), 1.0f / sqrtf(float(var < 0.0 ? 0.0 : var) + eps), rounding(mid), 0.0f);
                 if (blockIdx.x == 0) {
                     mean[g] = r.x;
                     rstd[g] = r.y;
@@ -592,6 +618,7 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
         for (int j = 0; j < VEC; ++j) {
             o[j] = stat[aff.group[j]].x;
             w[j] = stat[aff.group[j]].y;
+            l[j] = stat[aff.group[j]].z;
         }
         fold();
     }
@@ -603,12 +630,13 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
             const int64_t b = sample_of_row(s, r);
             aff.gather(s, mean, b, o);
             aff.gather(s, rstd, b, w);
+            aff.gather(s, low, b, l);
             fold();
         }
         float x[VEC];
         strip[u].get(x);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) x[j] = activate<ACT>((x[j] - o[j]) * w[j] + aff.beta[j]);
+        for (int j = 0; j < VEC; ++j) x[j] = activate<ACT>((x[j] - o[j]) * w[j] + bt[j]);
         gnn_store_row<T, VEC, NT>(Y + r * ldy + col, x);
     }
 }
@@ -895,15 +923,22 @@ struct Small {
     int groups;        // of a team (blockIdx.y: which); the last one may have fewer
     int cols, lanes, team, teams;
     int len;           // partial sums of a group: lanes x K, or x K / VEC where vectors lie inside groups
-    int team_sums;     // of a team in LDS
+    int team_sums;     // pairs of a team in LDS
 };
 
-template <int VEC, bool INSIDE, typename V> struct Team {
+// How vectors lie: inside groups; across groups; across groups, and there is a slice of fewer columns than a vector has
+enum Vectors { kInside, kAcross, kShort };
+
+// WHOLE: a thread with columns has a whole vector.  Without the partial loads and stores the forward kernel takes a fifth fewer registers (612 graphs of
+// 100 vertices x 128 fp32 in 16 groups 23 -> 17 us); the backward kernel is faster so across groups (2,449 graphs of 25 x 100 bf16 49 -> 44), slower
+// inside (x 64 fp32 27 -> 30).
+template <int VEC, Vectors HOW, bool WHOLE> struct Team {
+    static constexpr bool INSIDE = HOW == kInside, kWhole = WHOLE;
     int team, i, lane, row_lane, col, have, c0, groups;
     bool active;
-    V *sums;
+    float2 *room;  // of the team's sums, a value or a pair each
     int g0, k0;  // group of the first column, and its place there
-    __device__ __forceinline__ Team(const Small &s, V *lds) {
+    __device__ __forceinline__ Team(const Small &s, float2 *lds) {
         team = int(threadIdx.x / unsigned(s.team));
         i = int(threadIdx.x) - team * s.team;
         row_lane = int(unsigned(i) / unsigned(s.cols));
@@ -915,7 +950,7 @@ template <int VEC, bool INSIDE, typename V> struct Team {
         col = lane * VEC < columns - VEC || columns < VEC ? lane * VEC : columns - VEC;
         have = lane * VEC >= columns ? 0 : columns < VEC ? columns : VEC;
         active = team < s.teams && row_lane < s.lanes && have > 0;
-        sums = lds + (team < s.teams ? team : 0) * s.team_sums;
+        room = lds + (team < s.teams ? team : 0) * s.team_sums;
         g0 = int(unsigned(col) / unsigned(s.K));
         k0 = col - g0 * s.K;
     }
@@ -924,7 +959,7 @@ template <int VEC, bool INSIDE, typename V> struct Team {
         int g = g0, k = k0, at = g0 * s.len + row_lane * s.K + k0;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            if (j < have) f(j, g, at);
+            if (kWhole || j < have) f(j, g, at);
             if constexpr (!INSIDE) {
                 ++at;
                 if (++k == s.K) {
@@ -937,13 +972,16 @@ template <int VEC, bool INSIDE, typename V> struct Team {
     }
     // the sums of every group over the team's threads' v; the places that are returned hold them until the next call.  Sixteen to one at a
     // time; all threads of the workgroup call it together.
-    __device__ __forceinline__ const V *reduce(const Small &s, const V (&v)[VEC]) const {
+    // (v: of every column, or one of all columns of a vector that lies inside a group)
+    template <typename V, int S> __device__ __forceinline__ const V *reduce(const Small &s, const V (&v)[S]) const {
+        static_assert(S == VEC || (INSIDE && S == 1), "columns");
+        V *const sums = reinterpret_cast<V *>(room);
         __syncthreads();
         if (active) {
             if constexpr (INSIDE) {
                 V t = v[0];
 #pragma unroll
-                for (int j = 1; j < VEC; ++j) add_to(t, v[j]);
+                for (int j = 1; j < S; ++j) add_to(t, v[j]);
                 sums[g0 * s.len + row_lane * (s.K / VEC) + k0 / VEC] = t;
             } else {
                 columns(s, [&](int j, int, int at) { sums[at] = v[j]; });
@@ -959,7 +997,7 @@ template <typename T, typename P> struct Held {
     static constexpr int VEC = gnn_rows<T>::VEC;
     typename gnn_rows<T>::raw v[held<T>()];
     __device__ __forceinline__ static typename gnn_rows<T>::raw one(const P &t, const T *p) {
-        if (t.have == VEC) return gnn_rows<T>::fetch(p);
+        if (P::kWhole || t.have == VEC) return gnn_rows<T>::fetch(p);
         float f[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) f[j] = j < t.have ? gnn_rows<T>::get(p + j) : 0.0f;
@@ -980,7 +1018,7 @@ template <typename T, typename P> struct Held {
 };
 template <typename T, typename P> __device__ __forceinline__ void put_row(const P &t, T *q, const float (&f)[gnn_rows<T>::VEC]) {
     constexpr int VEC = gnn_rows<T>::VEC;
-    if (t.have == VEC) gnn_store_row<T, VEC>(q, f);
+    if (P::kWhole || t.have == VEC) gnn_store_row<T, VEC>(q, f);
     else
 #pragma unroll
         for (int j = 0; j < VEC; ++j)
@@ -1000,22 +1038,20 @@ struct Span {
     }
 };
 
-// Forward.  Mean first, then the squared distances from it, both from the registers.
-template <typename T, int ACT, bool INSIDE>
+// Forward.  Mean first, then the distances from it and their squares, both from the registers; the distances' mean takes off the rounding of the first (as in
+// row_kernel).
+template <typename T, int ACT, Vectors HOW>
 __global__ void __launch_bounds__(1024) small_kernel(const T *X, int64_t ldx, const Small s, const float *__restrict__ gamma,
                                                      const float *__restrict__ beta, float eps, float *__restrict__ mean, float *__restrict__ rstd,
                                                      T *Y, int64_t ldy) {
-    extern __shared__ float small_lds[];
+    extern __shared__ float2 small_lds2[];
     constexpr int VEC = gnn_rows<T>::VEC;
-    typedef Team<VEC, INSIDE, float> P;
-    const P t(s, small_lds);
-    float gm[VEC], bt[VEC];
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-        const int c = t.c0 + t.col + j;
-        gm[j] = gamma && j < t.have ? gamma[c] : 1.0f;
-        bt[j] = beta && j < t.have ? beta[c] : 0.0f;
-    }
+    typedef Team<VEC, HOW, HOW != kShort> P;
+    const P t(s, small_lds2);
+    // gamma and beta wait in LDS: in registers they are what a third workgroup of 512 threads a CU has no room for
+    float2 *const affine = small_lds2 + s.teams * s.team_sums;
+    for (int c = int(threadIdx.x); c < t.groups * s.K; c += int(blockDim.x))
+        affine[c] = make_float2(gamma ? gamma[t.c0 + c] : 1.0f, beta ? beta[t.c0 + c] : 0.0f);  // read behind the sums' barriers
     const int64_t xstep = s.lanes * ldx, ystep = s.lanes * ldy;
     for (int64_t b0 = int64_t(blockIdx.x) * s.teams; b0 < s.samples.count; b0 += int64_t(gridDim.x) * s.teams) {
         const int64_t b = b0 + t.team;
@@ -1023,52 +1059,104 @@ __global__ void __launch_bounds__(1024) small_kernel(const T *X, int64_t ldx, co
         const T *x = X + (n.lo + t.row_lane) * ldx + t.c0 + t.col;
         Held<T, P> h;
         h.fetch(t, x, xstep, n.mine);
-        const float inv = 1.0f / (float(n.rows > 0 ? n.rows : 1) * float(s.K));
+        const float count = float(n.rows > 0 ? n.rows : 1) * float(s.K), inv = 1.0f / count;
         // sums over the thread's rows; beyond the registers by thirty-two at a time, so that long sums do not lose bits
-        auto sum_rows = [&](float (&a)[VEC], auto term) {
+        // (by column, or of a vector's columns where it has one group)
+        constexpr bool INSIDE = P::INSIDE;
+        constexpr int S = INSIDE ? 1 : VEC;
+        auto add_row = [&](auto (&to)[S], const float (&f)[VEC], auto term) {
+            auto v = term(f[0], 0);
+            if constexpr (INSIDE) {
+                decltype(v) w[VEC];
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) a[j] = 0.0f;
+                for (int j = 0; j < VEC; ++j) w[j] = term(f[j], j);
+#pragma unroll
+                for (int d = VEC / 2; d > 0; d /= 2)
+#pragma unroll
+                    for (int j = 0; j < d; ++j) add_to(w[j], w[j + d]);
+                add_to(to[0], w[0]);
+            } else {
+                add_to(to[0], v);
+#pragma unroll
+                for (int j = 1; j < VEC; ++j) add_to(to[j], term(f[j], j));
+            }
+        };
+        auto sum_rows = [&](auto (&a)[S], auto term) {
+            typedef decltype(term(0.0f, 0)) V;
+#pragma unroll
+            for (int j = 0; j < S; ++j) a[j] = V{};
 #pragma unroll
             for (int k = 0; k < held<T>(); ++k)
                 if (k < n.mine) {
                     float f[VEC];
                     h.get(k, f);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) a[j] += term(f[j], j);
+                    add_row(a, f, term);
                 }
 #pragma clang loop unroll(disable)
             for (int k0 = held<T>(); k0 < n.mine; k0 += 32) {
-                float part[VEC];
+                V part[S];
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) part[j] = 0.0f;
+                for (int j = 0; j < S; ++j) part[j] = V{};
 #pragma clang loop unroll(disable)
                 for (int k = k0; k < k0 + 32 && k < n.mine; ++k) {
                     float f[VEC];
                     h.get_far(t, x, xstep, k, f);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) part[j] += term(f[j], j);
+                    add_row(part, f, term);
                 }
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) a[j] += part[j];
+                for (int j = 0; j < S; ++j) add_to(a[j], part[j]);
             }
         };
-        float a[VEC], m[VEC];
+        float m[VEC];
+        const float *sum;
+        {
+            float a[S];
+            sum_rows(a, [](float f, int) { return f; });
+            sum = t.reduce(s, a);
+        }
 #pragma unroll
         for (int j = 0; j < VEC; ++j) m[j] = 0.0f;
-        sum_rows(a, [](float f, int) { return f; });
-        const float *sum = t.reduce(s, a);
-        t.columns(s, [&](int j, int g, int) { m[j] = sum[g] * inv; });
-        if (n.there)
-            for (int g = t.i; g < t.groups; g += s.team) mean[b * s.G + int(blockIdx.y) * s.groups + g] = sum[g] * inv;
-        sum_rows(a, [&](float f, int j) { return (f - m[j]) * (f - m[j]); });
-        sum = t.reduce(s, a);
-        t.columns(s, [&](int j, int g, int) { a[j] = (1.0f / sqrtf(sum[g] * inv + eps)) * gm[j]; });
-        if (n.there)
-            for (int g = t.i; g < t.groups; g += s.team) rstd[b * s.G + int(blockIdx.y) * s.groups + g] = 1.0f / sqrtf(sum[g] * inv + eps);
+        t.columns(s, [&](int j, int g, int) { m[j] = product(sum[g], inv); });
+        float *const first = reinterpret_cast<float *>(t.room + s.team_sums - ((s.groups + 1) >> 1));  // by group: kept for the same threads
+        if (t.team < s.teams)
+            for (int g = t.i; g < t.groups; g += s.team) first[g] = product(sum[g], inv);
+        float2 b2[S];
+        sum_rows(b2, [&](float f, int j) {
+            const float d = f - m[j];
+            return make_float2(d, d * d);
+        });
+        float2 *const both = const_cast<float2 *>(t.reduce(s, b2));
+        // a group's thread turns its sums into the rest of the mean and the reciprocal deviation: every column's thread by itself is more registers
+        // than bf16 has
+        for (int g = t.i; g < t.groups && t.team < s.teams; g += s.team) {
+            const float rest = quotient(both[g].x, count, inv), var = both[g].y * inv - rest * rest;
+            const float r = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);
+            both[g] = make_float2(rest, r);
+            if (n.there) {
+                const int64_t p = b * s.G + int(blockIdx.y) * s.groups + g;
+                mean[p] = first[g] + rest;
+                rstd[p] = r;
+            }
+        }
+        __syncthreads();
+        float a[VEC], e[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) a[j] = e[j] = 0.0f;
+        t.columns(s, [&](int j, int g, int) {
+            e[j] = both[g].x;
+            a[j] = both[g].y;
+        });
+        float bt[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float2 p = j < t.have ? affine[t.col + j] : make_float2(0.0f, 0.0f);
+            a[j] *= p.x;
+            bt[j] = p.y;
+        }
         T *y = Y + (n.lo + t.row_lane) * ldy + t.c0 + t.col;
         auto write = [&](int k, float (&f)[VEC]) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) f[j] = activate<ACT>((f[j] - m[j]) * a[j] + bt[j]);
+            for (int j = 0; j < VEC; ++j) f[j] = activate<ACT>(((f[j] - m[j]) - e[j]) * a[j] + bt[j]);
             put_row<T>(t, y + k * ystep, f);
         };
 #pragma unroll
@@ -1089,14 +1177,14 @@ __global__ void __launch_bounds__(1024) small_kernel(const T *X, int64_t ldx, co
 
 // Backward.  A workgroup adds up its samples' column sums for dbeta and dgamma and leaves them in its row of `part`.  In fp32 the registers
 // of X and dY take xh and dz, so that the activation's derivative is formed once; bf16 pairs are unpacked twice.
-template <typename T, int ACT, bool INSIDE>
+template <typename T, int ACT, Vectors HOW>
 __global__ void __launch_bounds__(512) small_bwd_kernel(const T *X, int64_t ldx, const T *dY, int64_t ldy, const Small s,
                                                         const float *__restrict__ gamma, const float *__restrict__ beta, const float *__restrict__ mean,
                                                         const float *__restrict__ rstd, T *dX, int64_t lddx, float2 *__restrict__ part) {
     extern __shared__ float2 small_lds2[];
     constexpr int VEC = gnn_rows<T>::VEC;
     constexpr bool KEEP = VEC == 4;
-    typedef Team<VEC, INSIDE, float2> P;
+    typedef Team<VEC, HOW, HOW == kAcross> P;
     const P t(s, small_lds2);
     float gm[VEC], bt[VEC];
     float2 total[VEC];
@@ -1247,15 +1335,21 @@ struct PerRow {
 };
 constexpr int kRowThreads = 256;
 
-// sum over `width` neighbouring lanes, in all of them; all lanes of the wavefront are here
-__device__ __forceinline__ float add_lanes(float v, int width) {
-    if (width >= 2) v += gnn_from_lane<0xB1>(v);    // the other of a pair
-    if (width >= 4) v += gnn_from_lane<0x4E>(v);    // the other pair of four
-    if (width >= 8) v += gnn_from_lane<0x141>(v);   // mirrored in eight: the other four
-    if (width >= 16) v += gnn_from_lane<0x140>(v);  // mirrored in sixteen: the other eight
-    if (width >= 32) v += __shfl_xor(v, 16);
-    if (width >= 64) v += __shfl_xor(v, 32);
-    return v;
+// sums of M values over `width` neighbouring lanes, in all of them; all lanes of the wavefront are here
+template <int M> __device__ __forceinline__ void add_lanes(float (&v)[M], int width) {
+    const auto step = [&](auto other) {
+        float o[M];
+#pragma unroll
+        for (int i = 0; i < M; ++i) o[i] = other(v[i]);
+#pragma unroll
+        for (int i = 0; i < M; ++i) v[i] += o[i];
+    };
+    if (width >= 2) step([](float f) { return gnn_from_lane<0xB1>(f); });    // the other of a pair
+    if (width >= 4) step([](float f) { return gnn_from_lane<0x4E>(f); });    // the other pair of four
+    if (width >= 8) step([](float f) { return gnn_from_lane<0x141>(f); });   // mirrored in eight: the other four
+    if (width >= 16) step([](float f) { return gnn_from_lane<0x140>(f); });  // mirrored in sixteen: the other eight
+    if (width >= 32) step([](float f) { return __shfl_xor(f, 16); });
+    if (width >= 64) step([](float f) { return __shfl_xor(f, 32); });
 }
 
 // The last vector of a row ends with it; its first `skip` columns are the vector's before it, computed by both to the same bits and counted there.
@@ -1275,19 +1369,21 @@ template <int VEC, int NV> struct RowPlace {
             skip[i] = active[i] ? c - col[i] : VEC;
         }
     }
-    // a[i]: of vector i; sums of the groups they belong to
-    __device__ __forceinline__ void groups(const PerRow &s, float (&a)[NV]) const {
+    // a[i]: of vector i; sums of the groups they belong to.  Of two quantities at once: the second's steps wait with the first's
+    template <int M> __device__ __forceinline__ void groups(const PerRow &s, float (&a)[M]) const {
+        static_assert(M % NV == 0, "a value for every vector");
         if (s.G == 1) {
-            float t = a[0];
+            float t[M / NV];
 #pragma unroll
-            for (int i = 1; i < NV; ++i) t += a[i];
-            t = add_lanes(t, s.width);
+            for (int k = 0; k < M / NV; ++k) {
+                t[k] = a[k * NV];
 #pragma unroll
-            for (int i = 0; i < NV; ++i) a[i] = t;
-        } else {
+                for (int i = 1; i < NV; ++i) t[k] += a[k * NV + i];
+            }
+            add_lanes(t, s.width);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) a[i] = add_lanes(a[i], s.width);
-        }
+            for (int i = 0; i < M; ++i) a[i] = t[i / NV];
+        } else add_lanes(a, s.width);
     }
     template <typename T, bool NT> __device__ __forceinline__ void load(gnn_strip<T, VEC, NT> (&x)[NV], const T *row, bool there) const {
 #pragma unroll
@@ -1325,43 +1421,45 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const T *__restrict__ 
     at.columns(gamma, 1.0f, gm);
     at.columns(beta, 0.0f, bt);
     const float inv = 1.0f / float(s.K);
+    // The mean of the values as they are is off by its own rounding, units of its last place; their distances f from it (m) are not.  The distances' mean e
+    // completes it, and their squares' mean gives the variance.  All rows' sums go together: their steps wait for each other's lanes.
+    constexpr int M = R * NV;
+    float f[M][VEC], m[M], e[2 * M], *const q = e + M;
 #pragma unroll
-    for (int u = 0; u < R; ++u) {
-        const int64_t r = r0 + u * at.units;
-        float f[NV][VEC], m[NV], q[NV];
+    for (int i = 0; i < M; ++i) {
+        x[i / NV][i % NV].get(f[i]);
+        m[i] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            x[u][i].get(f[i]);
-            m[i] = 0.0f;
+        for (int j = 0; j < VEC; ++j) m[i] += j >= at.skip[i % NV] ? f[i][j] : 0.0f;
+    }
+    at.groups(s, m);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) m[i] += j >= at.skip[i] ? f[i][j] : 0.0f;
+    for (int i = 0; i < M; ++i) {
+        m[i] = product(m[i], inv);
+        e[i] = q[i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            f[i][j] -= m[i];
+            e[i] += j >= at.skip[i % NV] ? f[i][j] : 0.0f;
+            q[i] += j >= at.skip[i % NV] ? f[i][j] * f[i][j] : 0.0f;
         }
-        at.groups(s, m);
+    }
+    at.groups(s, e);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            m[i] *= inv;
-            q[i] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                f[i][j] -= m[i];
-                q[i] += j >= at.skip[i] ? f[i][j] * f[i][j] : 0.0f;
-            }
+    for (int n = 0; n < M; ++n) {
+        const int i = n % NV;
+        const int64_t r = r0 + n / NV * at.units;
+        if (r >= s.N || !at.active[i]) continue;
+        e[n] = quotient(e[n], float(s.K), inv);
+        const float var = q[n] * inv - e[n] * e[n], k = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);
+        if ((at.lane & (s.width - 1)) == 0 && (i == 0 || s.G > 1)) {
+            const int64_t p = r * s.G + at.col[i] / s.K;
+            mean[p] = m[n] + e[n];
+            rstd[p] = k;
         }
-        at.groups(s, q);
-        if (r >= s.N) continue;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (!at.active[i]) continue;
-            const float k = 1.0f / sqrtf(q[i] * inv + eps);
-            if ((at.lane & (s.width - 1)) == 0 && (i == 0 || s.G > 1)) {
-                const int64_t p = r * s.G + at.col[i] / s.K;
-                mean[p] = m[i];
-                rstd[p] = k;
-            }
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) f[i][j] = activate<ACT>(f[i][j] * (k * gm[i][j]) + bt[i][j]);
-            gnn_store_row<T, VEC, NT>(Y + r * ldy + at.col[i], f[i]);
-        }
+        for (int j = 0; j < VEC; ++j) f[n][j] = activate<ACT>((f[n][j] - e[n]) * (k * gm[i][j]) + bt[i][j]);
+        gnn_store_row<T, VEC, NT>(Y + r * ldy + at.col[i], f[n]);
     }
 }
 
@@ -1467,7 +1565,7 @@ __global__ void __launch_bounds__(kRowThreads) row_bwd_kernel(const T *__restric
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct Layout {
-    int64_t tile_rows, tiles, parts, map_off, total_off, sums_off, table_off, bytes;
+    int64_t tile_rows, tiles, parts, map_off, total_off, sums_off, table_off, low_off, bytes;
     bool inside;  // samples inside a tile are finished there
     int threads;  // of a tile
     bool joined;  // one sample, few tiles: two launches
@@ -1498,13 +1596,15 @@ Layout layout_of(int64_t N, int64_t C, int64_t G, int64_t B, bool backward) {
     if (B > 1) off += round_up(N * 4, 256);
     L.table_off = off;
     if (B == 1) off += round_up(4 * C * 4, 256);
+    L.low_off = off;
+    L.bytes = off + round_up(B * G * 4, 256);
     if (backward) {
         L.total_off = off;
         if (B > 1) off += round_up(L.tiles * C * int64_t(sizeof(float2)), 256);
         L.sums_off = off;
         off += round_up(B * G * int64_t(sizeof(float2)), 256);
+        L.bytes = off;
     }
-    L.bytes = off;
     return L;
 }
 
@@ -1596,18 +1696,19 @@ template <typename T, int PART, int OUT, int ACT, bool NT> int run_tiles(const C
     // what join_tiles keeps: the sums of every row lane, and a sixteenth
     const size_t values = size_t(w.row_lanes) * size_t(c.C), join = (values + c.G * ((values / c.G + 15) / 16)) * (c.backward ? sizeof(float2) : sizeof(double2));
     if (!c.backward) {
+        float *low = reinterpret_cast<float *>(c.scratch(c.L.low_off));
         if (c.L.joined) {
-            norm_part_kernel<T, PART, false, kThreads, true><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd);
-            norm_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, moments, c.o.eps, nullptr);
+            norm_part_kernel<T, PART, false, kThreads, true><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd, low);
+            norm_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, low, out, c.o.ldy, moments, c.o.eps, nullptr);
         } else {
             auto *sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, false> : norm_part_kernel<T, PART, NT, kLargeThreads, false>;
             if (c.B == 1) sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, true> : norm_part_kernel<T, PART, NT, kLargeThreads, true>;
-            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd);
-            if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, table);
-            else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, table);
-            else norm_stats_kernel<64><<<many, 64, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, table);
+            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd, low);
+            if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, table);
+            else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, table);
+            else norm_stats_kernel<64><<<many, 64, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, table);
             auto *apply = c.B == 1 ? norm_apply_kernel<T, OUT, ACT, NT, kOne> : norm_apply_kernel<T, OUT, ACT, NT, kMany>;
-            apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, out, c.o.ldy, nullptr, 0.0f, table);
+            apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, low, out, c.o.ldy, nullptr, 0.0f, table);
         }
     } else {
         float2 *sums = c.out ? reinterpret_cast<float2 *>(c.scratch(c.L.sums_off)) : nullptr;
@@ -1646,7 +1747,7 @@ struct SmallPlan {
     dim3 grid;
     int threads;
     size_t lds;
-    bool inside;
+    Vectors how;
 };
 bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     const int64_t rows = c.sample_ptr ? c.o.max_sample_rows : c.N / c.B;
@@ -1692,27 +1793,28 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     s.lanes = int(lanes);
     s.team = int(round_up(cols * lanes, 16) < most ? round_up(cols * lanes, 16) : cols * lanes);
     s.teams = s.team < wide ? int(wide) / s.team : 1;
-    p.inside = K % vec == 0;
-    s.len = int(lanes * (p.inside ? K / vec : K));
-    s.team_sums = int(groups) * (s.len + (s.len + 15) / 16);
+    const int64_t slices = (c.G + groups - 1) / groups;
+    p.how = K % vec == 0 ? kInside : (c.G - (slices - 1) * groups) * K >= vec ? kAcross : kShort;
+    s.len = int(lanes * (p.how == kInside ? K / vec : K));
+    s.team_sums = int(groups) * (s.len + (s.len + 15) / 16) + int((groups + 1) / 2);  // the last: a value of every group
     p.threads = int(round_up(s.team * s.teams, 64));
     const int64_t blocks = (c.B + s.teams - 1) / s.teams;
-    p.grid = dim3(unsigned(blocks), unsigned((c.G + groups - 1) / groups));
-    size_t values = size_t(s.teams) * s.team_sums;
+    p.grid = dim3(unsigned(blocks), unsigned(slices));
+    size_t pairs = size_t(s.teams) * s.team_sums;
     if (c.backward) {
         const size_t columns = size_t(s.teams) * s.lanes * s.cols * vec;
-        values = 2 * (values > columns ? values : columns);
-    }
-    p.lds = values * sizeof(float);
+        pairs = pairs > columns ? pairs : columns;
+    } else pairs += size_t(groups * K);
+    p.lds = pairs * sizeof(float2);
     return p.grid.y <= 65535 && p.lds <= 65536;
 }
 
 // Workgroups of small_bwd_kernel that are resident at once: wavefronts of its registers on the 256 CUs, and what fits their LDS.  More would be
 // a second round with few of them (2,449 graphs of 25 vertices x 100, us: 768 workgroups 35, 1024 40, 2048 45, 4096 48).
-template <typename T, int ACT, bool INSIDE> unsigned resident(const SmallPlan &p) {
+template <typename T, int ACT, Vectors HOW> unsigned resident(const SmallPlan &p) {
     static const int waves = [] {
         int blocks = 0;
-        const hipError_t err = hipOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, reinterpret_cast<const void *>(small_bwd_kernel<T, ACT, INSIDE>), int(kTeam), 0);
+        const hipError_t err = hipOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, reinterpret_cast<const void *>(small_bwd_kernel<T, ACT, HOW>), int(kTeam), 0);
         if (err != hipSuccess) (void)hipGetLastError();
         return err == hipSuccess && blocks > 0 ? blocks * int(kTeam / 64) : 8;
     }();
@@ -1721,19 +1823,19 @@ template <typename T, int ACT, bool INSIDE> unsigned resident(const SmallPlan &p
     return 256u * unsigned(each > 1 ? each : 1);
 }
 
-template <typename T, int ACT, bool INSIDE> int run_small(const Call &c, SmallPlan &p) {
+template <typename T, int ACT, Vectors HOW> int run_small(const Call &c, SmallPlan &p) {
     const T *X = static_cast<const T *>(c.X);
     hipStream_t stream = c.stream();
     if (c.backward) {
-        const int64_t here = resident<T, ACT, INSIDE>(p), most = here < c.L.parts ? here : c.L.parts;
+        const int64_t here = resident<T, ACT, HOW>(p), most = here < c.L.parts ? here : c.L.parts;
         if (p.grid.x > most) p.grid.x = unsigned(most);
     }
     if (!c.backward) {
-        small_kernel<T, ACT, INSIDE><<<p.grid, p.threads, p.lds, stream>>>(X, c.o.ldx, p.s, c.gamma, c.beta, c.o.eps, c.mean, c.rstd, static_cast<T *>(c.out),
+        small_kernel<T, ACT, HOW><<<p.grid, p.threads, p.lds, stream>>>(X, c.o.ldx, p.s, c.gamma, c.beta, c.o.eps, c.mean, c.rstd, static_cast<T *>(c.out),
                                                                            c.o.ldy);
     } else {
         float2 *part = c.dgamma || c.dbeta ? reinterpret_cast<float2 *>(c.scratch(0)) : nullptr;
-        small_bwd_kernel<T, ACT, INSIDE><<<p.grid, p.threads, p.lds, stream>>>(X, c.o.ldx, static_cast<const T *>(c.dY), c.o.ldy, p.s, c.gamma, c.beta, c.mean,
+        small_bwd_kernel<T, ACT, HOW><<<p.grid, p.threads, p.lds, stream>>>(X, c.o.ldx, static_cast<const T *>(c.dY), c.o.ldy, p.s, c.gamma, c.beta, c.mean,
                                                                                c.rstd, static_cast<T *>(c.out), c.o.lddx, part);
         if (part) norm_bwd_columns_kernel<<<unsigned((c.C + 15) / 16), 1024, 0, stream>>>(part, p.grid.x, int(c.C), c.dgamma, c.dbeta);
     }
@@ -1791,7 +1893,8 @@ template <typename T, int ACT> int run_act(const Call &c) {
         if constexpr (V == 4) return nv == 3 ? run_rows<T, ACT, 3>(c, rows) : run_rows<T, ACT, 4>(c, rows);
     }
     SmallPlan p;
-    if (small_plan(c, V, held<T>(), c.backward ? 512 : 1024, p)) return p.inside ? run_small<T, ACT, true>(c, p) : run_small<T, ACT, false>(c, p);
+    if (small_plan(c, V, held<T>(), c.backward ? 512 : 1024, p))
+        return p.how == kInside ? run_small<T, ACT, kInside>(c, p) : p.how == kAcross ? run_small<T, ACT, kAcross>(c, p) : run_small<T, ACT, kShort>(c, p);
     if (c.C < V) return run_tiles<T, 1, 1, ACT, false>(c);
     // The backward sums keep eleven values for every column: with eight bf16 columns a thread only two of its wavefronts fit a SIMD, and half vectors are faster
     // (us, eight -> four; 400 K x 128 silu 128 -> 109, 1 M x 256 446 -> 424, 103 K x 141 69 -> 47, 1.1 M x 351 identity 740 -> 765).  Results are written

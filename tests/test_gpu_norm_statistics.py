@@ -30,7 +30,7 @@ def within(got, want, bound, what):
     assert np.isfinite(got).all() and (err <= bound).all(), f"{what}: off by up to {np.max(err / bound):.3g} bounds"
 
 
-def check(x, groups, what, ptr=None, samples=1, hint=0, eps=1e-5):
+def check(x, groups, what, ptr=None, samples=1, hint=0, eps=1e-5, rounded=True):
     n, c = x.shape
     bounds = ptr or [n // samples * i for i in range(samples + 1)]
     y, mean, rstd = forward(x, groups, ptr, samples, hint, eps=eps)
@@ -46,9 +46,9 @@ def check(x, groups, what, ptr=None, samples=1, hint=0, eps=1e-5):
         where = f"{what}, sample {b}"
         within(rstd[b], r, U * K * r, "rstd, " + where)
         within(mean[b], m, U * np.abs(m) + U * K * np.abs(d).mean((0, 2)) + 1e-37, "mean, " + where)
-        # the result takes the mean as it is stored
+        # rounded: the result may take the mean as it is stored
         xh = d * r[None, :, None]
-        within(y[lo:hi].reshape(xh.shape), xh, U * K * (1 + np.abs(xh)) + U * (np.abs(m) * r)[None, :, None], "y, " + where)
+        within(y[lo:hi].reshape(xh.shape), xh, U * K * (1 + np.abs(xh)) + rounded * U * (np.abs(m) * r)[None, :, None], "y, " + where)
 
 
 def unlike(kind, n, c, seed):
@@ -98,3 +98,53 @@ def test_a_column_unlike_the_rest_of_its_group(samples, rows):
         x = unlike("none", samples * rows, 1000, at)
         x[:, at] += 1000
         check(x, 1, f"column {at}", samples=samples)
+
+
+def paths(c, groups):
+    """Ways through the kernels: (name, rows, arguments)."""
+    yield "every vertex", 40, dict(samples=40)
+    yield "a workgroup a sample", 300, dict(samples=12)
+    yield "a workgroup a sample, longer than its registers", 12, dict(ptr=[0, 1, 1, 12], hint=1)
+    yield "one sample", 5000, dict(samples=1)
+    yield "tiles", 3000, dict(ptr=[0, 3, 3, 900, 901, 3000])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("c,groups", [(60, 1), (100, 1), (37, 1), (64, 8), (100, 10), (6, 3), (1200, 4)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_equal_values_give_beta(c, groups, dtype):
+    """The mean of equal values is that value and their deviation 0, whatever the value and their number."""
+    beta = torch.linspace(-2, 3, c)
+    for name, n, kw in paths(c, groups):
+        for value in (1000.0, 1e4 + 1 / 3, -1e5, 3e-5):
+            print("equal", name, c, groups, value, flush=True)
+            x = torch.full((n, c), value).to(dtype)
+            y, mean, rstd = forward(x, groups, beta=beta, **kw)
+            rows = [n] if kw.get("samples") else [b - a for a, b in zip(kw["ptr"], kw["ptr"][1:])]
+            there = np.array([r > 0 for r in rows]) if "ptr" in kw else slice(None)
+            assert (mean[there] == float(x[0, 0])).all(), (name, value, mean)
+            assert np.array_equal(y, np.broadcast_to(beta.to(dtype).double().numpy(), y.shape)), (name, value)
+            # what is left of the squares is below the square of two units in the value's last place
+            within(rstd, 1 / np.sqrt(1e-5) + 0 * rstd, (U + (2 * U * value) ** 2 / 1e-5 / 2 * U + 2 * U) / np.sqrt(1e-5) + 0 * rstd, "rstd " + name)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("c,groups", [(60, 1), (100, 1), (37, 1), (64, 8), (100, 10), (6, 3), (1200, 4)])
+@pytest.mark.parametrize("mean,deviation", [(1e3, 0.1), (1e4, 1.0), (-1e5, 1.0)])
+def test_a_mean_far_beyond_the_deviation(c, groups, mean, deviation):
+    """The result is as close as that of the distances from the mean: its bound does not hold the mean."""
+    for name, n, kw in paths(c, groups):
+        print("large mean", name, c, groups, mean, deviation, flush=True)
+        x = torch.from_numpy((mean + deviation * np.random.default_rng(n + c).normal(size=(n, c))).astype(np.float32))
+        check(x, groups, name, rounded=False, **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("c,groups", [(1, 1), (16, 4), (100, 10), (256, 1), (1030, 5)])
+def test_a_row_unlike_the_rest_in_a_workgroup(kind, c, groups):
+    """As above, one workgroup a sample: hints that are right or too small."""
+    for sizes, hint in (([1, 17, 0, 2, 33, 10], 33), ([1, 1000, 17, 300, 0, 2], 1)):
+        ptr = [0] + [int(v) for v in np.cumsum(sizes)]
+        print("workgroups", kind, c, groups, hint, flush=True)
+        check(torch.cat([unlike(kind, n, c, 5 * n + c) for n in sizes]), groups, kind, ptr, hint=hint)
