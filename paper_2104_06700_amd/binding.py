@@ -594,7 +594,10 @@ class AdamWTensors:
     params, grads, exp_avg, exp_avg_sq: lists of contiguous device tensors of the same sizes; a gradient may be None (the
     tensor is left alone).  Parameters and gradients are float32 or bfloat16.  The states are float32, or 8 bits (torch.float8_e4m3fn or uint8) with
     float32 scales [ceil(n / GNN_ADAMW_BLOCK)] in `scale` and `scale_sq` (None for float32 states).  master: float32 copies of
-    bfloat16 parameters, or None.  weight_decay: one number, or one for each tensor."""
+    bfloat16 parameters, or None.  weight_decay: one number, or one for each tensor.
+
+    A step reads the tensors that are given here (or to set_grads), not whatever a program has come to call its gradients since: where
+    gradients are made anew for each step, set_grads takes them."""
 
     def __init__(self, params, grads, exp_avg, exp_avg_sq, scale=None, scale_sq=None, master=None, weight_decay=0.0):
         count = len(params)
@@ -606,8 +609,8 @@ class AdamWTensors:
         self.count = count
         self._array = (GnnAdamWTensor * max(count, 1))()
         eight = (torch.float8_e4m3fn, torch.uint8)
-        for d, w, (p, g, m, v, ms, vs, master_p) in zip(self._array, decay, zip(*lists)):
-            for t in (p, g, m, v, ms, vs, master_p):
+        for d, w, (p, _, m, v, ms, vs, master_p) in zip(self._array, decay, zip(*lists)):
+            for t in (p, m, v, ms, vs, master_p):
                 if t is not None and not (t.is_contiguous() and t.is_cuda):
                     raise ValueError("contiguous device tensors expected")
             n = p.numel()
@@ -615,11 +618,9 @@ class AdamWTensors:
                 raise TypeError("states must both be float32, or both float8_e4m3fn or uint8")
             bits = 32 if m.dtype == torch.float32 else 8
             blocks = -(-n // GNN_ADAMW_BLOCK)
-            if g is not None and g.dtype != p.dtype:
-                raise TypeError("a gradient must have its parameter's dtype")
             if bits == 8 and (ms is None or vs is None):
                 raise ValueError("8-bit states need their scales")
-            for t, want, dtype in ((g, n, None), (m, n, None), (v, n, None), (ms, blocks, torch.float32), (vs, blocks, torch.float32),
+            for t, want, dtype in ((m, n, None), (v, n, None), (ms, blocks, torch.float32), (vs, blocks, torch.float32),
                                    (master_p, n, torch.float32)):
                 if t is not None and t.numel() != want:
                     raise ValueError(f"{want} values expected, {t.numel()} given")
@@ -628,11 +629,29 @@ class AdamWTensors:
             if master_p is not None and p.dtype != torch.bfloat16:
                 raise TypeError("a master copy belongs to bfloat16 parameters")
             d.param, d.exp_avg, d.exp_avg_sq = p.data_ptr(), m.data_ptr(), v.data_ptr()
-            d.grad = g.data_ptr() if g is not None else None
             d.scale, d.scale_sq = (ms.data_ptr(), vs.data_ptr()) if bits == 8 else (None, None)
             d.master = master_p.data_ptr() if master_p is not None else None
             d.n, d.dtype, d.state_bits, d.weight_decay = n, _dtype_code(p), bits, w
+        self.set_grads(lists[1])
         self.address = ctypes.addressof(self._array)
+
+    def set_grads(self, grads) -> None:
+        """The gradients of the steps from now on, one a tensor; None leaves that tensor alone."""
+        grads = list(grads)
+        if len(grads) != self.count:
+            raise ValueError("one entry a tensor expected in every list")
+        for p, g in zip(self._tensors[0], grads):
+            if g is None:
+                continue
+            if not (g.is_contiguous() and g.is_cuda):
+                raise ValueError("contiguous device tensors expected")
+            if g.dtype != p.dtype:
+                raise TypeError("a gradient must have its parameter's dtype")
+            if g.numel() != p.numel():
+                raise ValueError(f"{p.numel()} values expected, {g.numel()} given")
+        self._tensors[1] = grads
+        for d, g in zip(self._array, grads):
+            d.grad = g.data_ptr() if g is not None else None
 
 
 def gnn_adamw_step(tensors: AdamWTensors, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, seed=0, stream=None) -> None:
