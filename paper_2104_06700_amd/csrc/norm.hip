@@ -31,6 +31,14 @@ constexpr int64_t kSmallParts = 4096;   // at most so many workgroups of samples
 constexpr int64_t kRowParts = 2048;     // and of workgroups that have samples of one row
 constexpr int64_t kJoined = 4096;       // partial sums that the writing kernel joins by itself
 
+// A dimension of a grid has less than 2^32 threads.  Kernels with a thread for every piece of the rows spread their workgroups over x and z.
+__device__ __forceinline__ int64_t workgroup() { return int64_t(blockIdx.z) * gridDim.x + blockIdx.x; }
+constexpr int64_t most_workgroups(int64_t threads) { return ((int64_t(1) << 32) - 1) / threads; }
+dim3 spread(int64_t workgroups, unsigned y, unsigned threads) {  // threads: of a workgroup in x
+    const int64_t most = most_workgroups(threads), z = (workgroups + most - 1) / most;
+    return dim3(unsigned((workgroups + z - 1) / z), y, unsigned(z));
+}
+
 // Rows of every sample: from `ptr` (ragged), or `rows` of them each.  What ptr holds is kept inside the matrix.
 struct Samples {
     const void *ptr;
@@ -571,7 +579,7 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
                                                          const float *__restrict__ low, T *__restrict__ Y, int64_t ldy, const double2 *__restrict__ part, float eps, const float *__restrict__ table) {
     constexpr int kRows = rows_of<T>(false);
     const int col = column_of_block<VEC>(s);
-    const int64_t r0 = int64_t(blockIdx.x) * (kRows * s.row_lanes) + threadIdx.y;
+    const int64_t r0 = workgroup() * (kRows * s.row_lanes) + threadIdx.y;
     if (STATS != kJoin && (col < 0 || r0 >= s.N)) return;
     gnn_strip<T, VEC, NT> strip[kRows];
 #pragma unroll
@@ -608,7 +616,7 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
             [&](int g, double2 u) {
                 const double off = u.x * inv, var = u.y * inv - off * off, mid = part[g * s.group_width].x + off;
                 const float4 r = make_float4(float(mid), 1.0f / sqrtf(float(var < 0.0 ? 0.0 : var) + eps), rounding(mid), 0.0f);
-                if (blockIdx.x == 0) {
+                if (workgroup() == 0) {
                     mean[g] = r.x;
                     rstd[g] = r.y;
                 }
@@ -846,7 +854,7 @@ __global__ void __launch_bounds__(512) norm_bwd_apply_kernel(const T *__restrict
                                                              const float2 *__restrict__ sums, T *__restrict__ dX, int64_t lddx, const float2 *__restrict__ part, const float *__restrict__ table) {
     constexpr int kRows = rows_of<T>(true);
     const int col = column_of_block<VEC>(s);
-    const int64_t r0 = int64_t(blockIdx.x) * (kRows * s.row_lanes) + threadIdx.y;
+    const int64_t r0 = workgroup() * (kRows * s.row_lanes) + threadIdx.y;
     if (STATS != kJoin && (col < 0 || r0 >= s.N)) return;
     gnn_strip<T, VEC, NT> sx[kRows], sd[kRows];
 #pragma unroll
@@ -1413,7 +1421,7 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const T *__restrict__ 
                                                           T *__restrict__ Y, int64_t ldy) {
     constexpr int VEC = gnn_rows<T>::VEC, R = rows_held<T>(NV, false);
     const RowPlace<VEC, NV> at(s);
-    const int64_t r0 = int64_t(blockIdx.x) * (at.units * R) + at.unit;
+    const int64_t r0 = workgroup() * (at.units * R) + at.unit;
     gnn_strip<T, VEC, NT> x[R][NV];
 #pragma unroll
     for (int u = 0; u < R; ++u) at.load(x[u], X + (r0 + u * at.units) * ldx, r0 + u * at.units < s.N);
@@ -1669,7 +1677,7 @@ Shape shape_of(const Call &c, int vec, int rows, dim3 *grid, dim3 *block) {  // 
     if (rows) {
         s.row_lanes = row_lanes_of(s.cols);
         *block = dim3(unsigned(s.cols), unsigned(s.row_lanes));
-        *grid = dim3(unsigned((c.N + rows * s.row_lanes - 1) / (rows * s.row_lanes)), unsigned(chunks));
+        *grid = spread((c.N + rows * s.row_lanes - 1) / (rows * s.row_lanes), unsigned(chunks), block->x);
     } else {
         s.row_lanes = c.L.threads / s.cols;
         *block = dim3(unsigned(c.L.threads));
@@ -1798,7 +1806,8 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     s.len = int(lanes * (p.how == kInside ? K / vec : K));
     s.team_sums = int(groups) * (s.len + (s.len + 15) / 16) + int((groups + 1) / 2);  // the last: a value of every group
     p.threads = int(round_up(s.team * s.teams, 64));
-    const int64_t blocks = (c.B + s.teams - 1) / s.teams;
+    int64_t blocks = (c.B + s.teams - 1) / s.teams;
+    if (blocks > most_workgroups(p.threads)) blocks = most_workgroups(p.threads);  // (workgroups walk over the samples)
     p.grid = dim3(unsigned(blocks), unsigned(slices));
     size_t pairs = size_t(s.teams) * s.team_sums;
     if (c.backward) {
@@ -1866,11 +1875,11 @@ template <typename T, int ACT, int NV, bool NT> int run_rows(const Call &c, cons
     hipStream_t stream = c.stream();
     const int64_t each = (kRowThreads >> s.shift) * rows_held<T>(NV, c.backward), blocks = (c.N + each - 1) / each;
     if (!c.backward) {
-        row_kernel<T, ACT, NV, NT><<<unsigned(blocks), kRowThreads, 0, stream>>>(X, c.o.ldx, s, c.gamma, c.beta, c.o.eps, c.mean, c.rstd, static_cast<T *>(c.out), c.o.ldy);
+        row_kernel<T, ACT, NV, NT><<<spread(blocks, 1, kRowThreads), kRowThreads, 0, stream>>>(X, c.o.ldx, s, c.gamma, c.beta, c.o.eps, c.mean, c.rstd, static_cast<T *>(c.out), c.o.ldy);
     } else {
         const bool sums = c.dgamma || c.dbeta;
         float2 *part = sums ? reinterpret_cast<float2 *>(c.scratch(0)) : nullptr;
-        const int64_t rows = c.N * c.C < kLarge ? kRowParts / 2 : kRowParts, most = rows < c.L.parts ? rows : c.L.parts, grid = sums && blocks > most ? most : blocks;
+        const int64_t rows = c.N * c.C < kLarge ? kRowParts / 2 : kRowParts, most = !sums ? most_workgroups(kRowThreads) : rows < c.L.parts ? rows : c.L.parts, grid = blocks < most ? blocks : most;
         const size_t lds = sums ? size_t(kRowThreads / 64 - 1) * NV * gnn_rows<T>::VEC * s.lanes * sizeof(float2) : 0;
         row_bwd_kernel<T, ACT, NV, NT><<<unsigned(grid), kRowThreads, lds, stream>>>(X, c.o.ldx, static_cast<const T *>(c.dY), c.o.ldy, s, c.gamma, c.beta, c.mean,
                                                                                      c.rstd, static_cast<T *>(c.out), c.o.lddx, part);
