@@ -30,6 +30,7 @@ constexpr int64_t kTiles = 512, kLargeTiles = 2048, kLarge = int64_t(1) << 28, k
 constexpr int64_t kSmallParts = 4096;   // at most so many workgroups of samples that fit one leave column sums
 constexpr int64_t kRowParts = 2048;     // and of workgroups that have samples of one row
 constexpr int64_t kJoined = 4096;       // partial sums that the writing kernel joins by itself
+constexpr int64_t kSlice = 1024;        // columns of many samples that a workgroup of tiles has at once
 
 // A dimension of a grid has less than 2^32 threads.  Kernels with a thread for every piece of the rows spread their workgroups over x and z.
 __device__ __forceinline__ int64_t workgroup() { return int64_t(blockIdx.z) * gridDim.x + blockIdx.x; }
@@ -106,31 +107,62 @@ struct Shape {
     int cols;       // vectors of columns of a workgroup; threads: cols x row_lanes
     int row_lanes;
     int32_t *sample_of;  // [N] ragged samples: the sample of every row, for the kernels that write results
-    bool inside;    // samples inside a tile are finished there (more than one sample, rows of one workgroup's width)
+    bool many;      // samples: those inside a tile are finished there
+    // Columns are worked on in slices of at most `slice`: of neighbouring vectors where there is one sample, else of whole groups, or a group in `pieces`
+    // that one workgroup has after the other.
+    int slice, pieces;
+    double2 *open;  // [samples][G] what the pieces before have come to
 };
 
-// The slot of a sample's part in tile t: at most one sample comes into a tile from the one before (2 t), one goes out of it (2 t + 1).  Without
-// `inside` every part has one, t + b: from one pair to the next at least one of the two grows.
-__device__ __forceinline__ int64_t slot_of(const Shape &s, int64_t t, int64_t b, int64_t begin) {
-    return !s.inside ? t + b : begin > t * s.tile_rows ? 2 * t + 1 : 2 * t;
+// The slot of a sample's part in tile t.  Of many: at most one comes into a tile from the one before (2 t), one goes out of it (2 t + 1).
+__device__ __forceinline__ int64_t slot_of(const Shape &s, int64_t t, int64_t begin) {
+    return !s.many ? t : begin > t * s.tile_rows ? 2 * t + 1 : 2 * t;
 }
 
-// What a thread of a tile works on: VEC neighbouring columns from `col`, every row_lanes-th row.  The last vector of a row starts
-// where it ends with the row: columns that it shares with the one before are computed twice, to the same bits.
-template <int VEC> struct Place {
-    int lane, row_lane, col;
-    bool active;
-    __device__ __forceinline__ explicit Place(const Shape &s) {
-        lane = int(threadIdx.x) % s.cols;
-        row_lane = int(threadIdx.x) / s.cols;
-        const int vec = int(blockIdx.y) * s.cols + lane;
-        active = row_lane < s.row_lanes && vec * VEC < s.C;
-        col = vec * VEC < s.C - VEC ? vec * VEC : s.C - VEC;
+// What a tile kernel knows when it is compiled: there is one sample; there are many; many, and groups in pieces
+enum Tiles { kOneSample, kManySamples, kPieces };
+
+// Columns c0 .. c1 - 1, in runs of `run` that belong to a group each.
+template <Tiles HOW> struct Slice {
+    int c0, c1, run, groups, group;  // group: the first
+    bool first, last;                // piece of it
+    __device__ __forceinline__ Slice(const Shape &s, int p) {
+        const int y = int(blockIdx.y);
+        if (HOW != kPieces) {
+            c0 = y * s.slice;
+            c1 = c0 + s.slice < s.C ? c0 + s.slice : s.C;
+            run = s.group_width;
+            group = c0 / s.group_width;
+        } else {
+            const int end = (y + 1) * s.group_width;
+            c0 = y * s.group_width + p * s.slice;
+            c1 = c0 + s.slice < end ? c0 + s.slice : end;
+            run = c1 - c0;
+            group = y;
+        }
+        groups = (c1 - c0) / run;
+        first = HOW != kPieces || p == 0;
+        last = HOW != kPieces || p == s.pieces - 1;
     }
 };
 
-// Runs f(sample, first row, row behind the last) for the parts of the samples in this workgroup's tile; ONE: there is one sample.  The same for all threads.
-template <bool ONE, typename F> __device__ __forceinline__ void for_parts(const Shape &s, F f) {
+// What a thread of a tile works on: VEC neighbouring columns from `col`, every row_lanes-th row.  The last vector of a row starts
+// where it ends with the slice: columns that it shares with the one before (in a narrow last slice, with the slice before) are computed twice, to the same bits.
+template <int VEC> struct Place {
+    int lane, row_lane, col;
+    bool active;
+    template <Tiles HOW> __device__ __forceinline__ Place(const Shape &s, const Slice<HOW> &slice) {
+        lane = int(threadIdx.x) % s.cols;
+        row_lane = int(threadIdx.x) / s.cols;
+        const int c = slice.c0 + lane * VEC;
+        active = row_lane < s.row_lanes && c < slice.c1;
+        col = c < slice.c1 - VEC ? c : slice.c1 - VEC;
+    }
+};
+
+// Runs f(sample, first row, row behind the last) for the parts of the samples in this workgroup's tile; ONE: there is one sample.  The same for all
+// threads.  map: the rows' samples are written down.
+template <bool ONE, typename F> __device__ __forceinline__ void for_parts(const Shape &s, bool map, F f) {
     const int64_t r0 = int64_t(blockIdx.x) * s.tile_rows;
     const int64_t r1 = r0 + s.tile_rows < s.N ? r0 + s.tile_rows : s.N;
     if constexpr (ONE) return f(int64_t(0), r0, r1);
@@ -139,7 +171,7 @@ template <bool ONE, typename F> __device__ __forceinline__ void for_parts(const 
         const int64_t end = s.samples.begin(b + 1);
         const int64_t stop = end < r1 ? end : r1;
         if (stop <= row) continue;
-        if (s.sample_of && blockIdx.y == 0)
+        if (map)
             for (int64_t r = row + threadIdx.x; r < stop; r += blockDim.x) s.sample_of[r] = int32_t(b);
         f(b, row, stop);
         row = stop;
@@ -192,8 +224,10 @@ template <typename V> __device__ __forceinline__ const V *group_sums(V *from, V 
 
 // What a tile has in LDS, in floats: `each` for every column of a thread.  Their place is taken by what finishes samples, the columns' contributions (V) by
 // group and the room to add these up, once the threads' values have been added up.
-template <typename V> __host__ __device__ constexpr int64_t tile_values(int64_t threads, int64_t vec, int64_t each, int64_t C, int64_t G, bool inside) {
-    const int64_t own = each * threads * vec, sums = inside ? int64_t(sizeof(V) / 4) * (C + (C > G ? G * ((C / G + 15) / 16) : 0)) : 0;
+// slice: columns to finish (0: none), in groups of K or one piece of a group
+template <typename V> __host__ __device__ constexpr int64_t tile_values(int64_t threads, int64_t vec, int64_t each, int64_t slice, int64_t K) {
+    const int64_t run = K < slice ? K : slice, sixteenth = run > 1 ? slice / run * ((run + 15) / 16) : 0;
+    const int64_t own = each * threads * vec, sums = int64_t(sizeof(V) / 4) * (slice + sixteenth);
     return (own > sums ? own : sums) + 3 & ~int64_t(3);
 }
 
@@ -235,122 +269,145 @@ template <int VEC> __device__ __forceinline__ void join_row_lanes(double *mean, 
 // joined to those of the rows before (d = difference of the means: m2 = m2 + m2' + d^2 n n' / (n + n'), all terms positive), so that
 // the difference s2 - s1^2 / n takes off at most what the run is worth, whatever row comes first: with all distances taken from a part's first row instead a zero
 // row in front of 16,384 of mean 100 and deviation 1 costs rstd 4e-4.
-template <typename T, int VEC, bool NT, int THREADS, bool ONE>
+template <typename T, int VEC, bool NT, int THREADS, Tiles HOW>
 __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, double2 *__restrict__ part, float eps,
                                                              float *__restrict__ mean_out, float *__restrict__ rstd_out, float *__restrict__ low) {
+    constexpr bool ONE = HOW == kOneSample;
     extern __shared__ double tile_lds[];
     double *const red_1 = tile_lds;
     float *const red_2 = reinterpret_cast<float *>(tile_lds + blockDim.x * VEC);
     double2 *const sums = reinterpret_cast<double2 *>(tile_lds);
-    double *const means = tile_lds + tile_values<double2>(blockDim.x, VEC, 3, s.C, s.G, s.inside) / 2;
-    const Place<VEC> at(s);
-    if (!ONE && s.inside && s.samples.ptr)  // samples without rows are in no tile
+    double *const means = tile_lds + tile_values<double2>(blockDim.x, VEC, 3, ONE ? 0 : s.slice, s.group_width) / 2;
+    if (!ONE && s.samples.ptr && blockIdx.y == 0)  // samples without rows are in no tile
         for (int64_t b = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; b < s.samples.count; b += int64_t(gridDim.x) * blockDim.x)
             if (s.samples.begin(b + 1) <= s.samples.begin(b))
                 for (int g = 0; g < s.G; ++g) {
                     mean_out[b * s.G + g] = 0.0f;
                     rstd_out[b * s.G + g] = 1.0f / sqrtf(eps);
                 }  // (no row asks for their part of `low`)
-    for_parts<ONE>(s, [&](int64_t b, int64_t row, int64_t stop) {
-        constexpr int U = 4, RUN = 32;
-        const int rows = int(stop - row), each = int(unsigned(rows) / unsigned(s.row_lanes)), rest = rows - each * s.row_lanes;
-        float base[VEC], off[VEC], m2[VEC];  // the mean is base + off
+    for (int piece = 0; piece < (HOW == kPieces ? s.pieces : 1); ++piece) {
+        const Slice<HOW> slice(s, piece);
+        const Place<VEC> at(s, slice);
+        for_parts<ONE>(s, s.sample_of && blockIdx.y == 0 && piece == 0, [&](int64_t b, int64_t row, int64_t stop) {
+            constexpr int U = 4, RUN = 32;
+            const int rows = int(stop - row), each = int(unsigned(rows) / unsigned(s.row_lanes)), rest = rows - each * s.row_lanes;
+            float base[VEC], off[VEC], m2[VEC];  // the mean is base + off
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) base[j] = off[j] = m2[j] = 0.0f;
-        if (at.active) {
-            const T *x = X + (row + at.row_lane) * ldx + at.col;
-            const int64_t step = s.row_lanes * ldx;
-            int left = each + (at.row_lane < rest);  // rows of this thread
-            float before = 0.0f;
-            if (left > 0) {
-                float v[U][VEC];
-#pragma unroll
-                for (int u = 0; u < U; ++u) gnn_load_row<T, VEC>(x + (u < left ? u : 0) * step, v[u]);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) base[j] = v[0][j] + 0.25f * ((v[1][j] - v[0][j]) + (v[2][j] - v[0][j]) + (v[3][j] - v[0][j]));
-            }
-            while (left > 0) {
-                const int run = left < RUN ? left : RUN;
-                float t1[VEC], t2[VEC];
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) t1[j] = t2[j] = 0.0f;
-                for (int k = 0; k < run; k += U, x += U * step) {
-                    gnn_strip<T, VEC, NT> strip[U];
-#pragma unroll
-                    for (int u = 0; u < U; ++u) strip[u].load(x + (k + u < run ? u : 0) * step);
+            for (int j = 0; j < VEC; ++j) base[j] = off[j] = m2[j] = 0.0f;
+            if (at.active) {
+                const T *x = X + (row + at.row_lane) * ldx + at.col;
+                const int64_t step = s.row_lanes * ldx;
+                int left = each + (at.row_lane < rest);  // rows of this thread
+                float before = 0.0f;
+                if (left > 0) {
                     float v[U][VEC];
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        strip[u].get(v[u]);
-                        if (u > 0)
+                    for (int u = 0; u < U; ++u) gnn_load_row<T, VEC>(x + (u < left ? u : 0) * step, v[u]);
 #pragma unroll
-                            for (int j = 0; j < VEC; ++j) v[u][j] = k + u < run ? v[u][j] : base[j];
+                    for (int j = 0; j < VEC; ++j) base[j] = v[0][j] + 0.25f * ((v[1][j] - v[0][j]) + (v[2][j] - v[0][j]) + (v[3][j] - v[0][j]));
+                }
+                while (left > 0) {
+                    const int run = left < RUN ? left : RUN;
+                    float t1[VEC], t2[VEC];
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) t1[j] = t2[j] = 0.0f;
+                    for (int k = 0; k < run; k += U, x += U * step) {
+                        gnn_strip<T, VEC, NT> strip[U];
+#pragma unroll
+                        for (int u = 0; u < U; ++u) strip[u].load(x + (k + u < run ? u : 0) * step);
+                        float v[U][VEC];
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            strip[u].get(v[u]);
+                            if (u > 0)
+#pragma unroll
+                                for (int j = 0; j < VEC; ++j) v[u][j] = k + u < run ? v[u][j] : base[j];
+                        }
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) {
+#pragma unroll
+                            for (int u = 0; u < U; ++u) v[u][j] -= base[j];
+                            t1[j] += (v[0][j] + v[1][j]) + (v[2][j] + v[3][j]);
+                            t2[j] += (v[0][j] * v[0][j] + v[1][j] * v[1][j]) + (v[2][j] * v[2][j] + v[3][j] * v[3][j]);
+                        }
                     }
+                    const float n = float(run), inv = __builtin_amdgcn_rcpf(n), share = n * __builtin_amdgcn_rcpf(before + n), weight = share * before;
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
-#pragma unroll
-                        for (int u = 0; u < U; ++u) v[u][j] -= base[j];
-                        t1[j] += (v[0][j] + v[1][j]) + (v[2][j] + v[3][j]);
-                        t2[j] += (v[0][j] * v[0][j] + v[1][j] * v[1][j]) + (v[2][j] * v[2][j] + v[3][j] * v[3][j]);
+                        const float o = t1[j] * inv, q = t2[j] - t1[j] * o;
+                        join(off[j], m2[j], o, q < 0.0f ? 0.0f : q, share, weight);
+                        const float next = base[j] + off[j];  // the next run's distances are from here
+                        off[j] -= next - base[j];
+                        base[j] = next;
                     }
+                    before += n;
+                    left -= run;
                 }
-                const float n = float(run), inv = __builtin_amdgcn_rcpf(n), share = n * __builtin_amdgcn_rcpf(before + n), weight = share * before;
+            }
+            if (at.active)
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    const float o = t1[j] * inv, q = t2[j] - t1[j] * o;
-                    join(off[j], m2[j], o, q < 0.0f ? 0.0f : q, share, weight);
-                    const float next = base[j] + off[j];  // the next run's distances are from here
-                    off[j] -= next - base[j];
-                    base[j] = next;
+                    red_1[threadIdx.x * VEC + j] = double(base[j]) + double(off[j]);
+                    red_2[threadIdx.x * VEC + j] = m2[j];
                 }
-                before += n;
-                left -= run;
-            }
-        }
-        if (at.active)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                red_1[threadIdx.x * VEC + j] = double(base[j]) + double(off[j]);
-                red_2[threadIdx.x * VEC + j] = m2[j];
-            }
-        join_row_lanes<VEC>(red_1, red_2, s, at, each, rest);
-        const int64_t begin = !ONE && s.inside ? s.samples.begin(b) : 0;
-        const bool whole = !ONE && s.inside && begin == row && s.samples.begin(b + 1) == stop;  // the same for all threads
-        const bool mine = at.active && at.row_lane == 0;
-        double2 v[VEC];
-        if (mine)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) v[j] = make_double2(red_1[at.lane * VEC + j], red_2[at.lane * VEC + j]);
-        if (!whole) {
-            if (mine) {
-                double2 *o = part + slot_of(s, blockIdx.x, b, begin) * s.C + at.col;
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) o[j] = v[j];
-            }
-        } else {
-            const double inv = 1.0 / (double(rows) * s.group_width);
+            join_row_lanes<VEC>(red_1, red_2, s, at, each, rest);
+            const int64_t begin = ONE ? 0 : s.samples.begin(b);
+            const bool whole = !ONE && begin == row && s.samples.begin(b + 1) == stop;  // the same for all threads
+            const bool mine = at.active && at.row_lane == 0;
+            double2 v[VEC];
             if (mine)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) means[at.col + j] = v[j].x;
-            __syncthreads();
-            if (mine) {
+                for (int j = 0; j < VEC; ++j) v[j] = make_double2(red_1[at.lane * VEC + j], red_2[at.lane * VEC + j]);
+            if (!whole) {
+                if (mine) {
+                    double2 *o = part + slot_of(s, blockIdx.x, begin) * s.C + at.col;
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const int c = at.col + j;
-                    const double d = v[j].x - means[c - c % s.group_width];
-                    sums[c] = make_double2(double(rows) * d, v[j].y + double(rows) * d * d);
+                    for (int j = 0; j < VEC; ++j) o[j] = v[j];
+                }
+            } else {
+                const double inv = 1.0 / (double(rows) * slice.run);
+                const int width = slice.c1 - slice.c0, k0 = at.col - slice.c0;  // (k0 < 0: columns of the slice before)
+                if (mine)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        if (k0 + j >= 0) means[k0 + j] = v[j].x;
+                __syncthreads();
+                if (mine) {
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const int k = k0 + j;
+                        if (k < 0) continue;
+                        const double d = v[j].x - means[k - k % slice.run];
+                        sums[k] = make_double2(double(rows) * d, v[j].y + double(rows) * d * d);
+                    }
+                }
+                const double2 *all = group_sums(sums, sums + width, slice.groups, slice.run, int(threadIdx.x), int(blockDim.x));
+                for (int g = int(threadIdx.x); g < slice.groups; g += int(blockDim.x)) {
+                    const double off = all[g].x * inv;
+                    double var = all[g].y * inv - off * off, mid = means[g * slice.run] + off;
+                    if constexpr (HOW == kPieces) {  // one group: this thread's in every piece
+                        double2 so_far = make_double2(mid, var * slice.run);
+                        if (!slice.first) {  // as in join(): mean, and the sum over columns of squared distances
+                            const double2 before = s.open[b * s.G + slice.group];
+                            const double n = slice.run, m = slice.c0 - int(blockIdx.y) * s.group_width, d = mid - before.x;
+                            so_far = make_double2(before.x + d * (n / (m + n)), before.y + so_far.y + d * d * (m * n / (m + n)));
+                        }
+                        if (!slice.last) {
+                            s.open[b * s.G + slice.group] = so_far;
+                            continue;
+                        }
+                        mid = so_far.x;
+                        var = so_far.y / s.group_width;
+                    }
+                    const int64_t p = b * s.G + slice.group + g;
+                    mean_out[p] = float(mid);
+                    low[p] = rounding(mid);
+                    rstd_out[p] = 1.0f / sqrtf(float(var < 0.0 ? 0.0 : var) + eps);
                 }
             }
-            const double2 *all = group_sums(sums, sums + s.C, s.G, s.group_width, int(threadIdx.x), int(blockDim.x));
-            for (int g = int(threadIdx.x); g < s.G; g += int(blockDim.x)) {
-                const double off = all[g].x * inv, var = all[g].y * inv - off * off, mid = means[g * s.group_width] + off;
-                mean_out[b * s.G + g] = float(mid);
-                low[b * s.G + g] = rounding(mid);
-                rstd_out[b * s.G + g] = 1.0f / sqrtf(float(var < 0.0 ? 0.0 : var) + eps);
-            }
-        }
-        __syncthreads();
-    });
+            __syncthreads();
+        });
+    }
 }
 
 template <int THREADS> __device__ __forceinline__ double2 team_sum(double2 v, double2 *red) {
@@ -383,21 +440,21 @@ template <int THREADS> struct Merge {
         hi = s.samples.begin(b + 1);
         t0 = lo / s.tile_rows;
         t1 = hi > lo ? (hi - 1) / s.tile_rows : t0 - 1;
-        done = s.inside && t1 <= t0;
+        done = s.many && t1 <= t0;
         wide = s.group_width < THREADS ? s.group_width : THREADS;
         deep = THREADS / wide;
         k = int(threadIdx.x) % wide;
         d = int(threadIdx.x) / wide;
     }
     // f(rows of the sample in tile t, partial sums of column c there), four loads in flight
-    template <typename V, typename F> __device__ __forceinline__ void tiles(const Shape &s, const V *part, int64_t b, int c, F f) const {
+    template <typename V, typename F> __device__ __forceinline__ void tiles(const Shape &s, const V *part, int c, F f) const {
         constexpr int U = 4;
         if (d >= deep) return;
         for (int64_t t = t0 + d; t <= t1; t += U * deep) {
             V v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (t + u * deep <= t1) v[u] = part[slot_of(s, t + u * deep, b, lo) * s.C + c];
+                if (t + u * deep <= t1) v[u] = part[slot_of(s, t + u * deep, lo) * s.C + c];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int64_t w = t + u * deep;
@@ -413,7 +470,7 @@ template <int THREADS> struct Merge {
 __device__ __forceinline__ int64_t sample_of_pair(const Shape &s, int64_t p, int64_t tiles, int *group) {
     const int64_t i = p / s.G;
     *group = int(p - i * s.G);
-    if (!s.inside || s.samples.count <= tiles) return i;
+    if (s.samples.count <= tiles) return i;
     const int64_t end = (i + 1) * s.tile_rows;
     if (end >= s.N) return -1;
     const int64_t b = s.samples.of(end - 1);
@@ -427,7 +484,7 @@ __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const double2 *__re
                                                              float *__restrict__ rstd, float *__restrict__ low, float *__restrict__ table) {
     __shared__ double2 red[THREADS / 64];
     const int64_t tiles = (s.N + s.tile_rows - 1) / s.tile_rows;
-    const int64_t pairs = (s.inside && s.samples.count > tiles ? tiles : s.samples.count) * s.G;
+    const int64_t pairs = (s.samples.count > tiles ? tiles : s.samples.count) * s.G;
     for (int64_t i = blockIdx.x; i < pairs; i += gridDim.x) {
         int group;
         const int64_t b = sample_of_pair(s, i, tiles, &group);
@@ -438,10 +495,10 @@ __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const double2 *__re
         if (m.done) continue;
         double mid = 0.0, var = 0.0;
         if (m.hi > m.lo) {
-            const double pivot = part[slot_of(s, m.t0, b, m.lo) * s.C + c0].x;
+            const double pivot = part[slot_of(s, m.t0, m.lo) * s.C + c0].x;
             double2 u = {0.0, 0.0};
             for (int k = m.k; k < s.group_width; k += m.wide)
-                m.tiles(s, part, b, c0 + k, [&](double rows, double2 v) {
+                m.tiles(s, part, c0 + k, [&](double rows, double2 v) {
                     const double d = v.x - pivot;
                     u.x += rows * d;
                     u.y += v.y + rows * d * d;
@@ -586,7 +643,8 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
     for (int u = 0; u < kRows; ++u)
         if (r0 + u * s.row_lanes < s.N) strip[u].load(X + (r0 + u * s.row_lanes) * ldx + col);
     const Affine<VEC> aff(s, col, gamma, beta);
-    float w[VEC], o[VEC], l[VEC], bt[VEC];  // z = (x - o) w + (beta - l w): the mean is o + l.  A value that is the mean gives beta where rstd is finite
+    // z = (x - o) w + (beta - l w): the mean is o + l.  A value that is the mean gives beta where rstd is finite.
+    float w[VEC], o[VEC], l[VEC], bt[VEC];
     auto fold = [&]() {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
@@ -650,103 +708,123 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
 }
 
 // Per part and column: sum dz and sum dz xh; per tile and column their sums over its parts (total; NULL where there is one sample).
-template <typename T, int VEC, int ACT, bool NT, int THREADS>
+template <typename T, int VEC, int ACT, bool NT, int THREADS, Tiles HOW>
 __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const Shape s,
                                                                  const float *__restrict__ gamma, const float *__restrict__ beta,
                                                                  const float *__restrict__ mean, const float *__restrict__ rstd,
                                                                  float2 *__restrict__ part, float2 *__restrict__ total, float2 *__restrict__ sums_out) {
+    constexpr bool ONE = HOW == kOneSample;
     extern __shared__ double tile_lds[];
     float *const red_1 = reinterpret_cast<float *>(tile_lds), *const red_x = red_1 + blockDim.x * VEC;
     float2 *const sums = reinterpret_cast<float2 *>(tile_lds);
-    const Place<VEC> at(s);
-    const Affine<VEC> aff(s, at.col, gamma, beta);
-    float t1[VEC], tx[VEC];
+    for (int piece = 0; piece < (HOW == kPieces ? s.pieces : 1); ++piece) {
+        const Slice<HOW> slice(s, piece);
+        const Place<VEC> at(s, slice);
+        const Affine<VEC> aff(s, at.col, gamma, beta);
+        float t1[VEC], tx[VEC];
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) t1[j] = tx[j] = 0.0f;
-    for_parts<false>(s, [&](int64_t b, int64_t row, int64_t stop) {
-        constexpr int U = 4;
-        float a1[VEC], ax[VEC];
+        for (int j = 0; j < VEC; ++j) t1[j] = tx[j] = 0.0f;
+        for_parts<ONE>(s, s.sample_of && blockIdx.y == 0 && piece == 0, [&](int64_t b, int64_t row, int64_t stop) {
+            constexpr int U = 4;
+            float a1[VEC], ax[VEC];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) a1[j] = ax[j] = 0.0f;
-        if (at.active) {
-            float o[VEC], rs[VEC];
-            aff.gather(s, mean, b, o);
-            aff.gather(s, rstd, b, rs);
-            int64_t r = row + at.row_lane;
-            while (r < stop) {
-                float c1[VEC], cx[VEC];
+            for (int j = 0; j < VEC; ++j) a1[j] = ax[j] = 0.0f;
+            if (at.active) {
+                float o[VEC], rs[VEC];
+                aff.gather(s, mean, b, o);
+                aff.gather(s, rstd, b, rs);
+                int64_t r = row + at.row_lane;
+                while (r < stop) {
+                    float c1[VEC], cx[VEC];
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) c1[j] = cx[j] = 0.0f;
-                for (int k = 0; k < 32 / U && r < stop; ++k, r += U * s.row_lanes) {
-                    gnn_strip<T, VEC, NT> sx[U], sd[U];
+                    for (int j = 0; j < VEC; ++j) c1[j] = cx[j] = 0.0f;
+                    for (int k = 0; k < 32 / U && r < stop; ++k, r += U * s.row_lanes) {
+                        gnn_strip<T, VEC, NT> sx[U], sd[U];
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const int64_t i = r + u * s.row_lanes;
-                        if (i < stop) {
-                            sx[u].load(X + i * ldx + at.col);
-                            sd[u].load(dY + i * ldy + at.col);
+                        for (int u = 0; u < U; ++u) {
+                            const int64_t i = r + u * s.row_lanes;
+                            if (i < stop) {
+                                sx[u].load(X + i * ldx + at.col);
+                                sd[u].load(dY + i * ldy + at.col);
+                            }
+                        }
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            if (r + u * s.row_lanes >= stop) break;
+                            float x[VEC], d[VEC];
+                            sx[u].get(x);
+                            sd[u].get(d);
+#pragma unroll
+                            for (int j = 0; j < VEC; ++j) {
+                                const float xh = (x[j] - o[j]) * rs[j];
+                                const float dz = d[j] * slope<ACT>(xh * aff.gamma[j] + aff.beta[j]);
+                                c1[j] += dz;
+                                cx[j] += dz * xh;
+                            }
                         }
                     }
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        if (r + u * s.row_lanes >= stop) break;
-                        float x[VEC], d[VEC];
-                        sx[u].get(x);
-                        sd[u].get(d);
-#pragma unroll
-                        for (int j = 0; j < VEC; ++j) {
-                            const float xh = (x[j] - o[j]) * rs[j];
-                            const float dz = d[j] * slope<ACT>(xh * aff.gamma[j] + aff.beta[j]);
-                            c1[j] += dz;
-                            cx[j] += dz * xh;
-                        }
+                    for (int j = 0; j < VEC; ++j) {
+                        a1[j] += c1[j];
+                        ax[j] += cx[j];
                     }
-                }
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    a1[j] += c1[j];
-                    ax[j] += cx[j];
                 }
             }
-        }
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            red_1[threadIdx.x * VEC + j] = a1[j];
-            red_x[threadIdx.x * VEC + j] = ax[j];
-        }
-        add_row_lanes<VEC>(red_1, red_x, s, at, s.row_lanes);
-        const int64_t begin = s.inside ? s.samples.begin(b) : 0;
-        const bool whole = s.inside && begin == row && s.samples.begin(b + 1) == stop;  // the same for all threads
-        const bool mine = at.active && at.row_lane == 0;
-        float u1[VEC], ux[VEC];
-        if (mine) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                u1[j] = red_1[at.lane * VEC + j];
-                ux[j] = red_x[at.lane * VEC + j];
-                t1[j] += u1[j];
-                tx[j] += ux[j];
+                red_1[threadIdx.x * VEC + j] = a1[j];
+                red_x[threadIdx.x * VEC + j] = ax[j];
             }
-            if (!whole) {
-                float2 *o = part + slot_of(s, blockIdx.x, b, begin) * s.C + at.col;
+            add_row_lanes<VEC>(red_1, red_x, s, at, s.row_lanes);
+            const int64_t begin = ONE ? 0 : s.samples.begin(b);
+            const bool whole = !ONE && begin == row && s.samples.begin(b + 1) == stop;  // the same for all threads
+            const bool mine = at.active && at.row_lane == 0;
+            float u1[VEC], ux[VEC];
+            if (mine) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) o[j] = make_float2(u1[j], ux[j]);
+                for (int j = 0; j < VEC; ++j) {
+                    u1[j] = red_1[at.lane * VEC + j];
+                    ux[j] = red_x[at.lane * VEC + j];
+                    if constexpr (!ONE) {
+                        t1[j] += u1[j];
+                        tx[j] += ux[j];
+                    }
+                }
+                if (!whole) {
+                    float2 *o = part + slot_of(s, blockIdx.x, begin) * s.C + at.col;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) o[j] = make_float2(u1[j], ux[j]);
+                }
             }
-        }
-        if (whole && sums_out) {
+            if (whole && sums_out) {
+                __syncthreads();
+                const int k0 = at.col - slice.c0;
+                if (mine)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        if (k0 + j >= 0) sums[k0 + j] = make_float2(u1[j] * aff.gamma[j], ux[j] * aff.gamma[j]);
+                const float2 *all = group_sums(sums, sums + (slice.c1 - slice.c0), slice.groups, slice.run, int(threadIdx.x), int(blockDim.x));
+                const float n = float(stop - row) * float(s.group_width);
+                for (int g = int(threadIdx.x); g < slice.groups; g += int(blockDim.x)) {
+                    float2 sum = all[g];
+                    if constexpr (HOW == kPieces) {  // one group: this thread's in every piece
+                        double2 so_far = make_double2(sum.x, sum.y);
+                        if (!slice.first) add_to(so_far, s.open[b * s.G + slice.group]);
+                        if (!slice.last) {
+                            s.open[b * s.G + slice.group] = so_far;
+                            continue;
+                        }
+                        sum = make_float2(float(so_far.x), float(so_far.y));
+                    }
+                    sums_out[b * s.G + slice.group + g] = make_float2(sum.x / n, sum.y / n);
+                }
+            }
             __syncthreads();
-            if (mine)
+        });
+        if (!ONE && total && at.active && at.row_lane == 0) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) sums[at.col + j] = make_float2(u1[j] * aff.gamma[j], ux[j] * aff.gamma[j]);
-            const float2 *all = group_sums(sums, sums + s.C, s.G, s.group_width, int(threadIdx.x), int(blockDim.x));
-            const float n = float(stop - row) * float(s.group_width);
-            for (int g = int(threadIdx.x); g < s.G; g += int(blockDim.x)) sums_out[b * s.G + g] = make_float2(all[g].x / n, all[g].y / n);
+            for (int j = 0; j < VEC; ++j) total[int64_t(blockIdx.x) * s.C + at.col + j] = make_float2(t1[j], tx[j]);
         }
-        __syncthreads();
-    });
-    if (total && at.active && at.row_lane == 0) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) total[int64_t(blockIdx.x) * s.C + at.col + j] = make_float2(t1[j], tx[j]);
     }
 }
 
@@ -775,7 +853,7 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_stats_kernel(const float2 *_
                                                                  const float *__restrict__ mean, const float *__restrict__ rstd, float *__restrict__ table) {
     __shared__ double2 red[THREADS];
     const int64_t tiles = (s.N + s.tile_rows - 1) / s.tile_rows;
-    const int64_t pairs = (s.inside && s.samples.count > tiles ? tiles : s.samples.count) * s.G;
+    const int64_t pairs = (s.samples.count > tiles ? tiles : s.samples.count) * s.G;
     for (int64_t i = blockIdx.x; i < pairs; i += gridDim.x) {
         int group;
         const int64_t b = sample_of_pair(s, i, tiles, &group);
@@ -790,7 +868,7 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_stats_kernel(const float2 *_
             const int c = c0 + k0 + m.k;
             const bool there = k0 + m.k < s.group_width;
             double2 u = {0.0, 0.0};
-            if (there) m.tiles(s, part, b, c, [&](double, float2 v) { u.x += v.x; u.y += v.y; });
+            if (there) m.tiles(s, part, c, [&](double, float2 v) { u.x += v.x; u.y += v.y; });
             if (dgamma || dbeta) {
                 u = add_deep<THREADS>(u, red, m.wide, m.deep);
                 if (there && m.d == 0) {
@@ -1573,8 +1651,7 @@ __global__ void __launch_bounds__(kRowThreads) row_bwd_kernel(const T *__restric
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct Layout {
-    int64_t tile_rows, tiles, parts, map_off, total_off, sums_off, table_off, low_off, bytes;
-    bool inside;  // samples inside a tile are finished there
+    int64_t tile_rows, tiles, parts, map_off, open_off, total_off, sums_off, table_off, low_off, bytes;
     int threads;  // of a tile
     bool joined;  // one sample, few tiles: two launches
 };
@@ -1591,17 +1668,15 @@ Layout layout_of(int64_t N, int64_t C, int64_t G, int64_t B, bool backward) {
     tiles = tiles < most ? tiles : most;
     L.tile_rows = (N + tiles - 1) / tiles;
     L.tiles = (N + L.tile_rows - 1) / L.tile_rows;
-    L.inside = B > 1 && C <= 1024;  // rows of at most 256 vectors: one workgroup has whole rows
-    // partial sums: of the tiles, or of the workgroups of small_bwd_kernel
-    L.parts = L.inside ? 2 * L.tiles : L.tiles + B;
-    const int64_t small = B < kSmallParts ? B : kSmallParts;
-    if (backward && L.parts < small) L.parts = small;
-    // (a backward call's workspace does for the forward call, too)
-    const int64_t moments = L.inside ? 2 * L.tiles : L.tiles + B;
-    int64_t off = round_up(L.parts * C * int64_t(sizeof(float2)) > moments * C * int64_t(sizeof(double2)) ? L.parts * C * int64_t(sizeof(float2))
-                                                                                                          : moments * C * int64_t(sizeof(double2)), 256);
+    // partial sums: of the tiles, or of the workgroups of small_bwd_kernel and row_bwd_kernel.  (A backward call's workspace does for the forward call, too.)
+    const int64_t slots = B > 1 ? 2 * L.tiles : L.tiles, small = backward ? (B < kSmallParts ? B : kSmallParts) : 0;
+    L.parts = slots > small ? slots : small;
+    const int64_t moments = slots * C * int64_t(sizeof(double2)), sums = L.parts * C * int64_t(sizeof(float2));
+    int64_t off = round_up(moments > sums ? moments : sums, 256);
     L.map_off = off;
     if (B > 1) off += round_up(N * 4, 256);
+    L.open_off = off;
+    if (B > 1 && C / G > kSlice) off += round_up(B * G * int64_t(sizeof(double2)), 256);
     L.table_off = off;
     if (B == 1) off += round_up(4 * C * 4, 256);
     L.low_off = off;
@@ -1670,10 +1745,24 @@ Shape shape_of(const Call &c, int vec, int rows, dim3 *grid, dim3 *block) {  // 
     s.G = int(c.G);
     s.group_width = int(c.C / c.G);
     s.tile_rows = c.L.tile_rows;
-    s.inside = c.L.inside;
+    s.many = c.B > 1;
     s.sample_of = c.sample_ptr && c.B > 1 ? reinterpret_cast<int32_t *>(c.scratch(c.L.map_off)) : nullptr;
-    const int64_t vecs = (c.C + vec - 1) / vec, chunks = (vecs + 255) / 256;
+    s.open = reinterpret_cast<double2 *>(c.scratch(c.L.open_off));
+    s.pieces = 1;
+    const int64_t vecs = (c.C + vec - 1) / vec, K = c.C / c.G;
+    int64_t chunks = (vecs + 255) / 256;
     s.cols = int((vecs + chunks - 1) / chunks);
+    s.slice = s.cols * vec;
+    if (!rows && s.many) {
+        s.slice = int(K <= kSlice ? (kSlice / K < c.G ? kSlice / K : c.G) * K : kSlice);
+        if (K > kSlice) {
+            s.pieces = int((K + kSlice - 1) / kSlice);
+            s.slice = int((K + s.pieces - 1) / s.pieces);
+            s.pieces = int((K + s.slice - 1) / s.slice);
+        }
+        s.cols = (s.slice + vec - 1) / vec;
+        chunks = K > kSlice ? c.G : (c.C + s.slice - 1) / s.slice;
+    }
     if (rows) {
         s.row_lanes = row_lanes_of(s.cols);
         *block = dim3(unsigned(s.cols), unsigned(s.row_lanes));
@@ -1696,21 +1785,23 @@ template <typename T, int PART, int OUT, int ACT, bool NT> int run_tiles(const C
     float2 *part = reinterpret_cast<float2 *>(c.scratch(0));
     double2 *moments = reinterpret_cast<double2 *>(c.scratch(0));
     float *table = c.B == 1 ? reinterpret_cast<float *>(c.scratch(c.L.table_off)) : nullptr;
-    const int64_t pairs = (c.L.inside && c.B > c.L.tiles ? c.L.tiles : c.B) * c.G;
+    const int64_t pairs = (c.B > c.L.tiles ? c.L.tiles : c.B) * c.G;
     const unsigned many = unsigned(pairs < 65536 ? pairs : 65536);
     size_t lds;
-    if (c.backward) lds = size_t(tile_values<float2>(threads.x, PART, 2, c.C, c.G, c.L.inside)) * sizeof(float);
-    else lds = size_t(tile_values<double2>(threads.x, PART, 3, c.C, c.G, c.L.inside) + (c.L.inside ? 2 * c.C : 0)) * sizeof(float);
+    const int64_t finish = s.many ? s.slice : 0;
+    if (c.backward) lds = size_t(tile_values<float2>(threads.x, PART, 2, finish, s.group_width)) * sizeof(float);
+    else lds = size_t(tile_values<double2>(threads.x, PART, 3, finish, s.group_width) + 2 * finish) * sizeof(float);
     // what join_tiles keeps: the sums of every row lane, and a sixteenth
     const size_t values = size_t(w.row_lanes) * size_t(c.C), join = (values + c.G * ((values / c.G + 15) / 16)) * (c.backward ? sizeof(float2) : sizeof(double2));
     if (!c.backward) {
         float *low = reinterpret_cast<float *>(c.scratch(c.L.low_off));
         if (c.L.joined) {
-            norm_part_kernel<T, PART, false, kThreads, true><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd, low);
+            norm_part_kernel<T, PART, false, kThreads, kOneSample><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd, low);
             norm_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, low, out, c.o.ldy, moments, c.o.eps, nullptr);
         } else {
-            auto *sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, false> : norm_part_kernel<T, PART, NT, kLargeThreads, false>;
-            if (c.B == 1) sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, true> : norm_part_kernel<T, PART, NT, kLargeThreads, true>;
+            auto *sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, kManySamples> : norm_part_kernel<T, PART, NT, kLargeThreads, kManySamples>;
+            if (c.B == 1) sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, kOneSample> : norm_part_kernel<T, PART, NT, kLargeThreads, kOneSample>;
+            else if (s.pieces > 1) sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, kPieces> : norm_part_kernel<T, PART, NT, kLargeThreads, kPieces>;
             sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd, low);
             if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, table);
             else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, table);
@@ -1722,13 +1813,17 @@ template <typename T, int PART, int OUT, int ACT, bool NT> int run_tiles(const C
         float2 *sums = c.out ? reinterpret_cast<float2 *>(c.scratch(c.L.sums_off)) : nullptr;
         float2 *total = c.B > 1 && (c.dgamma || c.dbeta) ? reinterpret_cast<float2 *>(c.scratch(c.L.total_off)) : nullptr;
         if (c.L.joined) {
-            norm_bwd_part_kernel<T, PART, ACT, false, kThreads><<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, nullptr, nullptr);
+            norm_bwd_part_kernel<T, PART, ACT, false, kThreads, kOneSample><<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, nullptr, nullptr);
             if (c.dgamma || c.dbeta) norm_bwd_columns_kernel<<<unsigned((c.C + 15) / 16), 1024, 0, stream>>>(part, c.L.tiles, int(c.C), c.dgamma, c.dbeta);
             if (c.out)
                 norm_bwd_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, dY, c.o.ldy, w, c.gamma, c.beta, c.mean, c.rstd,
                                                                                                      nullptr, out, c.o.lddx, part, nullptr);
         } else {
-            auto *sum = c.L.threads == kThreads ? norm_bwd_part_kernel<T, PART, ACT, NT, kThreads> : norm_bwd_part_kernel<T, PART, ACT, NT, kLargeThreads>;
+            auto *sum = c.L.threads == kThreads ? norm_bwd_part_kernel<T, PART, ACT, NT, kThreads, kManySamples> : norm_bwd_part_kernel<T, PART, ACT, NT, kLargeThreads, kManySamples>;
+            if (c.B == 1)
+                sum = c.L.threads == kThreads ? norm_bwd_part_kernel<T, PART, ACT, NT, kThreads, kOneSample> : norm_bwd_part_kernel<T, PART, ACT, NT, kLargeThreads, kOneSample>;
+            else if (s.pieces > 1)
+                sum = c.L.threads == kThreads ? norm_bwd_part_kernel<T, PART, ACT, NT, kThreads, kPieces> : norm_bwd_part_kernel<T, PART, ACT, NT, kLargeThreads, kPieces>;
             sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, dY, c.o.ldy, s, c.gamma, c.beta, c.mean, c.rstd, part, total, sums);
             float *dgamma = c.B == 1 ? c.dgamma : nullptr, *dbeta = c.B == 1 ? c.dbeta : nullptr;
             if (sums || dgamma || dbeta) {
