@@ -477,11 +477,12 @@ __device__ __forceinline__ int64_t sample_of_pair(const Shape &s, int64_t p, int
     return b < s.samples.count && s.samples.begin(b) >= i * s.tile_rows && s.samples.begin(b + 1) > end ? b : -1;
 }
 
-// Mean and reciprocal deviation of a sample and group from its parts: THREADS threads for a pair.  One sample: also for every column, as
-// the kernel that writes the result reads them.
+// Mean and reciprocal deviation of a sample and group from its parts: THREADS threads for a pair.  One sample: also for every column the mean o, and w and b of
+// the result act((x - o) w + b).
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const double2 *__restrict__ part, const Shape s, float eps, float *__restrict__ mean,
-                                                             float *__restrict__ rstd, float *__restrict__ low, float *__restrict__ table) {
+                                                             float *__restrict__ rstd, float *__restrict__ low, const float *__restrict__ gamma,
+                                                             const float *__restrict__ beta, float *__restrict__ table) {
     __shared__ double2 red[THREADS / 64];
     const int64_t tiles = (s.N + s.tile_rows - 1) / s.tile_rows;
     const int64_t pairs = (s.samples.count > tiles ? tiles : s.samples.count) * s.G;
@@ -517,9 +518,10 @@ __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const double2 *__re
         }
         if (table)
             for (int k = int(threadIdx.x); k < s.group_width; k += THREADS) {
+                const float w = gamma ? r * gamma[c0 + k] : r;
                 table[c0 + k] = float(mid);
-                table[s.C + c0 + k] = r;
-                table[2 * int64_t(s.C) + c0 + k] = rounding(mid);
+                table[s.C + c0 + k] = w;
+                table[2 * int64_t(s.C) + c0 + k] = (beta ? beta[c0 + k] : 0.0f) - rounding(mid) * w;
             }
     }
 }
@@ -605,14 +607,22 @@ __device__ __forceinline__ const R *join_tiles(const Shape &s, const V *part, in
             for (int j = 0; j < VEC; ++j) add_to(u[j], f(v[k][j], rows, col + j));
         }
     }
-    // [group][row lane][column of it]; columns that two vectors share are written twice, alike
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-        const int group = int(unsigned(col + j) / unsigned(s.group_width));
-        sums[(group * s.row_lanes + threadIdx.y) * s.group_width + col + j - group * s.group_width] = u[j];
-    }
     const int i = int(threadIdx.y) * s.cols + int(threadIdx.x), threads = s.cols * s.row_lanes;
-    const V *all = group_sums(sums, next, s.G, s.row_lanes * s.group_width, i, threads);
+    int run = s.row_lanes * s.group_width;
+    if (s.group_width % VEC == 0) {  // [group][row lane][vector of it]
+        const int each = s.group_width / VEC, vec = col / VEC, group = int(unsigned(vec) / unsigned(each));
+#pragma unroll
+        for (int j = 1; j < VEC; ++j) add_to(u[0], u[j]);
+        sums[(group * s.row_lanes + threadIdx.y) * each + vec - group * each] = u[0];
+        run = s.row_lanes * each;
+    } else {  // [group][row lane][column of it]; columns that two vectors share are written twice, alike
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const int group = int(unsigned(col + j) / unsigned(s.group_width));
+            sums[(group * s.row_lanes + threadIdx.y) * s.group_width + col + j - group * s.group_width] = u[j];
+        }
+    }
+    const V *all = group_sums(sums, next, s.G, run, i, threads);
     R *const out = reinterpret_cast<R *>(all == sums ? next : sums);
     __syncthreads();
     for (int k = i; k < s.G; k += threads) out[k] = g(k, all[k]);
@@ -642,7 +652,7 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
 #pragma unroll
     for (int u = 0; u < kRows; ++u)
         if (r0 + u * s.row_lanes < s.N) strip[u].load(X + (r0 + u * s.row_lanes) * ldx + col);
-    const Affine<VEC> aff(s, col, gamma, beta);
+    const Affine<VEC> aff(s, col, STATS == kOne ? nullptr : gamma, STATS == kOne ? nullptr : beta);
     // z = (x - o) w + (beta - l w): the mean is o + l.  A value that is the mean gives beta where rstd is finite.
     float w[VEC], o[VEC], l[VEC], bt[VEC];
     auto fold = [&]() {
@@ -653,16 +663,10 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
         }
     };
     if constexpr (STATS == kOne) {
-        if (s.group_width % VEC == 0) {  // a vector has one group: its three values instead of three vectors
-            aff.gather(s, mean, 0, o);
-            aff.gather(s, rstd, 0, w);
-            aff.gather(s, low, 0, l);
-        } else {
-            Affine<VEC>::columns(table + col, o);
-            Affine<VEC>::columns(table + s.C + col, w);
-            Affine<VEC>::columns(table + 2 * int64_t(s.C) + col, l);
-        }
-        fold();
+        if (s.group_width % VEC == 0) aff.gather(s, mean, 0, o);  // a vector has one group
+        else Affine<VEC>::columns(table + col, o);
+        Affine<VEC>::columns(table + s.C + col, w);
+        Affine<VEC>::columns(table + 2 * int64_t(s.C) + col, bt);
     } else if constexpr (STATS == kJoin) {
         // distances from the first tile's mean of the group's first column
         const double inv = 1.0 / (double(s.N) * s.group_width);
@@ -1803,9 +1807,9 @@ template <typename T, int PART, int OUT, int ACT, bool NT> int run_tiles(const C
             if (c.B == 1) sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, kOneSample> : norm_part_kernel<T, PART, NT, kLargeThreads, kOneSample>;
             else if (s.pieces > 1) sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, kPieces> : norm_part_kernel<T, PART, NT, kLargeThreads, kPieces>;
             sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd, low);
-            if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, table);
-            else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, table);
-            else norm_stats_kernel<64><<<many, 64, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, table);
+            if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, c.gamma, c.beta, table);
+            else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, c.gamma, c.beta, table);
+            else norm_stats_kernel<64><<<many, 64, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, c.gamma, c.beta, table);
             auto *apply = c.B == 1 ? norm_apply_kernel<T, OUT, ACT, NT, kOne> : norm_apply_kernel<T, OUT, ACT, NT, kMany>;
             apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, low, out, c.o.ldy, nullptr, 0.0f, table);
         }
