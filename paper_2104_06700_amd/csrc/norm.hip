@@ -711,7 +711,8 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
     }
 }
 
-// Per part and column: sum dz and sum dz xh; per tile and column their sums over its parts (total; NULL where there is one sample).
+// Per part and column: sum dz and sum dz xh; per tile and column their sums over its parts (total; NULL where there is one sample).  These are added up in 64
+// bits in LDS: a tile of samples of one row has as many parts as rows, and 8,192 equal terms one after the other in fp32 are off by 3e-5.
 template <typename T, int VEC, int ACT, bool NT, int THREADS, Tiles HOW>
 __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const Shape s,
                                                                  const float *__restrict__ gamma, const float *__restrict__ beta,
@@ -721,13 +722,14 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restr
     extern __shared__ double tile_lds[];
     float *const red_1 = reinterpret_cast<float *>(tile_lds), *const red_x = red_1 + blockDim.x * VEC;
     float2 *const sums = reinterpret_cast<float2 *>(tile_lds);
+    double2 *const totals = reinterpret_cast<double2 *>(tile_lds + tile_values<float2>(blockDim.x, VEC, 2, ONE ? 0 : s.slice, s.group_width) / 2);
     for (int piece = 0; piece < (HOW == kPieces ? s.pieces : 1); ++piece) {
         const Slice<HOW> slice(s, piece);
         const Place<VEC> at(s, slice);
         const Affine<VEC> aff(s, at.col, gamma, beta);
-        float t1[VEC], tx[VEC];
+        if (!ONE && at.row_lane == 0)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) t1[j] = tx[j] = 0.0f;
+            for (int j = 0; j < VEC; ++j) totals[at.lane * VEC + j] = make_double2(0.0, 0.0);
         for_parts<ONE>(s, s.sample_of && blockIdx.y == 0 && piece == 0, [&](int64_t b, int64_t row, int64_t stop) {
             constexpr int U = 4;
             float a1[VEC], ax[VEC];
@@ -789,10 +791,7 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restr
                 for (int j = 0; j < VEC; ++j) {
                     u1[j] = red_1[at.lane * VEC + j];
                     ux[j] = red_x[at.lane * VEC + j];
-                    if constexpr (!ONE) {
-                        t1[j] += u1[j];
-                        tx[j] += ux[j];
-                    }
+                    if constexpr (!ONE) add_to(totals[at.lane * VEC + j], make_double2(u1[j], ux[j]));
                 }
                 if (!whole) {
                     float2 *o = part + slot_of(s, blockIdx.x, begin) * s.C + at.col;
@@ -827,7 +826,10 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restr
         });
         if (!ONE && total && at.active && at.row_lane == 0) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) total[int64_t(blockIdx.x) * s.C + at.col + j] = make_float2(t1[j], tx[j]);
+            for (int j = 0; j < VEC; ++j) {
+                const double2 t = totals[at.lane * VEC + j];
+                total[int64_t(blockIdx.x) * s.C + at.col + j] = make_float2(float(t.x), float(t.y));
+            }
         }
     }
 }
@@ -1277,13 +1279,13 @@ __global__ void __launch_bounds__(512) small_bwd_kernel(const T *X, int64_t ldx,
     typedef Team<VEC, HOW, HOW == kAcross> P;
     const P t(s, small_lds2);
     float gm[VEC], bt[VEC];
-    float2 total[VEC];
+    double2 total[VEC];  // over all samples of a team: thousands, where they are small
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
         const int c = t.c0 + t.col + j;
         gm[j] = gamma && j < t.have ? gamma[c] : 1.0f;
         bt[j] = beta && j < t.have ? beta[c] : 0.0f;
-        total[j] = make_float2(0.0f, 0.0f);
+        total[j] = make_double2(0.0, 0.0);
     }
     const int64_t xstep = s.lanes * ldx, ystep = s.lanes * ldy, ostep = s.lanes * lddx;
     for (int64_t b0 = int64_t(blockIdx.x) * s.teams; b0 < s.samples.count; b0 += int64_t(gridDim.x) * s.teams) {
@@ -1352,8 +1354,7 @@ __global__ void __launch_bounds__(512) small_bwd_kernel(const T *X, int64_t ldx,
         }
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            total[j].x += a[j].x;
-            total[j].y += a[j].y;
+            add_to(total[j], make_double2(a[j].x, a[j].y));
             a[j].x *= gm[j];
             a[j].y *= gm[j];
         }
@@ -1394,7 +1395,7 @@ __global__ void __launch_bounds__(512) small_bwd_kernel(const T *X, int64_t ldx,
     __syncthreads();
     if (in)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) small_lds2[unit * width + t.lane * VEC + j] = total[j];
+        for (int j = 0; j < VEC; ++j) small_lds2[unit * width + t.lane * VEC + j] = make_float2(float(total[j].x), float(total[j].y));
     while (units > 1) {
         const int half = (units + 1) >> 1;
         __syncthreads();
@@ -1553,8 +1554,8 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const T *__restrict__ 
     }
 }
 
-// Workgroups walk over the rows where the parameters' gradients are asked for, with the column sums in registers, and leave them in their row
-// of `part`.
+// Workgroups walk over the rows where the parameters' gradients are asked for, with the column sums of 32 rows in registers and those of all in LDS, and leave
+// them in their row of `part`.  (One after the other, the thousand rows that a thread has of 8 M x 256 are off by 1e-5.)
 template <typename T, int ACT, int NV, bool NT>
 __global__ void __launch_bounds__(kRowThreads) row_bwd_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const PerRow s,
                                                               const float *__restrict__ gamma, const float *__restrict__ beta,
@@ -1571,6 +1572,14 @@ __global__ void __launch_bounds__(kRowThreads) row_bwd_kernel(const T *__restric
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) total[i][j] = make_float2(0.0f, 0.0f);
+    constexpr int RUN = 32 / R;
+    int walked = 0;
+    const auto all = [&](int i, int j) -> float2 & { return row_lds[(i * VEC + j) * kRowThreads + int(threadIdx.x)]; };
+    if (part)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) all(i, j) = make_float2(0.0f, 0.0f);
     const float inv = 1.0f / float(s.K);
     for (int64_t base = int64_t(blockIdx.x) * (at.units * R); base < s.N; base += int64_t(gridDim.x) * (at.units * R)) {
         const int64_t r0 = base + at.unit;
@@ -1621,8 +1630,23 @@ __global__ void __launch_bounds__(kRowThreads) row_bwd_kernel(const T *__restric
                 if (at.active[i]) gnn_store_row<T, VEC, NT>(dX + r * lddx + at.col[i], f[i]);
             }
         }
+        if (part && ++walked == RUN) {
+            walked = 0;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    add_to(all(i, j), total[i][j]);
+                    total[i][j] = make_float2(0.0f, 0.0f);
+                }
+        }
     }
     if (!part) return;  // the same for the whole launch
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) add_to(total[i][j], all(i, j));
+    __syncthreads();
     // the rows of a wavefront, then the wavefronts
     const int width = NV * VEC * s.lanes, wave = int(threadIdx.x) >> 6;
 #pragma unroll
@@ -1793,7 +1817,7 @@ template <typename T, int PART, int OUT, int ACT, bool NT> int run_tiles(const C
     const unsigned many = unsigned(pairs < 65536 ? pairs : 65536);
     size_t lds;
     const int64_t finish = s.many ? s.slice : 0;
-    if (c.backward) lds = size_t(tile_values<float2>(threads.x, PART, 2, finish, s.group_width)) * sizeof(float);
+    if (c.backward) lds = size_t(tile_values<float2>(threads.x, PART, 2, finish, s.group_width) + (s.many ? 4 * s.cols * PART : 0)) * sizeof(float);
     else lds = size_t(tile_values<double2>(threads.x, PART, 3, finish, s.group_width) + 2 * finish) * sizeof(float);
     // what join_tiles keeps: the sums of every row lane, and a sixteenth
     const size_t values = size_t(w.row_lanes) * size_t(c.C), join = (values + c.G * ((values / c.G + 15) / 16)) * (c.backward ? sizeof(float2) : sizeof(double2));
@@ -1979,7 +2003,7 @@ template <typename T, int ACT, int NV, bool NT> int run_rows(const Call &c, cons
         const bool sums = c.dgamma || c.dbeta;
         float2 *part = sums ? reinterpret_cast<float2 *>(c.scratch(0)) : nullptr;
         const int64_t rows = c.N * c.C < kLarge ? kRowParts / 2 : kRowParts, most = !sums ? most_workgroups(kRowThreads) : rows < c.L.parts ? rows : c.L.parts, grid = blocks < most ? blocks : most;
-        const size_t lds = sums ? size_t(kRowThreads / 64 - 1) * NV * gnn_rows<T>::VEC * s.lanes * sizeof(float2) : 0;
+        const size_t lds = sums ? size_t(kRowThreads) * NV * gnn_rows<T>::VEC * sizeof(float2) : 0;  // (joined in less: three wavefronts' lanes)
         row_bwd_kernel<T, ACT, NV, NT><<<unsigned(grid), kRowThreads, lds, stream>>>(X, c.o.ldx, static_cast<const T *>(c.dY), c.o.ldy, s, c.gamma, c.beta, c.mean,
                                                                                      c.rstd, static_cast<T *>(c.out), c.o.lddx, part);
         if (part) norm_bwd_columns_kernel<<<unsigned((c.C + 15) / 16), 1024, 0, stream>>>(part, grid, int(c.C), c.dgamma, c.dbeta);
