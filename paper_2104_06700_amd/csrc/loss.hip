@@ -6,8 +6,8 @@
 // of a wavefront (or a whole workgroup) have a row, and a workgroup ends with its rows.  Rows wider than that are read twice.
 //
 // Three launches: the labelled rows of every piece of the label array are counted, the rows are done with the sum of these
-// counts, and the workgroups' sums of row losses are added in their order; results do not depend on timing.  Up to kCountHere rows
-// every workgroup counts by itself, which is one launch less.
+// counts, and the workgroups' sums of row losses are added in their order; results do not depend on timing.  Of few rows every workgroup
+// counts by itself, which is one launch less.
 //
 // Bound by the memory in wide rows (24,490 x 8,195 bf16, all labelled, 176 us = 4.6 TB/s, a workgroup's row waits twice for all its wavefronts), by
 // instructions in narrow ones (2.4 M x 47 fp32, 8 % labelled, 98 us = 5.2 TB/s).
@@ -18,7 +18,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kCountBlocks = 256;       // partial counts
-constexpr int64_t kCountHere = 16384;
+// Rows up to which every workgroup counts all labels; Wide: where a row is a workgroup, so that the labels are read once a row (us, counted there and by a
+// launch of its own: 4,096 rows of 16, 47, 200, 500 fp32 7.9 10.4, 8.9 10.4, 9.9 10.5, 9.5 10.4; 5,000 8.7 9.5, 9.9 9.6, 11.2 10.3, 11.1 10.2; 16,384 14.9
+// 10.3 to 37.6 18.0.  Rows of 1,100: 1,300 9.2 11.2, 2,048 11.9 11.9, 2,900 15.4 12.8, 4,096 21.6 14.8, 16,384 151 33).
+constexpr int64_t kCountHere = 4096, kCountHereWide = 2048;
 constexpr int kLossBlocks = 65536;      // partial losses at most
 constexpr int64_t kMostStride = 1 << 22;  // 128 rows of it are offsets of 32 bits
 
@@ -345,6 +348,9 @@ template <typename T, int VEC, int LANES, int NV, int PASSES, int WEIGHT> int la
     return blocks;
 }
 
+// a workgroup has one row at a time
+template <typename T> bool wide(const Call &c) { return c.C > 128 * gnn_rows<T>::VEC || c.ldx >= kMostStride || c.ldg >= kMostStride; }
+
 template <typename T, int WEIGHT> int rows(const T *X, T *dX, const Call &c) {
     constexpr int V = gnn_rows<T>::VEC;
     if (c.ldx < kMostStride && c.ldg < kMostStride) {
@@ -368,7 +374,7 @@ template <typename T, int WEIGHT> int rows(const T *X, T *dX, const Call &c) {
 template <typename T> int xent(const T *X, T *dX, const Call &c) {
     int blocks;
     if (!c.mean) blocks = rows<T, kSum>(X, dX, c);
-    else if (c.N <= kCountHere) blocks = rows<T, kMeanHere>(X, dX, c);
+    else if (c.N <= (wide<T>(c) ? kCountHereWide : kCountHere)) blocks = rows<T, kMeanHere>(X, dX, c);
     else {
         count_labels_kernel<<<kCountBlocks, 1024, 0, c.stream>>>(c.labels, c.N, c.counts);
         blocks = rows<T, kMeanCounted>(X, dX, c);
