@@ -1782,14 +1782,17 @@ Shape shape_of(const Call &c, int vec, int rows, dim3 *grid, dim3 *block) {  // 
     s.cols = int((vecs + chunks - 1) / chunks);
     s.slice = s.cols * vec;
     if (!rows && s.many) {
-        s.slice = int(K <= kSlice ? (kSlice / K < c.G ? kSlice / K : c.G) * K : kSlice);
         if (K > kSlice) {
-            s.pieces = int((K + kSlice - 1) / kSlice);
-            s.slice = int((K + s.pieces - 1) / s.pieces);
+            const int64_t pieces = (K + kSlice - 1) / kSlice;
+            s.slice = int((K + pieces - 1) / pieces);
             s.pieces = int((K + s.slice - 1) / s.slice);
+            chunks = c.G;
+        } else {  // alike: a narrow last slice takes as many workgroups as a wide one
+            const int64_t most = kSlice / K, slices = (c.G + most - 1) / most;
+            s.slice = int((c.G + slices - 1) / slices * K);
+            chunks = (c.C + s.slice - 1) / s.slice;
         }
         s.cols = (s.slice + vec - 1) / vec;
-        chunks = K > kSlice ? c.G : (c.C + s.slice - 1) / s.slice;
     }
     if (rows) {
         s.row_lanes = row_lanes_of(s.cols);
@@ -1938,7 +1941,7 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
         pairs = pairs > columns ? pairs : columns;
     } else pairs += size_t(groups * K);
     p.lds = pairs * sizeof(float2);
-    return p.grid.y <= 65535 && p.lds <= 65536;
+    return p.grid.y <= 65535 && p.lds <= (160u << 10);
 }
 
 // Workgroups of small_bwd_kernel that are resident at once: wavefronts of its registers on the 256 CUs, and what fits their LDS.  More would be

@@ -38,3 +38,11 @@ def test_a_row_unlike_the_rest(kind, c, groups):
     x = torch.cat([unlike(kind, b - a, c, a + c) for a, b in zip(ptr, ptr[1:])])
     x[61:64, :7] += 500  # columns unlike the rest of their group
     check_statistics(x, groups, kind, ptr, rounded=False)
+
+
+@pytest.mark.parametrize("c,groups,dtype", [(8004, 4, torch.bfloat16), (8190, 9, torch.bfloat16), (4086, 9, torch.float32)])
+def test_few_rows_in_many_samples(c, groups, dtype):
+    """A workgroup's sums and parameters are more than 64 KB there."""
+    for rows in (1, 3, 9):
+        print("few rows", rows, c, groups, dtype, flush=True)
+        check(260 * rows, c, groups, list(range(0, 260 * rows + 1, rows)), "silu", dtype, uniform=1)
