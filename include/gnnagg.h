@@ -407,7 +407,9 @@ GNN_API int64_t gnn_sage_layer_workspace_bytes(int64_t N, int64_t F_in, int64_t 
  *     mean, var = their mean and (biased) variance,  rstd = 1 / sqrt(var + eps),
  *     Y[v, c] = act( (X[v, c] - mean) rstd gamma[c] + beta[c] )
  * X, Y [N, C] fp32 or bf16, not overlapping; gamma, beta [C] fp32 or NULL (1 and 0); mean, rstd [B, G] fp32, written (an empty sample
- * has mean 0 and rstd 1 / sqrt(eps)).  All sums are fp32 or wider, of distances from a value near the mean. */
+ * beside others has mean 0 and rstd 1 / sqrt(eps)).  All sums are fp32 or wider, var is one of squared distances from a value near the mean, and Y is
+ * formed from the mean before it is rounded to fp32: neither one row far from the others nor a mean far beyond the deviation costs it bits.
+ * Of equal values it is act(beta), with eps > 0. */
 typedef enum gnn_act { GNN_ACT_NONE = 0, GNN_ACT_RELU = 1, GNN_ACT_SILU = 2 /* z / (1 + exp(-z)) */ } gnn_act;
 typedef struct gnn_norm_opts {
     int32_t dtype;        /* gnn_dtype of X, Y, dY and dX */
@@ -420,8 +422,8 @@ typedef struct gnn_norm_opts {
     void *workspace;      /* device scratch of gnn_group_norm_workspace_bytes(), 16-byte aligned; nothing is kept in it */
     int64_t workspace_bytes;
 } gnn_norm_opts;
-/* Asynchronous on opts->stream; allocates nothing.  N == 0 or C == 0 is GNN_OK and does nothing.  At most 2^31 - 1 rows and samples and
- * 2^24 channels. */
+/* Asynchronous on opts->stream; allocates nothing.  N == 0 or C == 0 is GNN_OK and does nothing: mean and rstd are not written either.  At
+ * most 2^31 - 1 rows and samples and 2^24 channels. */
 GNN_API int gnn_group_norm_fwd(const void *X, const float *gamma, const float *beta, const void *sample_ptr, void *Y, float *mean,
                                float *rstd, int64_t N, int64_t C, int64_t G, int64_t B, const gnn_norm_opts *opts);
 /* Gradients of sum dY Y: dX [N, C] (type of X; does not overlap X or dY), dgamma, dbeta [C] fp32; each may be NULL.  X, gamma, beta
@@ -431,6 +433,7 @@ GNN_API int gnn_group_norm_fwd(const void *X, const float *gamma, const float *b
 GNN_API int gnn_group_norm_bwd(const void *X, const float *gamma, const float *beta, const float *mean, const float *rstd,
                                const void *dY, const void *sample_ptr, void *dX, float *dgamma, float *dbeta, int64_t N, int64_t C,
                                int64_t G, int64_t B, const gnn_norm_opts *opts);
+/* backward != 0: enough for both calls */
 GNN_API int64_t gnn_group_norm_workspace_bytes(int64_t N, int64_t C, int64_t G, int64_t B, int backward);
 
 /* Softmax cross-entropy of the labelled vertices, with the gradient of the class scores X [N, C] (fp32 or bf16) in the same pass.
@@ -466,7 +469,8 @@ GNN_API int64_t gnn_softmax_xent_workspace_bytes(int64_t N, int64_t C);
  * random bits are the upper ones of h, all mod 2^32:
  *     h = (i mod 2^32) 0x9E3779B9 + (i div 2^32) 0x6A09E667 + seed + step 0x3C6EF373 + k 0xBB67AE85;
  *     h = (h xor h >> 16) 0x6A09E667;  h = (h xor h >> 15) 0xBB67AE85
- * Gradients that are not finite make their own element's parameter and states NaN (or fp32 what the formulas give), no other's. */
+ * Gradients that are not finite make their own element's parameter and states NaN (or fp32 what the formulas give), no other's; in 8 bits so does one
+ * whose square is not, from about 1.8e19 on. */
 #define GNN_ADAMW_BLOCK 256
 typedef struct gnn_adamw_tensor {
     void *param;           /* [n] of dtype, updated */

@@ -2,6 +2,7 @@
 //
 // For a row x of C scores with label t:   m = max_j x_j,  s = sum_j exp(x_j - m),  loss = log s + m - x_t,
 //     dx_j = w (exp(x_j - m) / s - [j = t]),   w = scale, or scale / number of labelled rows.
+// exp and log are one instruction and a product in 32 bits each; an exponential of d is off by about (1 + |d|) 2^-22, less than a gradient in bf16 keeps.
 // A row without a label is not read; its gradient is 0.  Every row is read once and stays in registers, 16 bytes a lane: LANES lanes
 // of a wavefront (or a whole workgroup) have a row, and a workgroup ends with its rows.  Rows wider than that are read twice.
 //

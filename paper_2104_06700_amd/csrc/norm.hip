@@ -8,6 +8,10 @@
 //     dbeta[c] = sum dz,  dgamma[c] = sum dz xh  (over all rows),
 //     s1 = sum dz gamma / n,  s2 = sum dz gamma xh / n  (over the sample and group),  dX = rstd (dz gamma - s1 - xh s2).
 //
+// Sums of up to a few tens of values are formed in fp32, what they come to is joined in 64 bits or in a second level of fp32.  Neither statistic is a difference of
+// large numbers: variances are sums of squared distances from the mean or from a value close to it, and a mean keeps what fp32 rounds off it until the
+// result is formed.  The backward pass is given the rounded one.
+//
 // Three ways.  Rows that are samples of their own stay in the registers of a few lanes (row_kernel, row_bwd_kernel; 2.4 M x 256 fp32 in one group 846 us =
 // 5.9 TB/s, gradients 1460 = 5.2).  Samples that fit a workgroup, or nearly, are read once and done in one launch (small_kernel, small_bwd_kernel; 2,449
 // graphs of 25 vertices x 100 fp32 forward 20 us, gradients 32, bound by the chain load, sum, barrier, store of each).  All others: the
@@ -17,8 +21,6 @@
 // memory: 2.4 M x 256 fp32 in 32 groups forward 372 us (6.7 TB/s) and 782 (6.4), gradients 741 (6.8) and 1188 (6.3), merging 14.
 #include "common.h"
 #include "rows.h"
-
-#include <type_traits>
 
 namespace {
 
@@ -1008,7 +1010,8 @@ template <typename T> __host__ __device__ constexpr int held() { return 16 / gnn
 
 // A team of threads has a sample's rows of `groups` neighbouring groups in registers: cols x lanes threads, thread (lane, row
 // lane) the vector `lane` of every lanes-th row.  The last vector ends with the columns: those that it shares with the one before it are computed by
-// both to the same bits (2,449 graphs of 25 vertices x 100 bf16, backward, with a short last vector instead 90 us, so 69).  Fewer columns than a vector has are one short vector.
+// both to the same bits (a short last vector in its place was a third slower: 2,449 graphs of 25 vertices x 100 bf16, backward, 90 us and 69).  Fewer columns than a
+// vector has are one short vector.
 struct Small {
     Samples samples;
     int C, G, K;
@@ -1751,7 +1754,7 @@ struct Call {
     char *scratch(int64_t off) const { return static_cast<char *>(o.workspace) + off; }
 };
 
-// Rows of `cols` vectors that fill whole wavefronts best, in workgroups of about 256 threads.
+// Rows of `cols` vectors that fill whole wavefronts best, in workgroups of up to kBlockMost threads.
 int row_lanes_of(int cols) {
     int best = 1;
     double share = 0.0;
