@@ -12,21 +12,21 @@
 // large numbers: variances are sums of squared distances from the mean or from a value close to it, and a mean keeps what fp32 rounds off it until the
 // result is formed.  The backward pass is given the rounded one.
 //
-// Three ways.  Rows that are samples of their own stay in the registers of a few lanes (row_kernel, row_bwd_kernel; 2.4 M x 256 fp32 in one group 846 us =
-// 5.9 TB/s, gradients 1460 = 5.2).  Samples that fit a workgroup, or nearly, are read once and done in one launch (small_kernel, small_bwd_kernel; 2,449
-// graphs of 25 vertices x 100 fp32 forward 20 us, gradients 32, bound by the chain load, sum, barrier, store of each).  All others: the
+// Three ways.  Rows that are samples of their own stay in the registers of a few lanes (row_kernel, row_bwd_kernel; 2.4 M x 256 fp32 in one group 851 us =
+// 5.9 TB/s, gradients 1457 = 5.2).  Samples that fit a workgroup, or nearly, are read once and done in one launch (small_kernel, small_bwd_kernel; 2,449
+// graphs of 25 vertices x 100 fp32 forward 21 us, gradients 31, bound by the chain load, sum, barrier, store of each).  All others: the
 // rows are cut into tiles of equal size whatever the samples' sizes are, one workgroup each, which adds up each sample's part of
 // it per column.  A sample inside a tile is finished there; of one that crosses tiles, each leaves its partial sums in a slot of its own, and a second
 // kernel merges them in their order: results do not depend on timing.  A third reads the rows again and writes the result.  Both readers are bound by the
-// memory: 2.4 M x 256 fp32 in 32 groups forward 372 us (6.7 TB/s) and 782 (6.4), gradients 741 (6.8) and 1188 (6.3), merging 14.
+// memory: 2.4 M x 256 fp32 in 32 groups forward 383 us (6.5 TB/s) and 773 (6.5), gradients 743 (6.8) and 1189 (6.3), merging 13.
 #include "common.h"
 #include "rows.h"
 
 namespace {
 
 // Tiles of at least kTileValues values, at most kTiles of them with kThreads threads each; matrices of kLarge values and more in kLargeTiles with
-// kLargeThreads.  Few tiles are few partial sums to merge (103 K x 141 in 3 groups, backward, 512 tiles 41 us, 1024 47, 2048 of half the threads
-// 72), many small workgroups read best (2.4 M x 256 forward, 512 tiles 1186 us, 2048 of half the threads 1163).
+// kLargeThreads.  Few tiles are few partial sums to merge (103 K x 141 bf16 in 3 groups, backward, 512 tiles 43 us, 1024 49, 2048 of half the threads
+// 47); beside much data that does not count (2.4 M x 256 fp32 forward, 512 tiles 1154 us, 2048 of half the threads 1171; 3.5 M x 128 bf16 backward 748, 738).
 constexpr int kThreads = 512, kLargeThreads = 256;
 constexpr int64_t kTiles = 512, kLargeTiles = 2048, kLarge = int64_t(1) << 28, kTileValues = 16384;
 constexpr int64_t kSmallParts = 4096;   // at most so many workgroups of samples that fit one leave column sums
@@ -574,8 +574,7 @@ template <int VEC> struct Affine {
 // The kernels that write results: a workgroup of cols x row_lanes threads has rows_of() * row_lanes neighbouring rows and ends with them, a thread
 // rows_of() vectors of one column.  Small workgroups that end are faster here than ones that stay and walk: the writes
 // and reads of all of them move through the matrix as one front (2.5 GB copied by one-vector threads 6.5 TB/s, four vectors 6.1, resident
-// workgroups 5.0; norm of 2.4 M x 256 fp32 in workgroups of 128 threads with 1, 2, 4, 8 rows each 1268, 1159, 1205, 1224 us, of 256 threads with 2, 4, 8 1202,
-// 1237, 1248).
+// workgroups 5.0; norm of 2.4 M x 256 fp32 in workgroups of 128 threads with 1, 2, 4, 8 rows each 1301, 1170, 1225, 1242 us, of 256 threads with 2 1200).
 constexpr int kBlockMost = 128;
 template <int VEC> __device__ __forceinline__ int column_of_block(const Shape &s) {
     const int vec = int(blockIdx.y) * s.cols + int(threadIdx.x);
@@ -639,7 +638,8 @@ __device__ __forceinline__ int64_t sample_of_row(const Shape &s, int64_t r) {
 
 enum Stats { kMany, kOne, kJoin };  // statistics of many samples, of one (a table of columns), of one that has to be joined from tiles first
 
-// rows of a thread: with two the parameters of the gradient of a bf16 vector, six for each of eight columns, are more than its data
+// rows of a thread: with two the parameters of the gradient of a bf16 vector, six for each of eight columns, are more than its data (3.5 M x 128, two
+// 786 us, four 736, eight 735; its forward pass 445, 445, 448)
 template <typename T> __host__ __device__ constexpr int rows_of(bool backward) { return sizeof(T) == 4 || !backward ? 2 : 4; }
 
 template <typename T, int VEC, int ACT, bool NT, Stats STATS>
@@ -715,8 +715,9 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
 
 // Per part and column: sum dz and sum dz xh; per tile and column their sums over its parts (total; NULL where there is one sample).  These are added up in 64
 // bits in LDS: a tile of samples of one row has as many parts as rows, and 8,192 equal terms one after the other in fp32 are off by 3e-5.
+// (Four wavefronts a SIMD at most: the seven that have room in bf16 read slower, 1.1 M x 351 785 -> 808 us.)
 template <typename T, int VEC, int ACT, bool NT, int THREADS, Tiles HOW>
-__global__ void __launch_bounds__(THREADS) norm_bwd_part_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const Shape s,
+__global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(1, 4))) norm_bwd_part_kernel(const T *__restrict__ X, int64_t ldx, const T *__restrict__ dY, int64_t ldy, const Shape s,
                                                                  const float *__restrict__ gamma, const float *__restrict__ beta,
                                                                  const float *__restrict__ mean, const float *__restrict__ rstd,
                                                                  float2 *__restrict__ part, float2 *__restrict__ total, float2 *__restrict__ sums_out) {
@@ -1890,8 +1891,8 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     const int64_t rows = c.sample_ptr ? c.o.max_sample_rows : c.N / c.B;
     if (rows <= 0) return false;
     const int64_t K = c.C / c.G;
-    // many samples may have four times the rows that the registers of the largest workgroup hold: 612 graphs of 0 to 200 vertices x 128 bf16, 25 us, in
-    // tiles 78; sixteen times, 1,000 graphs of 0 to 800 x 64 backward, 147, in tiles 136
+    // many samples may have four times the rows that the registers of the largest workgroup hold: 612 graphs of 0 to 200 vertices x 128 bf16, 20 us, in
+    // tiles 81, backward 47 and 65; sixteen times, 1,000 graphs of 0 to 800 x 64 backward, 148, in tiles 136
     auto fits = [&](int64_t groups) {
         const int64_t cols = (groups * K + vec - 1) / vec;
         return cols <= most && rows <= (c.B < 256 ? 1 : 4) * held * (most / cols);
@@ -1905,15 +1906,14 @@ bool small_plan(const Call &c, int vec, int held, int most, SmallPlan &p) {
     while (groups > 1 && !fits(groups)) groups = (groups + 1) / 2;
     if (!fits(groups)) return false;
     // Slices of a row narrower than two 128-byte lines fetch lines that others fetch too: 100 samples of 1,000 rows, slices of 10 of 100 columns,
-    // 69 us, in tiles 25.
+    // 50 us, in tiles 38.
     if (groups < c.G && groups * K * (16 / vec) < 256 && c.N * c.C > (64 << 10)) return false;
     const int64_t cols = (groups * K + vec - 1) / vec;
     int64_t lanes = (rows + held - 1) / held;
     // A workgroup of 64 to 512 threads with about seven vectors each of a mean sample; what does not stay in its registers is fetched again by the
     // later passes, from the caches.  More threads wait for each other at every sum, fewer have too long a way through their rows (us; 2,449 graphs
-    // of 25 vertices, ragged, forward: 100 bf16 columns 64 threads 24, 128 27, 256 37, 384 that hold the longest 63; 100 fp32 31, 20, 23, 40;
-    // 256 fp32 62, 40, 35, 74.  612 graphs of 100 x 128 fp32 55, 30, 21 and 512 threads 18).  Backward, with its column sums to join, 256 (100 fp32 128
-    // threads 37, 256 33, 384 51).
+    // of 25 vertices, ragged, forward, 64, 128, 256 and 512 threads: 100 bf16 columns 21, 22, 29, 49; 100 fp32 29, 21, 29, 45; 256 fp32 57, 37, 32, 34.
+    // 612 graphs of 100 x 128 fp32 51, 29, 19, 17).  Backward, with its column sums to join, 256 (100 fp32 128 threads 37, 256 32, 384 51).
     const int64_t mean = (c.N + c.B - 1) / c.B;
     int64_t wide = c.backward ? kTeam : 2 * kTeam;
     while (!c.backward && wide > 64 && cols <= wide / 2 && mean * cols <= wide / 2 * 7) wide /= 2;
@@ -2034,9 +2034,9 @@ template <typename T, int ACT> int run_act(const Call &c) {
     if (small_plan(c, V, held<T>(), c.backward ? 512 : 1024, p))
         return p.how == kInside ? run_small<T, ACT, kInside>(c, p) : p.how == kAcross ? run_small<T, ACT, kAcross>(c, p) : run_small<T, ACT, kShort>(c, p);
     if (c.C < V) return run_tiles<T, 1, 1, ACT, false>(c);
-    // The backward sums keep eleven values for every column: with eight bf16 columns a thread only two of its wavefronts fit a SIMD, and half vectors are faster
-    // (us, eight -> four; 400 K x 128 silu 128 -> 109, 1 M x 256 446 -> 424, 103 K x 141 69 -> 47, 1.1 M x 351 identity 740 -> 765).  Results are written
-    // as whole vectors (1.1 M x 351 840 -> 765, 3.5 M x 128 749 -> 726).
+    // The backward sums keep many values for every column: with eight bf16 columns a thread two or three of its wavefronts fit a SIMD, and half vectors are
+    // faster (us, eight -> four; 400 K x 128 silu 121 -> 115, 1 M x 256 441 -> 430, 103 K x 141 52 -> 43, 3.5 M x 128 738 either way, 1.1 M x 351 identity
+    // 744 -> 785).  Results are written as whole vectors (halves instead: 1.1 M x 351 859, 3.5 M x 128 757).
     if (c.backward) return c.past_caches ? run_tiles<T, 4, V, ACT, true>(c) : run_tiles<T, 4, V, ACT, false>(c);
     return c.past_caches ? run_tiles<T, V, V, ACT, true>(c) : run_tiles<T, V, V, ACT, false>(c);
 }
