@@ -108,6 +108,7 @@ struct Shape {
     int C, group_width, G;
     int cols;       // vectors of columns of a workgroup; threads: cols x row_lanes
     int row_lanes;
+    int join;       // row lanes that are left after the first joining of their moments: a power of two of groups of a thread for each column
     int32_t *sample_of;  // [N] ragged samples: the sample of every row, for the kernels that write results
     bool many;      // samples: those inside a tile are finished there
     // Columns are worked on in slices of at most `slice`: of neighbouring vectors where there is one sample, else of whole groups, or a group in `pieces`
@@ -233,35 +234,40 @@ template <typename V> __host__ __device__ constexpr int64_t tile_values(int64_t 
     return (own > sums ? own : sums) + 3 & ~int64_t(3);
 }
 
-// Joins the moments (mean, sum of squared distances from it) of some values to those of others before: share = their part of all, weight =
-// share * number of values before
-template <typename M> __device__ __forceinline__ void join(M &mean, float &m2, M other, float other_m2, float share, float weight) {
-    const M d = other - mean;
-    mean += d * M(share);
-    m2 += other_m2 + float(d) * float(d) * weight;
-}
-
 // What a mean loses when it is rounded to fp32.  The results are formed from both: of values whose mean is 10,000 times their deviation a half unit of
 // the mean's last place is 5e-4 of the deviation.
 __device__ __forceinline__ float rounding(double mean) { return float(mean - double(float(mean))); }
 
-// The moments of a tile's row lanes, each of `each` rows and one more in the first `rest` lanes, are joined in LDS: mean and m2
-// [row_lanes][cols * VEC], the result in row lane 0's places.
-template <int VEC> __device__ __forceinline__ void join_row_lanes(double *mean, float *m2, const Shape &s, const Place<VEC> &at, int each, int rest) {
-    const int width = s.cols * VEC;
-    const auto count = [&](int first, int end) { return (end - first) * each + (rest > first ? (rest < end ? rest : end) - first : 0); };
-    for (int step = 1; step < s.row_lanes; step *= 2) {
+// The moments (mean, sum of squared distances from it) of a tile's row lanes, each of `each` rows and one more in the first `rest` lanes, are joined in
+// LDS: mean and m2 [row_lanes][cols * VEC], the result in row lane 0's places.  A thread has a column and every `join`-th row lane, then every
+// eighth of that, and the last: fewer columns side by side have more threads each.  About the mean of a join's first lane, sum n d^2 - (sum n d)^2 / n takes off at
+// most as many times what it leaves as there are lanes, some sixteen.
+__device__ __forceinline__ void join_row_lanes(double *mean, float *m2, const Shape &s, int width, int each, int rest) {
+    const int group = int(threadIdx.x) / width, first = int(threadIdx.x) - group * width;
+    int have = s.row_lanes;  // so many moments of each column, of the lanes l, l + have, ..
+    for (int groups = s.join; have > 1; groups = groups > 8 ? groups >> 3 : 1) {
+        const auto rows = [&](int l) {
+            return have == s.row_lanes ? each + (l < rest) : each * ((s.row_lanes - l + have - 1) / have) + (rest > l ? (rest - l + have - 1) / have : 0);
+        };
         __syncthreads();
-        const int other = at.row_lane + step;
-        if (!at.active || (at.row_lane & (2 * step - 1)) || other >= s.row_lanes) continue;
-        const int n = count(other, other + step < s.row_lanes ? other + step : s.row_lanes);
-        if (n == 0) continue;
-        const float before = float(count(at.row_lane, other)), share = float(n) * __builtin_amdgcn_rcpf(before + float(n));
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            const int i = at.row_lane * width + at.lane * VEC + j, o = i + step * width;
-            join(mean[i], m2[i], mean[o], m2[o], share, share * before);
-        }
+        if (group < groups)
+            for (int c = first; c < width; c += int(blockDim.x)) {
+                const int at = group * width + c;
+                const double center = mean[at];
+                float n = float(rows(group)), a = 0.0f, q = m2[at];
+                for (int l = group + groups; l < have; l += groups) {
+                    const float k = float(rows(l)), d = float(mean[l * width + c] - center);
+                    n += k;
+                    a += k * d;
+                    q += m2[l * width + c] + k * d * d;
+                }
+                if (n > 0.0f) {
+                    const float off = a * __builtin_amdgcn_rcpf(n), rest_of = q - a * off;
+                    mean[at] = center + double(off);
+                    m2[at] = rest_of < 0.0f ? 0.0f : rest_of;
+                }
+            }
+        have = groups;
     }
     __syncthreads();
 }
@@ -337,7 +343,9 @@ __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict_
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
                         const float o = t1[j] * inv, q = t2[j] - t1[j] * o;
-                        join(off[j], m2[j], o, q < 0.0f ? 0.0f : q, share, weight);
+                        const float d = o - off[j];
+                    off[j] += d * share;
+                    m2[j] += (q < 0.0f ? 0.0f : q) + d * d * weight;
                         const float next = base[j] + off[j];  // the next run's distances are from here
                         off[j] -= next - base[j];
                         base[j] = next;
@@ -352,7 +360,7 @@ __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict_
                     red_1[threadIdx.x * VEC + j] = double(base[j]) + double(off[j]);
                     red_2[threadIdx.x * VEC + j] = m2[j];
                 }
-            join_row_lanes<VEC>(red_1, red_2, s, at, each, rest);
+            join_row_lanes(red_1, red_2, s, s.cols * VEC, each, rest);
             const int64_t begin = ONE ? 0 : s.samples.begin(b);
             const bool whole = !ONE && begin == row && s.samples.begin(b + 1) == stop;  // the same for all threads
             const bool mine = at.active && at.row_lane == 0;
@@ -389,7 +397,7 @@ __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict_
                     double var = all[g].y * inv - off * off, mid = means[g * slice.run] + off;
                     if constexpr (HOW == kPieces) {  // one group: this thread's in every piece
                         double2 so_far = make_double2(mid, var * slice.run);
-                        if (!slice.first) {  // as in join(): mean, and the sum over columns of squared distances
+                        if (!slice.first) {  // the mean, and the sum over columns of squared distances from it
                             const double2 before = s.open[b * s.G + slice.group];
                             const double n = slice.run, m = slice.c0 - int(blockIdx.y) * s.group_width, d = mid - before.x;
                             so_far = make_double2(before.x + d * (n / (m + n)), before.y + so_far.y + d * d * (m * n / (m + n)));
@@ -1804,6 +1812,7 @@ Shape shape_of(const Call &c, int vec, int rows, dim3 *grid, dim3 *block) {  // 
         *grid = spread((c.N + rows * s.row_lanes - 1) / (rows * s.row_lanes), unsigned(chunks), block->x);
     } else {
         s.row_lanes = c.L.threads / s.cols;
+        for (s.join = 1; 2 * s.join * s.cols * vec <= c.L.threads && 2 * s.join < s.row_lanes;) s.join *= 2;
         *block = dim3(unsigned(c.L.threads));
         *grid = dim3(unsigned(c.L.tiles), unsigned(chunks));
     }
