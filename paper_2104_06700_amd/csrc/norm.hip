@@ -234,18 +234,18 @@ template <typename V> __host__ __device__ constexpr int64_t tile_values(int64_t 
     return (own > sums ? own : sums) + 3 & ~int64_t(3);
 }
 
-// What a mean loses when it is rounded to fp32.  The results are formed from both: of values whose mean is 10,000 times their deviation a half unit of
+// A mean in fp32 and what it loses there.  The results are formed from both: of values whose mean is 10,000 times their deviation a half unit of
 // the mean's last place is 5e-4 of the deviation.
-__device__ __forceinline__ float rounding(double mean) { return float(mean - double(float(mean))); }
+__device__ __forceinline__ float2 two_floats(double mean) { return make_float2(float(mean), float(mean - double(float(mean)))); }
 
 // The moments (mean, sum of squared distances from it) of a tile's row lanes, each of `each` rows and one more in the first `rest` lanes, are joined in
-// LDS: mean and m2 [row_lanes][cols * VEC], the result in row lane 0's places.  A thread has a column and every `join`-th row lane, then every
-// eighth of that, and the last: fewer columns side by side have more threads each.  About the mean of a join's first lane, sum n d^2 - (sum n d)^2 / n takes off at
-// most as many times what it leaves as there are lanes, some sixteen.
+// LDS: mean and m2 [row_lanes][cols * VEC], the result in row lane 0's places.  A thread has a column and every `join`-th row lane, eight or
+// more of them, and so on to the last sixteen at most: narrow rows have more threads a column.  About the mean of a join's first lane,
+// sum n d^2 - (sum n d)^2 / n takes off at most as many times what it leaves as there are lanes in it.
 __device__ __forceinline__ void join_row_lanes(double *mean, float *m2, const Shape &s, int width, int each, int rest) {
     const int group = int(threadIdx.x) / width, first = int(threadIdx.x) - group * width;
     int have = s.row_lanes;  // so many moments of each column, of the lanes l, l + have, ..
-    for (int groups = s.join; have > 1; groups = groups > 8 ? groups >> 3 : 1) {
+    for (int groups = s.join; have > 1; groups = groups > 16 ? groups >> 3 : 1) {
         const auto rows = [&](int l) {
             return have == s.row_lanes ? each + (l < rest) : each * ((s.row_lanes - l + have - 1) / have) + (rest > l ? (rest - l + have - 1) / have : 0);
         };
@@ -279,7 +279,7 @@ __device__ __forceinline__ void join_row_lanes(double *mean, float *m2, const Sh
 // row in front of 16,384 of mean 100 and deviation 1 costs rstd 4e-4.
 template <typename T, int VEC, bool NT, int THREADS, Tiles HOW>
 __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, double2 *__restrict__ part, float eps,
-                                                             float *__restrict__ mean_out, float *__restrict__ rstd_out, float *__restrict__ low) {
+                                                             float *__restrict__ mean_out, float *__restrict__ rstd_out, float2 *__restrict__ exact) {
     constexpr bool ONE = HOW == kOneSample;
     extern __shared__ double tile_lds[];
     double *const red_1 = tile_lds;
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict_
                 for (int g = 0; g < s.G; ++g) {
                     mean_out[b * s.G + g] = 0.0f;
                     rstd_out[b * s.G + g] = 1.0f / sqrtf(eps);
-                }  // (no row asks for their part of `low`)
+                }  // (no row asks for their place in `exact`)
     for (int piece = 0; piece < (HOW == kPieces ? s.pieces : 1); ++piece) {
         const Slice<HOW> slice(s, piece);
         const Place<VEC> at(s, slice);
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict_
                     }
                     const int64_t p = b * s.G + slice.group + g;
                     mean_out[p] = float(mid);
-                    low[p] = rounding(mid);
+                    exact[p] = two_floats(mid);
                     rstd_out[p] = 1.0f / sqrtf(float(var < 0.0 ? 0.0 : var) + eps);
                 }
             }
@@ -491,7 +491,7 @@ __device__ __forceinline__ int64_t sample_of_pair(const Shape &s, int64_t p, int
 // the result act((x - o) w + b).
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const double2 *__restrict__ part, const Shape s, float eps, float *__restrict__ mean,
-                                                             float *__restrict__ rstd, float *__restrict__ low, const float *__restrict__ gamma,
+                                                             float *__restrict__ rstd, float2 *__restrict__ exact, const float *__restrict__ gamma,
                                                              const float *__restrict__ beta, float *__restrict__ table) {
     __shared__ double2 red[THREADS / 64];
     const int64_t tiles = (s.N + s.tile_rows - 1) / s.tile_rows;
@@ -524,14 +524,14 @@ __global__ void __launch_bounds__(THREADS) norm_stats_kernel(const double2 *__re
         if (threadIdx.x == 0) {
             mean[p] = float(mid);
             rstd[p] = r;
-            low[p] = rounding(mid);
+            exact[p] = two_floats(mid);
         }
         if (table)
             for (int k = int(threadIdx.x); k < s.group_width; k += THREADS) {
                 const float w = gamma ? r * gamma[c0 + k] : r;
                 table[c0 + k] = float(mid);
                 table[s.C + c0 + k] = w;
-                table[2 * int64_t(s.C) + c0 + k] = (beta ? beta[c0 + k] : 0.0f) - rounding(mid) * w;
+                table[2 * int64_t(s.C) + c0 + k] = (beta ? beta[c0 + k] : 0.0f) - two_floats(mid).y * w;
             }
     }
 }
@@ -653,7 +653,7 @@ template <typename T> __host__ __device__ constexpr int rows_of(bool backward) {
 template <typename T, int VEC, int ACT, bool NT, Stats STATS>
 __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X, int64_t ldx, const Shape s, const float *__restrict__ gamma,
                                                          const float *__restrict__ beta, float *__restrict__ mean, float *__restrict__ rstd,
-                                                         const float *__restrict__ low, T *__restrict__ Y, int64_t ldy, const double2 *__restrict__ part, float eps, const float *__restrict__ table) {
+                                                         const float2 *__restrict__ exact, T *__restrict__ Y, int64_t ldy, const double2 *__restrict__ part, float eps, const float *__restrict__ table) {
     constexpr int kRows = rows_of<T>(false);
     const int col = column_of_block<VEC>(s);
     const int64_t r0 = workgroup() * (kRows * s.row_lanes) + threadIdx.y;
@@ -687,7 +687,8 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
             },
             [&](int g, double2 u) {
                 const double off = u.x * inv, var = u.y * inv - off * off, mid = part[g * s.group_width].x + off;
-                const float4 r = make_float4(float(mid), 1.0f / sqrtf(float(var < 0.0 ? 0.0 : var) + eps), rounding(mid), 0.0f);
+                const float2 m = two_floats(mid);
+                const float4 r = make_float4(m.x, 1.0f / sqrtf(float(var < 0.0 ? 0.0 : var) + eps), m.y, 0.0f);
                 if (workgroup() == 0) {
                     mean[g] = r.x;
                     rstd[g] = r.y;
@@ -708,9 +709,14 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(const T *__restrict__ X
         if (r >= s.N) break;
         if constexpr (STATS == kMany) {
             const int64_t b = sample_of_row(s, r);
-            aff.gather(s, mean, b, o);
+            float2 m[VEC];
+            aff.gather(s, exact, b, m);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                o[j] = m[j].x;
+                l[j] = m[j].y;
+            }
             aff.gather(s, rstd, b, w);
-            aff.gather(s, low, b, l);
             fold();
         }
         float x[VEC];
@@ -1691,7 +1697,7 @@ __global__ void __launch_bounds__(kRowThreads) row_bwd_kernel(const T *__restric
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct Layout {
-    int64_t tile_rows, tiles, parts, map_off, open_off, total_off, sums_off, table_off, low_off, bytes;
+    int64_t tile_rows, tiles, parts, map_off, open_off, total_off, sums_off, table_off, exact_off, bytes;
     int threads;  // of a tile
     bool joined;  // one sample, few tiles: two launches
 };
@@ -1719,8 +1725,8 @@ Layout layout_of(int64_t N, int64_t C, int64_t G, int64_t B, bool backward) {
     if (B > 1 && C / G > kSlice) off += round_up(B * G * int64_t(sizeof(double2)), 256);
     L.table_off = off;
     if (B == 1) off += round_up(4 * C * 4, 256);
-    L.low_off = off;
-    L.bytes = off + round_up(B * G * 4, 256);
+    L.exact_off = off;
+    L.bytes = off + round_up(B * G * int64_t(sizeof(float2)), 256);
     if (backward) {
         L.total_off = off;
         if (B > 1) off += round_up(L.tiles * C * int64_t(sizeof(float2)), 256);
@@ -1812,7 +1818,7 @@ Shape shape_of(const Call &c, int vec, int rows, dim3 *grid, dim3 *block) {  // 
         *grid = spread((c.N + rows * s.row_lanes - 1) / (rows * s.row_lanes), unsigned(chunks), block->x);
     } else {
         s.row_lanes = c.L.threads / s.cols;
-        for (s.join = 1; 2 * s.join * s.cols * vec <= c.L.threads && 2 * s.join < s.row_lanes;) s.join *= 2;
+        for (s.join = 1; 2 * s.join * s.cols * vec <= c.L.threads && 16 * s.join <= s.row_lanes;) s.join *= 2;  // eight to one and more
         *block = dim3(unsigned(c.L.threads));
         *grid = dim3(unsigned(c.L.tiles), unsigned(chunks));
     }
@@ -1838,20 +1844,20 @@ template <typename T, int PART, int OUT, int ACT, bool NT> int run_tiles(const C
     // what join_tiles keeps: the sums of every row lane, and a sixteenth
     const size_t values = size_t(w.row_lanes) * size_t(c.C), join = (values + c.G * ((values / c.G + 15) / 16)) * (c.backward ? sizeof(float2) : sizeof(double2));
     if (!c.backward) {
-        float *low = reinterpret_cast<float *>(c.scratch(c.L.low_off));
+        float2 *exact = reinterpret_cast<float2 *>(c.scratch(c.L.exact_off));
         if (c.L.joined) {
-            norm_part_kernel<T, PART, false, kThreads, kOneSample><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd, low);
-            norm_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, low, out, c.o.ldy, moments, c.o.eps, nullptr);
+            norm_part_kernel<T, PART, false, kThreads, kOneSample><<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd, exact);
+            norm_apply_kernel<T, OUT, ACT, false, kJoin><<<out_grid, out_threads, join, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, exact, out, c.o.ldy, moments, c.o.eps, nullptr);
         } else {
             auto *sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, kManySamples> : norm_part_kernel<T, PART, NT, kLargeThreads, kManySamples>;
             if (c.B == 1) sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, kOneSample> : norm_part_kernel<T, PART, NT, kLargeThreads, kOneSample>;
             else if (s.pieces > 1) sum = c.L.threads == kThreads ? norm_part_kernel<T, PART, NT, kThreads, kPieces> : norm_part_kernel<T, PART, NT, kLargeThreads, kPieces>;
-            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd, low);
-            if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, c.gamma, c.beta, table);
-            else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, c.gamma, c.beta, table);
-            else norm_stats_kernel<64><<<many, 64, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, low, c.gamma, c.beta, table);
+            sum<<<grid, threads, lds, stream>>>(X, c.o.ldx, s, moments, c.o.eps, c.mean, c.rstd, exact);
+            if (pairs <= 512) norm_stats_kernel<1024><<<unsigned(pairs), 1024, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, exact, c.gamma, c.beta, table);
+            else if (pairs < 4096) norm_stats_kernel<256><<<unsigned(pairs), 256, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, exact, c.gamma, c.beta, table);
+            else norm_stats_kernel<64><<<many, 64, 0, stream>>>(moments, s, c.o.eps, c.mean, c.rstd, exact, c.gamma, c.beta, table);
             auto *apply = c.B == 1 ? norm_apply_kernel<T, OUT, ACT, NT, kOne> : norm_apply_kernel<T, OUT, ACT, NT, kMany>;
-            apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, low, out, c.o.ldy, nullptr, 0.0f, table);
+            apply<<<out_grid, out_threads, 0, stream>>>(X, c.o.ldx, w, c.gamma, c.beta, c.mean, c.rstd, exact, out, c.o.ldy, nullptr, 0.0f, table);
         }
     } else {
         float2 *sums = c.out ? reinterpret_cast<float2 *>(c.scratch(c.L.sums_off)) : nullptr;
