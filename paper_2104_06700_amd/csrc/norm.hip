@@ -18,7 +18,7 @@
 // rows are cut into tiles of equal size whatever the samples' sizes are, one workgroup each, which adds up each sample's part of
 // it per column.  A sample inside a tile is finished there; of one that crosses tiles, each leaves its partial sums in a slot of its own, and a second
 // kernel merges them in their order: results do not depend on timing.  A third reads the rows again and writes the result.  Both readers are bound by the
-// memory: 2.4 M x 256 fp32 in 32 groups forward 383 us (6.5 TB/s) and 773 (6.5), gradients 743 (6.8) and 1189 (6.3), merging 13.
+// memory: 2.4 M x 256 fp32 in 32 groups forward 385 us (6.5 TB/s) and 777 (6.5), gradients 743 (6.8) and 1190 (6.3), merging 12 to 14.
 #include "common.h"
 #include "rows.h"
 
@@ -344,8 +344,8 @@ __global__ void __launch_bounds__(THREADS) norm_part_kernel(const T *__restrict_
                     for (int j = 0; j < VEC; ++j) {
                         const float o = t1[j] * inv, q = t2[j] - t1[j] * o;
                         const float d = o - off[j];
-                    off[j] += d * share;
-                    m2[j] += (q < 0.0f ? 0.0f : q) + d * d * weight;
+                        off[j] += d * share;
+                        m2[j] += (q < 0.0f ? 0.0f : q) + d * d * weight;
                         const float next = base[j] + off[j];  // the next run's distances are from here
                         off[j] -= next - base[j];
                         base[j] = next;
