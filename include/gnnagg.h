@@ -497,6 +497,124 @@ typedef struct gnn_adamw_opts {
  * allocates nothing; one launch for up to 40 tensors. */
 GNN_API int gnn_adamw_step(const gnn_adamw_tensor *tensors /* host */, int64_t n_tensors, const gnn_adamw_opts *opts);
 
+/* ------------------------------------- rows by vertex id: tables, their gradients, rows kept in 8 bits */
+
+/* Rows of a table by id, as a mini-batch reads learned embeddings of its vertices.  table [V, F], ids [n] int32 or int64, Y [n, F]:
+ *     Y[i, :] = scale * table[ids[i], :]
+ * An id outside 0 .. V-1 (usually -1, padding) names no row: its row of Y is 0, whatever the table holds.  table and Y are fp32 or bf16, each by
+ * itself; the product is fp32 and rounded once.  Y does not overlap the table.  An id may come any number of times. */
+typedef struct gnn_lookup_opts {
+    int32_t table_dtype;   /* gnn_dtype of table or dtable */
+    int32_t dtype;         /* gnn_dtype of Y or dY */
+    int32_t ids_is_64;     /* 0: ids are int32_t;  1: int64_t */
+    int32_t accumulate;    /* the gradient only.  0: dtable is overwritten;  1: the sums are added to it */
+    float scale;           /* set it: 1 for the plain rows */
+    int32_t reserved;      /* 0 */
+    int64_t ldt, ldy;      /* row strides in elements of table or dtable, and of Y or dY; 0 = F */
+    void *stream;
+    void *workspace;       /* the gradient only: device scratch of gnn_lookup_workspace_bytes(), 16-byte aligned; nothing is kept in it */
+    int64_t workspace_bytes;
+} gnn_lookup_opts;
+/* Asynchronous on opts->stream; allocates nothing.  n == 0 or F == 0 does nothing; V == 0 writes zeros.  At most 2^31 - 1 rows and ids and
+ * 2^24 columns. */
+GNN_API int gnn_lookup_fwd(const void *table, const void *ids, void *Y, int64_t V, int64_t n, int64_t F, const gnn_lookup_opts *opts);
+/* The gradient of sum dY Y with respect to the table:
+ *     dtable[v, :] = scale * (sum of dY[i, :] over the i with ids[i] = v)   (+ dtable[v, :] with accumulate)
+ * Rows that no id names become 0, and with accumulate are left as they are, unread.  The ids are sorted, so that each row is summed by one owner
+ * in a fixed order: results are reproducible run to run.  At most 64 terms are added one after the other in fp32, and what these leave is
+ * joined in fp64; a bf16 dtable is rounded once, with accumulate once a call.  dY and dtable do not overlap.  n == 0 sets dtable to 0 without
+ * accumulate. */
+GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dtable, int64_t V, int64_t n, int64_t F, const gnn_lookup_opts *opts);
+GNN_API int64_t gnn_lookup_workspace_bytes(int64_t V, int64_t n, int64_t F);
+
+/* Rows kept in 8 bits: features of a graph, or hidden rows that later batches read, a quarter of their size in fp32.  A row of F columns
+ * is F codes, OCP e4m3 numbers, and behind them a byte for every GNN_STORE_BLOCK columns (the last ones may be fewer), an OCP e8m0 exponent:
+ *     value[c] = code[c] * 2^(exponent[c / GNN_STORE_BLOCK] - 127)
+ * The exponent is the least one, at least 0, with which the block's largest finite magnitude is at most 448: no value is cut off, and being a power of
+ * two it rounds nothing.  A value is off by at most 2^-4 of itself, or 2^-10 times 2^(exponent - 127) where that is more.  What is not finite is
+ * held as NaN, and leaves the block's other values alone.  (What rounds up to 2^128, from 1.9375 * 2^127 on, reads back as infinity.)
+ * store [V, ld] bytes; bytes of a row behind its exponents are neither read nor written. */
+#define GNN_STORE_BLOCK 32
+typedef struct gnn_store_opts {
+    int32_t dtype;         /* gnn_dtype of X or Y */
+    int32_t ids_is_64;     /* 0: ids are int32_t;  1: int64_t */
+    int32_t unique;        /* writing only.  1: the caller guarantees that no id comes twice, and no workspace is needed */
+    int32_t reserved;      /* 0 */
+    int64_t lds;           /* bytes from a row of the store to the next, at least F + ceil(F / GNN_STORE_BLOCK); 0 = gnn_store_row_bytes(F) */
+    int64_t ldx;           /* row stride in elements of X or Y; 0 = F */
+    void *stream;
+    void *workspace;       /* writing only: device scratch of gnn_store_rows_workspace_bytes(), 4-byte aligned; nothing is kept in it */
+    int64_t workspace_bytes;
+} gnn_store_opts;
+/* Row i of X [n, F] to row ids[i] of the store; ids NULL: to row i (n <= V).  A row whose id is outside 0 .. V-1 goes nowhere.  Of rows with the same id
+ * the last one stays; rows that no id names stay as they are.  X does not overlap the store. */
+GNN_API int gnn_store_rows(const void *X, const void *ids, void *store, int64_t V, int64_t n, int64_t F, const gnn_store_opts *opts);
+/* Row ids[i] of the store to row i of Y [n, F]; ids NULL: row i (n <= V).  An id outside 0 .. V-1 gives a row of zeros.  Exact in fp32 and in
+ * bf16 but for what lies beyond the type's ends.  Both calls are asynchronous on opts->stream and allocate nothing.  At most 2^31 - 1 rows and ids and 2^24 columns. */
+GNN_API int gnn_load_rows(const void *store, const void *ids, void *Y, int64_t V, int64_t n, int64_t F, const gnn_store_opts *opts);
+GNN_API int64_t gnn_store_row_bytes(int64_t F);  /* codes and exponents, up to a multiple of 16 */
+GNN_API int64_t gnn_store_rows_workspace_bytes(int64_t V, int64_t n);  /* 0 where n is small */
+
+/* ------------------------------------- orthogonalised updates of weight matrices */
+
+/* Newton-Schulz products: a matrix U [rows, cols] becomes one with the same singular vectors and singular values near 1.  With X = U /
+ * (|U| + eps), |U| the root of the sum of squares, transposed where rows > cols, `steps` times
+ *     A = X X^T,   B = b A + c A A,   X = a X + B X
+ * and O = X (transposed back).  (a, b, c) = (3.4445, -4.7750, 2.0315) takes singular values of X from some 0.002 on to 0.7 .. 1.2 in five steps.
+ * fp32 matrices: products of operands split into three bf16 numbers, as in gnn_matmul, fp32 sums: as close as fp32 products.  bf16 matrices:
+ * operands between the products are held in two bf16 numbers (16 significant bits), and O is rounded once.  A zero matrix gives 0; a value that is not
+ * finite makes all of its matrix' results NaN, and no other's. */
+typedef struct gnn_orthogonalize_matrix {
+    const void *in;        /* U [rows, cols] of dtype, row stride ld_in */
+    void *out;             /* O [rows, cols] of dtype, row stride ld_out; may be `in`, with the same stride */
+    int64_t rows, cols;    /* at most 65,536 each */
+    int64_t ld_in, ld_out; /* in elements; 0 = cols */
+    int32_t dtype;         /* gnn_dtype */
+    int32_t reserved;      /* 0 */
+} gnn_orthogonalize_matrix;
+typedef struct gnn_orthogonalize_opts {
+    double a, b, c;        /* finite */
+    double eps;            /* > 0 */
+    int32_t steps;         /* 1 .. 100 */
+    int32_t reserved;      /* 0 */
+    void *stream;
+    void *workspace;       /* device scratch of gnn_orthogonalize_workspace_bytes(), 256-byte aligned; nothing is kept in it */
+    int64_t workspace_bytes;
+} gnn_orthogonalize_opts;
+/* All matrices at once; `matrices` is a HOST array, read before the call returns.  Apart from out = in no buffer may overlap another.
+ * Asynchronous on opts->stream; allocates nothing; results are reproducible run to run.  A matrix without elements is left alone. */
+GNN_API int gnn_orthogonalize(const gnn_orthogonalize_matrix *matrices /* host */, int64_t n_matrices, const gnn_orthogonalize_opts *opts);
+GNN_API int64_t gnn_orthogonalize_workspace_bytes(const gnn_orthogonalize_matrix *matrices /* host */, int64_t n_matrices);
+
+/* One Muon step over many weight matrices at once, in place: momentum whose update is orthogonalised,
+ *     g = grad * grad_scale,   M = momentum M + g,   U = g + momentum M (nesterov) or M,
+ *     W = W (1 - lr weight_decay) - lr update_scale O,   O = U orthogonalised as above
+ * For matrices only: vectors, embeddings and the last layer are usually AdamW's.  M is fp32.  A gradient that is not finite makes its own matrix
+ * NaN, and no other. */
+typedef struct gnn_muon_matrix {
+    void *param;           /* W [rows, cols] of dtype, dense, updated */
+    const void *grad;      /* [rows, cols] of dtype, dense; NULL: the matrix is left alone, decay included */
+    float *momentum;       /* M [rows, cols], updated; zeros are a new state */
+    float *master;         /* bf16 parameters: [rows, cols] fp32, the parameters themselves, of which param becomes the rounded copy; or NULL */
+    int64_t rows, cols;    /* at most 65,536 each */
+    int32_t dtype;         /* gnn_dtype of param and grad; a bf16 parameter is rounded to nearest-even once */
+    float weight_decay;    /* >= 0 */
+    float update_scale;    /* of the orthogonal update; sqrt(max(1, cols / rows)) for a weight that is multiplied from the right (X W) */
+    int32_t reserved;      /* 0 */
+} gnn_muon_matrix;
+typedef struct gnn_muon_opts {
+    double lr, momentum;   /* lr >= 0; momentum in [0, 1) */
+    double a, b, c, eps;   /* as in gnn_orthogonalize_opts */
+    int32_t nesterov, steps;
+    const float *grad_scale; /* device: one factor for all gradients; NULL = 1 */
+    void *stream;
+    void *workspace;       /* device scratch of gnn_muon_workspace_bytes(), 256-byte aligned; nothing is kept in it */
+    int64_t workspace_bytes;
+} gnn_muon_opts;
+/* As gnn_orthogonalize.  No buffer may appear twice or overlap another. */
+GNN_API int gnn_muon_step(const gnn_muon_matrix *matrices /* host */, int64_t n_matrices, const gnn_muon_opts *opts);
+GNN_API int64_t gnn_muon_workspace_bytes(const gnn_muon_matrix *matrices /* host */, int64_t n_matrices);
+
 /* ------------------------------------------------------- once-per-graph setup */
 
 /* Row pointers of the destination-indexed CSR (Section 4.1 requires the graph

@@ -20,6 +20,9 @@ from .binding import (  # noqa: F401
     GNN_ACT_NONE, GNN_ACT_RELU, GNN_ACT_SILU, GNN_LOSS_SUM, GNN_LOSS_MEAN, GNN_ADAMW_BLOCK,
     GnnNormOpts, GnnLossOpts, GnnAdamWTensor, GnnAdamWOpts, AdamWTensors, gnn_group_norm_fwd, gnn_group_norm_bwd, gnn_group_norm_workspace_bytes,
     gnn_softmax_xent, gnn_softmax_xent_workspace_bytes, gnn_adamw_step,
+    GNN_STORE_BLOCK, GNN_NEWTON_SCHULZ, GnnLookupOpts, GnnStoreOpts, GnnOrthogonalizeMatrix, GnnOrthogonalizeOpts, GnnMuonMatrix, GnnMuonOpts,
+    gnn_lookup_fwd, gnn_lookup_bwd, gnn_lookup_workspace_bytes, gnn_store_rows, gnn_load_rows, gnn_store_row_bytes, gnn_store_rows_workspace_bytes,
+    OrthogonalizeTensors, MuonTensors, gnn_orthogonalize, gnn_orthogonalize_workspace_bytes, gnn_muon_step, gnn_muon_workspace_bytes,
     gnn_sage_layer_fwd, gnn_sage_layer_bwd, gnn_sage_layer_saved_elems, gnn_sage_layer_workspace_bytes,
 )
 from .graph import DeviceGraph, build_device_graph  # noqa: F401

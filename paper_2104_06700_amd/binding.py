@@ -38,6 +38,8 @@ GNN_RED_SUM, GNN_RED_MAX, GNN_RED_MIN = range(3)
 GNN_ACT_NONE, GNN_ACT_RELU, GNN_ACT_SILU = range(3)
 GNN_LOSS_SUM, GNN_LOSS_MEAN = range(2)
 GNN_ADAMW_BLOCK = 256
+GNN_STORE_BLOCK = 32
+GNN_NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)  # coefficients of five steps
 
 EXPORTED_SYMBOLS = (
     "gnn_aggregate_fwd", "gnn_aggregate_bwd", "gnn_aggregate_fwd_noalloc", "gnn_packed_bytes", "gnn_pack_rows",
@@ -52,6 +54,9 @@ EXPORTED_SYMBOLS = (
     "gnn_sage_layer_fwd", "gnn_sage_layer_bwd", "gnn_sage_layer_saved_elems", "gnn_sage_layer_workspace_bytes",
     "gnn_group_norm_fwd", "gnn_group_norm_bwd", "gnn_group_norm_workspace_bytes", "gnn_softmax_xent", "gnn_softmax_xent_workspace_bytes",
     "gnn_adamw_step",
+    "gnn_lookup_fwd", "gnn_lookup_bwd", "gnn_lookup_workspace_bytes",
+    "gnn_store_rows", "gnn_load_rows", "gnn_store_row_bytes", "gnn_store_rows_workspace_bytes",
+    "gnn_orthogonalize", "gnn_orthogonalize_workspace_bytes", "gnn_muon_step", "gnn_muon_workspace_bytes",
     "gnn_status_string", "gnn_calib_copy", "gnn_calib_gather",
 )
 
@@ -111,6 +116,54 @@ class GnnAdamWOpts(ctypes.Structure):
     _fields_ = [
         ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
         ("step", ctypes.c_int64), ("seed", ctypes.c_int64), ("grad_scale", ctypes.c_void_p), ("stream", ctypes.c_void_p),
+    ]
+
+
+class GnnLookupOpts(ctypes.Structure):
+    _fields_ = [
+        ("table_dtype", ctypes.c_int32), ("dtype", ctypes.c_int32), ("ids_is_64", ctypes.c_int32), ("accumulate", ctypes.c_int32),
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32), ("ldt", ctypes.c_int64), ("ldy", ctypes.c_int64),
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64),
+    ]
+
+
+class GnnStoreOpts(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("ids_is_64", ctypes.c_int32), ("unique", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("lds", ctypes.c_int64), ("ldx", ctypes.c_int64),
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64),
+    ]
+
+
+class GnnOrthogonalizeMatrix(ctypes.Structure):
+    _fields_ = [
+        ("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+        ("ld_in", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class GnnOrthogonalizeOpts(ctypes.Structure):
+    _fields_ = [
+        ("a", ctypes.c_double), ("b", ctypes.c_double), ("c", ctypes.c_double), ("eps", ctypes.c_double),
+        ("steps", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64),
+    ]
+
+
+class GnnMuonMatrix(ctypes.Structure):
+    _fields_ = [
+        ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("momentum", ctypes.c_void_p), ("master", ctypes.c_void_p),
+        ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("dtype", ctypes.c_int32), ("weight_decay", ctypes.c_float),
+        ("update_scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+    ]
+
+
+class GnnMuonOpts(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_double), ("momentum", ctypes.c_double),
+        ("a", ctypes.c_double), ("b", ctypes.c_double), ("c", ctypes.c_double), ("eps", ctypes.c_double),
+        ("nesterov", ctypes.c_int32), ("steps", ctypes.c_int32), ("grad_scale", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64),
     ]
 
 
@@ -205,6 +258,16 @@ def load_library() -> ctypes.CDLL:
         lib.gnn_softmax_xent_workspace_bytes.argtypes = [i64, i64]
         lib.gnn_softmax_xent_workspace_bytes.restype = i64
         lib.gnn_adamw_step.argtypes = [vp, i64, ctypes.POINTER(GnnAdamWOpts)]
+        lib.gnn_lookup_fwd.argtypes = [vp] * 3 + [i64] * 3 + [ctypes.POINTER(GnnLookupOpts)]
+        lib.gnn_lookup_bwd.argtypes = lib.gnn_lookup_fwd.argtypes
+        lib.gnn_store_rows.argtypes = [vp] * 3 + [i64] * 3 + [ctypes.POINTER(GnnStoreOpts)]
+        lib.gnn_load_rows.argtypes = lib.gnn_store_rows.argtypes
+        lib.gnn_orthogonalize.argtypes = [vp, i64, ctypes.POINTER(GnnOrthogonalizeOpts)]
+        lib.gnn_muon_step.argtypes = [vp, i64, ctypes.POINTER(GnnMuonOpts)]
+        for name, args in (("gnn_lookup_workspace_bytes", [i64] * 3), ("gnn_store_row_bytes", [i64]), ("gnn_store_rows_workspace_bytes", [i64] * 2),
+                           ("gnn_orthogonalize_workspace_bytes", [vp, i64]), ("gnn_muon_workspace_bytes", [vp, i64])):
+            getattr(lib, name).argtypes = args
+            getattr(lib, name).restype = i64
         lib.gnn_status_string.argtypes = [i32]
         lib.gnn_status_string.restype = ctypes.c_char_p
         lib.gnn_calib_copy.argtypes = [vp, vp, i64, vp]
@@ -222,7 +285,8 @@ def _connect_calls():
         raise ImportError("the extension module _pycall is missing: run `python -c 'import __graft_entry__ as g; g.build()'`") from err
     names = ("gnn_aggregate_fwd", "gnn_aggregate_bwd", "gnn_ap_fwd", "gnn_ap_bwd_vertex", "gnn_ap_bwd_vertex_arg_edges",
              "gnn_ap_bwd_edge", "gnn_sage_layer_fwd", "gnn_sage_layer_bwd", "gnn_group_norm_fwd", "gnn_group_norm_bwd",
-             "gnn_softmax_xent", "gnn_adamw_step")
+             "gnn_softmax_xent", "gnn_adamw_step", "gnn_lookup_fwd", "gnn_lookup_bwd", "gnn_store_rows", "gnn_load_rows",
+             "gnn_orthogonalize", "gnn_muon_step")
     _pycall.connect({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names}, torch)
     _calls = _pycall
     return _pycall
@@ -658,6 +722,151 @@ def gnn_adamw_step(tensors: AdamWTensors, step, lr, beta1=0.9, beta2=0.999, eps=
     """One AdamW step over all tensors, in place; `step` is 1 in the first one (see include/gnnagg.h).  grad_scale: a float32
     device tensor of one value that multiplies every gradient."""
     _hot("gnn_adamw_step", "adamw_step", tensors.address, tensors.count, step, lr, beta1, beta2, eps, grad_scale, seed, stream)
+
+
+def gnn_lookup_workspace_bytes(V, n, F) -> int:
+    return int(load_library().gnn_lookup_workspace_bytes(int(V), int(n), int(F)))
+
+
+def gnn_lookup_fwd(table, ids, Y, scale=1.0, stream=None) -> None:
+    """Y[i] = scale * table[ids[i]]; an id outside the table gives a row of zeros (see include/gnnagg.h).  table and Y are float32 or
+    bfloat16, each by itself; ids int32 or int64."""
+    _hot("gnn_lookup_fwd", "lookup_fwd", table, ids, Y, scale, stream)
+
+
+def gnn_lookup_bwd(ids, dY, dtable, scale=1.0, accumulate=False, workspace=None, stream=None) -> None:
+    """dtable[v] = scale * the sum of dY[i] over the i with ids[i] = v, zeros where there is none; with accumulate the sums are added to
+    dtable (see include/gnnagg.h)."""
+    _hot("gnn_lookup_bwd", "lookup_bwd", ids, dY, dtable, scale, accumulate, workspace, stream)
+
+
+def gnn_store_row_bytes(F) -> int:
+    """Bytes of a row of F columns in a store of 8-bit rows, a multiple of 16; rows of any other length that holds them do too."""
+    return int(load_library().gnn_store_row_bytes(int(F)))
+
+
+def gnn_store_rows_workspace_bytes(V, n) -> int:
+    return int(load_library().gnn_store_rows_workspace_bytes(int(V), int(n)))
+
+
+def gnn_store_rows(X, store, ids=None, unique=False, workspace=None, stream=None) -> None:
+    """Row i of X [n, F] to row ids[i] (None: row i) of `store`, a uint8 matrix of rows in 8 bits (see include/gnnagg.h).  Of rows with the same id
+    the last one stays; unique: the caller guarantees that there are none."""
+    _hot("gnn_store_rows", "store_rows", X, store, ids, unique, workspace, stream)
+
+
+def gnn_load_rows(store, Y, ids=None, stream=None) -> None:
+    """Row ids[i] (None: row i) of `store` to row i of Y [n, F]; an id outside the store gives a row of zeros (see include/gnnagg.h)."""
+    _hot("gnn_load_rows", "load_rows", store, Y, ids, stream)
+
+
+def _matrix_of(t, what):
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what}: two-dimensional device tensors expected")
+    if t.numel() > 0 and (t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{what}: unit column stride and rows that do not overlap expected")
+    return t.stride(0) if t.shape[0] > 1 and t.numel() > 0 else 0
+
+
+class OrthogonalizeTensors:
+    """The matrices that gnn_orthogonalize takes, and where it writes: lists of two-dimensional device tensors, float32 or bfloat16, an output of
+    the shape and type of its input.  An output may be its input."""
+
+    def __init__(self, inputs, outputs):
+        inputs, outputs = list(inputs), list(outputs)
+        if len(inputs) != len(outputs):
+            raise ValueError("one output a matrix expected")
+        self._tensors = (inputs, outputs)  # what the descriptors point to stays alive
+        self.count = len(inputs)
+        self._array = (GnnOrthogonalizeMatrix * max(self.count, 1))()
+        for d, u, o in zip(self._array, inputs, outputs):
+            d.ld_in, d.ld_out, d.dtype = _matrix_of(u, "input"), _matrix_of(o, "output"), _dtype_code(u)
+            if o.dtype != u.dtype:
+                raise TypeError("an output must have its input's dtype")
+            if o.shape != u.shape:
+                raise ValueError("an output must have its input's shape")
+            d.in_, d.out, d.rows, d.cols = u.data_ptr(), o.data_ptr(), u.shape[0], u.shape[1]
+        self.address = ctypes.addressof(self._array)
+
+
+def gnn_orthogonalize_workspace_bytes(tensors: OrthogonalizeTensors) -> int:
+    return int(load_library().gnn_orthogonalize_workspace_bytes(tensors.address, tensors.count))
+
+
+def gnn_orthogonalize(tensors: OrthogonalizeTensors, steps=5, eps=1e-7, coefficients=GNN_NEWTON_SCHULZ, workspace=None, stream=None) -> None:
+    """Every matrix with its singular values brought near 1 by `steps` of Newton-Schulz products (see include/gnnagg.h)."""
+    _hot("gnn_orthogonalize", "orthogonalize", tensors.address, tensors.count, steps, eps, coefficients, workspace, stream)
+
+
+class MuonTensors:
+    """The weight matrices of a model as gnn_muon_step takes them: the descriptors, made once, and the tensors that they point to.
+
+    params, grads, momentum: lists of contiguous two-dimensional device tensors of the same shapes; a gradient may be None (the matrix is left
+    alone).  Parameters and gradients are float32 or bfloat16, the momentum float32.  master: float32 copies of bfloat16 parameters, or None.
+    weight_decay: one number, or one for each matrix.  update_scale: the same, of the orthogonal update; None: sqrt(max(1, cols / rows)).
+
+    A step reads the tensors that are given here (or to set_grads), as with AdamWTensors."""
+
+    def __init__(self, params, grads, momentum, master=None, weight_decay=0.0, update_scale=None):
+        count = len(params)
+        lists = [list(t) if t is not None else [None] * count for t in (params, grads, momentum, master)]
+        decay = [float(weight_decay)] * count if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        if update_scale is None:
+            scale = [max(1.0, p.shape[1] / max(1, p.shape[0])) ** 0.5 if p.dim() == 2 else 1.0 for p in lists[0]]
+        else:
+            scale = [float(update_scale)] * count if isinstance(update_scale, (int, float)) else [float(s) for s in update_scale]
+        if any(len(t) != count for t in lists + [decay, scale]):
+            raise ValueError("one entry a matrix expected in every list")
+        self._tensors = lists  # what the descriptors point to stays alive
+        self.count = count
+        self._array = (GnnMuonMatrix * max(count, 1))()
+        for d, w, s, (p, _, m, master_p) in zip(self._array, decay, scale, zip(*lists)):
+            for t in (p, m, master_p):
+                if t is not None and not (t.is_contiguous() and t.is_cuda):
+                    raise ValueError("contiguous device tensors expected")
+            if p.dim() != 2:
+                raise ValueError("two-dimensional parameters expected")
+            if any(t is not None and t.dtype != torch.float32 for t in (m, master_p)):
+                raise TypeError("the momentum and master copies are float32")
+            if any(t is not None and t.shape != p.shape for t in (m, master_p)):
+                raise ValueError("the momentum and a master copy have their parameter's shape")
+            if master_p is not None and p.dtype != torch.bfloat16:
+                raise TypeError("a master copy belongs to bfloat16 parameters")
+            d.param, d.momentum = p.data_ptr(), m.data_ptr()
+            d.master = master_p.data_ptr() if master_p is not None else None
+            d.rows, d.cols, d.dtype, d.weight_decay, d.update_scale = p.shape[0], p.shape[1], _dtype_code(p), w, s
+        self.set_grads(lists[1])
+        self.address = ctypes.addressof(self._array)
+
+    def set_grads(self, grads) -> None:
+        """The gradients of the steps from now on, one a matrix; None leaves that matrix alone."""
+        grads = list(grads)
+        if len(grads) != self.count:
+            raise ValueError("one entry a matrix expected in every list")
+        for p, g in zip(self._tensors[0], grads):
+            if g is None:
+                continue
+            if not (g.is_contiguous() and g.is_cuda):
+                raise ValueError("contiguous device tensors expected")
+            if g.dtype != p.dtype:
+                raise TypeError("a gradient must have its parameter's dtype")
+            if g.shape != p.shape:
+                raise ValueError("a gradient must have its parameter's shape")
+        self._tensors[1] = grads
+        for d, g in zip(self._array, grads):
+            d.grad = g.data_ptr() if g is not None else None
+
+
+def gnn_muon_workspace_bytes(tensors: MuonTensors) -> int:
+    """Of the matrices that have a gradient now; with all of them, enough for any."""
+    return int(load_library().gnn_muon_workspace_bytes(tensors.address, tensors.count))
+
+
+def gnn_muon_step(tensors: MuonTensors, lr, momentum=0.95, nesterov=True, steps=5, eps=1e-7, coefficients=GNN_NEWTON_SCHULZ, grad_scale=None,
+                  workspace=None, stream=None) -> None:
+    """One Muon step over all matrices, in place (see include/gnnagg.h).  grad_scale: a float32 device tensor of one value that multiplies
+    every gradient."""
+    _hot("gnn_muon_step", "muon_step", tensors.address, tensors.count, lr, momentum, nesterov, steps, eps, coefficients, grad_scale, workspace, stream)
 
 
 def gnn_csr_from_sorted_coo(dst_sorted: torch.Tensor, N: int, indptr_out: torch.Tensor, stream=None) -> None:

@@ -400,6 +400,13 @@ int gnn_radix_sort_pairs(uint32_t *buf_k[2], uint32_t *buf_v[2], int64_t n, int 
     *out = (bits + 7) / 8 % 2;
     return radix_sort(job, n, bits, table, sums, stream, nullptr, nullptr);
 }
+int gnn_radix_sort_positions(uint32_t *buf_k[2], uint32_t *buf_v[2], int64_t n, int bits, uint32_t *table, uint32_t *sums,
+                             hipStream_t stream, uint32_t **keys, uint32_t **positions) {
+    SortJob job;
+    job.first_keys = buf_k[0];
+    for (int i = 0; i < 2; ++i) { job.buf_k[i] = buf_k[i]; job.buf_v[i] = buf_v[i]; }
+    return radix_sort(job, n, bits, table, sums, stream, keys, positions);
+}
 int64_t gnn_sort_table_elems(int64_t n) { return (n + kSortTile - 1) / kSortTile * 256; }
 int64_t gnn_sort_sums_elems(int64_t n) { return gnn_scan_sums_elems(gnn_sort_table_elems(n)); }
 int64_t gnn_scan_sums_elems(int64_t n) { return (n + kScanChunk - 1) / kScanChunk + 1; }

@@ -1,0 +1,526 @@
+// Rows of a table by id, and the gradient of the table.
+//
+//     Y[i] = scale T[id_i]          dT[v] = scale sum of dY[i] over the i with id_i = v   (+ dT[v])
+//
+// Forward: a copy of rows.  A workgroup has some whole rows, their vectors side by side over its threads, four ids and four vectors of 16 bytes
+// of a thread on their way at once, and ends with them.
+//
+// Gradient: the positions are sorted by id (stable, so that rows of equal ids keep their order), and the sorted list is cut into runs of
+// kRun positions, whatever the ids: a group of lanes adds up its run's rows in registers and lets go of the sum where the id changes.  So every group
+// does the same work, with eight rows on their way, whether an id comes once or a million times.  A sum whose positions all lie in one run is
+// written by it; what crosses runs is joined in LDS, and what crosses workgroups by a second kernel, in fp64, in the order of the runs.  Rows
+// that no id names are zeroed by further workgroups of the same launch, which look their ids up in the sorted list.
+#include "common.h"
+#include "rows.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kAtOnce = 4;        // vectors of a thread on their way, forward
+constexpr int kRun = 32;          // sorted positions of a group of lanes: terms added one after the other in fp32
+constexpr int kBatch = 8;         // of them on their way at once
+constexpr int kZeroRows = 256;    // rows of a workgroup that zeroes
+constexpr int64_t kMostRows = INT32_MAX, kMostColumns = 1 << 24;
+constexpr unsigned kGridX = 1 << 20;  // workgroups in x: a launch has fewer than 2^32 threads a dimension
+
+// E neighbouring elements in fp32
+template <typename T, int E> struct Vector {
+    static constexpr int W = E < gnn_rows<T>::VEC ? E : gnn_rows<T>::VEC;
+    static_assert(E % W == 0, "whole strips");
+    gnn_strip<T, W, false> s[E / W];
+    __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+        for (int k = 0; k < E / W; ++k) s[k].load(p + k * W);
+    }
+    __device__ __forceinline__ void get(float (&v)[E]) const {
+#pragma unroll
+        for (int k = 0; k < E / W; ++k) {
+            float t[W];
+            s[k].get(t);
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[k * W + j] = t[j];
+        }
+    }
+};
+template <typename T, int E, bool NT> __device__ __forceinline__ void store_vector(T *p, const float (&v)[E]) {
+    constexpr int W = Vector<T, E>::W;
+#pragma unroll
+    for (int k = 0; k < E / W; ++k) {
+        float t[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) t[j] = v[k * W + j];
+        gnn_store_row<T, W, NT>(p + k * W, t);
+    }
+}
+
+struct Ids {
+    const void *p;
+    int is_64;
+    int64_t rows;
+    // the row that position i names, or -1
+    __device__ __forceinline__ int64_t at(int64_t i) const {
+        const int64_t v = is_64 ? static_cast<const int64_t *>(p)[i] : int64_t(static_cast<const int32_t *>(p)[i]);
+        return uint64_t(v) < uint64_t(rows) ? v : -1;
+    }
+};
+
+struct Lookup {
+    const void *table;
+    void *y;
+    Ids ids;
+    int64_t n, ldt, ldy;
+    int32_t f, vectors, rows;   // columns; vectors of a row; rows of a workgroup
+    uint32_t reciprocal;        // ceil(2^32 / vectors): quotients of numbers below 2^16
+    float scale;
+};
+
+__device__ __forceinline__ int64_t block_number() { return int64_t(blockIdx.z) * kGridX + blockIdx.x; }
+
+template <typename TT, typename TY, int E> __global__ void __launch_bounds__(kThreads) lookup_kernel(const Lookup a) {
+    const int64_t row0 = block_number() * a.rows;
+    if (row0 >= a.n) return;
+    const int rows = a.n - row0 < a.rows ? int(a.n - row0) : a.rows;
+    const int items = rows * a.vectors;
+    const TT *table = static_cast<const TT *>(a.table);
+    TY *y = static_cast<TY *>(a.y) + row0 * a.ldy;
+    for (int t0 = int(threadIdx.x); t0 < items; t0 += kThreads * kAtOnce) {
+        Vector<TT, E> v[kAtOnce];
+        int64_t id[kAtOnce];
+        int row[kAtOnce], col[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int t = t0 + u * kThreads;
+            id[u] = -1;
+            row[u] = a.vectors == 1 ? t : a.rows > 1 ? int(__umulhi(uint32_t(t), a.reciprocal)) : 0;
+            const int c = (t - row[u] * a.vectors) * E;
+            col[u] = c < a.f - E ? c : a.f - E;  // the last vector ends with the row
+            if (t < items) id[u] = a.ids.at(row0 + row[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (id[u] >= 0) v[u].load(table + id[u] * a.ldt + col[u]);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            if (t0 + u * kThreads >= items) continue;
+            float x[E];
+            if (id[u] >= 0) {
+                v[u].get(x);
+#pragma unroll
+                for (int j = 0; j < E; ++j) x[j] *= a.scale;
+            } else {
+#pragma unroll
+                for (int j = 0; j < E; ++j) x[j] = 0.0f;
+            }
+            store_vector<TY, E, true>(y + int64_t(row[u]) * a.ldy + col[u], x);
+        }
+    }
+}
+
+// ---- gradient
+
+struct Grad {
+    const void *dy;
+    void *dtable;
+    const uint32_t *key, *order;  // [n] ids sorted, `rows` where there is none; the positions they come from
+    float *head, *tail;           // [blocks][f] what a workgroup has of the sum that began before it, and of the one that goes on behind it
+    uint32_t *flags;              // [blocks]
+    int64_t rows, n, ldt, ldy, sum_blocks, zero_blocks;
+    int32_t f, vectors, lanes_log2;
+    int32_t accumulate;
+    float scale;
+};
+enum : uint32_t { kHead = 1, kThrough = 2, kTail = 4 };  // a run has: the end of a sum that began before, nothing but the middle of one, the beginning of one that goes on
+
+__global__ void __launch_bounds__(kThreads) key_kernel(const Ids ids, int64_t n, uint32_t *__restrict__ key) {
+    const int64_t i = block_number() * kThreads + threadIdx.x;
+    if (i >= n) return;
+    const int64_t v = ids.at(i);
+    key[i] = uint32_t(v < 0 ? ids.rows : v);
+}
+
+// first position of key[0 .. n) that is not below v
+__device__ __forceinline__ int64_t first_not_below(const uint32_t *key, int64_t lo, int64_t hi, uint32_t v) {
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (key[mid] < v) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// sum * scale into row v (or onto it), columns c .. c + E; `own`: how many of them, the last ones, are no other lane's
+template <typename TT, int E> __device__ __forceinline__ void write_sum(const Grad &a, int64_t v, int c, int own, const float (&sum)[E]) {
+    TT *p = static_cast<TT *>(a.dtable) + v * a.ldt + c;
+    float x[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) x[j] = sum[j] * a.scale;
+    if (!a.accumulate) {
+        store_vector<TT, E, false>(p, x);
+    } else if (own == E) {
+        Vector<TT, E> old;
+        old.load(p);
+        float o[E];
+        old.get(o);
+#pragma unroll
+        for (int j = 0; j < E; ++j) x[j] += o[j];
+        store_vector<TT, E, false>(p, x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            if (j >= E - own) gnn_rows<TT>::set(p + j, gnn_rows<TT>::get(p + j) + x[j]);
+    }
+}
+
+// rows [256 b, 256 b + 256) that no id names
+template <typename TT, int E> __device__ __forceinline__ void zero_rows(const Grad &a, int64_t b) {
+    static_assert(kZeroRows == kThreads, "a thread a row");
+    __shared__ uint8_t named[kZeroRows];
+    __shared__ int64_t range[2];
+    const int64_t v0 = b * kZeroRows;
+    const int rows = a.rows - v0 < kZeroRows ? int(a.rows - v0) : kZeroRows;
+    named[threadIdx.x] = 0;
+    if (threadIdx.x < 2) range[threadIdx.x] = first_not_below(a.key, 0, a.n, uint32_t(v0 + (threadIdx.x ? rows : 0)));
+    __syncthreads();
+    const int64_t lo = range[0], hi = range[1];
+    if (hi - lo <= 16 * kZeroRows) {
+        for (int64_t j = lo + threadIdx.x; j < hi; j += kThreads) named[a.key[j] - uint32_t(v0)] = 1;
+    } else if (int(threadIdx.x) < rows) {  // ids that come very often: one by one
+        const uint32_t v = uint32_t(v0 + threadIdx.x);
+        const int64_t j = first_not_below(a.key, lo, hi, v);
+        named[threadIdx.x] = j < hi && a.key[j] == v;
+    }
+    __syncthreads();
+    TT *p = static_cast<TT *>(a.dtable) + v0 * a.ldt;
+    const float zero[E] = {};
+    const int lanes = 1 << a.lanes_log2;
+    for (int r = int(threadIdx.x) >> a.lanes_log2; r < rows; r += kThreads >> a.lanes_log2) {
+        if (named[r]) continue;
+        for (int q = int(threadIdx.x) & (lanes - 1); q < a.vectors; q += lanes) {
+            const int c = q * E < a.f - E ? q * E : a.f - E;
+            store_vector<TT, E, true>(p + r * a.ldt + c, zero);
+        }
+    }
+}
+
+template <typename TY, typename TT, int E> __global__ void __launch_bounds__(kThreads) grad_kernel(const Grad a) {
+    const int64_t block = block_number();
+    if (block >= a.sum_blocks) {
+        if (block < a.sum_blocks + a.zero_blocks && blockIdx.y == 0) zero_rows<TT, E>(a, block - a.sum_blocks);
+        return;
+    }
+    __shared__ float parts[2][kThreads][E];  // what a group has of the sums that cross its ends
+    __shared__ uint32_t flags[kThreads];
+    const int lanes = 1 << a.lanes_log2, lane = int(threadIdx.x) & (lanes - 1), group = int(threadIdx.x) >> a.lanes_log2, groups = kThreads >> a.lanes_log2;
+    const int q = int(blockIdx.y) * lanes + lane;
+    const bool mine = q < a.vectors;
+    const int c = !mine ? 0 : q * E < a.f - E ? q * E : a.f - E;
+    const int own = q * E < a.f - E ? E : a.f - q * E;
+    const uint32_t none = uint32_t(a.rows);
+    const int64_t j0 = (block * groups + group) * kRun;
+    const TY *dy = static_cast<const TY *>(a.dy) + c;
+
+    float sum[E];
+    uint32_t my_flags = 0, id = none;
+    bool first = false;  // the sum began before this run
+    if (j0 < a.n) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum[j] = 0.0f;
+        id = a.key[j0];
+        first = j0 > 0 && id != none && a.key[j0 - 1] == id;
+        if (first) my_flags = kHead;
+        const int64_t end = j0 + kRun < a.n ? j0 + kRun : a.n;
+#pragma unroll 1
+        for (int64_t j = j0; j < end; j += kBatch) {
+            uint32_t k[kBatch];
+            Vector<TY, E> v[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                k[u] = j + u < end ? a.key[j + u] : none;
+                if (k[u] != none && mine) v[u].load(dy + int64_t(a.order[j + u]) * a.ldy);
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                if (k[u] != id) {
+                    if (j + u >= end) break;
+                    if (first) {
+#pragma unroll
+                        for (int i = 0; i < E; ++i) parts[0][threadIdx.x][i] = sum[i];
+                    } else if (id != none && mine) {
+                        write_sum<TT, E>(a, id, c, own, sum);
+                    }
+                    first = false;
+                    id = k[u];
+#pragma unroll
+                    for (int i = 0; i < E; ++i) sum[i] = 0.0f;
+                }
+                if (k[u] != none && mine) {
+                    float x[E];
+                    v[u].get(x);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) sum[i] += x[i];
+                }
+            }
+        }
+        const bool goes_on = id != none && end < a.n && a.key[end] == id;
+        if (first) {
+            if (goes_on) my_flags |= kThrough;
+#pragma unroll
+            for (int i = 0; i < E; ++i) parts[0][threadIdx.x][i] = sum[i];
+        } else if (goes_on) {
+            my_flags |= kTail;
+#pragma unroll
+            for (int i = 0; i < E; ++i) parts[1][threadIdx.x][i] = sum[i];
+        } else if (id != none && mine) {
+            write_sum<TT, E>(a, id, c, own, sum);
+        }
+    }
+    flags[group] = my_flags;  // (all lanes of the group the same)
+    __syncthreads();
+    // sums that cross runs: the run where one begins adds up the rest, as far as the workgroup goes
+    if (my_flags & kTail) {
+        double total[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) total[i] = double(sum[i]);
+        int g = group + 1;
+        for (; g < groups; ++g) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) total[i] += double(parts[0][(g << a.lanes_log2) + lane][i]);
+            if (!(flags[g] & kThrough)) break;
+        }
+        float x[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = float(total[i]);
+        if (g < groups) {
+            if (mine) write_sum<TT, E>(a, id, c, own, x);
+        } else {
+            if (mine) store_vector<float, E, false>(a.tail + block * a.f + c, x);
+        }
+    }
+    // what began before this workgroup
+    if (group == 0 && (my_flags & kHead)) {
+        double total[E] = {};
+        int g = 0;
+        for (; g < groups; ++g) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) total[i] += double(parts[0][(g << a.lanes_log2) + lane][i]);
+            if (!(flags[g] & kThrough)) break;
+        }
+        float x[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = float(total[i]);
+        if (mine) store_vector<float, E, false>(a.head + block * a.f + c, x);
+    }
+    if (threadIdx.x == 0 && blockIdx.y == 0) {
+        uint32_t all = flags[0] & kHead;
+        int g = groups - 1;
+        while (g >= 0 && (flags[g] & kThrough)) --g;
+        if (g < 0) all |= kThrough;
+        else if (flags[g] & kTail) all |= kTail;
+        a.flags[block] = all;
+    }
+}
+
+// The sums that cross workgroups: workgroup b joins the one that begins in runs of workgroup b.
+template <typename TT, int E> __global__ void __launch_bounds__(kThreads) join_kernel(const Grad a) {
+    const int64_t block = block_number();
+    if (block >= a.sum_blocks || !(a.flags[block] & kTail)) return;
+    __shared__ double parts[kThreads][E];
+    __shared__ int last;
+    const int lanes = 1 << a.lanes_log2, lane = int(threadIdx.x) & (lanes - 1), group = int(threadIdx.x) >> a.lanes_log2, groups = kThreads >> a.lanes_log2;
+    const int64_t chunk = int64_t(groups) * kRun;
+    // how many workgroups behind it have parts: up to the first that has more than the middle
+    int64_t more = 1;
+    if (a.flags[block + 1] & kThrough) {
+        for (;; more += kThreads) {
+            if (threadIdx.x == 0) last = kThreads;
+            __syncthreads();
+            const int64_t b = block + 1 + more + threadIdx.x;
+            if (b >= a.sum_blocks || !(a.flags[b] & kThrough)) atomicMin(&last, int(threadIdx.x));
+            __syncthreads();
+            const int found = last;
+            __syncthreads();
+            if (found < kThreads) {
+                more += found + 1;
+                break;
+            }
+        }
+    }
+    const int q = int(blockIdx.y) * lanes + lane;
+    const bool mine = q < a.vectors;
+    const int c = !mine ? 0 : q * E < a.f - E ? q * E : a.f - E;
+    const int own = q * E < a.f - E ? E : a.f - q * E;
+    double total[E] = {};
+    if (mine) {
+        for (int64_t k = group; k < more; k += groups) {
+            Vector<float, E> v;
+            v.load(a.head + (block + 1 + k) * a.f + c);
+            float x[E];
+            v.get(x);
+#pragma unroll
+            for (int i = 0; i < E; ++i) total[i] += double(x[i]);
+        }
+    }
+    if (more > 1) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) parts[threadIdx.x][i] = total[i];
+        __syncthreads();
+    }
+    if (group > 0 || !mine) return;
+    if (more > 1) {
+        const int64_t have = more < groups ? more : groups;
+        for (int g = 1; g < have; ++g)
+#pragma unroll
+            for (int i = 0; i < E; ++i) total[i] += parts[(g << a.lanes_log2) + lane][i];
+    }
+    Vector<float, E> v;
+    v.load(a.tail + block * a.f + c);
+    float x[E];
+    v.get(x);
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = float(total[i] + double(x[i]));
+    // (the last position of a workgroup with others behind it is there)
+    write_sum<TT, E>(a, a.key[(block + 1) * chunk - 1], c, own, x);
+}
+
+dim3 grid_of(int64_t blocks, int64_t slices = 1) {
+    return blocks <= kGridX ? dim3(unsigned(blocks), unsigned(slices)) : dim3(kGridX, unsigned(slices), unsigned((blocks + kGridX - 1) / kGridX));
+}
+
+bool known(int32_t dtype) { return dtype == GNN_F32 || dtype == GNN_BF16; }
+int64_t size_of(int32_t dtype) { return dtype == GNN_F32 ? 4 : 2; }
+bool misaligned(const void *p, int64_t to) { return reinterpret_cast<uintptr_t>(p) % uintptr_t(to) != 0; }
+
+// Elements of a vector: 16 bytes of the narrower type of a lookup, of dY's type in the gradient; one of rows narrower than that.
+int elements_of(bool eight, int64_t f) { return f >= (eight ? 8 : 4) ? (eight ? 8 : 4) : 1; }
+
+struct Room {  // of the gradient, in words
+    int lanes_log2;
+    int64_t vectors, chunk, blocks, table, sums, words;
+};
+Room room_of(int64_t V, int64_t n, int64_t F, bool eight) {
+    Room r;
+    const int e = elements_of(eight, F);
+    r.vectors = (F + e - 1) / e;
+    r.lanes_log2 = r.vectors >= 64 ? 6 : gnn_ilog2_ceil(r.vectors);
+    r.chunk = int64_t(kThreads >> r.lanes_log2) * kRun;
+    r.blocks = (n + r.chunk - 1) / r.chunk;
+    r.table = gnn_sort_table_elems(n);
+    r.sums = gnn_sort_sums_elems(n);
+    r.words = 4 * n + r.table + r.sums + r.blocks * (2 * F + 1);
+    return r;
+}
+
+int check(const void *table, const void *ids, const void *y, int64_t V, int64_t n, int64_t F, const gnn_lookup_opts &o) {
+    if (V < 0 || n < 0 || F < 0 || V > kMostRows || n > kMostRows || F > kMostColumns || !known(o.table_dtype) || !known(o.dtype)) return GNN_ERR_INVALID_ARG;
+    if ((o.ids_is_64 & ~1) || (o.accumulate & ~1) || (o.ldt && o.ldt < F) || (o.ldy && o.ldy < F)) return GNN_ERR_INVALID_ARG;
+    if (F == 0) return GNN_OK;
+    if ((V > 0 && !table) || (n > 0 && (!ids || !y)) || (V > 0 && n > 0 && table == y)) return GNN_ERR_INVALID_ARG;
+    if (misaligned(table, size_of(o.table_dtype)) || misaligned(y, size_of(o.dtype)) || misaligned(ids, o.ids_is_64 ? 8 : 4)) return GNN_ERR_INVALID_ARG;
+    return GNN_OK;
+}
+
+template <typename TT, typename TY, int E> void launch_lookup(const Lookup &a, hipStream_t stream) {
+    lookup_kernel<TT, TY, E><<<grid_of((a.n + a.rows - 1) / a.rows), kThreads, 0, stream>>>(a);
+}
+template <typename TT, typename TY> void lookup(Lookup &a, hipStream_t stream) {
+    constexpr bool eight = sizeof(TT) == 2 || sizeof(TY) == 2;
+    const int e = elements_of(eight, a.f);
+    a.vectors = (a.f + e - 1) / e;
+    a.rows = a.vectors >= kThreads * kAtOnce ? 1 : kThreads * kAtOnce / a.vectors;
+    a.reciprocal = a.vectors > 1 ? uint32_t(((uint64_t(1) << 32) + uint64_t(a.vectors) - 1) / uint64_t(a.vectors)) : 0;
+    if (e == 1) launch_lookup<TT, TY, 1>(a, stream);
+    else launch_lookup<TT, TY, eight ? 8 : 4>(a, stream);
+}
+
+template <typename TY, typename TT, int E> int launch_grad(const Grad &a, int64_t slices, hipStream_t stream) {
+    if (a.sum_blocks + a.zero_blocks == 0) return GNN_OK;
+    grad_kernel<TY, TT, E><<<grid_of(a.sum_blocks + a.zero_blocks, slices), kThreads, 0, stream>>>(a);
+    GNN_HIP_TRY(hipGetLastError());
+    if (a.sum_blocks > 1) {
+        join_kernel<TT, E><<<grid_of(a.sum_blocks, slices), kThreads, 0, stream>>>(a);
+        GNN_HIP_TRY(hipGetLastError());
+    }
+    return GNN_OK;
+}
+template <typename TY, typename TT> int grad(const Grad &a, int64_t slices, hipStream_t stream) {
+    constexpr int E = gnn_rows<TY>::VEC;
+    return a.f < E ? launch_grad<TY, TT, 1>(a, slices, stream) : launch_grad<TY, TT, E>(a, slices, stream);
+}
+
+}  // namespace
+
+extern "C" GNN_API int gnn_lookup_fwd(const void *table, const void *ids, void *Y, int64_t V, int64_t n, int64_t F, const gnn_lookup_opts *opts) {
+    if (!opts) return GNN_ERR_INVALID_ARG;
+    const gnn_lookup_opts &o = *opts;
+    const int rc = check(table, ids, Y, V, n, F, o);
+    if (rc != GNN_OK || n == 0 || F == 0) return rc;
+    (void)hipGetLastError();
+    Lookup a{};
+    a.table = table;
+    a.y = Y;
+    a.ids = {ids, o.ids_is_64, V};
+    a.n = n;
+    a.ldt = o.ldt ? o.ldt : F;
+    a.ldy = o.ldy ? o.ldy : F;
+    a.f = int32_t(F);
+    a.scale = o.scale;
+    hipStream_t stream = static_cast<hipStream_t>(o.stream);
+    if (o.table_dtype == GNN_F32) o.dtype == GNN_F32 ? lookup<float, float>(a, stream) : lookup<float, gnn_bf16>(a, stream);
+    else o.dtype == GNN_F32 ? lookup<gnn_bf16, float>(a, stream) : lookup<gnn_bf16, gnn_bf16>(a, stream);
+    GNN_HIP_TRY(hipGetLastError());
+    return GNN_OK;
+}
+
+extern "C" GNN_API int64_t gnn_lookup_workspace_bytes(int64_t V, int64_t n, int64_t F) {
+    if (V <= 0 || n <= 0 || F <= 0 || V > kMostRows || n > kMostRows || F > kMostColumns) return 0;
+    const Room a = room_of(V, n, F, false), b = room_of(V, n, F, true);
+    return 4 * (a.words > b.words ? a.words : b.words);
+}
+
+extern "C" GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dtable, int64_t V, int64_t n, int64_t F, const gnn_lookup_opts *opts) {
+    if (!opts) return GNN_ERR_INVALID_ARG;
+    const gnn_lookup_opts &o = *opts;
+    const int rc = check(dtable, ids, dY, V, n, F, o);
+    if (rc != GNN_OK || V == 0 || F == 0 || (n == 0 && o.accumulate)) return rc;
+    const bool eight = o.dtype == GNN_BF16;
+    const Room r = room_of(V, n, F, eight);
+    if (n > 0 && (!o.workspace || misaligned(o.workspace, 16) || o.workspace_bytes < 4 * r.words)) return GNN_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    hipStream_t stream = static_cast<hipStream_t>(o.stream);
+    Grad a{};
+    a.dy = dY;
+    a.dtable = dtable;
+    a.rows = V;
+    a.n = n;
+    a.ldt = o.ldt ? o.ldt : F;
+    a.ldy = o.ldy ? o.ldy : F;
+    a.f = int32_t(F);
+    a.vectors = int32_t(r.vectors);
+    a.lanes_log2 = r.lanes_log2;
+    a.accumulate = o.accumulate;
+    a.scale = o.scale;
+    a.sum_blocks = r.blocks;
+    a.zero_blocks = o.accumulate ? 0 : (V + kZeroRows - 1) / kZeroRows;
+    if (n > 0) {
+        uint32_t *next = static_cast<uint32_t *>(o.workspace);
+        a.head = reinterpret_cast<float *>(next);
+        next += r.blocks * F;
+        a.tail = reinterpret_cast<float *>(next);
+        next += r.blocks * F;
+        a.flags = next;
+        next += r.blocks;
+        uint32_t *buf_k[2] = {next, next + n}, *buf_v[2] = {next + 2 * n, next + 3 * n};
+        next += 4 * n;
+        key_kernel<<<grid_of((n + kThreads - 1) / kThreads), kThreads, 0, stream>>>(Ids{ids, o.ids_is_64, V}, n, buf_k[0]);
+        GNN_HIP_TRY(hipGetLastError());
+        uint32_t *keys = nullptr, *order = nullptr;
+        const int sorted = gnn_radix_sort_positions(buf_k, buf_v, n, gnn_ilog2_ceil(V + 1), next, next + r.table, stream, &keys, &order);
+        if (sorted != GNN_OK) return sorted;
+        a.key = keys;
+        a.order = order;
+    }
+    const int64_t slices = (r.vectors + (int64_t(1) << r.lanes_log2) - 1) >> r.lanes_log2;
+    if (slices > 65535) return GNN_ERR_UNSUPPORTED;
+    if (o.dtype == GNN_F32) return o.table_dtype == GNN_F32 ? grad<float, float>(a, slices, stream) : grad<float, gnn_bf16>(a, slices, stream);
+    return o.table_dtype == GNN_F32 ? grad<gnn_bf16, float>(a, slices, stream) : grad<gnn_bf16, gnn_bf16>(a, slices, stream);
+}

@@ -1,0 +1,654 @@
+// Orthogonalised updates of weight matrices: Newton-Schulz products, and the optimizer step that uses them.
+//
+// With X = U / (|U| + eps), m x n, m <= n (the transposed matrix where it is taller than wide), and per step
+//     A = X X^T,   Q = a I + b A + c A A,   X = Q X,
+// singular values s of X become a s + b s^3 + c s^5.  Three products a step, all of the form  C[i][j] = sum_k P[i][k] R[j][k]:  A from X and X, Q
+// from A and A (A is symmetric), X from Q and X^T, which is kept beside X.  A and Q are symmetric: only the tiles on and below the diagonal
+// are computed, and written to both places.
+//
+// Operands live in the workspace as the matrix cores take them: split into P bf16 numbers whose sum they are (P = 3: all 24 bits of fp32; P = 2: 16 bits,
+// for bf16 matrices), in fragments of 32 rows x 16 k, 1 KB a fragment, the 16 bytes of lane 32 * (k / 8) + row one after the other.  So whatever
+// fetches a fragment reads 1 KB in a row, nothing is split twice, and a product's epilogue, which has four neighbouring results of a column in a
+// lane, writes 8 bytes a plane.  Rows and columns are filled up with zeros to whole tiles, which the products keep zero.
+//
+// Of the products of parts those that matter are formed (P = 3: six of nine, the others are below 2^-26; P = 2: three of four, 2^-18), summed from zero over
+// 16 k, smallest first, and added to the result with one rounding: the matrix cores cut off what lies below a sum's last bit, so that long chains
+// through them would be the worse sums.
+//
+// Small matrices: a workgroup has a tile of 32 x 32 and its four wavefronts a quarter of k each, straight from the caches; such a product is one latency.
+// Large ones: tiles of 64 x 64 or 128 x 128 through LDS.  All matrices of a call of the same kind share the launches.
+#include "common.h"
+#include "rows.h"
+
+#include <math.h>
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMats = 16;               // of a launch
+constexpr int kNormBlocks = 256;        // partial sums of squares of a matrix, at most
+constexpr int kNormChunk = 4096;        // elements of a workgroup, at least
+constexpr int64_t kMostSide = 65536, kMostSteps = 100;
+
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+struct Mat {
+    uint16_t *x, *xt[2], *a, *q;        // planes: X (rows m, k n), X^T (rows n, k m) before and after a step, A and Q
+    double *squares;                    // [norm_blocks]
+    const void *in;                     // U, or the gradient
+    void *out;                          // O, or the parameters
+    float *momentum, *master;           // of a Muon step, or nullptr
+    int64_t ld_in, ld_out;
+    int32_t m, n, mp, np;               // m <= n, and filled up
+    int32_t rows, cols;                 // of U
+    int32_t norm_blocks, flags;         // kBf16, kTall
+    float decay, rate;                  // 1 - lr weight_decay; lr update_scale
+    int32_t first[4];                   // workgroup that begins it: of the norms, the first planes, symmetric products, others
+};
+enum { kBf16 = 1, kTall = 2 };          // tall: rows > cols
+enum Phase { kGram, kPolynomial, kUpdate, kLast };
+
+struct Job {
+    Mat mat[kMats];
+    int32_t count;
+    int32_t muon, nesterov;
+    float mu, a, b, c;
+    double eps;
+    const float *grad_scale;
+};
+static_assert(sizeof(Job) <= 4096, "kernel arguments");
+
+// the last matrix that begins at this workgroup or before
+__device__ __forceinline__ int matrix_of_block(const Job &j, int which) {
+    int k = 0;
+    for (int i = 1; i < j.count; ++i)
+        if (j.mat[i].first[which] <= int(blockIdx.x)) k = i;
+    return k;
+}
+
+__device__ __forceinline__ float element(const void *p, int64_t i, bool bf16) {
+    return bf16 ? gnn_rows<gnn_bf16>::get(static_cast<const gnn_bf16 *>(p) + i) : static_cast<const float *>(p)[i];
+}
+
+// ---- the update and its norm
+
+// The sums of squares are fp64: squares of fp32 numbers neither overflow nor vanish there.
+__global__ void __launch_bounds__(kThreads) norm_kernel(const Job j) {
+    const Mat &t = j.mat[matrix_of_block(j, 0)];
+    const int part = int(blockIdx.x) - t.first[0];
+    const int64_t total = int64_t(t.rows) * t.cols;
+    const int64_t per = (total + t.norm_blocks - 1) / t.norm_blocks, begin = part * per, end = begin + per < total ? begin + per : total;
+    const bool bf16 = t.flags & kBf16;
+    const float gs = j.grad_scale ? *j.grad_scale : 1.0f;
+    double s = 0.0;
+    for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) {
+        float u;
+        if (j.muon) {
+            const float g = element(t.in, i, bf16) * gs;
+            const float mo = j.mu * t.momentum[i] + g;
+            t.momentum[i] = mo;
+            u = j.nesterov ? g + j.mu * mo : mo;
+        } else {
+            u = element(t.in, t.ld_in == t.cols ? i : i / t.cols * t.ld_in + i % t.cols, bf16);
+        }
+        s += double(u) * double(u);
+    }
+    __shared__ double sums[kThreads / 64];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) t.squares[part] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
+
+// ---- planes
+
+// x = the sum of P bf16 numbers, exactly where P = 3
+template <int P> __device__ __forceinline__ void split(float x, float (&part)[P]) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        part[p] = float(__bf16(x));
+        x -= part[p];
+    }
+}
+__device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(gnn_f32x2{x, y}, gnn_bf16x2));
+}
+
+// Where element (row, k) of an operand of rows x depth lies in plane 0, in elements of 2 bytes; planes are rows * depth apart.
+__device__ __forceinline__ int64_t place(int depth, int row, int k) {
+    return (int64_t(row >> 5) * (depth >> 4) + (k >> 4)) * 512 + (((k >> 3) & 1) * 32 + (row & 31)) * 8 + (k & 7);
+}
+// four neighbouring k, the first a multiple of four
+template <int P> __device__ __forceinline__ void put4(uint16_t *planes, int rows, int depth, int row, int k, const float (&v)[4]) {
+    uint16_t *p = planes + place(depth, row, k);
+    float part[4][P];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split<P>(v[i], part[i]);
+#pragma unroll
+    for (int q = 0; q < P; ++q)
+        *reinterpret_cast<uint2 *>(p + int64_t(q) * rows * depth) = make_uint2(bf16_pair(part[0][q], part[1][q]), bf16_pair(part[2][q], part[3][q]));
+}
+template <int P> __device__ __forceinline__ void get4(const uint16_t *planes, int rows, int depth, int row, int k, float (&v)[4]) {
+    const uint16_t *p = planes + place(depth, row, k);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = 0.0f;
+#pragma unroll
+    for (int q = P - 1; q >= 0; --q) {  // smallest first: the sum is exact
+        const uint2 w = *reinterpret_cast<const uint2 *>(p + int64_t(q) * rows * depth);
+        v[0] += __uint_as_float(w.x << 16);
+        v[1] += __uint_as_float(w.x & 0xFFFF0000u);
+        v[2] += __uint_as_float(w.y << 16);
+        v[3] += __uint_as_float(w.y & 0xFFFF0000u);
+    }
+}
+
+// X and X^T from U: a workgroup has a tile of 64 x 64 of U.
+template <int P> __global__ void __launch_bounds__(kThreads) planes_kernel(const Job j) {
+    const Mat &t = j.mat[matrix_of_block(j, 1)];
+    const bool tall = t.flags & kTall, bf16 = t.flags & kBf16;
+    const int rp = tall ? t.np : t.mp, cp = tall ? t.mp : t.np;  // filled up sides of U
+    const int tiles = cp / 64, tile = int(blockIdx.x) - t.first[1];
+    const int r0 = tile / tiles * 64, c0 = tile % tiles * 64;
+    __shared__ float u[64][65];
+    __shared__ double sums[kThreads / 64];
+    double s = 0.0;
+    for (int i = int(threadIdx.x); i < t.norm_blocks; i += kThreads) s += t.squares[i];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+    __syncthreads();
+    const double norm = sqrt((sums[0] + sums[1]) + (sums[2] + sums[3]));
+    const double inverse = norm <= 1.7e308 ? 1.0 / (norm + j.eps) : __builtin_nan("");  // what is not finite reaches all of the matrix
+    const float gs = j.grad_scale ? *j.grad_scale : 1.0f;
+    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+    for (int r = wave; r < 64; r += 4) {
+        const int row = r0 + r, col = c0 + lane;
+        float x = 0.0f;
+        if (row < t.rows && col < t.cols) {
+            if (j.muon) {
+                const int64_t i = int64_t(row) * t.cols + col;
+                const float mo = t.momentum[i];
+                x = j.nesterov ? element(t.in, i, bf16) * gs + j.mu * mo : mo;
+            } else {
+                x = element(t.in, int64_t(row) * t.ld_in + col, bf16);
+            }
+            x = float(double(x) * inverse);
+        }
+        u[r][lane] = x;
+    }
+    __syncthreads();
+    uint16_t *by_row = tall ? t.xt[0] : t.x, *by_col = tall ? t.x : t.xt[0];  // rows of U as rows; columns of U as rows
+    for (int i = int(threadIdx.x); i < 64 * 16; i += kThreads) {
+        const int r = i & 63, k = (i >> 6) * 4;
+        const float v[4] = {u[r][k], u[r][k + 1], u[r][k + 2], u[r][k + 3]};
+        put4<P>(by_row, rp, cp, r0 + r, c0 + k, v);
+        const float w[4] = {u[k][r], u[k + 1][r], u[k + 2][r], u[k + 3][r]};
+        put4<P>(by_col, cp, rp, c0 + r, r0 + k, w);
+    }
+}
+
+// ---- products
+
+// The operands of a phase: C[i][j] = sum_k left[i][k] right[j][k]
+struct Operands {
+    const uint16_t *left, *right;
+    int rows, cols, depth;
+};
+template <Phase phase> __device__ __forceinline__ Operands operands(const Mat &t, int step) {
+    if constexpr (phase == kGram) return {t.x, t.x, t.mp, t.mp, t.np};
+    else if constexpr (phase == kPolynomial) return {t.a, t.a, t.mp, t.mp, t.mp};
+    else return {t.q, t.xt[step & 1], t.mp, t.np, t.mp};
+}
+
+// the tile of a workgroup; of symmetric results those on and below the diagonal
+__device__ __forceinline__ void tile_of(int number, bool symmetric, int tiles_across, int &ti, int &tj) {
+    if (!symmetric) {
+        ti = number / tiles_across;
+        tj = number - ti * tiles_across;
+        return;
+    }
+    ti = int((sqrtf(8.0f * float(number) + 1.0f) - 1.0f) * 0.5f);
+    while (ti * (ti + 1) / 2 > number) --ti;
+    while ((ti + 1) * (ti + 2) / 2 <= number) ++ti;
+    tj = number - ti * (ti + 1) / 2;
+}
+
+template <int P> __device__ __forceinline__ void products(float16v &sum, const bf16x8 (&a)[P], const bf16x8 (&b)[P]) {
+#pragma unroll
+    for (int s = P - 1; s >= 0; --s)
+#pragma unroll
+        for (int p = 0; p <= s; ++p) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[p], b[s - p], sum, 0, 0, 0);
+}
+
+// What a phase makes of four sums, rows row_i .. row_i + 3 of column row_c, or the same columns of that row: A is symmetric.
+template <int P, Phase phase> __device__ __forceinline__ void finish(const Job &j, const Mat &t, int row_i, int row_c, float (&v)[4]) {
+    if (phase != kPolynomial) return;
+    float a[4];
+    get4<P>(t.a, t.mp, t.mp, row_c, row_i, a);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = fmaf(j.c, v[i], j.b * a[i]) + (row_i + i == row_c && row_c < t.m ? j.a : 0.0f);
+}
+
+__device__ __forceinline__ void write_out(const Job &j, const Mat &t, int64_t r, int64_t c, float o) {
+    const bool bf16 = t.flags & kBf16;
+    const int64_t at = r * t.ld_out + c;
+    if (j.muon) {
+        const float p = t.master ? t.master[at] : element(t.out, at, bf16);
+        o = p * t.decay - t.rate * o;
+        if (t.master) t.master[at] = o;
+    }
+    if (bf16) gnn_rows<gnn_bf16>::set(static_cast<gnn_bf16 *>(t.out) + at, o);
+    else static_cast<float *>(t.out)[at] = o;
+}
+
+// Rows row .. row + 3 of column col of a phase's result.
+template <int P, Phase phase> __device__ __forceinline__ void write_down(const Job &j, const Mat &t, int step, int row, int col, const float (&v)[4]) {
+    if (phase == kGram) put4<P>(t.a, t.mp, t.mp, col, row, v);
+    else if (phase == kPolynomial) put4<P>(t.q, t.mp, t.mp, col, row, v);
+    else if (phase == kUpdate) put4<P>(t.xt[(step + 1) & 1], t.np, t.mp, col, row, v);
+    else if (!(t.flags & kTall)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (row + i < t.m && col < t.n) write_out(j, t, row + i, col, v[i]);
+    }
+}
+// Columns col .. col + 3 of row `row`.
+template <int P, Phase phase> __device__ __forceinline__ void write_across(const Job &j, const Mat &t, int row, int col, const float (&v)[4]) {
+    if (phase == kGram) put4<P>(t.a, t.mp, t.mp, row, col, v);
+    else if (phase == kPolynomial) put4<P>(t.q, t.mp, t.mp, row, col, v);
+    else if (phase == kUpdate) put4<P>(t.x, t.mp, t.np, row, col, v);
+    else if (t.flags & kTall) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (row < t.m && col + i < t.n) write_out(j, t, col + i, row, v[i]);
+    }
+}
+
+// Tiles of 32 x 32, the four wavefronts have every fourth 16 of k.
+template <int P, Phase phase> __global__ void __launch_bounds__(kThreads) small_product_kernel(const Job j, int step) {
+    constexpr bool symmetric = phase == kGram || phase == kPolynomial;
+    const Mat &t = j.mat[matrix_of_block(j, symmetric ? 2 : 3)];
+    const Operands o = operands<phase>(t, step);
+    int ti, tj;
+    tile_of(int(blockIdx.x) - t.first[symmetric ? 2 : 3], symmetric, o.cols / 32, ti, tj);
+    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+    const int ks = o.depth / 16;
+    const bf16x8 *left = reinterpret_cast<const bf16x8 *>(o.left) + int64_t(ti) * ks * 64 + lane;
+    const bf16x8 *right = reinterpret_cast<const bf16x8 *>(o.right) + int64_t(tj) * ks * 64 + lane;
+    const int64_t left_plane = int64_t(o.rows) * o.depth / 8, right_plane = int64_t(o.cols) * o.depth / 8;
+    float16v acc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
+    constexpr int U = 2;
+    for (int k = wave; k < ks; k += 4 * U) {
+        bf16x8 a[U][P], b[U][P];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (k + 4 * u < ks)
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    a[u][p] = left[p * left_plane + (k + 4 * u) * 64];
+                    b[u][p] = right[p * right_plane + (k + 4 * u) * 64];
+                }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (k + 4 * u < ks) {
+                float16v sum;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sum[v] = 0.0f;
+                products<P>(sum, a[u], b[u]);
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[v] += sum[v];
+            }
+    }
+    __shared__ float tile[4][32][33];
+    const int l32 = lane & 31, lk = lane >> 5;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) tile[wave][8 * (v / 4) + 4 * lk + v % 4][l32] = acc[v];
+    __syncthreads();
+    float v[4];
+    const int at = 8 * wave + 4 * lk;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (tile[0][at + i][l32] + tile[1][at + i][l32]) + (tile[2][at + i][l32] + tile[3][at + i][l32]);
+    finish<P, phase>(j, t, ti * 32 + at, tj * 32 + l32, v);
+    write_down<P, phase>(j, t, step, ti * 32 + at, tj * 32 + l32, v);
+    if (symmetric && ti == tj) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (tile[0][l32][at + i] + tile[1][l32][at + i]) + (tile[2][l32][at + i] + tile[3][l32][at + i]);
+    finish<P, phase>(j, t, tj * 32 + at, ti * 32 + l32, v);
+    write_across<P, phase>(j, t, ti * 32 + l32, tj * 32 + at, v);
+}
+
+// Tiles of (64 TI)^2 through LDS: four wavefronts of TI x TI fragments each, 16 k at a time, the next 16 k on their way to the other half.
+template <int P, int TI, Phase phase> __global__ void __launch_bounds__(kThreads, 2) product_kernel(const Job j, int step) {
+    constexpr int FRAGS = 4 * TI * P, MINE = FRAGS / 4, TILE = 64 * TI;  // fragments of a step, of a wavefront
+    __shared__ union {
+        u32x4 frag[2][FRAGS][64];
+        float turn[4][32][33];
+    } lds;
+    constexpr bool symmetric = phase == kGram || phase == kPolynomial;
+    const Mat &t = j.mat[matrix_of_block(j, symmetric ? 2 : 3)];
+    const Operands o = operands<phase>(t, step);
+    int ti, tj;
+    tile_of(int(blockIdx.x) - t.first[symmetric ? 2 : 3], symmetric, o.cols / TILE, ti, tj);
+    const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int ks = o.depth / 16;
+
+    // fragment f of a step: operand f / (2 TI P), then 32 rows, then plane
+    const u32x4 *from[MINE];
+#pragma unroll
+    for (int f = 0; f < MINE; ++f) {
+        const int g = wave * MINE + f, side = g / (2 * TI * P), r = g / P % (2 * TI), p = g % P;
+        const int64_t rb = int64_t(side ? tj : ti) * 2 * TI + r, plane = int64_t(side ? o.cols : o.rows) * o.depth;
+        from[f] = reinterpret_cast<const u32x4 *>((side ? o.right : o.left) + p * plane + rb * ks * 512) + lane;
+    }
+    u32x4 next[MINE];
+    auto load = [&](int k) {
+#pragma unroll
+        for (int f = 0; f < MINE; ++f) next[f] = from[f][int64_t(k < ks ? k : ks - 1) * 64];
+    };
+    auto stage = [&](int half) {
+#pragma unroll
+        for (int f = 0; f < MINE; ++f) lds.frag[half][wave * MINE + f][lane] = next[f];
+    };
+    const int wi = wave >> 1, wj = wave & 1;
+    float16v acc[TI][TI];
+#pragma unroll
+    for (int a = 0; a < TI; ++a)
+#pragma unroll
+        for (int b = 0; b < TI; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.0f;
+
+    load(0);
+    stage(0);
+    load(1);
+    __syncthreads();
+#pragma unroll 1
+    for (int k = 0; k < ks; ++k) {
+        bf16x8 a[TI][P], b[TI][P];
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                a[i][p] = __builtin_bit_cast(bf16x8, lds.frag[k & 1][(wi * TI + i) * P + p][lane]);
+                b[i][p] = __builtin_bit_cast(bf16x8, lds.frag[k & 1][(2 * TI + wj * TI + i) * P + p][lane]);
+            }
+#pragma unroll
+        for (int x = 0; x < TI; ++x)
+#pragma unroll
+            for (int y = 0; y < TI; ++y) {
+                float16v sum;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sum[v] = 0.0f;
+                products<P>(sum, a[x], b[y]);
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[x][y][v] += sum[v];
+            }
+        stage((k + 1) & 1);
+        load(k + 2);
+        __syncthreads();
+    }
+
+    const int l32 = lane & 31, lk = lane >> 5;
+#pragma unroll
+    for (int x = 0; x < TI; ++x)
+#pragma unroll
+        for (int y = 0; y < TI; ++y) {
+            const int row0 = ti * TILE + (wi * TI + x) * 32, col0 = tj * TILE + (wj * TI + y) * 32;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int at = 8 * g + 4 * lk;
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = acc[x][y][4 * g + i];
+                finish<P, phase>(j, t, row0 + at, col0 + l32, v);
+                write_down<P, phase>(j, t, step, row0 + at, col0 + l32, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) lds.turn[wave][at + i][l32] = v[i];
+            }
+            if (symmetric && ti == tj) continue;  // (a tile on the diagonal is computed whole)
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int at = 8 * g + 4 * lk;
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = lds.turn[wave][l32][at + i];
+                write_across<P, phase>(j, t, row0 + l32, col0 + at, v);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+}
+
+// ---- host
+
+bool misaligned(const void *p, int64_t to) { return reinterpret_cast<uintptr_t>(p) % uintptr_t(to) != 0; }
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// A matrix as both calls describe it.
+struct Entry {
+    const void *in;
+    void *out;
+    float *momentum, *master;
+    int64_t rows, cols, ld_in, ld_out;
+    int32_t dtype;
+    float decay, rate;
+    bool skip;
+};
+
+// How the products of a matrix are tiled: 0 tiles of 32, one latency; 1 of 64; 2 of 128.
+int kind_of(int64_t rows, int64_t cols) {
+    const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    if (n <= 512) return 0;
+    return up(m, 128) * up(n, 128) >= int64_t(256) * 128 * 128 ? 2 : 1;
+}
+int64_t tile_of_kind(int kind) { return kind == 0 ? 32 : kind == 1 ? 64 : 128; }
+
+struct Sizes {
+    int kind, parts;
+    int64_t m, n, mp, np, bytes;
+    int32_t norm_blocks;
+};
+Sizes sizes_of(int64_t rows, int64_t cols, int32_t dtype) {
+    Sizes s;
+    s.kind = kind_of(rows, cols);
+    s.parts = dtype == GNN_BF16 ? 2 : 3;
+    s.m = rows < cols ? rows : cols;
+    s.n = rows < cols ? cols : rows;
+    const int64_t to = tile_of_kind(s.kind) < 64 ? 64 : tile_of_kind(s.kind);  // the first planes are made in tiles of 64
+    s.mp = up(s.m, to);
+    s.np = up(s.n, to);
+    const int64_t blocks = (s.m * s.n + kNormChunk - 1) / kNormChunk;
+    s.norm_blocks = int32_t(blocks < kNormBlocks ? blocks : kNormBlocks);
+    s.bytes = 2 * s.parts * (3 * s.mp * s.np + 2 * s.mp * s.mp) + up(8 * s.norm_blocks, 256);
+    return s;
+}
+
+template <int P, Phase phase> int launch_products(const Job &j, int kind, int step, int64_t blocks, hipStream_t stream) {
+    if (blocks > INT32_MAX / kThreads) return GNN_ERR_UNSUPPORTED;
+    if (kind == 0) small_product_kernel<P, phase><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
+    else if (kind == 1) product_kernel<P, 1, phase><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
+    else product_kernel<P, 2, phase><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
+    GNN_HIP_TRY(hipGetLastError());
+    return GNN_OK;
+}
+
+template <int P> int launch_job(const Job &j, int kind, const int64_t (&blocks)[4], int steps, hipStream_t stream) {
+    norm_kernel<<<unsigned(blocks[0]), kThreads, 0, stream>>>(j);
+    planes_kernel<P><<<unsigned(blocks[1]), kThreads, 0, stream>>>(j);
+    GNN_HIP_TRY(hipGetLastError());
+    for (int s = 0; s < steps; ++s) {
+        int rc = launch_products<P, kGram>(j, kind, s, blocks[2], stream);
+        if (rc == GNN_OK) rc = launch_products<P, kPolynomial>(j, kind, s, blocks[2], stream);
+        if (rc == GNN_OK) rc = s + 1 < steps ? launch_products<P, kUpdate>(j, kind, s, blocks[3], stream) : launch_products<P, kLast>(j, kind, s, blocks[3], stream);
+        if (rc != GNN_OK) return rc;
+    }
+    return GNN_OK;
+}
+
+// Matrices of the same kind and type, kMats at a time.
+int orthogonalize(Entry (*at)(const void *, int64_t), const void *list, int64_t count, Job &j, int steps, uint8_t *room, hipStream_t stream) {
+    for (int kind = 0; kind < 3; ++kind)
+        for (int parts = 2; parts <= 3; ++parts) {
+            int64_t blocks[4] = {0, 0, 0, 0};
+            j.count = 0;
+            auto flush = [&]() -> int {
+                if (j.count == 0) return GNN_OK;
+                const int rc = parts == 2 ? launch_job<2>(j, kind, blocks, steps, stream) : launch_job<3>(j, kind, blocks, steps, stream);
+                j.count = 0;
+                for (int64_t &b : blocks) b = 0;
+                return rc;
+            };
+            for (int64_t k = 0; k < count; ++k) {
+                const Entry e = at(list, k);
+                if (e.skip || e.rows == 0 || e.cols == 0) continue;
+                const Sizes s = sizes_of(e.rows, e.cols, e.dtype);
+                if (s.kind != kind || s.parts != parts) continue;
+                const int64_t tile = tile_of_kind(kind), across = s.mp / tile;
+                const int64_t more[4] = {s.norm_blocks, s.mp / 64 * (s.np / 64), across * (across + 1) / 2, across * (s.np / tile)};
+                bool full = j.count == kMats;
+                for (int i = 0; i < 4; ++i) full |= blocks[i] + more[i] > INT32_MAX / kThreads;
+                if (full) {
+                    const int rc = flush();
+                    if (rc != GNN_OK) return rc;
+                }
+                Mat &t = j.mat[j.count++];
+                t = Mat{};
+                const int64_t xs = s.parts * s.mp * s.np, as = s.parts * s.mp * s.mp;
+                uint16_t *p = reinterpret_cast<uint16_t *>(room);
+                t.x = p;
+                t.xt[0] = p + xs;
+                t.xt[1] = p + 2 * xs;
+                t.a = p + 3 * xs;
+                t.q = t.a + as;
+                t.squares = reinterpret_cast<double *>(t.q + as);
+                room += s.bytes;
+                t.in = e.in;
+                t.out = e.out;
+                t.momentum = e.momentum;
+                t.master = e.master;
+                t.ld_in = e.ld_in;
+                t.ld_out = e.ld_out;
+                t.m = int32_t(s.m);
+                t.n = int32_t(s.n);
+                t.mp = int32_t(s.mp);
+                t.np = int32_t(s.np);
+                t.rows = int32_t(e.rows);
+                t.cols = int32_t(e.cols);
+                t.norm_blocks = s.norm_blocks;
+                t.flags = (e.dtype == GNN_BF16 ? kBf16 : 0) | (e.rows > e.cols ? kTall : 0);
+                t.decay = e.decay;
+                t.rate = e.rate;
+                for (int i = 0; i < 4; ++i) {
+                    t.first[i] = int32_t(blocks[i]);
+                    blocks[i] += more[i];
+                }
+            }
+            const int rc = flush();
+            if (rc != GNN_OK) return rc;
+        }
+    return GNN_OK;
+}
+
+bool sides_fit(int64_t rows, int64_t cols) { return rows >= 0 && cols >= 0 && rows <= kMostSide && cols <= kMostSide; }
+bool known(int32_t dtype) { return dtype == GNN_F32 || dtype == GNN_BF16; }
+int64_t size_of(int32_t dtype) { return dtype == GNN_F32 ? 4 : 2; }
+bool is_finite(double x) { return x - x == 0.0; }
+
+int check_matrix(const gnn_orthogonalize_matrix &t) {
+    if (!sides_fit(t.rows, t.cols) || !known(t.dtype)) return GNN_ERR_INVALID_ARG;
+    if ((t.ld_in && t.ld_in < t.cols) || (t.ld_out && t.ld_out < t.cols)) return GNN_ERR_INVALID_ARG;
+    if (t.rows == 0 || t.cols == 0) return GNN_OK;
+    if (!t.in || !t.out || misaligned(t.in, size_of(t.dtype)) || misaligned(t.out, size_of(t.dtype))) return GNN_ERR_INVALID_ARG;
+    if (t.in == t.out && t.rows > 1 && (t.ld_in ? t.ld_in : t.cols) != (t.ld_out ? t.ld_out : t.cols)) return GNN_ERR_INVALID_ARG;
+    return GNN_OK;
+}
+int check_matrix(const gnn_muon_matrix &t) {
+    if (!sides_fit(t.rows, t.cols) || !known(t.dtype) || !(t.weight_decay >= 0.0f) || !is_finite(t.update_scale)) return GNN_ERR_INVALID_ARG;
+    if (t.rows == 0 || t.cols == 0 || !t.grad) return GNN_OK;
+    if (!t.param || !t.momentum || (t.master && t.dtype == GNN_F32)) return GNN_ERR_INVALID_ARG;
+    if (misaligned(t.param, size_of(t.dtype)) || misaligned(t.grad, size_of(t.dtype)) || misaligned(t.momentum, 4) || misaligned(t.master, 4)) return GNN_ERR_INVALID_ARG;
+    return GNN_OK;
+}
+bool leaves_alone(const gnn_orthogonalize_matrix &) { return false; }
+bool leaves_alone(const gnn_muon_matrix &t) { return !t.grad; }
+
+// -1: a matrix that the call refuses
+template <typename M> int64_t room_of(const M *matrices, int64_t count) {
+    if (count < 0 || (count > 0 && !matrices)) return -1;
+    int64_t bytes = 0;
+    for (int64_t k = 0; k < count; ++k) {
+        if (check_matrix(matrices[k]) != GNN_OK) return -1;
+        if (matrices[k].rows > 0 && matrices[k].cols > 0 && !leaves_alone(matrices[k])) bytes += sizes_of(matrices[k].rows, matrices[k].cols, matrices[k].dtype).bytes;
+    }
+    return bytes;
+}
+bool coefficients_fit(double a, double b, double c, double eps, int32_t steps) {
+    return is_finite(a) && is_finite(b) && is_finite(c) && eps > 0.0 && is_finite(eps) && steps >= 1 && steps <= kMostSteps;
+}
+
+}  // namespace
+
+extern "C" GNN_API int64_t gnn_orthogonalize_workspace_bytes(const gnn_orthogonalize_matrix *matrices, int64_t n_matrices) {
+    const int64_t bytes = room_of(matrices, n_matrices);
+    return bytes < 0 ? 0 : bytes;
+}
+
+extern "C" GNN_API int gnn_orthogonalize(const gnn_orthogonalize_matrix *matrices, int64_t n_matrices, const gnn_orthogonalize_opts *opts) {
+    if (!opts || !coefficients_fit(opts->a, opts->b, opts->c, opts->eps, opts->steps)) return GNN_ERR_INVALID_ARG;
+    const gnn_orthogonalize_opts &o = *opts;
+    const int64_t bytes = room_of(matrices, n_matrices);
+    if (bytes < 0) return GNN_ERR_INVALID_ARG;
+    if (bytes == 0) return GNN_OK;
+    if (!o.workspace || misaligned(o.workspace, 256) || o.workspace_bytes < bytes) return GNN_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    Job j{};
+    j.a = float(o.a);
+    j.b = float(o.b);
+    j.c = float(o.c);
+    j.eps = o.eps;
+    return orthogonalize(
+        [](const void *list, int64_t k) {
+            const gnn_orthogonalize_matrix &t = static_cast<const gnn_orthogonalize_matrix *>(list)[k];
+            return Entry{t.in, t.out, nullptr, nullptr, t.rows, t.cols, t.ld_in ? t.ld_in : t.cols, t.ld_out ? t.ld_out : t.cols, t.dtype, 1.0f, 1.0f, false};
+        },
+        matrices, n_matrices, j, o.steps, static_cast<uint8_t *>(o.workspace), static_cast<hipStream_t>(o.stream));
+}
+
+extern "C" GNN_API int64_t gnn_muon_workspace_bytes(const gnn_muon_matrix *matrices, int64_t n_matrices) {
+    const int64_t bytes = room_of(matrices, n_matrices);
+    return bytes < 0 ? 0 : bytes;
+}
+
+extern "C" GNN_API int gnn_muon_step(const gnn_muon_matrix *matrices, int64_t n_matrices, const gnn_muon_opts *opts) {
+    if (!opts || !coefficients_fit(opts->a, opts->b, opts->c, opts->eps, opts->steps)) return GNN_ERR_INVALID_ARG;
+    const gnn_muon_opts &o = *opts;
+    if (!(o.lr >= 0.0) || !is_finite(o.lr) || !(o.momentum >= 0.0 && o.momentum < 1.0) || (o.nesterov & ~1)) return GNN_ERR_INVALID_ARG;
+    const int64_t bytes = room_of(matrices, n_matrices);
+    if (bytes < 0) return GNN_ERR_INVALID_ARG;
+    if (bytes == 0) return GNN_OK;
+    if (!o.workspace || misaligned(o.workspace, 256) || o.workspace_bytes < bytes) return GNN_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    Job j{};
+    j.muon = 1;
+    j.nesterov = o.nesterov;
+    j.mu = float(o.momentum);
+    j.a = float(o.a);
+    j.b = float(o.b);
+    j.c = float(o.c);
+    j.eps = o.eps;
+    j.grad_scale = o.grad_scale;
+    struct List { const gnn_muon_matrix *matrices; double lr; } list{matrices, o.lr};
+    return orthogonalize(
+        [](const void *p, int64_t k) {
+            const List &l = *static_cast<const List *>(p);
+            const gnn_muon_matrix &t = l.matrices[k];
+            return Entry{t.grad, t.param, t.momentum, t.master, t.rows, t.cols, t.cols, t.cols, t.dtype, float(1.0 - l.lr * double(t.weight_decay)),
+                      float(l.lr * double(t.update_scale)), t.grad == nullptr};
+        },
+        &list, n_matrices, j, o.steps, static_cast<uint8_t *>(o.workspace), static_cast<hipStream_t>(o.stream));
+}

@@ -12,7 +12,7 @@
 
 #include "gnnagg.h"
 
-static PyObject *dtype_f32, *dtype_bf16, *dtype_i32, *dtype_i64, *get_device, *get_raw_stream, *stream_type;
+static PyObject *dtype_f32, *dtype_bf16, *dtype_i32, *dtype_i64, *dtype_u8, *get_device, *get_raw_stream, *stream_type;
 static PyObject *s_data_ptr, *s_stride, *s_dtype, *s_handle, *s_cuda_stream, *s_is_contiguous, *s_nbytes, *s_shape, *s_is_cuda;
 
 static __typeof__(&gnn_aggregate_fwd) fn_aggregate_fwd;
@@ -27,6 +27,12 @@ static __typeof__(&gnn_group_norm_fwd) fn_group_norm_fwd;
 static __typeof__(&gnn_group_norm_bwd) fn_group_norm_bwd;
 static __typeof__(&gnn_softmax_xent) fn_softmax_xent;
 static __typeof__(&gnn_adamw_step) fn_adamw_step;
+static __typeof__(&gnn_lookup_fwd) fn_lookup_fwd;
+static __typeof__(&gnn_lookup_bwd) fn_lookup_bwd;
+static __typeof__(&gnn_store_rows) fn_store_rows;
+static __typeof__(&gnn_load_rows) fn_load_rows;
+static __typeof__(&gnn_orthogonalize) fn_orthogonalize;
+static __typeof__(&gnn_muon_step) fn_muon_step;
 
 /* ---- scalars: 0 on success, -1 with an exception set */
 
@@ -613,6 +619,175 @@ static PyObject *adamw_step(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     return PyLong_FromLong(status);
 }
 
+/* ---- rows by id */
+
+/* A matrix of features of its own shape and type */
+static int any_matrix(PyObject *t, int64_t shape[2], int32_t *dtype, void **out, int64_t *ld) {
+    shape[0] = shape[1] = -1;
+    return feature_matrix(t, 0, shape, dtype, out, ld);
+}
+
+static int same(int64_t a, int64_t b, const char *what) {
+    if (a == b) return 0;
+    PyErr_SetString(PyExc_ValueError, what);
+    return -1;
+}
+
+static const char *const one_id = "one id a row expected", *const same_columns = "both matrices must have the same number of columns";
+
+/* table, ids, Y, scale, stream */
+static PyObject *lookup_fwd(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    if (expect(n, 5)) return NULL;
+    if (!fn_lookup_fwd) { PyErr_SetString(PyExc_RuntimeError, "connect() first"); return NULL; }
+    gnn_lookup_opts o = {0};
+    void *table, *ids, *Y;
+    int64_t ts[2], ys[2], count;
+    double scale;
+    if (any_matrix(a[0], ts, &o.table_dtype, &table, &o.ldt) || integers(a[1], &ids, &o.ids_is_64, &count) ||
+        any_matrix(a[2], ys, &o.dtype, &Y, &o.ldy) || to_double(a[3], &scale) || stream_ptr(a[4], &o.stream) || same(count, ys[0], one_id) ||
+        same(ts[1], ys[1], same_columns))
+        return NULL;
+    o.scale = (float)scale;
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn_lookup_fwd(table, ids, Y, ts[0], ys[0], ys[1], &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* ids, dY, dtable, scale, accumulate, workspace, stream */
+static PyObject *lookup_bwd(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    if (expect(n, 7)) return NULL;
+    if (!fn_lookup_bwd) { PyErr_SetString(PyExc_RuntimeError, "connect() first"); return NULL; }
+    gnn_lookup_opts o = {0};
+    void *ids, *dY, *dtable;
+    int64_t ts[2], ys[2], count;
+    double scale;
+    if (integers(a[0], &ids, &o.ids_is_64, &count) || any_matrix(a[1], ys, &o.dtype, &dY, &o.ldy) ||
+        any_matrix(a[2], ts, &o.table_dtype, &dtable, &o.ldt) || to_double(a[3], &scale) || (o.accumulate = PyObject_IsTrue(a[4])) < 0 ||
+        scratch_of(a[5], &o.workspace, &o.workspace_bytes) || stream_ptr(a[6], &o.stream) || same(count, ys[0], one_id) ||
+        same(ts[1], ys[1], same_columns))
+        return NULL;
+    o.scale = (float)scale;
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn_lookup_bwd(ids, dY, dtable, ts[0], ys[0], ys[1], &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* Store [V, bytes of a row] of bytes with room for F columns: V and the bytes from row to row */
+static int store_of(PyObject *t, int64_t F, void **out, int64_t *V, int64_t *lds) {
+    PyObject *d = dtype_of(t);
+    if (!d) return -1;
+    const int bytes = d == dtype_u8;
+    Py_DECREF(d);
+    if (!bytes) { PyErr_SetString(PyExc_TypeError, "a store is a uint8 matrix"); return -1; }
+    int dims;
+    int64_t stride[2], size[2];
+    if (on_device(t) || strides_of(t, &dims, stride) || size_of(t, size)) return -1;
+    if (dims != 2 || (size[1] > 1 && size[0] > 0 && stride[1] != 1) || (size[0] > 1 && stride[0] < size[1])) {
+        PyErr_SetString(PyExc_ValueError, "a store is two-dimensional, with unit column stride and rows that do not overlap");
+        return -1;
+    }
+    if (size[0] > 0 && size[1] < F + (F + GNN_STORE_BLOCK - 1) / GNN_STORE_BLOCK) {
+        PyErr_SetString(PyExc_ValueError, "rows of the store are too short for the columns and their exponents");
+        return -1;
+    }
+    *V = size[0];
+    *lds = size[0] > 1 ? stride[0] : 0;
+    return data_ptr(t, out);
+}
+
+/* X, store, ids, unique, workspace, stream */
+static PyObject *store_rows(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    if (expect(n, 6)) return NULL;
+    if (!fn_store_rows) { PyErr_SetString(PyExc_RuntimeError, "connect() first"); return NULL; }
+    gnn_store_opts o = {0};
+    void *X, *store, *ids = NULL;
+    int64_t xs[2], V, count;
+    if (any_matrix(a[0], xs, &o.dtype, &X, &o.ldx) || store_of(a[1], xs[1], &store, &V, &o.lds) ||
+        (a[2] != Py_None && (integers(a[2], &ids, &o.ids_is_64, &count) || same(count, xs[0], one_id))) || (o.unique = PyObject_IsTrue(a[3])) < 0 ||
+        scratch_of(a[4], &o.workspace, &o.workspace_bytes) || stream_ptr(a[5], &o.stream))
+        return NULL;
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn_store_rows(X, ids, store, V, xs[0], xs[1], &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* store, Y, ids, stream */
+static PyObject *load_rows(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    if (expect(n, 4)) return NULL;
+    if (!fn_load_rows) { PyErr_SetString(PyExc_RuntimeError, "connect() first"); return NULL; }
+    gnn_store_opts o = {0};
+    void *Y, *store, *ids = NULL;
+    int64_t ys[2], V, count;
+    if (any_matrix(a[1], ys, &o.dtype, &Y, &o.ldx) || store_of(a[0], ys[1], &store, &V, &o.lds) ||
+        (a[2] != Py_None && (integers(a[2], &ids, &o.ids_is_64, &count) || same(count, ys[0], one_id))) || stream_ptr(a[3], &o.stream))
+        return NULL;
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn_load_rows(store, ids, Y, V, ys[0], ys[1], &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* ---- orthogonalised updates */
+
+/* the three coefficients */
+static int three(PyObject *t, double *a, double *b, double *c) {
+    PyObject *s = PySequence_Tuple(t);
+    if (!s) return -1;
+    int bad = PyTuple_GET_SIZE(s) != 3;
+    if (bad) PyErr_SetString(PyExc_ValueError, "three coefficients expected");
+    else bad = to_double(PyTuple_GET_ITEM(s, 0), a) || to_double(PyTuple_GET_ITEM(s, 1), b) || to_double(PyTuple_GET_ITEM(s, 2), c);
+    Py_DECREF(s);
+    return bad ? -1 : 0;
+}
+
+/* address of the descriptors, their number, steps, eps, coefficients, workspace, stream */
+static PyObject *orthogonalize(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    if (expect(n, 7)) return NULL;
+    if (!fn_orthogonalize) { PyErr_SetString(PyExc_RuntimeError, "connect() first"); return NULL; }
+    gnn_orthogonalize_opts o = {0};
+    int64_t address, count;
+    if (to_i64(a[0], &address) || to_i64(a[1], &count) || to_int(a[2], &o.steps) || to_double(a[3], &o.eps) || three(a[4], &o.a, &o.b, &o.c) ||
+        scratch_of(a[5], &o.workspace, &o.workspace_bytes) || stream_ptr(a[6], &o.stream))
+        return NULL;
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn_orthogonalize((const gnn_orthogonalize_matrix *)(intptr_t)address, count, &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* address of the descriptors, their number, lr, momentum, nesterov, steps, eps, coefficients, grad_scale, workspace, stream */
+static PyObject *muon_step(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    if (expect(n, 11)) return NULL;
+    if (!fn_muon_step) { PyErr_SetString(PyExc_RuntimeError, "connect() first"); return NULL; }
+    gnn_muon_opts o = {0};
+    int64_t address, count;
+    void *scale;
+    if (to_i64(a[0], &address) || to_i64(a[1], &count) || to_double(a[2], &o.lr) || to_double(a[3], &o.momentum) || (o.nesterov = PyObject_IsTrue(a[4])) < 0 ||
+        to_int(a[5], &o.steps) || to_double(a[6], &o.eps) || three(a[7], &o.a, &o.b, &o.c) || floats(a[8], 1, 1, &scale) ||
+        scratch_of(a[9], &o.workspace, &o.workspace_bytes) || stream_ptr(a[10], &o.stream))
+        return NULL;
+    o.grad_scale = scale;
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fn_muon_step((const gnn_muon_matrix *)(intptr_t)address, count, &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
 /* connect({name: address}, torch): the library's entry points and torch's types */
 static PyObject *connect(PyObject *self, PyObject *args) {
     (void)self;
@@ -624,9 +799,12 @@ static PyObject *connect(PyObject *self, PyObject *args) {
         {"gnn_ap_bwd_vertex_arg_edges", (void **)&fn_ap_bwd_vertex_arg}, {"gnn_ap_bwd_edge", (void **)&fn_ap_bwd_edge},
         {"gnn_sage_layer_fwd", (void **)&fn_sage_layer_fwd}, {"gnn_sage_layer_bwd", (void **)&fn_sage_layer_bwd},
         {"gnn_group_norm_fwd", (void **)&fn_group_norm_fwd}, {"gnn_group_norm_bwd", (void **)&fn_group_norm_bwd},
-        {"gnn_softmax_xent", (void **)&fn_softmax_xent}, {"gnn_adamw_step", (void **)&fn_adamw_step}};
+        {"gnn_softmax_xent", (void **)&fn_softmax_xent}, {"gnn_adamw_step", (void **)&fn_adamw_step},
+        {"gnn_lookup_fwd", (void **)&fn_lookup_fwd}, {"gnn_lookup_bwd", (void **)&fn_lookup_bwd},
+        {"gnn_store_rows", (void **)&fn_store_rows}, {"gnn_load_rows", (void **)&fn_load_rows},
+        {"gnn_orthogonalize", (void **)&fn_orthogonalize}, {"gnn_muon_step", (void **)&fn_muon_step}};
     const struct { const char *name; PyObject **slot; } attrs[] = {
-        {"float32", &dtype_f32}, {"bfloat16", &dtype_bf16}, {"int32", &dtype_i32}, {"int64", &dtype_i64}};
+        {"float32", &dtype_f32}, {"bfloat16", &dtype_bf16}, {"int32", &dtype_i32}, {"int64", &dtype_i64}, {"uint8", &dtype_u8}};
     for (size_t i = 0; i < sizeof(attrs) / sizeof(attrs[0]); ++i)
         if (!*attrs[i].slot && !(*attrs[i].slot = PyObject_GetAttrString(torch, attrs[i].name))) return NULL;
     if (!get_raw_stream) {
@@ -654,7 +832,8 @@ static PyObject *connect(PyObject *self, PyObject *args) {
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {FAST(aggregate), FAST(ap_fwd), FAST(ap_bwd_vertex), FAST(ap_bwd_vertex_arg), FAST(ap_bwd_edge),
                                 FAST(sage_layer_fwd), FAST(sage_layer_bwd), FAST(group_norm_fwd), FAST(group_norm_bwd),
-                                FAST(softmax_xent), FAST(adamw_step), {"connect", connect, METH_VARARGS, NULL},
+                                FAST(softmax_xent), FAST(adamw_step), FAST(lookup_fwd), FAST(lookup_bwd), FAST(store_rows), FAST(load_rows),
+                                FAST(orthogonalize), FAST(muon_step), {"connect", connect, METH_VARARGS, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", "Argument marshalling of the hot entry points.", -1, methods,
                                     NULL, NULL, NULL, NULL};

@@ -1,4 +1,4 @@
-// Rows of vertex matrices in fp32 and bf16 for the kernels of norm.hip, loss.hip and adamw.hip: VEC elements at a time, in fp32
+// Rows of vertex matrices in fp32 and bf16 for the kernels of norm.hip, loss.hip, adamw.hip, lookup.hip, store.hip and muon.hip: VEC elements at a time, in fp32
 // registers, at the alignment of one element (global loads and stores of 16 bytes need no more).
 #pragma once
 

@@ -1,0 +1,300 @@
+// Rows kept in 8 bits: e4m3 codes with an exponent for every 32 neighbouring columns, written and read by id.
+//
+//     value[c] = code[c] 2^(e - 127),   e = the least with max |x| 2^(127 - e) <= 448 = 1.75 * 2^8:
+//     of max = 1.f * 2^x   e - 127 = x - 8, or x - 7 where 1.f > 1.75.
+//
+// The factor is a power of two, so that products with it are exact and the code is the only rounding: results do not depend on how the kernel
+// is written.  A code has four significant bits wherever the block's largest value lies, so a power of two costs at most one of the 17 binary orders of
+// magnitude that a block spans, and takes one byte where a factor in fp32 takes four.  Codes and exponents of a row lie side by side: a row that is
+// read by id costs the lines of one place.
+//
+// Eight columns a thread, whole rows a workgroup; the four threads of a block find its largest value by lane permutations.  Of rows written with the same id
+// the last one has to stay: a row is written only if no later position has its id.  Few positions are compared in every workgroup;
+// else each position is entered at its id, then raised to the last one, in two small passes before the rows.
+#include "common.h"
+#include "rows.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kItems = 1024;           // pieces of eight columns of a workgroup
+constexpr int kBlock = GNN_STORE_BLOCK;
+constexpr int64_t kCompareHere = 4096; // positions up to which every workgroup compares its rows' ids with all of them
+constexpr int kCompareRows = 32;       // rows of a workgroup then
+constexpr int64_t kMostRows = INT32_MAX, kMostColumns = 1 << 24;
+constexpr unsigned kGridX = 1 << 20;   // workgroups in x: a launch has fewer than 2^32 threads a dimension
+
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+
+struct Rows {
+    const void *ids;       // or nullptr: row i is position i
+    void *x;               // matrix of numbers
+    uint8_t *store;
+    int32_t *last;         // [v] the last position with this id, or nullptr
+    int64_t v, n, ldx, lds;
+    int32_t f, pieces, rows;  // columns; pieces of eight of a row; rows of a workgroup
+    uint32_t reciprocal;      // ceil(2^32 / pieces): quotients of numbers below 2^16
+    int32_t is_64, compare;
+    __device__ __forceinline__ int64_t id(int64_t i) const {
+        if (!ids) return i;
+        const int64_t t = is_64 ? static_cast<const int64_t *>(ids)[i] : int64_t(static_cast<const int32_t *>(ids)[i]);
+        return uint64_t(t) < uint64_t(v) ? t : -1;
+    }
+    __device__ __forceinline__ int row_of(int t) const { return pieces == 1 ? t : rows > 1 ? int(__umulhi(uint32_t(t), reciprocal)) : 0; }
+};
+
+__device__ __forceinline__ int64_t block_number() { return int64_t(blockIdx.z) * kGridX + blockIdx.x; }
+
+// ---- the last position of every id
+
+__global__ void __launch_bounds__(kThreads) enter_kernel(const Rows a) {
+    const int64_t i = block_number() * kThreads + threadIdx.x;
+    if (i >= a.n) return;
+    const int64_t id = a.id(i);
+    if (id >= 0) a.last[id] = int32_t(i);  // of several any one
+}
+__global__ void __launch_bounds__(kThreads) raise_kernel(const Rows a) {
+    const int64_t i = block_number() * kThreads + threadIdx.x;
+    if (i >= a.n) return;
+    const int64_t id = a.id(i);
+    if (id >= 0 && a.last[id] < int32_t(i)) atomicMax(&a.last[id], int32_t(i));
+}
+
+// ---- writing
+
+// eight columns from c on, or as many as there are; the others are 0
+template <typename T> __device__ __forceinline__ void load8(const T *p, int have, float (&x)[8]) {
+    if (have == 8) {
+        constexpr int W = gnn_rows<T>::VEC;
+#pragma unroll
+        for (int k = 0; k < 8 / W; ++k) {
+            float t[W];
+            gnn_load_row<T, W, true>(p + k * W, t);
+#pragma unroll
+            for (int j = 0; j < W; ++j) x[k * W + j] = t[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = j < have ? gnn_rows<T>::get(p + j) : 0.0f;
+    }
+}
+
+template <typename T> __global__ void __launch_bounds__(kThreads) store_kernel(const Rows a) {
+    const int64_t row0 = block_number() * a.rows;
+    if (row0 >= a.n) return;
+    const int rows = a.n - row0 < a.rows ? int(a.n - row0) : a.rows;
+    __shared__ int64_t ids[kCompareRows];
+    __shared__ int again[kCompareRows];  // a later position has this row's id
+    if (a.compare) {
+        if (int(threadIdx.x) < rows) {
+            ids[threadIdx.x] = a.id(row0 + threadIdx.x);
+            again[threadIdx.x] = 0;
+        }
+        __syncthreads();
+        for (int64_t j = row0 + 1 + threadIdx.x; j < a.n; j += kThreads) {
+            const int64_t id = a.id(j);
+            for (int r = 0; r < rows; ++r)
+                if (id == ids[r] && j > row0 + r) again[r] = 1;
+        }
+        __syncthreads();
+    }
+    const int items = rows * a.pieces;
+    for (int t = int(threadIdx.x); t < items; t += kThreads) {  // (pieces is a multiple of four: the threads of a block take part together)
+        const int r = a.row_of(t), q = t - r * a.pieces, c = q * 8;
+        const int64_t i = row0 + r, id = a.id(i);
+        if (id < 0 || (a.compare ? again[r] != 0 : a.last && a.last[id] != int32_t(i))) continue;
+        const int left = a.f - c, have = left < 0 ? 0 : left < 8 ? left : 8;
+        float x[8];
+        load8<T>(static_cast<const T *>(a.x) + i * a.ldx + c, have, x);
+        uint32_t top = 0;
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t b = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+            const bool finite = b < 0x7F800000u;
+            odd |= !finite;
+            top = finite && b > top ? b : top;
+        }
+        const uint32_t other = __float_as_uint(gnn_from_lane<0xB1>(__uint_as_float(top)));  // the other of a pair
+        top = other > top ? other : top;
+        const uint32_t pair = __float_as_uint(gnn_from_lane<0x4E>(__uint_as_float(top)));   // the other pair of four
+        top = pair > top ? pair : top;
+        int e = int(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+        e = e > 0 ? e : 0;
+        const float factor = __uint_as_float(uint32_t(254 - e) << 23);
+        uint32_t w[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            int t4 = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k] * factor, x[4 * k + 1] * factor, 0, false);
+            w[k] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k + 2] * factor, x[4 * k + 3] * factor, t4, true));
+        }
+        if (odd)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if ((__float_as_uint(x[j]) & 0x7FFFFFFFu) >= 0x7F800000u) w[j / 4] |= 0x7Fu << (8 * (j % 4));
+        uint8_t *to = a.store + id * a.lds;
+        if (have == 8) {
+            *reinterpret_cast<u32x2_any *>(to + c) = u32x2_any{w[0], w[1]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < have) to[c + j] = uint8_t(w[j / 4] >> (8 * (j % 4)));
+        }
+        if ((q & 3) == 0) to[a.f + (q >> 2)] = uint8_t(e);
+    }
+}
+
+// ---- reading
+
+__device__ __forceinline__ float decoded(uint32_t w, int j, int e) {
+    float x;
+    if (j == 0) x = __builtin_amdgcn_cvt_f32_fp8(int(w), 0);
+    else if (j == 1) x = __builtin_amdgcn_cvt_f32_fp8(int(w), 1);
+    else if (j == 2) x = __builtin_amdgcn_cvt_f32_fp8(int(w), 2);
+    else x = __builtin_amdgcn_cvt_f32_fp8(int(w), 3);
+    return __builtin_amdgcn_ldexpf(x, e - 127);
+}
+
+// E columns a thread: eight, or one of rows narrower than that
+template <typename T, int E> __global__ void __launch_bounds__(kThreads) load_kernel(const Rows a) {
+    constexpr int U = 4;
+    const int64_t row0 = block_number() * a.rows;
+    if (row0 >= a.n) return;
+    const int rows = a.n - row0 < a.rows ? int(a.n - row0) : a.rows;
+    const int items = rows * a.pieces;
+    T *y = static_cast<T *>(a.x) + row0 * a.ldx;
+    for (int t0 = int(threadIdx.x); t0 < items; t0 += kThreads * U) {
+        int64_t id[U];
+        int row[U], col[U];
+        u32x2_any w[U];
+        uint8_t e[U][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int t = t0 + u * kThreads;
+            id[u] = -1;
+            row[u] = a.row_of(t);
+            const int c = (t - row[u] * a.pieces) * E;
+            col[u] = c < a.f - E ? c : a.f - E;  // the last piece ends with the row
+            if (t < items) id[u] = a.id(row0 + row[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (id[u] < 0) continue;
+            const uint8_t *p = a.store + id[u] * a.lds;
+            if constexpr (E == 8) w[u] = *reinterpret_cast<const u32x2_any *>(p + col[u]);
+            else w[u].x = p[col[u]];
+            e[u][0] = p[a.f + col[u] / kBlock];
+            e[u][1] = p[a.f + (col[u] + E - 1) / kBlock];  // of another block where the last piece reaches over its end
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (t0 + u * kThreads >= items) continue;
+            T *to = y + int64_t(row[u]) * a.ldx + col[u];
+            float x[E];
+            if (id[u] < 0) {
+#pragma unroll
+                for (int j = 0; j < E; ++j) x[j] = 0.0f;
+            } else {
+                const int first = kBlock - col[u] % kBlock;  // columns of the first block
+#pragma unroll
+                for (int j = 0; j < E; ++j) x[j] = decoded(j < 4 ? w[u].x : w[u].y, j % 4, j < first ? e[u][0] : e[u][1]);
+            }
+            if constexpr (E == 1) {
+                gnn_rows<T>::set(to, x[0]);
+            } else {
+                constexpr int W = gnn_rows<T>::VEC;
+#pragma unroll
+                for (int k = 0; k < E / W; ++k) {
+                    float v[W];
+#pragma unroll
+                    for (int j = 0; j < W; ++j) v[j] = x[k * W + j];
+                    gnn_store_row<T, W, true>(to + k * W, v);
+                }
+            }
+        }
+    }
+}
+
+dim3 grid_of(int64_t blocks) {
+    return blocks <= kGridX ? dim3(unsigned(blocks)) : dim3(kGridX, 1, unsigned((blocks + kGridX - 1) / kGridX));
+}
+
+bool misaligned(const void *p, int64_t to) { return reinterpret_cast<uintptr_t>(p) % uintptr_t(to) != 0; }
+int64_t used_bytes(int64_t F) { return F + (F + kBlock - 1) / kBlock; }
+
+int check(const void *x, const void *ids, const void *store, int64_t V, int64_t n, int64_t F, const gnn_store_opts &o) {
+    if (V < 0 || n < 0 || F < 0 || V > kMostRows || n > kMostRows || F > kMostColumns || (o.dtype != GNN_F32 && o.dtype != GNN_BF16)) return GNN_ERR_INVALID_ARG;
+    if ((o.ids_is_64 & ~1) || (o.unique & ~1) || (o.ldx && o.ldx < F) || (o.lds && o.lds < used_bytes(F))) return GNN_ERR_INVALID_ARG;
+    if (n == 0 || F == 0) return GNN_OK;
+    if (!x || (V > 0 && !store) || (!ids && n > V) || (V > 0 && x == store)) return GNN_ERR_INVALID_ARG;
+    if (misaligned(x, o.dtype == GNN_F32 ? 4 : 2) || misaligned(ids, o.ids_is_64 ? 8 : 4)) return GNN_ERR_INVALID_ARG;
+    return GNN_OK;
+}
+
+Rows rows_of(const void *x, const void *ids, const void *store, int64_t V, int64_t n, int64_t F, int64_t pieces, int64_t most, const gnn_store_opts &o) {
+    Rows a{};
+    a.ids = ids;
+    a.x = const_cast<void *>(x);
+    a.store = static_cast<uint8_t *>(const_cast<void *>(store));
+    a.v = V;
+    a.n = n;
+    a.ldx = o.ldx ? o.ldx : F;
+    a.lds = o.lds ? o.lds : gnn_store_row_bytes(F);
+    a.f = int32_t(F);
+    a.is_64 = o.ids_is_64;
+    a.pieces = int32_t(pieces);
+    a.rows = int32_t(pieces >= kItems ? 1 : kItems / pieces);
+    if (a.rows > most) a.rows = int32_t(most);
+    a.reciprocal = pieces > 1 ? uint32_t(((uint64_t(1) << 32) + uint64_t(pieces) - 1) / uint64_t(pieces)) : 0;
+    return a;
+}
+
+}  // namespace
+
+extern "C" GNN_API int64_t gnn_store_row_bytes(int64_t F) { return F <= 0 || F > kMostColumns ? 0 : (used_bytes(F) + 15) / 16 * 16; }
+
+extern "C" GNN_API int64_t gnn_store_rows_workspace_bytes(int64_t V, int64_t n) {
+    return V <= 0 || n <= kCompareHere || V > kMostRows || n > kMostRows ? 0 : 4 * V;
+}
+
+extern "C" GNN_API int gnn_store_rows(const void *X, const void *ids, void *store, int64_t V, int64_t n, int64_t F, const gnn_store_opts *opts) {
+    if (!opts) return GNN_ERR_INVALID_ARG;
+    const gnn_store_opts &o = *opts;
+    const int rc = check(X, ids, store, V, n, F, o);
+    if (rc != GNN_OK || n == 0 || F == 0 || V == 0) return rc;
+    const bool twice = ids && !o.unique;  // an id may come twice
+    const bool compare = twice && n <= kCompareHere;
+    if (twice && !compare && (!o.workspace || misaligned(o.workspace, 4) || o.workspace_bytes < 4 * V)) return GNN_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    Rows a = rows_of(X, ids, store, V, n, F, (F + kBlock - 1) / kBlock * (kBlock / 8), compare ? kCompareRows : kItems, o);
+    a.compare = compare;
+    hipStream_t stream = static_cast<hipStream_t>(o.stream);
+    if (twice && !compare) {
+        a.last = static_cast<int32_t *>(o.workspace);
+        const dim3 grid = grid_of((n + kThreads - 1) / kThreads);
+        enter_kernel<<<grid, kThreads, 0, stream>>>(a);
+        raise_kernel<<<grid, kThreads, 0, stream>>>(a);
+        GNN_HIP_TRY(hipGetLastError());
+    }
+    const dim3 grid = grid_of((n + a.rows - 1) / a.rows);
+    if (o.dtype == GNN_F32) store_kernel<float><<<grid, kThreads, 0, stream>>>(a);
+    else store_kernel<gnn_bf16><<<grid, kThreads, 0, stream>>>(a);
+    GNN_HIP_TRY(hipGetLastError());
+    return GNN_OK;
+}
+
+extern "C" GNN_API int gnn_load_rows(const void *store, const void *ids, void *Y, int64_t V, int64_t n, int64_t F, const gnn_store_opts *opts) {
+    if (!opts) return GNN_ERR_INVALID_ARG;
+    const gnn_store_opts &o = *opts;
+    const int rc = check(Y, ids, store, V, n, F, o);
+    if (rc != GNN_OK || n == 0 || F == 0) return rc;
+    (void)hipGetLastError();
+    const bool narrow = F < 8;
+    const Rows a = rows_of(Y, ids, store, V, n, F, narrow ? F : (F + 7) / 8, kItems, o);
+    hipStream_t stream = static_cast<hipStream_t>(o.stream);
+    const dim3 grid = grid_of((n + a.rows - 1) / a.rows);
+    if (o.dtype == GNN_F32) narrow ? load_kernel<float, 1><<<grid, kThreads, 0, stream>>>(a) : load_kernel<float, 8><<<grid, kThreads, 0, stream>>>(a);
+    else narrow ? load_kernel<gnn_bf16, 1><<<grid, kThreads, 0, stream>>>(a) : load_kernel<gnn_bf16, 8><<<grid, kThreads, 0, stream>>>(a);
+    GNN_HIP_TRY(hipGetLastError());
+    return GNN_OK;
+}

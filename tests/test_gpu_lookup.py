@@ -1,0 +1,230 @@
+"""Rows of a table by id, and the gradient of the table, against the formulas in 64 bits."""
+import pytest
+import torch
+
+import paper_2104_06700_amd as gnn
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8}  # half a step, relative
+# A sum: at most 64 terms one after the other in fp32 (63 roundings of sums that |x| bounds), the parts that are joined in fp64 rounded to fp32 on their way
+# through LDS, workgroups and the result (3), and the product with the scale (1).
+SUM = 70 * 2.0 ** -24
+
+
+def make_ids(n, v, kind, gen, dtype):
+    if kind == "uniform":
+        ids = torch.randint(0, max(v, 1), (n,), generator=gen)
+    elif kind == "hubs":
+        ids = (torch.rand(n, generator=gen, dtype=torch.float64) ** 4 * v).long().clamp(max=v - 1)
+    elif kind == "one":
+        ids = torch.full((n,), v // 2)
+    elif kind == "two":  # the first and the last row
+        ids = torch.where(torch.rand(n, generator=gen) < 0.5, 0, v - 1)
+    elif kind == "sorted":
+        ids = torch.arange(n) * max(v, 1) // max(n, 1)
+    elif kind == "none":
+        ids = torch.full((n,), -1)
+    else:  # some that name no row, on either side and beyond 32 bits
+        ids = torch.randint(-v, 2 * v, (n,), generator=gen)
+        if dtype == torch.int64:
+            ids[::7] += 1 << 32
+    return ids.to(dtype)
+
+
+def rows_of(gen, n, f, dtype, stride):
+    return torch.randn(n, stride, generator=gen).to(dtype).to(DEV)[:, :f]
+
+
+SHAPES = [  # v, n, f, ids
+    (1, 1, 1, "uniform"), (1, 300, 3, "uniform"), (5, 1, 4, "uniform"), (47, 1000, 7, "odd"), (300, 31, 8, "uniform"), (300, 33, 12, "sorted"),
+    (4096, 1021, 64, "uniform"), (4096, 257, 100, "hubs"), (257, 5000, 100, "hubs"), (2, 3000, 257, "two"), (1000, 2000, 602, "odd"), (7, 9000, 20, "one"),
+    (512, 512, 33, "none"), (100000, 3, 5, "uniform"), (33, 4000, 1030, "hubs")]
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, F32), (F32, BF16), (BF16, BF16)])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_rows_by_id(shape, types):
+    v, n, f, kind = shape
+    gen = torch.Generator().manual_seed(v + n + f)
+    ids = make_ids(n, v, kind, gen, torch.int64 if f % 2 else torch.int32)
+    table = rows_of(gen, v, f, types[0], f + (f % 3))
+    y = torch.full((n, f + 5), float("nan"), device=DEV, dtype=types[1])
+    scale = 0.3
+    gnn.gnn_lookup_fwd(table, ids.to(DEV), y[:, :f], scale=scale)
+    at = ids.long()
+    there = (at >= 0) & (at < v)
+    want = table.cpu().double()[at.clamp(0, v - 1)] * float(torch.tensor(scale)) * there[:, None]
+    got = y.cpu().double()
+    # the product is rounded to fp32, then to Y's type
+    assert ((got[:, :f] - want).abs() <= (2.0 ** -24 + HALF[types[1]]) * 1.01 * want.abs()).all()
+    assert torch.isnan(got[:, f:]).all()  # columns behind the row are left
+    assert not got[:, :f][~there].any()
+
+
+def reference(ids, dy, v, scale):
+    at = ids.long()
+    there = (at >= 0) & (at < v)
+    x = dy.cpu().double()[there]
+    zero = torch.zeros(v, dy.shape[1], dtype=torch.float64)
+    s = float(torch.tensor(scale))
+    return zero.index_add(0, at[there], x) * s, zero.index_add(0, at[there], x.abs()) * abs(s)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, F32), (F32, BF16), (BF16, BF16)])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_gradient_of_the_table(shape, types, accumulate):
+    v, n, f, kind = shape
+    gen = torch.Generator().manual_seed(v + n + f)
+    ids = make_ids(n, v, kind, gen, torch.int64 if f % 2 else torch.int32)
+    dy = rows_of(gen, n, f, types[1], f + (f % 3))
+    start = torch.randn(v, f, generator=gen).to(types[0]).to(DEV)
+    dt = torch.full((v, f + 5), float("nan"), device=DEV, dtype=types[0])
+    if accumulate:
+        dt[:, :f] = start
+    ws = torch.empty(gnn.gnn_lookup_workspace_bytes(v, n, f), device=DEV, dtype=torch.uint8)
+    gnn.gnn_lookup_bwd(ids.to(DEV), dy, dt[:, :f], scale=-0.7, accumulate=accumulate, workspace=ws)
+    want, size = reference(ids, dy, v, -0.7)
+    if accumulate:
+        want = want + start.cpu().double()
+    got = dt.cpu().double()
+    # with accumulate the sum is rounded to fp32 before it is to the table's type
+    bound = SUM * size + (HALF[types[0]] + (2.0 ** -24 if accumulate else 0)) * 1.01 * want.abs()
+    assert ((got[:, :f] - want).abs() <= bound + SUM * HALF[types[0]] * size).all()
+    assert torch.isnan(got[:, f:]).all()
+    untouched = size.sum(1) == 0
+    if accumulate:
+        assert torch.equal(dt[:, :f].cpu()[untouched], start.cpu()[untouched])
+    else:
+        assert not got[:, :f][untouched].any()
+    again = dt.clone()
+    if accumulate:
+        again[:, :f] = start
+    gnn.gnn_lookup_bwd(ids.to(DEV), dy, again[:, :f], scale=-0.7, accumulate=accumulate, workspace=ws)
+    assert torch.equal(again[:, :f], dt[:, :f])  # reproducible to the bit
+
+
+@pytest.mark.parametrize("n", [31, 32, 33, 63, 64, 65, 255, 256, 257, 511, 512, 513, 4095, 4096, 4097, 8193, 70000])
+@pytest.mark.parametrize("f", [64, 256])
+def test_sums_that_end_where_runs_and_workgroups_end(n, f):
+    """Ids in long stretches whose ends lie at and beside the ends of runs of 32 positions and of workgroups' positions."""
+    gen = torch.Generator().manual_seed(n)
+    cuts = sorted({c for c in (1, 31, 32, 33, 64, 127, 128, 129, 256, 384, 512, 1024, 2049, 4096, 8192, 40000) if c < n})
+    ids = torch.zeros(n, dtype=torch.int64)
+    for c in cuts:
+        ids[c:] += 1
+    dy = torch.randn(n, f, generator=gen).to(DEV)
+    v = len(cuts) + 1
+    order = torch.randperm(n, generator=gen)
+    for perm in (torch.arange(n), order):
+        dt = torch.empty(v, f, device=DEV)
+        ws = torch.empty(gnn.gnn_lookup_workspace_bytes(v, n, f), device=DEV, dtype=torch.uint8)
+        gnn.gnn_lookup_bwd(ids[perm].to(DEV), dy, dt, workspace=ws)
+        want, size = reference(ids[perm], dy, v, 1.0)
+        assert ((dt.cpu().double() - want).abs() <= SUM * size + 2.0 ** -24 * want.abs()).all()
+
+
+def test_what_names_no_row_is_not_read():
+    """NaN and infinities in rows whose id names none, and in rows of the table that no id names."""
+    ids = torch.tensor([0, -1, 2, 5, 2], dtype=torch.int32, device=DEV)
+    dy = torch.ones(5, 8, device=DEV)
+    dy[1], dy[3] = float("nan"), float("inf")
+    dt = torch.empty(4, 8, device=DEV)
+    ws = torch.empty(gnn.gnn_lookup_workspace_bytes(4, 5, 8), device=DEV, dtype=torch.uint8)
+    gnn.gnn_lookup_bwd(ids, dy, dt, workspace=ws)
+    assert dt[:, 0].tolist() == [1.0, 0.0, 2.0, 0.0]
+    table = torch.ones(4, 8, device=DEV)
+    table[1] = float("nan")
+    y = torch.empty(5, 8, device=DEV)
+    gnn.gnn_lookup_fwd(table, ids, y, scale=2.0)
+    assert y[:, 0].tolist() == [2.0, 0.0, 2.0, 0.0, 2.0]
+    # accumulate does not touch a row that no id names, NaN or not
+    dt = torch.full((4, 8), float("nan"), device=DEV)
+    dt[0] = dt[2] = 1.0
+    gnn.gnn_lookup_bwd(ids, dy, dt, accumulate=True, workspace=ws)
+    assert dt[0, 0] == 2.0 and dt[2, 7] == 3.0 and torch.isnan(dt[1]).all() and torch.isnan(dt[3]).all()
+
+
+def test_empty_calls():
+    table, none = torch.ones(4, 8, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV)
+    gnn.gnn_lookup_fwd(table, none, torch.empty(0, 8, device=DEV))
+    dt = torch.ones(300, 8, device=DEV)
+    gnn.gnn_lookup_bwd(none, torch.empty(0, 8, device=DEV), dt, accumulate=True)
+    assert (dt == 1).all()
+    gnn.gnn_lookup_bwd(none, torch.empty(0, 8, device=DEV), dt)
+    assert (dt == 0).all()
+    y = torch.ones(3, 8, device=DEV)
+    gnn.gnn_lookup_fwd(torch.empty(0, 8, device=DEV), torch.zeros(3, dtype=torch.int64, device=DEV), y)
+    assert (y == 0).all()
+
+
+def test_gradient_against_differences():
+    """The gradient is that of sum dY Y: a step of one entry of the table changes it by the step times the gradient."""
+    gen = torch.Generator().manual_seed(5)
+    ids = torch.randint(0, 9, (40,), generator=gen).to(DEV)
+    table, dy = torch.randn(9, 6, generator=gen).to(DEV), torch.randn(40, 6, generator=gen).to(DEV)
+    dt = torch.empty(9, 6, device=DEV)
+    ws = torch.empty(gnn.gnn_lookup_workspace_bytes(9, 40, 6), device=DEV, dtype=torch.uint8)
+    gnn.gnn_lookup_bwd(ids, dy, dt, scale=0.5, workspace=ws)
+
+    def value(t):
+        y = torch.empty(40, 6, device=DEV)
+        gnn.gnn_lookup_fwd(t, ids, y, scale=0.5)
+        return float((y.double() * dy.double()).sum())
+    for r, c in ((0, 0), (3, 5), (8, 2)):
+        up, down = table.clone(), table.clone()
+        up[r, c] += 1.0
+        down[r, c] -= 1.0
+        # linear: but for the rounding of 2 x 40 products of numbers below 8
+        assert abs((value(up) - value(down)) / 2 - float(dt[r, c])) <= 80 * 8 * 8 * 2.0 ** -24
+
+
+def test_other_streams_and_replays():
+    gen = torch.Generator().manual_seed(3)
+    v, n, f = 700, 5000, 100
+    ids = make_ids(n, v, "hubs", gen, torch.int32).to(DEV)
+    table, dy = torch.randn(v, f, generator=gen).to(DEV), torch.randn(n, f, generator=gen).to(DEV)
+    y, dt = torch.empty(n, f, device=DEV), torch.empty(v, f, device=DEV)
+    ws = torch.empty(gnn.gnn_lookup_workspace_bytes(v, n, f), device=DEV, dtype=torch.uint8)
+
+    def both(stream=None):
+        gnn.gnn_lookup_fwd(table, ids, y, scale=0.5, stream=stream)
+        gnn.gnn_lookup_bwd(ids, dy, dt, scale=0.5, workspace=ws, stream=stream)
+    both()
+    torch.cuda.synchronize()
+    want = y.clone(), dt.clone()
+    side = torch.cuda.Stream()
+    y.fill_(float("nan")), dt.fill_(float("nan"))
+    side.wait_stream(torch.cuda.current_stream())
+    both(side)
+    side.synchronize()
+    assert torch.equal(y, want[0]) and torch.equal(dt, want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for k in range(3):  # with other ids in each replay
+        ids.copy_(make_ids(n, v, "hubs" if k < 2 else "odd", gen, torch.int32))
+        y.fill_(float("nan")), dt.fill_(float("nan")), ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone(), dt.clone()
+        both()
+        torch.cuda.synchronize()
+        assert torch.equal(y, got[0]) and torch.equal(dt, got[1])
+
+
+def test_a_table_beyond_32_bits_of_offsets():
+    v, f = (1 << 32) // 512 + 1000, 512  # 4.3e9 elements of bf16
+    table = torch.zeros(v, f, device=DEV, dtype=BF16)
+    ids = torch.tensor([0, v - 1, v // 2, v - 1000], device=DEV)
+    table[ids] = torch.arange(1, 5, device=DEV, dtype=BF16)[:, None]
+    y = torch.empty(4, f, device=DEV)
+    gnn.gnn_lookup_fwd(table, ids, y)
+    assert torch.equal(y, torch.arange(1, 5, device=DEV)[:, None].expand(4, f).float())
+    ws = torch.empty(gnn.gnn_lookup_workspace_bytes(v, 4, f), device=DEV, dtype=torch.uint8)
+    gnn.gnn_lookup_bwd(ids, y, table, scale=2.0, workspace=ws)
+    assert torch.equal(table[ids], 2 * y.to(BF16))
+    assert float(table[1:v // 2].float().abs().amax()) == 0.0 and float(table[v // 2 + 1:v - 1000].float().abs().amax()) == 0.0
