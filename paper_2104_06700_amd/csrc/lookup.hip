@@ -17,8 +17,12 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kAtOnce = 4;        // vectors of a thread on their way, forward
-constexpr int kRun = 32;          // sorted positions of a group of lanes: terms added one after the other in fp32
-constexpr int kBatch = 8;         // of them on their way at once
+// Sorted positions of a group of lanes, which are terms added one after the other in fp32: many where there are enough groups, else as many as are on
+// their way at once.
+constexpr int kRun = 32, kBatch = 8;
+constexpr int64_t kLong = 1 << 17; // positions from which on runs are long
+constexpr int64_t kRankHere = 4096; // positions up to which every workgroup finds the places of its ones among all
+constexpr int kRankRows = 32;     // of a workgroup then
 constexpr int kZeroRows = 256;    // rows of a workgroup that zeroes
 constexpr int64_t kMostRows = INT32_MAX, kMostColumns = 1 << 24;
 constexpr unsigned kGridX = 1 << 20;  // workgroups in x: a launch has fewer than 2^32 threads a dimension
@@ -84,33 +88,28 @@ template <typename TT, typename TY, int E> __global__ void __launch_bounds__(kTh
     const TT *table = static_cast<const TT *>(a.table);
     TY *y = static_cast<TY *>(a.y) + row0 * a.ldy;
     for (int t0 = int(threadIdx.x); t0 < items; t0 += kThreads * kAtOnce) {
+        // no branch between the loads: what lies behind the end repeats the last vector, and an id that names no row reads row 0
         Vector<TT, E> v[kAtOnce];
         int64_t id[kAtOnce];
         int row[kAtOnce], col[kAtOnce];
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-            const int t = t0 + u * kThreads;
-            id[u] = -1;
+            const int t = t0 + u * kThreads < items ? t0 + u * kThreads : items - 1;
             row[u] = a.vectors == 1 ? t : a.rows > 1 ? int(__umulhi(uint32_t(t), a.reciprocal)) : 0;
             const int c = (t - row[u] * a.vectors) * E;
             col[u] = c < a.f - E ? c : a.f - E;  // the last vector ends with the row
-            if (t < items) id[u] = a.ids.at(row0 + row[u]);
+            id[u] = a.ids.at(row0 + row[u]);
         }
+        if (a.ids.rows > 0)
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u)
-            if (id[u] >= 0) v[u].load(table + id[u] * a.ldt + col[u]);
+            for (int u = 0; u < kAtOnce; ++u) v[u].load(table + (id[u] < 0 ? 0 : id[u]) * a.ldt + col[u]);
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-            if (t0 + u * kThreads >= items) continue;
+            if (t0 + u * kThreads >= items) break;
             float x[E];
-            if (id[u] >= 0) {
-                v[u].get(x);
+            v[u].get(x);
 #pragma unroll
-                for (int j = 0; j < E; ++j) x[j] *= a.scale;
-            } else {
-#pragma unroll
-                for (int j = 0; j < E; ++j) x[j] = 0.0f;
-            }
+            for (int j = 0; j < E; ++j) x[j] = id[u] < 0 ? 0.0f : x[j] * a.scale;
             store_vector<TY, E, true>(y + int64_t(row[u]) * a.ldy + col[u], x);
         }
     }
@@ -125,7 +124,7 @@ struct Grad {
     float *head, *tail;           // [blocks][f] what a workgroup has of the sum that began before it, and of the one that goes on behind it
     uint32_t *flags;              // [blocks]
     int64_t rows, n, ldt, ldy, sum_blocks, zero_blocks;
-    int32_t f, vectors, lanes_log2;
+    int32_t f, vectors, lanes_log2, run;
     int32_t accumulate;
     float scale;
 };
@@ -136,6 +135,36 @@ __global__ void __launch_bounds__(kThreads) key_kernel(const Ids ids, int64_t n,
     if (i >= n) return;
     const int64_t v = ids.at(i);
     key[i] = uint32_t(v < 0 ? ids.rows : v);
+}
+
+// Few positions: the place of each is the number of those that come before it.
+__global__ void __launch_bounds__(kThreads) rank_kernel(const Ids ids, int n, uint32_t *__restrict__ key, uint32_t *__restrict__ order) {
+    __shared__ __attribute__((aligned(16))) uint32_t all[kRankHere];
+    __shared__ int before[kThreads];
+    for (int j = int(threadIdx.x); j < (n + 3) / 4 * 4; j += kThreads) {
+        const int64_t v = j < n ? ids.at(j) : int64_t(UINT32_MAX);  // behind the last: after all others
+        all[j] = uint32_t(v < 0 ? ids.rows : v);
+    }
+    __syncthreads();
+    // a thread a position and an eighth of the others, four at a time
+    const int i = int(blockIdx.x) * kRankRows + int(threadIdx.x) % kRankRows;
+    int count = 0;
+    if (i < n) {
+        const uint32_t k = all[i];
+        for (int j = int(threadIdx.x) / kRankRows * 4; j < n; j += kThreads / kRankRows * 4) {
+            const uint4 t = *reinterpret_cast<const uint4 *>(all + j);
+            count += int(t.x < k || (t.x == k && j < i)) + int(t.y < k || (t.y == k && j + 1 < i)) + int(t.z < k || (t.z == k && j + 2 < i)) +
+                     int(t.w < k || (t.w == k && j + 3 < i));
+        }
+    }
+    before[threadIdx.x] = count;
+    __syncthreads();
+    if (int(threadIdx.x) >= kRankRows || i >= n) return;
+    int place = 0;
+#pragma unroll
+    for (int p = 0; p < kThreads / kRankRows; ++p) place += before[p * kRankRows + threadIdx.x];
+    key[place] = all[i];
+    order[place] = uint32_t(i);
 }
 
 // first position of key[0 .. n) that is not below v
@@ -203,9 +232,12 @@ template <typename TT, int E> __device__ __forceinline__ void zero_rows(const Gr
 }
 
 template <typename TY, typename TT, int E> __global__ void __launch_bounds__(kThreads) grad_kernel(const Grad a) {
-    const int64_t block = block_number();
-    if (block >= a.sum_blocks) {
-        if (block < a.sum_blocks + a.zero_blocks && blockIdx.y == 0) zero_rows<TT, E>(a, block - a.sum_blocks);
+    // the workgroups that zero lie between those that add up, so that writes and reads go on beside each other
+    const int64_t number = block_number(), all = a.sum_blocks + a.zero_blocks;
+    if (number >= all) return;
+    const int64_t block = number * a.sum_blocks / all;
+    if ((number + 1) * a.sum_blocks / all == block) {
+        if (blockIdx.y == 0) zero_rows<TT, E>(a, number - block);
         return;
     }
     __shared__ float parts[2][kThreads][E];  // what a group has of the sums that cross its ends
@@ -216,7 +248,7 @@ template <typename TY, typename TT, int E> __global__ void __launch_bounds__(kTh
     const int c = !mine ? 0 : q * E < a.f - E ? q * E : a.f - E;
     const int own = q * E < a.f - E ? E : a.f - q * E;
     const uint32_t none = uint32_t(a.rows);
-    const int64_t j0 = (block * groups + group) * kRun;
+    const int64_t j0 = (block * groups + group) * a.run;
     const TY *dy = static_cast<const TY *>(a.dy) + c;
 
     float sum[E];
@@ -228,20 +260,24 @@ template <typename TY, typename TT, int E> __global__ void __launch_bounds__(kTh
         id = a.key[j0];
         first = j0 > 0 && id != none && a.key[j0 - 1] == id;
         if (first) my_flags = kHead;
-        const int64_t end = j0 + kRun < a.n ? j0 + kRun : a.n;
+        const int64_t end = j0 + a.run < a.n ? j0 + a.run : a.n;
 #pragma unroll 1
         for (int64_t j = j0; j < end; j += kBatch) {
-            uint32_t k[kBatch];
+            // no branch between the loads: what lies behind the end repeats the last position, and ids that name no row are read as well
+            uint32_t k[kBatch], from[kBatch];
             Vector<TY, E> v[kBatch];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
-                k[u] = j + u < end ? a.key[j + u] : none;
-                if (k[u] != none && mine) v[u].load(dy + int64_t(a.order[j + u]) * a.ldy);
+                const int64_t at = j + u < end ? j + u : end - 1;
+                k[u] = a.key[at];
+                from[u] = a.order[at];
             }
 #pragma unroll
+            for (int u = 0; u < kBatch; ++u) v[u].load(dy + int64_t(from[u]) * a.ldy);
+#pragma unroll
             for (int u = 0; u < kBatch; ++u) {
+                if (j + u >= end) break;
                 if (k[u] != id) {
-                    if (j + u >= end) break;
                     if (first) {
 #pragma unroll
                         for (int i = 0; i < E; ++i) parts[0][threadIdx.x][i] = sum[i];
@@ -253,12 +289,10 @@ template <typename TY, typename TT, int E> __global__ void __launch_bounds__(kTh
 #pragma unroll
                     for (int i = 0; i < E; ++i) sum[i] = 0.0f;
                 }
-                if (k[u] != none && mine) {
-                    float x[E];
-                    v[u].get(x);
+                float x[E];
+                v[u].get(x);
 #pragma unroll
-                    for (int i = 0; i < E; ++i) sum[i] += x[i];
-                }
+                for (int i = 0; i < E; ++i) sum[i] += x[i];  // (of ids that name no row: a sum that goes nowhere)
             }
         }
         const bool goes_on = id != none && end < a.n && a.key[end] == id;
@@ -327,7 +361,7 @@ template <typename TT, int E> __global__ void __launch_bounds__(kThreads) join_k
     __shared__ double parts[kThreads][E];
     __shared__ int last;
     const int lanes = 1 << a.lanes_log2, lane = int(threadIdx.x) & (lanes - 1), group = int(threadIdx.x) >> a.lanes_log2, groups = kThreads >> a.lanes_log2;
-    const int64_t chunk = int64_t(groups) * kRun;
+    const int64_t chunk = int64_t(groups) * a.run;
     // how many workgroups behind it have parts: up to the first that has more than the middle
     int64_t more = 1;
     if (a.flags[block + 1] & kThrough) {
@@ -394,7 +428,7 @@ bool misaligned(const void *p, int64_t to) { return reinterpret_cast<uintptr_t>(
 int elements_of(bool eight, int64_t f) { return f >= (eight ? 8 : 4) ? (eight ? 8 : 4) : 1; }
 
 struct Room {  // of the gradient, in words
-    int lanes_log2;
+    int lanes_log2, run;
     int64_t vectors, chunk, blocks, table, sums, words;
 };
 Room room_of(int64_t V, int64_t n, int64_t F, bool eight) {
@@ -402,7 +436,8 @@ Room room_of(int64_t V, int64_t n, int64_t F, bool eight) {
     const int e = elements_of(eight, F);
     r.vectors = (F + e - 1) / e;
     r.lanes_log2 = r.vectors >= 64 ? 6 : gnn_ilog2_ceil(r.vectors);
-    r.chunk = int64_t(kThreads >> r.lanes_log2) * kRun;
+    r.run = n >= kLong ? kRun : kBatch;
+    r.chunk = int64_t(kThreads >> r.lanes_log2) * r.run;
     r.blocks = (n + r.chunk - 1) / r.chunk;
     r.table = gnn_sort_table_elems(n);
     r.sums = gnn_sort_sums_elems(n);
@@ -497,6 +532,7 @@ extern "C" GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dta
     a.f = int32_t(F);
     a.vectors = int32_t(r.vectors);
     a.lanes_log2 = r.lanes_log2;
+    a.run = r.run;
     a.accumulate = o.accumulate;
     a.scale = o.scale;
     a.sum_blocks = r.blocks;
@@ -511,13 +547,21 @@ extern "C" GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dta
         next += r.blocks;
         uint32_t *buf_k[2] = {next, next + n}, *buf_v[2] = {next + 2 * n, next + 3 * n};
         next += 4 * n;
-        key_kernel<<<grid_of((n + kThreads - 1) / kThreads), kThreads, 0, stream>>>(Ids{ids, o.ids_is_64, V}, n, buf_k[0]);
-        GNN_HIP_TRY(hipGetLastError());
-        uint32_t *keys = nullptr, *order = nullptr;
-        const int sorted = gnn_radix_sort_positions(buf_k, buf_v, n, gnn_ilog2_ceil(V + 1), next, next + r.table, stream, &keys, &order);
-        if (sorted != GNN_OK) return sorted;
-        a.key = keys;
-        a.order = order;
+        const Ids named{ids, o.ids_is_64, V};
+        if (n <= kRankHere) {
+            rank_kernel<<<unsigned((n + kRankRows - 1) / kRankRows), kThreads, 0, stream>>>(named, int(n), buf_k[0], buf_v[0]);
+            GNN_HIP_TRY(hipGetLastError());
+            a.key = buf_k[0];
+            a.order = buf_v[0];
+        } else {
+            key_kernel<<<grid_of((n + kThreads - 1) / kThreads), kThreads, 0, stream>>>(named, n, buf_k[0]);
+            GNN_HIP_TRY(hipGetLastError());
+            uint32_t *keys = nullptr, *order = nullptr;
+            const int sorted = gnn_radix_sort_positions(buf_k, buf_v, n, gnn_ilog2_ceil(V + 1), next, next + r.table, stream, &keys, &order);
+            if (sorted != GNN_OK) return sorted;
+            a.key = keys;
+            a.order = order;
+        }
     }
     const int64_t slices = (r.vectors + (int64_t(1) << r.lanes_log2) - 1) >> r.lanes_log2;
     if (slices > 65535) return GNN_ERR_UNSUPPORTED;

@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMats = 16;               // of a launch
-constexpr int kNormBlocks = 256;        // partial sums of squares of a matrix, at most
+constexpr int kNormBlocks = 1024;       // partial sums of squares of a matrix, at most
 constexpr int kNormChunk = 4096;        // elements of a workgroup, at least
 constexpr int64_t kMostSide = 65536, kMostSteps = 100;
 
@@ -45,14 +45,14 @@ struct Mat {
     int32_t rows, cols;                 // of U
     int32_t norm_blocks, flags;         // kBf16, kTall
     float decay, rate;                  // 1 - lr weight_decay; lr update_scale
-    int32_t first[4];                   // workgroup that begins it: of the norms, the first planes, symmetric products, others
 };
 enum { kBf16 = 1, kTall = 2 };          // tall: rows > cols
 enum Phase { kGram, kPolynomial, kUpdate, kLast };
+enum Launch { kNorms, kPlanes, kSymmetric, kOthers, kLaunches };
 
 struct Job {
     Mat mat[kMats];
-    int32_t count;
+    int32_t first[kLaunches][kMats];    // workgroup that begins a matrix; INT32_MAX behind the last
     int32_t muon, nesterov;
     float mu, a, b, c;
     double eps;
@@ -60,11 +60,12 @@ struct Job {
 };
 static_assert(sizeof(Job) <= 4096, "kernel arguments");
 
-// the last matrix that begins at this workgroup or before
-__device__ __forceinline__ int matrix_of_block(const Job &j, int which) {
-    int k = 0;
-    for (int i = 1; i < j.count; ++i)
-        if (j.mat[i].first[which] <= int(blockIdx.x)) k = i;
+// the last matrix that begins at this workgroup or before, and the workgroup's number in it
+template <Launch L> __device__ __forceinline__ int matrix_of_block(const Job &j, int &number) {
+    int k = -1;
+#pragma unroll
+    for (int i = 0; i < kMats; ++i) k += j.first[L][i] <= int(blockIdx.x) ? 1 : 0;
+    number = int(blockIdx.x) - j.first[L][k];
     return k;
 }
 
@@ -74,26 +75,55 @@ __device__ __forceinline__ float element(const void *p, int64_t i, bool bf16) {
 
 // ---- the update and its norm
 
+// elements i .. i + 3
+__device__ __forceinline__ void four(const void *p, int64_t i, bool bf16, float (&v)[4]) {
+    if (bf16) gnn_load_row<gnn_bf16, 4>(static_cast<const gnn_bf16 *>(p) + i, v);
+    else gnn_load_row<float, 4>(static_cast<const float *>(p) + i, v);
+}
+
 // The sums of squares are fp64: squares of fp32 numbers neither overflow nor vanish there.
 __global__ void __launch_bounds__(kThreads) norm_kernel(const Job j) {
-    const Mat &t = j.mat[matrix_of_block(j, 0)];
-    const int part = int(blockIdx.x) - t.first[0];
-    const int64_t total = int64_t(t.rows) * t.cols;
-    const int64_t per = (total + t.norm_blocks - 1) / t.norm_blocks, begin = part * per, end = begin + per < total ? begin + per : total;
+    int part;
+    const Mat &t = j.mat[matrix_of_block<kNorms>(j, part)];
     const bool bf16 = t.flags & kBf16;
-    const float gs = j.grad_scale ? *j.grad_scale : 1.0f;
     double s = 0.0;
-    for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) {
-        float u;
-        if (j.muon) {
-            const float g = element(t.in, i, bf16) * gs;
-            const float mo = j.mu * t.momentum[i] + g;
-            t.momentum[i] = mo;
-            u = j.nesterov ? g + j.mu * mo : mo;
-        } else {
-            u = element(t.in, t.ld_in == t.cols ? i : i / t.cols * t.ld_in + i % t.cols, bf16);
+    if (t.ld_in == t.cols) {
+        const int64_t total = int64_t(t.rows) * t.cols;
+        const int64_t per = ((total + t.norm_blocks - 1) / t.norm_blocks + 3) / 4 * 4, begin = part * per, end = begin + per < total ? begin + per : total;
+        const float gs = j.grad_scale ? *j.grad_scale : 1.0f;
+        for (int64_t i = begin + 4 * int(threadIdx.x); i < end; i += 4 * kThreads) {
+            float u[4] = {0.0f, 0.0f, 0.0f, 0.0f}, m[4];
+            const int have = end - i < 4 ? int(end - i) : 4;
+            if (have == 4) {
+                four(t.in, i, bf16, u);
+                if (j.muon) four(t.momentum, i, false, m);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < have) {
+                        u[e] = element(t.in, i + e, bf16);
+                        if (j.muon) m[e] = t.momentum[i + e];
+                    }
+            }
+            if (j.muon) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float g = u[e] * gs;
+                    m[e] = j.mu * m[e] + g;
+                    u[e] = e < have ? (j.nesterov ? g + j.mu * m[e] : m[e]) : 0.0f;
+                    if (have < 4 && e < have) t.momentum[i + e] = m[e];
+                }
+                if (have == 4) gnn_store_row<float, 4>(t.momentum + i, m);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s += double(u[e]) * double(u[e]);
         }
-        s += double(u) * double(u);
+    } else {
+        for (int r = part; r < t.rows; r += t.norm_blocks)
+            for (int c = int(threadIdx.x); c < t.cols; c += kThreads) {
+                const float u = element(t.in, r * t.ld_in + c, bf16);
+                s += double(u) * double(u);
+            }
     }
     __shared__ double sums[kThreads / 64];
 #pragma unroll
@@ -131,6 +161,20 @@ template <int P> __device__ __forceinline__ void put4(uint16_t *planes, int rows
     for (int q = 0; q < P; ++q)
         *reinterpret_cast<uint2 *>(p + int64_t(q) * rows * depth) = make_uint2(bf16_pair(part[0][q], part[1][q]), bf16_pair(part[2][q], part[3][q]));
 }
+// eight, the first a multiple of eight
+template <int P> __device__ __forceinline__ void put8(uint16_t *planes, int rows, int depth, int row, int k, const float (&v)[8]) {
+    uint16_t *p = planes + place(depth, row, k);
+    float part[8][P];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) split<P>(v[i], part[i]);
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = bf16_pair(part[2 * i][q], part[2 * i + 1][q]);
+        *reinterpret_cast<u32x4 *>(p + int64_t(q) * rows * depth) = w;
+    }
+}
 template <int P> __device__ __forceinline__ void get4(const uint16_t *planes, int rows, int depth, int row, int k, float (&v)[4]) {
     const uint16_t *p = planes + place(depth, row, k);
 #pragma unroll
@@ -147,10 +191,11 @@ template <int P> __device__ __forceinline__ void get4(const uint16_t *planes, in
 
 // X and X^T from U: a workgroup has a tile of 64 x 64 of U.
 template <int P> __global__ void __launch_bounds__(kThreads) planes_kernel(const Job j) {
-    const Mat &t = j.mat[matrix_of_block(j, 1)];
+    int tile;
+    const Mat &t = j.mat[matrix_of_block<kPlanes>(j, tile)];
     const bool tall = t.flags & kTall, bf16 = t.flags & kBf16;
     const int rp = tall ? t.np : t.mp, cp = tall ? t.mp : t.np;  // filled up sides of U
-    const int tiles = cp / 64, tile = int(blockIdx.x) - t.first[1];
+    const int tiles = cp / 64;
     const int r0 = tile / tiles * 64, c0 = tile % tiles * 64;
     __shared__ float u[64][65];
     __shared__ double sums[kThreads / 64];
@@ -181,12 +226,15 @@ template <int P> __global__ void __launch_bounds__(kThreads) planes_kernel(const
     }
     __syncthreads();
     uint16_t *by_row = tall ? t.xt[0] : t.x, *by_col = tall ? t.x : t.xt[0];  // rows of U as rows; columns of U as rows
-    for (int i = int(threadIdx.x); i < 64 * 16; i += kThreads) {
-        const int r = i & 63, k = (i >> 6) * 4;
-        const float v[4] = {u[r][k], u[r][k + 1], u[r][k + 2], u[r][k + 3]};
-        put4<P>(by_row, rp, cp, r0 + r, c0 + k, v);
-        const float w[4] = {u[k][r], u[k + 1][r], u[k + 2][r], u[k + 3][r]};
-        put4<P>(by_col, cp, rp, c0 + r, r0 + k, w);
+    for (int i = int(threadIdx.x); i < 64 * 8; i += kThreads) {
+        const int r = i & 63, k = (i >> 6) * 8;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = u[r][k + e];
+        put8<P>(by_row, rp, cp, r0 + r, c0 + k, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = u[k + e][r];
+        put8<P>(by_col, cp, rp, c0 + r, r0 + k, v);
     }
 }
 
@@ -203,24 +251,39 @@ template <Phase phase> __device__ __forceinline__ Operands operands(const Mat &t
     else return {t.q, t.xt[step & 1], t.mp, t.np, t.mp};
 }
 
-// the tile of a workgroup; of symmetric results those on and below the diagonal
-__device__ __forceinline__ void tile_of(int number, bool symmetric, int tiles_across, int &ti, int &tj) {
-    if (!symmetric) {
+// The tile of a workgroup; of symmetric results those on and below the diagonal, where a tile is as wide as one or two are high.
+template <bool SYMMETRIC, int WIDE> __device__ __forceinline__ void tile_of(int number, int tiles_across, int &ti, int &tj) {
+    if constexpr (!SYMMETRIC) {
         ti = number / tiles_across;
         tj = number - ti * tiles_across;
-        return;
+    } else {  // rows i * WIDE .. i * WIDE + WIDE - 1 have i + 1 tiles each
+        auto before = [](int i) { return WIDE * (i * (i + 1) / 2); };
+        int i = int((sqrtf(8.0f / WIDE * float(number) + 1.0f) - 1.0f) * 0.5f);
+        while (before(i) > number) --i;
+        while (before(i + 1) <= number) ++i;
+        const int rest = number - before(i);
+        ti = i * WIDE + rest / (i + 1);
+        tj = rest % (i + 1);
     }
-    ti = int((sqrtf(8.0f * float(number) + 1.0f) - 1.0f) * 0.5f);
-    while (ti * (ti + 1) / 2 > number) --ti;
-    while ((ti + 1) * (ti + 2) / 2 <= number) ++ti;
-    tj = number - ti * (ti + 1) / 2;
 }
 
-template <int P> __device__ __forceinline__ void products(float16v &sum, const bf16x8 (&a)[P], const bf16x8 (&b)[P]) {
+// The sums of the products of parts that matter.  P = 3: from zero, smallest first, and then added with one rounding; P = 2, whose operands are off by
+// more than what the matrix cores cut off, in one chain.
+template <int P> __device__ __forceinline__ void add_products(float16v &acc, const bf16x8 (&a)[P], const bf16x8 (&b)[P]) {
+    float16v sum = acc;
+    if constexpr (P == 3)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sum[v] = 0.0f;
 #pragma unroll
     for (int s = P - 1; s >= 0; --s)
 #pragma unroll
         for (int p = 0; p <= s; ++p) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[p], b[s - p], sum, 0, 0, 0);
+    if constexpr (P == 3) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[v] += sum[v];
+    } else {
+        acc = sum;
+    }
 }
 
 // What a phase makes of four sums, rows row_i .. row_i + 3 of column row_c, or the same columns of that row: A is symmetric.
@@ -267,138 +330,160 @@ template <int P, Phase phase> __device__ __forceinline__ void write_across(const
     }
 }
 
-// Tiles of 32 x 32, the four wavefronts have every fourth 16 of k.
-template <int P, Phase phase> __global__ void __launch_bounds__(kThreads) small_product_kernel(const Job j, int step) {
+// Tiles of (32 T)^2: each of four wavefronts has all of the tile and every fourth 16 of k, straight from the caches, and keeps SETS steps on their way.
+// Nothing waits but for its own loads; the four sums are added in LDS.
+template <int P, Phase phase, int T> __global__ void __launch_bounds__(kThreads) split_product_kernel(const Job j, int step) {
     constexpr bool symmetric = phase == kGram || phase == kPolynomial;
-    const Mat &t = j.mat[matrix_of_block(j, symmetric ? 2 : 3)];
+    constexpr int SETS = T == 1 ? 4 : 2;
+    int number, ti, tj;
+    const Mat &t = j.mat[matrix_of_block<symmetric ? kSymmetric : kOthers>(j, number)];
     const Operands o = operands<phase>(t, step);
-    int ti, tj;
-    tile_of(int(blockIdx.x) - t.first[symmetric ? 2 : 3], symmetric, o.cols / 32, ti, tj);
-    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+    tile_of<symmetric, 1>(number, o.cols / (32 * T), ti, tj);
+    const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int ks = o.depth / 16;
-    const bf16x8 *left = reinterpret_cast<const bf16x8 *>(o.left) + int64_t(ti) * ks * 64 + lane;
-    const bf16x8 *right = reinterpret_cast<const bf16x8 *>(o.right) + int64_t(tj) * ks * 64 + lane;
+    const bf16x8 *left = reinterpret_cast<const bf16x8 *>(o.left) + int64_t(ti) * T * ks * 64 + lane;
+    const bf16x8 *right = reinterpret_cast<const bf16x8 *>(o.right) + int64_t(tj) * T * ks * 64 + lane;
     const int64_t left_plane = int64_t(o.rows) * o.depth / 8, right_plane = int64_t(o.cols) * o.depth / 8;
-    float16v acc;
+    float16v acc[T][T];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
-    constexpr int U = 2;
-    for (int k = wave; k < ks; k += 4 * U) {
-        bf16x8 a[U][P], b[U][P];
+    for (int x = 0; x < T; ++x)
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (k + 4 * u < ks)
+        for (int y = 0; y < T; ++y)
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    a[u][p] = left[p * left_plane + (k + 4 * u) * 64];
-                    b[u][p] = right[p * right_plane + (k + 4 * u) * 64];
-                }
+            for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
+    bf16x8 a[SETS][T][P], b[SETS][T][P];
+    auto load = [&](int set, int k) {  // behind the last step: that one again
+        const int64_t at = k < ks ? k : ks - 1;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (k + 4 * u < ks) {
-                float16v sum;
+        for (int x = 0; x < T; ++x)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) sum[v] = 0.0f;
-                products<P>(sum, a[u], b[u]);
-#pragma unroll
-                for (int v = 0; v < 16; ++v) acc[v] += sum[v];
+            for (int p = 0; p < P; ++p) {
+                a[set][x][p] = left[p * left_plane + (int64_t(x) * ks + at) * 64];
+                b[set][x][p] = right[p * right_plane + (int64_t(x) * ks + at) * 64];
             }
+    };
+#pragma unroll
+    for (int u = 0; u < SETS; ++u) load(u, wave + 4 * u);
+    for (int k = wave; k < ks; k += 4 * SETS) {
+#pragma unroll
+        for (int u = 0; u < SETS; ++u) {
+            if (k + 4 * u >= ks) break;
+#pragma unroll
+            for (int x = 0; x < T; ++x)
+#pragma unroll
+                for (int y = 0; y < T; ++y) add_products<P>(acc[x][y], a[u][x], b[u][y]);
+            load(u, k + 4 * (u + SETS));
+        }
     }
+    // a fragment of the tile after the other through LDS
     __shared__ float tile[4][32][33];
-    const int l32 = lane & 31, lk = lane >> 5;
+    const int l32 = lane & 31, lk = lane >> 5, at = 8 * wave + 4 * lk;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) tile[wave][8 * (v / 4) + 4 * lk + v % 4][l32] = acc[v];
-    __syncthreads();
-    float v[4];
-    const int at = 8 * wave + 4 * lk;
+    for (int x = 0; x < T; ++x)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (tile[0][at + i][l32] + tile[1][at + i][l32]) + (tile[2][at + i][l32] + tile[3][at + i][l32]);
-    finish<P, phase>(j, t, ti * 32 + at, tj * 32 + l32, v);
-    write_down<P, phase>(j, t, step, ti * 32 + at, tj * 32 + l32, v);
-    if (symmetric && ti == tj) return;
+        for (int y = 0; y < T; ++y) {
+            if (x + y > 0) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (tile[0][l32][at + i] + tile[1][l32][at + i]) + (tile[2][l32][at + i] + tile[3][l32][at + i]);
-    finish<P, phase>(j, t, tj * 32 + at, ti * 32 + l32, v);
-    write_across<P, phase>(j, t, ti * 32 + l32, tj * 32 + at, v);
+            for (int v = 0; v < 16; ++v) tile[wave][8 * (v / 4) + 4 * lk + v % 4][l32] = acc[x][y][v];
+            __syncthreads();
+            const int row0 = (ti * T + x) * 32, col0 = (tj * T + y) * 32;
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = (tile[0][at + i][l32] + tile[1][at + i][l32]) + (tile[2][at + i][l32] + tile[3][at + i][l32]);
+            finish<P, phase>(j, t, row0 + at, col0 + l32, v);
+            write_down<P, phase>(j, t, step, row0 + at, col0 + l32, v);
+            if (symmetric && ti == tj) continue;  // (a tile on the diagonal is computed whole)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = (tile[0][l32][at + i] + tile[1][l32][at + i]) + (tile[2][l32][at + i] + tile[3][l32][at + i]);
+            finish<P, phase>(j, t, col0 + at, row0 + l32, v);
+            write_across<P, phase>(j, t, row0 + l32, col0 + at, v);
+        }
 }
 
-// Tiles of (64 TI)^2 through LDS: four wavefronts of TI x TI fragments each, 16 k at a time, the next 16 k on their way to the other half.
-template <int P, int TI, Phase phase> __global__ void __launch_bounds__(kThreads, 2) product_kernel(const Job j, int step) {
-    constexpr int FRAGS = 4 * TI * P, MINE = FRAGS / 4, TILE = 64 * TI;  // fragments of a step, of a wavefront
+// Tiles of 64 TI x 64 TJ through LDS: four wavefronts of TI x TJ fragments each, 16 k at a time, the next 16 k in the other half of the LDS and two more
+// steps on their way in registers.
+template <int P, int TI, int TJ, Phase phase> __global__ void __launch_bounds__(kThreads, 2) product_kernel(const Job j, int step) {
+    constexpr int FRAGS = 2 * (TI + TJ) * P, MINE = (FRAGS + 3) / 4;  // fragments of a step, of a wavefront
     __shared__ union {
         u32x4 frag[2][FRAGS][64];
         float turn[4][32][33];
     } lds;
     constexpr bool symmetric = phase == kGram || phase == kPolynomial;
-    const Mat &t = j.mat[matrix_of_block(j, symmetric ? 2 : 3)];
+    static_assert(TJ % TI == 0, "tiles of symmetric results");
+    int number, ti, tj;
+    const Mat &t = j.mat[matrix_of_block<symmetric ? kSymmetric : kOthers>(j, number)];
     const Operands o = operands<phase>(t, step);
-    int ti, tj;
-    tile_of(int(blockIdx.x) - t.first[symmetric ? 2 : 3], symmetric, o.cols / TILE, ti, tj);
+    tile_of<symmetric, TJ / TI>(number, o.cols / (64 * TJ), ti, tj);
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int ks = o.depth / 16;
 
-    // fragment f of a step: operand f / (2 TI P), then 32 rows, then plane
+    // fragment f of a step: of the left operand, then of the right one; 32 rows, then plane
     const u32x4 *from[MINE];
 #pragma unroll
     for (int f = 0; f < MINE; ++f) {
-        const int g = wave * MINE + f, side = g / (2 * TI * P), r = g / P % (2 * TI), p = g % P;
-        const int64_t rb = int64_t(side ? tj : ti) * 2 * TI + r, plane = int64_t(side ? o.cols : o.rows) * o.depth;
+        const int g = wave + 4 * f < FRAGS ? wave + 4 * f : wave, side = g >= 2 * TI * P, r = side ? g / P - 2 * TI : g / P, p = g % P;
+        const int64_t rb = side ? int64_t(tj) * 2 * TJ + r : int64_t(ti) * 2 * TI + r, plane = int64_t(side ? o.cols : o.rows) * o.depth;
         from[f] = reinterpret_cast<const u32x4 *>((side ? o.right : o.left) + p * plane + rb * ks * 512) + lane;
     }
-    u32x4 next[MINE];
-    auto load = [&](int k) {
+    u32x4 next[2][MINE];
+    auto load = [&](int set, int k) {  // behind the last step: that one again
 #pragma unroll
-        for (int f = 0; f < MINE; ++f) next[f] = from[f][int64_t(k < ks ? k : ks - 1) * 64];
+        for (int f = 0; f < MINE; ++f) next[set][f] = from[f][int64_t(k < ks ? k : ks - 1) * 64];
     };
-    auto stage = [&](int half) {
+    auto stage = [&](int set) {
 #pragma unroll
-        for (int f = 0; f < MINE; ++f) lds.frag[half][wave * MINE + f][lane] = next[f];
+        for (int f = 0; f < MINE; ++f)
+            if (FRAGS % 4 == 0 || wave + 4 * f < FRAGS) lds.frag[set][wave + 4 * f][lane] = next[set][f];
     };
     const int wi = wave >> 1, wj = wave & 1;
-    float16v acc[TI][TI];
+    float16v acc[TI][TJ];
 #pragma unroll
-    for (int a = 0; a < TI; ++a)
+    for (int x = 0; x < TI; ++x)
 #pragma unroll
-        for (int b = 0; b < TI; ++b)
+        for (int y = 0; y < TJ; ++y)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.0f;
-
-    load(0);
-    stage(0);
-    load(1);
-    __syncthreads();
-#pragma unroll 1
-    for (int k = 0; k < ks; ++k) {
-        bf16x8 a[TI][P], b[TI][P];
-#pragma unroll
-        for (int i = 0; i < TI; ++i)
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                a[i][p] = __builtin_bit_cast(bf16x8, lds.frag[k & 1][(wi * TI + i) * P + p][lane]);
-                b[i][p] = __builtin_bit_cast(bf16x8, lds.frag[k & 1][(2 * TI + wj * TI + i) * P + p][lane]);
-            }
+            for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
+    auto multiply = [&](int half) {
+        bf16x8 a[TI][P];
 #pragma unroll
         for (int x = 0; x < TI; ++x)
 #pragma unroll
-            for (int y = 0; y < TI; ++y) {
-                float16v sum;
+            for (int p = 0; p < P; ++p) a[x][p] = __builtin_bit_cast(bf16x8, lds.frag[half][(wi * TI + x) * P + p][lane]);
 #pragma unroll
-                for (int v = 0; v < 16; ++v) sum[v] = 0.0f;
-                products<P>(sum, a[x], b[y]);
+        for (int y = 0; y < TJ; ++y) {
+            bf16x8 b[P];
 #pragma unroll
-                for (int v = 0; v < 16; ++v) acc[x][y][v] += sum[v];
-            }
-        stage((k + 1) & 1);
-        load(k + 2);
+            for (int p = 0; p < P; ++p) b[p] = __builtin_bit_cast(bf16x8, lds.frag[half][(2 * TI + wj * TJ + y) * P + p][lane]);
+#pragma unroll
+            for (int x = 0; x < TI; ++x) add_products<P>(acc[x][y], a[x], b);
+        }
+    };
+    load(0, 0);
+    load(1, 1);
+    stage(0);
+    load(0, 2);
+    __syncthreads();
+#pragma unroll 1
+    for (int k = 0;; k += 2) {
+        multiply(0);
+        if (k + 1 >= ks) break;
+        stage(1);
+        load(1, k + 3);
+        __syncthreads();
+        multiply(1);
+        if (k + 2 >= ks) break;
+        stage(0);
+        load(0, k + 4);
         __syncthreads();
     }
+    __syncthreads();
 
     const int l32 = lane & 31, lk = lane >> 5;
 #pragma unroll
     for (int x = 0; x < TI; ++x)
 #pragma unroll
-        for (int y = 0; y < TI; ++y) {
-            const int row0 = ti * TILE + (wi * TI + x) * 32, col0 = tj * TILE + (wj * TI + y) * 32;
+        for (int y = 0; y < TJ; ++y) {
+            const int row0 = ti * 64 * TI + (wi * TI + x) * 32, col0 = tj * 64 * TJ + (wj * TJ + y) * 32;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int at = 8 * g + 4 * lk;
@@ -410,7 +495,8 @@ template <int P, int TI, Phase phase> __global__ void __launch_bounds__(kThreads
 #pragma unroll
                 for (int i = 0; i < 4; ++i) lds.turn[wave][at + i][l32] = v[i];
             }
-            if (symmetric && ti == tj) continue;  // (a tile on the diagonal is computed whole)
+            // squares of as many rows as a tile is wide are computed whole on the diagonal
+            if (symmetric && row0 / (64 * TJ) == tj) continue;
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
@@ -470,21 +556,22 @@ Sizes sizes_of(int64_t rows, int64_t cols, int32_t dtype) {
 
 template <int P, Phase phase> int launch_products(const Job &j, int kind, int step, int64_t blocks, hipStream_t stream) {
     if (blocks > INT32_MAX / kThreads) return GNN_ERR_UNSUPPORTED;
-    if (kind == 0) small_product_kernel<P, phase><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
-    else if (kind == 1) product_kernel<P, 1, phase><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
-    else product_kernel<P, 2, phase><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
+    constexpr int TI = phase == kGram || phase == kPolynomial ? 1 : 2;
+    if (kind == 0) split_product_kernel<P, phase, 1><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
+    else if (kind == 1) split_product_kernel<P, phase, 2><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
+    else product_kernel<P, TI, 2, phase><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
     GNN_HIP_TRY(hipGetLastError());
     return GNN_OK;
 }
 
-template <int P> int launch_job(const Job &j, int kind, const int64_t (&blocks)[4], int steps, hipStream_t stream) {
-    norm_kernel<<<unsigned(blocks[0]), kThreads, 0, stream>>>(j);
-    planes_kernel<P><<<unsigned(blocks[1]), kThreads, 0, stream>>>(j);
+template <int P> int launch_job(const Job &j, int kind, const int64_t (&blocks)[kLaunches], int steps, hipStream_t stream) {
+    norm_kernel<<<unsigned(blocks[kNorms]), kThreads, 0, stream>>>(j);
+    planes_kernel<P><<<unsigned(blocks[kPlanes]), kThreads, 0, stream>>>(j);
     GNN_HIP_TRY(hipGetLastError());
     for (int s = 0; s < steps; ++s) {
-        int rc = launch_products<P, kGram>(j, kind, s, blocks[2], stream);
-        if (rc == GNN_OK) rc = launch_products<P, kPolynomial>(j, kind, s, blocks[2], stream);
-        if (rc == GNN_OK) rc = s + 1 < steps ? launch_products<P, kUpdate>(j, kind, s, blocks[3], stream) : launch_products<P, kLast>(j, kind, s, blocks[3], stream);
+        int rc = launch_products<P, kGram>(j, kind, s, blocks[kSymmetric], stream);
+        if (rc == GNN_OK) rc = launch_products<P, kPolynomial>(j, kind, s, blocks[kSymmetric], stream);
+        if (rc == GNN_OK) rc = s + 1 < steps ? launch_products<P, kUpdate>(j, kind, s, blocks[kOthers], stream) : launch_products<P, kLast>(j, kind, s, blocks[kOthers], stream);
         if (rc != GNN_OK) return rc;
     }
     return GNN_OK;
@@ -494,29 +581,37 @@ template <int P> int launch_job(const Job &j, int kind, const int64_t (&blocks)[
 int orthogonalize(Entry (*at)(const void *, int64_t), const void *list, int64_t count, Job &j, int steps, uint8_t *room, hipStream_t stream) {
     for (int kind = 0; kind < 3; ++kind)
         for (int parts = 2; parts <= 3; ++parts) {
-            int64_t blocks[4] = {0, 0, 0, 0};
-            j.count = 0;
+            int64_t blocks[kLaunches];
+            int matrices = 0;
+            auto clear = [&]() {
+                matrices = 0;
+                for (int i = 0; i < kLaunches; ++i) {
+                    blocks[i] = 0;
+                    for (int32_t &f : j.first[i]) f = INT32_MAX;
+                }
+            };
             auto flush = [&]() -> int {
-                if (j.count == 0) return GNN_OK;
+                if (matrices == 0) return GNN_OK;
                 const int rc = parts == 2 ? launch_job<2>(j, kind, blocks, steps, stream) : launch_job<3>(j, kind, blocks, steps, stream);
-                j.count = 0;
-                for (int64_t &b : blocks) b = 0;
+                clear();
                 return rc;
             };
+            clear();
             for (int64_t k = 0; k < count; ++k) {
                 const Entry e = at(list, k);
                 if (e.skip || e.rows == 0 || e.cols == 0) continue;
                 const Sizes s = sizes_of(e.rows, e.cols, e.dtype);
                 if (s.kind != kind || s.parts != parts) continue;
                 const int64_t tile = tile_of_kind(kind), across = s.mp / tile;
-                const int64_t more[4] = {s.norm_blocks, s.mp / 64 * (s.np / 64), across * (across + 1) / 2, across * (s.np / tile)};
-                bool full = j.count == kMats;
-                for (int i = 0; i < 4; ++i) full |= blocks[i] + more[i] > INT32_MAX / kThreads;
+                // (large symmetric results: two tiles of half the height for each square one)
+                const int64_t more[kLaunches] = {s.norm_blocks, s.mp / 64 * (s.np / 64), across * (across + 1) / (kind == 2 ? 1 : 2), across * (s.np / tile)};
+                bool full = matrices == kMats;
+                for (int i = 0; i < kLaunches; ++i) full |= blocks[i] + more[i] > INT32_MAX / kThreads;
                 if (full) {
                     const int rc = flush();
                     if (rc != GNN_OK) return rc;
                 }
-                Mat &t = j.mat[j.count++];
+                Mat &t = j.mat[matrices];
                 t = Mat{};
                 const int64_t xs = s.parts * s.mp * s.np, as = s.parts * s.mp * s.mp;
                 uint16_t *p = reinterpret_cast<uint16_t *>(room);
@@ -543,10 +638,11 @@ int orthogonalize(Entry (*at)(const void *, int64_t), const void *list, int64_t 
                 t.flags = (e.dtype == GNN_BF16 ? kBf16 : 0) | (e.rows > e.cols ? kTall : 0);
                 t.decay = e.decay;
                 t.rate = e.rate;
-                for (int i = 0; i < 4; ++i) {
-                    t.first[i] = int32_t(blocks[i]);
+                for (int i = 0; i < kLaunches; ++i) {
+                    j.first[i][matrices] = int32_t(blocks[i]);
                     blocks[i] += more[i];
                 }
+                ++matrices;
             }
             const int rc = flush();
             if (rc != GNN_OK) return rc;

@@ -34,7 +34,7 @@ struct Rows {
     int64_t v, n, ldx, lds;
     int32_t f, pieces, rows;  // columns; pieces of eight of a row; rows of a workgroup
     uint32_t reciprocal;      // ceil(2^32 / pieces): quotients of numbers below 2^16
-    int32_t is_64, compare;
+    int32_t is_64;
     __device__ __forceinline__ int64_t id(int64_t i) const {
         if (!ids) return i;
         const int64_t t = is_64 ? static_cast<const int64_t *>(ids)[i] : int64_t(static_cast<const int32_t *>(ids)[i]);
@@ -54,8 +54,9 @@ __global__ void __launch_bounds__(kThreads) enter_kernel(const Rows a) {
     if (id >= 0) a.last[id] = int32_t(i);  // of several any one
 }
 __global__ void __launch_bounds__(kThreads) raise_kernel(const Rows a) {
-    const int64_t i = block_number() * kThreads + threadIdx.x;
-    if (i >= a.n) return;
+    // from the last position on: of an id that comes often most then find a later one there
+    const int64_t i = a.n - 1 - (block_number() * kThreads + threadIdx.x);
+    if (i < 0) return;
     const int64_t id = a.id(i);
     if (id >= 0 && a.last[id] < int32_t(i)) atomicMax(&a.last[id], int32_t(i));
 }
@@ -79,68 +80,99 @@ template <typename T> __device__ __forceinline__ void load8(const T *p, int have
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(kThreads) store_kernel(const Rows a) {
+// Columns 8 q .. 8 q + 8 of a row in 8 bits, with those of the three threads beside this one.
+__device__ __forceinline__ void write8(const Rows &a, int64_t id, int q, const float (&x)[8]) {
+    const int c = q * 8, left = a.f - c, have = left < 0 ? 0 : left < 8 ? left : 8;
+    uint32_t top = 0;
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t b = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+        const bool finite = b < 0x7F800000u;
+        odd |= !finite;
+        top = finite && b > top ? b : top;
+    }
+    const uint32_t other = __float_as_uint(gnn_from_lane<0xB1>(__uint_as_float(top)));  // the other of a pair
+    top = other > top ? other : top;
+    const uint32_t pair = __float_as_uint(gnn_from_lane<0x4E>(__uint_as_float(top)));   // the other pair of four
+    top = pair > top ? pair : top;
+    int e = int(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    e = e > 0 ? e : 0;
+    const float factor = __uint_as_float(uint32_t(254 - e) << 23);
+    uint32_t w[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        int t4 = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k] * factor, x[4 * k + 1] * factor, 0, false);
+        w[k] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k + 2] * factor, x[4 * k + 3] * factor, t4, true));
+    }
+    if (odd)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if ((__float_as_uint(x[j]) & 0x7FFFFFFFu) >= 0x7F800000u) w[j / 4] |= 0x7Fu << (8 * (j % 4));
+    uint8_t *to = a.store + id * a.lds;
+    if (have == 8) {
+        *reinterpret_cast<u32x2_any *>(to + c) = u32x2_any{w[0], w[1]};
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < have) to[c + j] = uint8_t(w[j / 4] >> (8 * (j % 4)));
+    }
+    if ((q & 3) == 0) to[a.f + (q >> 2)] = uint8_t(e);
+}
+
+template <typename T, bool COMPARE> __global__ void __launch_bounds__(kThreads) store_kernel(const Rows a) {
     const int64_t row0 = block_number() * a.rows;
     if (row0 >= a.n) return;
     const int rows = a.n - row0 < a.rows ? int(a.n - row0) : a.rows;
-    __shared__ int64_t ids[kCompareRows];
+    __shared__ __attribute__((aligned(16))) int32_t ids[COMPARE ? kCompareHere : 4];
     __shared__ int again[kCompareRows];  // a later position has this row's id
-    if (a.compare) {
-        if (int(threadIdx.x) < rows) {
-            ids[threadIdx.x] = a.id(row0 + threadIdx.x);
-            again[threadIdx.x] = 0;
-        }
+    if constexpr (COMPARE) {
+        const int n = int(a.n);
+        for (int j = int(threadIdx.x); j < n; j += kThreads) ids[j] = int32_t(a.id(j));
+        if (threadIdx.x < kCompareRows) again[threadIdx.x] = 0;
         __syncthreads();
-        for (int64_t j = row0 + 1 + threadIdx.x; j < a.n; j += kThreads) {
-            const int64_t id = a.id(j);
-            for (int r = 0; r < rows; ++r)
-                if (id == ids[r] && j > row0 + r) again[r] = 1;
+        // a thread a row and an eighth of the positions, four at a time
+        const int r = int(threadIdx.x) % kCompareRows, i = int(row0) + r;
+        if (r < rows) {
+            const int32_t id = ids[i];
+            bool found = false;
+            for (int j = int(threadIdx.x) / kCompareRows * 4; j < n; j += kThreads / kCompareRows * 4) {
+                const int4 t = *reinterpret_cast<const int4 *>(ids + j);  // (behind the last position: not looked at)
+                found |= (t.x == id && j > i) | (t.y == id && j + 1 > i && j + 1 < n) | (t.z == id && j + 2 > i && j + 2 < n) | (t.w == id && j + 3 > i && j + 3 < n);
+            }
+            if (found) again[r] = 1;
         }
         __syncthreads();
     }
     const int items = rows * a.pieces;
-    for (int t = int(threadIdx.x); t < items; t += kThreads) {  // (pieces is a multiple of four: the threads of a block take part together)
-        const int r = a.row_of(t), q = t - r * a.pieces, c = q * 8;
-        const int64_t i = row0 + r, id = a.id(i);
-        if (id < 0 || (a.compare ? again[r] != 0 : a.last && a.last[id] != int32_t(i))) continue;
-        const int left = a.f - c, have = left < 0 ? 0 : left < 8 ? left : 8;
-        float x[8];
-        load8<T>(static_cast<const T *>(a.x) + i * a.ldx + c, have, x);
-        uint32_t top = 0;
-        bool odd = false;
+    constexpr int U = 4;
+    for (int t0 = int(threadIdx.x); t0 < items; t0 += kThreads * U) {  // (pieces is a multiple of four: the threads of a block take part together)
+        int64_t id[U];
+        int row[U], last[U];
+        float x[U][8];
+        // the ids and what is known of them, then the rows that are written, all on their way at once
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t b = __float_as_uint(x[j]) & 0x7FFFFFFFu;
-            const bool finite = b < 0x7F800000u;
-            odd |= !finite;
-            top = finite && b > top ? b : top;
+        for (int u = 0; u < U; ++u) {
+            const int t = t0 + u * kThreads < items ? t0 + u * kThreads : items - 1;
+            row[u] = a.row_of(t);
+            id[u] = a.id(row0 + row[u]);
         }
-        const uint32_t other = __float_as_uint(gnn_from_lane<0xB1>(__uint_as_float(top)));  // the other of a pair
-        top = other > top ? other : top;
-        const uint32_t pair = __float_as_uint(gnn_from_lane<0x4E>(__uint_as_float(top)));   // the other pair of four
-        top = pair > top ? pair : top;
-        int e = int(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-        e = e > 0 ? e : 0;
-        const float factor = __uint_as_float(uint32_t(254 - e) << 23);
-        uint32_t w[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            int t4 = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k] * factor, x[4 * k + 1] * factor, 0, false);
-            w[k] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k + 2] * factor, x[4 * k + 3] * factor, t4, true));
+        for (int u = 0; u < U; ++u) {
+            if constexpr (COMPARE) last[u] = again[row[u]] ? -1 : int(row0) + row[u];
+            else last[u] = a.last ? a.last[id[u] < 0 ? 0 : id[u]] : int32_t(row0 + row[u]);
         }
-        if (odd)
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if ((__float_as_uint(x[j]) & 0x7FFFFFFFu) >= 0x7F800000u) w[j / 4] |= 0x7Fu << (8 * (j % 4));
-        uint8_t *to = a.store + id * a.lds;
-        if (have == 8) {
-            *reinterpret_cast<u32x2_any *>(to + c) = u32x2_any{w[0], w[1]};
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < have) to[c + j] = uint8_t(w[j / 4] >> (8 * (j % 4)));
+        for (int u = 0; u < U; ++u) {
+            if (t0 + u * kThreads >= items || last[u] != int32_t(row0 + row[u])) id[u] = -1;
+            const int q = t0 + u * kThreads - row[u] * a.pieces, left = a.f - q * 8, have = left < 0 ? 0 : left < 8 ? left : 8;
+            if (id[u] >= 0) load8<T>(static_cast<const T *>(a.x) + (row0 + row[u]) * a.ldx + q * 8, have, x[u]);
         }
-        if ((q & 3) == 0) to[a.f + (q >> 2)] = uint8_t(e);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int q = t0 + u * kThreads - row[u] * a.pieces;
+            if (id[u] >= 0) write8(a, id[u], q, x[u]);
+        }
     }
 }
 
@@ -170,25 +202,25 @@ template <typename T, int E> __global__ void __launch_bounds__(kThreads) load_ke
         uint8_t e[U][2];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int t = t0 + u * kThreads;
-            id[u] = -1;
+            // no branch between the loads: what lies behind the end repeats the last piece, and an id that names no row reads row 0
+            const int t = t0 + u * kThreads < items ? t0 + u * kThreads : items - 1;
             row[u] = a.row_of(t);
             const int c = (t - row[u] * a.pieces) * E;
             col[u] = c < a.f - E ? c : a.f - E;  // the last piece ends with the row
-            if (t < items) id[u] = a.id(row0 + row[u]);
+            id[u] = a.id(row0 + row[u]);
         }
+        if (a.v > 0)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint8_t *p = a.store + (id[u] < 0 ? 0 : id[u]) * a.lds;
+                if constexpr (E == 8) w[u] = *reinterpret_cast<const u32x2_any *>(p + col[u]);
+                else w[u].x = p[col[u]];
+                e[u][0] = p[a.f + col[u] / kBlock];
+                e[u][1] = p[a.f + (col[u] + E - 1) / kBlock];  // of another block where the last piece reaches over its end
+            }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (id[u] < 0) continue;
-            const uint8_t *p = a.store + id[u] * a.lds;
-            if constexpr (E == 8) w[u] = *reinterpret_cast<const u32x2_any *>(p + col[u]);
-            else w[u].x = p[col[u]];
-            e[u][0] = p[a.f + col[u] / kBlock];
-            e[u][1] = p[a.f + (col[u] + E - 1) / kBlock];  // of another block where the last piece reaches over its end
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (t0 + u * kThreads >= items) continue;
+            if (t0 + u * kThreads >= items) break;
             T *to = y + int64_t(row[u]) * a.ldx + col[u];
             float x[E];
             if (id[u] < 0) {
@@ -267,7 +299,6 @@ extern "C" GNN_API int gnn_store_rows(const void *X, const void *ids, void *stor
     if (twice && !compare && (!o.workspace || misaligned(o.workspace, 4) || o.workspace_bytes < 4 * V)) return GNN_ERR_INVALID_ARG;
     (void)hipGetLastError();
     Rows a = rows_of(X, ids, store, V, n, F, (F + kBlock - 1) / kBlock * (kBlock / 8), compare ? kCompareRows : kItems, o);
-    a.compare = compare;
     hipStream_t stream = static_cast<hipStream_t>(o.stream);
     if (twice && !compare) {
         a.last = static_cast<int32_t *>(o.workspace);
@@ -277,8 +308,8 @@ extern "C" GNN_API int gnn_store_rows(const void *X, const void *ids, void *stor
         GNN_HIP_TRY(hipGetLastError());
     }
     const dim3 grid = grid_of((n + a.rows - 1) / a.rows);
-    if (o.dtype == GNN_F32) store_kernel<float><<<grid, kThreads, 0, stream>>>(a);
-    else store_kernel<gnn_bf16><<<grid, kThreads, 0, stream>>>(a);
+    if (o.dtype == GNN_F32) compare ? store_kernel<float, true><<<grid, kThreads, 0, stream>>>(a) : store_kernel<float, false><<<grid, kThreads, 0, stream>>>(a);
+    else compare ? store_kernel<gnn_bf16, true><<<grid, kThreads, 0, stream>>>(a) : store_kernel<gnn_bf16, false><<<grid, kThreads, 0, stream>>>(a);
     GNN_HIP_TRY(hipGetLastError());
     return GNN_OK;
 }
