@@ -7,7 +7,8 @@
 // are computed, and written to both places.
 //
 // Operands live in the workspace as the matrix cores take them: split into P bf16 numbers whose sum they are (P = 3: all 24 bits of fp32; P = 2: 16 bits,
-// for bf16 matrices), in fragments of 32 rows x 16 k, 1 KB a fragment, the 16 bytes of lane 32 * (k / 8) + row one after the other.  So whatever
+// for bf16 matrices), in fragments of 32 rows x 16 k, 1 KB a fragment, the 16 bytes of lane 32 * (k / 8) + row one after the other; the fragments of the same
+// k side by side, so that workgroups that walk along k together spread over the channels of the L2s (along k first: 1000 x 1000 bf16 283 us).  So whatever
 // fetches a fragment reads 1 KB in a row, nothing is split twice, and a product's epilogue, which has four neighbouring results of a column in a
 // lane, writes 8 bytes a plane.  Rows and columns are filled up with zeros to whole tiles, which the products keep zero.
 //
@@ -148,12 +149,12 @@ __device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
 }
 
 // Where element (row, k) of an operand of rows x depth lies in plane 0, in elements of 2 bytes; planes are rows * depth apart.
-__device__ __forceinline__ int64_t place(int depth, int row, int k) {
-    return (int64_t(row >> 5) * (depth >> 4) + (k >> 4)) * 512 + (((k >> 3) & 1) * 32 + (row & 31)) * 8 + (k & 7);
+__device__ __forceinline__ int64_t place(int rows, int row, int k) {
+    return (int64_t(k >> 4) * (rows >> 5) + (row >> 5)) * 512 + (((k >> 3) & 1) * 32 + (row & 31)) * 8 + (k & 7);
 }
 // four neighbouring k, the first a multiple of four
 template <int P> __device__ __forceinline__ void put4(uint16_t *planes, int rows, int depth, int row, int k, const float (&v)[4]) {
-    uint16_t *p = planes + place(depth, row, k);
+    uint16_t *p = planes + place(rows, row, k);
     float part[4][P];
 #pragma unroll
     for (int i = 0; i < 4; ++i) split<P>(v[i], part[i]);
@@ -163,7 +164,7 @@ template <int P> __device__ __forceinline__ void put4(uint16_t *planes, int rows
 }
 // eight, the first a multiple of eight
 template <int P> __device__ __forceinline__ void put8(uint16_t *planes, int rows, int depth, int row, int k, const float (&v)[8]) {
-    uint16_t *p = planes + place(depth, row, k);
+    uint16_t *p = planes + place(rows, row, k);
     float part[8][P];
 #pragma unroll
     for (int i = 0; i < 8; ++i) split<P>(v[i], part[i]);
@@ -176,7 +177,7 @@ template <int P> __device__ __forceinline__ void put8(uint16_t *planes, int rows
     }
 }
 template <int P> __device__ __forceinline__ void get4(const uint16_t *planes, int rows, int depth, int row, int k, float (&v)[4]) {
-    const uint16_t *p = planes + place(depth, row, k);
+    const uint16_t *p = planes + place(rows, row, k);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = 0.0f;
 #pragma unroll
@@ -251,39 +252,47 @@ template <Phase phase> __device__ __forceinline__ Operands operands(const Mat &t
     else return {t.q, t.xt[step & 1], t.mp, t.np, t.mp};
 }
 
-// The tile of a workgroup; of symmetric results those on and below the diagonal, where a tile is as wide as one or two are high.
-template <bool SYMMETRIC, int WIDE> __device__ __forceinline__ void tile_of(int number, int tiles_across, int &ti, int &tj) {
+// The tile of a workgroup; of symmetric results those on and below the diagonal, where a tile is as wide as one or two are high.  Workgroup b of a launch
+// runs on XCD b % 8, each with an L2 of its own: an XCD gets tiles that lie side by side, in bands of kBand rows of tiles, so that it reads
+// few rows of either operand.
+constexpr int kBand = 8;
+template <bool SYMMETRIC, int WIDE> __device__ __forceinline__ void tile_of(int number, int tiles, int tiles_across, int &ti, int &tj) {
+    const int xcd = number & 7, rest8 = tiles & 7;
+    number = xcd * (tiles >> 3) + (xcd < rest8 ? xcd : rest8) + (number >> 3);
     if constexpr (!SYMMETRIC) {
-        ti = number / tiles_across;
-        tj = number - ti * tiles_across;
+        const int down = tiles / tiles_across, band = number / (kBand * tiles_across), first = band * kBand;
+        const int high = down - first < kBand ? down - first : kBand, rest = number - first * tiles_across;
+        tj = rest / high;
+        ti = first + rest - tj * high;
     } else {  // rows i * WIDE .. i * WIDE + WIDE - 1 have i + 1 tiles each
         auto before = [](int i) { return WIDE * (i * (i + 1) / 2); };
         int i = int((sqrtf(8.0f / WIDE * float(number) + 1.0f) - 1.0f) * 0.5f);
         while (before(i) > number) --i;
         while (before(i + 1) <= number) ++i;
         const int rest = number - before(i);
-        ti = i * WIDE + rest / (i + 1);
-        tj = rest % (i + 1);
+        ti = i * WIDE + rest % WIDE;
+        tj = rest / WIDE;
     }
 }
 
-// The sums of the products of parts that matter.  P = 3: from zero, smallest first, and then added with one rounding; P = 2, whose operands are off by
-// more than what the matrix cores cut off, in one chain.
-template <int P> __device__ __forceinline__ void add_products(float16v &acc, const bf16x8 (&a)[P], const bf16x8 (&b)[P]) {
-    float16v sum = acc;
-    if constexpr (P == 3)
+// The sums of the products of parts that matter, for N fragments of the right operand, in turn, so that no product waits for the one before.  P = 3:
+// from zero, smallest first, and then added with one rounding; P = 2, whose operands are off by more than what the matrix cores cut off, in one chain.
+template <int P, int N> __device__ __forceinline__ void add_products(float16v (&acc)[N], const bf16x8 (&a)[P], const bf16x8 (&b)[N][P]) {
+    float16v sum[N];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) sum[v] = 0.0f;
+    for (int y = 0; y < N; ++y)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sum[y][v] = P == 3 ? 0.0f : acc[y][v];
 #pragma unroll
     for (int s = P - 1; s >= 0; --s)
 #pragma unroll
-        for (int p = 0; p <= s; ++p) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[p], b[s - p], sum, 0, 0, 0);
-    if constexpr (P == 3) {
+        for (int p = 0; p <= s; ++p)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[v] += sum[v];
-    } else {
-        acc = sum;
-    }
+            for (int y = 0; y < N; ++y) sum[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[p], b[y][s - p], sum[y], 0, 0, 0);
+#pragma unroll
+    for (int y = 0; y < N; ++y)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[y][v] = P == 3 ? acc[y][v] + sum[y][v] : sum[y][v];
 }
 
 // What a phase makes of four sums, rows row_i .. row_i + 3 of column row_c, or the same columns of that row: A is symmetric.
@@ -330,19 +339,40 @@ template <int P, Phase phase> __device__ __forceinline__ void write_across(const
     }
 }
 
+// A fragment of results on its way out: rows row0 .. row0 + 31, columns col0 .. col0 + 31, to both places where `both`.  The loop is not unrolled: code that
+// a wavefront goes through once is as slow as it is fetched.
+template <int P, Phase phase> __device__ __forceinline__ void write_fragment(const Job &j, const Mat &t, int step, int row0, int col0, const float (&turn)[32][33], bool both) {
+    const int lane = int(threadIdx.x) & 63, l32 = lane & 31, lk = lane >> 5;
+#pragma unroll 1
+    for (int g = 0; g < 4; ++g) {
+        const int at = 8 * g + 4 * lk;
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = turn[at + i][l32];
+        finish<P, phase>(j, t, row0 + at, col0 + l32, v);
+        write_down<P, phase>(j, t, step, row0 + at, col0 + l32, v);
+        if (!both) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = turn[l32][at + i];
+        finish<P, phase>(j, t, col0 + at, row0 + l32, v);
+        write_across<P, phase>(j, t, row0 + l32, col0 + at, v);
+    }
+}
+
 // Tiles of (32 T)^2: each of four wavefronts has all of the tile and every fourth 16 of k, straight from the caches, and keeps SETS steps on their way.
 // Nothing waits but for its own loads; the four sums are added in LDS.
 template <int P, Phase phase, int T> __global__ void __launch_bounds__(kThreads) split_product_kernel(const Job j, int step) {
     constexpr bool symmetric = phase == kGram || phase == kPolynomial;
-    constexpr int SETS = T == 1 ? 4 : 2;
+    constexpr int SETS = 2;  // 600-1000-1000-41 bf16 247 us, four 277; a model of 256 columns 96, four 99, one 107
     int number, ti, tj;
     const Mat &t = j.mat[matrix_of_block<symmetric ? kSymmetric : kOthers>(j, number)];
     const Operands o = operands<phase>(t, step);
-    tile_of<symmetric, 1>(number, o.cols / (32 * T), ti, tj);
+    const int side = o.rows / (32 * T), across = o.cols / (32 * T);
+    tile_of<symmetric, 1>(number, symmetric ? side * (side + 1) / 2 : side * across, across, ti, tj);
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int ks = o.depth / 16;
-    const bf16x8 *left = reinterpret_cast<const bf16x8 *>(o.left) + int64_t(ti) * T * ks * 64 + lane;
-    const bf16x8 *right = reinterpret_cast<const bf16x8 *>(o.right) + int64_t(tj) * T * ks * 64 + lane;
+    const bf16x8 *left = reinterpret_cast<const bf16x8 *>(o.left) + int64_t(ti) * T * 64 + lane;
+    const bf16x8 *right = reinterpret_cast<const bf16x8 *>(o.right) + int64_t(tj) * T * 64 + lane;
     const int64_t left_plane = int64_t(o.rows) * o.depth / 8, right_plane = int64_t(o.cols) * o.depth / 8;
     float16v acc[T][T];
 #pragma unroll
@@ -358,8 +388,8 @@ template <int P, Phase phase, int T> __global__ void __launch_bounds__(kThreads)
         for (int x = 0; x < T; ++x)
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                a[set][x][p] = left[p * left_plane + (int64_t(x) * ks + at) * 64];
-                b[set][x][p] = right[p * right_plane + (int64_t(x) * ks + at) * 64];
+                a[set][x][p] = left[p * left_plane + at * (o.rows * 2) + x * 64];
+                b[set][x][p] = right[p * right_plane + at * (o.cols * 2) + x * 64];
             }
     };
 #pragma unroll
@@ -369,71 +399,95 @@ template <int P, Phase phase, int T> __global__ void __launch_bounds__(kThreads)
         for (int u = 0; u < SETS; ++u) {
             if (k + 4 * u >= ks) break;
 #pragma unroll
-            for (int x = 0; x < T; ++x)
-#pragma unroll
-                for (int y = 0; y < T; ++y) add_products<P>(acc[x][y], a[u][x], b[u][y]);
+            for (int x = 0; x < T; ++x) add_products<P, T>(acc[x], a[u][x], b[u]);
             load(u, k + 4 * (u + SETS));
         }
     }
-    // a fragment of the tile after the other through LDS
-    __shared__ float tile[4][32][33];
-    const int l32 = lane & 31, lk = lane >> 5, at = 8 * wave + 4 * lk;
+    const int l32 = lane & 31, lk = lane >> 5;
+    if constexpr (T == 1) {
+        // a wavefront adds up and writes eight rows, and eight columns for the other place
+        __shared__ float tile[4][32][33];
+        const int at = 8 * wave + 4 * lk, row0 = ti * 32, col0 = tj * 32;
 #pragma unroll
-    for (int x = 0; x < T; ++x)
+        for (int v = 0; v < 16; ++v) tile[wave][8 * (v / 4) + 4 * lk + v % 4][l32] = acc[0][0][v];
+        __syncthreads();
+        float v[4];
 #pragma unroll
-        for (int y = 0; y < T; ++y) {
-            if (x + y > 0) __syncthreads();
+        for (int i = 0; i < 4; ++i) v[i] = (tile[0][at + i][l32] + tile[1][at + i][l32]) + (tile[2][at + i][l32] + tile[3][at + i][l32]);
+        finish<P, phase>(j, t, row0 + at, col0 + l32, v);
+        write_down<P, phase>(j, t, step, row0 + at, col0 + l32, v);
+        if (symmetric && ti == tj) return;  // (a tile on the diagonal is computed whole)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) tile[wave][8 * (v / 4) + 4 * lk + v % 4][l32] = acc[x][y][v];
-            __syncthreads();
-            const int row0 = (ti * T + x) * 32, col0 = (tj * T + y) * 32;
-            float v[4];
+        for (int i = 0; i < 4; ++i) v[i] = (tile[0][l32][at + i] + tile[1][l32][at + i]) + (tile[2][l32][at + i] + tile[3][l32][at + i]);
+        finish<P, phase>(j, t, col0 + at, row0 + l32, v);
+        write_across<P, phase>(j, t, row0 + l32, col0 + at, v);
+    } else {
+        // a wavefront adds up and writes one fragment of the tile
+        static_assert(T == 2, "a fragment a wavefront");
+        __shared__ union {
+            float part[4][4][16][64];
+            float turn[4][32][33];
+        } lds;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = (tile[0][at + i][l32] + tile[1][at + i][l32]) + (tile[2][at + i][l32] + tile[3][at + i][l32]);
-            finish<P, phase>(j, t, row0 + at, col0 + l32, v);
-            write_down<P, phase>(j, t, step, row0 + at, col0 + l32, v);
-            if (symmetric && ti == tj) continue;  // (a tile on the diagonal is computed whole)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = (tile[0][l32][at + i] + tile[1][l32][at + i]) + (tile[2][l32][at + i] + tile[3][l32][at + i]);
-            finish<P, phase>(j, t, col0 + at, row0 + l32, v);
-            write_across<P, phase>(j, t, row0 + l32, col0 + at, v);
-        }
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) lds.part[wave][2 * x + y][v][lane] = acc[x][y][v];
+        __syncthreads();
+        float sum[16];
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            sum[v] = (lds.part[0][wave][v][lane] + lds.part[1][wave][v][lane]) + (lds.part[2][wave][v][lane] + lds.part[3][wave][v][lane]);
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < 16; ++v) lds.turn[wave][8 * (v / 4) + 4 * lk + v % 4][l32] = sum[v];
+        __builtin_amdgcn_wave_barrier();
+        write_fragment<P, phase>(j, t, step, (ti * 2 + (wave >> 1)) * 32, (tj * 2 + (wave & 1)) * 32, lds.turn[wave], !(symmetric && ti == tj));
+    }
 }
 
-// Tiles of 64 TI x 64 TJ through LDS: four wavefronts of TI x TJ fragments each, 16 k at a time, the next 16 k in the other half of the LDS and two more
-// steps on their way in registers.
-template <int P, int TI, int TJ, Phase phase> __global__ void __launch_bounds__(kThreads, 2) product_kernel(const Job j, int step) {
-    constexpr int FRAGS = 2 * (TI + TJ) * P, MINE = (FRAGS + 3) / 4;  // fragments of a step, of a wavefront
+// Tiles of 64 TI x 64 TJ through LDS: four wavefronts of TI x TJ fragments each, 16 KS k at a time, the next ones in the other half of the LDS and two more
+// such steps on their way in registers.
+template <int P, int TI, int TJ, int KS, Phase phase> __global__ void __launch_bounds__(kThreads, 3) product_kernel(const Job j, int step) {
+    constexpr int ROWS = 2 * (TI + TJ), FRAGS = ROWS * P * KS, MINE = (FRAGS + 3) / 4;  // 32 rows of an operand; fragments of a step, of a wavefront
+    static_assert(TJ % TI == 0, "tiles of symmetric results");
     __shared__ union {
         u32x4 frag[2][FRAGS][64];
         float turn[4][32][33];
     } lds;
     constexpr bool symmetric = phase == kGram || phase == kPolynomial;
-    static_assert(TJ % TI == 0, "tiles of symmetric results");
     int number, ti, tj;
     const Mat &t = j.mat[matrix_of_block<symmetric ? kSymmetric : kOthers>(j, number)];
     const Operands o = operands<phase>(t, step);
-    tile_of<symmetric, TJ / TI>(number, o.cols / (64 * TJ), ti, tj);
+    const int down = o.rows / (64 * TI), across = o.cols / (64 * TJ);
+    tile_of<symmetric, TJ / TI>(number, symmetric ? TJ / TI * (across * (across + 1) / 2) : down * across, across, ti, tj);
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-    const int ks = o.depth / 16;
+    const int steps = o.depth / (16 * KS);
 
-    // fragment f of a step: of the left operand, then of the right one; 32 rows, then plane
+    // fragment f of a step: its 16 k, then 32 rows (of the left operand, then of the right one), then plane.  Where they cannot be shared out evenly the last
+    // one is fetched more than once: branches around single loads cost more (2560 x 4000 3110 us, 2940 so).
     const u32x4 *from[MINE];
+    int64_t apart[MINE];  // from a step to the next, in 16 bytes
 #pragma unroll
     for (int f = 0; f < MINE; ++f) {
-        const int g = wave + 4 * f < FRAGS ? wave + 4 * f : wave, side = g >= 2 * TI * P, r = side ? g / P - 2 * TI : g / P, p = g % P;
-        const int64_t rb = side ? int64_t(tj) * 2 * TJ + r : int64_t(ti) * 2 * TI + r, plane = int64_t(side ? o.cols : o.rows) * o.depth;
-        from[f] = reinterpret_cast<const u32x4 *>((side ? o.right : o.left) + p * plane + rb * ks * 512) + lane;
+        const int g = wave * MINE + f < FRAGS ? wave * MINE + f : FRAGS - 1, kk = g / (ROWS * P), r = g / P % ROWS, p = g % P;
+        const bool right = r >= 2 * TI;
+        const int64_t high = right ? o.cols : o.rows, rb = right ? int64_t(tj) * 2 * TJ + r - 2 * TI : int64_t(ti) * 2 * TI + r;
+        from[f] = reinterpret_cast<const u32x4 *>((right ? o.right : o.left) + p * high * o.depth) + (kk * (high / 32) + rb) * 64;
+        apart[f] = high * 2 * KS;
     }
     u32x4 next[2][MINE];
     auto load = [&](int set, int k) {  // behind the last step: that one again
 #pragma unroll
-        for (int f = 0; f < MINE; ++f) next[set][f] = from[f][int64_t(k < ks ? k : ks - 1) * 64];
+        for (int f = 0; f < MINE; ++f) {
+            next[set][f] = from[f][lane];
+            from[f] += k + 1 < steps ? apart[f] : 0;
+        }
     };
-    auto stage = [&](int set) {
+    auto stage = [&](int half) {
 #pragma unroll
-        for (int f = 0; f < MINE; ++f)
-            if (FRAGS % 4 == 0 || wave + 4 * f < FRAGS) lds.frag[set][wave + 4 * f][lane] = next[set][f];
+        for (int f = 0; f < MINE; ++f) lds.frag[half][wave * MINE + f < FRAGS ? wave * MINE + f : FRAGS - 1][lane] = next[half][f];
     };
     const int wi = wave >> 1, wj = wave & 1;
     float16v acc[TI][TJ];
@@ -444,19 +498,22 @@ template <int P, int TI, int TJ, Phase phase> __global__ void __launch_bounds__(
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
     auto multiply = [&](int half) {
-        bf16x8 a[TI][P];
+        __builtin_amdgcn_s_setprio(1);  // ahead of the other workgroup's wavefronts, which are then free to fetch: 2560 x 4000 3255 -> 3110 us
 #pragma unroll
-        for (int x = 0; x < TI; ++x)
+        for (int kk = 0; kk < KS; ++kk) {
+            bf16x8 a[TI][P], b[TJ][P];
 #pragma unroll
-            for (int p = 0; p < P; ++p) a[x][p] = __builtin_bit_cast(bf16x8, lds.frag[half][(wi * TI + x) * P + p][lane]);
+            for (int x = 0; x < TI; ++x)
 #pragma unroll
-        for (int y = 0; y < TJ; ++y) {
-            bf16x8 b[P];
+                for (int p = 0; p < P; ++p) a[x][p] = __builtin_bit_cast(bf16x8, lds.frag[half][(kk * ROWS + wi * TI + x) * P + p][lane]);
 #pragma unroll
-            for (int p = 0; p < P; ++p) b[p] = __builtin_bit_cast(bf16x8, lds.frag[half][(2 * TI + wj * TJ + y) * P + p][lane]);
+            for (int y = 0; y < TJ; ++y)
 #pragma unroll
-            for (int x = 0; x < TI; ++x) add_products<P>(acc[x][y], a[x], b);
+                for (int p = 0; p < P; ++p) b[y][p] = __builtin_bit_cast(bf16x8, lds.frag[half][(kk * ROWS + 2 * TI + wj * TJ + y) * P + p][lane]);
+#pragma unroll
+            for (int x = 0; x < TI; ++x) add_products<P, TJ>(acc[x], a[x], b);
         }
+        __builtin_amdgcn_s_setprio(0);
     };
     load(0, 0);
     load(1, 1);
@@ -466,12 +523,12 @@ template <int P, int TI, int TJ, Phase phase> __global__ void __launch_bounds__(
 #pragma unroll 1
     for (int k = 0;; k += 2) {
         multiply(0);
-        if (k + 1 >= ks) break;
+        if (k + 1 >= steps) break;
         stage(1);
         load(1, k + 3);
         __syncthreads();
         multiply(1);
-        if (k + 2 >= ks) break;
+        if (k + 2 >= steps) break;
         stage(0);
         load(0, k + 4);
         __syncthreads();
@@ -479,35 +536,21 @@ template <int P, int TI, int TJ, Phase phase> __global__ void __launch_bounds__(
     __syncthreads();
 
     const int l32 = lane & 31, lk = lane >> 5;
+#pragma unroll 1
+    for (int q = 0; q < TI * TJ; ++q) {
 #pragma unroll
-    for (int x = 0; x < TI; ++x)
+        for (int x = 0; x < TI; ++x)
 #pragma unroll
-        for (int y = 0; y < TJ; ++y) {
-            const int row0 = ti * 64 * TI + (wi * TI + x) * 32, col0 = tj * 64 * TJ + (wj * TJ + y) * 32;
+            for (int y = 0; y < TJ; ++y)
+                if (q == x * TJ + y)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int at = 8 * g + 4 * lk;
-                float v[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = acc[x][y][4 * g + i];
-                finish<P, phase>(j, t, row0 + at, col0 + l32, v);
-                write_down<P, phase>(j, t, step, row0 + at, col0 + l32, v);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) lds.turn[wave][at + i][l32] = v[i];
-            }
-            // squares of as many rows as a tile is wide are computed whole on the diagonal
-            if (symmetric && row0 / (64 * TJ) == tj) continue;
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int at = 8 * g + 4 * lk;
-                float v[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = lds.turn[wave][l32][at + i];
-                write_across<P, phase>(j, t, row0 + l32, col0 + at, v);
-            }
-            __builtin_amdgcn_wave_barrier();
-        }
+                    for (int v = 0; v < 16; ++v) lds.turn[wave][8 * (v / 4) + 4 * lk + v % 4][l32] = acc[x][y][v];
+        __builtin_amdgcn_wave_barrier();
+        const int row0 = ti * 64 * TI + (wi * TI + q / TJ) * 32, col0 = tj * 64 * TJ + (wj * TJ + q % TJ) * 32;
+        // squares of as many rows as a tile is wide are computed whole on the diagonal
+        write_fragment<P, phase>(j, t, step, row0, col0, lds.turn[wave], !(symmetric && row0 / (64 * TJ) == tj));
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 // ---- host
@@ -526,11 +569,11 @@ struct Entry {
     bool skip;
 };
 
-// How the products of a matrix are tiled: 0 tiles of 32, one latency; 1 of 64; 2 of 128.
+// How the products of a matrix are tiled: 0 tiles of 32 x 32, k shared out; 1 of 64 x 64, the same; 2 of 64 x 128 through LDS.  Us for 600 x 600 fp32 157 and 223
+// (0 and 1), 1000 x 1000 333 and 326, bf16 231 and 240; 1500 x 1800 fp32 925 and 1030 (1 and 2), 2048 x 2048 1562 and 1340.
 int kind_of(int64_t rows, int64_t cols) {
-    const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
-    if (n <= 512) return 0;
-    return up(m, 128) * up(n, 128) >= int64_t(256) * 128 * 128 ? 2 : 1;
+    const double m = double(rows < cols ? rows : cols), n = double(rows < cols ? cols : rows), work = m * m * n;
+    return work <= 1.0e9 ? 0 : work <= 6.0e9 ? 1 : 2;
 }
 int64_t tile_of_kind(int kind) { return kind == 0 ? 32 : kind == 1 ? 64 : 128; }
 
@@ -556,10 +599,9 @@ Sizes sizes_of(int64_t rows, int64_t cols, int32_t dtype) {
 
 template <int P, Phase phase> int launch_products(const Job &j, int kind, int step, int64_t blocks, hipStream_t stream) {
     if (blocks > INT32_MAX / kThreads) return GNN_ERR_UNSUPPORTED;
-    constexpr int TI = phase == kGram || phase == kPolynomial ? 1 : 2;
     if (kind == 0) split_product_kernel<P, phase, 1><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
     else if (kind == 1) split_product_kernel<P, phase, 2><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
-    else product_kernel<P, TI, 2, phase><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
+    else product_kernel<P, 1, 2, P == 3 ? 1 : 2, phase><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
     GNN_HIP_TRY(hipGetLastError());
     return GNN_OK;
 }
@@ -603,8 +645,9 @@ int orthogonalize(Entry (*at)(const void *, int64_t), const void *list, int64_t 
                 const Sizes s = sizes_of(e.rows, e.cols, e.dtype);
                 if (s.kind != kind || s.parts != parts) continue;
                 const int64_t tile = tile_of_kind(kind), across = s.mp / tile;
-                // (large symmetric results: two tiles of half the height for each square one)
-                const int64_t more[kLaunches] = {s.norm_blocks, s.mp / 64 * (s.np / 64), across * (across + 1) / (kind == 2 ? 1 : 2), across * (s.np / tile)};
+                // (large ones: two tiles of half the height for each square one)
+                const int64_t more[kLaunches] = {s.norm_blocks, s.mp / 64 * (s.np / 64), across * (across + 1) / (kind == 2 ? 1 : 2),
+                                                 across * (s.np / tile) * (kind == 2 ? 2 : 1)};
                 bool full = matrices == kMats;
                 for (int i = 0; i < kLaunches; ++i) full |= blocks[i] + more[i] > INT32_MAX / kThreads;
                 if (full) {
