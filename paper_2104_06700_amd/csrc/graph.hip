@@ -206,17 +206,17 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const uint32_t
     }
 }
 
-// vals_in null: the value of pair i is i.  inverse: vals_out[value] = place of the pair, and no keys are written
+// totals: of the digits, where the table holds the places among pairs of the same digit; null: it holds the places.  vals_in null: the value of pair i is i.  inverse: vals_out[value] = place of the pair, and no keys are written
 template <bool INVERSE>
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const uint32_t *__restrict__ keys_in,
                                                                     const uint32_t *__restrict__ vals_in, int64_t n, int shift,
                                                                     uint32_t from_top, int64_t n_tiles,
-                                                                    const uint32_t *__restrict__ table,
+                                                                    const uint32_t *__restrict__ table, const uint32_t *__restrict__ totals,
                                                                     uint32_t *__restrict__ keys_out, uint32_t *__restrict__ vals_out) {
     __shared__ uint32_t hist[kSortWaves][256];  // pairs per wavefront and digit, then those of the wavefronts before
     __shared__ uint32_t digit_begin[256];       // first place of a digit in the tile
     __shared__ uint32_t digit_out[256];         // its first place in the output, minus that
-    __shared__ uint32_t wave_total[4];
+    __shared__ uint32_t wave_total[4], wave_all[4];
     __shared__ uint32_t sorted_key[kSortTile], sorted_val[kSortTile];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int d = threadIdx.x; d < kSortWaves * 256; d += kSortThreads) (&hist[0][0])[d] = 0;
@@ -256,14 +256,22 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const uint32
         const uint32_t upto = wave_scan_inclusive(total);
         if (lane == 63) wave_total[wave] = upto;
         digit_begin[d] = upto - total;
+        if (totals) {
+            const uint32_t all = totals[d], all_upto = wave_scan_inclusive(all);
+            if (lane == 63) wave_all[wave] = all_upto;
+            digit_out[d] = all_upto - all;
+        }
     }
     __syncthreads();
     if (threadIdx.x < 256) {
         const int d = threadIdx.x;
-        uint32_t begin = digit_begin[d];
-        for (int w = 0; w < wave; ++w) begin += wave_total[w];
+        uint32_t begin = digit_begin[d], first = totals ? digit_out[d] : 0u;
+        for (int w = 0; w < wave; ++w) {
+            begin += wave_total[w];
+            if (totals) first += wave_all[w];
+        }
         digit_begin[d] = begin;
-        digit_out[d] = table[int64_t(d) * n_tiles + blockIdx.x] - begin;
+        digit_out[d] = first + table[int64_t(d) * n_tiles + blockIdx.x] - begin;
     }
     __syncthreads();
 #pragma unroll
@@ -286,6 +294,28 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const uint32
             vals_out[out] = v;
         }
     }
+}
+
+// Few tiles: a workgroup scans the row of a digit and leaves its total behind, and the tiles add up the totals of the digits before.  One launch a pass instead of two.
+constexpr int64_t kRowScanTiles = 4096;
+__global__ void __launch_bounds__(256) sort_rows_kernel(uint32_t *__restrict__ table, int64_t n_tiles, uint32_t *__restrict__ totals) {
+    __shared__ uint32_t wave_total[4];
+    uint32_t *row = table + int64_t(blockIdx.x) * n_tiles;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t before = 0;
+    for (int64_t t0 = 0; t0 < n_tiles; t0 += 256) {
+        const int64_t t = t0 + threadIdx.x;
+        const uint32_t c = t < n_tiles ? row[t] : 0u;
+        const uint32_t upto = wave_scan_inclusive(c);
+        if (lane == 63) wave_total[wave] = upto;
+        __syncthreads();
+        uint32_t lower = before;
+        for (int w = 0; w < wave; ++w) lower += wave_total[w];
+        if (t < n_tiles) row[t] = lower + upto - c;
+        before += wave_total[0] + wave_total[1] + wave_total[2] + wave_total[3];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) totals[blockIdx.x] = before;
 }
 
 // Sorts n pairs by the low `bits` bits of the key.
@@ -311,12 +341,18 @@ int radix_sort(const SortJob &job, int64_t n, int bits, uint32_t *table, uint32_
         uint32_t *kout = last && job.last_keys ? job.last_keys : job.buf_k[cur ^ 1];
         uint32_t *vout = last && job.last_vals ? job.last_vals : job.buf_v[cur ^ 1];
         sort_count_kernel<<<grid, kSortThreads, 0, stream>>>(kin, n, shift, from_top, n_tiles, table);
-        const int rc = scan_exclusive<uint32_t>(table, n_tiles * 256, 1, 0, false, sums, stream);
-        if (rc != GNN_OK) return rc;
+        const bool rows = n_tiles <= kRowScanTiles;
+        if (rows) {
+            sort_rows_kernel<<<256, 256, 0, stream>>>(table, n_tiles, sums);
+        } else {
+            const int rc = scan_exclusive<uint32_t>(table, n_tiles * 256, 1, 0, false, sums, stream);
+            if (rc != GNN_OK) return rc;
+        }
+        const uint32_t *totals = rows ? sums : nullptr;
         if (last && job.inverse_last)
-            sort_scatter_kernel<true><<<grid, kSortThreads, 0, stream>>>(kin, vin, n, shift, from_top, n_tiles, table, kout, vout);
+            sort_scatter_kernel<true><<<grid, kSortThreads, 0, stream>>>(kin, vin, n, shift, from_top, n_tiles, table, totals, kout, vout);
         else
-            sort_scatter_kernel<false><<<grid, kSortThreads, 0, stream>>>(kin, vin, n, shift, from_top, n_tiles, table, kout, vout);
+            sort_scatter_kernel<false><<<grid, kSortThreads, 0, stream>>>(kin, vin, n, shift, from_top, n_tiles, table, totals, kout, vout);
         if (hipGetLastError() != hipSuccess) return GNN_ERR_LAUNCH;
         kin = kout;
         vin = vout;
@@ -408,7 +444,10 @@ int gnn_radix_sort_positions(uint32_t *buf_k[2], uint32_t *buf_v[2], int64_t n, 
     return radix_sort(job, n, bits, table, sums, stream, keys, positions);
 }
 int64_t gnn_sort_table_elems(int64_t n) { return (n + kSortTile - 1) / kSortTile * 256; }
-int64_t gnn_sort_sums_elems(int64_t n) { return gnn_scan_sums_elems(gnn_sort_table_elems(n)); }
+int64_t gnn_sort_sums_elems(int64_t n) {  // (256: the totals of the digits)
+    const int64_t sums = gnn_scan_sums_elems(gnn_sort_table_elems(n));
+    return sums > 256 ? sums : 256;
+}
 int64_t gnn_scan_sums_elems(int64_t n) { return (n + kScanChunk - 1) / kScanChunk + 1; }
 int gnn_scan_exclusive_u32(uint32_t *data, int64_t n, uint32_t *sums, hipStream_t stream) {
     return scan_exclusive<uint32_t>(data, n, 1, 0, false, sums, stream);

@@ -125,6 +125,7 @@ struct Grad {
     uint32_t *flags;              // [blocks]
     int64_t rows, n, ldt, ldy, sum_blocks, zero_blocks;
     int32_t f, vectors, lanes_log2, run;
+    uint32_t reciprocal;          // ceil(2^32 / vectors)
     int32_t accumulate;
     float scale;
 };
@@ -184,7 +185,7 @@ template <typename TT, int E> __device__ __forceinline__ void write_sum(const Gr
 #pragma unroll
     for (int j = 0; j < E; ++j) x[j] = sum[j] * a.scale;
     if (!a.accumulate) {
-        store_vector<TT, E, false>(p, x);
+        store_vector<TT, E, true>(p, x);
     } else if (own == E) {
         Vector<TT, E> old;
         old.load(p);
@@ -221,13 +222,13 @@ template <typename TT, int E> __device__ __forceinline__ void zero_rows(const Gr
     __syncthreads();
     TT *p = static_cast<TT *>(a.dtable) + v0 * a.ldt;
     const float zero[E] = {};
-    const int lanes = 1 << a.lanes_log2;
-    for (int r = int(threadIdx.x) >> a.lanes_log2; r < rows; r += kThreads >> a.lanes_log2) {
+    // the rows' vectors side by side over the threads: stores of neighbouring rows meet in the same lines
+    const int64_t items = int64_t(rows) * a.vectors;
+    for (int64_t t = threadIdx.x; t < items; t += kThreads) {
+        const int r = a.vectors == 1 ? int(t) : items < (1 << 16) ? int(__umulhi(uint32_t(t), a.reciprocal)) : int(t / a.vectors);
         if (named[r]) continue;
-        for (int q = int(threadIdx.x) & (lanes - 1); q < a.vectors; q += lanes) {
-            const int c = q * E < a.f - E ? q * E : a.f - E;
-            store_vector<TT, E, true>(p + r * a.ldt + c, zero);
-        }
+        const int q = int(t - int64_t(r) * a.vectors), c = q * E < a.f - E ? q * E : a.f - E;
+        store_vector<TT, E, true>(p + r * a.ldt + c, zero);
     }
 }
 
@@ -263,15 +264,16 @@ template <typename TY, typename TT, int E> __global__ void __launch_bounds__(kTh
         const int64_t end = j0 + a.run < a.n ? j0 + a.run : a.n;
 #pragma unroll 1
         for (int64_t j = j0; j < end; j += kBatch) {
-            // no branch between the loads: what lies behind the end repeats the last position, and ids that name no row are read as well
+            // no branch between the loads: behind the end row 0 is read, and ids that name no row are read as well (both arrays end with a whole batch)
             uint32_t k[kBatch], from[kBatch];
             Vector<TY, E> v[kBatch];
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int64_t at = j + u < end ? j + u : end - 1;
-                k[u] = a.key[at];
-                from[u] = a.order[at];
+            for (int u = 0; u < kBatch; u += 4) {
+                *reinterpret_cast<uint4 *>(k + u) = *reinterpret_cast<const uint4 *>(a.key + j + u);
+                *reinterpret_cast<uint4 *>(from + u) = *reinterpret_cast<const uint4 *>(a.order + j + u);
             }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) from[u] = j + u < end ? from[u] : 0;
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) v[u].load(dy + int64_t(from[u]) * a.ldy);
 #pragma unroll
@@ -385,13 +387,19 @@ template <typename TT, int E> __global__ void __launch_bounds__(kThreads) join_k
     const int own = q * E < a.f - E ? E : a.f - q * E;
     double total[E] = {};
     if (mine) {
-        for (int64_t k = group; k < more; k += groups) {
-            Vector<float, E> v;
-            v.load(a.head + (block + 1 + k) * a.f + c);
-            float x[E];
-            v.get(x);
+        constexpr int U = 4;  // on their way at once
+        for (int64_t k = group; k < more; k += U * groups) {
+            Vector<float, E> v[U];
 #pragma unroll
-            for (int i = 0; i < E; ++i) total[i] += double(x[i]);
+            for (int u = 0; u < U; ++u) v[u].load(a.head + (block + 1 + (k + u * groups < more ? k + u * groups : k)) * a.f + c);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (k + u * groups >= more) break;
+                float x[E];
+                v[u].get(x);
+#pragma unroll
+                for (int i = 0; i < E; ++i) total[i] += double(x[i]);
+            }
         }
     }
     if (more > 1) {
@@ -424,12 +432,12 @@ bool known(int32_t dtype) { return dtype == GNN_F32 || dtype == GNN_BF16; }
 int64_t size_of(int32_t dtype) { return dtype == GNN_F32 ? 4 : 2; }
 bool misaligned(const void *p, int64_t to) { return reinterpret_cast<uintptr_t>(p) % uintptr_t(to) != 0; }
 
-// Elements of a vector: 16 bytes of the narrower type of a lookup, of dY's type in the gradient; one of rows narrower than that.
+// Elements of a vector: 16 bytes of Y or dY; one of rows narrower than that.
 int elements_of(bool eight, int64_t f) { return f >= (eight ? 8 : 4) ? (eight ? 8 : 4) : 1; }
 
 struct Room {  // of the gradient, in words
     int lanes_log2, run;
-    int64_t vectors, chunk, blocks, table, sums, words;
+    int64_t vectors, chunk, blocks, table, sums, padded, words;
 };
 Room room_of(int64_t V, int64_t n, int64_t F, bool eight) {
     Room r;
@@ -441,7 +449,8 @@ Room room_of(int64_t V, int64_t n, int64_t F, bool eight) {
     r.blocks = (n + r.chunk - 1) / r.chunk;
     r.table = gnn_sort_table_elems(n);
     r.sums = gnn_sort_sums_elems(n);
-    r.words = 4 * n + r.table + r.sums + r.blocks * (2 * F + 1);
+    r.padded = (n + kBatch - 1) / kBatch * kBatch;
+    r.words = 4 * r.padded + r.table + r.sums + r.blocks * (2 * F + 1);
     return r;
 }
 
@@ -458,7 +467,8 @@ template <typename TT, typename TY, int E> void launch_lookup(const Lookup &a, h
     lookup_kernel<TT, TY, E><<<grid_of((a.n + a.rows - 1) / a.rows), kThreads, 0, stream>>>(a);
 }
 template <typename TT, typename TY> void lookup(Lookup &a, hipStream_t stream) {
-    constexpr bool eight = sizeof(TT) == 2 || sizeof(TY) == 2;
+    // 16 bytes of Y a thread, so that a wavefront's stores are whole lines (1.2 M rows x 256 bf16 into fp32 362 -> 305 us)
+    constexpr bool eight = sizeof(TY) == 2;
     const int e = elements_of(eight, a.f);
     a.vectors = (a.f + e - 1) / e;
     a.rows = a.vectors >= kThreads * kAtOnce ? 1 : kThreads * kAtOnce / a.vectors;
@@ -531,6 +541,7 @@ extern "C" GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dta
     a.ldy = o.ldy ? o.ldy : F;
     a.f = int32_t(F);
     a.vectors = int32_t(r.vectors);
+    a.reciprocal = r.vectors > 1 ? uint32_t(((uint64_t(1) << 32) + uint64_t(r.vectors) - 1) / uint64_t(r.vectors)) : 0;
     a.lanes_log2 = r.lanes_log2;
     a.run = r.run;
     a.accumulate = o.accumulate;
@@ -539,14 +550,14 @@ extern "C" GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dta
     a.zero_blocks = o.accumulate ? 0 : (V + kZeroRows - 1) / kZeroRows;
     if (n > 0) {
         uint32_t *next = static_cast<uint32_t *>(o.workspace);
+        uint32_t *buf_k[2] = {next, next + r.padded}, *buf_v[2] = {next + 2 * r.padded, next + 3 * r.padded};
+        next += 4 * r.padded;
         a.head = reinterpret_cast<float *>(next);
         next += r.blocks * F;
         a.tail = reinterpret_cast<float *>(next);
         next += r.blocks * F;
         a.flags = next;
         next += r.blocks;
-        uint32_t *buf_k[2] = {next, next + n}, *buf_v[2] = {next + 2 * n, next + 3 * n};
-        next += 4 * n;
         const Ids named{ids, o.ids_is_64, V};
         if (n <= kRankHere) {
             rank_kernel<<<unsigned((n + kRankRows - 1) / kRankRows), kThreads, 0, stream>>>(named, int(n), buf_k[0], buf_v[0]);
