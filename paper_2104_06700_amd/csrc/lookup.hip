@@ -27,6 +27,8 @@ constexpr int kZeroRows = 256;    // rows of a workgroup that zeroes
 constexpr int64_t kMostRows = INT32_MAX, kMostColumns = 1 << 24;
 constexpr unsigned kGridX = 1 << 20;  // workgroups in x: a launch has fewer than 2^32 threads a dimension
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));  // (a vector type may stand for its elements in memory, a struct may not)
+
 // E neighbouring elements in fp32
 template <typename T, int E> struct Vector {
     static constexpr int W = E < gnn_rows<T>::VEC ? E : gnn_rows<T>::VEC;
@@ -153,9 +155,9 @@ __global__ void __launch_bounds__(kThreads) rank_kernel(const Ids ids, int n, ui
     if (i < n) {
         const uint32_t k = all[i];
         for (int j = int(threadIdx.x) / kRankRows * 4; j < n; j += kThreads / kRankRows * 4) {
-            const uint4 t = *reinterpret_cast<const uint4 *>(all + j);
-            count += int(t.x < k || (t.x == k && j < i)) + int(t.y < k || (t.y == k && j + 1 < i)) + int(t.z < k || (t.z == k && j + 2 < i)) +
-                     int(t.w < k || (t.w == k && j + 3 < i));
+            const u32x4 t = *reinterpret_cast<const u32x4 *>(all + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) count += int(t[e] < k || (t[e] == k && j + e < i));
         }
     }
     before[threadIdx.x] = count;
@@ -269,8 +271,12 @@ template <typename TY, typename TT, int E> __global__ void __launch_bounds__(kTh
             Vector<TY, E> v[kBatch];
 #pragma unroll
             for (int u = 0; u < kBatch; u += 4) {
-                *reinterpret_cast<uint4 *>(k + u) = *reinterpret_cast<const uint4 *>(a.key + j + u);
-                *reinterpret_cast<uint4 *>(from + u) = *reinterpret_cast<const uint4 *>(a.order + j + u);
+                const u32x4 ku = *reinterpret_cast<const u32x4 *>(a.key + j + u), pu = *reinterpret_cast<const u32x4 *>(a.order + j + u);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    k[u + e] = ku[e];
+                    from[u + e] = pu[e];
+                }
             }
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) from[u] = j + u < end ? from[u] : 0;

@@ -34,6 +34,7 @@ constexpr int64_t kMostSide = 65536, kMostSteps = 100;
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 struct Mat {
     uint16_t *x, *xt[2], *a, *q;        // planes: X (rows m, k n), X^T (rows n, k m) before and after a step, A and Q
@@ -160,7 +161,7 @@ template <int P> __device__ __forceinline__ void put4(uint16_t *planes, int rows
     for (int i = 0; i < 4; ++i) split<P>(v[i], part[i]);
 #pragma unroll
     for (int q = 0; q < P; ++q)
-        *reinterpret_cast<uint2 *>(p + int64_t(q) * rows * depth) = make_uint2(bf16_pair(part[0][q], part[1][q]), bf16_pair(part[2][q], part[3][q]));
+        *reinterpret_cast<u32x2 *>(p + int64_t(q) * rows * depth) = u32x2{bf16_pair(part[0][q], part[1][q]), bf16_pair(part[2][q], part[3][q])};
 }
 // eight, the first a multiple of eight
 template <int P> __device__ __forceinline__ void put8(uint16_t *planes, int rows, int depth, int row, int k, const float (&v)[8]) {
@@ -182,7 +183,7 @@ template <int P> __device__ __forceinline__ void get4(const uint16_t *planes, in
     for (int i = 0; i < 4; ++i) v[i] = 0.0f;
 #pragma unroll
     for (int q = P - 1; q >= 0; --q) {  // smallest first: the sum is exact
-        const uint2 w = *reinterpret_cast<const uint2 *>(p + int64_t(q) * rows * depth);
+        const u32x2 w = *reinterpret_cast<const u32x2 *>(p + int64_t(q) * rows * depth);
         v[0] += __uint_as_float(w.x << 16);
         v[1] += __uint_as_float(w.x & 0xFFFF0000u);
         v[2] += __uint_as_float(w.y << 16);

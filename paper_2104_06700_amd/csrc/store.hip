@@ -24,6 +24,7 @@ constexpr int kCompareRows = 32;       // rows of a workgroup then
 constexpr int64_t kMostRows = INT32_MAX, kMostColumns = 1 << 24;
 constexpr unsigned kGridX = 1 << 20;   // workgroups in x: a launch has fewer than 2^32 threads a dimension
 
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 
 struct Rows {
@@ -137,8 +138,9 @@ template <typename T, bool COMPARE> __global__ void __launch_bounds__(kThreads) 
             const int32_t id = ids[i];
             bool found = false;
             for (int j = int(threadIdx.x) / kCompareRows * 4; j < n; j += kThreads / kCompareRows * 4) {
-                const int4 t = *reinterpret_cast<const int4 *>(ids + j);  // (behind the last position: not looked at)
-                found |= (t.x == id && j > i) | (t.y == id && j + 1 > i && j + 1 < n) | (t.z == id && j + 2 > i && j + 2 < n) | (t.w == id && j + 3 > i && j + 3 < n);
+                const i32x4 t = *reinterpret_cast<const i32x4 *>(ids + j);  // (behind the last position: not looked at)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) found |= t[e] == id && j + e > i && j + e < n;
             }
             if (found) again[r] = 1;
         }

@@ -126,6 +126,45 @@ def test_sums_that_end_where_runs_and_workgroups_end(n, f):
         assert ((dt.cpu().double() - want).abs() <= SUM * size + 2.0 ** -24 * want.abs()).all()
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F32, BF16)])
+@pytest.mark.parametrize("n,f", [(131072, 16), (150001, 100), (200003, 3), (131073, 260)])
+def test_long_and_short_sums_of_many_positions(n, f, types, accumulate):
+    """Sums of one to some thousand rows side by side, whose positions in the sorted list begin and end at and beside whole runs of 32."""
+    gen = torch.Generator().manual_seed(n)
+    lengths = torch.tensor([0, 0, 1, 1, 1, 2, 3, 31, 32, 33, 61, 62, 63, 64, 65, 95, 96, 97, 255, 256, 257, 1000, 5000])
+    rows = lengths[torch.randint(0, len(lengths), (n,), generator=gen)]
+    rows = rows[:int((rows.cumsum(0) < n - 40).sum())]
+    v = max(len(rows) + 300, n // 20)
+    ids = torch.repeat_interleave(torch.arange(len(rows)), rows)
+    ids = torch.cat([ids, torch.full((20,), -1), torch.full((n - 20 - len(ids),), v - 1)])
+    ids = ids[torch.randperm(n, generator=gen)]
+    dy = torch.randn(n, f, generator=gen).to(types[1]).to(DEV)
+    dt = torch.full((v, f), 3.0, device=DEV, dtype=types[0])
+    ws = torch.empty(gnn.gnn_lookup_workspace_bytes(v, n, f), device=DEV, dtype=torch.uint8)
+    for _ in range(2):
+        dt.fill_(3.0)
+        ws.fill_(255)
+        gnn.gnn_lookup_bwd(ids.to(DEV), dy, dt, scale=0.5, accumulate=accumulate, workspace=ws)
+        want, size = reference(ids, dy, v, 0.5)
+        want = want + 3.0 if accumulate else want
+        bound = SUM * size + (HALF[types[0]] + (2.0 ** -24 if accumulate else 0)) * 1.01 * want.abs() + SUM * HALF[types[0]] * size
+        assert ((dt.cpu().double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("n,v", [(131072, 4096), (131072, 5000000), (200000, 200000)])
+def test_tables_of_other_sizes_than_the_ids(n, v):
+    gen = torch.Generator().manual_seed(n + v)
+    for kind in ("uniform", "hubs", "one", "none"):
+        ids = make_ids(n, v, kind, gen, torch.int32)
+        dy = torch.randn(n, 8, generator=gen).to(DEV)
+        dt = torch.full((v, 8), float("nan"), device=DEV)
+        ws = torch.empty(gnn.gnn_lookup_workspace_bytes(v, n, 8), device=DEV, dtype=torch.uint8)
+        gnn.gnn_lookup_bwd(ids.to(DEV), dy, dt, scale=float("inf") if kind == "none" else 1.0, workspace=ws)
+        want, size = reference(ids, dy, v, 1.0)
+        assert ((dt.cpu().double() - want).abs() <= SUM * size + 2.0 ** -24 * want.abs()).all(), kind
+
+
 def test_what_names_no_row_is_not_read():
     """NaN and infinities in rows whose id names none, and in rows of the table that no id names."""
     ids = torch.tensor([0, -1, 2, 5, 2], dtype=torch.int32, device=DEV)
