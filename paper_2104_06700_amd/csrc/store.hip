@@ -21,6 +21,7 @@ constexpr int kItems = 1024;           // pieces of eight columns of a workgroup
 constexpr int kBlock = GNN_STORE_BLOCK;
 constexpr int64_t kCompareHere = 4096; // positions up to which every workgroup compares its rows' ids with all of them
 constexpr int kCompareRows = 32;       // rows of a workgroup then
+constexpr int kStoreRows = kItems / (kBlock / 8), kLoadRows = kItems;  // of a workgroup at most
 constexpr int64_t kMostRows = INT32_MAX, kMostColumns = 1 << 24;
 constexpr unsigned kGridX = 1 << 20;   // workgroups in x: a launch has fewer than 2^32 threads a dimension
 
@@ -43,6 +44,8 @@ struct Rows {
     }
     __device__ __forceinline__ int row_of(int t) const { return pieces == 1 ? t : rows > 1 ? int(__umulhi(uint32_t(t), reciprocal)) : 0; }
 };
+
+struct Place { int64_t store, x; };  // of a row, from the store's first and from the workgroup's first row of X
 
 __device__ __forceinline__ int64_t block_number() { return int64_t(blockIdx.z) * kGridX + blockIdx.x; }
 
@@ -81,38 +84,50 @@ template <typename T> __device__ __forceinline__ void load8(const T *p, int have
     }
 }
 
+typedef short v2i16 __attribute__((ext_vector_type(2)));
+
+// Four columns in 8 bits, over 2^(e - 127), given as the fp32 number of that exponent (2^-127 as 0): the conversion scales before it rounds, to the bit what a
+// product with the factor followed by a conversion gives, for every finite value and exponent.
+__device__ __forceinline__ uint32_t codes4(const float (&x)[8], int j, float scale) {
+    v2i16 t = {0, 0};
+    t = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(t, x[j], x[j + 1], scale, false);
+    t = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(t, x[j + 2], x[j + 3], scale, true);
+    return __builtin_bit_cast(uint32_t, t);
+}
+
 // Columns 8 q .. 8 q + 8 of a row in 8 bits, with those of the three threads beside this one.
-__device__ __forceinline__ void write8(const Rows &a, int64_t id, int q, const float (&x)[8]) {
+__device__ __forceinline__ void write8(const Rows &a, int64_t offset, int q, const float (&x)[8]) {
     const int c = q * 8, left = a.f - c, have = left < 0 ? 0 : left < 8 ? left : 8;
     uint32_t top = 0;
-    bool odd = false;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const uint32_t b = __float_as_uint(x[j]) & 0x7FFFFFFFu;
-        const bool finite = b < 0x7F800000u;
-        odd |= !finite;
-        top = finite && b > top ? b : top;
+        top = b > top ? b : top;
+    }
+    const bool odd = top >= 0x7F800000u;
+    if (odd) {
+        top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t b = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+            top = b < 0x7F800000u && b > top ? b : top;
+        }
     }
     const uint32_t other = __float_as_uint(gnn_from_lane<0xB1>(__uint_as_float(top)));  // the other of a pair
     top = other > top ? other : top;
     const uint32_t pair = __float_as_uint(gnn_from_lane<0x4E>(__uint_as_float(top)));   // the other pair of four
     top = pair > top ? pair : top;
-    int e = int(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    int e = int((top + 0x1FFFFFu) >> 23) - 8;  // (a mantissa above 0x600000 carries)
     e = e > 0 ? e : 0;
-    const float factor = __uint_as_float(uint32_t(254 - e) << 23);
-    uint32_t w[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        int t4 = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k] * factor, x[4 * k + 1] * factor, 0, false);
-        w[k] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k + 2] * factor, x[4 * k + 3] * factor, t4, true));
-    }
+    const float scale = __uint_as_float(uint32_t(e) << 23);
+    uint32_t w[2] = {codes4(x, 0, scale), codes4(x, 4, scale)};
     if (odd)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if ((__float_as_uint(x[j]) & 0x7FFFFFFFu) >= 0x7F800000u) w[j / 4] |= 0x7Fu << (8 * (j % 4));
-    uint8_t *to = a.store + id * a.lds;
+    uint8_t *to = a.store + offset;
     if (have == 8) {
-        *reinterpret_cast<u32x2_any *>(to + c) = u32x2_any{w[0], w[1]};
+        __builtin_nontemporal_store(u32x2_any{w[0], w[1]}, reinterpret_cast<u32x2_any *>(to + c));
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -127,6 +142,9 @@ template <typename T, bool COMPARE> __global__ void __launch_bounds__(kThreads) 
     const int rows = a.n - row0 < a.rows ? int(a.n - row0) : a.rows;
     __shared__ __attribute__((aligned(16))) int32_t ids[COMPARE ? kCompareHere : 4];
     __shared__ int again[kCompareRows];  // a later position has this row's id
+    __shared__ Place places[kStoreRows];
+    __shared__ int written;
+    if (threadIdx.x == 0) written = 0;
     if constexpr (COMPARE) {
         const int n = int(a.n);
         for (int j = int(threadIdx.x); j < n; j += kThreads) ids[j] = int32_t(a.id(j));
@@ -144,37 +162,43 @@ template <typename T, bool COMPARE> __global__ void __launch_bounds__(kThreads) 
             }
             if (found) again[r] = 1;
         }
-        __syncthreads();
     }
-    const int items = rows * a.pieces;
+    __syncthreads();
+    // the rows that are written, in any order
+    for (int r = int(threadIdx.x); r < rows; r += kThreads) {
+        int64_t id;
+        bool stays;
+        if constexpr (COMPARE) {
+            id = ids[row0 + r];
+            stays = id >= 0 && !again[r];
+        } else {
+            id = a.id(row0 + r);
+            stays = id >= 0 && (!a.last || a.last[id] == int32_t(row0 + r));
+        }
+        if (stays) places[atomicAdd(&written, 1)] = {id * a.lds, r * a.ldx};
+    }
+    __syncthreads();
+    const T *x0 = static_cast<const T *>(a.x) + row0 * a.ldx;
+    const int items = written * a.pieces;
     constexpr int U = 4;
     for (int t0 = int(threadIdx.x); t0 < items; t0 += kThreads * U) {  // (pieces is a multiple of four: the threads of a block take part together)
-        int64_t id[U];
-        int row[U], last[U];
+        Place at[U];
+        int q[U];
         float x[U][8];
-        // the ids and what is known of them, then the rows that are written, all on their way at once
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int t = t0 + u * kThreads < items ? t0 + u * kThreads : items - 1;
-            row[u] = a.row_of(t);
-            id[u] = a.id(row0 + row[u]);
+            const int t = t0 + u * kThreads < items ? t0 + u * kThreads : items - 1, row = a.row_of(t);
+            q[u] = t - row * a.pieces;
+            at[u] = places[row];
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if constexpr (COMPARE) last[u] = again[row[u]] ? -1 : int(row0) + row[u];
-            else last[u] = a.last ? a.last[id[u] < 0 ? 0 : id[u]] : int32_t(row0 + row[u]);
+            const int left = a.f - q[u] * 8, have = left < 0 ? 0 : left < 8 ? left : 8;
+            load8<T>(x0 + at[u].x + q[u] * 8, have, x[u]);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (t0 + u * kThreads >= items || last[u] != int32_t(row0 + row[u])) id[u] = -1;
-            const int q = t0 + u * kThreads - row[u] * a.pieces, left = a.f - q * 8, have = left < 0 ? 0 : left < 8 ? left : 8;
-            if (id[u] >= 0) load8<T>(static_cast<const T *>(a.x) + (row0 + row[u]) * a.ldx + q * 8, have, x[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int q = t0 + u * kThreads - row[u] * a.pieces;
-            if (id[u] >= 0) write8(a, id[u], q, x[u]);
-        }
+        for (int u = 0; u < U; ++u)
+            if (t0 + u * kThreads < items) write8(a, at[u].store, q[u], x[u]);
     }
 }
 
@@ -188,6 +212,24 @@ __device__ __forceinline__ float decoded(uint32_t w, int j, int e) {
     else x = __builtin_amdgcn_cvt_f32_fp8(int(w), 3);
     return __builtin_amdgcn_ldexpf(x, e - 127);
 }
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+// eight columns of one exponent below 255, as they lie in memory: two codes an instruction
+__device__ __forceinline__ void put8(float *to, const uint32_t (&w)[2], float scale) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[k], scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[k], scale, true);
+        __builtin_nontemporal_store(gnn_f32x4{lo.x, lo.y, hi.x, hi.y}, reinterpret_cast<gnn_f32x4 *>(to + 4 * k));
+    }
+}
+__device__ __forceinline__ void put8(gnn_bf16 *to, const uint32_t (&w)[2], float scale) {
+    gnn_u32x4 v;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        v[2 * k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[k], scale, false));
+        v[2 * k + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[k], scale, true));
+    }
+    __builtin_nontemporal_store(v, reinterpret_cast<gnn_u32x4 *>(to));
+}
 
 // E columns a thread: eight, or one of rows narrower than that
 template <typename T, int E> __global__ void __launch_bounds__(kThreads) load_kernel(const Rows a) {
@@ -195,13 +237,19 @@ template <typename T, int E> __global__ void __launch_bounds__(kThreads) load_ke
     const int64_t row0 = block_number() * a.rows;
     if (row0 >= a.n) return;
     const int rows = a.n - row0 < a.rows ? int(a.n - row0) : a.rows;
+    __shared__ int64_t places[kLoadRows];  // where a row is in the store, -1: nowhere
+    for (int r = int(threadIdx.x); r < rows; r += kThreads) {
+        const int64_t id = a.id(row0 + r);
+        places[r] = id < 0 ? -1 : id * a.lds;
+    }
+    __syncthreads();
     const int items = rows * a.pieces;
     T *y = static_cast<T *>(a.x) + row0 * a.ldx;
     for (int t0 = int(threadIdx.x); t0 < items; t0 += kThreads * U) {
-        int64_t id[U];
+        int64_t at[U];
         int row[U], col[U];
         u32x2_any w[U];
-        uint8_t e[U][2];
+        uint8_t e[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             // no branch between the loads: what lies behind the end repeats the last piece, and an id that names no row reads row 0
@@ -209,40 +257,33 @@ template <typename T, int E> __global__ void __launch_bounds__(kThreads) load_ke
             row[u] = a.row_of(t);
             const int c = (t - row[u] * a.pieces) * E;
             col[u] = c < a.f - E ? c : a.f - E;  // the last piece ends with the row
-            id[u] = a.id(row0 + row[u]);
+            at[u] = places[row[u]];
         }
         if (a.v > 0)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const uint8_t *p = a.store + (id[u] < 0 ? 0 : id[u]) * a.lds;
+                const uint8_t *p = a.store + (at[u] < 0 ? 0 : at[u]);
                 if constexpr (E == 8) w[u] = *reinterpret_cast<const u32x2_any *>(p + col[u]);
                 else w[u].x = p[col[u]];
-                e[u][0] = p[a.f + col[u] / kBlock];
-                e[u][1] = p[a.f + (col[u] + E - 1) / kBlock];  // of another block where the last piece reaches over its end
+                e[u] = p[a.f + col[u] / kBlock];
             }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (t0 + u * kThreads >= items) break;
-            T *to = y + int64_t(row[u]) * a.ldx + col[u];
-            float x[E];
-            if (id[u] < 0) {
-#pragma unroll
-                for (int j = 0; j < E; ++j) x[j] = 0.0f;
+            T *to = y + row[u] * a.ldx + col[u];
+            if constexpr (E == 1) {
+                gnn_rows<T>::set(to, at[u] < 0 ? 0.0f : decoded(w[u].x, 0, e[u]));
             } else {
                 const int first = kBlock - col[u] % kBlock;  // columns of the first block
+                uint32_t c[2] = {w[u].x, w[u].y};
+                int e0 = e[u];
+                if (at[u] < 0) c[0] = c[1] = 0, e0 = 127;
+                if ((first >= E || at[u] < 0) && e0 < 255) {
+                    put8(to, c, __uint_as_float(uint32_t(e0) << 23));
+                } else {  // the last piece reaches over a block's end, or an exponent whose power of two fp32 does not have
+                    const int e1 = a.store[at[u] + a.f + (col[u] + E - 1) / kBlock];
 #pragma unroll
-                for (int j = 0; j < E; ++j) x[j] = decoded(j < 4 ? w[u].x : w[u].y, j % 4, j < first ? e[u][0] : e[u][1]);
-            }
-            if constexpr (E == 1) {
-                gnn_rows<T>::set(to, x[0]);
-            } else {
-                constexpr int W = gnn_rows<T>::VEC;
-#pragma unroll
-                for (int k = 0; k < E / W; ++k) {
-                    float v[W];
-#pragma unroll
-                    for (int j = 0; j < W; ++j) v[j] = x[k * W + j];
-                    gnn_store_row<T, W, true>(to + k * W, v);
+                    for (int j = 0; j < E; ++j) gnn_rows<T>::set(to + j, decoded(c[j / 4], j % 4, j < first ? e0 : e1));
                 }
             }
         }
