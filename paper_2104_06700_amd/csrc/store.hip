@@ -22,6 +22,7 @@ constexpr int kBlock = GNN_STORE_BLOCK;
 constexpr int64_t kCompareHere = 4096; // positions up to which every workgroup compares its rows' ids with all of them
 constexpr int kCompareRows = 32;       // rows of a workgroup then
 constexpr int kStoreRows = kItems / (kBlock / 8), kLoadRows = kItems;  // of a workgroup at most
+constexpr int kPartsLog2 = 3, kParts = 1 << kPartsLog2, kChunk = 512;
 constexpr int64_t kMostRows = INT32_MAX, kMostColumns = 1 << 24;
 constexpr unsigned kGridX = 1 << 20;   // workgroups in x: a launch has fewer than 2^32 threads a dimension
 
@@ -51,18 +52,30 @@ __device__ __forceinline__ int64_t block_number() { return int64_t(blockIdx.z) *
 
 // ---- the last position of every id
 
+// Workgroup b takes the ids that share lines of `last` with others of part b mod 8, of chunk b / 8 of the positions: workgroups of one part run on one
+// XCD and begin in order, so that its L2 has whole lines and mostly the last position already when the first pass ends.
+__device__ __forceinline__ bool mine(int64_t id) { return id >= 0 && ((id >> 5) & (kParts - 1)) == int(blockIdx.x & (kParts - 1)); }
+
 __global__ void __launch_bounds__(kThreads) enter_kernel(const Rows a) {
-    const int64_t i = block_number() * kThreads + threadIdx.x;
-    if (i >= a.n) return;
-    const int64_t id = a.id(i);
-    if (id >= 0) a.last[id] = int32_t(i);  // of several any one
+    const int64_t i0 = (block_number() >> kPartsLog2) * kChunk + threadIdx.x;
+    int64_t id[kChunk / kThreads];
+#pragma unroll
+    for (int u = 0; u < kChunk / kThreads; ++u) id[u] = i0 + u * kThreads < a.n ? a.id(i0 + u * kThreads) : -1;
+#pragma unroll
+    for (int u = 0; u < kChunk / kThreads; ++u)
+        if (mine(id[u])) a.last[id[u]] = int32_t(i0 + u * kThreads);  // of several any one
 }
 __global__ void __launch_bounds__(kThreads) raise_kernel(const Rows a) {
-    // from the last position on: of an id that comes often most then find a later one there
-    const int64_t i = a.n - 1 - (block_number() * kThreads + threadIdx.x);
-    if (i < 0) return;
-    const int64_t id = a.id(i);
-    if (id >= 0 && a.last[id] < int32_t(i)) atomicMax(&a.last[id], int32_t(i));
+    const int64_t i0 = a.n - 1 - ((block_number() >> kPartsLog2) * kChunk + threadIdx.x);
+    int64_t id[kChunk / kThreads];
+    int32_t last[kChunk / kThreads];
+#pragma unroll
+    for (int u = 0; u < kChunk / kThreads; ++u) id[u] = i0 - u * kThreads >= 0 ? a.id(i0 - u * kThreads) : -1;
+#pragma unroll
+    for (int u = 0; u < kChunk / kThreads; ++u) last[u] = mine(id[u]) ? a.last[id[u]] : INT32_MAX;
+#pragma unroll
+    for (int u = 0; u < kChunk / kThreads; ++u)
+        if (last[u] < int32_t(i0 - u * kThreads)) atomicMax(&a.last[id[u]], int32_t(i0 - u * kThreads));
 }
 
 // ---- writing
@@ -345,7 +358,7 @@ extern "C" GNN_API int gnn_store_rows(const void *X, const void *ids, void *stor
     hipStream_t stream = static_cast<hipStream_t>(o.stream);
     if (twice && !compare) {
         a.last = static_cast<int32_t *>(o.workspace);
-        const dim3 grid = grid_of((n + kThreads - 1) / kThreads);
+        const dim3 grid = grid_of((n + kChunk - 1) / kChunk << kPartsLog2);
         enter_kernel<<<grid, kThreads, 0, stream>>>(a);
         raise_kernel<<<grid, kThreads, 0, stream>>>(a);
         GNN_HIP_TRY(hipGetLastError());
