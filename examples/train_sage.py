@@ -4,6 +4,7 @@ of the labelled vertices and AdamW over all parameters.
     python examples/train_sage.py                                   # 24 thousand vertices, three layers
     python examples/train_sage.py --scale 1.0 --steps 5             # 2.4 million vertices
     python examples/train_sage.py --embedding --state-bits 8        # learned vertex embeddings, optimizer states in 8 bits
+    python examples/train_sage.py --muon                            # weight matrices by orthogonalised updates, the rest by AdamW
 
 The graph is a seeded synthetic one; the labels are those of a random teacher on the aggregated features, so there is something to
 learn.  Everything a step needs is allocated once; a step is nothing but library calls.
@@ -29,8 +30,9 @@ import synth  # noqa: E402
 class Trainer:
     """Parameters, activations, gradients and states of a model on one graph."""
 
-    def __init__(self, graph, x, labels, widths, groups=8, embedding=False, state_bits=32, lr=1e-2, weight_decay=1e-2, seed=0):
-        self.g, self.x, self.labels, self.widths, self.groups, self.lr = graph, x, labels, widths, groups, lr
+    def __init__(self, graph, x, labels, widths, groups=8, embedding=False, state_bits=32, lr=1e-2, weight_decay=1e-2, seed=0, muon=False,
+                 muon_lr=2e-2):
+        self.g, self.x, self.labels, self.widths, self.groups, self.lr, self.muon_lr = graph, x, labels, widths, groups, lr, muon_lr
         n, dev = graph.n, x.device
         gen = torch.Generator(device=dev)
         gen.manual_seed(seed)
@@ -53,12 +55,14 @@ class Trainer:
             self.layers.append(l)
         self.dx = torch.empty_like(x) if embedding else None
         room = max(room, gnn.gnn_softmax_xent_workspace_bytes(n, widths[-1]))
-        self.workspace = torch.empty(room, device=dev, dtype=torch.uint8)
         self.loss = new(1)
-        self.optimizer(embedding, state_bits, weight_decay)
+        self.optimizer(embedding, state_bits, weight_decay, muon)
+        if self.muon is not None:
+            room = max(room, gnn.gnn_muon_workspace_bytes(self.muon))
+        self.workspace = torch.empty(room, device=dev, dtype=torch.uint8)
 
-    def optimizer(self, embedding, bits, weight_decay):
-        """Weights (decayed) and embeddings hold their states in `bits` bits, vectors in 32."""
+    def optimizer(self, embedding, bits, weight_decay, muon):
+        """Weights (decayed) and embeddings hold AdamW's states in `bits` bits, vectors in 32; with muon the weights have a momentum instead."""
         params, grads, decay = [], [], []
         if embedding:
             params, grads, decay = [self.x], [self.dx], [0.0]
@@ -70,13 +74,18 @@ class Trainer:
                 params += [l["gamma"], l["beta"]]
                 grads += [l["dgamma"], l["dbeta"]]
                 decay += [0.0, 0.0]
+        self.params, self.grads, self.muon = params, grads, None
+        if muon:
+            self.momentum = [torch.zeros_like(l["w"]) for l in self.layers]
+            self.muon = gnn.MuonTensors([l["w"] for l in self.layers], [l["dw"] for l in self.layers], self.momentum, weight_decay=weight_decay)
+            weights = [id(l["w"]) for l in self.layers]
+            params, grads, decay = zip(*[t for t in zip(params, grads, decay) if id(t[0]) not in weights])
         m, v, ms, vs = [], [], [], []
         for p in params:
             eight = bits == 8 and p.dim() == 2
             for states, scales in ((m, ms), (v, vs)):
                 states.append(torch.zeros(p.shape, device=p.device).to(torch.float8_e4m3fn) if eight else torch.zeros_like(p))
                 scales.append(torch.zeros(-(-p.numel() // gnn.GNN_ADAMW_BLOCK), device=p.device) if eight else None)
-        self.params, self.grads = params, grads
         self.tensors = gnn.AdamWTensors(params, grads, m, v, ms, vs, weight_decay=decay)
         self.steps = 0
 
@@ -105,12 +114,17 @@ class Trainer:
         self.forward()
         self.backward()
         self.steps += 1
-        gnn.gnn_adamw_step(self.tensors, self.steps, self.lr)
+        self.update()
         return self.loss
 
+    def update(self):
+        gnn.gnn_adamw_step(self.tensors, self.steps, self.lr)
+        if self.muon is not None:
+            gnn.gnn_muon_step(self.muon, self.muon_lr, workspace=self.workspace)
 
-def make(scale=0.01, widths=(100, 256, 256, 47), labelled=0.08, seed=3, device="cuda:0", **kw):
-    """A trainer on the synthetic 2.4-million-vertex graph times `scale`."""
+
+def data(scale, widths, labelled=0.08, seed=3, device="cuda:0"):
+    """The synthetic 2.4-million-vertex graph times `scale`, its edges, features and labels."""
     el = synth.make_graph("rmat_sparse_stack", device=device, scale=scale, seed=seed)
     graph = gnn.build_device_graph(el.dst, el.src, el.n)
     x = synth.normal_features(el.n, widths[0], seed, device=device)
@@ -120,6 +134,12 @@ def make(scale=0.01, widths=(100, 256, 256, 47), labelled=0.08, seed=3, device="
     gnn.gnn_matmul(z, synth.normal_features(widths[0], widths[-1], seed + 1, device=device), scores)
     labels = scores.argmax(1).to(torch.int32)
     labels[synth.uniform_features(el.n, 1, seed + 2, device=device).view(-1) >= 2 * labelled - 1] = -1
+    return graph, el.dst, el.src, x, labels
+
+
+def make(scale=0.01, widths=(100, 256, 256, 47), labelled=0.08, seed=3, device="cuda:0", **kw):
+    """A trainer on the synthetic graph."""
+    graph, _, _, x, labels = data(scale, widths, labelled, seed, device)
     return Trainer(graph, x, labels, widths, **kw)
 
 
@@ -132,8 +152,11 @@ def main():
     ap.add_argument("--lr", type=float, default=1e-2)
     ap.add_argument("--embedding", action="store_true", help="the input features are parameters too")
     ap.add_argument("--state-bits", type=int, choices=(8, 32), default=32)
+    ap.add_argument("--muon", action="store_true", help="weight matrices by Muon, the rest by AdamW")
+    ap.add_argument("--muon-lr", type=float, default=2e-2)
     a = ap.parse_args()
-    t = make(a.scale, tuple(int(f) for f in a.widths.split(",")), groups=a.groups, lr=a.lr, embedding=a.embedding, state_bits=a.state_bits)
+    t = make(a.scale, tuple(int(f) for f in a.widths.split(",")), groups=a.groups, lr=a.lr, embedding=a.embedding, state_bits=a.state_bits,
+             muon=a.muon, muon_lr=a.muon_lr)
     print(f"{t.g.n} vertices, {t.g.e} edges, {sum(p.numel() for p in t.params)} parameters", flush=True)
     for k in range(a.steps):
         torch.cuda.synchronize()
