@@ -25,6 +25,8 @@ constexpr int64_t kRankHere = 4096; // positions up to which every workgroup fin
 constexpr int kRankRows = 32;     // of a workgroup then
 constexpr int kZeroRows = 256;    // rows of a workgroup that zeroes
 constexpr int64_t kMostRows = INT32_MAX, kMostColumns = 1 << 24;
+constexpr int64_t kMostSlices = 65535;  // workgroups in y: pieces of a row of as many vectors as a group has lanes
+static_assert((kMostColumns / 4 + 127) / 128 <= kMostSlices, "the widest rows");
 constexpr unsigned kGridX = 1 << 20;  // workgroups in x: a launch has fewer than 2^32 threads a dimension
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));  // (a vector type may stand for its elements in memory, a struct may not)
@@ -144,9 +146,16 @@ __global__ void __launch_bounds__(kThreads) key_kernel(const Ids ids, int64_t n,
 __global__ void __launch_bounds__(kThreads) rank_kernel(const Ids ids, int n, uint32_t *__restrict__ key, uint32_t *__restrict__ order) {
     __shared__ __attribute__((aligned(16))) uint32_t all[kRankHere];
     __shared__ int before[kThreads];
-    for (int j = int(threadIdx.x); j < (n + 3) / 4 * 4; j += kThreads) {
-        const int64_t v = j < n ? ids.at(j) : int64_t(UINT32_MAX);  // behind the last: after all others
-        all[j] = uint32_t(v < 0 ? ids.rows : v);
+    const int fours = (n + 3) / 4;
+    for (int j0 = int(threadIdx.x); j0 < fours * 4; j0 += 4 * kThreads) {
+        int64_t v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = ids.at(j0 + u * kThreads < n ? j0 + u * kThreads : n - 1);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int j = j0 + u * kThreads;
+            if (j < fours * 4) all[j] = j >= n ? UINT32_MAX : uint32_t(v[u] < 0 ? ids.rows : v[u]);  // behind the last: after all others
+        }
     }
     __syncthreads();
     // a thread a position and an eighth of the others, four at a time
@@ -154,6 +163,7 @@ __global__ void __launch_bounds__(kThreads) rank_kernel(const Ids ids, int n, ui
     int count = 0;
     if (i < n) {
         const uint32_t k = all[i];
+#pragma unroll 4
         for (int j = int(threadIdx.x) / kRankRows * 4; j < n; j += kThreads / kRankRows * 4) {
             const u32x4 t = *reinterpret_cast<const u32x4 *>(all + j);
 #pragma unroll
@@ -449,7 +459,7 @@ Room room_of(int64_t V, int64_t n, int64_t F, bool eight) {
     Room r;
     const int e = elements_of(eight, F);
     r.vectors = (F + e - 1) / e;
-    r.lanes_log2 = r.vectors >= 64 ? 6 : gnn_ilog2_ceil(r.vectors);
+    r.lanes_log2 = r.vectors > kMostSlices * 64 ? 7 : r.vectors >= 64 ? 6 : gnn_ilog2_ceil(r.vectors);
     r.run = n >= kLong ? kRun : kBatch;
     r.chunk = int64_t(kThreads >> r.lanes_log2) * r.run;
     r.blocks = (n + r.chunk - 1) / r.chunk;
@@ -581,7 +591,6 @@ extern "C" GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dta
         }
     }
     const int64_t slices = (r.vectors + (int64_t(1) << r.lanes_log2) - 1) >> r.lanes_log2;
-    if (slices > 65535) return GNN_ERR_UNSUPPORTED;
     if (o.dtype == GNN_F32) return o.table_dtype == GNN_F32 ? grad<float, float>(a, slices, stream) : grad<float, gnn_bf16>(a, slices, stream);
     return o.table_dtype == GNN_F32 ? grad<gnn_bf16, float>(a, slices, stream) : grad<gnn_bf16, gnn_bf16>(a, slices, stream);
 }

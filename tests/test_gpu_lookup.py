@@ -267,3 +267,20 @@ def test_a_table_beyond_32_bits_of_offsets():
     gnn.gnn_lookup_bwd(ids, y, table, scale=2.0, workspace=ws)
     assert torch.equal(table[ids], 2 * y.to(BF16))
     assert float(table[1:v // 2].float().abs().amax()) == 0.0 and float(table[v // 2 + 1:v - 1000].float().abs().amax()) == 0.0
+
+
+def test_the_widest_rows():
+    f = 1 << 24
+    gen = torch.Generator(device=DEV).manual_seed(17)
+    ids = torch.tensor([2, -1, 0, 2, 2], device=DEV, dtype=torch.int32)
+    dy = torch.randn(5, f, device=DEV, generator=gen)
+    dt = torch.full((3, f), float("nan"), device=DEV)
+    ws = torch.empty(gnn.gnn_lookup_workspace_bytes(3, 5, f), device=DEV, dtype=torch.uint8)
+    gnn.gnn_lookup_bwd(ids, dy, dt, workspace=ws)
+    assert torch.equal(dt[0], dy[2]) and not dt[1].any()
+    want = dy[0].double() + dy[3].double() + dy[4].double()
+    # two additions, each off by half a step of a sum that is at most the sum of the magnitudes
+    assert ((dt[2].double() - want).abs() <= 2.02 * 2.0 ** -24 * (dy[0].abs() + dy[3].abs() + dy[4].abs())).all()
+    y = torch.empty(5, f, device=DEV)
+    gnn.gnn_lookup_fwd(dt, ids, y)
+    assert torch.equal(y[0], dt[2]) and not y[1].any() and torch.equal(y[2], dt[0])
