@@ -48,7 +48,7 @@ struct Mat {
     int32_t norm_blocks, flags;         // kBf16, kTall
     float decay, rate;                  // 1 - lr weight_decay; lr update_scale
 };
-enum { kBf16 = 1, kTall = 2 };          // tall: rows > cols
+enum { kBf16 = 1, kTall = 2 };          // of bf16, which P = 2 parts stand for as well; tall: rows > cols
 enum Phase { kGram, kPolynomial, kUpdate, kLast };
 enum Launch { kNorms, kPlanes, kSymmetric, kOthers, kLaunches };
 
@@ -195,36 +195,40 @@ template <int P> __device__ __forceinline__ void get4(const uint16_t *planes, in
 template <int P> __global__ void __launch_bounds__(kThreads) planes_kernel(const Job j) {
     int tile;
     const Mat &t = j.mat[matrix_of_block<kPlanes>(j, tile)];
-    const bool tall = t.flags & kTall, bf16 = t.flags & kBf16;
+    const bool tall = t.flags & kTall;
+    constexpr bool bf16 = P == 2;
     const int rp = tall ? t.np : t.mp, cp = tall ? t.mp : t.np;  // filled up sides of U
     const int tiles = cp / 64;
     const int r0 = tile / tiles * 64, c0 = tile % tiles * 64;
     __shared__ float u[64][65];
     __shared__ double sums[kThreads / 64];
+    const float gs = j.grad_scale ? *j.grad_scale : 1.0f;
+    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6, col = c0 + lane;
+    // all of the tile is on its way before the norm is waited for
+    constexpr int U = 16;
+    float x[U], mo[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const int row = r0 + wave + 4 * k;
+        x[k] = mo[k] = 0.0f;
+        if (row < t.rows && col < t.cols) {
+            x[k] = element(t.in, int64_t(row) * t.ld_in + col, bf16);
+            if (j.muon) mo[k] = t.momentum[int64_t(row) * t.cols + col];
+        }
+    }
     double s = 0.0;
     for (int i = int(threadIdx.x); i < t.norm_blocks; i += kThreads) s += t.squares[i];
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+    if (lane == 0) sums[wave] = s;
     __syncthreads();
     const double norm = sqrt((sums[0] + sums[1]) + (sums[2] + sums[3]));
     const double inverse = norm <= 1.7e308 ? 1.0 / (norm + j.eps) : __builtin_nan("");  // what is not finite reaches all of the matrix
-    const float gs = j.grad_scale ? *j.grad_scale : 1.0f;
-    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-    for (int r = wave; r < 64; r += 4) {
-        const int row = r0 + r, col = c0 + lane;
-        float x = 0.0f;
-        if (row < t.rows && col < t.cols) {
-            if (j.muon) {
-                const int64_t i = int64_t(row) * t.cols + col;
-                const float mo = t.momentum[i];
-                x = j.nesterov ? element(t.in, i, bf16) * gs + j.mu * mo : mo;
-            } else {
-                x = element(t.in, int64_t(row) * t.ld_in + col, bf16);
-            }
-            x = float(double(x) * inverse);
-        }
-        u[r][lane] = x;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const int row = r0 + wave + 4 * k;
+        if (j.muon) x[k] = j.nesterov ? x[k] * gs + j.mu * mo[k] : mo[k];
+        u[wave + 4 * k][lane] = row < t.rows && col < t.cols ? float(double(x[k]) * inverse) : 0.0f;
     }
     __syncthreads();
     uint16_t *by_row = tall ? t.xt[0] : t.x, *by_col = tall ? t.x : t.xt[0];  // rows of U as rows; columns of U as rows
@@ -305,8 +309,8 @@ template <int P, Phase phase> __device__ __forceinline__ void finish(const Job &
     for (int i = 0; i < 4; ++i) v[i] = fmaf(j.c, v[i], j.b * a[i]) + (row_i + i == row_c && row_c < t.m ? j.a : 0.0f);
 }
 
-__device__ __forceinline__ void write_out(const Job &j, const Mat &t, int64_t r, int64_t c, float o) {
-    const bool bf16 = t.flags & kBf16;
+template <int P> __device__ __forceinline__ void write_out(const Job &j, const Mat &t, int64_t r, int64_t c, float o) {
+    constexpr bool bf16 = P == 2;
     const int64_t at = r * t.ld_out + c;
     if (j.muon) {
         const float p = t.master ? t.master[at] : element(t.out, at, bf16);
@@ -325,7 +329,7 @@ template <int P, Phase phase> __device__ __forceinline__ void write_down(const J
     else if (!(t.flags & kTall)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (row + i < t.m && col < t.n) write_out(j, t, row + i, col, v[i]);
+            if (row + i < t.m && col < t.n) write_out<P>(j, t, row + i, col, v[i]);
     }
 }
 // Columns col .. col + 3 of row `row`.
@@ -336,9 +340,12 @@ template <int P, Phase phase> __device__ __forceinline__ void write_across(const
     else if (t.flags & kTall) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (row < t.m && col + i < t.n) write_out(j, t, col + i, row, v[i]);
+            if (row < t.m && col + i < t.n) write_out<P>(j, t, col + i, row, v[i]);
     }
 }
+
+// What lanes of a wavefront wrote to LDS is there for its other lanes: LDS keeps their order, the compiler has to.
+__device__ __forceinline__ void within_wavefront() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
 // A fragment of results on its way out: rows row0 .. row0 + 31, columns col0 .. col0 + 31, to both places where `both`.  The loop is not unrolled: code that
 // a wavefront goes through once is as slow as it is fetched.
@@ -443,7 +450,7 @@ template <int P, Phase phase, int T> __global__ void __launch_bounds__(kThreads)
         __syncthreads();
 #pragma unroll
         for (int v = 0; v < 16; ++v) lds.turn[wave][8 * (v / 4) + 4 * lk + v % 4][l32] = sum[v];
-        __builtin_amdgcn_wave_barrier();
+        within_wavefront();
         write_fragment<P, phase>(j, t, step, (ti * 2 + (wave >> 1)) * 32, (tj * 2 + (wave & 1)) * 32, lds.turn[wave], !(symmetric && ti == tj));
     }
 }
@@ -546,11 +553,11 @@ template <int P, int TI, int TJ, int KS, Phase phase> __global__ void __launch_b
                 if (q == x * TJ + y)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) lds.turn[wave][8 * (v / 4) + 4 * lk + v % 4][l32] = acc[x][y][v];
-        __builtin_amdgcn_wave_barrier();
+        within_wavefront();
         const int row0 = ti * 64 * TI + (wi * TI + q / TJ) * 32, col0 = tj * 64 * TJ + (wj * TJ + q % TJ) * 32;
         // squares of as many rows as a tile is wide are computed whole on the diagonal
         write_fragment<P, phase>(j, t, step, row0, col0, lds.turn[wave], !(symmetric && row0 / (64 * TJ) == tj));
-        __builtin_amdgcn_wave_barrier();
+        within_wavefront();
     }
 }
 

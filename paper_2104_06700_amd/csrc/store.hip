@@ -160,7 +160,14 @@ template <typename T, bool COMPARE> __global__ void __launch_bounds__(kThreads) 
     if (threadIdx.x == 0) written = 0;
     if constexpr (COMPARE) {
         const int n = int(a.n);
-        for (int j = int(threadIdx.x); j < n; j += kThreads) ids[j] = int32_t(a.id(j));
+        for (int j0 = int(threadIdx.x); j0 < n; j0 += 4 * kThreads) {
+            int32_t v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = int32_t(a.id(j0 + u * kThreads < n ? j0 + u * kThreads : n - 1));
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (j0 + u * kThreads < n) ids[j0 + u * kThreads] = v[u];
+        }
         if (threadIdx.x < kCompareRows) again[threadIdx.x] = 0;
         __syncthreads();
         // a thread a row and an eighth of the positions, four at a time
@@ -168,6 +175,7 @@ template <typename T, bool COMPARE> __global__ void __launch_bounds__(kThreads) 
         if (r < rows) {
             const int32_t id = ids[i];
             bool found = false;
+#pragma unroll 4
             for (int j = int(threadIdx.x) / kCompareRows * 4; j < n; j += kThreads / kCompareRows * 4) {
                 const i32x4 t = *reinterpret_cast<const i32x4 *>(ids + j);  // (behind the last position: not looked at)
 #pragma unroll
