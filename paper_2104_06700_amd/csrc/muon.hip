@@ -6,15 +6,19 @@
 // from A and A (A is symmetric), X from Q and X^T, which is kept beside X.  A and Q are symmetric: only the tiles on and below the diagonal
 // are computed, and written to both places.
 //
-// Operands live in the workspace as the matrix cores take them: split into P bf16 numbers whose sum they are (P = 3: all 24 bits of fp32; P = 2: 16 bits,
-// for bf16 matrices), in fragments of 32 rows x 16 k, 1 KB a fragment, the 16 bytes of lane 32 * (k / 8) + row one after the other; the fragments of the same
-// k side by side, so that workgroups that walk along k together spread over the channels of the L2s (along k first: 1000 x 1000 bf16 283 us).  So whatever
-// fetches a fragment reads 1 KB in a row, nothing is split twice, and a product's epilogue, which has four neighbouring results of a column in a
-// lane, writes 8 bytes a plane.  Rows and columns are filled up with zeros to whole tiles, which the products keep zero.
+// Operands live in the workspace as the matrix cores take them: split into P numbers of 16 bits whose sum they are, in fragments of 32 rows x 16 k, 1 KB
+// a fragment, the 16 bytes of lane 32 * (k / 8) + row one after the other; the fragments of the same k side by side, so that workgroups that walk along k
+// together spread over the channels of the L2s.  So whatever fetches a fragment reads 1 KB in a row, nothing is split twice, and a product's epilogue, which
+// has four neighbouring results of a column in a lane, writes 8 bytes a plane.  Rows and columns are filled up with zeros to whole tiles, which the
+// products keep zero.
 //
-// Of the products of parts those that matter are formed (P = 3: six of nine, the others are below 2^-26; P = 2: three of four, 2^-18), summed from zero over
-// 16 k, smallest first, and added to the result with one rounding: the matrix cores cut off what lies below a sum's last bit, so that long chains
-// through them would be the worse sums.
+// P = 2: fp16 numbers.  The rest behind the first is at most 2^-11 of it (in halves of its steps), of which the second keeps 11 bits: 23 of the 24 bits of fp32,
+// with X, A and Q multiplied by powers of two that take the largest number they can reach near the largest of fp16, so that the smallest are off by
+// 2^-40.  It holds where the coefficients keep the singular values small, as the usual ones do (at most 1.2); else P = 3: bf16 numbers, which have the range
+// and all 24 bits of fp32, at twice the products (2560 x 4000 fp32 2990 us instead of 1890).
+// Of the products of parts those that matter are formed (P = 2: three of four, the last is below 2^-23 of the first; P = 3: six of nine, 2^-26), summed
+// from zero over 32 k (P = 3 through LDS: 16), smallest first, and added to the result with one rounding: the matrix cores cut off what lies below a sum's last
+// bit, so that long chains through them would be the worse sums.  Over 64 k: as fast; over 16, where there are twice the additions: 2030 us.
 //
 // Small matrices: a workgroup has a tile of 32 x 32 and its four wavefronts a quarter of k each, straight from the caches; such a product is one latency.
 // Large ones: tiles of 64 x 64 or 128 x 128 through LDS.  All matrices of a call of the same kind share the launches.
@@ -33,12 +37,14 @@ constexpr int64_t kMostSide = 65536, kMostSteps = 100;
 
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 struct Mat {
     uint16_t *x, *xt[2], *a, *q;        // planes: X (rows m, k n), X^T (rows n, k m) before and after a step, A and Q
-    double *squares;                    // [norm_blocks]
+    double *squares;                    // [norm_blocks]; then the logarithm of X's norm
     const void *in;                     // U, or the gradient
     void *out;                          // O, or the parameters
     float *momentum, *master;           // of a Muon step, or nullptr
@@ -48,7 +54,7 @@ struct Mat {
     int32_t norm_blocks, flags;         // kBf16, kTall
     float decay, rate;                  // 1 - lr weight_decay; lr update_scale
 };
-enum { kBf16 = 1, kTall = 2 };          // of bf16, which P = 2 parts stand for as well; tall: rows > cols
+enum { kBf16 = 1, kTall = 2 };          // tall: rows > cols
 enum Phase { kGram, kPolynomial, kUpdate, kLast };
 enum Launch { kNorms, kPlanes, kSymmetric, kOthers, kLaunches };
 
@@ -56,8 +62,9 @@ struct Job {
     Mat mat[kMats];
     int32_t first[kLaunches][kMats];    // workgroup that begins a matrix; INT32_MAX behind the last
     int32_t muon, nesterov;
-    float mu, a, b, c;
+    float mu, a, b, c;                  // (a, b and c with the powers of two that the planes hold A and Q with)
     double eps;
+    float growth;                       // P = 2: the logarithm, to base 2, of what a step can multiply X by
     const float *grad_scale;
 };
 static_assert(sizeof(Job) <= 4096, "kernel arguments");
@@ -137,16 +144,49 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const Job j) {
 
 // ---- planes
 
-// x = the sum of P bf16 numbers, exactly where P = 3
+// What an operand is made of.  P = 2: fp16 numbers, with X, A and Q taken by powers of two that put the largest number they can hold near the type's.
+template <int P> struct Parts;
+template <> struct Parts<2> {
+    typedef f16x8 Eight;
+    static constexpr float kX = 32768.0f, kA = 16384.0f, kQ = 8192.0f;
+    static __device__ __forceinline__ float part(float x) { return float(_Float16(x)); }
+    static __device__ __forceinline__ uint32_t pair(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(gnn_f32x2{x, y}, f16x2)); }
+    static __device__ __forceinline__ float get(uint32_t w, int i) { return float(__builtin_bit_cast(f16x2, w)[i]); }
+    static __device__ __forceinline__ float16v product(f16x8 a, f16x8 b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Parts<3> {
+    typedef bf16x8 Eight;
+    static constexpr float kX = 1.0f, kA = 1.0f, kQ = 1.0f;
+    static __device__ __forceinline__ float part(float x) { return float(__bf16(x)); }
+    static __device__ __forceinline__ uint32_t pair(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(gnn_f32x2{x, y}, gnn_bf16x2)); }
+    static __device__ __forceinline__ float get(uint32_t w, int i) { return __uint_as_float(i ? w & 0xFFFF0000u : w << 16); }
+    static __device__ __forceinline__ float16v product(bf16x8 a, bf16x8 b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+// P = 2: a matrix whose norm is far below eps has an X as small, and gets another power of two: as many more as keep it below 1 in this step.  (A matters
+// beside 1 and stays as it is.)
+template <int P> __device__ __forceinline__ int exponent(const Job &j, float log_norm, int step) {
+    if constexpr (P == 3) return 0;
+    const float e = -fmaf(float(step), j.growth, log_norm);
+    return e > 0.0f ? int(fminf(e, 90.0f)) : 0;
+}
+// What a sum of a phase is times, to be the number that the planes hold, or the result.
+template <int P, Phase phase> __device__ __forceinline__ float factor(const Job &j, const Mat &t, int step) {
+    typedef Parts<P> S;
+    if (P == 3 || phase == kPolynomial) return 1.0f;
+    const float log_norm = float(t.squares[t.norm_blocks]);
+    const int now = exponent<P>(j, log_norm, step);
+    if constexpr (phase == kGram) return __builtin_amdgcn_ldexpf(S::kA / (S::kX * S::kX), -2 * now);
+    else if constexpr (phase == kUpdate) return __builtin_amdgcn_ldexpf(1.0f / S::kQ, exponent<P>(j, log_norm, step + 1) - now);
+    else return __builtin_amdgcn_ldexpf(1.0f / (S::kQ * S::kX), -now);
+}
+
+// x = the sum of P parts, exactly where P = 3
 template <int P> __device__ __forceinline__ void split(float x, float (&part)[P]) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        part[p] = float(__bf16(x));
+        part[p] = Parts<P>::part(x);
         x -= part[p];
     }
-}
-__device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(gnn_f32x2{x, y}, gnn_bf16x2));
 }
 
 // Where element (row, k) of an operand of rows x depth lies in plane 0, in elements of 2 bytes; planes are rows * depth apart.
@@ -161,7 +201,7 @@ template <int P> __device__ __forceinline__ void put4(uint16_t *planes, int rows
     for (int i = 0; i < 4; ++i) split<P>(v[i], part[i]);
 #pragma unroll
     for (int q = 0; q < P; ++q)
-        *reinterpret_cast<u32x2 *>(p + int64_t(q) * rows * depth) = u32x2{bf16_pair(part[0][q], part[1][q]), bf16_pair(part[2][q], part[3][q])};
+        *reinterpret_cast<u32x2 *>(p + int64_t(q) * rows * depth) = u32x2{Parts<P>::pair(part[0][q], part[1][q]), Parts<P>::pair(part[2][q], part[3][q])};
 }
 // eight, the first a multiple of eight
 template <int P> __device__ __forceinline__ void put8(uint16_t *planes, int rows, int depth, int row, int k, const float (&v)[8]) {
@@ -173,7 +213,7 @@ template <int P> __device__ __forceinline__ void put8(uint16_t *planes, int rows
     for (int q = 0; q < P; ++q) {
         u32x4 w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = bf16_pair(part[2 * i][q], part[2 * i + 1][q]);
+        for (int i = 0; i < 4; ++i) w[i] = Parts<P>::pair(part[2 * i][q], part[2 * i + 1][q]);
         *reinterpret_cast<u32x4 *>(p + int64_t(q) * rows * depth) = w;
     }
 }
@@ -184,19 +224,17 @@ template <int P> __device__ __forceinline__ void get4(const uint16_t *planes, in
 #pragma unroll
     for (int q = P - 1; q >= 0; --q) {  // smallest first: the sum is exact
         const u32x2 w = *reinterpret_cast<const u32x2 *>(p + int64_t(q) * rows * depth);
-        v[0] += __uint_as_float(w.x << 16);
-        v[1] += __uint_as_float(w.x & 0xFFFF0000u);
-        v[2] += __uint_as_float(w.y << 16);
-        v[3] += __uint_as_float(w.y & 0xFFFF0000u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += Parts<P>::get(i < 2 ? w.x : w.y, i & 1);
     }
 }
 
 // X and X^T from U: a workgroup has a tile of 64 x 64 of U.
-template <int P> __global__ void __launch_bounds__(kThreads) planes_kernel(const Job j) {
+template <int P, typename T> __global__ void __launch_bounds__(kThreads) planes_kernel(const Job j) {
     int tile;
     const Mat &t = j.mat[matrix_of_block<kPlanes>(j, tile)];
     const bool tall = t.flags & kTall;
-    constexpr bool bf16 = P == 2;
+    constexpr bool bf16 = sizeof(T) == 2;
     const int rp = tall ? t.np : t.mp, cp = tall ? t.mp : t.np;  // filled up sides of U
     const int tiles = cp / 64;
     const int r0 = tile / tiles * 64, c0 = tile % tiles * 64;
@@ -223,7 +261,10 @@ template <int P> __global__ void __launch_bounds__(kThreads) planes_kernel(const
     if (lane == 0) sums[wave] = s;
     __syncthreads();
     const double norm = sqrt((sums[0] + sums[1]) + (sums[2] + sums[3]));
-    const double inverse = norm <= 1.7e308 ? 1.0 / (norm + j.eps) : __builtin_nan("");  // what is not finite reaches all of the matrix
+    const bool fits = norm <= 1.7e308;
+    const float log_norm = fits ? log2f(float(norm / (norm + j.eps))) : 0.0f;
+    if (tile == 0 && threadIdx.x == 0) t.squares[t.norm_blocks] = double(log_norm);
+    const double inverse = fits ? ldexp(double(Parts<P>::kX), exponent<P>(j, log_norm, 0)) / (norm + j.eps) : __builtin_nan("");  // what is not finite reaches all of the matrix
 #pragma unroll
     for (int k = 0; k < U; ++k) {
         const int row = r0 + wave + 4 * k;
@@ -280,37 +321,49 @@ template <bool SYMMETRIC, int WIDE> __device__ __forceinline__ void tile_of(int 
     }
 }
 
-// The sums of the products of parts that matter, for N fragments of the right operand, in turn, so that no product waits for the one before.  P = 3:
-// from zero, smallest first, and then added with one rounding; P = 2, whose operands are off by more than what the matrix cores cut off, in one chain.
-template <int P, int N> __device__ __forceinline__ void add_products(float16v (&acc)[N], const bf16x8 (&a)[P], const bf16x8 (&b)[N][P]) {
-    float16v sum[N];
-#pragma unroll
-    for (int y = 0; y < N; ++y)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) sum[y][v] = P == 3 ? 0.0f : acc[y][v];
+// The products of parts that matter, smallest first, onto the sums of N fragments of the right operand, in turn, so that no product waits for the one before.
+template <int P, int N> __device__ __forceinline__ void add_products(float16v (&sum)[N], const typename Parts<P>::Eight (&a)[P], const typename Parts<P>::Eight (&b)[N][P]) {
 #pragma unroll
     for (int s = P - 1; s >= 0; --s)
 #pragma unroll
         for (int p = 0; p <= s; ++p)
 #pragma unroll
-            for (int y = 0; y < N; ++y) sum[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[p], b[y][s - p], sum[y], 0, 0, 0);
+            for (int y = 0; y < N; ++y) sum[y] = Parts<P>::product(a[p], b[y][s - p], sum[y]);
+}
+template <int TI, int TJ> __device__ __forceinline__ void clear(float16v (&sum)[TI][TJ]) {
 #pragma unroll
-    for (int y = 0; y < N; ++y)
+    for (int x = 0; x < TI; ++x)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[y][v] = P == 3 ? acc[y][v] + sum[y][v] : sum[y][v];
+        for (int y = 0; y < TJ; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sum[x][y][v] = 0.0f;
+}
+// with one rounding
+template <int TI, int TJ> __device__ __forceinline__ void add(float16v (&to)[TI][TJ], const float16v (&sum)[TI][TJ]) {
+#pragma unroll
+    for (int x = 0; x < TI; ++x)
+#pragma unroll
+        for (int y = 0; y < TJ; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) to[x][y][v] += sum[x][y][v];
 }
 
 // What a phase makes of four sums, rows row_i .. row_i + 3 of column row_c, or the same columns of that row: A is symmetric.
-template <int P, Phase phase> __device__ __forceinline__ void finish(const Job &j, const Mat &t, int row_i, int row_c, float (&v)[4]) {
-    if (phase != kPolynomial) return;
+template <int P, Phase phase> __device__ __forceinline__ void finish(const Job &j, const Mat &t, float times, int row_i, int row_c, float (&v)[4]) {
+    if constexpr (phase != kPolynomial) {
+        if constexpr (P == 2)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] *= times;
+        return;
+    }
     float a[4];
     get4<P>(t.a, t.mp, t.mp, row_c, row_i, a);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = fmaf(j.c, v[i], j.b * a[i]) + (row_i + i == row_c && row_c < t.m ? j.a : 0.0f);
 }
 
-template <int P> __device__ __forceinline__ void write_out(const Job &j, const Mat &t, int64_t r, int64_t c, float o) {
-    constexpr bool bf16 = P == 2;
+template <typename T> __device__ __forceinline__ void write_out(const Job &j, const Mat &t, int64_t r, int64_t c, float o) {
+    constexpr bool bf16 = sizeof(T) == 2;
     const int64_t at = r * t.ld_out + c;
     if (j.muon) {
         const float p = t.master ? t.master[at] : element(t.out, at, bf16);
@@ -322,25 +375,25 @@ template <int P> __device__ __forceinline__ void write_out(const Job &j, const M
 }
 
 // Rows row .. row + 3 of column col of a phase's result.
-template <int P, Phase phase> __device__ __forceinline__ void write_down(const Job &j, const Mat &t, int step, int row, int col, const float (&v)[4]) {
+template <int P, Phase phase, typename T> __device__ __forceinline__ void write_down(const Job &j, const Mat &t, int step, int row, int col, const float (&v)[4]) {
     if (phase == kGram) put4<P>(t.a, t.mp, t.mp, col, row, v);
     else if (phase == kPolynomial) put4<P>(t.q, t.mp, t.mp, col, row, v);
     else if (phase == kUpdate) put4<P>(t.xt[(step + 1) & 1], t.np, t.mp, col, row, v);
     else if (!(t.flags & kTall)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (row + i < t.m && col < t.n) write_out<P>(j, t, row + i, col, v[i]);
+            if (row + i < t.m && col < t.n) write_out<T>(j, t, row + i, col, v[i]);
     }
 }
 // Columns col .. col + 3 of row `row`.
-template <int P, Phase phase> __device__ __forceinline__ void write_across(const Job &j, const Mat &t, int row, int col, const float (&v)[4]) {
+template <int P, Phase phase, typename T> __device__ __forceinline__ void write_across(const Job &j, const Mat &t, int row, int col, const float (&v)[4]) {
     if (phase == kGram) put4<P>(t.a, t.mp, t.mp, row, col, v);
     else if (phase == kPolynomial) put4<P>(t.q, t.mp, t.mp, row, col, v);
     else if (phase == kUpdate) put4<P>(t.x, t.mp, t.np, row, col, v);
     else if (t.flags & kTall) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (row < t.m && col + i < t.n) write_out<P>(j, t, col + i, row, v[i]);
+            if (row < t.m && col + i < t.n) write_out<T>(j, t, col + i, row, v[i]);
     }
 }
 
@@ -349,7 +402,7 @@ __device__ __forceinline__ void within_wavefront() { __builtin_amdgcn_fence(__AT
 
 // A fragment of results on its way out: rows row0 .. row0 + 31, columns col0 .. col0 + 31, to both places where `both`.  The loop is not unrolled: code that
 // a wavefront goes through once is as slow as it is fetched.
-template <int P, Phase phase> __device__ __forceinline__ void write_fragment(const Job &j, const Mat &t, int step, int row0, int col0, const float (&turn)[32][33], bool both) {
+template <int P, Phase phase, typename T> __device__ __forceinline__ void write_fragment(const Job &j, const Mat &t, float times, int step, int row0, int col0, const float (&turn)[32][33], bool both) {
     const int lane = int(threadIdx.x) & 63, l32 = lane & 31, lk = lane >> 5;
 #pragma unroll 1
     for (int g = 0; g < 4; ++g) {
@@ -357,39 +410,36 @@ template <int P, Phase phase> __device__ __forceinline__ void write_fragment(con
         float v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = turn[at + i][l32];
-        finish<P, phase>(j, t, row0 + at, col0 + l32, v);
-        write_down<P, phase>(j, t, step, row0 + at, col0 + l32, v);
+        finish<P, phase>(j, t, times, row0 + at, col0 + l32, v);
+        write_down<P, phase, T>(j, t, step, row0 + at, col0 + l32, v);
         if (!both) continue;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = turn[l32][at + i];
-        finish<P, phase>(j, t, col0 + at, row0 + l32, v);
-        write_across<P, phase>(j, t, row0 + l32, col0 + at, v);
+        finish<P, phase>(j, t, times, col0 + at, row0 + l32, v);
+        write_across<P, phase, T>(j, t, row0 + l32, col0 + at, v);
     }
 }
 
 // Tiles of (32 T)^2: each of four wavefronts has all of the tile and every fourth 16 of k, straight from the caches, and keeps SETS steps on their way.
 // Nothing waits but for its own loads; the four sums are added in LDS.
-template <int P, Phase phase, int T> __global__ void __launch_bounds__(kThreads) split_product_kernel(const Job j, int step) {
+template <int P, Phase phase, typename OUT, int T> __global__ void __launch_bounds__(kThreads) split_product_kernel(const Job j, int step) {
     constexpr bool symmetric = phase == kGram || phase == kPolynomial;
-    constexpr int SETS = 2;  // 600-1000-1000-41 bf16 247 us, four 277; a model of 256 columns 96, four 99, one 107
+    constexpr int SETS = 2;  // 602-1000-1000-41 bf16 258 us, three 263, four 271; 100-256-256-47 fp32 80.8, 82.6, 81.3
+    typedef typename Parts<P>::Eight Eight;
     int number, ti, tj;
     const Mat &t = j.mat[matrix_of_block<symmetric ? kSymmetric : kOthers>(j, number)];
     const Operands o = operands<phase>(t, step);
+    const float times = factor<P, phase>(j, t, step);
     const int side = o.rows / (32 * T), across = o.cols / (32 * T);
     tile_of<symmetric, 1>(number, symmetric ? side * (side + 1) / 2 : side * across, across, ti, tj);
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int ks = o.depth / 16;
-    const bf16x8 *left = reinterpret_cast<const bf16x8 *>(o.left) + int64_t(ti) * T * 64 + lane;
-    const bf16x8 *right = reinterpret_cast<const bf16x8 *>(o.right) + int64_t(tj) * T * 64 + lane;
+    const Eight *left = reinterpret_cast<const Eight *>(o.left) + int64_t(ti) * T * 64 + lane;
+    const Eight *right = reinterpret_cast<const Eight *>(o.right) + int64_t(tj) * T * 64 + lane;
     const int64_t left_plane = int64_t(o.rows) * o.depth / 8, right_plane = int64_t(o.cols) * o.depth / 8;
     float16v acc[T][T];
-#pragma unroll
-    for (int x = 0; x < T; ++x)
-#pragma unroll
-        for (int y = 0; y < T; ++y)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
-    bf16x8 a[SETS][T][P], b[SETS][T][P];
+    clear<T, T>(acc);
+    Eight a[SETS][T][P], b[SETS][T][P];
     auto load = [&](int set, int k) {  // behind the last step: that one again
         const int64_t at = k < ks ? k : ks - 1;
 #pragma unroll
@@ -403,13 +453,16 @@ template <int P, Phase phase, int T> __global__ void __launch_bounds__(kThreads)
 #pragma unroll
     for (int u = 0; u < SETS; ++u) load(u, wave + 4 * u);
     for (int k = wave; k < ks; k += 4 * SETS) {
+        float16v sum[T][T];
+        clear<T, T>(sum);
 #pragma unroll
         for (int u = 0; u < SETS; ++u) {
             if (k + 4 * u >= ks) break;
 #pragma unroll
-            for (int x = 0; x < T; ++x) add_products<P, T>(acc[x], a[u][x], b[u]);
+            for (int x = 0; x < T; ++x) add_products<P, T>(sum[x], a[u][x], b[u]);
             load(u, k + 4 * (u + SETS));
         }
+        add<T, T>(acc, sum);
     }
     const int l32 = lane & 31, lk = lane >> 5;
     if constexpr (T == 1) {
@@ -422,13 +475,13 @@ template <int P, Phase phase, int T> __global__ void __launch_bounds__(kThreads)
         float v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = (tile[0][at + i][l32] + tile[1][at + i][l32]) + (tile[2][at + i][l32] + tile[3][at + i][l32]);
-        finish<P, phase>(j, t, row0 + at, col0 + l32, v);
-        write_down<P, phase>(j, t, step, row0 + at, col0 + l32, v);
+        finish<P, phase>(j, t, times, row0 + at, col0 + l32, v);
+        write_down<P, phase, OUT>(j, t, step, row0 + at, col0 + l32, v);
         if (symmetric && ti == tj) return;  // (a tile on the diagonal is computed whole)
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = (tile[0][l32][at + i] + tile[1][l32][at + i]) + (tile[2][l32][at + i] + tile[3][l32][at + i]);
-        finish<P, phase>(j, t, col0 + at, row0 + l32, v);
-        write_across<P, phase>(j, t, row0 + l32, col0 + at, v);
+        finish<P, phase>(j, t, times, col0 + at, row0 + l32, v);
+        write_across<P, phase, OUT>(j, t, row0 + l32, col0 + at, v);
     } else {
         // a wavefront adds up and writes one fragment of the tile
         static_assert(T == 2, "a fragment a wavefront");
@@ -451,13 +504,14 @@ template <int P, Phase phase, int T> __global__ void __launch_bounds__(kThreads)
 #pragma unroll
         for (int v = 0; v < 16; ++v) lds.turn[wave][8 * (v / 4) + 4 * lk + v % 4][l32] = sum[v];
         within_wavefront();
-        write_fragment<P, phase>(j, t, step, (ti * 2 + (wave >> 1)) * 32, (tj * 2 + (wave & 1)) * 32, lds.turn[wave], !(symmetric && ti == tj));
+        write_fragment<P, phase, OUT>(j, t, times, step, (ti * 2 + (wave >> 1)) * 32, (tj * 2 + (wave & 1)) * 32, lds.turn[wave], !(symmetric && ti == tj));
     }
 }
 
-// Tiles of 64 TI x 64 TJ through LDS: four wavefronts of TI x TJ fragments each, 16 KS k at a time, the next ones in the other half of the LDS and two more
+// Tiles of 64 TI x 64 TJ through LDS (64 x 128; 128 x 128 2150 us for 2560 x 4000 instead of 1890): four wavefronts of TI x TJ fragments each, 16 KS k at a time, the next ones in the other half of the LDS and two more
 // such steps on their way in registers.
-template <int P, int TI, int TJ, int KS, Phase phase> __global__ void __launch_bounds__(kThreads, 3) product_kernel(const Job j, int step) {
+template <int P, int TI, int TJ, int KS, Phase phase, typename T> __global__ void __launch_bounds__(kThreads, 3) product_kernel(const Job j, int step) {
+    typedef typename Parts<P>::Eight Eight;
     constexpr int ROWS = 2 * (TI + TJ), FRAGS = ROWS * P * KS, MINE = (FRAGS + 3) / 4;  // 32 rows of an operand; fragments of a step, of a wavefront
     static_assert(TJ % TI == 0, "tiles of symmetric results");
     __shared__ union {
@@ -468,13 +522,14 @@ template <int P, int TI, int TJ, int KS, Phase phase> __global__ void __launch_b
     int number, ti, tj;
     const Mat &t = j.mat[matrix_of_block<symmetric ? kSymmetric : kOthers>(j, number)];
     const Operands o = operands<phase>(t, step);
+    const float times = factor<P, phase>(j, t, step);
     const int down = o.rows / (64 * TI), across = o.cols / (64 * TJ);
     tile_of<symmetric, TJ / TI>(number, symmetric ? TJ / TI * (across * (across + 1) / 2) : down * across, across, ti, tj);
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int steps = o.depth / (16 * KS);
 
     // fragment f of a step: its 16 k, then 32 rows (of the left operand, then of the right one), then plane.  Where they cannot be shared out evenly the last
-    // one is fetched more than once: branches around single loads cost more (2560 x 4000 3110 us, 2940 so).
+    // one is fetched more than once: branches around single loads cost more (three parts, 2560 x 4000 3110 us, 2940 so).
     const u32x4 *from[MINE];
     int64_t apart[MINE];  // from a step to the next, in 16 bytes
 #pragma unroll
@@ -499,28 +554,26 @@ template <int P, int TI, int TJ, int KS, Phase phase> __global__ void __launch_b
     };
     const int wi = wave >> 1, wj = wave & 1;
     float16v acc[TI][TJ];
-#pragma unroll
-    for (int x = 0; x < TI; ++x)
-#pragma unroll
-        for (int y = 0; y < TJ; ++y)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
+    clear<TI, TJ>(acc);
     auto multiply = [&](int half) {
-        __builtin_amdgcn_s_setprio(1);  // ahead of the other workgroup's wavefronts, which are then free to fetch: 2560 x 4000 3255 -> 3110 us
+        __builtin_amdgcn_s_setprio(1);  // ahead of the other workgroup's wavefronts, which are then free to fetch: 2560 x 4000 1990 -> 1880 us
+        float16v sum[TI][TJ];
+        clear<TI, TJ>(sum);
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk) {
-            bf16x8 a[TI][P], b[TJ][P];
+            Eight a[TI][P], b[TJ][P];
 #pragma unroll
             for (int x = 0; x < TI; ++x)
 #pragma unroll
-                for (int p = 0; p < P; ++p) a[x][p] = __builtin_bit_cast(bf16x8, lds.frag[half][(kk * ROWS + wi * TI + x) * P + p][lane]);
+                for (int p = 0; p < P; ++p) a[x][p] = __builtin_bit_cast(Eight, lds.frag[half][(kk * ROWS + wi * TI + x) * P + p][lane]);
 #pragma unroll
             for (int y = 0; y < TJ; ++y)
 #pragma unroll
-                for (int p = 0; p < P; ++p) b[y][p] = __builtin_bit_cast(bf16x8, lds.frag[half][(kk * ROWS + 2 * TI + wj * TJ + y) * P + p][lane]);
+                for (int p = 0; p < P; ++p) b[y][p] = __builtin_bit_cast(Eight, lds.frag[half][(kk * ROWS + 2 * TI + wj * TJ + y) * P + p][lane]);
 #pragma unroll
-            for (int x = 0; x < TI; ++x) add_products<P, TJ>(acc[x], a[x], b);
+            for (int x = 0; x < TI; ++x) add_products<P, TJ>(sum[x], a[x], b);
         }
+        add<TI, TJ>(acc, sum);
         __builtin_amdgcn_s_setprio(0);
     };
     load(0, 0);
@@ -556,7 +609,7 @@ template <int P, int TI, int TJ, int KS, Phase phase> __global__ void __launch_b
         within_wavefront();
         const int row0 = ti * 64 * TI + (wi * TI + q / TJ) * 32, col0 = tj * 64 * TJ + (wj * TJ + q % TJ) * 32;
         // squares of as many rows as a tile is wide are computed whole on the diagonal
-        write_fragment<P, phase>(j, t, step, row0, col0, lds.turn[wave], !(symmetric && row0 / (64 * TJ) == tj));
+        write_fragment<P, phase, T>(j, t, times, step, row0, col0, lds.turn[wave], !(symmetric && row0 / (64 * TJ) == tj));
         within_wavefront();
     }
 }
@@ -577,8 +630,8 @@ struct Entry {
     bool skip;
 };
 
-// How the products of a matrix are tiled: 0 tiles of 32 x 32, k shared out; 1 of 64 x 64, the same; 2 of 64 x 128 through LDS.  Us for 600 x 600 fp32 157 and 223
-// (0 and 1), 1000 x 1000 333 and 326, bf16 231 and 240; 1500 x 1800 fp32 925 and 1030 (1 and 2), 2048 x 2048 1562 and 1340.
+// How the products of a matrix are tiled: 0 tiles of 32 x 32, k shared out; 1 of 64 x 64, the same; 2 of 64 x 128 through LDS.  Us in fp32 and bf16 alike:
+// 800 x 800 151, 186 and 365, 1000 x 1000 209, 204 and 399, 1500 x 1800 588, 546 and 617, 2048 x 2048 1216, 957 and 864.
 int kind_of(int64_t rows, int64_t cols) {
     const double m = double(rows < cols ? rows : cols), n = double(rows < cols ? cols : rows), work = m * m * n;
     return work <= 1.0e9 ? 0 : work <= 6.0e9 ? 1 : 2;
@@ -590,10 +643,10 @@ struct Sizes {
     int64_t m, n, mp, np, bytes;
     int32_t norm_blocks;
 };
-Sizes sizes_of(int64_t rows, int64_t cols, int32_t dtype) {
+Sizes sizes_of(int64_t rows, int64_t cols, int parts) {
     Sizes s;
     s.kind = kind_of(rows, cols);
-    s.parts = dtype == GNN_BF16 ? 2 : 3;
+    s.parts = parts;
     s.m = rows < cols ? rows : cols;
     s.n = rows < cols ? cols : rows;
     const int64_t to = tile_of_kind(s.kind) < 64 ? 64 : tile_of_kind(s.kind);  // the first planes are made in tiles of 64
@@ -601,36 +654,71 @@ Sizes sizes_of(int64_t rows, int64_t cols, int32_t dtype) {
     s.np = up(s.n, to);
     const int64_t blocks = (s.m * s.n + kNormChunk - 1) / kNormChunk;
     s.norm_blocks = int32_t(blocks < kNormBlocks ? blocks : kNormBlocks);
-    s.bytes = 2 * s.parts * (3 * s.mp * s.np + 2 * s.mp * s.mp) + up(8 * s.norm_blocks, 256);
+    s.bytes = 2 * s.parts * (3 * s.mp * s.np + 2 * s.mp * s.mp) + up(8 * (s.norm_blocks + 1), 256);
     return s;
 }
 
-template <int P, Phase phase> int launch_products(const Job &j, int kind, int step, int64_t blocks, hipStream_t stream) {
+template <int P, Phase phase, typename T> int launch_products(const Job &j, int kind, int step, int64_t blocks, hipStream_t stream) {
     if (blocks > INT32_MAX / kThreads) return GNN_ERR_UNSUPPORTED;
-    if (kind == 0) split_product_kernel<P, phase, 1><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
-    else if (kind == 1) split_product_kernel<P, phase, 2><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
-    else product_kernel<P, 1, 2, P == 3 ? 1 : 2, phase><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
+    if (kind == 0) split_product_kernel<P, phase, T, 1><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
+    else if (kind == 1) split_product_kernel<P, phase, T, 2><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
+    else product_kernel<P, 1, 2, P == 3 ? 1 : 2, phase, T><<<unsigned(blocks), kThreads, 0, stream>>>(j, step);
     GNN_HIP_TRY(hipGetLastError());
     return GNN_OK;
 }
 
-template <int P> int launch_job(const Job &j, int kind, const int64_t (&blocks)[kLaunches], int steps, hipStream_t stream) {
+template <int P, typename T> int launch_job(const Job &j, int kind, const int64_t (&blocks)[kLaunches], int steps, hipStream_t stream) {
     norm_kernel<<<unsigned(blocks[kNorms]), kThreads, 0, stream>>>(j);
-    planes_kernel<P><<<unsigned(blocks[kPlanes]), kThreads, 0, stream>>>(j);
+    planes_kernel<P, T><<<unsigned(blocks[kPlanes]), kThreads, 0, stream>>>(j);
     GNN_HIP_TRY(hipGetLastError());
-    for (int s = 0; s < steps; ++s) {
-        int rc = launch_products<P, kGram>(j, kind, s, blocks[kSymmetric], stream);
-        if (rc == GNN_OK) rc = launch_products<P, kPolynomial>(j, kind, s, blocks[kSymmetric], stream);
-        if (rc == GNN_OK) rc = s + 1 < steps ? launch_products<P, kUpdate>(j, kind, s, blocks[kOthers], stream) : launch_products<P, kLast>(j, kind, s, blocks[kOthers], stream);
+    for (int s = 0; s < steps; ++s) {  // (what stays in planes is the same for all types)
+        int rc = launch_products<P, kGram, float>(j, kind, s, blocks[kSymmetric], stream);
+        if (rc == GNN_OK) rc = launch_products<P, kPolynomial, float>(j, kind, s, blocks[kSymmetric], stream);
+        if (rc == GNN_OK) rc = s + 1 < steps ? launch_products<P, kUpdate, float>(j, kind, s, blocks[kOthers], stream) : launch_products<P, kLast, T>(j, kind, s, blocks[kOthers], stream);
         if (rc != GNN_OK) return rc;
     }
     return GNN_OK;
 }
 
+// Whether X, A and Q stay within what two fp16 numbers hold with the powers of two of Parts<2>, and directions of small singular values do not shrink below it.
+// Singular values of X begin within 0 .. 1, and the step takes s to s q(s^2), q(t) = a + b t + c t^2: both have their extremes at the ends or where their
+// derivative is 0.
+bool two_parts_do(double a, double b, double c, int steps, float &growth) {
+    if (!(fabs(a) >= 1.0)) return false;
+    double most = 1.0 + 1e-6, grows = 1.0;
+    for (int k = 0; k < steps; ++k) {
+        const double top = most * most;
+        auto q = [&](double t) { return fabs(a + t * (b + t * c)); };
+        double q_most = fmax(q(0.0), q(top)), next = most * q(top);
+        if (c != 0.0) {
+            const double t = -b / (2.0 * c), root = 9.0 * b * b - 20.0 * a * c;
+            if (t > 0.0 && t < top) q_most = fmax(q_most, q(t));
+            if (root >= 0.0)
+                for (int sign = -1; sign <= 1; sign += 2) {
+                    const double u = (-3.0 * b + sign * sqrt(root)) / (10.0 * c);
+                    if (u > 0.0 && u < top) next = fmax(next, sqrt(u) * q(u));
+                }
+        } else if (b != 0.0) {
+            const double u = -a / (3.0 * b);
+            if (u > 0.0 && u < top) next = fmax(next, sqrt(u) * q(u));
+        }
+        most = next * (1.0 + 1e-4);  // (roundings of the products)
+        if (!(most <= 1.9) || !(q_most <= 7.5)) return false;
+        grows = fmax(grows, q_most);
+    }
+    growth = float(log2(grows) + 1e-4);
+    return true;
+}
+
 // Matrices of the same kind and type, kMats at a time.
-int orthogonalize(Entry (*at)(const void *, int64_t), const void *list, int64_t count, Job &j, int steps, uint8_t *room, hipStream_t stream) {
+int orthogonalize(Entry (*at)(const void *, int64_t), const void *list, int64_t count, Job &j, double a, double b, double c, int steps, uint8_t *room, hipStream_t stream) {
+    const int parts = two_parts_do(a, b, c, steps, j.growth) ? 2 : 3;
+    const double unit_a = parts == 2 ? Parts<2>::kA : 1.0, unit_q = parts == 2 ? Parts<2>::kQ : 1.0;
+    j.a = float(a * unit_q);
+    j.b = float(b * (unit_q / unit_a));
+    j.c = float(c * (unit_q / (unit_a * unit_a)));
     for (int kind = 0; kind < 3; ++kind)
-        for (int parts = 2; parts <= 3; ++parts) {
+        for (int32_t dtype : {GNN_F32, GNN_BF16}) {
             int64_t blocks[kLaunches];
             int matrices = 0;
             auto clear = [&]() {
@@ -642,7 +730,8 @@ int orthogonalize(Entry (*at)(const void *, int64_t), const void *list, int64_t 
             };
             auto flush = [&]() -> int {
                 if (matrices == 0) return GNN_OK;
-                const int rc = parts == 2 ? launch_job<2>(j, kind, blocks, steps, stream) : launch_job<3>(j, kind, blocks, steps, stream);
+                const int rc = parts == 2 ? dtype == GNN_F32 ? launch_job<2, float>(j, kind, blocks, steps, stream) : launch_job<2, gnn_bf16>(j, kind, blocks, steps, stream)
+                               : dtype == GNN_F32 ? launch_job<3, float>(j, kind, blocks, steps, stream) : launch_job<3, gnn_bf16>(j, kind, blocks, steps, stream);
                 clear();
                 return rc;
             };
@@ -650,8 +739,8 @@ int orthogonalize(Entry (*at)(const void *, int64_t), const void *list, int64_t 
             for (int64_t k = 0; k < count; ++k) {
                 const Entry e = at(list, k);
                 if (e.skip || e.rows == 0 || e.cols == 0) continue;
-                const Sizes s = sizes_of(e.rows, e.cols, e.dtype);
-                if (s.kind != kind || s.parts != parts) continue;
+                const Sizes s = sizes_of(e.rows, e.cols, parts);
+                if (s.kind != kind || e.dtype != dtype) continue;
                 const int64_t tile = tile_of_kind(kind), across = s.mp / tile;
                 // (large ones: two tiles of half the height for each square one)
                 const int64_t more[kLaunches] = {s.norm_blocks, s.mp / 64 * (s.np / 64), across * (across + 1) / (kind == 2 ? 1 : 2),
@@ -730,7 +819,7 @@ template <typename M> int64_t room_of(const M *matrices, int64_t count) {
     int64_t bytes = 0;
     for (int64_t k = 0; k < count; ++k) {
         if (check_matrix(matrices[k]) != GNN_OK) return -1;
-        if (matrices[k].rows > 0 && matrices[k].cols > 0 && !leaves_alone(matrices[k])) bytes += sizes_of(matrices[k].rows, matrices[k].cols, matrices[k].dtype).bytes;
+        if (matrices[k].rows > 0 && matrices[k].cols > 0 && !leaves_alone(matrices[k])) bytes += sizes_of(matrices[k].rows, matrices[k].cols, 3).bytes;
     }
     return bytes;
 }
@@ -754,16 +843,13 @@ extern "C" GNN_API int gnn_orthogonalize(const gnn_orthogonalize_matrix *matrice
     if (!o.workspace || misaligned(o.workspace, 256) || o.workspace_bytes < bytes) return GNN_ERR_INVALID_ARG;
     (void)hipGetLastError();
     Job j{};
-    j.a = float(o.a);
-    j.b = float(o.b);
-    j.c = float(o.c);
     j.eps = o.eps;
     return orthogonalize(
         [](const void *list, int64_t k) {
             const gnn_orthogonalize_matrix &t = static_cast<const gnn_orthogonalize_matrix *>(list)[k];
             return Entry{t.in, t.out, nullptr, nullptr, t.rows, t.cols, t.ld_in ? t.ld_in : t.cols, t.ld_out ? t.ld_out : t.cols, t.dtype, 1.0f, 1.0f, false};
         },
-        matrices, n_matrices, j, o.steps, static_cast<uint8_t *>(o.workspace), static_cast<hipStream_t>(o.stream));
+        matrices, n_matrices, j, o.a, o.b, o.c, o.steps, static_cast<uint8_t *>(o.workspace), static_cast<hipStream_t>(o.stream));
 }
 
 extern "C" GNN_API int64_t gnn_muon_workspace_bytes(const gnn_muon_matrix *matrices, int64_t n_matrices) {
@@ -784,9 +870,6 @@ extern "C" GNN_API int gnn_muon_step(const gnn_muon_matrix *matrices, int64_t n_
     j.muon = 1;
     j.nesterov = o.nesterov;
     j.mu = float(o.momentum);
-    j.a = float(o.a);
-    j.b = float(o.b);
-    j.c = float(o.c);
     j.eps = o.eps;
     j.grad_scale = o.grad_scale;
     struct List { const gnn_muon_matrix *matrices; double lr; } list{matrices, o.lr};
@@ -797,5 +880,5 @@ extern "C" GNN_API int gnn_muon_step(const gnn_muon_matrix *matrices, int64_t n_
             return Entry{t.grad, t.param, t.momentum, t.master, t.rows, t.cols, t.cols, t.cols, t.dtype, float(1.0 - l.lr * double(t.weight_decay)),
                       float(l.lr * double(t.update_scale)), t.grad == nullptr};
         },
-        &list, n_matrices, j, o.steps, static_cast<uint8_t *>(o.workspace), static_cast<hipStream_t>(o.stream));
+        &list, n_matrices, j, o.a, o.b, o.c, o.steps, static_cast<uint8_t *>(o.workspace), static_cast<hipStream_t>(o.stream));
 }

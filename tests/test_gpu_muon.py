@@ -224,3 +224,50 @@ def test_replays_and_other_streams(shapes):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, w) for x, w in zip(ps + ms, want))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(60, 100), (1100, 1000), (2049, 2100)])
+@pytest.mark.parametrize("coefficients", [(8.0, -2.0, 0.5), (0.5, 0.2, 0.1), (3.0, 4.0, 0.0), (2.0, 0.0, 0.0)])
+def test_coefficients_that_let_singular_values_grow_or_vanish(coefficients, rows, cols, dtype):
+    steps = 3
+    a, b, c = (abs(x) for x in coefficients)
+    u = matrix(rows, cols, dtype, torch.Generator().manual_seed(9))
+    o = orthogonalize([u], steps=steps, coefficients=coefficients)[0]
+    # A step's products are off by some ten times 2^-24 sqrt(m) (operands of 23 bits at least: twice that) of what they sum, whose size the same polynomial with
+    # positive coefficients bounds; later steps take an error by at most the largest slope of the polynomial between 0 and the largest singular value.
+    x = u.double()
+    x = x / (x.norm() + 1e-7)
+    far, m = 2.0 ** -23 * float(x.norm()), min(rows, cols)
+    for _ in range(steps):
+        top = float(torch.linalg.matrix_norm(x, 2))
+        terms, slope = a + b * top ** 2 + c * top ** 4, a + 3 * b * top ** 2 + 5 * c * top ** 4
+        far = far * slope + 20 * 2.0 ** -24 * m ** 0.5 * terms * float(x.norm())
+        x = newton_schulz_step(x, coefficients)
+    half = 2.0 ** -24 if dtype == F32 else 2.0 ** -8
+    assert torch.isfinite(o).all()
+    assert float((o.double() - x).norm()) <= far + half * float(x.norm())
+
+
+def newton_schulz_step(x, coefficients):
+    a, b, c = coefficients
+    if x.shape[0] > x.shape[1]:
+        return newton_schulz_step(x.t(), coefficients).t()
+    m = x @ x.t()
+    return a * x + (b * m + c * (m @ m)) @ x
+
+
+@pytest.mark.parametrize("steps", [1, 5, 9])
+@pytest.mark.parametrize("rows,cols", [(40, 90), (300, 200), (1100, 1000)])
+@pytest.mark.parametrize("factor", [1e-3, 1e-10, 1e-14, 1e-20, 1e-28])
+def test_matrices_far_smaller_than_eps(factor, rows, cols, steps):
+    """X is as small then, and the result is as close to it as that of a large one, relative to its size."""
+    u = matrix(rows, cols, F32, torch.Generator().manual_seed(10)) * factor
+    eps = 1e-7
+    o = orthogonalize([u], steps=steps, eps=eps)[0]
+    want = newton_schulz(u, steps=steps, eps=eps)
+    # while X is small a step multiplies it by 3.4445, its errors with it; near 1 as in allowed()
+    grows = min(3.4445 ** steps, max(1.0, float(want.norm())) * 485 / float((u.double() / (u.double().norm() + eps)).norm()))
+    start = float((u.double() / (u.double().norm() + eps)).norm())
+    assert torch.isfinite(o).all()
+    assert float((o.double() - want).norm()) <= 4 * 2.0 ** -24 * grows * start + steps * 20 * 2.0 ** -24 * min(rows, cols) ** 0.5 * float(want.norm())
