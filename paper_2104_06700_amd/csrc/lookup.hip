@@ -10,6 +10,9 @@
 // does the same work, with eight rows on their way, whether an id comes once or a million times.  A sum whose positions all lie in one run is
 // written by it; what crosses runs is joined in LDS, and what crosses workgroups by a second kernel, in fp64, in the order of the runs.  Rows
 // that no id names are zeroed by further workgroups of the same launch, which look their ids up in the sorted list.
+//
+// Gradient of few positions: one launch, no list (4,096 x 64 of 1,021 positions 16.1 -> 5.0 us, of 2,048 22.5 -> 5.9, all of one id 25 -> 31).  A workgroup compares some positions with all, which gives a bit for every position of the same id; the
+// position that comes first adds up the rows of them all, in fp64.
 #include "common.h"
 #include "rows.h"
 
@@ -21,9 +24,14 @@ constexpr int kAtOnce = 4;        // vectors of a thread on their way, forward
 // their way at once.
 constexpr int kRun = 32, kBatch = 8;
 constexpr int64_t kLong = 1 << 17; // positions from which on runs are long
-constexpr int64_t kRankHere = 4096; // positions up to which every workgroup finds the places of its ones among all
-constexpr int kRankRows = 32;     // of a workgroup then
-constexpr int kZeroRows = 256;    // rows of a workgroup that zeroes
+constexpr int64_t kRankHere = 8192; // positions up to which every workgroup finds the places of its ones among all (4,096 x 64 of 8,192: sorting 42 us, so 29)
+constexpr int kRankRows = 8;      // of a workgroup then (of 4,000: 32 rows 30 us, 8 rows 18)
+constexpr int kFew = 2048;        // positions up to which there is one launch, if ids do not come more often than eight times on average
+constexpr int kFewRows = 16;      // of a workgroup then
+constexpr int kFewLanesLog2 = 4;  // lanes of a group then, at most
+constexpr int kTogether = 32;     // positions of an id from which on all of the workgroup adds them up
+constexpr int kZeroWide = 2048;   // rows of a workgroup that zeroes then, at most
+constexpr int kZeroRows = 256;    // rows of a workgroup that zeroes, at most
 constexpr int64_t kMostRows = INT32_MAX, kMostColumns = 1 << 24;
 constexpr int64_t kMostSlices = 65535;  // workgroups in y: pieces of a row of as many vectors as a group has lanes
 static_assert((kMostColumns / 4 + 127) / 128 <= kMostSlices, "the widest rows");
@@ -130,7 +138,7 @@ struct Grad {
     int64_t rows, n, ldt, ldy, sum_blocks, zero_blocks;
     int32_t f, vectors, lanes_log2, run;
     uint32_t reciprocal;          // ceil(2^32 / vectors)
-    int32_t accumulate;
+    int32_t accumulate, zero_rows;
     float scale;
 };
 enum : uint32_t { kHead = 1, kThrough = 2, kTail = 4 };  // a run has: the end of a sum that began before, nothing but the middle of one, the beginning of one that goes on
@@ -158,7 +166,7 @@ __global__ void __launch_bounds__(kThreads) rank_kernel(const Ids ids, int n, ui
         }
     }
     __syncthreads();
-    // a thread a position and an eighth of the others, four at a time
+    // a thread a position and a 32nd of the others, four at a time
     const int i = int(blockIdx.x) * kRankRows + int(threadIdx.x) % kRankRows;
     int count = 0;
     if (i < n) {
@@ -213,13 +221,27 @@ template <typename TT, int E> __device__ __forceinline__ void write_sum(const Gr
     }
 }
 
-// rows [256 b, 256 b + 256) that no id names
+// rows v0 .. v0 + rows - 1, at most 256, where they are not named
+template <typename TT, int E> __device__ __forceinline__ void zero_unnamed(const Grad &a, int64_t v0, int rows, const uint8_t *named) {
+    TT *p = static_cast<TT *>(a.dtable) + v0 * a.ldt;
+    const float zero[E] = {};
+    // the rows' vectors side by side over the threads: stores of neighbouring rows meet in the same lines
+    const int64_t items = int64_t(rows) * a.vectors;
+    for (int64_t t = threadIdx.x; t < items; t += kThreads) {
+        const int r = a.vectors == 1 ? int(t) : items < (1 << 16) ? int(__umulhi(uint32_t(t), a.reciprocal)) : int(t / a.vectors);
+        if (named[r]) continue;
+        const int q = int(t - int64_t(r) * a.vectors), c = q * E < a.f - E ? q * E : a.f - E;
+        store_vector<TT, E, true>(p + r * a.ldt + c, zero);
+    }
+}
+
+// rows of part b, at most 256, that no id names
 template <typename TT, int E> __device__ __forceinline__ void zero_rows(const Grad &a, int64_t b) {
     static_assert(kZeroRows == kThreads, "a thread a row");
     __shared__ uint8_t named[kZeroRows];
     __shared__ int64_t range[2];
-    const int64_t v0 = b * kZeroRows;
-    const int rows = a.rows - v0 < kZeroRows ? int(a.rows - v0) : kZeroRows;
+    const int64_t v0 = b * a.zero_rows;
+    const int rows = a.rows - v0 < a.zero_rows ? int(a.rows - v0) : a.zero_rows;
     named[threadIdx.x] = 0;
     if (threadIdx.x < 2) range[threadIdx.x] = first_not_below(a.key, 0, a.n, uint32_t(v0 + (threadIdx.x ? rows : 0)));
     __syncthreads();
@@ -232,15 +254,143 @@ template <typename TT, int E> __device__ __forceinline__ void zero_rows(const Gr
         named[threadIdx.x] = j < hi && a.key[j] == v;
     }
     __syncthreads();
-    TT *p = static_cast<TT *>(a.dtable) + v0 * a.ldt;
-    const float zero[E] = {};
-    // the rows' vectors side by side over the threads: stores of neighbouring rows meet in the same lines
-    const int64_t items = int64_t(rows) * a.vectors;
-    for (int64_t t = threadIdx.x; t < items; t += kThreads) {
-        const int r = a.vectors == 1 ? int(t) : items < (1 << 16) ? int(__umulhi(uint32_t(t), a.reciprocal)) : int(t / a.vectors);
-        if (named[r]) continue;
-        const int q = int(t - int64_t(r) * a.vectors), c = q * E < a.f - E ? q * E : a.f - E;
-        store_vector<TT, E, true>(p + r * a.ldt + c, zero);
+    zero_unnamed<TT, E>(a, v0, rows, named);
+}
+
+// total += the rows of dY at positions `words` names words of `match` for: bit p of word w for position 32 w + p; B rows on their way
+template <typename TY, int E, int B> __device__ __forceinline__ void add_positions(const TY *dy, int64_t ldy, const uint32_t *match, uint64_t words, double (&total)[E]) {
+    uint32_t m = 0;
+    int w = 0;
+    for (;;) {
+        int from[B];
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
+            if (m == 0 && words != 0) {  // (a word that is named has a bit)
+                w = __builtin_ctzll(words);
+                words &= words - 1;
+                m = match[w];
+            }
+            from[u] = m ? w * 32 + __builtin_ctz(m) : -1;
+            m &= m - 1;  // (0 stays 0)
+        }
+        if (from[0] < 0) return;
+        Vector<TY, E> v[B];
+#pragma unroll
+        for (int u = 0; u < B; ++u) v[u].load(dy + int64_t(from[u] < 0 ? from[0] : from[u]) * ldy);
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
+            if (from[u] < 0) return;
+            float x[E];
+            v[u].get(x);
+#pragma unroll
+            for (int i = 0; i < E; ++i) total[i] += double(x[i]);
+        }
+    }
+}
+
+// At most kFew positions: workgroups of kFewRows of them, then those that zero.
+template <typename TY, typename TT, int E> __global__ void __launch_bounds__(kThreads) few_grad_kernel(const Grad a, const Ids ids, int zero_wide) {
+    static_assert(kFew == 64 * 32, "a bit a word");
+    const int n = int(a.n);
+    if (block_number() >= a.sum_blocks) {
+        if (blockIdx.y > 0) return;
+        __shared__ uint8_t named[kZeroWide];
+        const int64_t number = block_number() - a.sum_blocks;
+        if (number >= a.zero_blocks) return;
+        const int64_t v0 = number * zero_wide;
+        const int rows = a.rows - v0 < zero_wide ? int(a.rows - v0) : zero_wide;
+        for (int r = int(threadIdx.x); r < rows; r += kThreads) named[r] = 0;
+        __syncthreads();
+        for (int j = int(threadIdx.x); j < n; j += kThreads) {
+            const int64_t r = ids.at(j) - v0;
+            if (r >= 0 && r < rows) named[r] = 1;
+        }
+        __syncthreads();
+        for (int r = 0; r < rows; r += kZeroRows) zero_unnamed<TT, E>(a, v0 + r, rows - r < kZeroRows ? rows - r : kZeroRows, named + r);
+        return;
+    }
+    __shared__ __attribute__((aligned(16))) uint32_t all[kFew];
+    __shared__ uint32_t match[kFewRows][65];  // bit j of a row's: position j has its id
+    __shared__ unsigned long long words[kFewRows];
+    __shared__ int count[kFewRows];
+    __shared__ double parts[kThreads][E];
+    const int n_words = (n + 31) / 32, i0 = int(blockIdx.x) * kFewRows;
+    for (int j0 = int(threadIdx.x); j0 < n_words * 32; j0 += 4 * kThreads) {
+        int64_t v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = ids.at(j0 + u * kThreads < n ? j0 + u * kThreads : n - 1);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int j = j0 + u * kThreads;
+            if (j < n_words * 32) all[j] = j >= n || v[u] < 0 ? UINT32_MAX : uint32_t(v[u]);
+        }
+    }
+    if (threadIdx.x < kFewRows) {
+        words[threadIdx.x] = 0;
+        count[threadIdx.x] = 0;
+    }
+    __syncthreads();
+    {
+        const int r = int(threadIdx.x) % kFewRows;
+        const uint32_t k = i0 + r < n ? all[i0 + r] : UINT32_MAX;
+        if (k != UINT32_MAX)
+            for (int w = int(threadIdx.x) / kFewRows; w < n_words; w += kThreads / kFewRows) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    const u32x4 t = *reinterpret_cast<const u32x4 *>(all + w * 32 + j);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) m |= uint32_t(t[e] == k) << (j + e);
+                }
+                match[r][w] = m;
+                if (m) {
+                    atomicOr(&words[r], 1ull << w);
+                    atomicAdd(&count[r], __builtin_popcount(m));
+                }
+            }
+    }
+    __syncthreads();
+    const int lanes = 1 << a.lanes_log2, lane = int(threadIdx.x) & (lanes - 1), group = int(threadIdx.x) >> a.lanes_log2, groups = kThreads >> a.lanes_log2;
+    const int q = int(blockIdx.y) * lanes + lane;
+    const bool mine = q < a.vectors;
+    const int c = !mine ? 0 : q * E < a.f - E ? q * E : a.f - E;
+    const int own = q * E < a.f - E ? E : a.f - q * E;
+    const TY *dy = static_cast<const TY *>(a.dy) + c;
+    auto first_of_its_id = [&](int r) {
+        const int w = __builtin_ctzll(words[r]);
+        return w * 32 + __builtin_ctz(match[r][w]) == i0 + r;
+    };
+    bool together = false;
+    for (int r = 0; r < kFewRows; ++r) together |= count[r] >= kTogether;
+    for (int r = group; r < kFewRows; r += groups) {
+        if (count[r] == 0 || count[r] >= kTogether || !first_of_its_id(r)) continue;
+        double total[E] = {};
+        add_positions<TY, E, 4>(dy, a.ldy, match[r], words[r], total);
+        float x[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = float(total[i]);
+        if (mine) write_sum<TT, E>(a, all[i0 + r], c, own, x);
+    }
+    if (!together) return;
+    const uint64_t every = groups >= 64 ? (group < 64 ? 1ull << group : 0ull) : ~0ull / ((1ull << groups) - 1) << group;  // words group, group + groups, ...
+    for (int r = 0; r < kFewRows; ++r) {
+        if (count[r] < kTogether || !first_of_its_id(r)) continue;
+        double total[E] = {};
+        add_positions<TY, E, 8>(dy, a.ldy, match[r], words[r] & every, total);
+#pragma unroll
+        for (int i = 0; i < E; ++i) parts[threadIdx.x][i] = total[i];
+        __syncthreads();
+        if (group == 0 && mine) {
+            float x[E];
+            const int have = groups < 64 ? groups : 64;
+            for (int g = 1; g < have; ++g)
+#pragma unroll
+                for (int i = 0; i < E; ++i) total[i] += parts[(g << a.lanes_log2) + lane][i];
+#pragma unroll
+            for (int i = 0; i < E; ++i) x[i] = float(total[i]);
+            write_sum<TT, E>(a, all[i0 + r], c, own, x);
+        }
+        __syncthreads();
     }
 }
 
@@ -503,6 +653,23 @@ template <typename TY, typename TT, int E> int launch_grad(const Grad &a, int64_
     }
     return GNN_OK;
 }
+template <typename TY, typename TT, int E> int launch_few(Grad a, const Ids &ids, hipStream_t stream) {
+    // groups of few lanes, so that a workgroup has many: 1,021 and 2,048 positions of one id x 602 52 and 184 us with 64 lanes, 21 and 60 so
+    if (a.lanes_log2 > kFewLanesLog2 && a.vectors <= kMostSlices) a.lanes_log2 = kFewLanesLog2;
+    const int64_t slices = (a.vectors + (int64_t(1) << a.lanes_log2) - 1) >> a.lanes_log2;
+    // rows of a workgroup that zeroes: about 64 KB of fp32, several times the ids that it reads (4,096 x 602 of 1,021 positions in 16 workgroups 24 us, in 256 7.2)
+    int wide = kZeroWide;
+    while (wide > 16 && int64_t(wide) * a.f > 16384) wide /= 2;
+    a.sum_blocks = (a.n + kFewRows - 1) / kFewRows;
+    a.zero_blocks = a.accumulate ? 0 : (a.rows + wide - 1) / wide;
+    few_grad_kernel<TY, TT, E><<<grid_of(a.sum_blocks + a.zero_blocks, slices), kThreads, 0, stream>>>(a, ids, wide);
+    GNN_HIP_TRY(hipGetLastError());
+    return GNN_OK;
+}
+template <typename TY, typename TT> int few(const Grad &a, const Ids &ids, hipStream_t stream) {
+    constexpr int E = gnn_rows<TY>::VEC;
+    return a.f < E ? launch_few<TY, TT, 1>(a, ids, stream) : launch_few<TY, TT, E>(a, ids, stream);
+}
 template <typename TY, typename TT> int grad(const Grad &a, int64_t slices, hipStream_t stream) {
     constexpr int E = gnn_rows<TY>::VEC;
     return a.f < E ? launch_grad<TY, TT, 1>(a, slices, stream) : launch_grad<TY, TT, E>(a, slices, stream);
@@ -563,7 +730,15 @@ extern "C" GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dta
     a.accumulate = o.accumulate;
     a.scale = o.scale;
     a.sum_blocks = r.blocks;
-    a.zero_blocks = o.accumulate ? 0 : (V + kZeroRows - 1) / kZeroRows;
+    // small tables: less rows a workgroup, so that there are 1,024 of them (4,096 x 602 of 5,000 positions 56 us with 256 rows, 41 with 16)
+    a.zero_rows = kZeroRows;
+    while (a.zero_rows > 16 && V < int64_t(a.zero_rows) * 1024) a.zero_rows /= 2;
+    a.zero_blocks = o.accumulate ? 0 : (V + a.zero_rows - 1) / a.zero_rows;
+    const Ids named{ids, o.ids_is_64, V};
+    if (n > 0 && n <= kFew && n <= 8 * V) {
+        if (o.dtype == GNN_F32) return o.table_dtype == GNN_F32 ? few<float, float>(a, named, stream) : few<float, gnn_bf16>(a, named, stream);
+        return o.table_dtype == GNN_F32 ? few<gnn_bf16, float>(a, named, stream) : few<gnn_bf16, gnn_bf16>(a, named, stream);
+    }
     if (n > 0) {
         uint32_t *next = static_cast<uint32_t *>(o.workspace);
         uint32_t *buf_k[2] = {next, next + r.padded}, *buf_v[2] = {next + 2 * r.padded, next + 3 * r.padded};
@@ -574,7 +749,6 @@ extern "C" GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dta
         next += r.blocks * F;
         a.flags = next;
         next += r.blocks;
-        const Ids named{ids, o.ids_is_64, V};
         if (n <= kRankHere) {
             rank_kernel<<<unsigned((n + kRankRows - 1) / kRankRows), kThreads, 0, stream>>>(named, int(n), buf_k[0], buf_v[0]);
             GNN_HIP_TRY(hipGetLastError());

@@ -20,7 +20,7 @@ constexpr int kThreads = 256;
 constexpr int kItems = 1024;           // pieces of eight columns of a workgroup
 constexpr int kBlock = GNN_STORE_BLOCK;
 constexpr int64_t kCompareHere = 4096; // positions up to which every workgroup compares its rows' ids with all of them
-constexpr int kCompareRows = 32;       // rows of a workgroup then
+constexpr int kCompareRows = 16;       // rows of a workgroup then
 constexpr int kStoreRows = kItems / (kBlock / 8), kLoadRows = kItems;  // of a workgroup at most
 constexpr int kPartsLog2 = 3, kParts = 1 << kPartsLog2, kChunk = 512;
 constexpr int64_t kMostRows = INT32_MAX, kMostColumns = 1 << 24;
@@ -109,7 +109,7 @@ __device__ __forceinline__ uint32_t codes4(const float (&x)[8], int j, float sca
 }
 
 // Columns 8 q .. 8 q + 8 of a row in 8 bits, with those of the three threads beside this one.
-__device__ __forceinline__ void write8(const Rows &a, int64_t offset, int q, const float (&x)[8]) {
+template <bool NT> __device__ __forceinline__ void write8(const Rows &a, int64_t offset, int q, const float (&x)[8]) {
     const int c = q * 8, left = a.f - c, have = left < 0 ? 0 : left < 8 ? left : 8;
     uint32_t top = 0;
 #pragma unroll
@@ -140,7 +140,8 @@ __device__ __forceinline__ void write8(const Rows &a, int64_t offset, int q, con
             if ((__float_as_uint(x[j]) & 0x7FFFFFFFu) >= 0x7F800000u) w[j / 4] |= 0x7Fu << (8 * (j % 4));
     uint8_t *to = a.store + offset;
     if (have == 8) {
-        __builtin_nontemporal_store(u32x2_any{w[0], w[1]}, reinterpret_cast<u32x2_any *>(to + c));
+        if constexpr (NT) __builtin_nontemporal_store(u32x2_any{w[0], w[1]}, reinterpret_cast<u32x2_any *>(to + c));
+        else *reinterpret_cast<u32x2_any *>(to + c) = u32x2_any{w[0], w[1]};
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -149,59 +150,82 @@ __device__ __forceinline__ void write8(const Rows &a, int64_t offset, int q, con
     if ((q & 3) == 0) to[a.f + (q >> 2)] = uint8_t(e);
 }
 
-template <typename T, bool COMPARE> __global__ void __launch_bounds__(kThreads) store_kernel(const Rows a) {
+constexpr int kAtOnce = 4;  // pieces of a thread on their way
+
+// Few positions: rows are fetched before their ids are compared (1,021 rows x 64 fp32 9.0 us in the kernel with the way below, 5.0 so).
+template <typename T> __global__ void __launch_bounds__(kThreads) few_store_kernel(const Rows a) {
+    const int row0 = int(blockIdx.x) * a.rows, n = int(a.n), rows = n - row0 < a.rows ? n - row0 : a.rows;
+    __shared__ __attribute__((aligned(16))) int32_t ids[kCompareHere];
+    __shared__ int again[kCompareRows];  // a later position has this row's id
+    const T *x0 = static_cast<const T *>(a.x) + row0 * a.ldx;
+    const int items = rows * a.pieces;
+    int row[kAtOnce], q[kAtOnce];
+    float x[kAtOnce][8];
+    auto fetch = [&](int t0) {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int t = t0 + u * kThreads < items ? t0 + u * kThreads : items - 1;
+            row[u] = a.row_of(t);
+            q[u] = t - row[u] * a.pieces;
+            const int left = a.f - q[u] * 8, have = left < 0 ? 0 : left < 8 ? left : 8;
+            load8<T>(x0 + row[u] * a.ldx + q[u] * 8, have, x[u]);
+        }
+    };
+    const int fours = (n + 3) / 4 * 4;
+    for (int j0 = row0 / 4 * 4 + int(threadIdx.x); j0 < fours; j0 += 4 * kThreads) {  // (positions before do not matter)
+        int32_t v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = int32_t(a.id(j0 + u * kThreads < n ? j0 + u * kThreads : n - 1));
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (j0 + u * kThreads < fours) ids[j0 + u * kThreads] = j0 + u * kThreads < n ? v[u] : INT32_MIN;
+    }
+    fetch(int(threadIdx.x));
+    if (threadIdx.x < kCompareRows) again[threadIdx.x] = 0;
+    __syncthreads();
+    // a thread a row and a sixteenth of the positions, four at a time
+    const int r = int(threadIdx.x) % kCompareRows, i = row0 + r;
+    if (r < rows) {
+        const int32_t id = ids[i];
+        bool found = false;
+#pragma unroll 4
+        for (int j = row0 / 4 * 4 + int(threadIdx.x) / kCompareRows * 4; j < n; j += kThreads / kCompareRows * 4) {
+            const i32x4 t = *reinterpret_cast<const i32x4 *>(ids + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) found |= t[e] == id && j + e > i;
+        }
+        if (found) again[r] = 1;
+    }
+    __syncthreads();
+    for (int t0 = int(threadIdx.x); t0 < items;) {  // (pieces is a multiple of four: the threads of a block take part together)
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            if (t0 + u * kThreads >= items) continue;
+            const int64_t id = ids[row0 + row[u]];
+            if (id >= 0 && !again[row[u]]) write8<false>(a, id * a.lds, q[u], x[u]);
+        }
+        t0 += kThreads * kAtOnce;
+        if (t0 < items) fetch(t0);
+    }
+}
+
+template <typename T> __global__ void __launch_bounds__(kThreads) store_kernel(const Rows a) {
     const int64_t row0 = block_number() * a.rows;
     if (row0 >= a.n) return;
     const int rows = a.n - row0 < a.rows ? int(a.n - row0) : a.rows;
-    __shared__ __attribute__((aligned(16))) int32_t ids[COMPARE ? kCompareHere : 4];
-    __shared__ int again[kCompareRows];  // a later position has this row's id
     __shared__ Place places[kStoreRows];
     __shared__ int written;
     if (threadIdx.x == 0) written = 0;
-    if constexpr (COMPARE) {
-        const int n = int(a.n);
-        for (int j0 = int(threadIdx.x); j0 < n; j0 += 4 * kThreads) {
-            int32_t v[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = int32_t(a.id(j0 + u * kThreads < n ? j0 + u * kThreads : n - 1));
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (j0 + u * kThreads < n) ids[j0 + u * kThreads] = v[u];
-        }
-        if (threadIdx.x < kCompareRows) again[threadIdx.x] = 0;
-        __syncthreads();
-        // a thread a row and an eighth of the positions, four at a time
-        const int r = int(threadIdx.x) % kCompareRows, i = int(row0) + r;
-        if (r < rows) {
-            const int32_t id = ids[i];
-            bool found = false;
-#pragma unroll 4
-            for (int j = int(threadIdx.x) / kCompareRows * 4; j < n; j += kThreads / kCompareRows * 4) {
-                const i32x4 t = *reinterpret_cast<const i32x4 *>(ids + j);  // (behind the last position: not looked at)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) found |= t[e] == id && j + e > i && j + e < n;
-            }
-            if (found) again[r] = 1;
-        }
-    }
     __syncthreads();
     // the rows that are written, in any order
     for (int r = int(threadIdx.x); r < rows; r += kThreads) {
-        int64_t id;
-        bool stays;
-        if constexpr (COMPARE) {
-            id = ids[row0 + r];
-            stays = id >= 0 && !again[r];
-        } else {
-            id = a.id(row0 + r);
-            stays = id >= 0 && (!a.last || a.last[id] == int32_t(row0 + r));
-        }
-        if (stays) places[atomicAdd(&written, 1)] = {id * a.lds, r * a.ldx};
+        const int64_t id = a.id(row0 + r);
+        if (id >= 0 && (!a.last || a.last[id] == int32_t(row0 + r))) places[atomicAdd(&written, 1)] = {id * a.lds, r * a.ldx};
     }
     __syncthreads();
     const T *x0 = static_cast<const T *>(a.x) + row0 * a.ldx;
     const int items = written * a.pieces;
-    constexpr int U = 4;
+    constexpr int U = kAtOnce;
     for (int t0 = int(threadIdx.x); t0 < items; t0 += kThreads * U) {  // (pieces is a multiple of four: the threads of a block take part together)
         Place at[U];
         int q[U];
@@ -219,7 +243,7 @@ template <typename T, bool COMPARE> __global__ void __launch_bounds__(kThreads) 
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (t0 + u * kThreads < items) write8(a, at[u].store, q[u], x[u]);
+            if (t0 + u * kThreads < items) write8<true>(a, at[u].store, q[u], x[u]);
     }
 }
 
@@ -372,8 +396,8 @@ extern "C" GNN_API int gnn_store_rows(const void *X, const void *ids, void *stor
         GNN_HIP_TRY(hipGetLastError());
     }
     const dim3 grid = grid_of((n + a.rows - 1) / a.rows);
-    if (o.dtype == GNN_F32) compare ? store_kernel<float, true><<<grid, kThreads, 0, stream>>>(a) : store_kernel<float, false><<<grid, kThreads, 0, stream>>>(a);
-    else compare ? store_kernel<gnn_bf16, true><<<grid, kThreads, 0, stream>>>(a) : store_kernel<gnn_bf16, false><<<grid, kThreads, 0, stream>>>(a);
+    if (o.dtype == GNN_F32) compare ? few_store_kernel<float><<<grid, kThreads, 0, stream>>>(a) : store_kernel<float><<<grid, kThreads, 0, stream>>>(a);
+    else compare ? few_store_kernel<gnn_bf16><<<grid, kThreads, 0, stream>>>(a) : store_kernel<gnn_bf16><<<grid, kThreads, 0, stream>>>(a);
     GNN_HIP_TRY(hipGetLastError());
     return GNN_OK;
 }

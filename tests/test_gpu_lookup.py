@@ -284,3 +284,51 @@ def test_the_widest_rows():
     y = torch.empty(5, f, device=DEV)
     gnn.gnn_lookup_fwd(dt, ids, y)
     assert torch.equal(y[0], dt[2]) and not y[1].any() and torch.equal(y[2], dt[0])
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16)])
+@pytest.mark.parametrize("f", [1, 4, 33, 100, 260, 602])
+@pytest.mark.parametrize("n,repeats", [(15, 1), (16, 16), (17, 17), (64, 31), (500, 32), (500, 33), (2047, 700), (2048, 2048), (2049, 2049)])
+def test_sums_of_few_positions(n, repeats, f, types, accumulate):
+    """One id `repeats` times among others, at random places."""
+    gen = torch.Generator().manual_seed(n + f)
+    v = max(600, n)
+    ids = torch.randperm(v, generator=gen)[:n]
+    ids[torch.randperm(n, generator=gen)[:repeats]] = 5
+    ids[n // 3] = v + 1
+    dy = rows_of(gen, n, f, types[1], f + 3)
+    dtable = torch.randn(v, f + 1, generator=gen).to(types[0]).to(DEV)
+    start = dtable.cpu().double()
+    ws = torch.full((gnn.gnn_lookup_workspace_bytes(v, n, f),), 255, device=DEV, dtype=torch.uint8)
+    gnn.gnn_lookup_bwd(ids.to(DEV), dy, dtable[:, :f], scale=0.5, accumulate=accumulate, workspace=ws)
+    got = dtable.cpu().double()
+    assert torch.equal(got[:, f], start[:, f])
+    keep = ids < v
+    want, size = torch.zeros(v, f, dtype=torch.float64), torch.zeros(v, f, dtype=torch.float64)
+    d = dy.cpu().double()
+    want.index_add_(0, ids[keep], 0.5 * d[keep])
+    size.index_add_(0, ids[keep], 0.5 * d[keep].abs())
+    if accumulate:
+        want, size = want + start[:, :f], size + start[:, :f].abs()
+    # SUM, a rounding of the sum with what was there, and that to the table's type
+    assert ((got[:, :f] - want).abs() <= (SUM + 2.0 ** -24) * size + HALF[types[0]] * want.abs() * 1.01).all()
+    if not accumulate:
+        unnamed = torch.ones(v, dtype=torch.bool)
+        unnamed[ids[keep]] = False
+        assert (got[unnamed][:, :f] == 0).all()
+
+
+@pytest.mark.parametrize("v", [262144, 262145, 1000003])
+def test_few_positions_of_large_tables(v):
+    gen = torch.Generator().manual_seed(v)
+    ids = torch.randint(0, v, (100,), generator=gen)
+    ids[:3] = torch.tensor([0, v - 1, v - 2])
+    dy = torch.randn(100, 6, generator=gen).to(DEV)
+    dtable = torch.full((v, 6), float("nan"), device=DEV)
+    ws = torch.empty(gnn.gnn_lookup_workspace_bytes(v, 100, 6), device=DEV, dtype=torch.uint8)
+    gnn.gnn_lookup_bwd(ids.to(DEV), dy, dtable, scale=1.0, workspace=ws)
+    want = torch.zeros(v, 6, dtype=torch.float64).index_add_(0, ids, dy.cpu().double())
+    size = torch.zeros(v, 6, dtype=torch.float64).index_add_(0, ids, dy.cpu().double().abs())
+    assert ((dtable.cpu().double() - want).abs() <= SUM * size).all()
+    assert int((dtable != 0).any(1).sum()) == len(set(ids.tolist()))
