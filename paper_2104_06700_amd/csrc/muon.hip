@@ -264,7 +264,8 @@ template <int P, typename T> __global__ void __launch_bounds__(kThreads) planes_
     const bool fits = norm <= 1.7e308;
     const float log_norm = fits ? log2f(float(norm / (norm + j.eps))) : 0.0f;
     if (tile == 0 && threadIdx.x == 0) t.squares[t.norm_blocks] = double(log_norm);
-    const double inverse = fits ? ldexp(double(Parts<P>::kX), exponent<P>(j, log_norm, 0)) / (norm + j.eps) : __builtin_nan("");  // what is not finite reaches all of the matrix
+    // what is not finite reaches all of the matrix; of zeros nothing is divided by an eps whose reciprocal may not be finite
+    const double inverse = !fits ? __builtin_nan("") : norm > 0.0 ? ldexp(double(Parts<P>::kX), exponent<P>(j, log_norm, 0)) / (norm + j.eps) : 0.0;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
         const int row = r0 + wave + 4 * k;

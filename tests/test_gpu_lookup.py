@@ -332,3 +332,21 @@ def test_few_positions_of_large_tables(v):
     size = torch.zeros(v, 6, dtype=torch.float64).index_add_(0, ids, dy.cpu().double().abs())
     assert ((dtable.cpu().double() - want).abs() <= SUM * size).all()
     assert int((dtable != 0).any(1).sum()) == len(set(ids.tolist()))
+
+
+@pytest.mark.parametrize("n,v,dtype", [(530000, 1000, F32), (1050001, 47, BF16), (1050000, 2000000, BF16)])
+def test_whole_lines_beyond_the_caches(n, v, dtype):
+    f = 128
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    ids = torch.randint(-1, v, (n,), device=DEV, generator=gen)
+    dy = torch.randn(n, f, device=DEV, generator=gen).to(dtype)
+    assert n * f * dy.element_size() > 256 << 20
+    dtable = torch.full((v, f), float("nan"), device=DEV)
+    ws = torch.empty(gnn.gnn_lookup_workspace_bytes(v, n, f), device=DEV, dtype=torch.uint8)
+    gnn.gnn_lookup_bwd(ids, dy, dtable, scale=1.0, workspace=ws)
+    at = torch.where(ids < 0, v, ids)
+    want, size = (torch.zeros(v + 1, f, device=DEV, dtype=torch.float64) for _ in range(2))
+    for part in torch.arange(n, device=DEV).split(200000):
+        want.index_add_(0, at[part], dy[part].double())
+        size.index_add_(0, at[part], dy[part].double().abs())
+    assert ((dtable.double() - want[:v]).abs() <= SUM * size[:v]).all()

@@ -271,3 +271,9 @@ def test_matrices_far_smaller_than_eps(factor, rows, cols, steps):
     start = float((u.double() / (u.double().norm() + eps)).norm())
     assert torch.isfinite(o).all()
     assert float((o.double() - want).norm()) <= 4 * 2.0 ** -24 * grows * start + steps * 20 * 2.0 ** -24 * min(rows, cols) ** 0.5 * float(want.norm())
+
+
+@pytest.mark.parametrize("coefficients", [COEFFICIENTS, (3.0, 4.0, 0.0)])
+@pytest.mark.parametrize("eps", [1e-300, 5e-324, 1e300])
+def test_zeros_with_any_eps(eps, coefficients):
+    assert (orthogonalize([torch.zeros(40, 50, device=DEV)], eps=eps, coefficients=coefficients)[0] == 0).all()
