@@ -206,12 +206,14 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const uint32_t
     }
 }
 
-// totals: of the digits, where the table holds the places among pairs of the same digit; null: it holds the places.  vals_in null: the value of pair i is i.  inverse: vals_out[value] = place of the pair, and no keys are written
+// What the table has of a tile's digit: its first place, its first place among pairs of the same digit (`totals` has how many there are), or the tile's count.
+enum SortTable { kPlaces, kPlacesOfDigit, kCounts };
+// vals_in null: the value of pair i is i.  inverse: vals_out[value] = place of the pair, and no keys are written
 template <bool INVERSE>
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const uint32_t *__restrict__ keys_in,
                                                                     const uint32_t *__restrict__ vals_in, int64_t n, int shift,
                                                                     uint32_t from_top, int64_t n_tiles,
-                                                                    const uint32_t *__restrict__ table, const uint32_t *__restrict__ totals,
+                                                                    const uint32_t *__restrict__ table, SortTable has, const uint32_t *__restrict__ totals,
                                                                     uint32_t *__restrict__ keys_out, uint32_t *__restrict__ vals_out) {
     __shared__ uint32_t hist[kSortWaves][256];  // pairs per wavefront and digit, then those of the wavefronts before
     __shared__ uint32_t digit_begin[256];       // first place of a digit in the tile
@@ -229,6 +231,21 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const uint32
         key[r] = i < n ? keys_in[i] : 0u;
         if (from_top) key[r] = from_top - key[r];
         val[r] = vals_in ? (i < n ? vals_in[i] : 0u) : uint32_t(i);
+    }
+    uint32_t all = 0, lower = 0;  // pairs of thread d's digit, and how many of them lie in tiles before
+    if (threadIdx.x < 256 && has != kPlaces) {
+        const uint32_t *row = table + int64_t(threadIdx.x) * n_tiles;
+        if (has == kPlacesOfDigit) {
+            all = totals[threadIdx.x];
+            lower = row[blockIdx.x];
+        } else {
+#pragma unroll 8
+            for (int t = 0; t < int(n_tiles); ++t) {
+                const uint32_t c = row[t];
+                all += c;
+                if (t < int(blockIdx.x)) lower += c;
+            }
+        }
     }
     __syncthreads();
 #pragma unroll
@@ -256,8 +273,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const uint32
         const uint32_t upto = wave_scan_inclusive(total);
         if (lane == 63) wave_total[wave] = upto;
         digit_begin[d] = upto - total;
-        if (totals) {
-            const uint32_t all = totals[d], all_upto = wave_scan_inclusive(all);
+        if (has != kPlaces) {
+            const uint32_t all_upto = wave_scan_inclusive(all);
             if (lane == 63) wave_all[wave] = all_upto;
             digit_out[d] = all_upto - all;
         }
@@ -265,13 +282,13 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const uint32
     __syncthreads();
     if (threadIdx.x < 256) {
         const int d = threadIdx.x;
-        uint32_t begin = digit_begin[d], first = totals ? digit_out[d] : 0u;
+        uint32_t begin = digit_begin[d], first = has != kPlaces ? digit_out[d] + lower : table[int64_t(d) * n_tiles + blockIdx.x];
         for (int w = 0; w < wave; ++w) {
             begin += wave_total[w];
-            if (totals) first += wave_all[w];
+            if (has != kPlaces) first += wave_all[w];
         }
         digit_begin[d] = begin;
-        digit_out[d] = first + table[int64_t(d) * n_tiles + blockIdx.x] - begin;
+        digit_out[d] = first - begin;
     }
     __syncthreads();
 #pragma unroll
@@ -297,7 +314,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const uint32
 }
 
 // Few tiles: a workgroup scans the row of a digit and leaves its total behind, and the tiles add up the totals of the digits before.  One launch a pass instead of two.
-constexpr int64_t kRowScanTiles = 4096;
+// Very few: every tile adds up the counts by itself, no launch (gradient of a table of 50 K positions of 300 K x 64 66 us, scanned 73).
+constexpr int64_t kRowScanTiles = 4096, kNoScanTiles = 64;
 __global__ void __launch_bounds__(256) sort_rows_kernel(uint32_t *__restrict__ table, int64_t n_tiles, uint32_t *__restrict__ totals) {
     __shared__ uint32_t wave_total[4];
     uint32_t *row = table + int64_t(blockIdx.x) * n_tiles;
@@ -341,18 +359,17 @@ int radix_sort(const SortJob &job, int64_t n, int bits, uint32_t *table, uint32_
         uint32_t *kout = last && job.last_keys ? job.last_keys : job.buf_k[cur ^ 1];
         uint32_t *vout = last && job.last_vals ? job.last_vals : job.buf_v[cur ^ 1];
         sort_count_kernel<<<grid, kSortThreads, 0, stream>>>(kin, n, shift, from_top, n_tiles, table);
-        const bool rows = n_tiles <= kRowScanTiles;
-        if (rows) {
+        const SortTable has = n_tiles <= kNoScanTiles ? kCounts : n_tiles <= kRowScanTiles ? kPlacesOfDigit : kPlaces;
+        if (has == kPlacesOfDigit) {
             sort_rows_kernel<<<256, 256, 0, stream>>>(table, n_tiles, sums);
-        } else {
+        } else if (has == kPlaces) {
             const int rc = scan_exclusive<uint32_t>(table, n_tiles * 256, 1, 0, false, sums, stream);
             if (rc != GNN_OK) return rc;
         }
-        const uint32_t *totals = rows ? sums : nullptr;
         if (last && job.inverse_last)
-            sort_scatter_kernel<true><<<grid, kSortThreads, 0, stream>>>(kin, vin, n, shift, from_top, n_tiles, table, totals, kout, vout);
+            sort_scatter_kernel<true><<<grid, kSortThreads, 0, stream>>>(kin, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
         else
-            sort_scatter_kernel<false><<<grid, kSortThreads, 0, stream>>>(kin, vin, n, shift, from_top, n_tiles, table, totals, kout, vout);
+            sort_scatter_kernel<false><<<grid, kSortThreads, 0, stream>>>(kin, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
         if (hipGetLastError() != hipSuccess) return GNN_ERR_LAUNCH;
         kin = kout;
         vin = vout;
