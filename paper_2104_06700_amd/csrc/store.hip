@@ -108,8 +108,9 @@ __device__ __forceinline__ uint32_t codes4(const float (&x)[8], int j, float sca
     return __builtin_bit_cast(uint32_t, t);
 }
 
-// Columns 8 q .. 8 q + 8 of a row in 8 bits, with those of the three threads beside this one.
-__device__ __forceinline__ void write8(const Rows &a, int64_t offset, int q, const float (&x)[8]) {
+// Columns 8 q .. 8 q + 8 of a row in 8 bits, with those of the three threads beside this one.  PAST: past the caches, as many rows as they do not hold are
+// (1.2 M rows x 256 bf16 with other inputs between 213 us, through the caches 237; written again and again to the same places 213 and 177).
+template <bool PAST> __device__ __forceinline__ void write8(const Rows &a, int64_t offset, int q, const float (&x)[8]) {
     const int c = q * 8, left = a.f - c, have = left < 0 ? 0 : left < 8 ? left : 8;
     uint32_t top = 0;
 #pragma unroll
@@ -140,8 +141,8 @@ __device__ __forceinline__ void write8(const Rows &a, int64_t offset, int q, con
             if ((__float_as_uint(x[j]) & 0x7FFFFFFFu) >= 0x7F800000u) w[j / 4] |= 0x7Fu << (8 * (j % 4));
     uint8_t *to = a.store + offset;
     if (have == 8) {
-        // (through the caches, where neighbouring rows that share a line may meet: 1.2 M rows x 256 bf16 of 2.4 M 213 -> 177 us)
-        *reinterpret_cast<u32x2_any *>(to + c) = u32x2_any{w[0], w[1]};
+        if constexpr (PAST) __builtin_nontemporal_store(u32x2_any{w[0], w[1]}, reinterpret_cast<u32x2_any *>(to + c));
+        else *reinterpret_cast<u32x2_any *>(to + c) = u32x2_any{w[0], w[1]};
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -202,7 +203,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) few_store_kern
         for (int u = 0; u < kAtOnce; ++u) {
             if (t0 + u * kThreads >= items) continue;
             const int64_t id = ids[row0 + row[u]];
-            if (id >= 0 && !again[row[u]]) write8(a, id * a.lds, q[u], x[u]);
+            if (id >= 0 && !again[row[u]]) write8<false>(a, id * a.lds, q[u], x[u]);
         }
         t0 += kThreads * kAtOnce;
         if (t0 < items) fetch(t0);
@@ -243,7 +244,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) store_kernel(c
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (t0 + u * kThreads < items) write8(a, at[u].store, q[u], x[u]);
+            if (t0 + u * kThreads < items) write8<true>(a, at[u].store, q[u], x[u]);
     }
 }
 
