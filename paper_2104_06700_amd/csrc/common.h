@@ -285,8 +285,14 @@ void gnn_host_block_free(void *p);
 // gnn_sort_sums_elems(n) words.
 int gnn_radix_sort_pairs(uint32_t *buf_k[2], uint32_t *buf_v[2], int64_t n, int bits, uint32_t *table, uint32_t *sums,
                          hipStream_t stream, int *out);
-// The same of keys alone, at least one bit of them: positions[i] is where the i-th of the sorted keys stood.  buf_k[0] holds the input.
-int gnn_radix_sort_positions(uint32_t *buf_k[2], uint32_t *buf_v[2], int64_t n, int bits, uint32_t *table, uint32_t *sums,
+// The same of ids, by at least one bit of the keys that they become: the id, or `rows` where it names none of the rows.  positions[i] is where the i-th
+// of the sorted keys stood.
+struct gnn_sort_ids {
+    const void *p;   // [n] int32_t or int64_t
+    int32_t is_64;
+    int64_t rows;
+};
+int gnn_radix_sort_positions(const gnn_sort_ids &ids, uint32_t *buf_k[2], uint32_t *buf_v[2], int64_t n, int bits, uint32_t *table, uint32_t *sums,
                              hipStream_t stream, uint32_t **keys, uint32_t **positions);
 int64_t gnn_sort_table_elems(int64_t n);
 int64_t gnn_sort_sums_elems(int64_t n);

@@ -175,8 +175,16 @@ __device__ __forceinline__ unsigned long long same_digit_lanes(unsigned digit, b
     return peers;
 }
 
+// Key i: of 32 bits, or (ids) that of an id of 32 or 64 bits, `rows` where it names none of them.
+template <bool IDS> __device__ __forceinline__ uint32_t sort_key(const void *__restrict__ keys, const gnn_sort_ids &ids, int64_t i) {
+    if constexpr (!IDS) return static_cast<const uint32_t *>(keys)[i];
+    const int64_t id = ids.is_64 ? static_cast<const int64_t *>(keys)[i] : int64_t(static_cast<const int32_t *>(keys)[i]);
+    return uint64_t(id) < uint64_t(ids.rows) ? uint32_t(id) : uint32_t(ids.rows);
+}
+
 // from_top: the first pass of a descending order reads key k as from_top - k
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const uint32_t *__restrict__ keys, int64_t n, int shift,
+template <bool IDS>
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const void *__restrict__ keys, gnn_sort_ids ids, int64_t n, int shift,
                                                                   uint32_t from_top, int64_t n_tiles, uint32_t *__restrict__ table) {
     __shared__ uint32_t hist[kSortWaves][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -185,7 +193,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const uint32_t
     uint32_t key[kSortRounds];
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r) {
-        key[r] = i0 + r * 64 < n ? keys[i0 + r * 64] : 0u;
+        key[r] = i0 + r * 64 < n ? sort_key<IDS>(keys, ids, i0 + r * 64) : 0u;
         if (from_top) key[r] = from_top - key[r];
     }
     __syncthreads();
@@ -209,8 +217,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const uint32_t
 // What the table has of a tile's digit: its first place, its first place among pairs of the same digit (`totals` has how many there are), or the tile's count.
 enum SortTable { kPlaces, kPlacesOfDigit, kCounts };
 // vals_in null: the value of pair i is i.  inverse: vals_out[value] = place of the pair, and no keys are written
-template <bool INVERSE>
-__global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const uint32_t *__restrict__ keys_in,
+template <bool INVERSE, bool IDS>
+__global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const void *__restrict__ keys_in, gnn_sort_ids ids,
                                                                     const uint32_t *__restrict__ vals_in, int64_t n, int shift,
                                                                     uint32_t from_top, int64_t n_tiles,
                                                                     const uint32_t *__restrict__ table, SortTable has, const uint32_t *__restrict__ totals,
@@ -228,7 +236,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const uint32
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r) {
         const int64_t i = i0 + r * 64;
-        key[r] = i < n ? keys_in[i] : 0u;
+        key[r] = i < n ? sort_key<IDS>(keys_in, ids, i) : 0u;
         if (from_top) key[r] = from_top - key[r];
         val[r] = vals_in ? (i < n ? vals_in[i] : 0u) : uint32_t(i);
     }
@@ -339,6 +347,7 @@ __global__ void __launch_bounds__(256) sort_rows_kernel(uint32_t *__restrict__ t
 // Sorts n pairs by the low `bits` bits of the key.
 struct SortJob {
     const uint32_t *first_keys = nullptr;  // input of the first pass (read only)
+    gnn_sort_ids first_ids = {nullptr, 0, 0};  // or ids, which become keys
     const uint32_t *first_vals = nullptr;  // null: 0, 1, 2, ...
     uint32_t from_top = 0;                 // the first pass reads key k as from_top - k
     uint32_t *buf_k[2] = {nullptr, nullptr}, *buf_v[2] = {nullptr, nullptr};  // written alternately, [1] first; [0] may hold the input
@@ -358,7 +367,9 @@ int radix_sort(const SortJob &job, int64_t n, int bits, uint32_t *table, uint32_
         const bool last = shift + 8 >= bits;
         uint32_t *kout = last && job.last_keys ? job.last_keys : job.buf_k[cur ^ 1];
         uint32_t *vout = last && job.last_vals ? job.last_vals : job.buf_v[cur ^ 1];
-        sort_count_kernel<<<grid, kSortThreads, 0, stream>>>(kin, n, shift, from_top, n_tiles, table);
+        const bool from_ids = shift == 0 && job.first_ids.p;
+        if (from_ids) sort_count_kernel<true><<<grid, kSortThreads, 0, stream>>>(job.first_ids.p, job.first_ids, n, shift, from_top, n_tiles, table);
+        else sort_count_kernel<false><<<grid, kSortThreads, 0, stream>>>(kin, {}, n, shift, from_top, n_tiles, table);
         const SortTable has = n_tiles <= kNoScanTiles ? kCounts : n_tiles <= kRowScanTiles ? kPlacesOfDigit : kPlaces;
         if (has == kPlacesOfDigit) {
             sort_rows_kernel<<<256, 256, 0, stream>>>(table, n_tiles, sums);
@@ -366,10 +377,12 @@ int radix_sort(const SortJob &job, int64_t n, int bits, uint32_t *table, uint32_
             const int rc = scan_exclusive<uint32_t>(table, n_tiles * 256, 1, 0, false, sums, stream);
             if (rc != GNN_OK) return rc;
         }
-        if (last && job.inverse_last)
-            sort_scatter_kernel<true><<<grid, kSortThreads, 0, stream>>>(kin, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
+        if (from_ids)
+            sort_scatter_kernel<false, true><<<grid, kSortThreads, 0, stream>>>(job.first_ids.p, job.first_ids, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
+        else if (last && job.inverse_last)
+            sort_scatter_kernel<true, false><<<grid, kSortThreads, 0, stream>>>(kin, {}, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
         else
-            sort_scatter_kernel<false><<<grid, kSortThreads, 0, stream>>>(kin, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
+            sort_scatter_kernel<false, false><<<grid, kSortThreads, 0, stream>>>(kin, {}, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
         if (hipGetLastError() != hipSuccess) return GNN_ERR_LAUNCH;
         kin = kout;
         vin = vout;
@@ -453,10 +466,10 @@ int gnn_radix_sort_pairs(uint32_t *buf_k[2], uint32_t *buf_v[2], int64_t n, int 
     *out = (bits + 7) / 8 % 2;
     return radix_sort(job, n, bits, table, sums, stream, nullptr, nullptr);
 }
-int gnn_radix_sort_positions(uint32_t *buf_k[2], uint32_t *buf_v[2], int64_t n, int bits, uint32_t *table, uint32_t *sums,
+int gnn_radix_sort_positions(const gnn_sort_ids &ids, uint32_t *buf_k[2], uint32_t *buf_v[2], int64_t n, int bits, uint32_t *table, uint32_t *sums,
                              hipStream_t stream, uint32_t **keys, uint32_t **positions) {
     SortJob job;
-    job.first_keys = buf_k[0];
+    job.first_ids = ids;
     for (int i = 0; i < 2; ++i) { job.buf_k[i] = buf_k[i]; job.buf_v[i] = buf_v[i]; }
     return radix_sort(job, n, bits, table, sums, stream, keys, positions);
 }

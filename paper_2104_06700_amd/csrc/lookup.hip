@@ -144,13 +144,6 @@ struct Grad {
 };
 enum : uint32_t { kHead = 1, kThrough = 2, kTail = 4 };  // a run has: the end of a sum that began before, nothing but the middle of one, the beginning of one that goes on
 
-__global__ void __launch_bounds__(kThreads) key_kernel(const Ids ids, int64_t n, uint32_t *__restrict__ key) {
-    const int64_t i = block_number() * kThreads + threadIdx.x;
-    if (i >= n) return;
-    const int64_t v = ids.at(i);
-    key[i] = uint32_t(v < 0 ? ids.rows : v);
-}
-
 // Few positions: the place of each is the number of those that come before it.
 __global__ void __launch_bounds__(kThreads) rank_kernel(const Ids ids, int n, uint32_t *__restrict__ key, uint32_t *__restrict__ order) {
     __shared__ __attribute__((aligned(16))) uint32_t all[kRankHere];
@@ -761,10 +754,8 @@ extern "C" GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dta
             a.key = buf_k[0];
             a.order = buf_v[0];
         } else {
-            key_kernel<<<grid_of((n + kThreads - 1) / kThreads), kThreads, 0, stream>>>(named, n, buf_k[0]);
-            GNN_HIP_TRY(hipGetLastError());
             uint32_t *keys = nullptr, *order = nullptr;
-            const int sorted = gnn_radix_sort_positions(buf_k, buf_v, n, gnn_ilog2_ceil(V + 1), next, next + r.table, stream, &keys, &order);
+            const int sorted = gnn_radix_sort_positions({ids, o.ids_is_64, V}, buf_k, buf_v, n, gnn_ilog2_ceil(V + 1), next, next + r.table, stream, &keys, &order);
             if (sorted != GNN_OK) return sorted;
             a.key = keys;
             a.order = order;
