@@ -153,16 +153,22 @@ int scan_exclusive(T *data, int64_t n, int n_arrays, int64_t stride, bool want_t
 
 // ---------------------------------------------------------------- stable radix sort
 // LSD radix sort of (key, value) pairs of 32-bit words, 8 bits per pass, stable.  A workgroup of 8 wavefronts owns a tile
-// of 4096 consecutive pairs, a wavefront 512 of them.  Per pass: (1) every tile counts its digits, (2) the [digit][tile]
+// of 4096 consecutive pairs, a wavefront 512 of them (less where there would be few tiles).  Per pass: (1) every tile counts its digits, (2) the [digit][tile]
 // table is prefix-summed (digit-major, so equal digits of earlier tiles come first), (3) every tile orders its pairs by
 // digit in LDS and writes each digit's run in one piece.  Lanes with the same digit are found with eight ballots, so the
 // counters of a wavefront have one writer per digit and round.
 // Bound by the latency of the 8 dependent rounds of a wavefront, not by the 16 bytes per pair and pass: one wavefront per
 // tile took 64 rounds and wrote single pairs (3.1 M pairs, 16 bits: 2 x (36 + 15 + 58) us).
 constexpr int kSortWaves = 8;
-constexpr int kSortRounds = 8;
 constexpr int kSortThreads = 64 * kSortWaves;
-constexpr int kSortTile = kSortThreads * kSortRounds;
+constexpr int kSortRounds = 8, kLeastRounds = 2;  // of a wavefront: pairs of a tile / kSortThreads
+constexpr int64_t kNoScanTiles = 64;              // up to which every tile adds up the counts of all
+// Two or four rounds where that makes no more tiles than that (gradient of a table of 50 K positions of 300 K x 64 52 us, eight rounds 66)
+int sort_rounds(int64_t n) {
+    int rounds = kLeastRounds;
+    while (rounds < kSortRounds && n > kNoScanTiles * kSortThreads * rounds) rounds *= 2;
+    return rounds;
+}
 
 __device__ __forceinline__ unsigned long long same_digit_lanes(unsigned digit, bool valid) {
     unsigned long long peers = __ballot(valid);
@@ -183,22 +189,23 @@ template <bool IDS> __device__ __forceinline__ uint32_t sort_key(const void *__r
 }
 
 // from_top: the first pass of a descending order reads key k as from_top - k
-template <bool IDS>
+template <int ROUNDS, bool IDS>
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const void *__restrict__ keys, gnn_sort_ids ids, int64_t n, int shift,
                                                                   uint32_t from_top, int64_t n_tiles, uint32_t *__restrict__ table) {
+    constexpr int TILE = kSortThreads * ROUNDS;
     __shared__ uint32_t hist[kSortWaves][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int d = threadIdx.x; d < kSortWaves * 256; d += kSortThreads) (&hist[0][0])[d] = 0;
-    const int64_t i0 = int64_t(blockIdx.x) * kSortTile + wave * (64 * kSortRounds) + lane;
-    uint32_t key[kSortRounds];
+    const int64_t i0 = int64_t(blockIdx.x) * TILE + wave * (64 * ROUNDS) + lane;
+    uint32_t key[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         key[r] = i0 + r * 64 < n ? sort_key<IDS>(keys, ids, i0 + r * 64) : 0u;
         if (from_top) key[r] = from_top - key[r];
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const bool valid = i0 + r * 64 < n;
         const unsigned digit = (key[r] >> shift) & 255u;
         const unsigned long long peers = same_digit_lanes(digit, valid);
@@ -217,24 +224,25 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const void *__
 // What the table has of a tile's digit: its first place, its first place among pairs of the same digit (`totals` has how many there are), or the tile's count.
 enum SortTable { kPlaces, kPlacesOfDigit, kCounts };
 // vals_in null: the value of pair i is i.  inverse: vals_out[value] = place of the pair, and no keys are written
-template <bool INVERSE, bool IDS>
+template <int ROUNDS, bool INVERSE, bool IDS>
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const void *__restrict__ keys_in, gnn_sort_ids ids,
                                                                     const uint32_t *__restrict__ vals_in, int64_t n, int shift,
                                                                     uint32_t from_top, int64_t n_tiles,
                                                                     const uint32_t *__restrict__ table, SortTable has, const uint32_t *__restrict__ totals,
                                                                     uint32_t *__restrict__ keys_out, uint32_t *__restrict__ vals_out) {
+    constexpr int TILE = kSortThreads * ROUNDS;
     __shared__ uint32_t hist[kSortWaves][256];  // pairs per wavefront and digit, then those of the wavefronts before
     __shared__ uint32_t digit_begin[256];       // first place of a digit in the tile
     __shared__ uint32_t digit_out[256];         // its first place in the output, minus that
     __shared__ uint32_t wave_total[4], wave_all[4];
-    __shared__ uint32_t sorted_key[kSortTile], sorted_val[kSortTile];
+    __shared__ uint32_t sorted_key[TILE], sorted_val[TILE];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int d = threadIdx.x; d < kSortWaves * 256; d += kSortThreads) (&hist[0][0])[d] = 0;
-    const int64_t tile0 = int64_t(blockIdx.x) * kSortTile;
-    const int64_t i0 = tile0 + wave * (64 * kSortRounds) + lane;
-    uint32_t key[kSortRounds], val[kSortRounds], place[kSortRounds];
+    const int64_t tile0 = int64_t(blockIdx.x) * TILE;
+    const int64_t i0 = tile0 + wave * (64 * ROUNDS) + lane;
+    uint32_t key[ROUNDS], val[ROUNDS], place[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int64_t i = i0 + r * 64;
         key[r] = i < n ? sort_key<IDS>(keys_in, ids, i) : 0u;
         if (from_top) key[r] = from_top - key[r];
@@ -257,7 +265,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const void *
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const bool valid = i0 + r * 64 < n;
         const unsigned digit = (key[r] >> shift) & 255u;
         const unsigned long long peers = same_digit_lanes(digit, valid);
@@ -300,7 +308,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const void *
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         if (i0 + r * 64 >= n) continue;
         const unsigned digit = (key[r] >> shift) & 255u;
         const uint32_t at = digit_begin[digit] + hist[wave][digit] + place[r];
@@ -308,7 +316,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const void *
         sorted_val[at] = val[r];
     }
     __syncthreads();
-    const int count = n - tile0 < kSortTile ? int(n - tile0) : kSortTile;
+    const int count = n - tile0 < TILE ? int(n - tile0) : TILE;
     for (int j = threadIdx.x; j < count; j += kSortThreads) {
         const uint32_t k = sorted_key[j], v = sorted_val[j];
         const uint32_t out = digit_out[(k >> shift) & 255u] + uint32_t(j);
@@ -322,8 +330,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const void *
 }
 
 // Few tiles: a workgroup scans the row of a digit and leaves its total behind, and the tiles add up the totals of the digits before.  One launch a pass instead of two.
-// Very few: every tile adds up the counts by itself, no launch (gradient of a table of 50 K positions of 300 K x 64 66 us, scanned 73).
-constexpr int64_t kRowScanTiles = 4096, kNoScanTiles = 64;
+// Very few: every tile adds up the counts by itself, no launch (gradient of a table of 50 K positions of 300 K x 64, then in tiles of eight rounds, 66 us, scanned 73).
+constexpr int64_t kRowScanTiles = 4096;
 __global__ void __launch_bounds__(256) sort_rows_kernel(uint32_t *__restrict__ table, int64_t n_tiles, uint32_t *__restrict__ totals) {
     __shared__ uint32_t wave_total[4];
     uint32_t *row = table + int64_t(blockIdx.x) * n_tiles;
@@ -355,9 +363,10 @@ struct SortJob {
     bool inverse_last = false;             // the last pass writes last_vals[value] = place, and no keys
 };
 
-int radix_sort(const SortJob &job, int64_t n, int bits, uint32_t *table, uint32_t *sums, hipStream_t stream, uint32_t **keys_out,
-               uint32_t **vals_out) {
-    const int64_t n_tiles = (n + kSortTile - 1) / kSortTile;
+template <int ROUNDS>
+int radix_sort_by(const SortJob &job, int64_t n, int bits, uint32_t *table, uint32_t *sums, hipStream_t stream, uint32_t **keys_out,
+                  uint32_t **vals_out) {
+    const int64_t n_tiles = (n + kSortThreads * ROUNDS - 1) / (kSortThreads * ROUNDS);
     if (n_tiles > INT32_MAX) return GNN_ERR_UNSUPPORTED;
     const unsigned grid = static_cast<unsigned>(n_tiles);
     const uint32_t *kin = job.first_keys, *vin = job.first_vals;
@@ -368,8 +377,8 @@ int radix_sort(const SortJob &job, int64_t n, int bits, uint32_t *table, uint32_
         uint32_t *kout = last && job.last_keys ? job.last_keys : job.buf_k[cur ^ 1];
         uint32_t *vout = last && job.last_vals ? job.last_vals : job.buf_v[cur ^ 1];
         const bool from_ids = shift == 0 && job.first_ids.p;
-        if (from_ids) sort_count_kernel<true><<<grid, kSortThreads, 0, stream>>>(job.first_ids.p, job.first_ids, n, shift, from_top, n_tiles, table);
-        else sort_count_kernel<false><<<grid, kSortThreads, 0, stream>>>(kin, {}, n, shift, from_top, n_tiles, table);
+        if (from_ids) sort_count_kernel<ROUNDS, true><<<grid, kSortThreads, 0, stream>>>(job.first_ids.p, job.first_ids, n, shift, from_top, n_tiles, table);
+        else sort_count_kernel<ROUNDS, false><<<grid, kSortThreads, 0, stream>>>(kin, {}, n, shift, from_top, n_tiles, table);
         const SortTable has = n_tiles <= kNoScanTiles ? kCounts : n_tiles <= kRowScanTiles ? kPlacesOfDigit : kPlaces;
         if (has == kPlacesOfDigit) {
             sort_rows_kernel<<<256, 256, 0, stream>>>(table, n_tiles, sums);
@@ -378,11 +387,11 @@ int radix_sort(const SortJob &job, int64_t n, int bits, uint32_t *table, uint32_
             if (rc != GNN_OK) return rc;
         }
         if (from_ids)
-            sort_scatter_kernel<false, true><<<grid, kSortThreads, 0, stream>>>(job.first_ids.p, job.first_ids, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
+            sort_scatter_kernel<ROUNDS, false, true><<<grid, kSortThreads, 0, stream>>>(job.first_ids.p, job.first_ids, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
         else if (last && job.inverse_last)
-            sort_scatter_kernel<true, false><<<grid, kSortThreads, 0, stream>>>(kin, {}, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
+            sort_scatter_kernel<ROUNDS, true, false><<<grid, kSortThreads, 0, stream>>>(kin, {}, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
         else
-            sort_scatter_kernel<false, false><<<grid, kSortThreads, 0, stream>>>(kin, {}, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
+            sort_scatter_kernel<ROUNDS, false, false><<<grid, kSortThreads, 0, stream>>>(kin, {}, vin, n, shift, from_top, n_tiles, table, has, sums, kout, vout);
         if (hipGetLastError() != hipSuccess) return GNN_ERR_LAUNCH;
         kin = kout;
         vin = vout;
@@ -392,6 +401,14 @@ int radix_sort(const SortJob &job, int64_t n, int bits, uint32_t *table, uint32_
     if (keys_out) *keys_out = const_cast<uint32_t *>(kin);
     if (vals_out) *vals_out = const_cast<uint32_t *>(vin);
     return GNN_OK;
+}
+
+int radix_sort(const SortJob &job, int64_t n, int bits, uint32_t *table, uint32_t *sums, hipStream_t stream, uint32_t **keys_out,
+               uint32_t **vals_out) {
+    const int rounds = sort_rounds(n);
+    if (rounds == 2) return radix_sort_by<2>(job, n, bits, table, sums, stream, keys_out, vals_out);
+    if (rounds == 4) return radix_sort_by<4>(job, n, bits, table, sums, stream, keys_out, vals_out);
+    return radix_sort_by<8>(job, n, bits, table, sums, stream, keys_out, vals_out);
 }
 
 int grid_for(int64_t n, int block, int64_t cap = (int64_t(1) << 16)) {
@@ -473,7 +490,11 @@ int gnn_radix_sort_positions(const gnn_sort_ids &ids, uint32_t *buf_k[2], uint32
     for (int i = 0; i < 2; ++i) { job.buf_k[i] = buf_k[i]; job.buf_v[i] = buf_v[i]; }
     return radix_sort(job, n, bits, table, sums, stream, keys, positions);
 }
-int64_t gnn_sort_table_elems(int64_t n) { return (n + kSortTile - 1) / kSortTile * 256; }
+int64_t gnn_sort_table_elems(int64_t n) {  // (enough for less than n as well, whose tiles may be smaller and more)
+    const int64_t least = kSortThreads * kLeastRounds, most = kSortThreads * kSortRounds;
+    const int64_t small = (n + least - 1) / least, large = (n + most - 1) / most;
+    return (large > kNoScanTiles ? large : small < kNoScanTiles ? small : kNoScanTiles) * 256;
+}
 int64_t gnn_sort_sums_elems(int64_t n) {  // (256: the totals of the digits)
     const int64_t sums = gnn_scan_sums_elems(gnn_sort_table_elems(n));
     return sums > 256 ? sums : 256;

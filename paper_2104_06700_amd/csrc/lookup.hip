@@ -24,7 +24,7 @@ constexpr int kAtOnce = 4;        // vectors of a thread on their way, forward
 // their way at once.
 constexpr int kRun = 32, kBatch = 8;
 constexpr int64_t kLong = 1 << 17; // positions from which on runs are long
-constexpr int64_t kRankHere = 8192; // positions up to which every workgroup finds the places of its ones among all (4,096 x 64 of 8,192: sorting 42 us, so 29)
+constexpr int64_t kRankHere = 6144; // positions up to which every workgroup finds the places of its ones among all (4,096 x 64 of 4,000: sorting 23 us, so 18; of 8,192: 24 and 29; of 300 K rows 43 and 41)
 constexpr int kRankRows = 8;      // of a workgroup then (of 4,000: 32 rows 30 us, 8 rows 18)
 constexpr int kFew = 2048;        // positions up to which there is one launch, if ids do not come more often than eight times on average
 constexpr int kFewRows = 16;      // of a workgroup then
