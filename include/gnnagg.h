@@ -525,6 +525,7 @@ GNN_API int gnn_lookup_fwd(const void *table, const void *ids, void *Y, int64_t 
  * joined in fp64; a bf16 dtable is rounded once, with accumulate once a call.  dY and dtable do not overlap.  n == 0 sets dtable to 0 without
  * accumulate. */
 GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dtable, int64_t V, int64_t n, int64_t F, const gnn_lookup_opts *opts);
+/* Does not fall as V, n or F grow: scratch for the largest call is enough for every smaller one.  (A call of at most 2,048 positions demands it too.) */
 GNN_API int64_t gnn_lookup_workspace_bytes(int64_t V, int64_t n, int64_t F);
 
 /* Rows kept in 8 bits: features of a graph, or hidden rows that later batches read, a quarter of their size in fp32.  A row of F columns

@@ -725,6 +725,7 @@ def gnn_adamw_step(tensors: AdamWTensors, step, lr, beta1=0.9, beta2=0.999, eps=
 
 
 def gnn_lookup_workspace_bytes(V, n, F) -> int:
+    """Bytes for the gradient of a table; does not fall as V, n or F grow, so that scratch for the largest call does for all."""
     return int(load_library().gnn_lookup_workspace_bytes(int(V), int(n), int(F)))
 
 

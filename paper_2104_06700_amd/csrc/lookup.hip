@@ -697,8 +697,17 @@ extern "C" GNN_API int gnn_lookup_fwd(const void *table, const void *ids, void *
 
 extern "C" GNN_API int64_t gnn_lookup_workspace_bytes(int64_t V, int64_t n, int64_t F) {
     if (V <= 0 || n <= 0 || F <= 0 || V > kMostRows || n > kMostRows || F > kMostColumns) return 0;
-    const Room a = room_of(V, n, F, false), b = room_of(V, n, F, true);
-    return 4 * (a.words > b.words ? a.words : b.words);
+    // Enough for every smaller call as well: a call's room falls only where its runs become long, at kLong positions, and where its vectors become wide, at 4 and 8 columns.
+    int64_t words = 0;
+    for (const bool eight : {false, true})
+        for (const int64_t positions : {n, n < kLong ? n : kLong - 1}) {
+            const int64_t wide = eight ? 8 : 4;
+            for (const int64_t columns : {F, F < wide ? F : wide - 1}) {
+                const int64_t w = room_of(V, positions, columns, eight).words;
+                words = w > words ? w : words;
+            }
+        }
+    return 4 * words;
 }
 
 extern "C" GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dtable, int64_t V, int64_t n, int64_t F, const gnn_lookup_opts *opts) {
