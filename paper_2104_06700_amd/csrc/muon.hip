@@ -681,12 +681,13 @@ template <int P, typename T> int launch_job(const Job &j, int kind, const int64_
     return GNN_OK;
 }
 
-// Whether X, A and Q stay within what two fp16 numbers hold with the powers of two of Parts<2>, and directions of small singular values do not shrink below it.
+// Whether X, A and Q stay within what two fp16 numbers hold with the powers of two of Parts<2>, and directions of small singular values do not shrink below it; a
+// matrix far below eps, which a step multiplies by a, keeps its power of two only where nothing grows faster.
 // Singular values of X begin within 0 .. 1, and the step takes s to s q(s^2), q(t) = a + b t + c t^2: both have their extremes at the ends or where their
 // derivative is 0.
 bool two_parts_do(double a, double b, double c, int steps, float &growth) {
     if (!(fabs(a) >= 1.0)) return false;
-    double most = 1.0 + 1e-6, grows = 1.0;
+    double most = 1.0 + 1e-6;
     for (int k = 0; k < steps; ++k) {
         const double top = most * most;
         auto q = [&](double t) { return fabs(a + t * (b + t * c)); };
@@ -704,10 +705,9 @@ bool two_parts_do(double a, double b, double c, int steps, float &growth) {
             if (u > 0.0 && u < top) next = fmax(next, sqrt(u) * q(u));
         }
         most = next * (1.0 + 1e-4);  // (roundings of the products)
-        if (!(most <= 1.9) || !(q_most <= 7.5)) return false;
-        grows = fmax(grows, q_most);
+        if (!(most <= 1.9) || !(q_most <= 7.5) || q_most > fabs(a)) return false;
     }
-    growth = float(log2(grows) + 1e-4);
+    growth = float(log2(fabs(a)) + 1e-4);
     return true;
 }
 

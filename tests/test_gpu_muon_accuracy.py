@@ -1,0 +1,25 @@
+"""Newton-Schulz products of matrices that are far smaller than eps or have rows or columns far smaller than the rest, against the formulas in 64 bits."""
+import pytest
+import torch
+
+from test_gpu_muon import newton_schulz, orthogonalize
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def normal(rows, cols, seed):
+    return torch.randn(rows, cols, generator=torch.Generator().manual_seed(seed))
+
+
+@pytest.mark.parametrize("rows,cols,size,steps", [(40, 90, 1e-12, 100), (300, 200, 1e-19, 60), (1100, 1000, 1e-19, 100), (40, 90, 1e-19, 100)])
+def test_polynomials_that_are_largest_between_the_ends(rows, cols, size, steps):
+    """x + 0.9 x^3 - 0.9 x^5 multiplies a small matrix by 1 a step, and singular values near 0.7 by 1.2."""
+    u, eps = normal(rows, cols, 1), 1e-7
+    u = (u * (size / u.norm())).to(DEV)
+    coefficients = (1.0, 0.9, -0.9)
+    o = orthogonalize([u], steps=steps, eps=eps, coefficients=coefficients)[0]
+    want = newton_schulz(u, steps=steps, eps=eps, coefficients=coefficients)
+    # X is 1e-5 at most, so X X^T does not matter beside 1 and a step only rounds X: as an operand (2^-23) and as a result (2^-24)
+    assert float(want.norm()) < 1.1e-5
+    assert float((o.double() - want).norm()) <= (steps + 1) * 2.0 ** -22 * float(want.norm())
