@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const Job j) {
 template <int P> struct Parts;
 template <> struct Parts<2> {
     typedef f16x8 Eight;
-    static constexpr float kX = 32768.0f, kA = 16384.0f, kQ = 8192.0f;
+    static constexpr int kXLog2 = 15, kALog2 = 14, kQLog2 = 13;
     static __device__ __forceinline__ float part(float x) { return float(_Float16(x)); }
     static __device__ __forceinline__ uint32_t pair(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(gnn_f32x2{x, y}, f16x2)); }
     static __device__ __forceinline__ float get(uint32_t w, int i) { return float(__builtin_bit_cast(f16x2, w)[i]); }
@@ -156,7 +156,7 @@ template <> struct Parts<2> {
 };
 template <> struct Parts<3> {
     typedef bf16x8 Eight;
-    static constexpr float kX = 1.0f, kA = 1.0f, kQ = 1.0f;
+    static constexpr int kXLog2 = 0, kALog2 = 0, kQLog2 = 0;
     static __device__ __forceinline__ float part(float x) { return float(__bf16(x)); }
     static __device__ __forceinline__ uint32_t pair(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(gnn_f32x2{x, y}, gnn_bf16x2)); }
     static __device__ __forceinline__ float get(uint32_t w, int i) { return __uint_as_float(i ? w & 0xFFFF0000u : w << 16); }
@@ -164,20 +164,21 @@ template <> struct Parts<3> {
 };
 // P = 2: a matrix whose norm is far below eps has an X as small, and gets another power of two: as many more as keep it below 1 in this step.  (A matters
 // beside 1 and stays as it is.)
+constexpr float kMostExponent = 1000.0f;  // (an X below 2^-1000 vanishes in fp32, whatever the steps)
 template <int P> __device__ __forceinline__ int exponent(const Job &j, float log_norm, int step) {
     if constexpr (P == 3) return 0;
     const float e = -fmaf(float(step), j.growth, log_norm);
-    return e > 0.0f ? int(fminf(e, 90.0f)) : 0;
+    return e > 0.0f ? int(fminf(e, kMostExponent)) : 0;
 }
-// What a sum of a phase is times, to be the number that the planes hold, or the result.
-template <int P, Phase phase> __device__ __forceinline__ float factor(const Job &j, const Mat &t, int step) {
+// What a sum of a phase is times 2 to, to be the number that the planes hold, or the result.
+template <int P, Phase phase> __device__ __forceinline__ int shift(const Job &j, const Mat &t, int step) {
     typedef Parts<P> S;
-    if (P == 3 || phase == kPolynomial) return 1.0f;
+    if (P == 3 || phase == kPolynomial) return 0;
     const float log_norm = float(t.squares[t.norm_blocks]);
     const int now = exponent<P>(j, log_norm, step);
-    if constexpr (phase == kGram) return __builtin_amdgcn_ldexpf(S::kA / (S::kX * S::kX), -2 * now);
-    else if constexpr (phase == kUpdate) return __builtin_amdgcn_ldexpf(1.0f / S::kQ, exponent<P>(j, log_norm, step + 1) - now);
-    else return __builtin_amdgcn_ldexpf(1.0f / (S::kQ * S::kX), -now);
+    if constexpr (phase == kGram) return S::kALog2 - 2 * (S::kXLog2 + now);
+    else if constexpr (phase == kUpdate) return exponent<P>(j, log_norm, step + 1) - now - S::kQLog2;
+    else return -(S::kQLog2 + S::kXLog2 + now);
 }
 
 // x = the sum of P parts, exactly where P = 3
@@ -262,10 +263,11 @@ template <int P, typename T> __global__ void __launch_bounds__(kThreads) planes_
     __syncthreads();
     const double norm = sqrt((sums[0] + sums[1]) + (sums[2] + sums[3]));
     const bool fits = norm <= 1.7e308;
-    const float log_norm = fits ? log2f(float(norm / (norm + j.eps))) : 0.0f;
+    const double size = fits ? norm / (norm + j.eps) : 1.0;  // of X, which may be below what fp32 holds
+    const float log_norm = log2f(float(__builtin_amdgcn_frexp_mant(size))) + float(__builtin_amdgcn_frexp_exp(size));
     if (tile == 0 && threadIdx.x == 0) t.squares[t.norm_blocks] = double(log_norm);
     // what is not finite reaches all of the matrix; of zeros nothing is divided by an eps whose reciprocal may not be finite
-    const double inverse = !fits ? __builtin_nan("") : norm > 0.0 ? ldexp(double(Parts<P>::kX), exponent<P>(j, log_norm, 0)) / (norm + j.eps) : 0.0;
+    const double inverse = !fits ? __builtin_nan("") : norm > 0.0 ? ldexp(1.0, Parts<P>::kXLog2 + exponent<P>(j, log_norm, 0)) / (norm + j.eps) : 0.0;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
         const int row = r0 + wave + 4 * k;
@@ -350,11 +352,11 @@ template <int TI, int TJ> __device__ __forceinline__ void add(float16v (&to)[TI]
 }
 
 // What a phase makes of four sums, rows row_i .. row_i + 3 of column row_c, or the same columns of that row: A is symmetric.
-template <int P, Phase phase> __device__ __forceinline__ void finish(const Job &j, const Mat &t, float times, int row_i, int row_c, float (&v)[4]) {
+template <int P, Phase phase> __device__ __forceinline__ void finish(const Job &j, const Mat &t, int times_log2, int row_i, int row_c, float (&v)[4]) {
     if constexpr (phase != kPolynomial) {
         if constexpr (P == 2)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] *= times;
+            for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_ldexpf(v[i], times_log2);
         return;
     }
     float a[4];
@@ -403,7 +405,7 @@ __device__ __forceinline__ void within_wavefront() { __builtin_amdgcn_fence(__AT
 
 // A fragment of results on its way out: rows row0 .. row0 + 31, columns col0 .. col0 + 31, to both places where `both`.  The loop is not unrolled: code that
 // a wavefront goes through once is as slow as it is fetched.
-template <int P, Phase phase, typename T> __device__ __forceinline__ void write_fragment(const Job &j, const Mat &t, float times, int step, int row0, int col0, const float (&turn)[32][33], bool both) {
+template <int P, Phase phase, typename T> __device__ __forceinline__ void write_fragment(const Job &j, const Mat &t, int times_log2, int step, int row0, int col0, const float (&turn)[32][33], bool both) {
     const int lane = int(threadIdx.x) & 63, l32 = lane & 31, lk = lane >> 5;
 #pragma unroll 1
     for (int g = 0; g < 4; ++g) {
@@ -411,12 +413,12 @@ template <int P, Phase phase, typename T> __device__ __forceinline__ void write_
         float v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = turn[at + i][l32];
-        finish<P, phase>(j, t, times, row0 + at, col0 + l32, v);
+        finish<P, phase>(j, t, times_log2, row0 + at, col0 + l32, v);
         write_down<P, phase, T>(j, t, step, row0 + at, col0 + l32, v);
         if (!both) continue;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = turn[l32][at + i];
-        finish<P, phase>(j, t, times, col0 + at, row0 + l32, v);
+        finish<P, phase>(j, t, times_log2, col0 + at, row0 + l32, v);
         write_across<P, phase, T>(j, t, row0 + l32, col0 + at, v);
     }
 }
@@ -430,7 +432,7 @@ template <int P, Phase phase, typename OUT, int T> __global__ void __launch_boun
     int number, ti, tj;
     const Mat &t = j.mat[matrix_of_block<symmetric ? kSymmetric : kOthers>(j, number)];
     const Operands o = operands<phase>(t, step);
-    const float times = factor<P, phase>(j, t, step);
+    const int times_log2 = shift<P, phase>(j, t, step);
     const int side = o.rows / (32 * T), across = o.cols / (32 * T);
     tile_of<symmetric, 1>(number, symmetric ? side * (side + 1) / 2 : side * across, across, ti, tj);
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
@@ -476,12 +478,12 @@ template <int P, Phase phase, typename OUT, int T> __global__ void __launch_boun
         float v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = (tile[0][at + i][l32] + tile[1][at + i][l32]) + (tile[2][at + i][l32] + tile[3][at + i][l32]);
-        finish<P, phase>(j, t, times, row0 + at, col0 + l32, v);
+        finish<P, phase>(j, t, times_log2, row0 + at, col0 + l32, v);
         write_down<P, phase, OUT>(j, t, step, row0 + at, col0 + l32, v);
         if (symmetric && ti == tj) return;  // (a tile on the diagonal is computed whole)
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = (tile[0][l32][at + i] + tile[1][l32][at + i]) + (tile[2][l32][at + i] + tile[3][l32][at + i]);
-        finish<P, phase>(j, t, times, col0 + at, row0 + l32, v);
+        finish<P, phase>(j, t, times_log2, col0 + at, row0 + l32, v);
         write_across<P, phase, OUT>(j, t, row0 + l32, col0 + at, v);
     } else {
         // a wavefront adds up and writes one fragment of the tile
@@ -505,7 +507,7 @@ template <int P, Phase phase, typename OUT, int T> __global__ void __launch_boun
 #pragma unroll
         for (int v = 0; v < 16; ++v) lds.turn[wave][8 * (v / 4) + 4 * lk + v % 4][l32] = sum[v];
         within_wavefront();
-        write_fragment<P, phase, OUT>(j, t, times, step, (ti * 2 + (wave >> 1)) * 32, (tj * 2 + (wave & 1)) * 32, lds.turn[wave], !(symmetric && ti == tj));
+        write_fragment<P, phase, OUT>(j, t, times_log2, step, (ti * 2 + (wave >> 1)) * 32, (tj * 2 + (wave & 1)) * 32, lds.turn[wave], !(symmetric && ti == tj));
     }
 }
 
@@ -523,7 +525,7 @@ template <int P, int TI, int TJ, int KS, Phase phase, typename T> __global__ voi
     int number, ti, tj;
     const Mat &t = j.mat[matrix_of_block<symmetric ? kSymmetric : kOthers>(j, number)];
     const Operands o = operands<phase>(t, step);
-    const float times = factor<P, phase>(j, t, step);
+    const int times_log2 = shift<P, phase>(j, t, step);
     const int down = o.rows / (64 * TI), across = o.cols / (64 * TJ);
     tile_of<symmetric, TJ / TI>(number, symmetric ? TJ / TI * (across * (across + 1) / 2) : down * across, across, ti, tj);
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
@@ -610,7 +612,7 @@ template <int P, int TI, int TJ, int KS, Phase phase, typename T> __global__ voi
         within_wavefront();
         const int row0 = ti * 64 * TI + (wi * TI + q / TJ) * 32, col0 = tj * 64 * TJ + (wj * TJ + q % TJ) * 32;
         // squares of as many rows as a tile is wide are computed whole on the diagonal
-        write_fragment<P, phase, T>(j, t, times, step, row0, col0, lds.turn[wave], !(symmetric && row0 / (64 * TJ) == tj));
+        write_fragment<P, phase, T>(j, t, times_log2, step, row0, col0, lds.turn[wave], !(symmetric && row0 / (64 * TJ) == tj));
         within_wavefront();
     }
 }
@@ -714,7 +716,7 @@ bool two_parts_do(double a, double b, double c, int steps, float &growth) {
 // Matrices of the same kind and type, kMats at a time.
 int orthogonalize(Entry (*at)(const void *, int64_t), const void *list, int64_t count, Job &j, double a, double b, double c, int steps, uint8_t *room, hipStream_t stream) {
     const int parts = two_parts_do(a, b, c, steps, j.growth) ? 2 : 3;
-    const double unit_a = parts == 2 ? Parts<2>::kA : 1.0, unit_q = parts == 2 ? Parts<2>::kQ : 1.0;
+    const double unit_a = parts == 2 ? ldexp(1.0, Parts<2>::kALog2) : 1.0, unit_q = parts == 2 ? ldexp(1.0, Parts<2>::kQLog2) : 1.0;
     j.a = float(a * unit_q);
     j.b = float(b * (unit_q / unit_a));
     j.c = float(c * (unit_q / (unit_a * unit_a)));

@@ -23,3 +23,19 @@ def test_polynomials_that_are_largest_between_the_ends(rows, cols, size, steps):
     # X is 1e-5 at most, so X X^T does not matter beside 1 and a step only rounds X: as an operand (2^-23) and as a result (2^-24)
     assert float(want.norm()) < 1.1e-5
     assert float((o.double() - want).norm()) <= (steps + 1) * 2.0 ** -22 * float(want.norm())
+
+
+@pytest.mark.parametrize("steps", [1, 9, 90])
+@pytest.mark.parametrize("rows,cols", [(40, 90), (200, 60), (1100, 1000)])
+def test_matrices_near_the_least_numbers(rows, cols, steps):
+    """X begins some 2^-115 of 1 and grows by 3.4445 a step, up to the usual singular values in the last case."""
+    u, eps = (normal(rows, cols, 2) * 2.0 ** -122).to(DEV), 1.0
+    o = orthogonalize([u], steps=steps, eps=eps)[0]
+    want = newton_schulz(u, steps=steps, eps=eps)
+    if steps < 90:  # X X^T does not matter beside 1: as above
+        assert float((o.double() - want).norm()) <= (steps + 1) * 2.0 ** -22 * float(want.norm())
+    else:
+        # the steps before leave X off by (steps + 1) 2^-22 of itself, and what is off grows with the small singular values, by 485 in the last five steps of which the
+        # matrix' norm, 1, is the start; their own roundings as for any matrix: four times 485 2^-24 of the norm
+        assert float(want.norm()) > 1.0
+        assert float((o.double() - want).norm()) <= 485 * ((steps + 1) * 2.0 ** -22 + 4 * 2.0 ** -24 * float(want.norm()))
