@@ -562,9 +562,10 @@ GNN_API int64_t gnn_store_rows_workspace_bytes(int64_t V, int64_t n);  /* 0 wher
  * (|U| + eps), |U| the root of the sum of squares, transposed where rows > cols, `steps` times
  *     A = X X^T,   B = b A + c A A,   X = a X + B X
  * and O = X (transposed back).  (a, b, c) = (3.4445, -4.7750, 2.0315) takes singular values of X from some 0.002 on to 0.7 .. 1.2 in five steps.
- * Operands between the products are held in two fp16 numbers (23 significant bits), or, with coefficients that let singular values leave
- * 0 .. 1.9 or those of B + a exceed 7.5 or |a|, or |a| < 1, in three bf16 numbers (24 bits, at about 1.6 times the time); sums are fp32: as close as fp32
- * products.  O is rounded once.  A zero matrix gives 0; a value that is not finite makes all of its matrix' results NaN, and no other's. */
+ * Operands between the products are held in two fp16 numbers (23 significant bits, but no steps below 2^-49 of the largest: rows and columns down to some 10^-7 of
+ * the others are as close as the others), or, with coefficients that let singular values leave 0 .. 1.9 or those of B + a exceed 7.5 or |a|, or
+ * |a| < 1, in three bf16 numbers (24 bits and the range of fp32, at about 1.5 times the time); sums are fp32: as close as fp32 products.  O is
+ * rounded once.  A zero matrix gives 0; a value that is not finite makes all of its matrix' results NaN, and no other's. */
 typedef struct gnn_orthogonalize_matrix {
     const void *in;        /* U [rows, cols] of dtype, row stride ld_in */
     void *out;             /* O [rows, cols] of dtype, row stride ld_out; may be `in`, with the same stride */

@@ -12,13 +12,16 @@
 // has four neighbouring results of a column in a lane, writes 8 bytes a plane.  Rows and columns are filled up with zeros to whole tiles, which the
 // products keep zero.
 //
-// P = 2: fp16 numbers.  The rest behind the first is at most 2^-11 of it (in halves of its steps), of which the second keeps 11 bits: 23 of the 24 bits of fp32,
-// with X, A and Q multiplied by powers of two that take the largest number they can reach near the largest of fp16, so that the smallest are off by
-// 2^-40.  It holds where the coefficients keep the singular values small, as the usual ones do (at most 1.2); else P = 3: bf16 numbers, which have the range
-// and all 24 bits of fp32, at twice the products (2560 x 4000 fp32 2990 us instead of 1890).
-// Of the products of parts those that matter are formed (P = 2: three of four, the last is below 2^-23 of the first; P = 3: six of nine, 2^-26), summed
-// from zero over 32 k (P = 3 through LDS: 16), smallest first, and added to the result with one rounding: the matrix cores cut off what lies below a sum's last
-// bit, so that long chains through them would be the worse sums.  Over 64 k: as fast; over 16, where there are twice the additions: 2030 us.
+// P = 2: fp16 numbers.  The rest behind the first is at most 2^-11 of it, of which the second keeps 11 bits and a sign: 23 of the 24 bits of fp32,
+// with X, A and Q multiplied by powers of two that take the largest number they can reach near the largest of fp16.  The second number is held 2^11 times as large as
+// it is, so that it loses bits only where the first one does: steps end at 2^-49 of the largest number, and rows or columns down to some 10^-7 of the others are as
+// close as in fp32 (100 x 256, ten rows 10^-5 of the others, by themselves: 2 10^-7; with second numbers as they are, which end at 2^-38, 9 10^-6, and 10^-3 at 10^-7).  So
+// products with a second number have sums of their own: 2560 x 4000 fp32 1972 us instead of 1888.  Two numbers do where the coefficients keep the
+// singular values small, as the usual ones do (at most 1.2); else P = 3: bf16 numbers, which have the range and all 24 bits of fp32, at twice the products (2990 us).
+// Of the products of parts those that matter are formed (P = 2: three of four, the last is at most 2^-22 of the first, 2^-25 on average; P = 3: six of nine, 2^-23 and 2^-26),
+// summed from zero over 32 k (P = 3 through LDS: 16), smallest first, and added to the result with one rounding: the matrix cores cut off what lies below a sum's
+// last bit, so that long chains through them would be the worse sums (not of second numbers, which are 2^-11 of the others).  Over 64 k: as fast; over 16, where
+// there are twice the additions: 2030 us instead of 1890.
 //
 // Small matrices: a workgroup has a tile of 32 x 32 and its four wavefronts a quarter of k each, straight from the caches; such a product is one latency.
 // Large ones: tiles of 64 x 64 or 128 x 128 through LDS.  All matrices of a call of the same kind share the launches.
@@ -149,6 +152,7 @@ template <int P> struct Parts;
 template <> struct Parts<2> {
     typedef f16x8 Eight;
     static constexpr int kXLog2 = 15, kALog2 = 14, kQLog2 = 13;
+    static constexpr float kRest = 2048.0f;  // what the second number holds the rest times
     static __device__ __forceinline__ float part(float x) { return float(_Float16(x)); }
     static __device__ __forceinline__ uint32_t pair(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(gnn_f32x2{x, y}, f16x2)); }
     static __device__ __forceinline__ float get(uint32_t w, int i) { return float(__builtin_bit_cast(f16x2, w)[i]); }
@@ -157,6 +161,7 @@ template <> struct Parts<2> {
 template <> struct Parts<3> {
     typedef bf16x8 Eight;
     static constexpr int kXLog2 = 0, kALog2 = 0, kQLog2 = 0;
+    static constexpr float kRest = 1.0f;
     static __device__ __forceinline__ float part(float x) { return float(__bf16(x)); }
     static __device__ __forceinline__ uint32_t pair(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(gnn_f32x2{x, y}, gnn_bf16x2)); }
     static __device__ __forceinline__ float get(uint32_t w, int i) { return __uint_as_float(i ? w & 0xFFFF0000u : w << 16); }
@@ -186,7 +191,7 @@ template <int P> __device__ __forceinline__ void split(float x, float (&part)[P]
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         part[p] = Parts<P>::part(x);
-        x -= part[p];
+        x = (x - part[p]) * Parts<P>::kRest;
     }
 }
 
@@ -226,7 +231,7 @@ template <int P> __device__ __forceinline__ void get4(const uint16_t *planes, in
     for (int q = P - 1; q >= 0; --q) {  // smallest first: the sum is exact
         const u32x2 w = *reinterpret_cast<const u32x2 *>(p + int64_t(q) * rows * depth);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += Parts<P>::get(i < 2 ? w.x : w.y, i & 1);
+        for (int i = 0; i < 4; ++i) v[i] = fmaf(v[i], 1.0f / Parts<P>::kRest, Parts<P>::get(i < 2 ? w.x : w.y, i & 1));
     }
 }
 
@@ -325,13 +330,23 @@ template <bool SYMMETRIC, int WIDE> __device__ __forceinline__ void tile_of(int 
 }
 
 // The products of parts that matter, smallest first, onto the sums of N fragments of the right operand, in turn, so that no product waits for the one before.
-template <int P, int N> __device__ __forceinline__ void add_products(float16v (&sum)[N], const typename Parts<P>::Eight (&a)[P], const typename Parts<P>::Eight (&b)[N][P]) {
+// P = 2: those with a second number onto `low`, which is kRest times as large and goes on over all of k.
+template <int P, int N> __device__ __forceinline__ void add_products(float16v (&sum)[N], float16v (&low)[P == 2 ? N : 1], const typename Parts<P>::Eight (&a)[P], const typename Parts<P>::Eight (&b)[N][P]) {
+    if constexpr (P == 2) {
 #pragma unroll
-    for (int s = P - 1; s >= 0; --s)
+        for (int y = 0; y < N; ++y) low[y] = Parts<P>::product(a[0], b[y][1], low[y]);
 #pragma unroll
-        for (int p = 0; p <= s; ++p)
+        for (int y = 0; y < N; ++y) sum[y] = Parts<P>::product(a[0], b[y][0], sum[y]);
 #pragma unroll
-            for (int y = 0; y < N; ++y) sum[y] = Parts<P>::product(a[p], b[y][s - p], sum[y]);
+        for (int y = 0; y < N; ++y) low[y] = Parts<P>::product(a[1], b[y][0], low[y]);
+    } else {
+#pragma unroll
+        for (int s = P - 1; s >= 0; --s)
+#pragma unroll
+            for (int p = 0; p <= s; ++p)
+#pragma unroll
+                for (int y = 0; y < N; ++y) sum[y] = Parts<P>::product(a[p], b[y][s - p], sum[y]);
+    }
 }
 template <int TI, int TJ> __device__ __forceinline__ void clear(float16v (&sum)[TI][TJ]) {
 #pragma unroll
@@ -342,13 +357,13 @@ template <int TI, int TJ> __device__ __forceinline__ void clear(float16v (&sum)[
             for (int v = 0; v < 16; ++v) sum[x][y][v] = 0.0f;
 }
 // with one rounding
-template <int TI, int TJ> __device__ __forceinline__ void add(float16v (&to)[TI][TJ], const float16v (&sum)[TI][TJ]) {
+template <int TI, int TJ> __device__ __forceinline__ void add(float16v (&to)[TI][TJ], const float16v (&sum)[TI][TJ], float times = 1.0f) {
 #pragma unroll
     for (int x = 0; x < TI; ++x)
 #pragma unroll
         for (int y = 0; y < TJ; ++y)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) to[x][y][v] += sum[x][y][v];
+            for (int v = 0; v < 16; ++v) to[x][y][v] = fmaf(sum[x][y][v], times, to[x][y][v]);
 }
 
 // What a phase makes of four sums, rows row_i .. row_i + 3 of column row_c, or the same columns of that row: A is symmetric.
@@ -440,8 +455,10 @@ template <int P, Phase phase, typename OUT, int T> __global__ void __launch_boun
     const Eight *left = reinterpret_cast<const Eight *>(o.left) + int64_t(ti) * T * 64 + lane;
     const Eight *right = reinterpret_cast<const Eight *>(o.right) + int64_t(tj) * T * 64 + lane;
     const int64_t left_plane = int64_t(o.rows) * o.depth / 8, right_plane = int64_t(o.cols) * o.depth / 8;
-    float16v acc[T][T];
+    constexpr int LOW = P == 2 ? T : 1;
+    float16v acc[T][T], low[LOW][LOW];
     clear<T, T>(acc);
+    clear<LOW, LOW>(low);
     Eight a[SETS][T][P], b[SETS][T][P];
     auto load = [&](int set, int k) {  // behind the last step: that one again
         const int64_t at = k < ks ? k : ks - 1;
@@ -462,11 +479,12 @@ template <int P, Phase phase, typename OUT, int T> __global__ void __launch_boun
         for (int u = 0; u < SETS; ++u) {
             if (k + 4 * u >= ks) break;
 #pragma unroll
-            for (int x = 0; x < T; ++x) add_products<P, T>(sum[x], a[u][x], b[u]);
+            for (int x = 0; x < T; ++x) add_products<P, T>(sum[x], low[P == 2 ? x : 0], a[u][x], b[u]);
             load(u, k + 4 * (u + SETS));
         }
         add<T, T>(acc, sum);
     }
+    if constexpr (P == 2) add<T, T>(acc, low, 1.0f / Parts<P>::kRest);
     const int l32 = lane & 31, lk = lane >> 5;
     if constexpr (T == 1) {
         // a wavefront adds up and writes eight rows, and eight columns for the other place
@@ -511,9 +529,9 @@ template <int P, Phase phase, typename OUT, int T> __global__ void __launch_boun
     }
 }
 
-// Tiles of 64 TI x 64 TJ through LDS (64 x 128; 128 x 128 2150 us for 2560 x 4000 instead of 1890): four wavefronts of TI x TJ fragments each, 16 KS k at a time, the next ones in the other half of the LDS and two more
-// such steps on their way in registers.
-template <int P, int TI, int TJ, int KS, Phase phase, typename T> __global__ void __launch_bounds__(kThreads, 3) product_kernel(const Job j, int step) {
+// Tiles of 64 TI x 64 TJ through LDS (64 x 128; 128 x 128 2150 us for 2560 x 4000 where these took 1890): four wavefronts of TI x TJ fragments each, 16 KS k at a time, the next ones in the other half of the LDS and two more
+// such steps on their way in registers (P = 2: 182, so two workgroups a unit; sums of second numbers that are scaled in place leave room for three and take as long).
+template <int P, int TI, int TJ, int KS, Phase phase, typename T> __global__ void __launch_bounds__(kThreads, P == 2 ? 2 : 3) product_kernel(const Job j, int step) {
     typedef typename Parts<P>::Eight Eight;
     constexpr int ROWS = 2 * (TI + TJ), FRAGS = ROWS * P * KS, MINE = (FRAGS + 3) / 4;  // 32 rows of an operand; fragments of a step, of a wavefront
     static_assert(TJ % TI == 0, "tiles of symmetric results");
@@ -556,10 +574,12 @@ template <int P, int TI, int TJ, int KS, Phase phase, typename T> __global__ voi
         for (int f = 0; f < MINE; ++f) lds.frag[half][wave * MINE + f < FRAGS ? wave * MINE + f : FRAGS - 1][lane] = next[half][f];
     };
     const int wi = wave >> 1, wj = wave & 1;
-    float16v acc[TI][TJ];
+    constexpr int LOW_I = P == 2 ? TI : 1, LOW_J = P == 2 ? TJ : 1;
+    float16v acc[TI][TJ], low[LOW_I][LOW_J];
     clear<TI, TJ>(acc);
+    clear<LOW_I, LOW_J>(low);
     auto multiply = [&](int half) {
-        __builtin_amdgcn_s_setprio(1);  // ahead of the other workgroup's wavefronts, which are then free to fetch: 2560 x 4000 1990 -> 1880 us
+        __builtin_amdgcn_s_setprio(1);  // ahead of the other workgroup's wavefronts, which are then free to fetch: 2560 x 4000 1990 -> 1880 us when there were three
         float16v sum[TI][TJ];
         clear<TI, TJ>(sum);
 #pragma unroll
@@ -574,7 +594,7 @@ template <int P, int TI, int TJ, int KS, Phase phase, typename T> __global__ voi
 #pragma unroll
                 for (int p = 0; p < P; ++p) b[y][p] = __builtin_bit_cast(Eight, lds.frag[half][(kk * ROWS + 2 * TI + wj * TJ + y) * P + p][lane]);
 #pragma unroll
-            for (int x = 0; x < TI; ++x) add_products<P, TJ>(sum[x], a[x], b);
+            for (int x = 0; x < TI; ++x) add_products<P, TJ>(sum[x], low[P == 2 ? x : 0], a[x], b);
         }
         add<TI, TJ>(acc, sum);
         __builtin_amdgcn_s_setprio(0);
@@ -598,6 +618,7 @@ template <int P, int TI, int TJ, int KS, Phase phase, typename T> __global__ voi
         __syncthreads();
     }
     __syncthreads();
+    if constexpr (P == 2) add<TI, TJ>(acc, low, 1.0f / Parts<P>::kRest);
 
     const int l32 = lane & 31, lk = lane >> 5;
 #pragma unroll 1

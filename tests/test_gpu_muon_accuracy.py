@@ -39,3 +39,31 @@ def test_matrices_near_the_least_numbers(rows, cols, steps):
         # matrix' norm, 1, is the start; their own roundings as for any matrix: four times 485 2^-24 of the norm
         assert float(want.norm()) > 1.0
         assert float((o.double() - want).norm()) <= 485 * ((steps + 1) * 2.0 ** -22 + 4 * 2.0 ** -24 * float(want.norm()))
+
+
+SCALES = [1e-3, 1e-5, 1e-6, 1e-7]
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("what", ["rows", "columns"])
+@pytest.mark.parametrize("rows,cols", [(100, 256), (256, 100), (256, 256), (602, 1000), (1100, 1000), (2000, 2100)])
+def test_rows_and_columns_far_smaller_than_the_rest(rows, cols, what, scale):
+    """Each of them by itself, relative to what it was: a row of X goes through products that are as small as it, and fp32 keeps its 24 bits in them."""
+    u = normal(rows, cols, 3)
+    small = slice(-10, None)
+    if what == "rows":
+        u[small] *= scale
+    else:
+        u[:, small] *= scale
+    o = orthogonalize([u.to(DEV)])[0].cpu().double()
+    want = newton_schulz(u)
+    far, start = o - want, u.double() / u.double().norm()
+    if what == "columns":
+        far, start = far.t(), start.t()
+    # A row grows by at most 3.4445 a step, 485 in five, and so does what a step leaves it off by, relative to it: its operands (2^-23), the two products that its
+    # entries of the polynomial come from (2^-23 each) and the sums (some 2^-24).  Four halves of 2^-21 a step, for five steps; and 2^-49 of the matrix for each of a row's
+    # elements and each of its entries of the polynomial, which the least steps of 16 bits leave.
+    relative, least = 20 * 2.0 ** -23, 2.0 ** -49 * (max(rows, cols) ** 0.5 + min(rows, cols) ** 0.5)
+    assert (far[small].norm(dim=1) <= 485 * (relative * start[small].norm(dim=1) + least)).all()
+
+
