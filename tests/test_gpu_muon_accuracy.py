@@ -1,11 +1,14 @@
-"""Newton-Schulz products of matrices that are far smaller than eps or have rows or columns far smaller than the rest, against the formulas in 64 bits."""
+"""Newton-Schulz products of matrices that are far smaller than eps or have rows or columns far smaller than the rest, against the formulas in 64 bits; of bf16
+matrices, against those of the same numbers in fp32."""
 import pytest
 import torch
 
+import paper_2104_06700_amd as gnn
 from test_gpu_muon import newton_schulz, orthogonalize
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
+BF16 = torch.bfloat16
 
 
 def normal(rows, cols, seed):
@@ -67,3 +70,21 @@ def test_rows_and_columns_far_smaller_than_the_rest(rows, cols, what, scale):
     assert (far[small].norm(dim=1) <= 485 * (relative * start[small].norm(dim=1) + least)).all()
 
 
+@pytest.mark.parametrize("rows,cols", [(47, 256), (256, 256), (300, 100), (1000, 130), (1100, 1300), (2049, 2100)])
+def test_bf16_matrices_are_computed_as_in_fp32(rows, cols):
+    """A bf16 matrix gives what the same numbers in fp32 give, rounded once."""
+    u = normal(rows, cols, 4).to(BF16).to(DEV)
+    assert torch.equal(orthogonalize([u])[0], orthogonalize([u.float()])[0].to(BF16))
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("rows,cols", [(100, 256), (1100, 1300), (2049, 2100)])
+def test_a_bf16_step_is_computed_as_in_fp32(rows, cols, nesterov):
+    p, g, m = normal(rows, cols, 5), normal(rows, cols, 6).to(BF16) * 1e-3, normal(rows, cols, 7) * 1e-3
+    full, half, master = p.to(DEV), p.to(BF16).to(DEV), p.to(DEV)
+    g, moments = g.to(DEV), [m.to(DEV), m.to(DEV)]
+    for args in (([full], [g.float()], moments[:1]), ([half], [g], moments[1:], [master])):
+        t = gnn.MuonTensors(*args, weight_decay=0.1)
+        ws = torch.empty(gnn.gnn_muon_workspace_bytes(t), device=DEV, dtype=torch.uint8)
+        gnn.gnn_muon_step(t, 0.02, nesterov=nesterov, workspace=ws)
+    assert torch.equal(moments[0], moments[1]) and torch.equal(master, full) and torch.equal(half, full.to(BF16))
