@@ -420,7 +420,8 @@ template <typename TY, typename TT, int E, bool PAST> __global__ void __launch_b
         const int64_t end = j0 + a.run < a.n ? j0 + a.run : a.n;
 #pragma unroll 1
         for (int64_t j = j0; j < end; j += kBatch) {
-            // no branch between the loads: behind the end row 0 is read, and ids that name no row are read as well (both arrays end with a whole batch)
+            if (id == none) break;  // the list ends with the positions whose id names no row
+            // no branch between the loads: behind the end and for ids that name no row row 0 is read (both arrays end with a whole batch)
             uint32_t k[kBatch], from[kBatch];
             Vector<TY, E, PAST> v[kBatch];
 #pragma unroll
@@ -433,7 +434,7 @@ template <typename TY, typename TT, int E, bool PAST> __global__ void __launch_b
                 }
             }
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) from[u] = j + u < end ? from[u] : 0;
+            for (int u = 0; u < kBatch; ++u) from[u] = j + u < end && k[u] != none ? from[u] : 0;
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) v[u].load(dy + int64_t(from[u]) * a.ldy);
 #pragma unroll
