@@ -521,8 +521,8 @@ GNN_API int gnn_lookup_fwd(const void *table, const void *ids, void *Y, int64_t 
 /* The gradient of sum dY Y with respect to the table:
  *     dtable[v, :] = scale * (sum of dY[i, :] over the i with ids[i] = v)   (+ dtable[v, :] with accumulate)
  * Rows that no id names become 0, and with accumulate are left as they are, unread.  The ids are sorted, so that each row is summed by one owner
- * in a fixed order: results are reproducible run to run.  At most 64 terms are added one after the other in fp32, and what these leave is
- * joined in fp64; a bf16 dtable is rounded once, with accumulate once a call.  dY and dtable do not overlap.  n == 0 sets dtable to 0 without
+ * in a fixed order: results are reproducible run to run.  At most 32 terms are added one after the other in fp32, and what these leave is
+ * joined in fp64 (2,048 positions and less: all in fp64, where ids come at most eight times on average); a bf16 dtable is rounded once, with accumulate once a call.  dY and dtable do not overlap.  n == 0 sets dtable to 0 without
  * accumulate. */
 GNN_API int gnn_lookup_bwd(const void *ids, const void *dY, void *dtable, int64_t V, int64_t n, int64_t F, const gnn_lookup_opts *opts);
 /* Does not fall as V, n or F grow: scratch for the largest call is enough for every smaller one.  (A call of at most 2,048 positions demands it too.) */
