@@ -655,7 +655,7 @@ struct Entry {
 };
 
 // How the products of a matrix are tiled: 0 tiles of 32 x 32, k shared out; 1 of 64 x 64, the same; 2 of 64 x 128 through LDS.  Us in fp32 and bf16 alike:
-// 800 x 800 151, 186 and 365, 1000 x 1000 209, 204 and 399, 1500 x 1800 588, 546 and 617, 2048 x 2048 1216, 957 and 864.
+// 800 x 800 157, 194 and 364, 1000 x 1000 203, 208 and 398, 1500 x 1800 604, 531 and 616, 2048 x 2048 1192, 923 and 838.
 int kind_of(int64_t rows, int64_t cols) {
     const double m = double(rows < cols ? rows : cols), n = double(rows < cols ? cols : rows), work = m * m * n;
     return work <= 1.0e9 ? 0 : work <= 6.0e9 ? 1 : 2;
