@@ -16,8 +16,8 @@
 // with X, A and Q multiplied by powers of two that take the largest number they can reach near the largest of fp16.  The second number is held 2^11 times as large as
 // it is, so that it loses bits only where the first one does: steps end at 2^-49 of the largest number, and rows or columns down to some 10^-7 of the others are as
 // close as in fp32 (100 x 256, ten rows 10^-5 of the others, by themselves: 2 10^-7; with second numbers as they are, which end at 2^-38, 9 10^-6, and 10^-3 at 10^-7).  So
-// products with a second number have sums of their own: 2560 x 4000 fp32 1972 us instead of 1888.  Two numbers do where the coefficients keep the
-// singular values small, as the usual ones do (at most 1.2); else P = 3: bf16 numbers, which have the range and all 24 bits of fp32, at twice the products (2990 us).
+// products with a second number have sums of their own: 2560 x 4000 fp32 1944 us instead of 1890.  Two numbers do where the coefficients keep the
+// singular values small, as the usual ones do (at most 1.2); else P = 3: bf16 numbers, which have the range and all 24 bits of fp32, at twice the products (2900 us).
 // Of the products of parts those that matter are formed (P = 2: three of four, the last is at most 2^-22 of the first, 2^-25 on average; P = 3: six of nine, 2^-23 and 2^-26),
 // summed from zero over 32 k (P = 3 through LDS: 16), smallest first, and added to the result with one rounding: the matrix cores cut off what lies below a sum's
 // last bit, so that long chains through them would be the worse sums (not of second numbers, which are 2^-11 of the others).  Over 64 k: as fast; over 16, where
